@@ -333,6 +333,84 @@ typedef struct {
 sagips_status sagips_adam_step(sagips_ctx* ctx, const sagips_param_set* set, int32_t step, double lr,
                                double beta1, double beta2, double eps);
 
+/* 9. Advantages within each row's events (rewards normalised in their group):
+ * over the valid events of row i,
+ *   adv = (reward - mean_i) / (std_i + eps),  std_i the population deviation;
+ * with normalise == 0 only reward - mean_i.  Events outside the mask get 0 and
+ * their rewards are not looked at; a row with none is all 0.  A row of equal
+ * rewards gives exactly 0.
+ *   reward  [n_rows][events_per_row] fp32
+ *   mask    [n_rows][events_per_row] bytes, nonzero = valid, any alignment; NULL: all valid
+ *   adv     as reward; may be reward itself, otherwise must not overlap it
+ * 1 <= n_rows, events_per_row; n_rows * events_per_row < 2^31; eps >= 0.     */
+sagips_status sagips_group_advantage(sagips_ctx* ctx, const float* reward, const uint8_t* mask, int32_t n_rows,
+                                     int64_t events_per_row, int normalise, double eps, float* adv);
+
+/* 10. Clipped policy loss with a KL term and its gradient, for pipelines that
+ * only score events.  The policy is the sampler: l(x) is the log density of
+ * event x at a parameter row (Kumaraswamy, summed over coordinates).  For the
+ * events x drawn at theta_old, with advantages A,
+ *   rho = exp(l_theta - l_theta_old),
+ *   L = mean(-min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_coef K),
+ *   K = exp(r) - 1 - r,  r = l_theta_ref - l_theta   (without theta_ref: 0).
+ * Means run over the valid events: MEAN_EVENTS over all of them alike,
+ * MEAN_ROWS over each row's and then over the rows that have any.  Without
+ * any valid event every output is 0.  Events outside the mask are not looked
+ * at.  Events are read clamped to [2^-126, 1 - 2^-24].
+ *   theta, theta_old, theta_ref  [n_theta][2d] fp32, 4-byte aligned, positive;
+ *             theta_ref may be NULL; 1 <= n_theta <= 65535, d in {2, 3}
+ *   x         [n_theta * events_per_theta][d] fp32; n_theta * E < 2^31
+ *   adv       [n_theta * events_per_theta] fp32
+ *   mask      [n_theta * events_per_theta] bytes as in 9., or NULL
+ *   loss, kl, clip_frac [1]  L, the mean of K, the mean share of events whose
+ *             clipped term is the smaller; each may be NULL
+ *   dtheta    [n_theta][2d] dL/dtheta, or NULL
+ * 0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.                           */
+typedef enum { SAGIPS_MEAN_EVENTS = 0, SAGIPS_MEAN_ROWS = 1 } sagips_mean;
+typedef struct {
+  const float* theta;
+  const float* theta_old;
+  const float* theta_ref;
+  int32_t n_theta;
+  int32_t d;
+  int64_t events_per_theta;
+  double clip_low, clip_high, kl_coef;
+  int32_t average;  /* sagips_mean */
+} sagips_policy;
+
+sagips_status sagips_policy_loss(sagips_ctx* ctx, const sagips_policy* P, const float* x, const float* adv,
+                                 const uint8_t* mask, float* loss, float* kl, float* clip_frac, float* dtheta);
+
+/* 11. Preference loss over pairs of event sets and its gradient.  With
+ *   R(set) = sum over the set's events of l_theta - l_theta_ref  (0 if empty),
+ *   h = beta (R(chosen) - R(rejected)),
+ *   L = mean over all pairs of (1 - s) softplus(-h) + s softplus(h),
+ * s = label_smoothing; l as in 10., with the same clamp.
+ *   theta, theta_ref  [n_theta][2d] fp32 as in 10.; pairs i * pairs_per_theta
+ *             .. + pairs_per_theta - 1 belong to row i
+ *   chosen    [n_theta * pairs_per_theta][len_chosen][d] fp32, rejected alike
+ *             with len_rejected events a set
+ *   n_chosen, n_rejected  [n_theta * pairs_per_theta] int32 events of each set
+ *             that count (the first ones; values outside [0, len] are taken as
+ *             the nearer end), or NULL: all; 4-byte aligned
+ *   loss [1], margin [n_theta * pairs_per_theta] (h), dtheta [n_theta][2d];
+ *             each may be NULL, not all
+ * n_theta * pairs_per_theta * len < 2^31 for either set; beta > 0,
+ * 0 <= label_smoothing <= 1.                                                 */
+typedef struct {
+  const float* theta;
+  const float* theta_ref;
+  int32_t n_theta;
+  int32_t d;
+  int64_t pairs_per_theta;
+  int64_t len_chosen, len_rejected;
+  double beta, label_smoothing;
+} sagips_preference;
+
+sagips_status sagips_preference_loss(sagips_ctx* ctx, const sagips_preference* P, const float* chosen,
+                                     const int32_t* n_chosen, const float* rejected, const int32_t* n_rejected,
+                                     float* loss, float* margin, float* dtheta);
+
 #ifdef __cplusplus
 }
 #endif

@@ -48,6 +48,10 @@ Parity status per function (what pins it, see tests/test_oracle_*.py):
                      shift, the with-replacement statistics (unique
                      fraction 1 - (1 - 1/n)^m, per-row counts binomial),
                      step and seed independence.
+  learn              pinned: the density against the sampler's CDF and its
+                     integral, its gradient and the policy and preference
+                     losses' by finite differences, closed values at equal
+                     rows, brute-force means over masks.
 """
 from .philox import philox4x32_10, event_words  # noqa: F401
 from .sampler import (uniform_from_words, kumaraswamy_icdf, kumaraswamy_cdf,  # noqa: F401
@@ -59,3 +63,4 @@ from .bootstrap import bootstrap, bootstrap_indices, bootstrap_row_order, STREAM
 from .optim import adam_step  # noqa: F401
 from .gan import gan_step, initial_state  # noqa: F401
 from .generator import G_WIDTHS, generator_forward, generator_backward, ensemble_response, residual  # noqa: F401
+from .learn import event_logp, group_advantage, policy_loss, preference_loss  # noqa: F401

@@ -24,12 +24,14 @@ OK, E_INVAL, E_ARCH, E_NOMEM, E_HIP, E_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 F32, BF16 = 0, 1
 FEAT_IDENTITY, FEAT_HD8, FEAT_PROXY2 = 0, 1, 2
 CRITIC_BUFFER, CRITIC_QUADRATIC = 0, 1
+MEAN_EVENTS, MEAN_ROWS = 0, 1
 
 EXPORTED = ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_bf16_chunk_rows",
             "sagips_last_error", "sagips_set_timing",
             "sagips_kernel_times", "sagips_sample_events", "sagips_disc_fwd_bwd", "sagips_param_grad",
             "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
-            "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_noalloc_scratch_bytes")
+            "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_noalloc_scratch_bytes",
+            "sagips_group_advantage", "sagips_policy_loss", "sagips_preference_loss")
 
 
 class SagipsError(RuntimeError):
@@ -60,6 +62,19 @@ class ParamSet(ctypes.Structure):
     _fields_ = [("n_tensors", ctypes.c_int32), ("param", ctypes.c_void_p * MAX_TENSORS),
                 ("grad", ctypes.c_void_p * MAX_TENSORS), ("m", ctypes.c_void_p * MAX_TENSORS),
                 ("v", ctypes.c_void_p * MAX_TENSORS), ("size", ctypes.c_int64 * MAX_TENSORS)]
+
+
+class Policy(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_void_p), ("theta_old", ctypes.c_void_p), ("theta_ref", ctypes.c_void_p),
+                ("n_theta", ctypes.c_int32), ("d", ctypes.c_int32), ("events_per_theta", ctypes.c_int64),
+                ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_coef", ctypes.c_double),
+                ("average", ctypes.c_int32)]
+
+
+class Preference(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_void_p), ("theta_ref", ctypes.c_void_p), ("n_theta", ctypes.c_int32),
+                ("d", ctypes.c_int32), ("pairs_per_theta", ctypes.c_int64), ("len_chosen", ctypes.c_int64),
+                ("len_rejected", ctypes.c_int64), ("beta", ctypes.c_double), ("label_smoothing", ctypes.c_double)]
 
 
 class DiscOut(ctypes.Structure):
@@ -105,11 +120,15 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.sagips_ensemble_response.argtypes = [vp, ctypes.POINTER(GenStack), vp, i64, vp, vp, vp, vp]
     lib.sagips_adam_step.argtypes = [vp, ctypes.POINTER(ParamSet), i32, ctypes.c_double, ctypes.c_double,
                                      ctypes.c_double, ctypes.c_double]
+    lib.sagips_group_advantage.argtypes = [vp, vp, vp, ctypes.c_int32, i64, i32, ctypes.c_double, vp]
+    lib.sagips_policy_loss.argtypes = [vp, ctypes.POINTER(Policy), vp, vp, vp, vp, vp, vp, vp]
+    lib.sagips_preference_loss.argtypes = [vp, ctypes.POINTER(Preference), vp, vp, vp, vp, vp, vp, vp]
     for name in ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_bf16_chunk_rows",
                  "sagips_set_timing",
                  "sagips_kernel_times", "sagips_sample_events", "sagips_disc_fwd_bwd", "sagips_param_grad",
                  "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
-                 "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc"):
+                 "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_group_advantage", "sagips_policy_loss",
+                 "sagips_preference_loss"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -483,6 +502,104 @@ class Context:
         self._check(self.lib.sagips_param_grad(self.h, ctypes.byref(src), critic, _ptr(dL_dx), g.data_ptr(),
                                                _ptr(loss)))
         return (g, loss) if critic == CRITIC_QUADRATIC else g
+
+
+    # -- training without a differentiable pipeline ------------------------------------------
+    def _rows(self, t, name, like=None):
+        """A table of parameter rows [n_theta][4] or [n_theta][6]."""
+        import torch
+        _check_tensor(t, name, torch.float32, None if like is None else like.shape, self.device)
+        if t.dim() != 2 or t.shape[1] not in (4, 6):
+            raise ValueError(f"{name} must be [n_theta][4] or [n_theta][6]")
+
+    def _mask(self, mask, shape):
+        import torch
+        if mask is None:
+            return None
+        _check_tensor(mask, "mask", None, shape, self.device)
+        if mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError(f"mask must be torch.bool or torch.uint8, got {mask.dtype}")
+        return mask.data_ptr()
+
+    def group_advantage(self, reward, mask=None, normalise: bool = True, eps: float = 1e-6, out=None):
+        """Advantages [n_rows][E]: each row's rewards less their mean, over their deviation plus eps if
+        normalise, among the events that the mask (bool or uint8, like reward) leaves; 0 elsewhere."""
+        import torch
+        self._enter()
+        _check_tensor(reward, "reward", torch.float32, None, self.device)
+        if reward.dim() != 2:
+            raise ValueError("reward must be [n_rows][events_per_row]")
+        m = self._mask(mask, reward.shape)
+        adv = out if out is not None else torch.empty_like(reward)
+        if out is not None:
+            _check_tensor(out, "out", torch.float32, reward.shape, self.device)
+        else:
+            self._owned(adv)
+        self._check(self.lib.sagips_group_advantage(self.h, reward.data_ptr(), m, reward.shape[0], reward.shape[1],
+                                                    1 if normalise else 0, eps, adv.data_ptr()))
+        return adv
+
+    def policy_loss(self, theta, theta_old, x, adv, theta_ref=None, mask=None, clip_low: float = 0.2,
+                    clip_high: float = 0.2, kl_coef: float = 0.0, average: str = "events", want_grad: bool = True) -> dict:
+        """Clipped policy loss of events x [n_theta][E][d] drawn at theta_old with advantages adv
+        [n_theta][E], and its gradient with respect to theta; the KL term needs theta_ref.
+        average: "events" or "rows".  Returns loss, kl, clip_frac [1] and dtheta."""
+        import torch
+        self._enter()
+        f32, dev = torch.float32, self.device
+        self._rows(theta, "theta")
+        self._rows(theta_old, "theta_old", theta)
+        if theta_ref is not None:
+            self._rows(theta_ref, "theta_ref", theta)
+        n, d = theta.shape[0], theta.shape[1] // 2
+        _check_tensor(adv, "adv", f32, None, dev)
+        if adv.dim() != 2 or adv.shape[0] != n:
+            raise ValueError(f"adv must be [{n}][events_per_theta]")
+        E = adv.shape[1]
+        _check_tensor(x, "x", f32, (n, E, d), dev)
+        m = self._mask(mask, adv.shape)
+        if average not in ("events", "rows"):
+            raise ValueError("average must be 'events' or 'rows'")
+        P = Policy(theta.data_ptr(), theta_old.data_ptr(), _ptr(theta_ref), n, d, E, clip_low, clip_high, kl_coef,
+                   MEAN_ROWS if average == "rows" else MEAN_EVENTS)
+        scalars = torch.empty(3, dtype=f32, device=theta.device)
+        dtheta = torch.empty_like(theta) if want_grad else None
+        self._owned(scalars, dtheta)
+        at = scalars.data_ptr()
+        self._check(self.lib.sagips_policy_loss(self.h, ctypes.byref(P), x.data_ptr(), adv.data_ptr(), m, at, at + 4,
+                                                at + 8, _ptr(dtheta)))
+        return {"loss": scalars[0:1], "kl": scalars[1:2], "clip_frac": scalars[2:3], "dtheta": dtheta}
+
+    def preference_loss(self, theta, theta_ref, chosen, rejected, len_chosen=None, len_rejected=None, beta: float = 0.1,
+                        label_smoothing: float = 0.0, want_grad: bool = True) -> dict:
+        """Preference loss over pairs of event sets, chosen [n_pairs][T][d] against rejected
+        [n_pairs][T'][d] with n_pairs a multiple of n_theta (row i's pairs follow each other), of which
+        the first len_* [n_pairs] int32 events count.  Returns loss [1], margin [n_pairs] and dtheta."""
+        import torch
+        self._enter()
+        f32, dev = torch.float32, self.device
+        self._rows(theta, "theta")
+        self._rows(theta_ref, "theta_ref", theta)
+        n, d = theta.shape[0], theta.shape[1] // 2
+        _check_tensor(chosen, "chosen", f32, None, dev)
+        _check_tensor(rejected, "rejected", f32, None, dev)
+        P = chosen.shape[0]
+        if chosen.dim() != 3 or rejected.dim() != 3 or rejected.shape[0] != P or chosen.shape[2] != d or rejected.shape[2] != d:
+            raise ValueError(f"chosen and rejected must be [n_pairs][events][{d}]")
+        if n == 0 or P == 0 or P % n:
+            raise ValueError("the number of pairs must be a multiple of the number of rows")
+        for t, name in ((len_chosen, "len_chosen"), (len_rejected, "len_rejected")):
+            _check_tensor(t, name, torch.int32, (P,), dev)
+        a = Preference(theta.data_ptr(), theta_ref.data_ptr(), n, d, P // n, chosen.shape[1], rejected.shape[1], beta,
+                       label_smoothing)
+        loss = torch.empty(1, dtype=f32, device=theta.device)
+        margin = torch.empty(P, dtype=f32, device=theta.device)
+        dtheta = torch.empty_like(theta) if want_grad else None
+        self._owned(loss, margin, dtheta)
+        self._check(self.lib.sagips_preference_loss(self.h, ctypes.byref(a), chosen.data_ptr(), _ptr(len_chosen),
+                                                    rejected.data_ptr(), _ptr(len_rejected), loss.data_ptr(),
+                                                    margin.data_ptr(), _ptr(dtheta)))
+        return {"loss": loss, "margin": margin, "dtheta": dtheta}
 
 
 _default: Dict[int, Context] = {}

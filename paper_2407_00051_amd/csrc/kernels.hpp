@@ -93,6 +93,18 @@ hipError_t launch_ensemble(const sagips_gen& G, const float* noise, int64_t k, c
 hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double beta1, double beta2, double eps,
                        hipStream_t st, Timer* tm);
 
+// policy.hip -----------------------------------------------------------------
+size_t advantage_workspace(int64_t n_rows, int64_t E);
+hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,
+                            float* adv, void* ws, hipStream_t st, Timer* tm);
+size_t policy_workspace(const sagips_policy& P);
+hipError_t launch_policy(const sagips_policy& P, const float* x, const float* adv, const uint8_t* mask, float* loss,
+                         float* kl, float* clip_frac, float* dtheta, void* ws, hipStream_t st, Timer* tm);
+size_t preference_workspace(const sagips_preference& P);
+hipError_t launch_preference(const sagips_preference& P, const float* chosen, const int32_t* n_chosen,
+                             const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta,
+                             void* ws, hipStream_t st, Timer* tm);
+
 // disc_bf16.hip --------------------------------------------------------------
 // Samples the fake events itself when a.fake_src is set (any E); never writes dLg_dtheta.
 bool disc_bf16_supported(const sagips_mlp& D, int d, const char** why);

@@ -1,0 +1,752 @@
+// Training the parameter rows without a differentiable pipeline: advantages
+// within a row's events, the clipped policy loss and the preference loss, each
+// with its gradient with respect to theta.  The policy is the sampler's own
+// density: an event x drawn at row (a_j, b_j) has
+//   l(x) = sum_j ln a_j + ln b_j + (a_j - 1) ln x_j + (b_j - 1) ln(1 - x_j^a_j),
+//   dl/da_j = 1/a_j + ln x_j (1 - (b_j - 1) x_j^a_j / (1 - x_j^a_j)),
+//   dl/db_j = 1/b_j + ln(1 - x_j^a_j).
+// Two rows' densities are only ever needed as a difference, and it is formed
+// term by term,
+//   l - l' = ln(a/a') + ln(b/b') + (a - a') ln x + (b - 1)(g - g') + (b - b') g',
+// g = ln(1 - x^a), g' = ln(1 - x^a'): its rounding then shrinks with the
+// distance between the rows instead of staying at that of l.
+#include "device_math.hpp"
+#include "kernels.hpp"
+
+namespace sagips {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+// Events are read clamped to the open unit interval: a draw may have rounded to
+// 0 or 1.  NaN stays NaN.
+__device__ __forceinline__ float clamp_event(float x) {
+  x = x < 0x1p-126f ? 0x1p-126f : x;
+  return x > 1.0f - 0x1p-24f ? 1.0f - 0x1p-24f : x;
+}
+
+// 1 - x^a, from l2 = log2 x < 0.  Above x^a = 3/4 by the series of expm1 (its
+// first term left out is 4e-9 of the sum), so that no step cancels.
+__device__ __forceinline__ float one_minus_power(float a, float l2, float* w_out) {
+  const float t = a * l2, w = fast_exp2(t), y = t * kLn2;
+  float p = 1.0f / 5040.0f;
+  p = fmaf(p, y, 1.0f / 720.0f);
+  p = fmaf(p, y, 1.0f / 120.0f);
+  p = fmaf(p, y, 1.0f / 24.0f);
+  p = fmaf(p, y, 1.0f / 6.0f);
+  p = fmaf(p, y, 0.5f);
+  p = fmaf(p, y, 1.0f);
+  *w_out = w;
+  return w < 0.75f ? 1.0f - w : -y * p;
+}
+
+// A row that the gradient is taken at, and one that its density is compared with.
+template <int D>
+struct Row {
+  float a[D], ra[D], rb[D], bm1[D], b[D];
+};
+template <int D>
+struct Against {
+  float a[D], da[D], db[D], c;   // c: sum log2(a/a') + log2(b/b')
+};
+
+template <int D>
+__device__ __forceinline__ Row<D> load_row(const float* __restrict__ th) {
+  Row<D> r;
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    r.a[j] = th[2 * j];
+    r.b[j] = th[2 * j + 1];
+    r.ra[j] = 1.0f / r.a[j];
+    r.rb[j] = 1.0f / r.b[j];
+    r.bm1[j] = r.b[j] - 1.0f;
+  }
+  return r;
+}
+template <int D>
+__device__ __forceinline__ Against<D> load_against(const float* __restrict__ th, const Row<D>& r) {
+  Against<D> o;
+  o.c = 0.0f;
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    const float a = th[2 * j], b = th[2 * j + 1];
+    o.a[j] = a;
+    o.da[j] = r.a[j] - a;
+    o.db[j] = r.b[j] - b;
+    // log2(a/a') = log1p((a - a') / a') / ln 2: the difference is exact for rows within a factor of two
+    o.c += (log1pf(o.da[j] / a) + log1pf(o.db[j] / b)) * kLog2e;
+  }
+  return o;
+}
+
+// What the current row needs of an event.
+template <int D>
+struct Event {
+  float l2[D], lg[D], q[D];   // log2 x, log2(1 - x^a), x^a / (1 - x^a)
+};
+template <int D>
+__device__ __forceinline__ Event<D> at_row(const float (&x)[D], const Row<D>& r) {
+  Event<D> e;
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    float w;
+    e.l2[j] = fast_log2(clamp_event(x[j]));
+    const float g = one_minus_power(r.a[j], e.l2[j], &w);
+    e.lg[j] = fast_log2(g);
+    e.q[j] = w * fast_rcp(g);
+  }
+  return e;
+}
+// log2 of the density's ratio, current row over the other.
+template <int D>
+__device__ __forceinline__ float log2_ratio(const Event<D>& e, const Row<D>& r, const Against<D>& o) {
+  float s = o.c;
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    float w;
+    const float lo = fast_log2(one_minus_power(o.a[j], e.l2[j], &w));
+    s = fmaf(o.da[j], e.l2[j], s);
+    s = fmaf(r.bm1[j], e.lg[j] - lo, s);
+    s = fmaf(o.db[j], lo, s);
+  }
+  return s;
+}
+// acc += wt * dl/d(a, b).
+template <int D>
+__device__ __forceinline__ void add_grad(const Event<D>& e, const Row<D>& r, float wt, float* acc) {
+#pragma unroll
+  for (int j = 0; j < D; ++j) {
+    const float k = fmaf(-r.bm1[j], e.q[j], 1.0f);
+    acc[2 * j] = fmaf(wt, fmaf(e.l2[j] * kLn2, k, r.ra[j]), acc[2 * j]);
+    acc[2 * j + 1] = fmaf(wt, fmaf(e.lg[j], kLn2, r.rb[j]), acc[2 * j + 1]);
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void load_event(const float* __restrict__ x, int64_t i, float (&v)[D]) {
+  const float* p = x + i * D;
+#pragma unroll
+  for (int j = 0; j < D; ++j) v[j] = p[j];
+}
+
+// e^r - 1 - r: by its series below 1/2 (next term 2e-8 of it), where the subtraction would cancel.
+__device__ __forceinline__ float exp_minus_line(float r) {
+  float p = 1.0f / 40320.0f;
+  p = fmaf(p, r, 1.0f / 5040.0f);
+  p = fmaf(p, r, 1.0f / 720.0f);
+  p = fmaf(p, r, 1.0f / 120.0f);
+  p = fmaf(p, r, 1.0f / 24.0f);
+  p = fmaf(p, r, 1.0f / 6.0f);
+  p = fmaf(p, r, 0.5f);
+  return fabsf(r) < 0.5f ? r * r * p : fast_exp(r) - 1.0f - r;
+}
+
+// Sum over groups of 2^lg neighbouring lanes, in every lane of the group.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], int lg) {
+  for (int s = 0; s < lg; ++s)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], 1 << s, 64);
+}
+
+__device__ __forceinline__ double wave_sum_d(double v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// Sum over the workgroup, in every thread.
+template <int N, int kT>
+__device__ __forceinline__ void block_sum_d(double (&v)[N]) {
+  __shared__ double part[kT / 64][N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum_d(v[i]);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) part[threadIdx.x >> 6][i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    double s = 0.0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) s += part[w][i];
+    v[i] = s;
+  }
+}
+
+// ---- advantages --------------------------------------------------------------
+// (r - mean) / (std + eps) over a row's valid events.  The mean is a 64-bit sum,
+// so that a row of equal rewards gives zeros; deviations are formed in 64 bits
+// and rounded once.
+
+constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing
+constexpr int kAdvBlock = 1024;
+
+// A row in a group of 2^lg lanes (kBlock false; up to 64 x 16 events) or in a
+// workgroup (up to 1,024 x 16): read once, held in registers, written once.
+template <bool kBlock>
+__global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(const float* reward, const uint8_t* __restrict__ mask,
+                                                                            int n_rows, int E, int lg, float eps, int normalise,
+                                                                            float* adv) {
+  const int lane = threadIdx.x & 63, step = kBlock ? blockDim.x : 1 << lg;
+  const int64_t row = kBlock ? blockIdx.x
+                             : (((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) << (6 - lg)) + (lane >> lg);
+  const int l = kBlock ? threadIdx.x : lane & (step - 1);
+  const bool on = row < n_rows;
+  const int64_t base = row * E;
+  float v[kAdvHeld];
+  uint32_t valid = 0;
+  double t[2] = {0.0, 0.0};
+#pragma unroll
+  for (int i = 0; i < kAdvHeld; ++i) {
+    const int e = l + i * step;
+    v[i] = 0.0f;
+    if (on && e < E && (!mask || mask[base + e])) {
+      v[i] = reward[base + e];
+      valid |= 1u << i;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kAdvHeld; ++i) t[0] += (double)v[i];
+  t[1] = (double)__popc(valid);
+  if constexpr (kBlock) block_sum_d<2, kAdvBlock>(t);
+  else
+    for (int s = 0; s < lg; ++s) {
+      t[0] += __shfl_xor(t[0], 1 << s, 64);
+      t[1] += __shfl_xor(t[1], 1 << s, 64);
+    }
+  const double n = t[1], mean = n > 0.0 ? t[0] / n : 0.0;
+  double q[1] = {0.0};
+#pragma unroll
+  for (int i = 0; i < kAdvHeld; ++i) {
+    v[i] = (valid >> i) & 1u ? (float)((double)v[i] - mean) : 0.0f;
+    q[0] = fma((double)v[i], (double)v[i], q[0]);
+  }
+  float inv = 1.0f;
+  if (normalise) {
+    if constexpr (kBlock) block_sum_d<1, kAdvBlock>(q);
+    else
+      for (int s = 0; s < lg; ++s) q[0] += __shfl_xor(q[0], 1 << s, 64);
+    const float sd = n > 0.0 ? (float)sqrt(q[0] / n) : 0.0f;
+    inv = 1.0f / (sd + eps);
+  }
+#pragma unroll
+  for (int i = 0; i < kAdvHeld; ++i) {
+    const int e = l + i * step;
+    if (on && e < E) adv[base + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
+  }
+}
+
+// Long rows, in slices of kAdvSlice events: each slice's count, mean and sum of
+// squared deviations, then one pass that joins a row's slices (Chan's update)
+// and writes.
+constexpr int kAdvSlice = 16384;
+__global__ __launch_bounds__(kAdvBlock) void k_adv_slices(const float* __restrict__ reward, const uint8_t* __restrict__ mask,
+                                                          int64_t E, int n_slices, double* __restrict__ part) {
+  const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices;
+  const int64_t base = row * E, e0 = s * kAdvSlice, left = E - e0;
+  float v[kAdvSlice / kAdvBlock];
+  uint32_t valid = 0;
+  double t[2] = {0.0, 0.0};
+#pragma unroll
+  for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) {
+    const int e = threadIdx.x + i * kAdvBlock;
+    v[i] = 0.0f;
+    if (e < left && (!mask || mask[base + e0 + e])) {
+      v[i] = reward[base + e0 + e];
+      valid |= 1u << i;
+      t[0] += (double)v[i];
+    }
+  }
+  t[1] = (double)__popc(valid);
+  block_sum_d<2, kAdvBlock>(t);
+  const double mean = t[1] > 0.0 ? t[0] / t[1] : 0.0;
+  double q[1] = {0.0};
+#pragma unroll
+  for (int i = 0; i < kAdvSlice / kAdvBlock; ++i)
+    if ((valid >> i) & 1u) q[0] += ((double)v[i] - mean) * ((double)v[i] - mean);
+  block_sum_d<1, kAdvBlock>(q);
+  if (threadIdx.x == 0) {
+    part[(int64_t)blockIdx.x * 3] = t[1];
+    part[(int64_t)blockIdx.x * 3 + 1] = mean;
+    part[(int64_t)blockIdx.x * 3 + 2] = q[0];
+  }
+}
+__global__ __launch_bounds__(kAdvBlock) void k_adv_apply(const float* reward, const uint8_t* __restrict__ mask, int64_t E,
+                                                         int n_slices, const double* __restrict__ part, float eps,
+                                                         int normalise, float* adv) {
+  const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices;
+  const double* p = part + row * n_slices * 3;
+  double t[2] = {0.0, 0.0};
+  for (int i = threadIdx.x; i < n_slices; i += kAdvBlock) {
+    t[0] += p[3 * i] * p[3 * i + 1];
+    t[1] += p[3 * i];
+  }
+  block_sum_d<2, kAdvBlock>(t);
+  const double mean = t[1] > 0.0 ? t[0] / t[1] : 0.0;
+  double q[1] = {0.0};
+  for (int i = threadIdx.x; i < n_slices; i += kAdvBlock) {
+    const double dm = p[3 * i + 1] - mean;
+    q[0] += p[3 * i] > 0.0 ? p[3 * i + 2] + p[3 * i] * dm * dm : 0.0;
+  }
+  float inv = 1.0f;
+  if (normalise) {
+    block_sum_d<1, kAdvBlock>(q);
+    inv = 1.0f / ((t[1] > 0.0 ? (float)sqrt(q[0] / t[1]) : 0.0f) + eps);
+  }
+  const int64_t base = row * E, e1 = min(E, (s + 1) * (int64_t)kAdvSlice);
+  for (int64_t e = s * kAdvSlice + threadIdx.x; e < e1; e += kAdvBlock)
+    adv[base + e] = !mask || mask[base + e] ? (float)((double)reward[base + e] - mean) * inv : 0.0f;
+}
+
+// ---- policy loss ---------------------------------------------------------------
+// A unit is one slice of one row, run by a group of 2^lg lanes (a wave, or less
+// where rows have fewer events).  It leaves its sums over valid events: of the
+// loss, the KL term, the clipped events and the events, and of the gradient.
+struct PolicyArgs {
+  const float *theta, *theta_old, *theta_ref, *x, *adv;
+  const uint8_t* mask;
+  int64_t E, chunk, units;
+  int S, lg;
+  float lo, hi, beta;
+  float4* tot;   // [units]
+  float* grad;   // [units][2d]
+};
+
+template <int D, bool kRef>
+__global__ __launch_bounds__(kThreads) void k_policy(PolicyArgs p) {
+  const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
+  const int64_t unit = (((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) << (6 - p.lg)) + (lane >> p.lg);
+  const bool on = unit < p.units;
+  const int64_t row = on ? unit / p.S : 0, s = on ? unit % p.S : 0;
+  const Row<D> r = load_row<D>(p.theta + row * 2 * D);
+  const Against<D> old = load_against<D>(p.theta_old + row * 2 * D, r);
+  Against<D> ref;
+  if constexpr (kRef) ref = load_against<D>(p.theta_ref + row * 2 * D, r);
+  const int64_t e1 = on ? min(p.E, (s + 1) * p.chunk) : 0;
+  float acc[2 * D + 4] = {};   // the gradient, then loss, KL, clipped, events
+  for (int64_t e = s * p.chunk + l; e < e1; e += step) {
+    const int64_t i = row * p.E + e;
+    if (p.mask && !p.mask[i]) continue;
+    float x[D];
+    load_event<D>(p.x, i, x);
+    const float A = p.adv[i];
+    const Event<D> ev = at_row<D>(x, r);
+    const float rho = fast_exp2(log2_ratio<D>(ev, r, old));
+    const bool up = A > 0.0f && rho > p.hi, down = A < 0.0f && rho < p.lo;
+    const bool cut = up || down;
+    float loss = -(cut ? (up ? p.hi : p.lo) : rho) * A;
+    float wt = cut ? 0.0f : -rho * A;
+    if constexpr (kRef) {
+      const float t = -log2_ratio<D>(ev, r, ref) * kLn2, k = exp_minus_line(t);
+      loss = fmaf(p.beta, k, loss);
+      wt = fmaf(-p.beta, t + k, wt);
+      acc[2 * D + 1] += k;
+    }
+    acc[2 * D] += loss;
+    acc[2 * D + 2] += cut ? 1.0f : 0.0f;
+    acc[2 * D + 3] += 1.0f;
+    add_grad<D>(ev, r, wt, acc);
+  }
+  group_sum(acc, p.lg);
+  if (on && l == 0) {
+    p.tot[unit] = make_float4(acc[2 * D], acc[2 * D + 1], acc[2 * D + 2], acc[2 * D + 3]);
+#pragma unroll
+    for (int j = 0; j < 2 * D; ++j) p.grad[unit * 2 * D + j] = acc[j];
+  }
+}
+
+// Joins the units' sums in 64 bits and applies the average.  Every workgroup
+// forms the totals that its rows' weights need; the first writes the scalars.
+struct PolicyFinish {
+  const float4* tot;
+  const float* grad;
+  int64_t rows, E;
+  int S, by_rows, masked;
+  float *loss, *kl, *clip, *dtheta;
+};
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
+  if (p.masked || blockIdx.x == 0) {
+    if (p.by_rows && p.S > 1) {        // a wave per row
+      for (int64_t row = wave; row < p.rows; row += kWaves) {
+        double u[4] = {};
+        for (int s = lane; s < p.S; s += 64) {
+          const float4 v = p.tot[row * p.S + s];
+          u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = wave_sum_d(u[i]);
+        if (lane == 0 && u[3] > 0.0) {
+          for (int i = 0; i < 4; ++i) t[i] += u[i] / u[3];
+          t[4] += 1.0;
+        }
+      }
+    } else {
+      for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) {
+        const float4 v = p.tot[k];
+        const double w = !p.by_rows ? 1.0 : v.w > 0.0f ? 1.0 / v.w : 0.0;
+        t[0] += w * v.x; t[1] += w * v.y; t[2] += w * v.z; t[3] += w * v.w;
+        t[4] += v.w > 0.0f ? 1.0 : 0.0;
+      }
+    }
+    block_sum_d<5, kThreads>(t);
+  }
+  const double all = p.by_rows ? (p.masked ? t[4] : (double)p.rows) : (p.masked ? t[3] : (double)p.rows * (double)p.E);
+  const double inv = all > 0.0 ? 1.0 / all : 0.0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (p.loss) *p.loss = (float)(t[0] * inv);
+    if (p.kl) *p.kl = (float)(t[1] * inv);
+    if (p.clip) *p.clip = (float)(t[2] * inv);
+  }
+  if (!p.dtheta) return;
+  if (p.S == 1) {
+    for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)gridDim.x * kThreads) {
+      double w = inv;
+      if (p.by_rows) {
+        const float n = p.masked ? p.tot[k / (2 * D)].w : (float)p.E;
+        w = n > 0.0f ? inv / n : 0.0;
+      }
+      p.dtheta[k] = (float)(p.grad[k] * w);
+    }
+    return;
+  }
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < p.rows; row += (int64_t)gridDim.x * kWaves) {
+    double u[2 * D + 1] = {};
+    for (int s = lane; s < p.S; s += 64) {
+      const int64_t k = row * p.S + s;
+      u[2 * D] += p.tot[k].w;
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) u[j] += p.grad[k * 2 * D + j];
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * D + 1; ++j) u[j] = wave_sum_d(u[j]);
+    const double w = !p.by_rows ? inv : u[2 * D] > 0.0 ? inv / u[2 * D] : 0.0;
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
+  }
+}
+
+// ---- preference loss -----------------------------------------------------------
+// A pair's sums over its two sets, chosen minus rejected: of the log2 ratios and
+// of dl/dtheta; both are linear, so one pass over the events gives the margin
+// and, once it is known, the gradient.
+struct PrefArgs {
+  const float *theta, *theta_ref;
+  const float* x[2];          // chosen, rejected
+  const int32_t* len[2];      // or NULL
+  int64_t T[2];
+  int64_t pairs, chunk, units;   // pairs a row; pairs (or, k_pref_slices, events) a unit
+  int S, lg;
+  float beta, eps;
+  double inv_pairs;           // 1 / all pairs
+  float* margin;              // or NULL
+  const float* part;          // k_pref<D, true>: [all pairs][slices][2d + 1]
+  int slices;
+  float* out;                 // [units][2d + 1] (gradient, loss), or the slices' part
+};
+
+template <int D>
+__device__ __forceinline__ void add_set(const PrefArgs& p, int which, int64_t pair, int64_t e0, int64_t e1, int l, int step,
+                                        const Row<D>& r, const Against<D>& ref, float (&v)[2 * D + 1]) {
+  int64_t n = p.T[which];
+  if (p.len[which]) {
+    const int64_t given = p.len[which][pair];
+    n = given < 0 ? 0 : given < n ? given : n;
+  }
+  n = min(n, e1);
+  const float sign = which ? -1.0f : 1.0f;
+  for (int64_t e = e0 + l; e < n; e += step) {
+    float x[D];
+    load_event<D>(p.x[which], pair * p.T[which] + e, x);
+    const Event<D> ev = at_row<D>(x, r);
+    v[2 * D] = fmaf(sign, log2_ratio<D>(ev, r, ref), v[2 * D]);
+    add_grad<D>(ev, r, sign, v);
+  }
+}
+
+// A unit: one wave, some pairs of one row, 2^lg lanes a pair.  kJoin: the pairs'
+// sums come in slices from k_pref_slices.
+template <int D, bool kJoin>
+__global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
+  const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (unit >= p.units) return;   // the whole wave
+  const int64_t row = unit / p.S, s = unit % p.S;
+  const Row<D> r = load_row<D>(p.theta + row * 2 * D);
+  const Against<D> ref = load_against<D>(p.theta_ref + row * 2 * D, r);
+  const int64_t q0 = s * p.chunk, q1 = min(p.pairs, q0 + p.chunk);
+  float acc[2 * D + 1] = {};
+  for (int64_t q = q0; q < q1; q += 64 >> p.lg) {
+    const int64_t mine = q + (lane >> p.lg), pair = row * p.pairs + mine;
+    const bool on = mine < q1;
+    float v[2 * D + 1] = {};
+    if (on) {
+      if constexpr (kJoin) {
+        for (int i = l; i < p.slices; i += step)
+#pragma unroll
+          for (int j = 0; j < 2 * D + 1; ++j) v[j] += p.part[(pair * p.slices + i) * (2 * D + 1) + j];
+      } else {
+        add_set<D>(p, 0, pair, 0, p.T[0], l, step, r, ref, v);
+        add_set<D>(p, 1, pair, 0, p.T[1], l, step, r, ref, v);
+      }
+    }
+    group_sum(v, p.lg);
+    if (on && l == 0) {
+      const float h = p.beta * (v[2 * D] * kLn2);
+      if (p.margin) p.margin[pair] = h;
+      // softplus(-h) and softplus(h) = softplus(-h) + h; the sigmoid of |h| from the same exponential
+      const float t = fast_exp(-fabsf(h)), sp = fmaxf(-h, 0.0f) + log1p_k(t);
+      const float sig = (h >= 0.0f ? 1.0f : t) * fast_rcp(1.0f + t);       // sigmoid(h)
+      const float one_m = (h >= 0.0f ? t : 1.0f) * fast_rcp(1.0f + t);     // 1 - sigmoid(h)
+      acc[2 * D] += (1.0f - p.eps) * sp + p.eps * (sp + h);
+      const float g = p.eps * sig - (1.0f - p.eps) * one_m;
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) acc[j] = fmaf(g, v[j], acc[j]);
+    }
+  }
+  group_sum(acc, 6);
+  if (lane == 0)
+#pragma unroll
+    for (int j = 0; j < 2 * D + 1; ++j) p.out[unit * (2 * D + 1) + j] = acc[j];
+}
+
+// Long sets: a unit is a wave on one slice of one pair's sets.
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (unit >= p.units) return;
+  const int64_t pair = unit / p.slices, s = unit % p.slices, row = pair / p.pairs;
+  const Row<D> r = load_row<D>(p.theta + row * 2 * D);
+  const Against<D> ref = load_against<D>(p.theta_ref + row * 2 * D, r);
+  float v[2 * D + 1] = {};
+  add_set<D>(p, 0, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref, v);
+  add_set<D>(p, 1, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref, v);
+  group_sum(v, 6);
+  if (lane == 0)
+#pragma unroll
+    for (int j = 0; j < 2 * D + 1; ++j) p.out[unit * (2 * D + 1) + j] = v[j];
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_pref_finish(const float* __restrict__ in, int64_t rows, int S, double beta,
+                                                          double inv_pairs, float* loss, float* dtheta) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x == 0 && loss) {
+    double t[1] = {0.0};
+    for (int64_t k = threadIdx.x; k < rows * S; k += kThreads) t[0] += in[k * (2 * D + 1) + 2 * D];
+    block_sum_d<1, kThreads>(t);
+    if (threadIdx.x == 0) *loss = (float)(t[0] * inv_pairs);
+  }
+  if (!dtheta) return;
+  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < rows; row += (int64_t)gridDim.x * kWaves) {
+    double u[2 * D] = {};
+    for (int s = lane; s < S; s += 64)
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) u[j] += in[(row * S + s) * (2 * D + 1) + j];
+#pragma unroll
+    for (int j = 0; j < 2 * D; ++j) u[j] = wave_sum_d(u[j]);
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) dtheta[row * 2 * D + j] = (float)(u[j] * (beta * inv_pairs));
+  }
+}
+
+// ---- plans ---------------------------------------------------------------------
+constexpr int64_t kTargetUnits = 8192;   // waves that fill the device: 256 compute units x 32
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+// Lanes (as a power of two) for n items: at most a wave.
+int lanes_log(int64_t n) {
+  int lg = 0;
+  while (lg < 6 && ((int64_t)1 << lg) < n) ++lg;
+  return lg;
+}
+
+struct PolicyPlan {
+  int lg, S;
+  int64_t chunk, units;
+  size_t grad_off, bytes;
+};
+PolicyPlan policy_plan(int64_t rows, int64_t E, int d) {
+  PolicyPlan p;
+  p.lg = lanes_log(E);
+  // slices of at least four events a lane
+  const int64_t most = ceil_div(E, 256), want = kTargetUnits / rows;
+  p.S = (int)(want < 1 ? 1 : want > most ? most : want);
+  p.chunk = ceil_div(E, p.S);
+  p.S = (int)ceil_div(E, p.chunk);
+  p.units = rows * p.S;
+  p.grad_off = align256((size_t)p.units * sizeof(float4));
+  p.bytes = p.grad_off + (size_t)p.units * 2 * d * sizeof(float);
+  return p;
+}
+
+struct PrefPlan {
+  int lg, S, slices;          // slices > 0: long sets, joined after
+  int64_t chunk, units, slice_chunk;
+  size_t part_off, bytes;
+};
+constexpr int64_t kLongSet = 4096;
+PrefPlan pref_plan(int64_t rows, int64_t pairs, int64_t T, int d) {
+  PrefPlan p;
+  p.slices = 0;
+  p.slice_chunk = T;
+  if (T > kLongSet && rows * pairs < kTargetUnits) {
+    const int64_t most = ceil_div(T, 256), want = ceil_div(kTargetUnits, rows * pairs);
+    p.slices = (int)(want > most ? most : want);
+    p.slice_chunk = ceil_div(T, p.slices);
+    p.slices = (int)ceil_div(T, p.slice_chunk);
+  }
+  p.lg = lanes_log(p.slices ? p.slices : T);
+  const int64_t most = ceil_div(pairs, 64 >> p.lg), want = kTargetUnits / rows;
+  p.S = (int)(want < 1 ? 1 : want > most ? most : want);
+  p.chunk = ceil_div(pairs, p.S);
+  p.S = (int)ceil_div(pairs, p.chunk);
+  p.units = rows * p.S;
+  p.part_off = align256((size_t)p.units * (2 * d + 1) * sizeof(float));
+  p.bytes = p.part_off + (size_t)rows * pairs * p.slices * (2 * d + 1) * sizeof(float);
+  return p;
+}
+
+unsigned wave_blocks(int64_t waves) { return (unsigned)ceil_div(waves, kWaves); }
+
+template <int D>
+hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x, const float* adv, const uint8_t* mask,
+                    float* loss, float* kl, float* clip, float* dtheta, char* ws, hipStream_t st, Timer* tm) {
+  PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg,
+               (float)(1.0 - P.clip_low), (float)(1.0 + P.clip_high), (float)P.kl_coef,
+               reinterpret_cast<float4*>(ws), reinterpret_cast<float*>(ws + pl.grad_off)};
+  const dim3 grid(wave_blocks(ceil_div(pl.units, 64 >> pl.lg)));
+  if (tm) tm->begin("policy");
+  if (P.theta_ref) hipLaunchKernelGGL((k_policy<D, true>), grid, dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_policy<D, false>), grid, dim3(kThreads), 0, st, a);
+  if (tm) tm->end();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  PolicyFinish f{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.S, P.average == SAGIPS_MEAN_ROWS, mask != nullptr,
+                 loss, kl, clip, dtheta};
+  const int64_t blocks = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
+  if (tm) tm->begin("policy_finish");
+  hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, f);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* chosen, const int32_t* n_chosen,
+                  const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta, char* ws,
+                  hipStream_t st, Timer* tm) {
+  const int64_t all = (int64_t)P.n_theta * P.pairs_per_theta;
+  PrefArgs a{};
+  a.theta = P.theta;
+  a.theta_ref = P.theta_ref;
+  a.x[0] = chosen;
+  a.x[1] = rejected;
+  a.len[0] = n_chosen;
+  a.len[1] = n_rejected;
+  a.T[0] = P.len_chosen;
+  a.T[1] = P.len_rejected;
+  a.pairs = P.pairs_per_theta;
+  a.beta = (float)P.beta;
+  a.eps = (float)P.label_smoothing;
+  a.inv_pairs = 1.0 / (double)all;
+  a.margin = margin;
+  a.slices = pl.slices;
+  float* sums = reinterpret_cast<float*>(ws);
+  float* part = reinterpret_cast<float*>(ws + pl.part_off);
+  if (pl.slices) {
+    a.chunk = pl.slice_chunk;
+    a.units = all * pl.slices;
+    a.out = part;
+    if (tm) tm->begin("preference_slices");
+    hipLaunchKernelGGL((k_pref_slices<D>), dim3(wave_blocks(a.units)), dim3(kThreads), 0, st, a);
+    if (tm) tm->end();
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  a.chunk = pl.chunk;
+  a.units = pl.units;
+  a.S = pl.S;
+  a.lg = pl.lg;
+  a.part = part;
+  a.out = sums;
+  if (tm) tm->begin("preference");
+  if (pl.slices) hipLaunchKernelGGL((k_pref<D, true>), dim3(wave_blocks(pl.units)), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_pref<D, false>), dim3(wave_blocks(pl.units)), dim3(kThreads), 0, st, a);
+  if (tm) tm->end();
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || (!loss && !dtheta)) return e;
+  const int64_t blocks = ceil_div(P.n_theta, kWaves);
+  if (tm) tm->begin("preference_finish");
+  hipLaunchKernelGGL((k_pref_finish<D>), dim3((unsigned)(blocks > 4096 ? 4096 : blocks)), dim3(kThreads), 0, st, sums,
+                     P.n_theta, pl.S, P.beta, a.inv_pairs, loss, dtheta);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t advantage_workspace(int64_t n_rows, int64_t E) {
+  return E <= kAdvSlice ? 0 : (size_t)n_rows * ceil_div(E, kAdvSlice) * 3 * sizeof(double);
+}
+
+hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,
+                            float* adv, void* ws, hipStream_t st, Timer* tm) {
+  if (tm) tm->begin("advantage");
+  if (E <= 64 * kAdvHeld) {
+    // the fewest lanes that hold a row, but a lane for every event up to 64
+    const int lg = lanes_log(E);
+    const int64_t waves = ceil_div(n_rows, 64 >> lg);
+    hipLaunchKernelGGL((k_advantage<false>), dim3(wave_blocks(waves)), dim3(kThreads), 0, st, reward, mask, (int)n_rows,
+                       (int)E, lg, eps, (int)normalise, adv);
+  } else if (E <= kAdvBlock * kAdvHeld) {
+    const int threads = (int)(ceil_div(E, 64 * kAdvHeld) * 64);
+    hipLaunchKernelGGL((k_advantage<true>), dim3((unsigned)n_rows), dim3(threads), 0, st, reward, mask, (int)n_rows, (int)E,
+                       6, eps, (int)normalise, adv);
+  } else {
+    const int slices = (int)ceil_div(E, kAdvSlice);
+    const dim3 grid((unsigned)(n_rows * slices));
+    double* part = static_cast<double*>(ws);
+    hipLaunchKernelGGL(k_adv_slices, grid, dim3(kAdvBlock), 0, st, reward, mask, E, slices, part);
+    if (tm) {
+      tm->end();
+      tm->begin("advantage_apply");
+    }
+    hipLaunchKernelGGL(k_adv_apply, grid, dim3(kAdvBlock), 0, st, reward, mask, E, slices, part, eps, (int)normalise, adv);
+  }
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+size_t policy_workspace(const sagips_policy& P) { return policy_plan(P.n_theta, P.events_per_theta, P.d).bytes; }
+
+hipError_t launch_policy(const sagips_policy& P, const float* x, const float* adv, const uint8_t* mask, float* loss,
+                         float* kl, float* clip_frac, float* dtheta, void* ws, hipStream_t st, Timer* tm) {
+  const PolicyPlan pl = policy_plan(P.n_theta, P.events_per_theta, P.d);
+  char* w = static_cast<char*>(ws);
+  return P.d == 2 ? policy_d<2>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, st, tm)
+                  : policy_d<3>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, st, tm);
+}
+
+static PrefPlan plan_of(const sagips_preference& P) {
+  return pref_plan(P.n_theta, P.pairs_per_theta, P.len_chosen > P.len_rejected ? P.len_chosen : P.len_rejected, P.d);
+}
+
+size_t preference_workspace(const sagips_preference& P) { return plan_of(P).bytes; }
+
+hipError_t launch_preference(const sagips_preference& P, const float* chosen, const int32_t* n_chosen,
+                             const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta,
+                             void* ws, hipStream_t st, Timer* tm) {
+  const PrefPlan pl = plan_of(P);
+  char* w = static_cast<char*>(ws);
+  return P.d == 2 ? pref_d<2>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, st, tm)
+                  : pref_d<3>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, st, tm);
+}
+
+}  // namespace sagips
