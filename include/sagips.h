@@ -411,6 +411,61 @@ sagips_status sagips_preference_loss(sagips_ctx* ctx, const sagips_preference* P
                                      const int32_t* n_chosen, const float* rejected, const int32_t* n_rejected,
                                      float* loss, float* margin, float* dtheta);
 
+/* 12. Orthogonalising matrices, and the optimiser step built on it (Muon:
+ * momentum, then the update replaced by its orthogonal factor, approximately).
+ * A matrix U is oriented with its shorter side as rows, X = U / (|U|_F + eps),
+ * and `steps` times
+ *   A = X X^T,  X <- a X + (b A + c A^2) X,   (a, b, c) = coef.
+ * With the default coefficients every singular value of U that is not far
+ * below the largest ends between 0.68 and 1.14; singular vectors stay.
+ * A zero matrix stays zero; an infinity or NaN makes the whole matrix NaN.
+ * Products are formed from bf16 terms with fp32 accumulation as described at
+ * sagips_mlp: three terms where the result is fp32, two (16 bits) where it is
+ * bf16.  `coef` all zero means (3.4445, -4.7750, 2.0315), `steps` 0 means 5.
+ * 0 <= steps <= 16, eps > 0.                                                */
+typedef struct {
+  int32_t steps;
+  double coef[3];
+  double eps;
+} sagips_newton_schulz;
+
+/*   x, out  [count][rows][cols] of `type` (SAGIPS_F32, or SAGIPS_BF16: bf16
+ *           values); out may be x itself, otherwise must not overlap it.
+ * count, rows, cols >= 1; rows, cols <= 16384; count <= 65535;
+ * count * rows * cols < 2^31.                                               */
+sagips_status sagips_orthogonalise(sagips_ctx* ctx, const sagips_newton_schulz* ns, int32_t type, const void* x,
+                                   int32_t count, int32_t rows, int32_t cols, void* out);
+
+/* One step on up to SAGIPS_MAX_TENSORS stacks of matrices (count[i] matrices
+ * of rows[i] x cols[i] each, sizes as above; at most 65535 matrices in all).
+ * For every matrix, with g its gradient:
+ *   m <- momentum m + g,   u = nesterov ? g + momentum m : m,
+ *   p <- (1 - lr weight_decay) p - lr s orthogonalise(u),
+ *   s = 1 (SCALE_NONE), sqrt(max(1, rows / cols)) (SCALE_SHAPE), or
+ *       0.2 sqrt(max(rows, cols)) (SCALE_RMS: the size of an Adam update).
+ * param and m (which starts at zero) are fp32, updated in place; grad is
+ * `grad_type` (SAGIPS_F32 or SAGIPS_BF16), read only.  No two arrays of a set
+ * may overlap.  lr, weight_decay >= 0, 0 <= momentum < 1.                   */
+typedef enum { SAGIPS_SCALE_NONE = 0, SAGIPS_SCALE_SHAPE = 1, SAGIPS_SCALE_RMS = 2 } sagips_muon_scale;
+typedef struct {
+  int32_t n_tensors;
+  int32_t grad_type;
+  float* param[SAGIPS_MAX_TENSORS];
+  const void* grad[SAGIPS_MAX_TENSORS];
+  float* m[SAGIPS_MAX_TENSORS];
+  int32_t count[SAGIPS_MAX_TENSORS];
+  int32_t rows[SAGIPS_MAX_TENSORS];
+  int32_t cols[SAGIPS_MAX_TENSORS];
+} sagips_matrix_set;
+typedef struct {
+  double lr, momentum, weight_decay;
+  int32_t nesterov;
+  int32_t scale;  /* sagips_muon_scale */
+  sagips_newton_schulz ns;
+} sagips_muon;
+
+sagips_status sagips_muon_step(sagips_ctx* ctx, const sagips_matrix_set* set, const sagips_muon* options);
+
 #ifdef __cplusplus
 }
 #endif

@@ -51,7 +51,8 @@ Parity status per function (what pins it, see tests/test_oracle_*.py):
   learn              pinned: the density against the sampler's CDF and its
                      integral, its gradient and the policy and preference
                      losses' by finite differences, closed values at equal
-                     rows, brute-force means over masks.
+                     rows, brute-force means over masks; the orthogonalisation
+                     against its matrix products.
 """
 from .philox import philox4x32_10, event_words  # noqa: F401
 from .sampler import (uniform_from_words, kumaraswamy_icdf, kumaraswamy_cdf,  # noqa: F401
@@ -63,4 +64,5 @@ from .bootstrap import bootstrap, bootstrap_indices, bootstrap_row_order, STREAM
 from .optim import adam_step  # noqa: F401
 from .gan import gan_step, initial_state  # noqa: F401
 from .generator import G_WIDTHS, generator_forward, generator_backward, ensemble_response, residual  # noqa: F401
-from .learn import event_logp, group_advantage, policy_loss, preference_loss  # noqa: F401
+from .learn import (event_logp, group_advantage, policy_loss, preference_loss,  # noqa: F401
+                    orthogonalise, muon_step)

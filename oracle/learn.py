@@ -10,9 +10,12 @@ KL estimate exp(r) - 1 - r, r = l_ref - l_theta; preference_loss the logistic
 loss of paired log ratios (Rafailov et al. 2023, eq. 7) with label smoothing,
 over event sets; group_advantage centres and scales rewards within a row.
 
+orthogonalise and muon_step: at the end of the file.
+
 Pins (tests/test_oracle_learn.py): the density integrates to one and is the
 derivative of the sampler's CDF, its gradient and both losses' gradients by
-finite differences, and closed values where nothing has moved.
+finite differences, closed values where nothing has moved, and the
+orthogonalisation against its matrix products.
 """
 from __future__ import annotations
 
@@ -107,3 +110,27 @@ def preference_loss(theta, theta_ref, chosen, rejected, len_chosen=None, len_rej
         ab[i] += abs(slope) * Sabs
     loss = np.mean((1.0 - label_smoothing) * _softplus(-margin) + label_smoothing * _softplus(margin))
     return dict(loss=loss, margin=margin, dtheta=dtheta, abs_dtheta=ab)
+
+
+NS_COEF = (3.4445, -4.7750, 2.0315)
+
+
+def orthogonalise(u, steps=5, coef=NS_COEF, eps=1e-7):
+    """Newton-Schulz steps on the matrices u [...][rows][cols], shorter side as rows (Jordan et al.
+    2024): stated on the singular values, which the odd polynomial a s + b s^3 + c s^5 acts on."""
+    U, s, Vt = np.linalg.svd(np.asarray(u, np.float64), full_matrices=False)
+    s = s / (np.sqrt(np.sum(s * s, axis=-1, keepdims=True)) + eps)
+    a, b, c = coef
+    for _ in range(steps):
+        s = a * s + b * s ** 3 + c * s ** 5
+    return (U * s[..., None, :]) @ Vt
+
+
+def muon_step(p, g, m, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scale="shape", steps=5, coef=NS_COEF, eps=1e-7):
+    """(p, m) after one step on matrices of any stack shape."""
+    p, g = np.asarray(p, np.float64), np.asarray(g, np.float64)
+    m = momentum * np.asarray(m, np.float64) + g
+    o = orthogonalise(g + momentum * m if nesterov else m, steps, coef, eps)
+    rows, cols = p.shape[-2:]
+    s = {"none": 1.0, "shape": max(1.0, rows / cols) ** 0.5, "rms": 0.2 * max(rows, cols) ** 0.5}[scale]
+    return (1.0 - lr * weight_decay) * p - lr * s * o, m

@@ -25,13 +25,16 @@ F32, BF16 = 0, 1
 FEAT_IDENTITY, FEAT_HD8, FEAT_PROXY2 = 0, 1, 2
 CRITIC_BUFFER, CRITIC_QUADRATIC = 0, 1
 MEAN_EVENTS, MEAN_ROWS = 0, 1
+SCALE_NONE, SCALE_SHAPE, SCALE_RMS = 0, 1, 2
+NS_COEF = (3.4445, -4.7750, 2.0315)
 
 EXPORTED = ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_bf16_chunk_rows",
             "sagips_last_error", "sagips_set_timing",
             "sagips_kernel_times", "sagips_sample_events", "sagips_disc_fwd_bwd", "sagips_param_grad",
             "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
             "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_noalloc_scratch_bytes",
-            "sagips_group_advantage", "sagips_policy_loss", "sagips_preference_loss")
+            "sagips_group_advantage", "sagips_policy_loss", "sagips_preference_loss", "sagips_orthogonalise",
+            "sagips_muon_step")
 
 
 class SagipsError(RuntimeError):
@@ -75,6 +78,22 @@ class Preference(ctypes.Structure):
     _fields_ = [("theta", ctypes.c_void_p), ("theta_ref", ctypes.c_void_p), ("n_theta", ctypes.c_int32),
                 ("d", ctypes.c_int32), ("pairs_per_theta", ctypes.c_int64), ("len_chosen", ctypes.c_int64),
                 ("len_rejected", ctypes.c_int64), ("beta", ctypes.c_double), ("label_smoothing", ctypes.c_double)]
+
+
+class NewtonSchulz(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int32), ("coef", ctypes.c_double * 3), ("eps", ctypes.c_double)]
+
+
+class MatrixSet(ctypes.Structure):
+    _fields_ = [("n_tensors", ctypes.c_int32), ("grad_type", ctypes.c_int32), ("param", ctypes.c_void_p * MAX_TENSORS),
+                ("grad", ctypes.c_void_p * MAX_TENSORS), ("m", ctypes.c_void_p * MAX_TENSORS),
+                ("count", ctypes.c_int32 * MAX_TENSORS), ("rows", ctypes.c_int32 * MAX_TENSORS),
+                ("cols", ctypes.c_int32 * MAX_TENSORS)]
+
+
+class Muon(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("momentum", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32), ("ns", NewtonSchulz)]
 
 
 class DiscOut(ctypes.Structure):
@@ -122,13 +141,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                      ctypes.c_double, ctypes.c_double]
     lib.sagips_group_advantage.argtypes = [vp, vp, vp, ctypes.c_int32, i64, i32, ctypes.c_double, vp]
     lib.sagips_policy_loss.argtypes = [vp, ctypes.POINTER(Policy), vp, vp, vp, vp, vp, vp, vp]
+    lib.sagips_orthogonalise.argtypes = [vp, ctypes.POINTER(NewtonSchulz), ctypes.c_int32, vp, ctypes.c_int32,
+                                         ctypes.c_int32, ctypes.c_int32, vp]
+    lib.sagips_muon_step.argtypes = [vp, ctypes.POINTER(MatrixSet), ctypes.POINTER(Muon)]
     lib.sagips_preference_loss.argtypes = [vp, ctypes.POINTER(Preference), vp, vp, vp, vp, vp, vp, vp]
     for name in ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_bf16_chunk_rows",
                  "sagips_set_timing",
                  "sagips_kernel_times", "sagips_sample_events", "sagips_disc_fwd_bwd", "sagips_param_grad",
                  "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
                  "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_group_advantage", "sagips_policy_loss",
-                 "sagips_preference_loss"):
+                 "sagips_preference_loss", "sagips_orthogonalise", "sagips_muon_step"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -600,6 +622,66 @@ class Context:
                                                     rejected.data_ptr(), _ptr(len_rejected), loss.data_ptr(),
                                                     margin.data_ptr(), _ptr(dtheta)))
         return {"loss": loss, "margin": margin, "dtheta": dtheta}
+
+    # -- orthogonalised updates ----------------------------------------------------------------
+    @staticmethod
+    def _stack(t):
+        """(count, rows, cols) of a matrix or a stack of matrices."""
+        if t.dim() == 2:
+            return 1, t.shape[0], t.shape[1]
+        if t.dim() == 3:
+            return tuple(t.shape)
+        raise ValueError("matrices must be [rows][cols] or [count][rows][cols]")
+
+    def orthogonalise(self, x, steps: int = 5, coef: Sequence[float] = NS_COEF, eps: float = 1e-7, out=None):
+        """Newton-Schulz steps on every matrix of x, [rows][cols] or [count][rows][cols], fp32 or bf16:
+        singular values to a band around 1, singular vectors kept.  out may be x."""
+        import torch
+        self._enter()
+        _check_tensor(x, "x", None, None, self.device)
+        if x.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"x must be torch.float32 or torch.bfloat16, got {x.dtype}")
+        count, rows, cols = self._stack(x)
+        o = out if out is not None else torch.empty_like(x)
+        if out is not None:
+            _check_tensor(out, "out", x.dtype, x.shape, self.device)
+        else:
+            self._owned(o)
+        if steps < 1:
+            raise ValueError("steps must be >= 1")
+        ns = NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps)
+        self._check(self.lib.sagips_orthogonalise(self.h, ctypes.byref(ns), F32 if x.dtype == torch.float32 else BF16,
+                                                  x.data_ptr(), count, rows, cols, o.data_ptr()))
+        return o
+
+    def muon_step(self, params: Sequence, grads: Sequence, momenta: Sequence, lr: float, momentum: float = 0.95,
+                  nesterov: bool = True, weight_decay: float = 0.0, scale: int = SCALE_SHAPE, steps: int = 5,
+                  coef: Sequence[float] = NS_COEF, eps: float = 1e-7) -> None:
+        """In-place step on up to 16 fp32 matrices or stacks of matrices: momentum (fp32, starting at
+        zero), then the parameters move along the orthogonalised momentum.  grads are fp32 or bf16."""
+        import torch
+        self._enter()
+        n = len(params)
+        if not (n == len(grads) == len(momenta)) or not 1 <= n <= MAX_TENSORS:
+            raise ValueError("params, grads and momenta must have the same length, 1..16")
+        if steps < 1:
+            raise ValueError("steps must be >= 1")
+        dtype = grads[0].dtype
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"grads must be torch.float32 or torch.bfloat16, got {dtype}")
+        ms = MatrixSet()
+        ms.n_tensors = n
+        ms.grad_type = F32 if dtype == torch.float32 else BF16
+        for i in range(n):
+            p = params[i]
+            _check_tensor(p, f"params[{i}]", torch.float32, None, self.device)
+            _check_tensor(grads[i], f"grads[{i}]", dtype, p.shape, self.device)
+            _check_tensor(momenta[i], f"momenta[{i}]", torch.float32, p.shape, self.device)
+            ms.count[i], ms.rows[i], ms.cols[i] = self._stack(p)
+            ms.param[i], ms.grad[i], ms.m[i] = p.data_ptr(), grads[i].data_ptr(), momenta[i].data_ptr()
+        o = Muon(lr, momentum, weight_decay, 1 if nesterov else 0, scale,
+                 NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps))
+        self._check(self.lib.sagips_muon_step(self.h, ctypes.byref(ms), ctypes.byref(o)))
 
 
 _default: Dict[int, Context] = {}

@@ -1,4 +1,4 @@
-// C ABI of the learning operators (declared in include/sagips.h, 9. to 11.):
+// C ABI of the learning operators (declared in include/sagips.h, 9. to 12.):
 // argument validation, workspace and dispatch to the kernel files.
 #include <hip/hip_runtime.h>
 
@@ -37,6 +37,32 @@ sagips_status check_sizes(sagips_ctx* c, int32_t n_theta, int32_t d) {
   return SAGIPS_OK;
 }
 bool finite_at_least(double v, double lo) { return v >= lo && isfinite(v); }
+
+// Sizes of a stack of matrices.
+sagips_status check_stack(sagips_ctx* c, int32_t count, int32_t rows, int32_t cols, int i) {
+  if (count < 1 || count > 65535 || rows < 1 || rows > 16384 || cols < 1 || cols > 16384 ||
+      (int64_t)rows * cols * count >= ((int64_t)1 << 31))
+    return fail(c, SAGIPS_E_INVAL,
+                "stack %d of %d matrices of %d x %d: need 1 <= count <= 65535, 1 <= rows, cols <= 16384 and fewer than "
+                "2^31 elements",
+                i, count, rows, cols);
+  return SAGIPS_OK;
+}
+
+sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJobs* js) {
+  if (ns.steps < 0 || ns.steps > 16) return fail(c, SAGIPS_E_INVAL, "steps = %d outside [0, 16]", ns.steps);
+  if (!(ns.eps > 0.0) || !isfinite(ns.eps)) return fail(c, SAGIPS_E_INVAL, "eps must be finite and > 0");
+  static const double standard[3] = {3.4445, -4.7750, 2.0315};
+  const bool given = ns.coef[0] != 0.0 || ns.coef[1] != 0.0 || ns.coef[2] != 0.0;
+  for (int k = 0; k < 3; ++k) {
+    const double v = given ? ns.coef[k] : standard[k];
+    if (!isfinite(v)) return fail(c, SAGIPS_E_INVAL, "coef[%d] is not finite", k);
+    js->coef[k] = (float)v;
+  }
+  js->steps = ns.steps ? ns.steps : 5;
+  js->eps = ns.eps;
+  return SAGIPS_OK;
+}
 
 // Host allocations (messages, the timer's records) may throw; no exception leaves the C ABI.
 template <class F>
@@ -137,6 +163,86 @@ sagips_status sagips_preference_loss(sagips_ctx* c, const sagips_preference* P, 
     hipError_t e = launch_preference(*P, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, c->ws, c->stream,
                                      timer_of(c));
     return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "preference_loss launch");
+  });
+}
+
+sagips_status sagips_orthogonalise(sagips_ctx* c, const sagips_newton_schulz* ns, int32_t type, const void* x,
+                                   int32_t count, int32_t rows, int32_t cols, void* out) {
+  return guarded([&]() -> sagips_status {
+    if (!c) return fail(nullptr, SAGIPS_E_INVAL, "ctx is NULL");
+    if (!ns || !x || !out) return fail(c, SAGIPS_E_INVAL, "ns, x or out is NULL");
+    if (type != SAGIPS_F32 && type != SAGIPS_BF16) return fail(c, SAGIPS_E_INVAL, "unknown type %d", type);
+    if (!aligned16(x) || !aligned16(out)) return fail(c, SAGIPS_E_INVAL, "x and out must be 16-byte aligned");
+    sagips_status s = check_stack(c, count, rows, cols, 0);
+    if (s != SAGIPS_OK) return s;
+    MatrixJobs js{};
+    s = fill_steps(c, *ns, &js);
+    if (s != SAGIPS_OK) return s;
+    const size_t bytes = (size_t)count * rows * cols * (type == SAGIPS_BF16 ? 2 : 4);
+    if (x != out && overlap(x, bytes, out, bytes)) return fail(c, SAGIPS_E_INVAL, "out overlaps x without being it");
+    js.n_jobs = 1;
+    js.job[0] = MatrixJob{x, nullptr, out, count, rows, cols, 1.0};
+    js.src_bf16 = js.out_bf16 = type == SAGIPS_BF16;
+    DeviceGuard g(c->device);
+    s = ensure_ws(c, muon_workspace(js));
+    if (s != SAGIPS_OK) return s;
+    hipError_t e = launch_muon(js, c->ws, c->stream, timer_of(c));
+    return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "orthogonalise launch");
+  });
+}
+
+sagips_status sagips_muon_step(sagips_ctx* c, const sagips_matrix_set* set, const sagips_muon* o) {
+  return guarded([&]() -> sagips_status {
+    if (!c) return fail(nullptr, SAGIPS_E_INVAL, "ctx is NULL");
+    if (!set || !o) return fail(c, SAGIPS_E_INVAL, "set or options is NULL");
+    if (set->n_tensors < 1 || set->n_tensors > SAGIPS_MAX_TENSORS)
+      return fail(c, SAGIPS_E_INVAL, "n_tensors = %d outside [1, %d]", set->n_tensors, SAGIPS_MAX_TENSORS);
+    if (set->grad_type != SAGIPS_F32 && set->grad_type != SAGIPS_BF16)
+      return fail(c, SAGIPS_E_INVAL, "unknown grad_type %d", set->grad_type);
+    if (!finite_at_least(o->lr, 0.0) || !finite_at_least(o->weight_decay, 0.0) || !(o->momentum >= 0.0 && o->momentum < 1.0))
+      return fail(c, SAGIPS_E_INVAL, "need lr, weight_decay >= 0 and 0 <= momentum < 1");
+    if (o->scale != SAGIPS_SCALE_NONE && o->scale != SAGIPS_SCALE_SHAPE && o->scale != SAGIPS_SCALE_RMS)
+      return fail(c, SAGIPS_E_INVAL, "unknown scale %d", o->scale);
+    MatrixJobs js{};
+    sagips_status s = fill_steps(c, o->ns, &js);
+    if (s != SAGIPS_OK) return s;
+    const size_t grad_size = set->grad_type == SAGIPS_BF16 ? 2 : 4;
+    int64_t matrices = 0;
+    for (int i = 0; i < set->n_tensors; ++i) {
+      if (!set->param[i] || !set->grad[i] || !set->m[i]) return fail(c, SAGIPS_E_INVAL, "tensor %d has a NULL array", i);
+      if (!aligned16(set->param[i]) || !aligned16(set->grad[i]) || !aligned16(set->m[i]))
+        return fail(c, SAGIPS_E_INVAL, "tensor %d has an array that is not 16-byte aligned", i);
+      s = check_stack(c, set->count[i], set->rows[i], set->cols[i], i);
+      if (s != SAGIPS_OK) return s;
+      matrices += set->count[i];
+      const int32_t rows = set->rows[i], cols = set->cols[i];
+      const double scale = o->scale == SAGIPS_SCALE_NONE ? 1.0
+                         : o->scale == SAGIPS_SCALE_RMS ? 0.2 * sqrt((double)(rows > cols ? rows : cols))
+                         : rows > cols ? sqrt((double)rows / cols) : 1.0;
+      js.job[i] = MatrixJob{set->grad[i], set->m[i], set->param[i], set->count[i], rows, cols, scale};
+      // every array that is written against every other
+      const size_t n = (size_t)set->count[i] * rows * cols;
+      for (int k = 0; k < set->n_tensors; ++k) {
+        if (set->count[k] < 1 || set->rows[k] < 1 || set->cols[k] < 1) continue;   // refused when its turn comes
+        const size_t nk = (size_t)set->count[k] * set->rows[k] * set->cols[k];
+        if (overlap(set->param[i], n * 4, set->grad[k], nk * grad_size) || overlap(set->m[i], n * 4, set->grad[k], nk * grad_size) ||
+            overlap(set->param[i], n * 4, set->m[k], nk * 4) ||
+            (k < i && (overlap(set->param[i], n * 4, set->param[k], nk * 4) || overlap(set->m[i], n * 4, set->m[k], nk * 4))))
+          return fail(c, SAGIPS_E_INVAL, "arrays of tensors %d and %d overlap", i, k);
+      }
+    }
+    if (matrices > 65535) return fail(c, SAGIPS_E_INVAL, "%lld matrices, at most 65535", (long long)matrices);
+    js.n_jobs = set->n_tensors;
+    js.src_bf16 = set->grad_type == SAGIPS_BF16;
+    js.nesterov = o->nesterov != 0;
+    js.momentum = (float)o->momentum;
+    js.decay = (float)(1.0 - o->lr * o->weight_decay);
+    js.lr = o->lr;
+    DeviceGuard g(c->device);
+    s = ensure_ws(c, muon_workspace(js));
+    if (s != SAGIPS_OK) return s;
+    hipError_t e = launch_muon(js, c->ws, c->stream, timer_of(c));
+    return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "muon_step launch");
   });
 }
 

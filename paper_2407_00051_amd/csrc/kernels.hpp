@@ -105,6 +105,25 @@ hipError_t launch_preference(const sagips_preference& P, const float* chosen, co
                              const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta,
                              void* ws, hipStream_t st, Timer* tm);
 
+// muon.hip -------------------------------------------------------------------
+struct MatrixJob {
+  const void* src;   // gradient, or the matrices to orthogonalise
+  float* m;          // momentum, or NULL
+  void* out;         // parameters, or the orthogonalised matrices
+  int count, rows, cols;
+  double scale;      // of the update
+};
+struct MatrixJobs {
+  MatrixJob job[SAGIPS_MAX_TENSORS];
+  int n_jobs;
+  bool src_bf16, out_bf16, nesterov;
+  float momentum, decay, coef[3];
+  double lr, eps;
+  int steps;
+};
+size_t muon_workspace(const MatrixJobs& js);
+hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm);
+
 // disc_bf16.hip --------------------------------------------------------------
 // Samples the fake events itself when a.fake_src is set (any E); never writes dLg_dtheta.
 bool disc_bf16_supported(const sagips_mlp& D, int d, const char** why);

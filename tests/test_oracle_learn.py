@@ -101,3 +101,28 @@ def test_group_advantage():
     c = oracle.group_advantage(r, m, normalise=False)
     np.testing.assert_allclose(c[0, m[0]], r[0, m[0]] - r[0, m[0]].mean(), rtol=1e-14)
     assert np.all(oracle.group_advantage(np.full((2, 7), 3.25)) == 0.0)
+
+
+@pytest.mark.parametrize("shape", [(1, 1), (5, 9), (9, 5), (3, 16, 16), (2, 40, 7)])
+def test_orthogonalise_against_its_products(shape):
+    rng = np.random.default_rng(10)
+    u = rng.standard_normal(shape)
+    a, b, c = oracle.learn.NS_COEF
+    x = u.reshape((-1,) + shape[-2:])
+    x = np.swapaxes(x, 1, 2) if shape[-2] > shape[-1] else x
+    x = x / (np.sqrt((x * x).sum((1, 2), keepdims=True)) + 1e-7)
+    for _ in range(5):
+        A = x @ np.swapaxes(x, 1, 2)
+        x = a * x + (b * A + c * (A @ A)) @ x
+    x = (np.swapaxes(x, 1, 2) if shape[-2] > shape[-1] else x).reshape(shape)
+    np.testing.assert_allclose(oracle.orthogonalise(u), x, atol=1e-12)
+
+
+def test_muon_step():
+    rng = np.random.default_rng(11)
+    p, g = rng.standard_normal((2, 6, 4)), rng.standard_normal((2, 6, 4))
+    p1, m1 = oracle.muon_step(p, g, np.zeros_like(p), 0.1, weight_decay=0.5)
+    np.testing.assert_array_equal(m1, g)
+    np.testing.assert_allclose(p1, 0.95 * p - 0.1 * np.sqrt(1.5) * oracle.orthogonalise(1.95 * g), rtol=1e-12, atol=1e-14)
+    s = np.linalg.svd((0.95 * p - p1) / (0.1 * np.sqrt(1.5)), compute_uv=False)
+    assert s.min() > 0.6 and s.max() < 1.21
