@@ -419,10 +419,12 @@ sagips_status sagips_preference_loss(sagips_ctx* ctx, const sagips_preference* P
  * With the default coefficients every singular value of U that is not far
  * below the largest ends between 0.68 and 1.14; singular vectors stay.
  * A zero matrix stays zero; an infinity or NaN makes the whole matrix NaN.
- * Products are formed from bf16 terms with fp32 accumulation as described at
- * sagips_mlp: three terms where the result is fp32, two (16 bits) where it is
- * bf16.  `coef` all zero means (3.4445, -4.7750, 2.0315), `steps` 0 means 5.
- * 0 <= steps <= 16, eps > 0.                                                */
+ * X, A and the polynomial are held as two fp16 terms (24 bits; X is scaled,
+ * so the range of U does not matter) and multiplied with fp32 accumulation,
+ * at or below the error of fp32 products.  `coef` all zero means
+ * (3.4445, -4.7750, 2.0315), `steps` 0 means 5.  0 <= steps <= 16, eps > 0;
+ * coefficients that let singular values grow beyond 64 from at most 1 are
+ * SAGIPS_E_UNSUPPORTED.                                                     */
 typedef struct {
   int32_t steps;
   double coef[3];

@@ -49,6 +49,26 @@ sagips_status check_stack(sagips_ctx* c, int32_t count, int32_t rows, int32_t co
   return SAGIPS_OK;
 }
 
+// max |a s + b s^3 + c s^5| over 0 <= s <= most: at the end, or where the derivative
+// a + 3 b q + 5 c q^2, q = s^2, is zero.
+double largest_value(double a, double b, double c, double most) {
+  const auto value = [&](double s) { return fabs(s * (a + s * s * (b + c * s * s))); };
+  double v = value(most), q[2];
+  int n = 0;
+  if (c != 0.0) {
+    const double disc = 9.0 * b * b - 20.0 * a * c;
+    if (disc >= 0.0) {
+      q[n++] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
+      q[n++] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
+    }
+  } else if (b != 0.0) {
+    q[n++] = -a / (3.0 * b);
+  }
+  for (int i = 0; i < n; ++i)
+    if (q[i] > 0.0 && q[i] < most * most) v = fmax(v, value(sqrt(q[i])));
+  return v;
+}
+
 sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJobs* js) {
   if (ns.steps < 0 || ns.steps > 16) return fail(c, SAGIPS_E_INVAL, "steps = %d outside [0, 16]", ns.steps);
   if (!(ns.eps > 0.0) || !isfinite(ns.eps)) return fail(c, SAGIPS_E_INVAL, "eps must be finite and > 0");
@@ -61,6 +81,19 @@ sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJo
   }
   js->steps = ns.steps ? ns.steps : 5;
   js->eps = ns.eps;
+  // The kernels hold X, X X^T and the polynomial of it in fp16 terms: no entry exceeds
+  // the largest singular value, which starts below 1 and is bounded step by step.
+  const double a = js->coef[0], b = js->coef[1], k = js->coef[2];
+  double most = 1.0;
+  for (int i = 0; i < js->steps; ++i) {
+    const double poly = fabs(b) * most * most + fabs(k) * most * most * most * most;
+    if (!(most <= 64.0) || !(poly <= 32768.0))
+      return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 64 within %d steps", a,
+                  b, k, i + 1);
+    most = largest_value(a, b, k, most);
+  }
+  if (!(most <= 64.0))
+    return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 64", a, b, k);
   return SAGIPS_OK;
 }
 

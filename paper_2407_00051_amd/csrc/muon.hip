@@ -4,11 +4,18 @@
 // side (n rows of L).  The steps drive every singular value of X towards one
 // band around 1 and keep its singular vectors.
 //
-// Products run on the bf16 matrix cores from the operands' bf16 terms with fp32
-// accumulation (split_bf16.hpp): three terms (24 bits) where the result is fp32,
-// two terms (16 bits, three products) where it is rounded to bf16 anyway.  X,
-// A = X X^T and B = b A + c A^2 are kept as their terms, which hold an fp32
-// value exactly (two terms: to 2^-17 of it), so no fp32 copy is needed.
+// Every matrix is held as two fp16 terms, x = hi + 2^-11 lo with
+//   hi = fp16(x), lo = fp16(2^11 (x - hi)),
+// each rounded to nearest even: |x - hi| <= 2^-12 |x| and the rest is at most
+// 2^-24 |x|, half a unit in the last place of fp32 (while hi is not subnormal,
+// |x| above 6e-5; below, at most 2^-36).  Products of fp16 values are exact in
+// fp32, and of the four term products lo lo is at most 2^-24 |x y|, no more than
+// the rounding of one fp32 product.  Three products on the fp16 matrix cores,
+// hi hi into one fp32 accumulator and hi lo + lo hi into another that is scaled
+// at the end, therefore replace an fp32 product at 16/3 of the rate of the fp32
+// matrix instructions.  fp16 ends at 65,504: X, X X^T and the polynomial of it
+// stay below that because the singular values do (launch_muon's caller bounds
+// them from the coefficients).
 #include "kernels.hpp"
 #include "split_bf16.hpp"
 
@@ -16,7 +23,15 @@ namespace sagips {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kT = 2;                          // terms
+constexpr float kLo = 2048.0f, kInvLo = 1.0f / 2048.0f;
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef MatrixJob Job;
 
 // The matrices of one launch: tensors of one shape.  Matrix z lies in the tensor
@@ -51,25 +66,41 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   return v;
 }
 
-// The terms of two values, kT of them.
-template <int kT>
-__device__ __forceinline__ void split2(float a, float b, uint32_t (&t)[kT]) {
-  uint32_t s[kTerms];
-  split_pair(a, b, s);
-#pragma unroll
-  for (int k = 0; k < kT; ++k) t[k] = s[k];
+// The terms of two values, packed in pairs.  The subtractions are exact.
+__device__ __forceinline__ uint32_t pk_f16(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
 }
+__device__ __forceinline__ float f16_lo(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }
+__device__ __forceinline__ float f16_hi(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[1]; }
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+#pragma clang fp contract(off)
+  hi = pk_f16(a, b);
+  lo = pk_f16((a - f16_lo(hi)) * kLo, (b - f16_hi(hi)) * kLo);
+}
+__device__ __forceinline__ f32x16 mfma16(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f16x8 lds_row(const char* p) { return *reinterpret_cast<const f16x8*>(p); }
+// A column of four values for each lane, from rows that 16 lanes address together.
+__device__ __forceinline__ f16x8 lds_col2(const char* p, const char* q) {
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+  return __builtin_bit_cast(f16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// The LDS accesses of the workgroup so far are done; global loads stay in flight.
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // ---- norm -------------------------------------------------------------------------
 // The momentum update, and each matrix's sum of squares of U in 64 bits (neither
 // large nor small gradients leave its range), in chunks of kChunk elements.
-constexpr int64_t kChunk = 8192;
+constexpr int64_t kChunk = 4096;
 __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double* __restrict__ part) {
   const int z = blockIdx.x / chunks, k = blockIdx.x % chunks;
   const int t = tensor_of(j, z);
   const int64_t size = (int64_t)j.rows * j.cols, base = (z - j.first[t]) * size;
   const int64_t e1 = min(size, (k + 1) * kChunk);
   double s = 0.0;
+#pragma unroll 4
   for (int64_t e = k * kChunk + threadIdx.x; e < e1; e += kThreads) {
     float u = load_src(j.src[t], base + e, j.src_bf16);
     if (j.m[t]) {
@@ -86,20 +117,40 @@ __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double
   if (threadIdx.x == 0) part[blockIdx.x] = w[0] + w[1] + w[2] + w[3];
 }
 
-// X's terms [term][np][lp], zero beyond n x L, in tiles of 64 x 64.
-template <int kT>
+// 1 / (||U||_F + eps) from the chunks' sums, in every thread.
+__device__ __forceinline__ float inverse_norm(const double* __restrict__ part, int chunks, double eps) {
+  __shared__ double w[kThreads / 64];
+  double s = 0.0;
+  for (int k = threadIdx.x; k < chunks; k += kThreads) s += part[k];
+  s = wave_sum_d(s);
+  if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return (float)(1.0 / (sqrt(w[0] + w[1] + w[2] + w[3]) + eps));
+}
+
+// Layout of a matrix of np x width values (both multiples of 64) in the workspace:
+// blocks of 64 rows x 32 columns, row-major, each block its hi terms and then its lo
+// terms.  A stage of a product (32 along K) is then whole blocks or half blocks,
+// contiguous, whichever way K runs; in plain rows the pieces of a stage lie a power
+// of two apart and meet in one memory channel (2,048 x 2,048: 182 us a product so,
+// against 41 us of matrix instructions).
+constexpr int kBlockRows = 64, kBlockCols = 32, kTermSize = kBlockRows * kBlockCols, kBlockSize = kT * kTermSize;
+__device__ __forceinline__ int64_t at_value(int i, int j, int width) {   // of the hi term; lo: kTermSize further
+  return ((int64_t)(i / kBlockRows) * (width / kBlockCols) + j / kBlockCols) * kBlockSize + (i % kBlockRows) * kBlockCols +
+         j % kBlockCols;
+}
+
+// X's terms, zero beyond n x L, in tiles of 64 x 64.
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
                                                        u16* __restrict__ X, int np, int lp) {
   __shared__ float tile[64][65];
   const int z = blockIdx.z, t = tensor_of(j, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
   const bool flip = j.rows > j.cols;
   const int64_t base = (int64_t)(z - j.first[t]) * j.rows * j.cols;
-  double s = 0.0;
-  for (int k = 0; k < chunks; ++k) s += part[(int64_t)z * chunks + k];
-  const float inv = (float)(1.0 / (sqrt(s) + j.eps));
+  const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
   // read along the source's rows
   const int r0 = flip ? l0 : i0, c0 = flip ? i0 : l0;
-#pragma unroll 4
+#pragma unroll 8
   for (int q = threadIdx.x; q < 4096; q += kThreads) {
     const int r = q >> 6, c = q & 63;
     float u = 0.0f;
@@ -112,18 +163,16 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
     else tile[r][c] = u * inv;
   }
   __syncthreads();
-  const int64_t plane = (int64_t)np * lp;
-  u16* x = X + (int64_t)z * kT * plane;
+  u16* x = X + (int64_t)z * kT * np * lp;
 #pragma unroll
   for (int q = threadIdx.x; q < 512; q += kThreads) {   // 8 values of a row
     const int i = q >> 3, l = (q & 7) * 8;
-    uint32_t v[4][kT];
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) split2<kT>(tile[i][l + 2 * h], tile[i][l + 2 * h + 1], v[h]);
-#pragma unroll
-    for (int s2 = 0; s2 < kT; ++s2)
-      *reinterpret_cast<uint4*>(x + s2 * plane + (int64_t)(i0 + i) * lp + l0 + l) =
-          make_uint4(v[0][s2], v[1][s2], v[2][s2], v[3][s2]);
+    for (int h = 0; h < 4; ++h) split2(tile[i][l + 2 * h], tile[i][l + 2 * h + 1], hi[h], lo[h]);
+    u16* at = x + at_value(i0 + i, l0 + l, lp);
+    *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(at + kTermSize) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
@@ -131,17 +180,17 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
 enum Mode { kGram, kPoly, kApply, kStore };
 
 struct GemmArgs {
-  const u16* P;      // [matrices][term][np][kp]: rows i of the result, K along a row
-  const u16* Q;      // kGram, kPoly: rows j of the result, K along a row; otherwise [kp][width]: K down a column
+  const u16* P;      // [matrices][np x kp]: rows i of the result, K along a row
+  const u16* Q;      // kGram, kPoly: rows j of the result, K along a row; otherwise [kp x width]: K down a column
   const u16* X;      // kApply, kStore: X, as Q; kPoly: P
-  u16* out;          // [matrices][term][np][width]
+  u16* out;          // [matrices][np x width]
   int np, kp, width; // padded sizes
-  int tiles_i, tiles_j;
+  int tiles_i, tiles_j, tiles, per_xcd;   // of all matrices together
 };
 
-// One TI x TI tile of the result, 4 waves of (TI / 2)^2.  K in steps of 32 through
+// One TI x TI tile of the result, 4 waves of (TI / 2)^2.  K in stages of 32 through
 // two LDS buffers.
-template <int kT, int TI>
+template <int TI>
 struct Tile {
   static constexpr int KB = 32;
   static constexpr int ROWB = 2 * KB;                  // bytes of an operand row along K
@@ -151,154 +200,173 @@ struct Tile {
   static constexpr int WB = TI / 64;                   // 32-blocks a wave has in each direction
 };
 
-// Products over one K step of 16: hi hi into c, the corrections, smallest first, into d.
-template <int kT, int WB>
-__device__ __forceinline__ void products(const bf16x8 (&q)[WB][kT], const bf16x8 (&p)[WB][kT], f32x16 (&c)[WB][WB],
-                                         f32x16 (&d)[WB][WB]) {
-  constexpr int n = kT == 3 ? 5 : 2;
-  constexpr int tq[5] = {kT == 3 ? 2 : 1, 0, 1, 1, 0}, tp[5] = {0, kT == 3 ? 2 : 1, 1, 0, 1};
-#pragma unroll
-  for (int x = 0; x < WB; ++x)
-#pragma unroll
-    for (int y = 0; y < WB; ++y) c[x][y] = mfma32(q[x][0], p[y][0], c[x][y]);
-#pragma unroll
-  for (int k = 0; k < n; ++k)
-#pragma unroll
-    for (int x = 0; x < WB; ++x)
-#pragma unroll
-      for (int y = 0; y < WB; ++y) d[x][y] = mfma32(q[x][tq[k]], p[y][tp[k]], d[x][y]);
+// Tile of a workgroup.  Workgroups go to the 8 XCDs in turn; each XCD gets a
+// contiguous run of tiles, and within a matrix the tiles run through groups of four
+// tile rows, so that the run's operands (4 x 8 tiles of 128: 6 MB at 2,048) are
+// shared in the XCD's L2.
+__device__ __forceinline__ bool tile_of(const GemmArgs& g, int& z, int& ti, int& tj) {
+  const int id = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);
+  if (id >= g.tiles) return false;
+  const int per = g.tiles_i * g.tiles_j;
+  z = id / per;
+  const int t = id - z * per, group = t / (4 * g.tiles_j), i0 = group * 4, rows = min(4, g.tiles_i - i0);
+  const int r = t - i0 * g.tiles_j;
+  ti = i0 + r % rows;
+  tj = r / rows;
+  return true;
 }
 
-template <int kMode, int kT, int TI>
-__global__ __launch_bounds__(kThreads) void k_ns_gemm(GemmArgs g, Jobs jobs) {
-  typedef Tile<kT, TI> T;
+template <int kMode, int TI>
+__global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
+  typedef Tile<TI> T;
   constexpr bool kDown = kMode == kApply || kMode == kStore;   // Q's K runs down its columns
+  constexpr int WB = T::WB;
   __shared__ __attribute__((aligned(16))) char lds[2][T::BUF];
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int wave = threadIdx.x >> 6, wi = wave & 1, wj = wave >> 1;
-  const int z = blockIdx.y;
-  const int ti = blockIdx.x / g.tiles_j, tj = blockIdx.x % g.tiles_j;
-  const int64_t pp = (int64_t)g.np * g.kp, qp = kDown ? (int64_t)g.kp * g.width : (int64_t)g.width * g.kp;
-  const u16* P = g.P + z * kT * pp + (int64_t)ti * TI * g.kp;
-  const u16* Q = g.Q + z * kT * qp + (kDown ? (int64_t)tj * TI : (int64_t)tj * TI * g.kp);
+  int z, ti, tj;
+  if (!tile_of(g, z, ti, tj)) return;
+  const int64_t pp = (int64_t)kT * g.np * g.kp, qp = (int64_t)kT * g.kp * g.width, op = (int64_t)kT * g.np * g.width;
 
-  // A thread's 16-byte pieces of a K step.  Along K: piece (term, row, unit u of 4),
-  // kept at unit u ^ (row / 2 % 4), so that 8 lanes (rows) of a read hit distinct
-  // banks.  Down K: piece (term, k, unit u of TI / 8); the 32-byte granule u / 2 is
-  // kept at u / 2 ^ k % 4, so that the 4 rows of a transposed read do.
+  // A thread's 16-byte pieces of a stage.  K along a row: piece (term, row, unit u of
+  // 4), kept at unit u ^ (row / 2 % 4), so that 8 lanes (rows) of a read hit distinct
+  // banks.  K down a column: piece (block of 32 columns, term, k, unit u of 4), whose
+  // half u / 2 is kept at u / 2 ^ (k / 2 % 2), so that the 4 rows of a transposed
+  // read do.
   const u16* from[T::LOADS];
-  int64_t step[T::LOADS];
   uint32_t to[T::LOADS];
 #pragma unroll
   for (int n = 0; n < T::LOADS; ++n) {
-    const int q = n * kThreads + threadIdx.x;
-    constexpr int per = T::PT / 16;                    // pieces of a term of one operand
-    const int term = q / per % kT, r = q % per;
-    if (q < kT * per || !kDown) {
-      const int row = r >> 2, u = r & 3;
-      from[n] = (q < kT * per ? P + term * pp : Q + term * qp) + (int64_t)row * g.kp + u * 8;
-      step[n] = T::KB;
-      to[n] = q / per * T::PT + row * T::ROWB + ((u ^ ((row >> 1) & 3)) << 4);
+    const bool isQ = n >= T::LOADS / 2;
+    const int m = isQ ? n - T::LOADS / 2 : n;
+    if (!isQ || !kDown) {
+      const int rb = m / 2, term = m % 2, row = rb * kBlockRows + (threadIdx.x >> 2), u = threadIdx.x & 3;
+      from[n] = (isQ ? g.Q + z * qp : g.P + z * pp) +
+                (int64_t)((isQ ? tj : ti) * (TI / kBlockRows) + rb) * (g.kp / kBlockCols) * kBlockSize + term * kTermSize +
+                threadIdx.x * 8;
+      to[n] = ((isQ ? kT : 0) + term) * T::PT + row * T::ROWB + ((u ^ ((row >> 1) & 3)) << 4);
     } else {
-      const int k = r / (TI / 8), u = r % (TI / 8);
-      from[n] = Q + term * qp + (int64_t)k * g.width + u * 8;
-      step[n] = (int64_t)T::KB * g.width;
-      to[n] = q / per * T::PT + k * (2 * TI) + ((((u >> 1) ^ (k & 3)) << 1 | (u & 1)) << 4);
+      const int term = threadIdx.x >> 7, r = threadIdx.x & 127, k = r >> 2, u = r & 3;
+      from[n] = g.Q + z * qp + (int64_t)(tj * (TI / kBlockCols) + m) * kBlockSize + term * kTermSize + r * 8;
+      to[n] = (kT + term) * T::PT + m * (T::KB * 64) + k * 64 + ((((u >> 1) ^ ((k >> 1) & 1)) << 1 | (u & 1)) << 4);
     }
   }
-  uint4 hold[T::LOADS];
-  const auto fetch = [&] {
+  u32x4 hold0[T::LOADS], hold1[T::LOADS];
+  const int stages = g.kp / T::KB;                     // even: kp is a multiple of 64
+  // past the end: the last stage again, into a buffer that is not read any more
+  const auto fetch = [&](int k, u32x4 (&h)[T::LOADS]) __attribute__((always_inline)) {
+    k = min(k, stages - 1);
+    const int64_t along = (int64_t)k * kBlockSize;
+    const int64_t down = (int64_t)(k >> 1) * (g.width / kBlockCols) * kBlockSize + (k & 1) * (T::KB * kBlockCols);
 #pragma unroll
-    for (int n = 0; n < T::LOADS; ++n) {
-      hold[n] = *reinterpret_cast<const uint4*>(from[n]);
-      from[n] += step[n];
+    for (int n = 0; n < T::LOADS; ++n)
+      h[n] = *reinterpret_cast<const u32x4*>(from[n] + (kDown && n >= T::LOADS / 2 ? down : along));
+  };
+  const auto put = [&](char* buf, const u32x4 (&h)[T::LOADS]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int n = 0; n < T::LOADS; ++n) *reinterpret_cast<u32x4*>(buf + to[n]) = h[n];
+  };
+  // A K step's operands: of 16 along K a lane half has 8.
+  struct Frag {
+    f16x8 p[WB][kT], q[WB][kT];
+  };
+  const auto read = [&](const char* buf, int ks, Frag& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int y = 0; y < WB; ++y) {
+      const int row = wi * (TI / 2) + y * 32 + lr;
+      const uint32_t at = row * T::ROWB + (((2 * ks + lh) ^ ((row >> 1) & 3)) << 4);
+#pragma unroll
+      for (int t = 0; t < kT; ++t) f.p[y][t] = lds_row(buf + t * T::PT + at);
     }
-  };
-  const auto put = [&](char* buf) {
 #pragma unroll
-    for (int n = 0; n < T::LOADS; ++n) *reinterpret_cast<uint4*>(buf + to[n]) = hold[n];
-  };
-
-  f32x16 c[T::WB][T::WB] = {}, d[T::WB][T::WB] = {};   // [block of j][block of i]
-  const int steps = g.kp / T::KB;
-  fetch();
-  put(lds[0]);
-  __syncthreads();
-  for (int k = 0; k < steps; ++k) {
-    const char* buf = lds[k & 1];
-    if (k + 1 < steps) fetch();
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 p[T::WB][kT], q[T::WB][kT];
-#pragma unroll
-      for (int y = 0; y < T::WB; ++y) {
-        const int row = wi * (TI / 2) + y * 32 + lr;
+    for (int x = 0; x < WB; ++x) {
+      if constexpr (!kDown) {
+        const int row = wj * (TI / 2) + x * 32 + lr;
         const uint32_t at = row * T::ROWB + (((2 * ks + lh) ^ ((row >> 1) & 3)) << 4);
 #pragma unroll
-        for (int t = 0; t < kT; ++t) p[y][t] = *reinterpret_cast<const bf16x8*>(buf + t * T::PT + at);
-      }
+        for (int t = 0; t < kT; ++t) f.q[x][t] = lds_row(buf + (kT + t) * T::PT + at);
+      } else {
+        // 16 lanes read 4 rows of 16 values and get a column of 4 each
+        const int i = lane & 15, half = (lane >> 4) & 1;
+        const int k0 = 16 * ks + 8 * lh + (i >> 2);    // and k0 + 4: the same k / 2 % 2
+        const uint32_t at = (wj * (TI / 64) + x) * (T::KB * 64) + k0 * 64 + ((half ^ ((k0 >> 1) & 1)) << 5) + (i & 3) * 8;
 #pragma unroll
-      for (int x = 0; x < T::WB; ++x) {
-        if constexpr (!kDown) {
-          const int row = wj * (TI / 2) + x * 32 + lr;
-          const uint32_t at = row * T::ROWB + (((2 * ks + lh) ^ ((row >> 1) & 3)) << 4);
-#pragma unroll
-          for (int t = 0; t < kT; ++t) q[x][t] = *reinterpret_cast<const bf16x8*>(buf + (kT + t) * T::PT + at);
-        } else {
-          // 16 lanes read 4 rows of 16 values and get a column of 4 each
-          const int i = lane & 15, half = (lane >> 4) & 1;
-          const int G = (wj * (TI / 2) + x * 32) / 16 + half;
-#pragma unroll
-          for (int t = 0; t < kT; ++t) {
-            bf16x4 v[2];
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const int kk = 16 * ks + 8 * lh + 4 * s + (i >> 2);
-              const uint32_t at = kk * (2 * TI) + ((G ^ (kk & 3)) << 5) + (i & 3) * 8;
-              v[s] = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(buf + (kT + t) * T::PT + at));
-            }
-            q[x][t] = bf16x8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
-          }
+        for (int t = 0; t < kT; ++t) {
+          const char* b = buf + (kT + t) * T::PT + at;
+          f.q[x][t] = lds_col2(b, b + 4 * 64);
         }
       }
-      products<kT, T::WB>(q, p, c, d);
     }
-    if (k + 1 < steps) put(lds[(k + 1) & 1]);
-    __syncthreads();
+  };
+  f32x16 c[WB][WB] = {}, d[WB][WB] = {};   // [block of j][block of i]: hi hi; hi lo + lo hi
+  const auto multiply = [&](const Frag& f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+      for (int x = 0; x < WB; ++x)
+#pragma unroll
+        for (int y = 0; y < WB; ++y) {
+          if (s == 0) d[x][y] = mfma16(f.q[x][0], f.p[y][1], d[x][y]);
+          if (s == 1) c[x][y] = mfma16(f.q[x][0], f.p[y][0], c[x][y]);
+          if (s == 2) d[x][y] = mfma16(f.q[x][1], f.p[y][0], d[x][y]);
+        }
+  };
+
+  // Stage k's second half reads the first operands of stage k + 1, whose pieces went
+  // to LDS during the first half; two more stages are on their way in registers.
+  fetch(0, hold0);
+  fetch(1, hold1);
+  put(lds[0], hold0);
+  fetch(2, hold0);
+  lds_barrier();
+  Frag f0, f1;
+  read(lds[0], 0, f0);
+  for (int k = 0; k < stages; k += 2) {
+    read(lds[0], 1, f1);
+    put(lds[1], hold1);
+    multiply(f0);
+    lds_barrier();
+    read(lds[1], 0, f0);
+    fetch(k + 3, hold1);
+    multiply(f1);
+
+    read(lds[1], 1, f1);
+    put(lds[0], hold0);
+    multiply(f0);
+    lds_barrier();
+    read(lds[0], 0, f0);
+    fetch(k + 4, hold0);
+    multiply(f1);
   }
 
   // A lane has row i, columns j .. j + 3 of each group.
-  const int64_t op = (int64_t)g.np * g.width;
   const int t = kMode == kStore ? tensor_of(jobs, z) : 0;
 #pragma unroll
-  for (int x = 0; x < T::WB; ++x)
+  for (int x = 0; x < WB; ++x)
 #pragma unroll
-    for (int y = 0; y < T::WB; ++y)
+    for (int y = 0; y < WB; ++y)
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int i = ti * TI + wi * (TI / 2) + y * 32 + lr, j = tj * TI + wj * (TI / 2) + x * 32 + 8 * s + 4 * lh;
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = c[x][y][4 * s + e] + d[x][y][4 * s + e];
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(d[x][y][4 * s + e], kInvLo, c[x][y][4 * s + e]);
         if constexpr (kMode != kGram) {
-          const u16* old = g.X + z * kT * op + (int64_t)i * g.width + j;
+          const u16* old = g.X + z * op + at_value(i, j, g.width);
           const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = kMode == kPoly ? jobs.c : 1.0f;
-          float o[4] = {};
-#pragma unroll
-          for (int w = kT - 1; w >= 0; --w) {          // smallest term first
-            const uint2 r = *reinterpret_cast<const uint2*>(old + w * op);
-            o[0] += bf16_lo(r.x); o[1] += bf16_hi(r.x); o[2] += bf16_lo(r.y); o[3] += bf16_hi(r.y);
-          }
+          const uint2 h = *reinterpret_cast<const uint2*>(old), l = *reinterpret_cast<const uint2*>(old + kTermSize);
+          const float o[4] = {fmaf(f16_lo(l.x), kInvLo, f16_lo(h.x)), fmaf(f16_hi(l.x), kInvLo, f16_hi(h.x)),
+                              fmaf(f16_lo(l.y), kInvLo, f16_lo(h.y)), fmaf(f16_hi(l.y), kInvLo, f16_hi(h.y))};
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = fmaf(keep, o[e], mul * v[e]);
         }
         if constexpr (kMode != kStore) {
-          uint32_t a[kT], b[kT];
-          split2<kT>(v[0], v[1], a);
-          split2<kT>(v[2], v[3], b);
-          u16* out = g.out + z * kT * op + (int64_t)i * g.width + j;
-#pragma unroll
-          for (int w = 0; w < kT; ++w) *reinterpret_cast<uint2*>(out + w * op) = make_uint2(a[w], b[w]);
+          uint2 h, l;
+          split2(v[0], v[1], h.x, l.x);
+          split2(v[2], v[3], h.y, l.y);
+          u16* out = g.out + z * op + at_value(i, j, g.width);
+          *reinterpret_cast<uint2*>(out) = h;
+          *reinterpret_cast<uint2*>(out + kTermSize) = l;
         } else {
           const bool flip = jobs.rows > jobs.cols;
           const int64_t base = (int64_t)(z - jobs.first[t]) * jobs.rows * jobs.cols;
@@ -325,21 +393,22 @@ int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Plan {
-  int n, L, np, lp, tile, chunks, mats, terms;
+  int n, L, np, lp, tile, chunks, mats;
   size_t x0, x1, A, B, bytes;   // offsets; the partial sums come first
 };
-Plan plan_of(int rows, int cols, int mats, int terms) {
+// Tiles of 128 where they alone occupy the device, of 64 otherwise.
+constexpr int kManyTiles = 192;
+Plan plan_of(int rows, int cols, int mats) {
   Plan p;
   p.n = rows < cols ? rows : cols;
   p.L = rows < cols ? cols : rows;
   p.mats = mats;
-  p.terms = terms;
-  p.tile = 64;
+  p.tile = round_up(p.n, 128) / 128 * (round_up(p.n, 128) / 128) * mats >= kManyTiles ? 128 : 64;
   p.np = (int)round_up(p.n, p.tile);
   p.lp = (int)round_up(p.L, p.tile);
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
-  const size_t x = align256((size_t)mats * terms * p.np * p.lp * 2), a = align256((size_t)mats * terms * p.np * p.np * 2);
+  const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
   p.x0 = part;
   p.x1 = p.x0 + x;
   p.A = p.x1 + x;
@@ -348,12 +417,16 @@ Plan plan_of(int rows, int cols, int mats, int terms) {
   return p;
 }
 
-template <int kMode, int kT, int TI>
-void gemm(const GemmArgs& g, const Jobs& j, int mats, hipStream_t st) {
-  hipLaunchKernelGGL((k_ns_gemm<kMode, kT, TI>), dim3(g.tiles_i * g.tiles_j, mats), dim3(kThreads), 0, st, g, j);
+template <int kMode, int TI>
+void gemm(GemmArgs g, const Jobs& j, int mats, hipStream_t st) {
+  g.tiles_i = g.np / TI;
+  g.tiles_j = g.width / TI;
+  g.tiles = g.tiles_i * g.tiles_j * mats;
+  g.per_xcd = (g.tiles + 7) / 8;
+  hipLaunchKernelGGL((k_ns_gemm<kMode, TI>), dim3(8 * g.per_xcd), dim3(kThreads), 0, st, g, j);
 }
 
-template <int kT, int TI>
+template <int TI>
 hipError_t steps_of(const Plan& p, const Jobs& j, int steps, char* ws, hipStream_t st, Timer* tm) {
   double* part = reinterpret_cast<double*>(ws);
   u16 *x0 = reinterpret_cast<u16*>(ws + p.x0), *x1 = reinterpret_cast<u16*>(ws + p.x1);
@@ -362,21 +435,20 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, char* ws, hipStream
   hipLaunchKernelGGL(k_ns_norm, dim3((unsigned)p.mats * p.chunks), dim3(kThreads), 0, st, j, p.chunks, part);
   if (tm) tm->end();
   if (tm) tm->begin("ns_split");
-  hipLaunchKernelGGL((k_ns_split<kT>), dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, x0,
-                     p.np, p.lp);
+  hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, x0, p.np,
+                     p.lp);
   if (tm) tm->end();
-  const int ti = p.np / TI, tl = p.lp / TI;
   for (int s = 0; s < steps; ++s) {
     if (tm) tm->begin("ns_gram");
-    gemm<kGram, kT, TI>(GemmArgs{x0, x0, nullptr, A, p.np, p.lp, p.np, ti, ti}, j, p.mats, st);
+    gemm<kGram, TI>(GemmArgs{x0, x0, nullptr, A, p.np, p.lp, p.np}, j, p.mats, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_poly");
-    gemm<kPoly, kT, TI>(GemmArgs{A, A, A, B, p.np, p.np, p.np, ti, ti}, j, p.mats, st);
+    gemm<kPoly, TI>(GemmArgs{A, A, A, B, p.np, p.np, p.np}, j, p.mats, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_apply");
-    const GemmArgs g{B, x0, x0, x1, p.np, p.np, p.lp, ti, tl};
-    if (s + 1 < steps) gemm<kApply, kT, TI>(g, j, p.mats, st);
-    else gemm<kStore, kT, TI>(g, j, p.mats, st);
+    const GemmArgs g{B, x0, x0, x1, p.np, p.np, p.lp};
+    if (s + 1 < steps) gemm<kApply, TI>(g, j, p.mats, st);
+    else gemm<kStore, TI>(g, j, p.mats, st);
     if (tm) tm->end();
     u16* t = x0;
     x0 = x1;
@@ -416,7 +488,7 @@ size_t muon_workspace(const MatrixJobs& js) {
   size_t most = 0;
   (void)for_each_shape(js, [&](const int* list, int n) {
     const Job& a = js.job[list[0]];
-    const size_t b = plan_of(a.rows, a.cols, total_of(js, list, n), js.out_bf16 ? 2 : 3).bytes;
+    const size_t b = plan_of(a.rows, a.cols, total_of(js, list, n)).bytes;
     most = b > most ? b : most;
     return hipSuccess;
   });
@@ -447,9 +519,9 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm
     j.b = js.coef[1];
     j.c = js.coef[2];
     j.eps = js.eps;
-    const Plan p = plan_of(a.rows, a.cols, j.first[n], js.out_bf16 ? 2 : 3);
+    const Plan p = plan_of(a.rows, a.cols, j.first[n]);
     char* w = static_cast<char*>(ws);
-    return js.out_bf16 ? steps_of<2, 64>(p, j, js.steps, w, st, tm) : steps_of<3, 64>(p, j, js.steps, w, st, tm);
+    return p.tile == 128 ? steps_of<128>(p, j, js.steps, w, st, tm) : steps_of<64>(p, j, js.steps, w, st, tm);
   });
 }
 
