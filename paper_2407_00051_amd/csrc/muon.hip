@@ -388,6 +388,304 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
       }
 }
 
+// ---- small matrices -------------------------------------------------------------------
+// All steps of one matrix in one workgroup, from the momentum update to the
+// parameters, X never leaving registers and LDS: n <= NP and L <= 16384 / NP, for NP
+// of 32, 64 and 128.  Wave (rw, cw) of NP / 32 x 128 / NP owns rows 32 rw .. + 31 of X
+// and every (128 / NP)-th block of 32 columns, four at most; lane lr (of half lh) holds
+// row 32 rw + lr, columns 8 g + 4 lh + 0..3 of each block, as accumulators do.
+//   A = X X^T: the wave forms the columns 32 rw .. of A (all of them: waves of one rw
+//   repeat each other).  A is symmetric, so a lane's accumulators are pieces of a row
+//   of A, and in the K order (4 lh + 0..3, 8 + 4 lh + 0..3) of every 16 they are the
+//   operand of the next products as they stand: A never leaves the registers.
+//   Y = A X, then X <- a X + b Y + c A Y: the other operand is X, then Y, read down
+//   its columns from LDS in the same K order.
+// LDS holds X (or Y) as [term][row][unit of 8 columns]: unit 4 J + 2 s + h of a row has
+// columns 32 J + 16 s + 4 h + 0..3 and + 8..11, what one lane half has of a K step, and
+// is kept at unit ^ swz(row), so that 8 lanes (rows) of a 16-byte access and the 4 rows
+// of a transposed read hit distinct banks.
+struct SmallJobs {
+  const void* src[SAGIPS_MAX_TENSORS];
+  float* m[SAGIPS_MAX_TENSORS];
+  void* out[SAGIPS_MAX_TENSORS];
+  int first[SAGIPS_MAX_TENSORS + 1];
+  int rows[SAGIPS_MAX_TENSORS], cols[SAGIPS_MAX_TENSORS];
+  float rate[SAGIPS_MAX_TENSORS];
+  int n_tensors, src_bf16, out_bf16, nesterov, steps;
+  float momentum, decay, a, b, c;
+  double eps;
+};
+
+constexpr int kSmallValues = 16384;                    // NP x LP
+constexpr int kSmallLds = 128 * 129 * 4;               // the fp32 copy, rows one value longer if even; X's terms: 64 KB
+
+template <int NP>
+struct Small {
+  static constexpr int LP = kSmallValues / NP;
+  static constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
+  static constexpr int RB = 2 * LP;                    // bytes of a row of one term
+  static constexpr int PL = NP * RB;                   // bytes of a term
+  typedef f16x8 Operand[NI][2][kT];                    // A's columns of a lane's row: [block][step]
+
+  static __device__ __forceinline__ uint32_t swz(int f) { return (uint32_t)(2 * (f & 3) + ((f >> 2) & 1)); }
+  static __device__ __forceinline__ uint32_t at_row(int row, int unit) { return row * RB + ((unit ^ swz(row)) << 4); }
+};
+
+template <int NP>
+__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jb) {
+  typedef Small<NP> S;
+  __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+  __shared__ double sums[kThreads / 64];
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int wave = threadIdx.x >> 6, rw = wave % S::RW, cw = wave / S::RW;
+  int t = 0;
+  while (t + 1 < jb.n_tensors && (int)blockIdx.x >= jb.first[t + 1]) ++t;
+  const int rows = jb.rows[t], cols = jb.cols[t], size = rows * cols;
+  const bool flip = rows > cols;
+  const int n = flip ? cols : rows, L = flip ? rows : cols, NJ = (L + 31) / 32;
+  const int64_t base = (int64_t)((int)blockIdx.x - jb.first[t]) * size;
+  float* const flat = reinterpret_cast<float*>(lds);
+  const int pitch = cols | 1;
+  const float inv_cols = 1.0f / cols;
+  const bool quads = size % 4 == 0;                    // then every matrix of the stack is 16-byte aligned
+
+  // U into LDS, the momentum on the way, and its norm
+  double sq = 0.0;
+  const auto update = [&](float u, float* m) __attribute__((always_inline)) {
+    if (m) {
+      *m = fmaf(jb.momentum, *m, u);
+      u = jb.nesterov ? fmaf(jb.momentum, *m, u) : *m;
+    }
+    sq = fma((double)u, (double)u, sq);
+    return u;
+  };
+  float* const mom = jb.m[t] ? jb.m[t] + base : nullptr;
+  if (quads) {
+#pragma unroll 4
+    for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
+      f32x4 u, m = {};
+      if (jb.src_bf16) {
+        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const u16*>(jb.src[t]) + base + e);
+        u = f32x4{bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)};
+      } else {
+        u = *reinterpret_cast<const f32x4*>(static_cast<const float*>(jb.src[t]) + base + e);
+      }
+      if (mom) m = *reinterpret_cast<const f32x4*>(mom + e);
+      int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;   // e < 2^14: exact
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float mk = m[k];
+        const float v = update(u[k], mom ? &mk : nullptr);
+        m[k] = mk;
+        flat[r * pitch + c] = v;
+        if (++c == cols) {
+          c = 0;
+          ++r;
+        }
+      }
+      if (mom) *reinterpret_cast<f32x4*>(mom + e) = m;
+    }
+  } else {
+    for (int e = threadIdx.x; e < size; e += kThreads) {
+      const int r = (int)((e + 0.5f) * inv_cols);
+      flat[r * pitch + e - r * cols] = update(load_src(jb.src[t], base + e, jb.src_bf16), mom ? mom + e : nullptr);
+    }
+  }
+  sq = wave_sum_d(sq);
+  if (lane == 0) sums[wave] = sq;
+  __syncthreads();
+  const float inv = (float)(1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + jb.eps));
+
+  const int i = 32 * rw + lr;
+  const auto place = [&](int j) { return flip ? j * pitch + i : i * pitch + j; };   // of X's (i, j) in the fp32 copy
+  f32x16 x[4];
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int j = 32 * (b * S::CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
+      x[b][r] = i < n && j < L ? flat[place(j)] * inv : 0.0f;
+    }
+  __syncthreads();
+
+  // terms of a block's 16 values: two units
+  const auto store = [&](int b, const f32x16& v) __attribute__((always_inline)) {
+    const int J = b * S::CW + cw;
+    if (J >= NJ) return;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 h, l;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t a, c;
+        split2(v[8 * s + 2 * q], v[8 * s + 2 * q + 1], a, c);
+        h[q] = a;
+        l[q] = c;
+      }
+      char* at = lds + S::at_row(i, 4 * J + 2 * s + lh);
+      *reinterpret_cast<u32x4*>(at) = h;
+      *reinterpret_cast<u32x4*>(at + S::PL) = l;
+    }
+  };
+  // two blocks of A times what LDS holds
+  const int i16 = lane & 15, half = (lane >> 4) & 1;
+  const auto times = [&](const typename S::Operand& af, int b0, f32x16 (&v)[2]) __attribute__((always_inline)) {
+    f32x16 c[2] = {}, d[2] = {};
+#pragma unroll
+    for (int ib = 0; ib < S::NI; ++ib)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        f16x8 q[2][kT];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int J = (b0 + y) * S::CW + cw, unit = 4 * J + 2 * half + (i16 & 1);
+          const int r0 = 32 * ib + 16 * s + 4 * lh + (i16 >> 2), r1 = r0 + 8;
+          const char* p0 = lds + S::at_row(r0, unit) + 8 * (i16 >> 1 & 1);
+          const char* p1 = lds + S::at_row(r1, unit) + 8 * (i16 >> 1 & 1);
+#pragma unroll
+          for (int w = 0; w < kT; ++w) q[y][w] = lds_col2(p0 + w * S::PL, p1 + w * S::PL);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) d[y] = mfma16(q[y][0], af[ib][s][1], d[y]);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) c[y] = mfma16(q[y][0], af[ib][s][0], c[y]);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) d[y] = mfma16(q[y][1], af[ib][s][0], d[y]);
+      }
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) v[y][r] = fmaf(d[y][r], kInvLo, c[y][r]);
+  };
+
+#pragma unroll
+  for (int b = 0; b < 4; ++b) store(b, x[b]);
+  for (int step = 0; step < jb.steps; ++step) {
+    lds_barrier();
+    typename S::Operand af;
+    {
+      f32x16 c[S::NI] = {}, d[S::NI] = {};
+      for (int J = 0; J < NJ; ++J)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int unit = 4 * J + 2 * s + lh;
+          f16x8 p[kT], q[S::NI][kT];
+#pragma unroll
+          for (int w = 0; w < kT; ++w) {
+            p[w] = lds_row(lds + w * S::PL + S::at_row(i, unit));
+#pragma unroll
+            for (int ib = 0; ib < S::NI; ++ib) q[ib][w] = lds_row(lds + w * S::PL + S::at_row(32 * ib + lr, unit));
+          }
+#pragma unroll
+          for (int ib = 0; ib < S::NI; ++ib) d[ib] = mfma16(q[ib][0], p[1], d[ib]);
+#pragma unroll
+          for (int ib = 0; ib < S::NI; ++ib) c[ib] = mfma16(q[ib][0], p[0], c[ib]);
+#pragma unroll
+          for (int ib = 0; ib < S::NI; ++ib) d[ib] = mfma16(q[ib][1], p[0], d[ib]);
+        }
+#pragma unroll
+      for (int ib = 0; ib < S::NI; ++ib)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u32x4 h, l;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int r = 8 * s + 2 * q;
+            uint32_t hq, lq;
+            split2(fmaf(d[ib][r], kInvLo, c[ib][r]), fmaf(d[ib][r + 1], kInvLo, c[ib][r + 1]), hq, lq);
+            h[q] = hq;
+            l[q] = lq;
+          }
+          af[ib][s][0] = __builtin_bit_cast(f16x8, h);
+          af[ib][s][1] = __builtin_bit_cast(f16x8, l);
+        }
+    }
+    f32x16 y[4];
+#pragma unroll
+    for (int b0 = 0; b0 < 4; b0 += 2)
+      if (b0 * S::CW + cw < NJ) {
+        f32x16 v[2];
+        times(af, b0, v);
+        y[b0] = v[0];
+        y[b0 + 1] = v[1];
+      }
+    lds_barrier();                                     // X has been read
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      store(b, y[b]);
+      x[b] = jb.a * x[b] + jb.b * y[b];
+    }
+    lds_barrier();
+#pragma unroll
+    for (int b0 = 0; b0 < 4; b0 += 2)
+      if (b0 * S::CW + cw < NJ) {
+        f32x16 v[2];
+        times(af, b0, v);
+        x[b0] += jb.c * v[0];
+        x[b0 + 1] += jb.c * v[1];
+      }
+    lds_barrier();                                     // Y has been read
+    if (step + 1 < jb.steps)
+#pragma unroll
+      for (int b = 0; b < 4; ++b) store(b, x[b]);
+  }
+
+  // the result through the fp32 copy, so that the parameters are read and written in order
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int j = 32 * (b * S::CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
+      if (i < n && j < L) flat[place(j)] = x[b][r];
+    }
+  __syncthreads();
+  const float rate = jb.rate[t];
+  if (quads) {
+#pragma unroll 4
+    for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
+      f32x4 v;
+      int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[k] = flat[r * pitch + c];
+        if (++c == cols) {
+          c = 0;
+          ++r;
+        }
+      }
+      if (mom) {
+        f32x4* w = reinterpret_cast<f32x4*>(static_cast<float*>(jb.out[t]) + base + e);
+        *w = jb.decay * *w - rate * v;
+      } else if (jb.out_bf16) {
+        *reinterpret_cast<uint2*>(static_cast<u16*>(jb.out[t]) + base + e) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+      } else {
+        *reinterpret_cast<f32x4*>(static_cast<float*>(jb.out[t]) + base + e) = v;
+      }
+    }
+  } else {
+    for (int e = threadIdx.x; e < size; e += kThreads) {
+      const int r = (int)((e + 0.5f) * inv_cols);
+      const float v = flat[r * pitch + e - r * cols];
+      if (mom) {
+        float* w = static_cast<float*>(jb.out[t]) + base + e;
+        *w = fmaf(-rate, v, jb.decay * *w);
+      } else if (jb.out_bf16) {
+        static_cast<u16*>(jb.out[t])[base + e] = to_bf16(v);
+      } else {
+        static_cast<float*>(jb.out[t])[base + e] = v;
+      }
+    }
+  }
+}
+
+// NP of the workgroup that holds a matrix, or 0.
+int small_class(int rows, int cols) {
+  const int n = rows < cols ? rows : cols, L = rows < cols ? cols : rows;
+  for (int np = 32; np <= 128; np *= 2)
+    if (n <= np && L <= kSmallValues / np) return np;
+  return 0;
+}
+
 // ---- plan ---------------------------------------------------------------------------
 int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -465,7 +763,7 @@ template <class F>
 static hipError_t for_each_shape(const MatrixJobs& js, F&& f) {
   bool done[SAGIPS_MAX_TENSORS] = {};
   for (int i = 0; i < js.n_jobs; ++i) {
-    if (done[i]) continue;
+    if (done[i] || small_class(js.job[i].rows, js.job[i].cols)) continue;
     int list[SAGIPS_MAX_TENSORS], n = 0;
     for (int k = i; k < js.n_jobs; ++k)
       if (!done[k] && js.job[k].rows == js.job[i].rows && js.job[k].cols == js.job[i].cols) {
@@ -495,7 +793,45 @@ size_t muon_workspace(const MatrixJobs& js) {
   return most;
 }
 
+static hipError_t launch_small(const MatrixJobs& js, int np, hipStream_t st, Timer* tm) {
+  SmallJobs j{};
+  for (int k = 0; k < js.n_jobs; ++k) {
+    const Job& q = js.job[k];
+    if (small_class(q.rows, q.cols) != np) continue;
+    const int t = j.n_tensors++;
+    j.src[t] = q.src;
+    j.m[t] = q.m;
+    j.out[t] = q.out;
+    j.first[t + 1] = j.first[t] + q.count;
+    j.rows[t] = q.rows;
+    j.cols[t] = q.cols;
+    j.rate[t] = (float)(js.lr * q.scale);
+  }
+  if (!j.n_tensors) return hipSuccess;
+  j.src_bf16 = js.src_bf16;
+  j.out_bf16 = js.out_bf16;
+  j.nesterov = js.nesterov;
+  j.steps = js.steps;
+  j.momentum = js.momentum;
+  j.decay = js.decay;
+  j.a = js.coef[0];
+  j.b = js.coef[1];
+  j.c = js.coef[2];
+  j.eps = js.eps;
+  const dim3 grid(j.first[j.n_tensors]);
+  if (tm) tm->begin("ns_small");
+  if (np == 32) hipLaunchKernelGGL((k_ns_small<32>), grid, dim3(kThreads), 0, st, j);
+  else if (np == 64) hipLaunchKernelGGL((k_ns_small<64>), grid, dim3(kThreads), 0, st, j);
+  else hipLaunchKernelGGL((k_ns_small<128>), grid, dim3(kThreads), 0, st, j);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
 hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm) {
+  for (int np = 32; np <= 128; np *= 2) {
+    const hipError_t e = launch_small(js, np, st, tm);
+    if (e != hipSuccess) return e;
+  }
   return for_each_shape(js, [&](const int* list, int n) {
     const Job& a = js.job[list[0]];
     Jobs j{};
