@@ -16,6 +16,8 @@
 // matrix instructions.  fp16 ends at 65,504: X, X X^T and the polynomial of it
 // stay below that because the singular values do (launch_muon's caller bounds
 // them from the coefficients).
+#include <limits.h>
+
 #include "kernels.hpp"
 #include "split_bf16.hpp"
 
@@ -41,7 +43,6 @@ struct Jobs {
   float* m[SAGIPS_MAX_TENSORS];          // momenta, or NULL
   void* out[SAGIPS_MAX_TENSORS];         // parameters, or the orthogonalised matrices
   int first[SAGIPS_MAX_TENSORS + 1];
-  int n_tensors;
   int rows, cols;                        // of every matrix
   int src_bf16, out_bf16;
   float momentum, decay, rate;           // m <- momentum m + g;  p <- decay p - rate X
@@ -50,9 +51,11 @@ struct Jobs {
   double eps;
 };
 
-__device__ __forceinline__ int tensor_of(const Jobs& j, int z) {
+// Tensor of matrix z: first[] is INT_MAX past the last tensor.
+__device__ __forceinline__ int tensor_of(const int (&first)[SAGIPS_MAX_TENSORS + 1], int z) {
   int t = 0;
-  while (t + 1 < j.n_tensors && z >= j.first[t + 1]) ++t;
+#pragma unroll
+  for (int k = 1; k < SAGIPS_MAX_TENSORS; ++k) t += z >= first[k];
   return t;
 }
 __device__ __forceinline__ float load_src(const void* p, int64_t i, int bf16) {
@@ -66,16 +69,17 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   return v;
 }
 
-// The terms of two values, packed in pairs.  The subtractions are exact.
+// The terms of two values, packed in pairs.  2^11 (x - hi) is exact in fp32.
 __device__ __forceinline__ uint32_t pk_f16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
 }
 __device__ __forceinline__ float f16_lo(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }
 __device__ __forceinline__ float f16_hi(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[1]; }
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-#pragma clang fp contract(off)
-  hi = pk_f16(a, b);
-  lo = pk_f16((a - f16_lo(hi)) * kLo, (b - f16_hi(hi)) * kLo);
+  const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
+  const f16x2 l = {(_Float16)fmaf((float)h[0], -kLo, a * kLo), (_Float16)fmaf((float)h[1], -kLo, b * kLo)};
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, l);
 }
 __device__ __forceinline__ f32x16 mfma16(f16x8 a, f16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
@@ -96,7 +100,7 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 constexpr int64_t kChunk = 4096;
 __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double* __restrict__ part) {
   const int z = blockIdx.x / chunks, k = blockIdx.x % chunks;
-  const int t = tensor_of(j, z);
+  const int t = tensor_of(j.first, z);
   const int64_t size = (int64_t)j.rows * j.cols, base = (z - j.first[t]) * size;
   const int64_t e1 = min(size, (k + 1) * kChunk);
   double s = 0.0;
@@ -144,7 +148,7 @@ __device__ __forceinline__ int64_t at_value(int i, int j, int width) {   // of t
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
                                                        u16* __restrict__ X, int np, int lp) {
   __shared__ float tile[64][65];
-  const int z = blockIdx.z, t = tensor_of(j, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
+  const int z = blockIdx.z, t = tensor_of(j.first, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
   const bool flip = j.rows > j.cols;
   const int64_t base = (int64_t)(z - j.first[t]) * j.rows * j.cols;
   const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
   }
 
   // A lane has row i, columns j .. j + 3 of each group.
-  const int t = kMode == kStore ? tensor_of(jobs, z) : 0;
+  const int t = kMode == kStore ? tensor_of(jobs.first, z) : 0;
 #pragma unroll
   for (int x = 0; x < WB; ++x)
 #pragma unroll
@@ -392,126 +396,144 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
 // All steps of one matrix in one workgroup, from the momentum update to the
 // parameters, X never leaving registers and LDS: n <= NP and L <= 16384 / NP, for NP
 // of 32, 64 and 128.  Wave (rw, cw) of NP / 32 x 128 / NP owns rows 32 rw .. + 31 of X
-// and every (128 / NP)-th block of 32 columns, four at most; lane lr (of half lh) holds
-// row 32 rw + lr, columns 8 g + 4 lh + 0..3 of each block, as accumulators do.
-//   A = X X^T: the wave forms the columns 32 rw .. of A (all of them: waves of one rw
-//   repeat each other).  A is symmetric, so a lane's accumulators are pieces of a row
-//   of A, and in the K order (4 lh + 0..3, 8 + 4 lh + 0..3) of every 16 they are the
-//   operand of the next products as they stand: A never leaves the registers.
+// and every (128 / NP)-th block of 32 columns, JB of them (the fewest of 1, 2 and 4
+// that hold L); lane lr (of half lh) holds row 32 rw + lr, columns 8 g + 4 lh + 0..3 of
+// each block, as accumulators do.
+//   A = X X^T: the wave forms columns 32 rw .. of A, summed over its own columns of X,
+//   whose terms it has in registers; waves of one rw add their sums through LDS.  A is
+//   symmetric, so a lane's accumulators are pieces of a row of A, and in the K order
+//   (4 lh + 0..3, 8 + 4 lh + 0..3) of every 16 they are the operand of the next
+//   products as they stand: A never leaves the registers.
 //   Y = A X, then X <- a X + b Y + c A Y: the other operand is X, then Y, read down
 //   its columns from LDS in the same K order.
 // LDS holds X (or Y) as [term][row][unit of 8 columns]: unit 4 J + 2 s + h of a row has
 // columns 32 J + 16 s + 4 h + 0..3 and + 8..11, what one lane half has of a K step, and
 // is kept at unit ^ swz(row), so that 8 lanes (rows) of a 16-byte access and the 4 rows
 // of a transposed read hit distinct banks.
+struct SmallJob {
+  const void* src;
+  float* m;
+  void* out;
+  int rows, cols;
+  float rate;
+};
 struct SmallJobs {
-  const void* src[SAGIPS_MAX_TENSORS];
-  float* m[SAGIPS_MAX_TENSORS];
-  void* out[SAGIPS_MAX_TENSORS];
+  SmallJob job[SAGIPS_MAX_TENSORS];
   int first[SAGIPS_MAX_TENSORS + 1];
-  int rows[SAGIPS_MAX_TENSORS], cols[SAGIPS_MAX_TENSORS];
-  float rate[SAGIPS_MAX_TENSORS];
-  int n_tensors, src_bf16, out_bf16, nesterov, steps;
+  int src_bf16, out_bf16, nesterov, steps;
   float momentum, decay, a, b, c;
   double eps;
 };
 
 constexpr int kSmallValues = 16384;                    // NP x LP
-constexpr int kSmallLds = 128 * 129 * 4;               // the fp32 copy, rows one value longer if even; X's terms: 64 KB
+constexpr int kSmallCopy = 128 * 129 * 4;              // the fp32 copy, rows one value longer if even; X's terms: 64 KB
 
-template <int NP>
-struct Small {
-  static constexpr int LP = kSmallValues / NP;
-  static constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
-  static constexpr int RB = 2 * LP;                    // bytes of a row of one term
-  static constexpr int PL = NP * RB;                   // bytes of a term
-  typedef f16x8 Operand[NI][2][kT];                    // A's columns of a lane's row: [block][step]
-
-  static __device__ __forceinline__ uint32_t swz(int f) { return (uint32_t)(2 * (f & 3) + ((f >> 2) & 1)); }
-  static __device__ __forceinline__ uint32_t at_row(int row, int unit) { return row * RB + ((unit ^ swz(row)) << 4); }
-};
-
-template <int NP>
-__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jb) {
-  typedef Small<NP> S;
-  __shared__ __attribute__((aligned(16))) char lds[kSmallLds];
+template <int NP, int JB>
+__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
+  constexpr int LP = kSmallValues / NP;
+  constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
+  constexpr int RB = 2 * LP, PL = NP * RB;             // bytes of a row of one term, of a term
+  constexpr int IP = NI > 1 ? 2 : 1, JP = JB > 1 ? 2 : 1;   // blocks multiplied at a time
+  __shared__ __attribute__((aligned(16))) char lds[kSmallCopy];
+  __shared__ float part[CW > 1 ? 4 : 1][NI * 16][64];  // the waves' sums for A
   __shared__ double sums[kThreads / 64];
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
-  const int wave = threadIdx.x >> 6, rw = wave % S::RW, cw = wave / S::RW;
-  int t = 0;
-  while (t + 1 < jb.n_tensors && (int)blockIdx.x >= jb.first[t + 1]) ++t;
-  const int rows = jb.rows[t], cols = jb.cols[t], size = rows * cols;
+  const int wave = threadIdx.x >> 6, rw = wave % RW, cw = wave / RW;
+  const int t = tensor_of(jobs.first, blockIdx.x);
+  const SmallJob job = jobs.job[t];
+  const int rows = job.rows, cols = job.cols, size = rows * cols;
   const bool flip = rows > cols;
-  const int n = flip ? cols : rows, L = flip ? rows : cols, NJ = (L + 31) / 32;
-  const int64_t base = (int64_t)((int)blockIdx.x - jb.first[t]) * size;
+  const int n = flip ? cols : rows, L = flip ? rows : cols;
+  const int64_t base = (int64_t)((int)blockIdx.x - jobs.first[t]) * size;
   float* const flat = reinterpret_cast<float*>(lds);
   const int pitch = cols | 1;
   const float inv_cols = 1.0f / cols;
   const bool quads = size % 4 == 0;                    // then every matrix of the stack is 16-byte aligned
+  float* const mom = job.m ? job.m + base : nullptr;
+  constexpr int kQuads = kSmallValues / 4 / kThreads;
 
-  // U into LDS, the momentum on the way, and its norm
+  // U into LDS, the momentum on the way, and its norm; every load in flight at once
   double sq = 0.0;
-  const auto update = [&](float u, float* m) __attribute__((always_inline)) {
-    if (m) {
-      *m = fmaf(jb.momentum, *m, u);
-      u = jb.nesterov ? fmaf(jb.momentum, *m, u) : *m;
-    }
-    sq = fma((double)u, (double)u, sq);
-    return u;
-  };
-  float* const mom = jb.m[t] ? jb.m[t] + base : nullptr;
   if (quads) {
-#pragma unroll 4
-    for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
-      f32x4 u, m = {};
-      if (jb.src_bf16) {
-        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const u16*>(jb.src[t]) + base + e);
-        u = f32x4{bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)};
+    f32x4 u[kQuads], m[kQuads];
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      const int e = (k * kThreads + threadIdx.x) * 4;
+      if (e >= size) continue;
+      if (jobs.src_bf16) {
+        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const u16*>(job.src) + base + e);
+        u[k][0] = __uint_as_float(q.x);
+        u[k][1] = __uint_as_float(q.y);
       } else {
-        u = *reinterpret_cast<const f32x4*>(static_cast<const float*>(jb.src[t]) + base + e);
+        u[k] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(job.src) + base + e);
       }
-      if (mom) m = *reinterpret_cast<const f32x4*>(mom + e);
+      if (mom) m[k] = *reinterpret_cast<const f32x4*>(mom + e);
+    }
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      const int e = (k * kThreads + threadIdx.x) * 4;
+      if (e >= size) continue;
+      f32x4 v = u[k];
+      if (jobs.src_bf16) {
+        const uint32_t q0 = __float_as_uint(u[k][0]), q1 = __float_as_uint(u[k][1]);
+        v = f32x4{bf16_lo(q0), bf16_hi(q0), bf16_lo(q1), bf16_hi(q1)};
+      }
+      if (mom) {
+        f32x4 w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          w[q] = fmaf(jobs.momentum, m[k][q], v[q]);
+          v[q] = jobs.nesterov ? fmaf(jobs.momentum, w[q], v[q]) : w[q];
+        }
+        *reinterpret_cast<f32x4*>(mom + e) = w;
+      }
       int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;   // e < 2^14: exact
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float mk = m[k];
-        const float v = update(u[k], mom ? &mk : nullptr);
-        m[k] = mk;
-        flat[r * pitch + c] = v;
+      for (int q = 0; q < 4; ++q) {
+        sq = fma((double)v[q], (double)v[q], sq);
+        flat[r * pitch + c] = v[q];
         if (++c == cols) {
           c = 0;
           ++r;
         }
       }
-      if (mom) *reinterpret_cast<f32x4*>(mom + e) = m;
     }
   } else {
+#pragma unroll 4
     for (int e = threadIdx.x; e < size; e += kThreads) {
       const int r = (int)((e + 0.5f) * inv_cols);
-      flat[r * pitch + e - r * cols] = update(load_src(jb.src[t], base + e, jb.src_bf16), mom ? mom + e : nullptr);
+      float u = load_src(job.src, base + e, jobs.src_bf16);
+      if (mom) {
+        const float w = fmaf(jobs.momentum, mom[e], u);
+        mom[e] = w;
+        u = jobs.nesterov ? fmaf(jobs.momentum, w, u) : w;
+      }
+      sq = fma((double)u, (double)u, sq);
+      flat[r * pitch + e - r * cols] = u;
     }
   }
   sq = wave_sum_d(sq);
   if (lane == 0) sums[wave] = sq;
   __syncthreads();
-  const float inv = (float)(1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + jb.eps));
+  const float inv = (float)(1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + jobs.eps));
 
   const int i = 32 * rw + lr;
-  const auto place = [&](int j) { return flip ? j * pitch + i : i * pitch + j; };   // of X's (i, j) in the fp32 copy
-  f32x16 x[4];
+  const int pi = flip ? 1 : pitch, pj = flip ? pitch : 1;   // X's (i, j) in the fp32 copy: i pi + j pj
+  f32x16 x[JB];
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+  for (int b = 0; b < JB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int j = 32 * (b * S::CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      x[b][r] = i < n && j < L ? flat[place(j)] * inv : 0.0f;
+      const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
+      x[b][r] = i < n && j < L ? flat[i * pi + j * pj] * inv : 0.0f;
     }
   __syncthreads();
 
-  // terms of a block's 16 values: two units
-  const auto store = [&](int b, const f32x16& v) __attribute__((always_inline)) {
-    const int J = b * S::CW + cw;
-    if (J >= NJ) return;
+  // Terms of 16 values, two units of 8.
+  struct Terms {
+    f16x8 v[2][kT];
+  };
+  const auto split = [](const f32x16& v, Terms& o) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 h, l;
@@ -522,168 +544,198 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jb) {
         h[q] = a;
         l[q] = c;
       }
-      char* at = lds + S::at_row(i, 4 * J + 2 * s + lh);
-      *reinterpret_cast<u32x4*>(at) = h;
-      *reinterpret_cast<u32x4*>(at + S::PL) = l;
+      o.v[s][0] = __builtin_bit_cast(f16x8, h);
+      o.v[s][1] = __builtin_bit_cast(f16x8, l);
     }
   };
-  // two blocks of A times what LDS holds
-  const int i16 = lane & 15, half = (lane >> 4) & 1;
-  const auto times = [&](const typename S::Operand& af, int b0, f32x16 (&v)[2]) __attribute__((always_inline)) {
-    f32x16 c[2] = {}, d[2] = {};
+  const auto swz = [](int f) { return (uint32_t)(2 * (f & 3) + ((f >> 2) & 1)); };
+  const uint32_t own = i * RB, own_swz = swz(i);       // rows 32 ib + lr: the same swizzle
+  const auto put = [&](int b, const Terms& o) __attribute__((always_inline)) {
 #pragma unroll
-    for (int ib = 0; ib < S::NI; ++ib)
+    for (int s = 0; s < 2; ++s) {
+      char* at = lds + own + (((4 * (b * CW + cw) + 2 * s + lh) ^ own_swz) << 4);
+      *reinterpret_cast<f16x8*>(at) = o.v[s][0];
+      *reinterpret_cast<f16x8*>(at + PL) = o.v[s][1];
+    }
+  };
+  // JP blocks of A times what LDS holds.
+  const int i16 = lane & 15, half = (lane >> 4) & 1;
+  const uint32_t row0 = 4 * lh + (i16 >> 2), swz0 = swz(row0);   // rows 32 ib + 16 s (+ 8) + row0: the same swizzle
+  const auto times = [&](const Terms (&A)[NI], int b0, f32x16 (&v)[JP]) __attribute__((always_inline)) {
+    f32x16 c[JP] = {}, d[JP] = {};
+#pragma unroll
+    for (int ib = 0; ib < NI; ++ib)
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        f16x8 q[2][kT];
+        f16x8 q[JP][kT];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const int J = (b0 + y) * S::CW + cw, unit = 4 * J + 2 * half + (i16 & 1);
-          const int r0 = 32 * ib + 16 * s + 4 * lh + (i16 >> 2), r1 = r0 + 8;
-          const char* p0 = lds + S::at_row(r0, unit) + 8 * (i16 >> 1 & 1);
-          const char* p1 = lds + S::at_row(r1, unit) + 8 * (i16 >> 1 & 1);
+        for (int y = 0; y < JP; ++y) {
+          const int unit = 4 * ((b0 + y) * CW + cw) + 2 * half + (i16 & 1);
+          const char* p = lds + (32 * ib + 16 * s + row0) * RB + ((unit ^ swz0) << 4) + 8 * (i16 >> 1 & 1);
 #pragma unroll
-          for (int w = 0; w < kT; ++w) q[y][w] = lds_col2(p0 + w * S::PL, p1 + w * S::PL);
+          for (int w = 0; w < kT; ++w) q[y][w] = lds_col2(p + w * PL, p + w * PL + 8 * RB);
         }
 #pragma unroll
-        for (int y = 0; y < 2; ++y) d[y] = mfma16(q[y][0], af[ib][s][1], d[y]);
+        for (int y = 0; y < JP; ++y) d[y] = mfma16(q[y][0], A[ib].v[s][1], d[y]);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) c[y] = mfma16(q[y][0], af[ib][s][0], c[y]);
+        for (int y = 0; y < JP; ++y) c[y] = mfma16(q[y][0], A[ib].v[s][0], c[y]);
 #pragma unroll
-        for (int y = 0; y < 2; ++y) d[y] = mfma16(q[y][1], af[ib][s][0], d[y]);
+        for (int y = 0; y < JP; ++y) d[y] = mfma16(q[y][1], A[ib].v[s][0], d[y]);
       }
 #pragma unroll
-    for (int y = 0; y < 2; ++y)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) v[y][r] = fmaf(d[y][r], kInvLo, c[y][r]);
+    for (int y = 0; y < JP; ++y) v[y] = c[y] + d[y] * kInvLo;
   };
 
+  Terms xt[JB];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) store(b, x[b]);
-  for (int step = 0; step < jb.steps; ++step) {
+  for (int b = 0; b < JB; ++b) {
+    split(x[b], xt[b]);
+    put(b, xt[b]);
+  }
+  for (int step = 0; step < jobs.steps; ++step) {
     lds_barrier();
-    typename S::Operand af;
-    {
-      f32x16 c[S::NI] = {}, d[S::NI] = {};
-      for (int J = 0; J < NJ; ++J)
+    Terms A[NI];
+#pragma unroll
+    for (int i0 = 0; i0 < NI; i0 += IP) {
+      f32x16 c[IP] = {}, d[IP] = {};
+#pragma unroll
+      for (int b = 0; b < JB; ++b)
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-          const int unit = 4 * J + 2 * s + lh;
-          f16x8 p[kT], q[S::NI][kT];
+          f16x8 q[IP][kT];
 #pragma unroll
-          for (int w = 0; w < kT; ++w) {
-            p[w] = lds_row(lds + w * S::PL + S::at_row(i, unit));
+          for (int y = 0; y < IP; ++y)
 #pragma unroll
-            for (int ib = 0; ib < S::NI; ++ib) q[ib][w] = lds_row(lds + w * S::PL + S::at_row(32 * ib + lr, unit));
-          }
+            for (int w = 0; w < kT; ++w)
+              q[y][w] = lds_row(lds + w * PL + (32 * (i0 + y) + lr) * RB + (((4 * (b * CW + cw) + 2 * s + lh) ^ own_swz) << 4));
 #pragma unroll
-          for (int ib = 0; ib < S::NI; ++ib) d[ib] = mfma16(q[ib][0], p[1], d[ib]);
+          for (int y = 0; y < IP; ++y) d[y] = mfma16(q[y][0], xt[b].v[s][1], d[y]);
 #pragma unroll
-          for (int ib = 0; ib < S::NI; ++ib) c[ib] = mfma16(q[ib][0], p[0], c[ib]);
+          for (int y = 0; y < IP; ++y) c[y] = mfma16(q[y][0], xt[b].v[s][0], c[y]);
 #pragma unroll
-          for (int ib = 0; ib < S::NI; ++ib) d[ib] = mfma16(q[ib][1], p[0], d[ib]);
+          for (int y = 0; y < IP; ++y) d[y] = mfma16(q[y][1], xt[b].v[s][0], d[y]);
         }
 #pragma unroll
-      for (int ib = 0; ib < S::NI; ++ib)
+      for (int y = 0; y < IP; ++y) {
+        const f32x16 v = c[y] + d[y] * kInvLo;
+        if constexpr (CW == 1) {
+          split(v, A[i0 + y]);
+        } else {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u32x4 h, l;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int r = 8 * s + 2 * q;
-            uint32_t hq, lq;
-            split2(fmaf(d[ib][r], kInvLo, c[ib][r]), fmaf(d[ib][r + 1], kInvLo, c[ib][r + 1]), hq, lq);
-            h[q] = hq;
-            l[q] = lq;
-          }
-          af[ib][s][0] = __builtin_bit_cast(f16x8, h);
-          af[ib][s][1] = __builtin_bit_cast(f16x8, l);
+          for (int r = 0; r < 16; ++r) part[wave][(i0 + y) * 16 + r][lane] = v[r];
         }
-    }
-    f32x16 y[4];
-#pragma unroll
-    for (int b0 = 0; b0 < 4; b0 += 2)
-      if (b0 * S::CW + cw < NJ) {
-        f32x16 v[2];
-        times(af, b0, v);
-        y[b0] = v[0];
-        y[b0 + 1] = v[1];
       }
+    }
+    if constexpr (CW > 1) {
+      lds_barrier();
+#pragma unroll
+      for (int ib = 0; ib < NI; ++ib) {
+        f32x16 v = {};
+#pragma unroll
+        for (int w = 0; w < CW; ++w)                   // the same order in every wave
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v[r] += part[w * RW + rw][ib * 16 + r][lane];
+        split(v, A[ib]);
+      }
+    }
+#pragma unroll
+    for (int b0 = 0; b0 < JB; b0 += JP) {
+      f32x16 v[JP];
+      times(A, b0, v);
+#pragma unroll
+      for (int y = 0; y < JP; ++y) {
+        split(v[y], xt[b0 + y]);
+        x[b0 + y] = jobs.a * x[b0 + y] + jobs.b * v[y];
+      }
+    }
     lds_barrier();                                     // X has been read
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      store(b, y[b]);
-      x[b] = jb.a * x[b] + jb.b * y[b];
-    }
+    for (int b = 0; b < JB; ++b) put(b, xt[b]);
     lds_barrier();
 #pragma unroll
-    for (int b0 = 0; b0 < 4; b0 += 2)
-      if (b0 * S::CW + cw < NJ) {
-        f32x16 v[2];
-        times(af, b0, v);
-        x[b0] += jb.c * v[0];
-        x[b0 + 1] += jb.c * v[1];
-      }
-    lds_barrier();                                     // Y has been read
-    if (step + 1 < jb.steps)
+    for (int b0 = 0; b0 < JB; b0 += JP) {
+      f32x16 v[JP];
+      times(A, b0, v);
 #pragma unroll
-      for (int b = 0; b < 4; ++b) store(b, x[b]);
+      for (int y = 0; y < JP; ++y) {
+        x[b0 + y] += jobs.c * v[y];
+        split(x[b0 + y], xt[b0 + y]);
+      }
+    }
+    lds_barrier();                                     // Y has been read
+    if (step + 1 < jobs.steps)
+#pragma unroll
+      for (int b = 0; b < JB; ++b) put(b, xt[b]);
   }
 
   // the result through the fp32 copy, so that the parameters are read and written in order
+  f32x4 old[kQuads];
+  if (quads && mom)
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+    for (int k = 0; k < kQuads; ++k) {
+      const int e = (k * kThreads + threadIdx.x) * 4;
+      if (e < size) old[k] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(job.out) + base + e);
+    }
+#pragma unroll
+  for (int b = 0; b < JB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      const int j = 32 * (b * S::CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      if (i < n && j < L) flat[place(j)] = x[b][r];
+      const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
+      if (i < n && j < L) flat[i * pi + j * pj] = x[b][r];
     }
   __syncthreads();
-  const float rate = jb.rate[t];
   if (quads) {
-#pragma unroll 4
-    for (int e = threadIdx.x * 4; e < size; e += kThreads * 4) {
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      const int e = (k * kThreads + threadIdx.x) * 4;
+      if (e >= size) continue;
       f32x4 v;
       int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        v[k] = flat[r * pitch + c];
+      for (int q = 0; q < 4; ++q) {
+        v[q] = flat[r * pitch + c];
         if (++c == cols) {
           c = 0;
           ++r;
         }
       }
       if (mom) {
-        f32x4* w = reinterpret_cast<f32x4*>(static_cast<float*>(jb.out[t]) + base + e);
-        *w = jb.decay * *w - rate * v;
-      } else if (jb.out_bf16) {
-        *reinterpret_cast<uint2*>(static_cast<u16*>(jb.out[t]) + base + e) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+        *reinterpret_cast<f32x4*>(static_cast<float*>(job.out) + base + e) = jobs.decay * old[k] - job.rate * v;
+      } else if (jobs.out_bf16) {
+        *reinterpret_cast<uint2*>(static_cast<u16*>(job.out) + base + e) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
       } else {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(jb.out[t]) + base + e) = v;
+        *reinterpret_cast<f32x4*>(static_cast<float*>(job.out) + base + e) = v;
       }
     }
   } else {
+#pragma unroll 4
     for (int e = threadIdx.x; e < size; e += kThreads) {
       const int r = (int)((e + 0.5f) * inv_cols);
       const float v = flat[r * pitch + e - r * cols];
       if (mom) {
-        float* w = static_cast<float*>(jb.out[t]) + base + e;
-        *w = fmaf(-rate, v, jb.decay * *w);
-      } else if (jb.out_bf16) {
-        static_cast<u16*>(jb.out[t])[base + e] = to_bf16(v);
+        float* w = static_cast<float*>(job.out) + base + e;
+        *w = fmaf(-job.rate, v, jobs.decay * *w);
+      } else if (jobs.out_bf16) {
+        static_cast<u16*>(job.out)[base + e] = to_bf16(v);
       } else {
-        static_cast<float*>(jb.out[t])[base + e] = v;
+        static_cast<float*>(job.out)[base + e] = v;
       }
     }
   }
 }
 
-// NP of the workgroup that holds a matrix, or 0.
+// The workgroup that holds a matrix, as 3 (log2 NP - 5) + log2 JB; -1: none does.
+constexpr int kSmallClasses = 9;
 int small_class(int rows, int cols) {
   const int n = rows < cols ? rows : cols, L = rows < cols ? cols : rows;
-  for (int np = 32; np <= 128; np *= 2)
-    if (n <= np && L <= kSmallValues / np) return np;
-  return 0;
+  for (int p = 0; p < 3; ++p)
+    for (int b = 0; b < 3 && n <= 32 << p; ++b)
+      if (L <= ((32 << b) * 4 >> p)) return 3 * p + b;   // 32 JB columns a wave, 4 / 2^p waves
+  return -1;
+}
+template <int P, int B>
+void small_kernel(const SmallJobs& j, hipStream_t st) {
+  hipLaunchKernelGGL((k_ns_small<(32 << P), (1 << B)>), dim3(j.first[SAGIPS_MAX_TENSORS]), dim3(kThreads), 0, st, j);
 }
 
 // ---- plan ---------------------------------------------------------------------------
@@ -763,7 +815,7 @@ template <class F>
 static hipError_t for_each_shape(const MatrixJobs& js, F&& f) {
   bool done[SAGIPS_MAX_TENSORS] = {};
   for (int i = 0; i < js.n_jobs; ++i) {
-    if (done[i] || small_class(js.job[i].rows, js.job[i].cols)) continue;
+    if (done[i] || small_class(js.job[i].rows, js.job[i].cols) >= 0) continue;
     int list[SAGIPS_MAX_TENSORS], n = 0;
     for (int k = i; k < js.n_jobs; ++k)
       if (!done[k] && js.job[k].rows == js.job[i].rows && js.job[k].cols == js.job[i].cols) {
@@ -793,21 +845,19 @@ size_t muon_workspace(const MatrixJobs& js) {
   return most;
 }
 
-static hipError_t launch_small(const MatrixJobs& js, int np, hipStream_t st, Timer* tm) {
+static hipError_t launch_small(const MatrixJobs& js, int which, hipStream_t st, Timer* tm) {
   SmallJobs j{};
+  int n = 0, total = 0;
   for (int k = 0; k < js.n_jobs; ++k) {
     const Job& q = js.job[k];
-    if (small_class(q.rows, q.cols) != np) continue;
-    const int t = j.n_tensors++;
-    j.src[t] = q.src;
-    j.m[t] = q.m;
-    j.out[t] = q.out;
-    j.first[t + 1] = j.first[t] + q.count;
-    j.rows[t] = q.rows;
-    j.cols[t] = q.cols;
-    j.rate[t] = (float)(js.lr * q.scale);
+    if (small_class(q.rows, q.cols) != which) continue;
+    j.job[n] = SmallJob{q.src, q.m, q.out, q.rows, q.cols, (float)(js.lr * q.scale)};
+    j.first[n++] = total;
+    total += q.count;
   }
-  if (!j.n_tensors) return hipSuccess;
+  if (!n) return hipSuccess;
+  for (int k = n; k < SAGIPS_MAX_TENSORS; ++k) j.first[k] = INT_MAX;
+  j.first[SAGIPS_MAX_TENSORS] = total;
   j.src_bf16 = js.src_bf16;
   j.out_bf16 = js.out_bf16;
   j.nesterov = js.nesterov;
@@ -818,31 +868,40 @@ static hipError_t launch_small(const MatrixJobs& js, int np, hipStream_t st, Tim
   j.b = js.coef[1];
   j.c = js.coef[2];
   j.eps = js.eps;
-  const dim3 grid(j.first[j.n_tensors]);
   if (tm) tm->begin("ns_small");
-  if (np == 32) hipLaunchKernelGGL((k_ns_small<32>), grid, dim3(kThreads), 0, st, j);
-  else if (np == 64) hipLaunchKernelGGL((k_ns_small<64>), grid, dim3(kThreads), 0, st, j);
-  else hipLaunchKernelGGL((k_ns_small<128>), grid, dim3(kThreads), 0, st, j);
+  switch (which) {
+    case 0: small_kernel<0, 0>(j, st); break;
+    case 1: small_kernel<0, 1>(j, st); break;
+    case 2: small_kernel<0, 2>(j, st); break;
+    case 3: small_kernel<1, 0>(j, st); break;
+    case 4: small_kernel<1, 1>(j, st); break;
+    case 5: small_kernel<1, 2>(j, st); break;
+    case 6: small_kernel<2, 0>(j, st); break;
+    case 7: small_kernel<2, 1>(j, st); break;
+    default: small_kernel<2, 2>(j, st); break;
+  }
   if (tm) tm->end();
   return hipGetLastError();
 }
 
 hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm) {
-  for (int np = 32; np <= 128; np *= 2) {
-    const hipError_t e = launch_small(js, np, st, tm);
+  for (int which = 0; which < kSmallClasses; ++which) {
+    const hipError_t e = launch_small(js, which, st, tm);
     if (e != hipSuccess) return e;
   }
   return for_each_shape(js, [&](const int* list, int n) {
     const Job& a = js.job[list[0]];
     Jobs j{};
-    j.n_tensors = n;
+    int total = 0;
     for (int k = 0; k < n; ++k) {
       const Job& q = js.job[list[k]];
       j.src[k] = q.src;
       j.m[k] = q.m;
       j.out[k] = q.out;
-      j.first[k + 1] = j.first[k] + q.count;
+      j.first[k] = total;
+      total += q.count;
     }
+    for (int k = n; k <= SAGIPS_MAX_TENSORS; ++k) j.first[k] = INT_MAX;
     j.rows = a.rows;
     j.cols = a.cols;
     j.src_bf16 = js.src_bf16;
@@ -855,7 +914,7 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm
     j.b = js.coef[1];
     j.c = js.coef[2];
     j.eps = js.eps;
-    const Plan p = plan_of(a.rows, a.cols, j.first[n]);
+    const Plan p = plan_of(a.rows, a.cols, total);
     char* w = static_cast<char*>(ws);
     return p.tile == 128 ? steps_of<128>(p, j, js.steps, w, st, tm) : steps_of<64>(p, j, js.steps, w, st, tm);
   });
