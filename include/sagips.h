@@ -423,7 +423,8 @@ sagips_status sagips_preference_loss(sagips_ctx* ctx, const sagips_preference* P
  * so the range of U does not matter) and multiplied with fp32 accumulation,
  * at or below the error of fp32 products.  `coef` all zero means
  * (3.4445, -4.7750, 2.0315), `steps` 0 means 5.  0 <= steps <= 16, eps > 0;
- * coefficients that let singular values grow beyond 64 from at most 1 are
+ * coefficients that let singular values grow beyond 3.9 from at most 1, or
+ * |b| s^2 + |c| s^4 beyond 15.9 for the largest of them s, are
  * SAGIPS_E_UNSUPPORTED.                                                     */
 typedef struct {
   int32_t steps;

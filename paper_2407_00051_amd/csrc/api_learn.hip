@@ -81,19 +81,20 @@ sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJo
   }
   js->steps = ns.steps ? ns.steps : 5;
   js->eps = ns.eps;
-  // The kernels hold X, X X^T and the polynomial of it in fp16 terms: no entry exceeds
-  // the largest singular value, which starts below 1 and is bounded step by step.
+  // The kernels hold 2^12 X, X X^T and the polynomial of it in fp16 terms, up to 15.9:
+  // no entry exceeds the largest singular value, which starts below 1 and is bounded step
+  // by step.
   const double a = js->coef[0], b = js->coef[1], k = js->coef[2];
   double most = 1.0;
   for (int i = 0; i < js->steps; ++i) {
     const double poly = fabs(b) * most * most + fabs(k) * most * most * most * most;
-    if (!(most <= 64.0) || !(poly <= 32768.0))
-      return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 64 within %d steps", a,
+    if (!(most <= 3.9) || !(poly <= 15.9))
+      return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 3.9 within %d steps", a,
                   b, k, i + 1);
     most = largest_value(a, b, k, most);
   }
-  if (!(most <= 64.0))
-    return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 64", a, b, k);
+  if (!(most <= 3.9))
+    return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 3.9", a, b, k);
   return SAGIPS_OK;
 }
 

@@ -4,18 +4,17 @@
 // side (n rows of L).  The steps drive every singular value of X towards one
 // band around 1 and keep its singular vectors.
 //
-// Every matrix is held as two fp16 terms, x = hi + 2^-11 lo with
-//   hi = fp16(x), lo = fp16(2^11 (x - hi)),
-// each rounded to nearest even: |x - hi| <= 2^-12 |x| and the rest is at most
-// 2^-24 |x|, half a unit in the last place of fp32 (while hi is not subnormal,
-// |x| above 6e-5; below, at most 2^-36).  Products of fp16 values are exact in
-// fp32, and of the four term products lo lo is at most 2^-24 |x y|, no more than
-// the rounding of one fp32 product.  Three products on the fp16 matrix cores,
-// hi hi into one fp32 accumulator and hi lo + lo hi into another that is scaled
-// at the end, therefore replace an fp32 product at 16/3 of the rate of the fp32
-// matrix instructions.  fp16 ends at 65,504: X, X X^T and the polynomial of it
-// stay below that because the singular values do (launch_muon's caller bounds
-// them from the coefficients).
+// Every matrix M (X, X X^T, the polynomial of it) is held as two fp16 terms of 2^12 M,
+//   2^12 m = hi + lo,  hi = fp16(2^12 m), lo = fp16(2^12 m - hi),
+// each rounded to nearest even: |2^12 m - hi| <= 2^-12 |2^12 m|, and the rest is at most
+// 2^-24 of it, half a unit in the last place of fp32, while lo is not subnormal (|m|
+// above 6e-5; below, at most 2^-37).  Products of fp16 values are exact in fp32, and of
+// the four term products lo lo is at most 2^-24 of the whole, no more than the rounding
+// of one fp32 product.  Three products on the fp16 matrix cores into one fp32
+// accumulator, smallest first, therefore replace an fp32 product at 16/3 of the rate of
+// the fp32 matrix instructions.  fp16 ends at 65,504, so entries must stay below 15.9:
+// they do because the singular values do (the entry points bound them from the
+// coefficients).
 #include <limits.h>
 
 #include "kernels.hpp"
@@ -26,7 +25,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kT = 2;                          // terms
-constexpr float kLo = 2048.0f, kInvLo = 1.0f / 2048.0f;
+constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -69,15 +68,12 @@ __device__ __forceinline__ double wave_sum_d(double v) {
   return v;
 }
 
-// The terms of two values, packed in pairs.  2^11 (x - hi) is exact in fp32.
-__device__ __forceinline__ uint32_t pk_f16(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), f16x2));
-}
+// The terms of scale a and scale b, packed in pairs; scale is a power of two.
 __device__ __forceinline__ float f16_lo(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }
 __device__ __forceinline__ float f16_hi(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[1]; }
-__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
-  const f16x2 h = __builtin_convertvector((f32x2{a, b}), f16x2);
-  const f16x2 l = {(_Float16)fmaf((float)h[0], -kLo, a * kLo), (_Float16)fmaf((float)h[1], -kLo, b * kLo)};
+__device__ __forceinline__ void split2(float a, float b, float scale, uint32_t& hi, uint32_t& lo) {
+  const f16x2 h = {(_Float16)(a * scale), (_Float16)(b * scale)};
+  const f16x2 l = {(_Float16)fmaf(a, scale, -(float)h[0]), (_Float16)fmaf(b, scale, -(float)h[1])};   // the fma is exact
   hi = __builtin_bit_cast(uint32_t, h);
   lo = __builtin_bit_cast(uint32_t, l);
 }
@@ -173,7 +169,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
     const int i = q >> 3, l = (q & 7) * 8;
     uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) split2(tile[i][l + 2 * h], tile[i][l + 2 * h + 1], hi[h], lo[h]);
+    for (int h = 0; h < 4; ++h) split2(tile[i][l + 2 * h], tile[i][l + 2 * h + 1], kScale, hi[h], lo[h]);
     u16* at = x + at_value(i0 + i, l0 + l, lp);
     *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     *reinterpret_cast<uint4*>(at + kTermSize) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -221,7 +217,7 @@ __device__ __forceinline__ bool tile_of(const GemmArgs& g, int& z, int& ti, int&
 }
 
 template <int kMode, int TI>
-__global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
+__global__ __launch_bounds__(kThreads, 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
   typedef Tile<TI> T;
   constexpr bool kDown = kMode == kApply || kMode == kStore;   // Q's K runs down its columns
   constexpr int WB = T::WB;
@@ -302,18 +298,14 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
       }
     }
   };
-  f32x16 c[WB][WB] = {}, d[WB][WB] = {};   // [block of j][block of i]: hi hi; hi lo + lo hi
+  f32x16 c[WB][WB] = {};                               // [block of j][block of i], 2^24 times the product
   const auto multiply = [&](const Frag& f) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 3; ++s)
 #pragma unroll
       for (int x = 0; x < WB; ++x)
 #pragma unroll
-        for (int y = 0; y < WB; ++y) {
-          if (s == 0) d[x][y] = mfma16(f.q[x][0], f.p[y][1], d[x][y]);
-          if (s == 1) c[x][y] = mfma16(f.q[x][0], f.p[y][0], c[x][y]);
-          if (s == 2) d[x][y] = mfma16(f.q[x][1], f.p[y][0], d[x][y]);
-        }
+        for (int y = 0; y < WB; ++y) c[x][y] = mfma16(f.q[x][s == 1], f.p[y][s == 0], c[x][y]);
   };
 
   // Stage k's second half reads the first operands of stage k + 1, whose pieces went
@@ -352,22 +344,24 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
         const int i = ti * TI + wi * (TI / 2) + y * 32 + lr, j = tj * TI + wj * (TI / 2) + x * 32 + 8 * s + 4 * lh;
+        // kGram: 2^24 times the result; otherwise 2^12 times
         float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(d[x][y][4 * s + e], kInvLo, c[x][y][4 * s + e]);
+        for (int e = 0; e < 4; ++e) v[e] = c[x][y][4 * s + e];
         if constexpr (kMode != kGram) {
           const u16* old = g.X + z * op + at_value(i, j, g.width);
-          const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = kMode == kPoly ? jobs.c : 1.0f;
+          const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = (kMode == kPoly ? jobs.c : 1.0f) * kInvScale;
           const uint2 h = *reinterpret_cast<const uint2*>(old), l = *reinterpret_cast<const uint2*>(old + kTermSize);
-          const float o[4] = {fmaf(f16_lo(l.x), kInvLo, f16_lo(h.x)), fmaf(f16_hi(l.x), kInvLo, f16_hi(h.x)),
-                              fmaf(f16_lo(l.y), kInvLo, f16_lo(h.y)), fmaf(f16_hi(l.y), kInvLo, f16_hi(h.y))};
+          const float o[4] = {f16_lo(l.x) + f16_lo(h.x), f16_hi(l.x) + f16_hi(h.x), f16_lo(l.y) + f16_lo(h.y),
+                              f16_hi(l.y) + f16_hi(h.y)};
 #pragma unroll
           for (int e = 0; e < 4; ++e) v[e] = fmaf(keep, o[e], mul * v[e]);
         }
         if constexpr (kMode != kStore) {
+          constexpr float scale = kMode == kGram ? kInvScale : 1.0f;
           uint2 h, l;
-          split2(v[0], v[1], h.x, l.x);
-          split2(v[2], v[3], h.y, l.y);
+          split2(v[0], v[1], scale, h.x, l.x);
+          split2(v[2], v[3], scale, h.y, l.y);
           u16* out = g.out + z * op + at_value(i, j, g.width);
           *reinterpret_cast<uint2*>(out) = h;
           *reinterpret_cast<uint2*>(out + kTermSize) = l;
@@ -379,13 +373,14 @@ __global__ __launch_bounds__(kThreads, TI == 128 ? 1 : 2) void k_ns_gemm(GemmArg
             const int r = flip ? j + e : i, cc = flip ? i : j + e;
             if (r >= jobs.rows || cc >= jobs.cols) continue;
             const int64_t at = base + (int64_t)r * jobs.cols + cc;
+            const float o = v[e] * kInvScale;
             if (jobs.m[t]) {
               float* w = static_cast<float*>(jobs.out[t]) + at;
-              *w = fmaf(-jobs.rate, v[e], jobs.decay * *w);
+              *w = fmaf(-jobs.rate, o, jobs.decay * *w);
             } else if (jobs.out_bf16) {
-              static_cast<u16*>(jobs.out[t])[at] = to_bf16(v[e]);
+              static_cast<u16*>(jobs.out[t])[at] = to_bf16(o);
             } else {
-              static_cast<float*>(jobs.out[t])[at] = v[e];
+              static_cast<float*>(jobs.out[t])[at] = o;
             }
           }
         }
@@ -426,121 +421,154 @@ struct SmallJobs {
 };
 
 constexpr int kSmallValues = 16384;                    // NP x LP
-constexpr int kSmallCopy = 128 * 129 * 4;              // the fp32 copy, rows one value longer if even; X's terms: 64 KB
+constexpr int kSmallBuffer = kSmallValues * kT * 2;    // X's terms, and Y's
+constexpr int kQuads = kSmallValues / 4 / kThreads;
 
-template <int NP, int JB>
-__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
-  constexpr int LP = kSmallValues / NP;
-  constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
-  constexpr int RB = 2 * LP, PL = NP * RB;             // bytes of a row of one term, of a term
-  constexpr int IP = NI > 1 ? 2 : 1, JP = JB > 1 ? 2 : 1;   // blocks multiplied at a time
-  __shared__ __attribute__((aligned(16))) char lds[kSmallCopy];
-  __shared__ float part[CW > 1 ? 4 : 1][NI * 16][64];  // the waves' sums for A
-  __shared__ double sums[kThreads / 64];
-  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
-  const int wave = threadIdx.x >> 6, rw = wave % RW, cw = wave / RW;
-  const int t = tensor_of(jobs.first, blockIdx.x);
-  const SmallJob job = jobs.job[t];
-  const int rows = job.rows, cols = job.cols, size = rows * cols;
-  const bool flip = rows > cols;
-  const int n = flip ? cols : rows, L = flip ? rows : cols;
-  const int64_t base = (int64_t)((int)blockIdx.x - jobs.first[t]) * size;
-  float* const flat = reinterpret_cast<float*>(lds);
-  const int pitch = cols | 1;
+// U of a small matrix into its fp32 copy, the momentum on the way; returns the
+// thread's sum of squares.  Quads (cols a multiple of 4) have every load in flight.
+template <bool kBf16, bool kMom>
+__device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJob& job, int64_t base, float* flat, int pitch) {
+  const int cols = job.cols, size = job.rows * cols;
   const float inv_cols = 1.0f / cols;
-  const bool quads = size % 4 == 0;                    // then every matrix of the stack is 16-byte aligned
-  float* const mom = job.m ? job.m + base : nullptr;
-  constexpr int kQuads = kSmallValues / 4 / kThreads;
-
-  // U into LDS, the momentum on the way, and its norm; every load in flight at once
+  const float* const f32 = static_cast<const float*>(job.src) + base;
+  const u16* const b16 = static_cast<const u16*>(job.src) + base;
+  float* const mom = kMom ? job.m + base : nullptr;
   double sq = 0.0;
-  if (quads) {
+  if (cols % 4 == 0) {
     f32x4 u[kQuads], m[kQuads];
 #pragma unroll
     for (int k = 0; k < kQuads; ++k) {
       const int e = (k * kThreads + threadIdx.x) * 4;
-      if (e >= size) continue;
-      if (jobs.src_bf16) {
-        const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const u16*>(job.src) + base + e);
-        u[k][0] = __uint_as_float(q.x);
-        u[k][1] = __uint_as_float(q.y);
+      if (e >= size) break;
+      if constexpr (kBf16) {
+        const uint2 q = *reinterpret_cast<const uint2*>(b16 + e);
+        u[k] = f32x4{bf16_lo(q.x), bf16_hi(q.x), bf16_lo(q.y), bf16_hi(q.y)};
       } else {
-        u[k] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(job.src) + base + e);
+        u[k] = *reinterpret_cast<const f32x4*>(f32 + e);
       }
-      if (mom) m[k] = *reinterpret_cast<const f32x4*>(mom + e);
+      if constexpr (kMom) m[k] = *reinterpret_cast<const f32x4*>(mom + e);
     }
 #pragma unroll
     for (int k = 0; k < kQuads; ++k) {
       const int e = (k * kThreads + threadIdx.x) * 4;
-      if (e >= size) continue;
+      if (e >= size) break;
       f32x4 v = u[k];
-      if (jobs.src_bf16) {
-        const uint32_t q0 = __float_as_uint(u[k][0]), q1 = __float_as_uint(u[k][1]);
-        v = f32x4{bf16_lo(q0), bf16_hi(q0), bf16_lo(q1), bf16_hi(q1)};
-      }
-      if (mom) {
-        f32x4 w;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          w[q] = fmaf(jobs.momentum, m[k][q], v[q]);
-          v[q] = jobs.nesterov ? fmaf(jobs.momentum, w[q], v[q]) : w[q];
-        }
+      if constexpr (kMom) {
+        const f32x4 w = jobs.momentum * m[k] + v;
         *reinterpret_cast<f32x4*>(mom + e) = w;
+        v = jobs.nesterov ? jobs.momentum * w + v : w;
       }
-      int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;   // e < 2^14: exact
+      const int r = (int)((e + 0.5f) * inv_cols);      // e < 2^14: exact
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         sq = fma((double)v[q], (double)v[q], sq);
-        flat[r * pitch + c] = v[q];
-        if (++c == cols) {
-          c = 0;
-          ++r;
-        }
+        flat[r * (pitch - cols) + e + q] = v[q];
       }
     }
   } else {
 #pragma unroll 4
     for (int e = threadIdx.x; e < size; e += kThreads) {
       const int r = (int)((e + 0.5f) * inv_cols);
-      float u = load_src(job.src, base + e, jobs.src_bf16);
-      if (mom) {
+      float u = kBf16 ? bf16_lo(b16[e]) : f32[e];
+      if constexpr (kMom) {
         const float w = fmaf(jobs.momentum, mom[e], u);
         mom[e] = w;
         u = jobs.nesterov ? fmaf(jobs.momentum, w, u) : w;
       }
       sq = fma((double)u, (double)u, sq);
-      flat[r * pitch + e - r * cols] = u;
+      flat[r * (pitch - cols) + e] = u;
     }
   }
+  return sq;
+}
+
+// The result from the fp32 copy: parameters moved, or the matrix written.
+template <bool kBf16, bool kMom>
+__device__ __forceinline__ void small_store(const SmallJobs& jobs, const SmallJob& job, int64_t base, const float* flat, int pitch) {
+  const int cols = job.cols, size = job.rows * cols;
+  const float inv_cols = 1.0f / cols;
+  float* const f32 = static_cast<float*>(job.out) + base;
+  u16* const b16 = static_cast<u16*>(job.out) + base;
+  if (cols % 4 == 0) {
+    f32x4 old[kQuads];
+    if constexpr (kMom)
+#pragma unroll
+      for (int k = 0; k < kQuads; ++k) {
+        const int e = (k * kThreads + threadIdx.x) * 4;
+        if (e >= size) break;
+        old[k] = *reinterpret_cast<const f32x4*>(f32 + e);
+      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kQuads; ++k) {
+      const int e = (k * kThreads + threadIdx.x) * 4;
+      if (e >= size) break;
+      const int r = (int)((e + 0.5f) * inv_cols);
+      f32x4 v;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = flat[r * (pitch - cols) + e + q];
+      if constexpr (kMom) *reinterpret_cast<f32x4*>(f32 + e) = jobs.decay * old[k] - job.rate * v;
+      else if constexpr (kBf16) *reinterpret_cast<uint2*>(b16 + e) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
+      else *reinterpret_cast<f32x4*>(f32 + e) = v;
+    }
+  } else {
+    __syncthreads();
+#pragma unroll 4
+    for (int e = threadIdx.x; e < size; e += kThreads) {
+      const int r = (int)((e + 0.5f) * inv_cols);
+      const float v = flat[r * (pitch - cols) + e];
+      if constexpr (kMom) f32[e] = fmaf(-job.rate, v, jobs.decay * f32[e]);
+      else if constexpr (kBf16) b16[e] = to_bf16(v);
+      else f32[e] = v;
+    }
+  }
+}
+
+template <int NP, int JB>
+__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
+  constexpr int LP = kSmallValues / NP;
+  constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
+  constexpr int RB = 2 * LP, PL = NP * RB;             // bytes of a row of one term, of a term
+  constexpr int IK = 4 / NI, JK = 4 / JB;              // accumulators a block, so that four products run side by side
+  // X's terms, then Y's; before the first and after the last step the fp32 copy (rows
+  // one value longer if even: 66 KB at most); Y's part also takes the waves' sums for A
+  __shared__ __attribute__((aligned(16))) char lds[2 * kSmallBuffer];
+  __shared__ double sums[kThreads / 64];
+  char* const ldsX = lds;
+  char* const ldsY = lds + kSmallBuffer;
+  float* const flat = reinterpret_cast<float*>(lds);
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int wave = threadIdx.x >> 6, rw = wave % RW, cw = wave / RW;
+  const int t = tensor_of(jobs.first, blockIdx.x);
+  const SmallJob job = jobs.job[t];
+  const int rows = job.rows, cols = job.cols;
+  const bool flip = rows > cols;
+  const int n = flip ? cols : rows, L = flip ? rows : cols;
+  const int64_t base = (int64_t)((int)blockIdx.x - jobs.first[t]) * rows * cols;
+  const int pitch = cols | 1;
+
+  double sq;
+  if (job.m) sq = jobs.src_bf16 ? small_load<true, true>(jobs, job, base, flat, pitch) : small_load<false, true>(jobs, job, base, flat, pitch);
+  else sq = jobs.src_bf16 ? small_load<true, false>(jobs, job, base, flat, pitch) : small_load<false, false>(jobs, job, base, flat, pitch);
   sq = wave_sum_d(sq);
   if (lane == 0) sums[wave] = sq;
   __syncthreads();
   const float inv = (float)(1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + jobs.eps));
 
-  const int i = 32 * rw + lr;
-  const int pi = flip ? 1 : pitch, pj = flip ? pitch : 1;   // X's (i, j) in the fp32 copy: i pi + j pj
-  f32x16 x[JB];
-#pragma unroll
-  for (int b = 0; b < JB; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      x[b][r] = i < n && j < L ? flat[i * pi + j * pj] * inv : 0.0f;
-    }
-  __syncthreads();
-
+  float one = 1.0f;                                    // not a constant to the compiler: a multiplication by it lets
+  asm("" : "+s"(one));                                 // fp16 operands go straight into an fp32 fma
   // Terms of 16 values, two units of 8.
   struct Terms {
     f16x8 v[2][kT];
   };
-  const auto split = [](const f32x16& v, Terms& o) __attribute__((always_inline)) {
+  const auto split = [](const f32x16& v, float scale, Terms& o) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       u32x4 h, l;
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         uint32_t a, c;
-        split2(v[8 * s + 2 * q], v[8 * s + 2 * q + 1], a, c);
+        split2(v[8 * s + 2 * q], v[8 * s + 2 * q + 1], scale, a, c);
         h[q] = a;
         l[q] = c;
       }
@@ -549,80 +577,107 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
     }
   };
   const auto swz = [](int f) { return (uint32_t)(2 * (f & 3) + ((f >> 2) & 1)); };
+  const int i = 32 * rw + lr;
   const uint32_t own = i * RB, own_swz = swz(i);       // rows 32 ib + lr: the same swizzle
-  const auto put = [&](int b, const Terms& o) __attribute__((always_inline)) {
+  const auto put = [&](char* buf, int b, const Terms& o) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      char* at = lds + own + (((4 * (b * CW + cw) + 2 * s + lh) ^ own_swz) << 4);
+      char* at = buf + own + (((4 * (b * CW + cw) + 2 * s + lh) ^ own_swz) << 4);
       *reinterpret_cast<f16x8*>(at) = o.v[s][0];
       *reinterpret_cast<f16x8*>(at + PL) = o.v[s][1];
     }
   };
-  // JP blocks of A times what LDS holds.
-  const int i16 = lane & 15, half = (lane >> 4) & 1;
-  const uint32_t row0 = 4 * lh + (i16 >> 2), swz0 = swz(row0);   // rows 32 ib + 16 s (+ 8) + row0: the same swizzle
-  const auto times = [&](const Terms (&A)[NI], int b0, f32x16 (&v)[JP]) __attribute__((always_inline)) {
-    f32x16 c[JP] = {}, d[JP] = {};
-#pragma unroll
-    for (int ib = 0; ib < NI; ++ib)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        f16x8 q[JP][kT];
-#pragma unroll
-        for (int y = 0; y < JP; ++y) {
-          const int unit = 4 * ((b0 + y) * CW + cw) + 2 * half + (i16 & 1);
-          const char* p = lds + (32 * ib + 16 * s + row0) * RB + ((unit ^ swz0) << 4) + 8 * (i16 >> 1 & 1);
-#pragma unroll
-          for (int w = 0; w < kT; ++w) q[y][w] = lds_col2(p + w * PL, p + w * PL + 8 * RB);
-        }
-#pragma unroll
-        for (int y = 0; y < JP; ++y) d[y] = mfma16(q[y][0], A[ib].v[s][1], d[y]);
-#pragma unroll
-        for (int y = 0; y < JP; ++y) c[y] = mfma16(q[y][0], A[ib].v[s][0], c[y]);
-#pragma unroll
-        for (int y = 0; y < JP; ++y) d[y] = mfma16(q[y][1], A[ib].v[s][0], d[y]);
-      }
-#pragma unroll
-    for (int y = 0; y < JP; ++y) v[y] = c[y] + d[y] * kInvLo;
-  };
 
   Terms xt[JB];
+  {
+    const int pi = flip ? 1 : pitch, pj = flip ? pitch : 1;   // X's (i, j) in the fp32 copy: i pi + j pj
 #pragma unroll
-  for (int b = 0; b < JB; ++b) {
-    split(x[b], xt[b]);
-    put(b, xt[b]);
+    for (int b = 0; b < JB; ++b) {
+      f32x16 x;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
+        x[r] = i < n && j < L ? flat[i * pi + j * pj] * inv : 0.0f;
+      }
+      split(x, kScale, xt[b]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < JB; ++b) put(ldsX, b, xt[b]);
   }
-  for (int step = 0; step < jobs.steps; ++step) {
-    lds_barrier();
-    Terms A[NI];
+
+  // A times the wave's blocks of what buf holds; done(b, 2^24 times that of block b).
+  const int i16 = lane & 15, half = (lane >> 4) & 1;
+  const uint32_t row0 = 4 * lh + (i16 >> 2), swz0 = swz(row0);   // rows 32 ib + 16 s (+ 8) + row0: the same swizzle
+  const auto times = [&](const char* buf, const Terms (&A)[NI], auto done) __attribute__((always_inline)) {
+    constexpr int kSteps = NI * 2;                     // along K
+    f16x8 q[2][JB][kT];
+    const auto read = [&](int ks, int y) __attribute__((always_inline)) {   // 16 rows 16 ks .. of block y
+      const int unit = 4 * (y * CW + cw) + 2 * half + (i16 & 1);
+      const char* p = buf + (16 * ks + row0) * RB + ((unit ^ swz0) << 4) + 8 * (i16 >> 1 & 1);
 #pragma unroll
-    for (int i0 = 0; i0 < NI; i0 += IP) {
-      f32x16 c[IP] = {}, d[IP] = {};
+      for (int w = 0; w < kT; ++w) q[ks & 1][y][w] = lds_col2(p + w * PL, p + w * PL + 8 * RB);
+    };
 #pragma unroll
-      for (int b = 0; b < JB; ++b)
+    for (int y = 0; y < JB; ++y) read(0, y);
+    f32x16 c[JB][JK] = {};
+    // a step's first products each with the reads of a block of the next step behind it, in this order
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          f16x8 q[IP][kT];
+    for (int ks = 0; ks < kSteps; ++ks)
 #pragma unroll
-          for (int y = 0; y < IP; ++y)
+      for (int s = 0; s < 3; ++s)
 #pragma unroll
-            for (int w = 0; w < kT; ++w)
-              q[y][w] = lds_row(lds + w * PL + (32 * (i0 + y) + lr) * RB + (((4 * (b * CW + cw) + 2 * s + lh) ^ own_swz) << 4));
-#pragma unroll
-          for (int y = 0; y < IP; ++y) d[y] = mfma16(q[y][0], xt[b].v[s][1], d[y]);
-#pragma unroll
-          for (int y = 0; y < IP; ++y) c[y] = mfma16(q[y][0], xt[b].v[s][0], c[y]);
-#pragma unroll
-          for (int y = 0; y < IP; ++y) d[y] = mfma16(q[y][1], xt[b].v[s][0], d[y]);
+        for (int y = 0; y < JB; ++y) {
+          f32x16& o = c[y][(3 * ks + s) % JK];
+          o = mfma16(q[ks & 1][y][s == 1], A[ks / 2].v[ks % 2][s == 0], o);
+          if (s == 0 && ks + 1 < kSteps) read(ks + 1, y);
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-      for (int y = 0; y < IP; ++y) {
-        const f32x16 v = c[y] + d[y] * kInvLo;
-        if constexpr (CW == 1) {
-          split(v, A[i0 + y]);
-        } else {
+    for (int y = 0; y < JB; ++y) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) part[wave][(i0 + y) * 16 + r][lane] = v[r];
+      for (int k = 1; k < JK; ++k) c[y][0] += c[y][k];
+      done(y, c[y][0]);
+    }
+  };
+
+  f32x16 x[JB];                                        // 2^12 times X
+  for (int step = 0; step < jobs.steps; ++step) {
+    lds_barrier();                                     // X is there, Y has been read
+    Terms A[NI];
+    {
+      constexpr int kSteps = JB * 2;
+      f16x8 q[2][NI][kT];
+      const auto read = [&](int ks, int y) __attribute__((always_inline)) {
+#pragma unroll
+        for (int w = 0; w < kT; ++w)
+          q[ks & 1][y][w] =
+              lds_row(ldsX + w * PL + (32 * y + lr) * RB + (((4 * (ks / 2 * CW + cw) + 2 * (ks % 2) + lh) ^ own_swz) << 4));
+      };
+#pragma unroll
+      for (int y = 0; y < NI; ++y) read(0, y);
+      f32x16 c[NI][IK] = {};
+#pragma unroll
+      for (int ks = 0; ks < kSteps; ++ks)
+#pragma unroll
+        for (int s = 0; s < 3; ++s)
+#pragma unroll
+          for (int y = 0; y < NI; ++y) {
+            f32x16& v = c[y][(3 * ks + s) % IK];
+            v = mfma16(q[ks & 1][y][s == 1], xt[ks / 2].v[ks % 2][s == 0], v);
+            if (s == 0 && ks + 1 < kSteps) read(ks + 1, y);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+#pragma unroll
+      for (int y = 0; y < NI; ++y) {
+#pragma unroll
+        for (int k = 1; k < IK; ++k) c[y][0] += c[y][k];
+        if constexpr (CW == 1) {
+          split(c[y][0], kInvScale, A[y]);
+        } else {
+          float* part = reinterpret_cast<float*>(ldsY) + (wave * NI + y) * 16 * 64 + lane;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) part[r * 64] = c[y][0][r];
         }
       }
     }
@@ -632,96 +687,43 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
       for (int ib = 0; ib < NI; ++ib) {
         f32x16 v = {};
 #pragma unroll
-        for (int w = 0; w < CW; ++w)                   // the same order in every wave
+        for (int w = 0; w < CW; ++w) {                 // the same order in every wave
+          const float* part = reinterpret_cast<const float*>(ldsY) + ((w * RW + rw) * NI + ib) * 16 * 64 + lane;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) v[r] += part[w * RW + rw][ib * 16 + r][lane];
-        split(v, A[ib]);
+          for (int r = 0; r < 16; ++r) v[r] += part[r * 64];
+        }
+        split(v, kInvScale, A[ib]);
       }
+      lds_barrier();
     }
+    times(ldsX, A, [&](int b, const f32x16& y) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b0 = 0; b0 < JB; b0 += JP) {
-      f32x16 v[JP];
-      times(A, b0, v);
-#pragma unroll
-      for (int y = 0; y < JP; ++y) {
-        split(v[y], xt[b0 + y]);
-        x[b0 + y] = jobs.a * x[b0 + y] + jobs.b * v[y];
-      }
-    }
-    lds_barrier();                                     // X has been read
-#pragma unroll
-    for (int b = 0; b < JB; ++b) put(b, xt[b]);
-    lds_barrier();
-#pragma unroll
-    for (int b0 = 0; b0 < JB; b0 += JP) {
-      f32x16 v[JP];
-      times(A, b0, v);
-#pragma unroll
-      for (int y = 0; y < JP; ++y) {
-        x[b0 + y] += jobs.c * v[y];
-        split(x[b0 + y], xt[b0 + y]);
-      }
-    }
-    lds_barrier();                                     // Y has been read
-    if (step + 1 < jobs.steps)
-#pragma unroll
-      for (int b = 0; b < JB; ++b) put(b, xt[b]);
+      for (int r = 0; r < 16; ++r)                     // 2^12 X from its terms: exact
+        x[b][r] = fmaf(jobs.b * kInvScale, y[r], jobs.a * fmaf((float)xt[b].v[r / 8][0][r % 8], one, (float)xt[b].v[r / 8][1][r % 8]));
+      split(y, kInvScale, xt[b]);
+      put(ldsY, b, xt[b]);
+    });
+    lds_barrier();                                     // Y is there, X has been read
+    times(ldsY, A, [&](int b, const f32x16& y) __attribute__((always_inline)) {
+      x[b] += (jobs.c * kInvScale) * y;
+      split(x[b], one, xt[b]);
+      put(ldsX, b, xt[b]);
+    });
   }
 
   // the result through the fp32 copy, so that the parameters are read and written in order
-  f32x4 old[kQuads];
-  if (quads && mom)
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int e = (k * kThreads + threadIdx.x) * 4;
-      if (e < size) old[k] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(job.out) + base + e);
-    }
+  lds_barrier();
+  const int pi = flip ? 1 : pitch, pj = flip ? pitch : 1;
 #pragma unroll
   for (int b = 0; b < JB; ++b)
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      if (i < n && j < L) flat[i * pi + j * pj] = x[b][r];
+      if (i < n && j < L) flat[i * pi + j * pj] = x[b][r] * kInvScale;
     }
-  __syncthreads();
-  if (quads) {
-#pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int e = (k * kThreads + threadIdx.x) * 4;
-      if (e >= size) continue;
-      f32x4 v;
-      int r = (int)((e + 0.5f) * inv_cols), c = e - r * cols;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        v[q] = flat[r * pitch + c];
-        if (++c == cols) {
-          c = 0;
-          ++r;
-        }
-      }
-      if (mom) {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(job.out) + base + e) = jobs.decay * old[k] - job.rate * v;
-      } else if (jobs.out_bf16) {
-        *reinterpret_cast<uint2*>(static_cast<u16*>(job.out) + base + e) = make_uint2(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]));
-      } else {
-        *reinterpret_cast<f32x4*>(static_cast<float*>(job.out) + base + e) = v;
-      }
-    }
-  } else {
-#pragma unroll 4
-    for (int e = threadIdx.x; e < size; e += kThreads) {
-      const int r = (int)((e + 0.5f) * inv_cols);
-      const float v = flat[r * pitch + e - r * cols];
-      if (mom) {
-        float* w = static_cast<float*>(job.out) + base + e;
-        *w = fmaf(-job.rate, v, jobs.decay * *w);
-      } else if (jobs.out_bf16) {
-        static_cast<u16*>(job.out)[base + e] = to_bf16(v);
-      } else {
-        static_cast<float*>(job.out)[base + e] = v;
-      }
-    }
-  }
+  if (job.m) small_store<false, true>(jobs, job, base, flat, pitch);
+  else if (jobs.out_bf16) small_store<true, false>(jobs, job, base, flat, pitch);
+  else small_store<false, false>(jobs, job, base, flat, pitch);
 }
 
 // The workgroup that holds a matrix, as 3 (log2 NP - 5) + log2 JB; -1: none does.
