@@ -128,21 +128,19 @@ __device__ __forceinline__ float inverse_norm(const double* __restrict__ part, i
   return (float)(1.0 / (sqrt(w[0] + w[1] + w[2] + w[3]) + eps));
 }
 
-// Layout of a matrix of np x width values (both multiples of 64) in the workspace:
-// blocks of 64 rows x 32 columns, row-major, each block its hi terms and then its lo
-// terms.  A stage of a product (32 along K) is then whole blocks or half blocks,
-// contiguous, whichever way K runs; in plain rows the pieces of a stage lie a power
-// of two apart and meet in one memory channel (2,048 x 2,048: 182 us a product so,
-// against 41 us of matrix instructions).
-constexpr int kBlockRows = 64, kBlockCols = 32, kTermSize = kBlockRows * kBlockCols, kBlockSize = kT * kTermSize;
-__device__ __forceinline__ int64_t at_value(int i, int j, int width) {   // of the hi term; lo: kTermSize further
-  return ((int64_t)(i / kBlockRows) * (width / kBlockCols) + j / kBlockCols) * kBlockSize + (i % kBlockRows) * kBlockCols +
-         j % kBlockCols;
-}
+// Layout of an operand of R rows and K columns (K runs along them) in the workspace:
+// fragments of 32 rows x 16 columns in the order in which a wave holds them for a
+// 32 x 32 x 16 product, [R / 32][K / 16][term][64 lanes][8 values].  Lane lr + 32 h has
+// row lr and columns 4 h + 0..3 and 8 + 4 h + 0..3: any order along K serves as long as
+// both operands keep it, and this one is that in which accumulators hold a row.  A
+// fragment is one contiguous kilobyte and goes from memory straight into registers.
+constexpr int kFrag = 512;                             // values of a fragment's term
+__device__ __forceinline__ int64_t frag_at(int rb, int ks, int K) { return ((int64_t)rb * (K / 16) + ks) * (kT * kFrag); }
 
-// X's terms, zero beyond n x L, in tiles of 64 x 64.
+// X's terms, zero beyond n x L, in tiles of 64 x 64: XR with K along X's rows, XC with
+// K down its columns.
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
-                                                       u16* __restrict__ X, int np, int lp) {
+                                                       u16* __restrict__ XR, u16* __restrict__ XC, int np, int lp) {
   __shared__ float tile[64][65];
   const int z = blockIdx.z, t = tensor_of(j.first, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
   const bool flip = j.rows > j.cols;
@@ -163,228 +161,221 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
     else tile[r][c] = u * inv;
   }
   __syncthreads();
-  u16* x = X + (int64_t)z * kT * np * lp;
+  const int64_t size = (int64_t)kT * np * lp;
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
 #pragma unroll
-  for (int q = threadIdx.x; q < 512; q += kThreads) {   // 8 values of a row
-    const int i = q >> 3, l = (q & 7) * 8;
+  for (int q = threadIdx.x >> 6; q < 16; q += kThreads / 64) {   // 8 fragments of either kind
+    const bool down = q >= 8;
+    const int rb = (q >> 2) & 1, ks = q & 3;
     uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) split2(tile[i][l + 2 * h], tile[i][l + 2 * h + 1], kScale, hi[h], lo[h]);
-    u16* at = x + at_value(i0 + i, l0 + l, lp);
+    for (int h = 0; h < 4; ++h) {
+      const int row = 32 * rb + lr, k = 16 * ks + 8 * (h >> 1) + 4 * lh + 2 * (h & 1);
+      split2(down ? tile[k][row] : tile[row][k], down ? tile[k + 1][row] : tile[row][k + 1], kScale, hi[h], lo[h]);
+    }
+    u16* at = (down ? XC : XR) + z * size + lane * 8 +
+              (down ? frag_at(l0 / 32 + rb, i0 / 16 + ks, np) : frag_at(i0 / 32 + rb, l0 / 16 + ks, lp));
     *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4*>(at + kTermSize) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    *reinterpret_cast<uint4*>(at + kFrag) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
 // ---- products -----------------------------------------------------------------------
+// One tile of 32 TB x 32 TB of P Q^T in a workgroup whose four waves each take a quarter
+// of K: every wave multiplies the whole tile, from fragments that it alone reads and
+// that go from memory straight into registers, kDepth steps of 16 ahead.  The loop has no
+// LDS traffic and no barrier (the same tile with operands shared through LDS was bound by
+// LDS: 61 us a product at 2,048 x 2,048, of which 21 are matrix instructions).  The
+// quarters are added through LDS at the end, each wave keeping a quarter of the tile.
 enum Mode { kGram, kPoly, kApply, kStore };
 
 struct GemmArgs {
-  const u16* P;      // [matrices][np x kp]: rows i of the result, K along a row
-  const u16* Q;      // kGram, kPoly: rows j of the result, K along a row; otherwise [kp x width]: K down a column
-  const u16* X;      // kApply, kStore: X, as Q; kPoly: P
-  u16* out;          // [matrices][np x width]
-  int np, kp, width; // padded sizes
-  int tiles_i, tiles_j, tiles, per_xcd;   // of all matrices together
+  const u16* P;      // [matrices] operands of np rows: rows i of the result
+  const u16* Q;      // [matrices] operands of `width` rows: columns j of the result
+  const u16* old;    // kPoly: P;  kApply, kStore: X with K along its rows
+  u16* out;          // the result with K along its rows
+  u16* outT;         // kApply: the same with K down its columns
+  int np, kp, width; // rows, K, columns
+  int tiles_i, tiles_j, per_mat, tiles, per_xcd;   // per_mat: tiles of a matrix; tiles: of all
 };
 
-// One TI x TI tile of the result, 4 waves of (TI / 2)^2.  K in stages of 32 through
-// two LDS buffers.
-template <int TI>
-struct Tile {
-  static constexpr int KB = 32;
-  static constexpr int ROWB = 2 * KB;                  // bytes of an operand row along K
-  static constexpr int PT = TI * ROWB;                 // bytes of one term of an operand tile
-  static constexpr int BUF = 2 * kT * PT;              // both operands
-  static constexpr int LOADS = BUF / 16 / kThreads;    // 16-byte loads a thread
-  static constexpr int WB = TI / 64;                   // 32-blocks a wave has in each direction
-};
-
-// Tile of a workgroup.  Workgroups go to the 8 XCDs in turn; each XCD gets a
-// contiguous run of tiles, and within a matrix the tiles run through groups of four
-// tile rows, so that the run's operands (4 x 8 tiles of 128: 6 MB at 2,048) are
+// Tile of a workgroup.  Workgroups go to the 8 XCDs in turn; each XCD gets a contiguous
+// run of tiles.  Of a symmetric result only tiles ti >= tj are formed; otherwise a
+// matrix's tiles run through groups of four tile rows, so that the run's operands are
 // shared in the XCD's L2.
+template <bool kSym>
 __device__ __forceinline__ bool tile_of(const GemmArgs& g, int& z, int& ti, int& tj) {
   const int id = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);
   if (id >= g.tiles) return false;
-  const int per = g.tiles_i * g.tiles_j;
-  z = id / per;
-  const int t = id - z * per, group = t / (4 * g.tiles_j), i0 = group * 4, rows = min(4, g.tiles_i - i0);
-  const int r = t - i0 * g.tiles_j;
-  ti = i0 + r % rows;
-  tj = r / rows;
+  z = id / g.per_mat;
+  const int t = id - z * g.per_mat;
+  if constexpr (kSym) {
+    ti = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+    while (ti * (ti + 1) / 2 > t) --ti;
+    tj = t - ti * (ti + 1) / 2;
+  } else {
+    const int group = t / (4 * g.tiles_j), i0 = group * 4, rows = min(4, g.tiles_i - i0), r = t - i0 * g.tiles_j;
+    ti = i0 + r % rows;
+    tj = r / rows;
+  }
   return true;
 }
 
-template <int kMode, int TI>
-__global__ __launch_bounds__(kThreads, 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
-  typedef Tile<TI> T;
-  constexpr bool kDown = kMode == kApply || kMode == kStore;   // Q's K runs down its columns
-  constexpr int WB = T::WB;
-  __shared__ __attribute__((aligned(16))) char lds[2][T::BUF];
-  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
-  const int wave = threadIdx.x >> 6, wi = wave & 1, wj = wave >> 1;
-  int z, ti, tj;
-  if (!tile_of(g, z, ti, tj)) return;
-  const int64_t pp = (int64_t)kT * g.np * g.kp, qp = (int64_t)kT * g.kp * g.width, op = (int64_t)kT * g.np * g.width;
-
-  // A thread's 16-byte pieces of a stage.  K along a row: piece (term, row, unit u of
-  // 4), kept at unit u ^ (row / 2 % 4), so that 8 lanes (rows) of a read hit distinct
-  // banks.  K down a column: piece (block of 32 columns, term, k, unit u of 4), whose
-  // half u / 2 is kept at u / 2 ^ (k / 2 % 2), so that the 4 rows of a transposed
-  // read do.
-  const u16* from[T::LOADS];
-  uint32_t to[T::LOADS];
+// 16 values of a row of a 32 x 32 block (as accumulators hold them) as terms: the
+// fragments of two K steps.
+__device__ __forceinline__ void write_block(u16* at, const f32x16& v, float scale) {
 #pragma unroll
-  for (int n = 0; n < T::LOADS; ++n) {
-    const bool isQ = n >= T::LOADS / 2;
-    const int m = isQ ? n - T::LOADS / 2 : n;
-    if (!isQ || !kDown) {
-      const int rb = m / 2, term = m % 2, row = rb * kBlockRows + (threadIdx.x >> 2), u = threadIdx.x & 3;
-      from[n] = (isQ ? g.Q + z * qp : g.P + z * pp) +
-                (int64_t)((isQ ? tj : ti) * (TI / kBlockRows) + rb) * (g.kp / kBlockCols) * kBlockSize + term * kTermSize +
-                threadIdx.x * 8;
-      to[n] = ((isQ ? kT : 0) + term) * T::PT + row * T::ROWB + ((u ^ ((row >> 1) & 3)) << 4);
-    } else {
-      const int term = threadIdx.x >> 7, r = threadIdx.x & 127, k = r >> 2, u = r & 3;
-      from[n] = g.Q + z * qp + (int64_t)(tj * (TI / kBlockCols) + m) * kBlockSize + term * kTermSize + r * 8;
-      to[n] = (kT + term) * T::PT + m * (T::KB * 64) + k * 64 + ((((u >> 1) ^ ((k >> 1) & 1)) << 1 | (u & 1)) << 4);
+  for (int s = 0; s < 2; ++s) {
+    u32x4 h, l;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t a, b;
+      split2(v[8 * s + 2 * q], v[8 * s + 2 * q + 1], scale, a, b);
+      h[q] = a;
+      l[q] = b;
     }
+    *reinterpret_cast<u32x4*>(at + s * kT * kFrag) = h;
+    *reinterpret_cast<u32x4*>(at + s * kT * kFrag + kFrag) = l;
   }
-  u32x4 hold0[T::LOADS], hold1[T::LOADS];
-  const int stages = g.kp / T::KB;                     // even: kp is a multiple of 64
-  // past the end: the last stage again, into a buffer that is not read any more
-  const auto fetch = [&](int k, u32x4 (&h)[T::LOADS]) __attribute__((always_inline)) {
-    k = min(k, stages - 1);
-    const int64_t along = (int64_t)k * kBlockSize;
-    const int64_t down = (int64_t)(k >> 1) * (g.width / kBlockCols) * kBlockSize + (k & 1) * (T::KB * kBlockCols);
-#pragma unroll
-    for (int n = 0; n < T::LOADS; ++n)
-      h[n] = *reinterpret_cast<const u32x4*>(from[n] + (kDown && n >= T::LOADS / 2 ? down : along));
+}
+
+template <int kMode, int TB>
+__global__ __launch_bounds__(kThreads, TB == 4 ? 1 : 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
+  constexpr bool kSym = kMode == kGram || kMode == kPoly;
+  constexpr int kDepth = TB == 4 ? 3 : 4;
+  constexpr int OB = TB * TB / 4;                      // blocks a wave keeps: x TB + y in [wave OB, wave OB + OB)
+  constexpr int PB = OB > 2 ? 2 : OB;                  // of them added at a time
+  __shared__ __attribute__((aligned(16))) f32x4 sums[4][4][PB][4][64];   // [from][to][block][quad of values][lane]
+  const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int z, ti, tj;
+  if (!tile_of<kSym>(g, z, ti, tj)) return;
+  const int64_t pp = (int64_t)kT * g.np * g.kp, qp = (int64_t)kT * g.width * g.kp, op = (int64_t)kT * g.np * g.width;
+  const u16* P = g.P + z * pp + frag_at(ti * TB, wave, g.kp) + lane * 8;
+  const u16* Q = g.Q + z * qp + frag_at(tj * TB, wave, g.kp) + lane * 8;
+  const int64_t row = frag_at(1, 0, g.kp);             // from one block of 32 rows to the next
+  const int steps = g.kp / 64;                         // of this wave: every fourth
+
+  struct Frags {
+    f16x8 p[TB][kT], q[TB][kT];
   };
-  const auto put = [&](char* buf, const u32x4 (&h)[T::LOADS]) __attribute__((always_inline)) {
+  Frags f[kDepth];
+  f32x16 c[TB][TB] = {};                               // [block of j][block of i], 2^24 times the product
+  const auto fetch = [&](int k, Frags& o) __attribute__((always_inline)) {
+    const int64_t at = (int64_t)min(k, steps - 1) * (4 * kT * kFrag);
 #pragma unroll
-    for (int n = 0; n < T::LOADS; ++n) *reinterpret_cast<u32x4*>(buf + to[n]) = h[n];
-  };
-  // A K step's operands: of 16 along K a lane half has 8.
-  struct Frag {
-    f16x8 p[WB][kT], q[WB][kT];
-  };
-  const auto read = [&](const char* buf, int ks, Frag& f) __attribute__((always_inline)) {
+    for (int b = 0; b < TB; ++b)
 #pragma unroll
-    for (int y = 0; y < WB; ++y) {
-      const int row = wi * (TI / 2) + y * 32 + lr;
-      const uint32_t at = row * T::ROWB + (((2 * ks + lh) ^ ((row >> 1) & 3)) << 4);
-#pragma unroll
-      for (int t = 0; t < kT; ++t) f.p[y][t] = lds_row(buf + t * T::PT + at);
-    }
-#pragma unroll
-    for (int x = 0; x < WB; ++x) {
-      if constexpr (!kDown) {
-        const int row = wj * (TI / 2) + x * 32 + lr;
-        const uint32_t at = row * T::ROWB + (((2 * ks + lh) ^ ((row >> 1) & 3)) << 4);
-#pragma unroll
-        for (int t = 0; t < kT; ++t) f.q[x][t] = lds_row(buf + (kT + t) * T::PT + at);
-      } else {
-        // 16 lanes read 4 rows of 16 values and get a column of 4 each
-        const int i = lane & 15, half = (lane >> 4) & 1;
-        const int k0 = 16 * ks + 8 * lh + (i >> 2);    // and k0 + 4: the same k / 2 % 2
-        const uint32_t at = (wj * (TI / 64) + x) * (T::KB * 64) + k0 * 64 + ((half ^ ((k0 >> 1) & 1)) << 5) + (i & 3) * 8;
-#pragma unroll
-        for (int t = 0; t < kT; ++t) {
-          const char* b = buf + (kT + t) * T::PT + at;
-          f.q[x][t] = lds_col2(b, b + 4 * 64);
-        }
+      for (int t = 0; t < kT; ++t) {
+        o.p[b][t] = *reinterpret_cast<const f16x8*>(P + b * row + at + t * kFrag);
+        o.q[b][t] = *reinterpret_cast<const f16x8*>(Q + b * row + at + t * kFrag);
       }
-    }
   };
-  f32x16 c[WB][WB] = {};                               // [block of j][block of i], 2^24 times the product
-  const auto multiply = [&](const Frag& f) __attribute__((always_inline)) {
+  const auto multiply = [&](const Frags& o) __attribute__((always_inline)) {
 #pragma unroll
     for (int s = 0; s < 3; ++s)
 #pragma unroll
-      for (int x = 0; x < WB; ++x)
+      for (int x = 0; x < TB; ++x)
 #pragma unroll
-        for (int y = 0; y < WB; ++y) c[x][y] = mfma16(f.q[x][s == 1], f.p[y][s == 0], c[x][y]);
+        for (int y = 0; y < TB; ++y) c[x][y] = mfma16(o.q[x][s == 1], o.p[y][s == 0], c[x][y]);
   };
+#pragma unroll
+  for (int d = 0; d < kDepth; ++d) fetch(d, f[d]);
+  int k = 0;
+  for (; k + kDepth <= steps; k += kDepth)
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      multiply(f[d]);
+      fetch(k + d + kDepth, f[d]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+  for (int d = 0; d < kDepth - 1; ++d)
+    if (k + d < steps) multiply(f[d]);
 
-  // Stage k's second half reads the first operands of stage k + 1, whose pieces went
-  // to LDS during the first half; two more stages are on their way in registers.
-  fetch(0, hold0);
-  fetch(1, hold1);
-  put(lds[0], hold0);
-  fetch(2, hold0);
-  lds_barrier();
-  Frag f0, f1;
-  read(lds[0], 0, f0);
-  for (int k = 0; k < stages; k += 2) {
-    read(lds[0], 1, f1);
-    put(lds[1], hold1);
-    multiply(f0);
-    lds_barrier();
-    read(lds[1], 0, f0);
-    fetch(k + 3, hold1);
-    multiply(f1);
-
-    read(lds[1], 1, f1);
-    put(lds[0], hold0);
-    multiply(f0);
-    lds_barrier();
-    read(lds[0], 0, f0);
-    fetch(k + 4, hold0);
-    multiply(f1);
+  // the four quarters of K, in the waves' order
+  f32x16 o[OB];
+#pragma unroll
+  for (int pass = 0; pass < OB / PB; ++pass) {
+    if (pass) __syncthreads();
+#pragma unroll
+    for (int to = 0; to < 4; ++to)
+#pragma unroll
+      for (int b = 0; b < PB; ++b) {
+        const f32x16& v = c[(to * OB + pass * PB + b) / TB][(to * OB + pass * PB + b) % TB];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sums[wave][to][b][q][lane] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+      }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < PB; ++b)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        f32x4 v = sums[0][wave][b][q][lane];
+#pragma unroll
+        for (int w = 1; w < 4; ++w) v += sums[w][wave][b][q][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[pass * PB + b][4 * q + e] = v[e];
+      }
   }
+  __syncthreads();
 
-  // A lane has row i, columns j .. j + 3 of each group.
+  // Each kept block: lane lr + 32 h has row i, columns 8 g + 4 h + 0..3.
+  float* const turn = reinterpret_cast<float*>(sums) + wave * (32 * 33);
   const int t = kMode == kStore ? tensor_of(jobs.first, z) : 0;
+  const bool flip = jobs.rows > jobs.cols;
 #pragma unroll
-  for (int x = 0; x < WB; ++x)
+  for (int b = 0; b < OB; ++b) {
+    const int at = wave * OB + b, bi = ti * TB + at % TB, bj = tj * TB + at / TB;   // in blocks of 32
+    f32x16 v = o[b];
+    // kGram: 2^24 times the result; otherwise 2^12 times
+    if constexpr (kMode != kGram) {
+      const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = (kMode == kPoly ? jobs.c : 1.0f) * kInvScale;
+      const u16* from = g.old + z * op + frag_at(bi, 2 * bj, g.width) + lane * 8;
 #pragma unroll
-    for (int y = 0; y < WB; ++y)
+      for (int s = 0; s < 2; ++s) {
+        const f16x8 h = *reinterpret_cast<const f16x8*>(from + s * kT * kFrag);
+        const f16x8 l = *reinterpret_cast<const f16x8*>(from + s * kT * kFrag + kFrag);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const int i = ti * TI + wi * (TI / 2) + y * 32 + lr, j = tj * TI + wj * (TI / 2) + x * 32 + 8 * s + 4 * lh;
-        // kGram: 2^24 times the result; otherwise 2^12 times
-        float v[4];
+        for (int e = 0; e < 8; ++e) v[8 * s + e] = fmaf(keep, (float)h[e] + (float)l[e], mul * v[8 * s + e]);
+      }
+    }
+    constexpr float scale = kMode == kGram ? kInvScale : 1.0f;
+    if constexpr (kMode != kStore) write_block(g.out + z * op + frag_at(bi, 2 * bj, g.width) + lane * 8, v, scale);
+    // the block turned round: lane lr has column lr, rows 8 g + 4 h + 0..3
+    const bool turned = kMode == kApply || (kSym && ti != tj) || (kMode == kStore && !flip);
+    if (turned) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = c[x][y][4 * s + e];
-        if constexpr (kMode != kGram) {
-          const u16* old = g.X + z * op + at_value(i, j, g.width);
-          const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = (kMode == kPoly ? jobs.c : 1.0f) * kInvScale;
-          const uint2 h = *reinterpret_cast<const uint2*>(old), l = *reinterpret_cast<const uint2*>(old + kTermSize);
-          const float o[4] = {f16_lo(l.x) + f16_lo(h.x), f16_hi(l.x) + f16_hi(h.x), f16_lo(l.y) + f16_lo(h.y),
-                              f16_hi(l.y) + f16_hi(h.y)};
+      for (int r = 0; r < 16; ++r) turn[lr * 33 + 8 * (r >> 2) + 4 * lh + (r & 3)] = v[r];
+      __builtin_amdgcn_wave_barrier();
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = fmaf(keep, o[e], mul * v[e]);
-        }
-        if constexpr (kMode != kStore) {
-          constexpr float scale = kMode == kGram ? kInvScale : 1.0f;
-          uint2 h, l;
-          split2(v[0], v[1], scale, h.x, l.x);
-          split2(v[2], v[3], scale, h.y, l.y);
-          u16* out = g.out + z * op + at_value(i, j, g.width);
-          *reinterpret_cast<uint2*>(out) = h;
-          *reinterpret_cast<uint2*>(out + kTermSize) = l;
+      for (int r = 0; r < 16; ++r) v[r] = turn[(8 * (r >> 2) + 4 * lh + (r & 3)) * 33 + lr];
+      __builtin_amdgcn_wave_barrier();
+      if constexpr (kMode != kStore)
+        write_block((kSym ? g.out : g.outT) + z * op + frag_at(bj, 2 * bi, g.np) + lane * 8, v, scale);
+    }
+    if constexpr (kMode == kStore) {
+      // lanes run along the rows of the caller's matrix
+      const int64_t base = (int64_t)(z - jobs.first[t]) * jobs.rows * jobs.cols;
+      const int r0 = 32 * (flip ? bj : bi), col = 32 * (flip ? bi : bj) + lr;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int rr = r0 + 8 * (r >> 2) + 4 * lh + (r & 3);
+        if (rr >= jobs.rows || col >= jobs.cols) continue;
+        const int64_t to = base + (int64_t)rr * jobs.cols + col;
+        const float x = v[r] * kInvScale;
+        if (jobs.m[t]) {
+          float* w = static_cast<float*>(jobs.out[t]) + to;
+          *w = fmaf(-jobs.rate, x, jobs.decay * *w);
+        } else if (jobs.out_bf16) {
+          static_cast<u16*>(jobs.out[t])[to] = to_bf16(x);
         } else {
-          const bool flip = jobs.rows > jobs.cols;
-          const int64_t base = (int64_t)(z - jobs.first[t]) * jobs.rows * jobs.cols;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = flip ? j + e : i, cc = flip ? i : j + e;
-            if (r >= jobs.rows || cc >= jobs.cols) continue;
-            const int64_t at = base + (int64_t)r * jobs.cols + cc;
-            const float o = v[e] * kInvScale;
-            if (jobs.m[t]) {
-              float* w = static_cast<float*>(jobs.out[t]) + at;
-              *w = fmaf(-jobs.rate, o, jobs.decay * *w);
-            } else if (jobs.out_bf16) {
-              static_cast<u16*>(jobs.out[t])[at] = to_bf16(o);
-            } else {
-              static_cast<float*>(jobs.out[t])[at] = o;
-            }
-          }
+          static_cast<float*>(jobs.out[t])[to] = x;
         }
       }
+    }
+  }
 }
 
 // ---- small matrices -------------------------------------------------------------------
@@ -745,8 +736,9 @@ int64_t round_up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Plan {
-  int n, L, np, lp, tile, chunks, mats;
-  size_t x0, x1, A, B, bytes;   // offsets; the partial sums come first
+  int n, L, np, lp, chunks, mats;
+  bool wide;                     // tiles of 128, otherwise of 64
+  size_t r0, r1, c0, c1, A, B, bytes;   // offsets; the partial sums come first
 };
 // Tiles of 128 where they alone occupy the device, of 64 otherwise.
 constexpr int kManyTiles = 192;
@@ -755,56 +747,61 @@ Plan plan_of(int rows, int cols, int mats) {
   p.n = rows < cols ? rows : cols;
   p.L = rows < cols ? cols : rows;
   p.mats = mats;
-  p.tile = round_up(p.n, 128) / 128 * (round_up(p.n, 128) / 128) * mats >= kManyTiles ? 128 : 64;
-  p.np = (int)round_up(p.n, p.tile);
-  p.lp = (int)round_up(p.L, p.tile);
+  p.wide = round_up(p.n, 128) / 128 * (round_up(p.L, 128) / 128) * mats >= kManyTiles;
+  p.np = (int)round_up(p.n, p.wide ? 128 : 64);
+  p.lp = (int)round_up(p.L, p.wide ? 128 : 64);
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
   const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
-  p.x0 = part;
-  p.x1 = p.x0 + x;
-  p.A = p.x1 + x;
+  p.r0 = part;
+  p.r1 = p.r0 + x;
+  p.c0 = p.r1 + x;
+  p.c1 = p.c0 + x;
+  p.A = p.c1 + x;
   p.B = p.A + a;
   p.bytes = p.B + a;
   return p;
 }
 
-template <int kMode, int TI>
+template <int kMode, int TB>
 void gemm(GemmArgs g, const Jobs& j, int mats, hipStream_t st) {
-  g.tiles_i = g.np / TI;
-  g.tiles_j = g.width / TI;
-  g.tiles = g.tiles_i * g.tiles_j * mats;
+  g.tiles_i = g.np / (32 * TB);
+  g.tiles_j = g.width / (32 * TB);
+  g.per_mat = kMode == kGram || kMode == kPoly ? g.tiles_i * (g.tiles_i + 1) / 2 : g.tiles_i * g.tiles_j;
+  g.tiles = g.per_mat * mats;
   g.per_xcd = (g.tiles + 7) / 8;
-  hipLaunchKernelGGL((k_ns_gemm<kMode, TI>), dim3(8 * g.per_xcd), dim3(kThreads), 0, st, g, j);
+  hipLaunchKernelGGL((k_ns_gemm<kMode, TB>), dim3(8 * g.per_xcd), dim3(kThreads), 0, st, g, j);
 }
 
-template <int TI>
+template <int TB>
 hipError_t steps_of(const Plan& p, const Jobs& j, int steps, char* ws, hipStream_t st, Timer* tm) {
+  const auto at = [&](size_t offset) { return reinterpret_cast<u16*>(ws + offset); };
   double* part = reinterpret_cast<double*>(ws);
-  u16 *x0 = reinterpret_cast<u16*>(ws + p.x0), *x1 = reinterpret_cast<u16*>(ws + p.x1);
-  u16 *A = reinterpret_cast<u16*>(ws + p.A), *B = reinterpret_cast<u16*>(ws + p.B);
+  u16 *r0 = at(p.r0), *r1 = at(p.r1), *c0 = at(p.c0), *c1 = at(p.c1), *A = at(p.A), *B = at(p.B);
   if (tm) tm->begin("ns_norm");
   hipLaunchKernelGGL(k_ns_norm, dim3((unsigned)p.mats * p.chunks), dim3(kThreads), 0, st, j, p.chunks, part);
   if (tm) tm->end();
   if (tm) tm->begin("ns_split");
-  hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, x0, p.np,
-                     p.lp);
+  hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
+                     p.np, p.lp);
   if (tm) tm->end();
   for (int s = 0; s < steps; ++s) {
     if (tm) tm->begin("ns_gram");
-    gemm<kGram, TI>(GemmArgs{x0, x0, nullptr, A, p.np, p.lp, p.np}, j, p.mats, st);
+    gemm<kGram, TB>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_poly");
-    gemm<kPoly, TI>(GemmArgs{A, A, A, B, p.np, p.np, p.np}, j, p.mats, st);
+    gemm<kPoly, TB>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_apply");
-    const GemmArgs g{B, x0, x0, x1, p.np, p.np, p.lp};
-    if (s + 1 < steps) gemm<kApply, TI>(g, j, p.mats, st);
-    else gemm<kStore, TI>(g, j, p.mats, st);
+    const GemmArgs g{B, c0, r0, r1, c1, p.np, p.np, p.lp};
+    if (s + 1 < steps) gemm<kApply, TB>(g, j, p.mats, st);
+    else gemm<kStore, TB>(g, j, p.mats, st);
     if (tm) tm->end();
-    u16* t = x0;
-    x0 = x1;
-    x1 = t;
+    u16 *r = r0, *c = c0;
+    r0 = r1;
+    r1 = r;
+    c0 = c1;
+    c1 = c;
   }
   return hipGetLastError();
 }
@@ -918,7 +915,7 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm
     j.eps = js.eps;
     const Plan p = plan_of(a.rows, a.cols, total);
     char* w = static_cast<char*>(ws);
-    return p.tile == 128 ? steps_of<128>(p, j, js.steps, w, st, tm) : steps_of<64>(p, j, js.steps, w, st, tm);
+    return p.wide ? steps_of<4>(p, j, js.steps, w, st, tm) : steps_of<2>(p, j, js.steps, w, st, tm);
   });
 }
 
