@@ -220,7 +220,7 @@ sagips_status sagips_orthogonalise(sagips_ctx* c, const sagips_newton_schulz* ns
     DeviceGuard g(c->device);
     s = ensure_ws(c, muon_workspace(js));
     if (s != SAGIPS_OK) return s;
-    hipError_t e = launch_muon(js, c->ws, c->stream, timer_of(c));
+    hipError_t e = launch_muon(js, c->ws, c->n_cu, c->stream, timer_of(c));
     return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "orthogonalise launch");
   });
 }
@@ -275,7 +275,7 @@ sagips_status sagips_muon_step(sagips_ctx* c, const sagips_matrix_set* set, cons
     DeviceGuard g(c->device);
     s = ensure_ws(c, muon_workspace(js));
     if (s != SAGIPS_OK) return s;
-    hipError_t e = launch_muon(js, c->ws, c->stream, timer_of(c));
+    hipError_t e = launch_muon(js, c->ws, c->n_cu, c->stream, timer_of(c));
     return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "muon_step launch");
   });
 }

@@ -122,7 +122,7 @@ struct MatrixJobs {
   int steps;
 };
 size_t muon_workspace(const MatrixJobs& js);
-hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm);
+hipError_t launch_muon(const MatrixJobs& js, void* ws, int n_cu, hipStream_t st, Timer* tm);
 
 // disc_bf16.hip --------------------------------------------------------------
 // Samples the fake events itself when a.fake_src is set (any E); never writes dLg_dtheta.

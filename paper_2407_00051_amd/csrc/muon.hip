@@ -241,22 +241,28 @@ __device__ __forceinline__ void write_block(u16* at, const f32x16& v, float scal
 }
 
 template <int kMode, int TB>
-__global__ __launch_bounds__(kThreads, TB == 4 ? 1 : 2) void k_ns_gemm(GemmArgs g, Jobs jobs) {
+__global__ __launch_bounds__(kThreads, TB == 2 ? 2 : 1) void k_ns_gemm(GemmArgs g, Jobs jobs) {
   constexpr bool kSym = kMode == kGram || kMode == kPoly;
   constexpr int kDepth = TB == 4 ? 3 : 4;
-  constexpr int OB = TB * TB / 4;                      // blocks a wave keeps: x TB + y in [wave OB, wave OB + OB)
-  constexpr int PB = OB > 2 ? 2 : OB;                  // of them added at a time
+  constexpr int OB = (TB * TB + 3) / 4;                // blocks a wave keeps: x TB + y in [wave OB, wave OB + OB)
+  constexpr int PB = OB == 4 ? 2 : 1;                  // of them added at a time
   __shared__ __attribute__((aligned(16))) f32x4 sums[4][4][PB][4][64];   // [from][to][block][quad of values][lane]
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int z, ti, tj;
   if (!tile_of<kSym>(g, z, ti, tj)) return;
   const int64_t pp = (int64_t)kT * g.np * g.kp, qp = (int64_t)kT * g.width * g.kp, op = (int64_t)kT * g.np * g.width;
-  const u16* P = g.P + z * pp + frag_at(ti * TB, wave, g.kp) + lane * 8;
-  const u16* Q = g.Q + z * qp + frag_at(tj * TB, wave, g.kp) + lane * 8;
-  const int64_t row = frag_at(1, 0, g.kp);             // from one block of 32 rows to the next
+  // a tile may reach past the last block: those rows repeat it, and their results go nowhere
+  const int ni = g.np / 32, nj = g.width / 32;
+  int64_t P[TB], Q[TB];                                // offsets of the wave's first fragments
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    P[b] = z * pp + frag_at(min(ti * TB + b, ni - 1), wave, g.kp);
+    Q[b] = z * qp + frag_at(min(tj * TB + b, nj - 1), wave, g.kp);
+  }
   const int steps = g.kp / 64;                         // of this wave: every fourth
 
+  const uint32_t lane16 = lane * 16;
   struct Frags {
     f16x8 p[TB][kT], q[TB][kT];
   };
@@ -268,8 +274,8 @@ __global__ __launch_bounds__(kThreads, TB == 4 ? 1 : 2) void k_ns_gemm(GemmArgs 
     for (int b = 0; b < TB; ++b)
 #pragma unroll
       for (int t = 0; t < kT; ++t) {
-        o.p[b][t] = *reinterpret_cast<const f16x8*>(P + b * row + at + t * kFrag);
-        o.q[b][t] = *reinterpret_cast<const f16x8*>(Q + b * row + at + t * kFrag);
+        o.p[b][t] = *reinterpret_cast<const f16x8*>(reinterpret_cast<const char*>(g.P + P[b] + at) + (lane16 + t * 2 * kFrag));
+        o.q[b][t] = *reinterpret_cast<const f16x8*>(reinterpret_cast<const char*>(g.Q + Q[b] + at) + (lane16 + t * 2 * kFrag));
       }
   };
   const auto multiply = [&](const Frags& o) __attribute__((always_inline)) {
@@ -303,7 +309,9 @@ __global__ __launch_bounds__(kThreads, TB == 4 ? 1 : 2) void k_ns_gemm(GemmArgs 
     for (int to = 0; to < 4; ++to)
 #pragma unroll
       for (int b = 0; b < PB; ++b) {
-        const f32x16& v = c[(to * OB + pass * PB + b) / TB][(to * OB + pass * PB + b) % TB];
+        const int at = to * OB + pass * PB + b;
+        if (at >= TB * TB) continue;
+        const f32x16& v = c[at / TB][at % TB];
 #pragma unroll
         for (int q = 0; q < 4; ++q) sums[wave][to][b][q][lane] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
       }
@@ -328,6 +336,7 @@ __global__ __launch_bounds__(kThreads, TB == 4 ? 1 : 2) void k_ns_gemm(GemmArgs 
 #pragma unroll
   for (int b = 0; b < OB; ++b) {
     const int at = wave * OB + b, bi = ti * TB + at % TB, bj = tj * TB + at / TB;   // in blocks of 32
+    if (at >= TB * TB || bi >= ni || bj >= nj) continue;
     f32x16 v = o[b];
     // kGram: 2^24 times the result; otherwise 2^12 times
     if constexpr (kMode != kGram) {
@@ -737,19 +746,15 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Plan {
   int n, L, np, lp, chunks, mats;
-  bool wide;                     // tiles of 128, otherwise of 64
   size_t r0, r1, c0, c1, A, B, bytes;   // offsets; the partial sums come first
 };
-// Tiles of 128 where they alone occupy the device, of 64 otherwise.
-constexpr int kManyTiles = 192;
 Plan plan_of(int rows, int cols, int mats) {
   Plan p;
   p.n = rows < cols ? rows : cols;
   p.L = rows < cols ? cols : rows;
   p.mats = mats;
-  p.wide = round_up(p.n, 128) / 128 * (round_up(p.L, 128) / 128) * mats >= kManyTiles;
-  p.np = (int)round_up(p.n, p.wide ? 128 : 64);
-  p.lp = (int)round_up(p.L, p.wide ? 128 : 64);
+  p.np = (int)round_up(p.n, 64);
+  p.lp = (int)round_up(p.L, 64);
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
   const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
@@ -763,18 +768,41 @@ Plan plan_of(int rows, int cols, int mats) {
   return p;
 }
 
+// Blocks in a tile's side: 2, 3 or 4.  A tile costs a compute unit 0.35, 0.6 or 1 (its
+// products go as the square, the fragments it reads as the side), and units take tiles
+// in rounds.
+int tile_side(bool sym, int np, int width, int mats, int n_cu) {
+  static const double cost[5] = {0, 0, 0.35, 0.6, 1.0};
+  int best = 2;
+  double least = 0.0;
+  for (int tb = 2; tb <= 4; ++tb) {
+    const int64_t i = (np / 32 + tb - 1) / tb, j = (width / 32 + tb - 1) / tb, tiles = (sym ? i * (i + 1) / 2 : i * j) * mats;
+    const double t = cost[tb] * (double)((tiles + n_cu - 1) / n_cu);
+    if (tb == 2 || t < least) {
+      best = tb;
+      least = t;
+    }
+  }
+  return best;
+}
+
 template <int kMode, int TB>
-void gemm(GemmArgs g, const Jobs& j, int mats, hipStream_t st) {
-  g.tiles_i = g.np / (32 * TB);
-  g.tiles_j = g.width / (32 * TB);
+void gemm_of(GemmArgs g, const Jobs& j, int mats, hipStream_t st) {
+  g.tiles_i = (g.np / 32 + TB - 1) / TB;
+  g.tiles_j = (g.width / 32 + TB - 1) / TB;
   g.per_mat = kMode == kGram || kMode == kPoly ? g.tiles_i * (g.tiles_i + 1) / 2 : g.tiles_i * g.tiles_j;
   g.tiles = g.per_mat * mats;
   g.per_xcd = (g.tiles + 7) / 8;
   hipLaunchKernelGGL((k_ns_gemm<kMode, TB>), dim3(8 * g.per_xcd), dim3(kThreads), 0, st, g, j);
 }
+template <int kMode>
+void gemm(const GemmArgs& g, const Jobs& j, int mats, int side, hipStream_t st) {
+  if (side == 2) gemm_of<kMode, 2>(g, j, mats, st);
+  else if (side == 3) gemm_of<kMode, 3>(g, j, mats, st);
+  else gemm_of<kMode, 4>(g, j, mats, st);
+}
 
-template <int TB>
-hipError_t steps_of(const Plan& p, const Jobs& j, int steps, char* ws, hipStream_t st, Timer* tm) {
+hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws, hipStream_t st, Timer* tm) {
   const auto at = [&](size_t offset) { return reinterpret_cast<u16*>(ws + offset); };
   double* part = reinterpret_cast<double*>(ws);
   u16 *r0 = at(p.r0), *r1 = at(p.r1), *c0 = at(p.c0), *c1 = at(p.c1), *A = at(p.A), *B = at(p.B);
@@ -785,17 +813,18 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, char* ws, hipStream
   hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
                      p.np, p.lp);
   if (tm) tm->end();
+  const int sym = tile_side(true, p.np, p.np, p.mats, n_cu), all = tile_side(false, p.np, p.lp, p.mats, n_cu);
   for (int s = 0; s < steps; ++s) {
     if (tm) tm->begin("ns_gram");
-    gemm<kGram, TB>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, st);
+    gemm<kGram>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, sym, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_poly");
-    gemm<kPoly, TB>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, st);
+    gemm<kPoly>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, sym, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_apply");
     const GemmArgs g{B, c0, r0, r1, c1, p.np, p.np, p.lp};
-    if (s + 1 < steps) gemm<kApply, TB>(g, j, p.mats, st);
-    else gemm<kStore, TB>(g, j, p.mats, st);
+    if (s + 1 < steps) gemm<kApply>(g, j, p.mats, all, st);
+    else gemm<kStore>(g, j, p.mats, all, st);
     if (tm) tm->end();
     u16 *r = r0, *c = c0;
     r0 = r1;
@@ -883,7 +912,7 @@ static hipError_t launch_small(const MatrixJobs& js, int which, hipStream_t st, 
   return hipGetLastError();
 }
 
-hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm) {
+hipError_t launch_muon(const MatrixJobs& js, void* ws, int n_cu, hipStream_t st, Timer* tm) {
   for (int which = 0; which < kSmallClasses; ++which) {
     const hipError_t e = launch_small(js, which, st, tm);
     if (e != hipSuccess) return e;
@@ -914,8 +943,7 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, hipStream_t st, Timer* tm
     j.c = js.coef[2];
     j.eps = js.eps;
     const Plan p = plan_of(a.rows, a.cols, total);
-    char* w = static_cast<char*>(ws);
-    return p.wide ? steps_of<4>(p, j, js.steps, w, st, tm) : steps_of<2>(p, j, js.steps, w, st, tm);
+    return steps_of(p, j, js.steps, n_cu, static_cast<char*>(ws), st, tm);
   });
 }
 
