@@ -93,22 +93,33 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // ---- norm -------------------------------------------------------------------------
 // The momentum update, and each matrix's sum of squares of U in 64 bits (neither
 // large nor small gradients leave its range), in chunks of kChunk elements.
-constexpr int64_t kChunk = 4096;
+constexpr int kChunk = 4096;
 __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double* __restrict__ part) {
   const int z = blockIdx.x / chunks, k = blockIdx.x % chunks;
   const int t = tensor_of(j.first, z);
   const int64_t size = (int64_t)j.rows * j.cols, base = (z - j.first[t]) * size;
-  const int64_t e1 = min(size, (k + 1) * kChunk);
-  double s = 0.0;
-#pragma unroll 4
-  for (int64_t e = k * kChunk + threadIdx.x; e < e1; e += kThreads) {
-    float u = load_src(j.src[t], base + e, j.src_bf16);
-    if (j.m[t]) {
-      const float m = fmaf(j.momentum, j.m[t][base + e], u);
-      j.m[t][base + e] = m;
-      u = j.nesterov ? fmaf(j.momentum, m, u) : m;
+  const int64_t e0 = (int64_t)k * kChunk + threadIdx.x;
+  constexpr int kEach = kChunk / kThreads;
+  float u[kEach], m[kEach];
+#pragma unroll
+  for (int q = 0; q < kEach; ++q) {
+    const int64_t e = e0 + q * kThreads;
+    u[q] = m[q] = 0.0f;
+    if (e < size) {
+      u[q] = load_src(j.src[t], base + e, j.src_bf16);
+      if (j.m[t]) m[q] = j.m[t][base + e];
     }
-    s = fma((double)u, (double)u, s);
+  }
+  double s = 0.0;
+#pragma unroll
+  for (int q = 0; q < kEach; ++q) {
+    const int64_t e = e0 + q * kThreads;
+    if (j.m[t] && e < size) {
+      const float w = fmaf(j.momentum, m[q], u[q]);
+      j.m[t][base + e] = w;
+      u[q] = j.nesterov ? fmaf(j.momentum, w, u[q]) : w;
+    }
+    s = fma((double)u[q], (double)u[q], s);
   }
   __shared__ double w[kThreads / 64];
   s = wave_sum_d(s);
@@ -145,20 +156,26 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
   const int z = blockIdx.z, t = tensor_of(j.first, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
   const bool flip = j.rows > j.cols;
   const int64_t base = (int64_t)(z - j.first[t]) * j.rows * j.cols;
-  const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
-  // read along the source's rows
+  // read along the source's rows, before the norm is waited for
   const int r0 = flip ? l0 : i0, c0 = flip ? i0 : l0;
-#pragma unroll 8
-  for (int q = threadIdx.x; q < 4096; q += kThreads) {
-    const int r = q >> 6, c = q & 63;
-    float u = 0.0f;
-    if (r0 + r < j.rows && c0 + c < j.cols) {
-      const int64_t e = base + (int64_t)(r0 + r) * j.cols + c0 + c;
-      u = j.m[t] && !j.nesterov ? 0.0f : load_src(j.src[t], e, j.src_bf16);
-      if (j.m[t]) u = j.nesterov ? fmaf(j.momentum, j.m[t][e], u) : j.m[t][e];
+  const int c = threadIdx.x & 63, col = c0 + c;
+  float u[16];
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int r = r0 + 4 * q + (threadIdx.x >> 6);
+    u[q] = 0.0f;
+    if (r < j.rows && col < j.cols) {
+      const int64_t e = base + (int64_t)r * j.cols + col;
+      if (!j.m[t]) u[q] = load_src(j.src[t], e, j.src_bf16);
+      else u[q] = j.nesterov ? fmaf(j.momentum, j.m[t][e], load_src(j.src[t], e, j.src_bf16)) : j.m[t][e];
     }
-    if (flip) tile[c][r] = u * inv;
-    else tile[r][c] = u * inv;
+  }
+  const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
+#pragma unroll
+  for (int q = 0; q < 16; ++q) {
+    const int r = 4 * q + (threadIdx.x >> 6);
+    if (flip) tile[c][r] = u[q] * inv;
+    else tile[r][c] = u[q] * inv;
   }
   __syncthreads();
   const int64_t size = (int64_t)kT * np * lp;
