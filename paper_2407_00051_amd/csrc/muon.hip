@@ -785,16 +785,18 @@ Plan plan_of(int rows, int cols, int mats) {
   return p;
 }
 
-// Blocks in a tile's side: 2, 3 or 4.  A tile costs a compute unit 0.35, 0.6 or 1 (its
-// products go as the square, the fragments it reads as the side), and units take tiles
-// in rounds.
-int tile_side(bool sym, int np, int width, int mats, int n_cu) {
-  static const double cost[5] = {0, 0, 0.35, 0.6, 1.0};
+// Blocks in a tile's side: 2, 3 or 4.  Compute units take tiles in rounds; a round takes
+// about fixed + per_k K microseconds (measured from K = 256 to 2,048; a larger side reads
+// less per product but has more to add up at the end, and only tiles of 2 run two to a
+// unit).  Products at 2,048 x 2,048: symmetric 45, 31, 37 us with sides 2, 3, 4, others
+// 63, 63, 51; at K = 512 a side of 2 is the fastest at every count.
+int tile_side(bool sym, int np, int width, int K, int mats, int n_cu) {
+  static const double fixed[5] = {0, 0, 2.6, 7.6, 13.0}, per_k[5] = {0, 0, 0.0064, 0.0115, 0.018};
   int best = 2;
   double least = 0.0;
   for (int tb = 2; tb <= 4; ++tb) {
     const int64_t i = (np / 32 + tb - 1) / tb, j = (width / 32 + tb - 1) / tb, tiles = (sym ? i * (i + 1) / 2 : i * j) * mats;
-    const double t = cost[tb] * (double)((tiles + n_cu - 1) / n_cu);
+    const double t = (fixed[tb] + per_k[tb] * K) * (double)((tiles + n_cu - 1) / n_cu);
     if (tb == 2 || t < least) {
       best = tb;
       least = t;
@@ -830,18 +832,19 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws,
   hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
                      p.np, p.lp);
   if (tm) tm->end();
-  const int sym = tile_side(true, p.np, p.np, p.mats, n_cu), all = tile_side(false, p.np, p.lp, p.mats, n_cu);
+  const int gram = tile_side(true, p.np, p.np, p.lp, p.mats, n_cu), poly = tile_side(true, p.np, p.np, p.np, p.mats, n_cu);
+  const int apply = tile_side(false, p.np, p.lp, p.np, p.mats, n_cu);
   for (int s = 0; s < steps; ++s) {
     if (tm) tm->begin("ns_gram");
-    gemm<kGram>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, sym, st);
+    gemm<kGram>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, gram, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_poly");
-    gemm<kPoly>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, sym, st);
+    gemm<kPoly>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, poly, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_apply");
     const GemmArgs g{B, c0, r0, r1, c1, p.np, p.np, p.lp};
-    if (s + 1 < steps) gemm<kApply>(g, j, p.mats, all, st);
-    else gemm<kStore>(g, j, p.mats, all, st);
+    if (s + 1 < steps) gemm<kApply>(g, j, p.mats, apply, st);
+    else gemm<kStore>(g, j, p.mats, apply, st);
     if (tm) tm->end();
     u16 *r = r0, *c = c0;
     r0 = r1;
