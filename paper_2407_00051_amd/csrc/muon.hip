@@ -407,9 +407,8 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 2 : 1) void k_ns_gemm(GemmArgs 
 // ---- small matrices -------------------------------------------------------------------
 // All steps of one matrix in one workgroup, from the momentum update to the
 // parameters, X never leaving registers and LDS: n <= NP and L <= 16384 / NP, for NP
-// of 32, 64 and 128.  Wave (rw, cw) of NP / 32 x 128 / NP owns rows 32 rw .. + 31 of X
-// and every (128 / NP)-th block of 32 columns, JB of them (the fewest of 1, 2 and 4
-// that hold L); lane lr (of half lh) holds row 32 rw + lr, columns 8 g + 4 lh + 0..3 of
+// of 32, 64 and 128.  Wave (rw, cw) of RW x CW = W owns rows 32 rw .. + 31 of X and every
+// CW-th block of 32 columns, JB of them (the fewest that hold L); lane lr (of half lh) holds row 32 rw + lr, columns 8 g + 4 lh + 0..3 of
 // each block, as accumulators do.
 //   A = X X^T: the wave forms columns 32 rw .. of A, summed over its own columns of X,
 //   whose terms it has in registers; waves of one rw add their sums through LDS.  A is
@@ -439,11 +438,10 @@ struct SmallJobs {
 
 constexpr int kSmallValues = 16384;                    // NP x LP
 constexpr int kSmallBuffer = kSmallValues * kT * 2;    // X's terms, and Y's
-constexpr int kQuads = kSmallValues / 4 / kThreads;
 
 // U of a small matrix into its fp32 copy, the momentum on the way; returns the
 // thread's sum of squares.  Quads (cols a multiple of 4) have every load in flight.
-template <bool kBf16, bool kMom>
+template <int kN, bool kBf16, bool kMom>   // kN threads
 __device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJob& job, int64_t base, float* flat, int pitch) {
   const int cols = job.cols, size = job.rows * cols;
   const float inv_cols = 1.0f / cols;
@@ -452,10 +450,10 @@ __device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJ
   float* const mom = kMom ? job.m + base : nullptr;
   double sq = 0.0;
   if (cols % 4 == 0) {
-    f32x4 u[kQuads], m[kQuads];
+    f32x4 u[(kSmallValues / 4 / kN)], m[(kSmallValues / 4 / kN)];
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int e = (k * kThreads + threadIdx.x) * 4;
+    for (int k = 0; k < (kSmallValues / 4 / kN); ++k) {
+      const int e = (k * kN + threadIdx.x) * 4;
       if (e >= size) break;
       if constexpr (kBf16) {
         const uint2 q = *reinterpret_cast<const uint2*>(b16 + e);
@@ -466,8 +464,8 @@ __device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJ
       if constexpr (kMom) m[k] = *reinterpret_cast<const f32x4*>(mom + e);
     }
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int e = (k * kThreads + threadIdx.x) * 4;
+    for (int k = 0; k < (kSmallValues / 4 / kN); ++k) {
+      const int e = (k * kN + threadIdx.x) * 4;
       if (e >= size) break;
       f32x4 v = u[k];
       if constexpr (kMom) {
@@ -484,7 +482,7 @@ __device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJ
     }
   } else {
 #pragma unroll 4
-    for (int e = threadIdx.x; e < size; e += kThreads) {
+    for (int e = threadIdx.x; e < size; e += kN) {
       const int r = (int)((e + 0.5f) * inv_cols);
       float u = kBf16 ? bf16_lo(b16[e]) : f32[e];
       if constexpr (kMom) {
@@ -500,25 +498,25 @@ __device__ __forceinline__ double small_load(const SmallJobs& jobs, const SmallJ
 }
 
 // The result from the fp32 copy: parameters moved, or the matrix written.
-template <bool kBf16, bool kMom>
+template <int kN, bool kBf16, bool kMom>   // kN threads
 __device__ __forceinline__ void small_store(const SmallJobs& jobs, const SmallJob& job, int64_t base, const float* flat, int pitch) {
   const int cols = job.cols, size = job.rows * cols;
   const float inv_cols = 1.0f / cols;
   float* const f32 = static_cast<float*>(job.out) + base;
   u16* const b16 = static_cast<u16*>(job.out) + base;
   if (cols % 4 == 0) {
-    f32x4 old[kQuads];
+    f32x4 old[(kSmallValues / 4 / kN)];
     if constexpr (kMom)
 #pragma unroll
-      for (int k = 0; k < kQuads; ++k) {
-        const int e = (k * kThreads + threadIdx.x) * 4;
+      for (int k = 0; k < (kSmallValues / 4 / kN); ++k) {
+        const int e = (k * kN + threadIdx.x) * 4;
         if (e >= size) break;
         old[k] = *reinterpret_cast<const f32x4*>(f32 + e);
       }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < kQuads; ++k) {
-      const int e = (k * kThreads + threadIdx.x) * 4;
+    for (int k = 0; k < (kSmallValues / 4 / kN); ++k) {
+      const int e = (k * kN + threadIdx.x) * 4;
       if (e >= size) break;
       const int r = (int)((e + 0.5f) * inv_cols);
       f32x4 v;
@@ -531,7 +529,7 @@ __device__ __forceinline__ void small_store(const SmallJobs& jobs, const SmallJo
   } else {
     __syncthreads();
 #pragma unroll 4
-    for (int e = threadIdx.x; e < size; e += kThreads) {
+    for (int e = threadIdx.x; e < size; e += kN) {
       const int r = (int)((e + 0.5f) * inv_cols);
       const float v = flat[r * (pitch - cols) + e];
       if constexpr (kMom) f32[e] = fmaf(-job.rate, v, jobs.decay * f32[e]);
@@ -541,16 +539,18 @@ __device__ __forceinline__ void small_store(const SmallJobs& jobs, const SmallJo
   }
 }
 
-template <int NP, int JB>
-__global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
+template <int NP, int JB, int W>
+__global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
   constexpr int LP = kSmallValues / NP;
-  constexpr int RW = NP / 32, CW = 4 / RW, NI = NP / 32;
+  constexpr int RW = NP / 32, CW = W / RW, NI = NP / 32;
+  constexpr int kN = 64 * W;
+  constexpr bool kShare = W == 8;                      // A's blocks are shared out, otherwise its sums
+  constexpr int IB = kShare ? NI / CW : NI;            // blocks of A that the wave forms
   constexpr int RB = 2 * LP, PL = NP * RB;             // bytes of a row of one term, of a term
-  constexpr int IK = 4 / NI, JK = 4 / JB;              // accumulators a block, so that four products run side by side
   // X's terms, then Y's; before the first and after the last step the fp32 copy (rows
   // one value longer if even: 66 KB at most); Y's part also takes the waves' sums for A
   __shared__ __attribute__((aligned(16))) char lds[2 * kSmallBuffer];
-  __shared__ double sums[kThreads / 64];
+  __shared__ double sums[W];
   char* const ldsX = lds;
   char* const ldsY = lds + kSmallBuffer;
   float* const flat = reinterpret_cast<float*>(lds);
@@ -565,12 +565,15 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
   const int pitch = cols | 1;
 
   double sq;
-  if (job.m) sq = jobs.src_bf16 ? small_load<true, true>(jobs, job, base, flat, pitch) : small_load<false, true>(jobs, job, base, flat, pitch);
-  else sq = jobs.src_bf16 ? small_load<true, false>(jobs, job, base, flat, pitch) : small_load<false, false>(jobs, job, base, flat, pitch);
+  if (job.m) sq = jobs.src_bf16 ? small_load<kN, true, true>(jobs, job, base, flat, pitch) : small_load<kN, false, true>(jobs, job, base, flat, pitch);
+  else sq = jobs.src_bf16 ? small_load<kN, true, false>(jobs, job, base, flat, pitch) : small_load<kN, false, false>(jobs, job, base, flat, pitch);
   sq = wave_sum_d(sq);
   if (lane == 0) sums[wave] = sq;
   __syncthreads();
-  const float inv = (float)(1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + jobs.eps));
+  double total = 0.0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) total += sums[w];
+  const float inv = (float)(1.0 / (sqrt(total) + jobs.eps));
 
   float one = 1.0f;                                    // not a constant to the compiler: a multiplication by it lets
   asm("" : "+s"(one));                                 // fp16 operands go straight into an fp32 fma
@@ -637,7 +640,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
     };
 #pragma unroll
     for (int y = 0; y < JB; ++y) read(0, y);
-    f32x16 c[JB][JK] = {};
+    f32x16 c[JB] = {};
     // a step's first products each with the reads of a block of the next step behind it, in this order
 #pragma unroll
     for (int ks = 0; ks < kSteps; ++ks)
@@ -645,17 +648,12 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
       for (int s = 0; s < 3; ++s)
 #pragma unroll
         for (int y = 0; y < JB; ++y) {
-          f32x16& o = c[y][(3 * ks + s) % JK];
-          o = mfma16(q[ks & 1][y][s == 1], A[ks / 2].v[ks % 2][s == 0], o);
+          c[y] = mfma16(q[ks & 1][y][s == 1], A[ks / 2].v[ks % 2][s == 0], c[y]);
           if (s == 0 && ks + 1 < kSteps) read(ks + 1, y);
           __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-    for (int y = 0; y < JB; ++y) {
-#pragma unroll
-      for (int k = 1; k < JK; ++k) c[y][0] += c[y][k];
-      done(y, c[y][0]);
-    }
+    for (int y = 0; y < JB; ++y) done(y, c[y]);
   };
 
   f32x16 x[JB];                                        // 2^12 times X
@@ -663,42 +661,67 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
     lds_barrier();                                     // X is there, Y has been read
     Terms A[NI];
     {
-      constexpr int kSteps = JB * 2;
-      f16x8 q[2][NI][kT];
+      // kShare: all of X's columns, the wave's own first; otherwise its own
+      constexpr int kSteps = JB * 2 * (kShare ? CW : 1);
+      f16x8 q[2][IB][kT], p[2][kT];
+      const auto column = [&](int ks) { return 4 * ((ks / 2) % JB * CW + (cw ^ (ks / 2 / JB))) + 2 * (ks % 2) + lh; };
       const auto read = [&](int ks, int y) __attribute__((always_inline)) {
+        const int ib = kShare ? IB * cw + y : y;
 #pragma unroll
-        for (int w = 0; w < kT; ++w)
-          q[ks & 1][y][w] =
-              lds_row(ldsX + w * PL + (32 * y + lr) * RB + (((4 * (ks / 2 * CW + cw) + 2 * (ks % 2) + lh) ^ own_swz) << 4));
+        for (int w = 0; w < kT; ++w) {
+          q[ks & 1][y][w] = lds_row(ldsX + w * PL + (32 * ib + lr) * RB + ((column(ks) ^ own_swz) << 4));
+          if (y == 0 && ks >= 2 * JB) p[ks & 1][w] = lds_row(ldsX + w * PL + own + ((column(ks) ^ own_swz) << 4));
+        }
       };
 #pragma unroll
-      for (int y = 0; y < NI; ++y) read(0, y);
-      f32x16 c[NI][IK] = {};
+      for (int y = 0; y < IB; ++y) read(0, y);
+      f32x16 c[IB] = {};
 #pragma unroll
       for (int ks = 0; ks < kSteps; ++ks)
 #pragma unroll
         for (int s = 0; s < 3; ++s)
 #pragma unroll
-          for (int y = 0; y < NI; ++y) {
-            f32x16& v = c[y][(3 * ks + s) % IK];
-            v = mfma16(q[ks & 1][y][s == 1], xt[ks / 2].v[ks % 2][s == 0], v);
+          for (int y = 0; y < IB; ++y) {
+            const f16x8& o = ks < 2 * JB ? xt[ks / 2 % JB].v[ks % 2][s == 0] : p[ks & 1][s == 0];
+            c[y] = mfma16(q[ks & 1][y][s == 1], o, c[y]);
             if (s == 0 && ks + 1 < kSteps) read(ks + 1, y);
             __builtin_amdgcn_sched_barrier(0);
           }
+      if constexpr (kShare) {
+        // the blocks of a row go to the other waves of that row through LDS
+        char* const give = ldsY + (rw * NI + IB * cw) * 4096 + lane * 16;
 #pragma unroll
-      for (int y = 0; y < NI; ++y) {
+        for (int y = 0; y < IB; ++y) {
+          Terms o;
+          split(c[y], kInvScale, o);
 #pragma unroll
-        for (int k = 1; k < IK; ++k) c[y][0] += c[y][k];
-        if constexpr (CW == 1) {
-          split(c[y][0], kInvScale, A[y]);
-        } else {
-          float* part = reinterpret_cast<float*>(ldsY) + (wave * NI + y) * 16 * 64 + lane;
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) part[r * 64] = c[y][0][r];
+            for (int w = 0; w < kT; ++w) *reinterpret_cast<f16x8*>(give + y * 4096 + (2 * s + w) * 1024) = o.v[s][w];
+        }
+        lds_barrier();
+        const char* const take = ldsY + rw * NI * 4096 + lane * 16;
+#pragma unroll
+        for (int ib = 0; ib < NI; ++ib)
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int w = 0; w < kT; ++w) A[ib].v[s][w] = lds_row(take + ib * 4096 + (2 * s + w) * 1024);
+        lds_barrier();
+      } else {
+#pragma unroll
+        for (int y = 0; y < NI; ++y) {
+          if constexpr (CW == 1) {
+            split(c[y], kInvScale, A[y]);
+          } else {
+            float* part = reinterpret_cast<float*>(ldsY) + (wave * NI + y) * 16 * 64 + lane;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) part[r * 64] = c[y][r];
+          }
         }
       }
     }
-    if constexpr (CW > 1) {
+    if constexpr (CW > 1 && !kShare) {
       lds_barrier();
 #pragma unroll
       for (int ib = 0; ib < NI; ++ib) {
@@ -738,12 +761,13 @@ __global__ __launch_bounds__(kThreads, 1) void k_ns_small(SmallJobs jobs) {
       const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
       if (i < n && j < L) flat[i * pi + j * pj] = x[b][r] * kInvScale;
     }
-  if (job.m) small_store<false, true>(jobs, job, base, flat, pitch);
-  else if (jobs.out_bf16) small_store<true, false>(jobs, job, base, flat, pitch);
-  else small_store<false, false>(jobs, job, base, flat, pitch);
+  if (job.m) small_store<kN, false, true>(jobs, job, base, flat, pitch);
+  else if (jobs.out_bf16) small_store<kN, true, false>(jobs, job, base, flat, pitch);
+  else small_store<kN, false, false>(jobs, job, base, flat, pitch);
 }
 
-// The workgroup that holds a matrix, as 3 (log2 NP - 5) + log2 JB; -1: none does.
+// The workgroup that holds a matrix, as 3 (log2 NP - 5) + log2 of the blocks of 32
+// columns that four waves would have; -1: none does.
 constexpr int kSmallClasses = 9;
 int small_class(int rows, int cols) {
   const int n = rows < cols ? rows : cols, L = rows < cols ? cols : rows;
@@ -752,9 +776,9 @@ int small_class(int rows, int cols) {
       if (L <= ((32 << b) * 4 >> p)) return 3 * p + b;   // 32 JB columns a wave, 4 / 2^p waves
   return -1;
 }
-template <int P, int B>
+template <int NP, int JB, int W>
 void small_kernel(const SmallJobs& j, hipStream_t st) {
-  hipLaunchKernelGGL((k_ns_small<(32 << P), (1 << B)>), dim3(j.first[SAGIPS_MAX_TENSORS]), dim3(kThreads), 0, st, j);
+  hipLaunchKernelGGL((k_ns_small<NP, JB, W>), dim3(j.first[SAGIPS_MAX_TENSORS]), dim3(64 * W), 0, st, j);
 }
 
 // ---- plan ---------------------------------------------------------------------------
@@ -918,15 +942,15 @@ static hipError_t launch_small(const MatrixJobs& js, int which, hipStream_t st, 
   j.eps = js.eps;
   if (tm) tm->begin("ns_small");
   switch (which) {
-    case 0: small_kernel<0, 0>(j, st); break;
-    case 1: small_kernel<0, 1>(j, st); break;
-    case 2: small_kernel<0, 2>(j, st); break;
-    case 3: small_kernel<1, 0>(j, st); break;
-    case 4: small_kernel<1, 1>(j, st); break;
-    case 5: small_kernel<1, 2>(j, st); break;
-    case 6: small_kernel<2, 0>(j, st); break;
-    case 7: small_kernel<2, 1>(j, st); break;
-    default: small_kernel<2, 2>(j, st); break;
+    case 0: small_kernel<32, 1, 4>(j, st); break;
+    case 1: small_kernel<32, 2, 4>(j, st); break;
+    case 2: small_kernel<32, 4, 4>(j, st); break;
+    case 3: small_kernel<64, 1, 4>(j, st); break;
+    case 4: small_kernel<64, 2, 4>(j, st); break;
+    case 5: small_kernel<64, 4, 4>(j, st); break;
+    case 6: small_kernel<128, 1, 4>(j, st); break;
+    case 7: small_kernel<128, 1, 8>(j, st); break;
+    default: small_kernel<128, 2, 8>(j, st); break;
   }
   if (tm) tm->end();
   return hipGetLastError();
