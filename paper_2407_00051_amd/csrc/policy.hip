@@ -26,25 +26,24 @@ __device__ __forceinline__ float clamp_event(float x) {
   return x > 1.0f - 0x1p-24f ? 1.0f - 0x1p-24f : x;
 }
 
-// 1 - x^a, from l2 = log2 x < 0.  Above x^a = 3/4 by the series of expm1 (its
-// first term left out is 4e-9 of the sum), so that no step cancels.
+// 1 - x^a, from l2 = log2 x < 0.  With t = a l2, 1 - 2^t = -t P(t): above 2^t = 3/4 by the
+// polynomial of degree 4 that interpolates P at the Chebyshev nodes of [log2 3/4, 0]
+// (relative error 1.3e-8 with these fp32 coefficients), so that no step cancels.
 __device__ __forceinline__ float one_minus_power(float a, float l2, float* w_out) {
-  const float t = a * l2, w = fast_exp2(t), y = t * kLn2;
-  float p = 1.0f / 5040.0f;
-  p = fmaf(p, y, 1.0f / 720.0f);
-  p = fmaf(p, y, 1.0f / 120.0f);
-  p = fmaf(p, y, 1.0f / 24.0f);
-  p = fmaf(p, y, 1.0f / 6.0f);
-  p = fmaf(p, y, 0.5f);
-  p = fmaf(p, y, 1.0f);
+  const float t = a * l2, w = fast_exp2(t);
+  float p = 0x1.364d2ep-10f;
+  p = fmaf(p, t, 0x1.396c7ap-7f);
+  p = fmaf(p, t, 0x1.c6a02cp-5f);
+  p = fmaf(p, t, 0x1.ebfbaap-3f);
+  p = fmaf(p, t, 0x1.62e430p-1f);
   *w_out = w;
-  return w < 0.75f ? 1.0f - w : -y * p;
+  return w < 0.75f ? 1.0f - w : -t * p;
 }
 
 // A row that the gradient is taken at, and one that its density is compared with.
 template <int D>
 struct Row {
-  float a[D], ra[D], rb[D], bm1[D], b[D];
+  float a[D], b[D], ra[D], rb[D], bm1[D];
 };
 template <int D>
 struct Against {
@@ -117,8 +116,8 @@ template <int D>
 __device__ __forceinline__ void add_grad(const Event<D>& e, const Row<D>& r, float wt, float* acc) {
 #pragma unroll
   for (int j = 0; j < D; ++j) {
-    const float k = fmaf(-r.bm1[j], e.q[j], 1.0f);
-    acc[2 * j] = fmaf(wt, fmaf(e.l2[j] * kLn2, k, r.ra[j]), acc[2 * j]);
+    const float k = fmaf(-kLn2 * r.bm1[j], e.q[j], kLn2);
+    acc[2 * j] = fmaf(wt, fmaf(e.l2[j], k, r.ra[j]), acc[2 * j]);
     acc[2 * j + 1] = fmaf(wt, fmaf(e.lg[j], kLn2, r.rb[j]), acc[2 * j + 1]);
   }
 }
@@ -139,7 +138,9 @@ __device__ __forceinline__ float exp_minus_line(float r) {
   p = fmaf(p, r, 1.0f / 24.0f);
   p = fmaf(p, r, 1.0f / 6.0f);
   p = fmaf(p, r, 0.5f);
-  return fabsf(r) < 0.5f ? r * r * p : fast_exp(r) - 1.0f - r;
+  float k = r * r * p;
+  if (__any(!(fabsf(r) < 0.5f))) k = fabsf(r) < 0.5f ? k : fast_exp(r) - 1.0f - r;   // rarely any lane
+  return k;
 }
 
 // Sum over groups of 2^lg neighbouring lanes, in every lane of the group.
@@ -179,12 +180,12 @@ __device__ __forceinline__ void block_sum_d(double (&v)[N]) {
 // so that a row of equal rewards gives zeros; deviations are formed in 64 bits
 // and rounded once.
 
-constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing
+constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing, at most
 constexpr int kAdvBlock = 1024;
 
 // A row in a group of 2^lg lanes (kBlock false; up to 64 x 16 events) or in a
 // workgroup (up to 1,024 x 16): read once, held in registers, written once.
-template <bool kBlock>
+template <bool kBlock, int kHeld>
 __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(const float* reward, const uint8_t* __restrict__ mask,
                                                                             int n_rows, int E, int lg, float eps, int normalise,
                                                                             float* adv) {
@@ -194,11 +195,11 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
   const int l = kBlock ? threadIdx.x : lane & (step - 1);
   const bool on = row < n_rows;
   const int64_t base = row * E;
-  float v[kAdvHeld];
+  float v[kHeld];
   uint32_t valid = 0;
   double t[2] = {0.0, 0.0};
 #pragma unroll
-  for (int i = 0; i < kAdvHeld; ++i) {
+  for (int i = 0; i < kHeld; ++i) {
     const int e = l + i * step;
     v[i] = 0.0f;
     if (on && e < E && (!mask || mask[base + e])) {
@@ -207,7 +208,7 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
     }
   }
 #pragma unroll
-  for (int i = 0; i < kAdvHeld; ++i) t[0] += (double)v[i];
+  for (int i = 0; i < kHeld; ++i) t[0] += (double)v[i];
   t[1] = (double)__popc(valid);
   if constexpr (kBlock) block_sum_d<2, kAdvBlock>(t);
   else
@@ -218,7 +219,7 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
   const double n = t[1], mean = n > 0.0 ? t[0] / n : 0.0;
   double q[1] = {0.0};
 #pragma unroll
-  for (int i = 0; i < kAdvHeld; ++i) {
+  for (int i = 0; i < kHeld; ++i) {
     v[i] = (valid >> i) & 1u ? (float)((double)v[i] - mean) : 0.0f;
     q[0] = fma((double)v[i], (double)v[i], q[0]);
   }
@@ -231,7 +232,7 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
     inv = 1.0f / (sd + eps);
   }
 #pragma unroll
-  for (int i = 0; i < kAdvHeld; ++i) {
+  for (int i = 0; i < kHeld; ++i) {
     const int e = l + i * step;
     if (on && e < E) adv[base + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
   }
@@ -302,15 +303,19 @@ __global__ __launch_bounds__(kAdvBlock) void k_adv_apply(const float* reward, co
 // ---- policy loss ---------------------------------------------------------------
 // A unit is one slice of one row, run by a group of 2^lg lanes (a wave, or less
 // where rows have fewer events).  It leaves its sums over valid events: of the
-// loss, the KL term, the clipped events and the events, and of the gradient.
+// loss, the KL term, the clipped events and the events, and of the gradient; where
+// a row has whole workgroups of slices, a workgroup's four units leave one record.
+// Bound by VALU issue: an event of three coordinates takes 30 transcendental and
+// about 200 other operations against two rows (1,024 x 16,384 events with mask and KL
+// term: see the figures in the commit of this file's last change).
 struct PolicyArgs {
   const float *theta, *theta_old, *theta_ref, *x, *adv;
   const uint8_t* mask;
   int64_t E, chunk, units;
-  int S, lg;
+  int S, lg, per_block;
   float lo, hi, beta;
-  float4* tot;   // [units]
-  float* grad;   // [units][2d]
+  float4* tot;   // [records]
+  float* grad;   // [records][2d]
 };
 
 template <int D, bool kRef>
@@ -349,6 +354,21 @@ __global__ __launch_bounds__(kThreads) void k_policy(PolicyArgs p) {
     add_grad<D>(ev, r, wt, acc);
   }
   group_sum(acc, p.lg);
+  if (p.per_block) {
+    __shared__ float sums[kWaves][2 * D + 4];
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < 2 * D + 4; ++j) sums[threadIdx.x >> 6][j] = acc[j];
+    __syncthreads();
+    if (threadIdx.x < 2 * D + 4) {
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) v += sums[w][threadIdx.x];
+      if (threadIdx.x < 2 * D) p.grad[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = v;
+      else reinterpret_cast<float*>(p.tot + blockIdx.x)[threadIdx.x - 2 * D] = v;
+    }
+    return;
+  }
   if (on && l == 0) {
     p.tot[unit] = make_float4(acc[2 * D], acc[2 * D + 1], acc[2 * D + 2], acc[2 * D + 3]);
 #pragma unroll
@@ -569,7 +589,7 @@ int lanes_log(int64_t n) {
 }
 
 struct PolicyPlan {
-  int lg, S;
+  int lg, S, per_block, records;   // records: of a row
   int64_t chunk, units;
   size_t grad_off, bytes;
 };
@@ -579,11 +599,13 @@ PolicyPlan policy_plan(int64_t rows, int64_t E, int d) {
   // slices of at least four events a lane
   const int64_t most = ceil_div(E, 256), want = kTargetUnits / rows;
   p.S = (int)(want < 1 ? 1 : want > most ? most : want);
-  p.chunk = ceil_div(E, p.S);
-  p.S = (int)ceil_div(E, p.chunk);
+  p.per_block = p.S >= kWaves;
+  if (p.per_block) p.S = p.S / kWaves * kWaves;
+  p.chunk = ceil_div(E, p.S);       // the last slices may be short or empty
   p.units = rows * p.S;
-  p.grad_off = align256((size_t)p.units * sizeof(float4));
-  p.bytes = p.grad_off + (size_t)p.units * 2 * d * sizeof(float);
+  p.records = p.per_block ? p.S / kWaves : p.S;
+  p.grad_off = align256((size_t)rows * p.records * sizeof(float4));
+  p.bytes = p.grad_off + (size_t)rows * p.records * 2 * d * sizeof(float);
   return p;
 }
 
@@ -619,7 +641,7 @@ unsigned wave_blocks(int64_t waves) { return (unsigned)ceil_div(waves, kWaves); 
 template <int D>
 hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x, const float* adv, const uint8_t* mask,
                     float* loss, float* kl, float* clip, float* dtheta, char* ws, hipStream_t st, Timer* tm) {
-  PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg,
+  PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg, pl.per_block,
                (float)(1.0 - P.clip_low), (float)(1.0 + P.clip_high), (float)P.kl_coef,
                reinterpret_cast<float4*>(ws), reinterpret_cast<float*>(ws + pl.grad_off)};
   const dim3 grid(wave_blocks(ceil_div(pl.units, 64 >> pl.lg)));
@@ -629,9 +651,9 @@ hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  PolicyFinish f{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.S, P.average == SAGIPS_MEAN_ROWS, mask != nullptr,
+  PolicyFinish f{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, P.average == SAGIPS_MEAN_ROWS, mask != nullptr,
                  loss, kl, clip, dtheta};
-  const int64_t blocks = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
+  const int64_t blocks = pl.records == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
   if (tm) tm->begin("policy_finish");
   hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, f);
   if (tm) tm->end();
@@ -703,11 +725,12 @@ hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_
     // the fewest lanes that hold a row, but a lane for every event up to 64
     const int lg = lanes_log(E);
     const int64_t waves = ceil_div(n_rows, 64 >> lg);
-    hipLaunchKernelGGL((k_advantage<false>), dim3(wave_blocks(waves)), dim3(kThreads), 0, st, reward, mask, (int)n_rows,
-                       (int)E, lg, eps, (int)normalise, adv);
+    const auto kernel = E <= 64 ? k_advantage<false, 1> : E <= 256 ? k_advantage<false, 4> : k_advantage<false, kAdvHeld>;
+    hipLaunchKernelGGL(kernel, dim3(wave_blocks(waves)), dim3(kThreads), 0, st, reward, mask, (int)n_rows, (int)E, lg, eps,
+                       (int)normalise, adv);
   } else if (E <= kAdvBlock * kAdvHeld) {
     const int threads = (int)(ceil_div(E, 64 * kAdvHeld) * 64);
-    hipLaunchKernelGGL((k_advantage<true>), dim3((unsigned)n_rows), dim3(threads), 0, st, reward, mask, (int)n_rows, (int)E,
+    hipLaunchKernelGGL((k_advantage<true, kAdvHeld>), dim3((unsigned)n_rows), dim3(threads), 0, st, reward, mask, (int)n_rows, (int)E,
                        6, eps, (int)normalise, adv);
   } else {
     const int slices = (int)ceil_div(E, kAdvSlice);
