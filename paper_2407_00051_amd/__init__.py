@@ -161,9 +161,15 @@ def _ptr(t) -> Optional[int]:
 
 
 def _check_tensor(t, name, dtype=None, shape=None, device=None):
-    import torch
     if t is None:
         return
+    try:                        # the usual case first; what fails here is named below
+        if (t.is_cuda and (device is None or t.get_device() == device) and t.is_contiguous()
+                and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape)):
+            return
+    except (AttributeError, TypeError):
+        pass
+    import torch
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
     if not t.is_cuda:
@@ -176,6 +182,15 @@ def _check_tensor(t, name, dtype=None, shape=None, device=None):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if shape is not None and t.shape != shape and tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _raw_stream(device: int) -> int:
+    """The handle of torch's current stream of the device."""
+    import torch
+    try:
+        return torch._C._cuda_getCurrentRawStream(device)
+    except AttributeError:
+        return torch.cuda.current_stream(device).cuda_stream
 
 
 class Context:
@@ -196,6 +211,7 @@ class Context:
         if stream is None:
             stream = torch.cuda.current_stream(device)
         self._stream = stream
+        self._raw = stream.cuda_stream
         h = ctypes.c_void_p()
         st = self.lib.sagips_create(ctypes.byref(h), device, ctypes.c_void_p(stream.cuda_stream))
         if st != OK:
@@ -226,19 +242,21 @@ class Context:
         """Run later calls on `stream` (and stop following torch's current stream)."""
         self._check(self.lib.sagips_set_stream(self.h, ctypes.c_void_p(stream.cuda_stream)))
         self._stream = stream
+        self._raw = stream.cuda_stream
         self._follow = False
 
     def _enter(self):
         """Before a call: in follow mode, switch to torch's current stream if it changed."""
-        if self._follow:
+        if self._follow and _raw_stream(self.device) != self._raw:
             import torch
             cur = torch.cuda.current_stream(self.device)
-            if cur.cuda_stream != self._stream.cuda_stream:
-                self._check(self.lib.sagips_set_stream(self.h, ctypes.c_void_p(cur.cuda_stream)))
-                self._stream = cur
+            self._check(self.lib.sagips_set_stream(self.h, ctypes.c_void_p(cur.cuda_stream)))
+            self._stream = cur
+            self._raw = cur.cuda_stream
 
     def _owned(self, *tensors):
-        """Outputs the binding allocated on torch's current stream, used by the library's stream."""
+        """Tensors that belong to torch's current stream (outputs the binding allocated there, inputs
+        that the caller may drop), used by the library's stream."""
         if self._follow:
             return
         import torch
@@ -555,8 +573,7 @@ class Context:
         adv = out if out is not None else torch.empty_like(reward)
         if out is not None:
             _check_tensor(out, "out", torch.float32, reward.shape, self.device)
-        else:
-            self._owned(adv)
+        self._owned(adv if out is None else None, reward, mask)
         self._check(self.lib.sagips_group_advantage(self.h, reward.data_ptr(), m, reward.shape[0], reward.shape[1],
                                                     1 if normalise else 0, eps, adv.data_ptr()))
         return adv
@@ -586,7 +603,7 @@ class Context:
                    MEAN_ROWS if average == "rows" else MEAN_EVENTS)
         scalars = torch.empty(3, dtype=f32, device=theta.device)
         dtheta = torch.empty_like(theta) if want_grad else None
-        self._owned(scalars, dtheta)
+        self._owned(scalars, dtheta, theta, theta_old, theta_ref, x, adv, mask)
         at = scalars.data_ptr()
         self._check(self.lib.sagips_policy_loss(self.h, ctypes.byref(P), x.data_ptr(), adv.data_ptr(), m, at, at + 4,
                                                 at + 8, _ptr(dtheta)))
@@ -617,7 +634,7 @@ class Context:
         loss = torch.empty(1, dtype=f32, device=theta.device)
         margin = torch.empty(P, dtype=f32, device=theta.device)
         dtheta = torch.empty_like(theta) if want_grad else None
-        self._owned(loss, margin, dtheta)
+        self._owned(loss, margin, dtheta, theta, theta_ref, chosen, rejected, len_chosen, len_rejected)
         self._check(self.lib.sagips_preference_loss(self.h, ctypes.byref(a), chosen.data_ptr(), _ptr(len_chosen),
                                                     rejected.data_ptr(), _ptr(len_rejected), loss.data_ptr(),
                                                     margin.data_ptr(), _ptr(dtheta)))
@@ -645,10 +662,9 @@ class Context:
         o = out if out is not None else torch.empty_like(x)
         if out is not None:
             _check_tensor(out, "out", x.dtype, x.shape, self.device)
-        else:
-            self._owned(o)
         if steps < 1:
             raise ValueError("steps must be >= 1")
+        self._owned(o if out is None else None, x)
         ns = NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps)
         self._check(self.lib.sagips_orthogonalise(self.h, ctypes.byref(ns), F32 if x.dtype == torch.float32 else BF16,
                                                   x.data_ptr(), count, rows, cols, o.data_ptr()))
@@ -679,6 +695,7 @@ class Context:
             _check_tensor(momenta[i], f"momenta[{i}]", torch.float32, p.shape, self.device)
             ms.count[i], ms.rows[i], ms.cols[i] = self._stack(p)
             ms.param[i], ms.grad[i], ms.m[i] = p.data_ptr(), grads[i].data_ptr(), momenta[i].data_ptr()
+        self._owned(params, grads, momenta)
         o = Muon(lr, momentum, weight_decay, 1 if nesterov else 0, scale,
                  NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps))
         self._check(self.lib.sagips_muon_step(self.h, ctypes.byref(ms), ctypes.byref(o)))
