@@ -215,6 +215,7 @@ sagips_status sagips_destroy(sagips_ctx* c) {
     DeviceGuard g(c->device);
     (void)hipStreamSynchronize(c->stream);
     if (c->ws) (void)hipFree(c->ws);
+    if (c->ticket) (void)hipFree(c->ticket);
   }
   delete c;
   return SAGIPS_OK;

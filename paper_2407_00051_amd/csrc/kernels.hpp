@@ -94,16 +94,19 @@ hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double b
                        hipStream_t st, Timer* tm);
 
 // policy.hip -----------------------------------------------------------------
+// `ticket`: one counter on the device, 0 before and after every launch that uses it.
+hipError_t launch_clear(uint32_t* p, hipStream_t st);
 size_t advantage_workspace(int64_t n_rows, int64_t E);
 hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,
                             float* adv, void* ws, hipStream_t st, Timer* tm);
 size_t policy_workspace(const sagips_policy& P);
 hipError_t launch_policy(const sagips_policy& P, const float* x, const float* adv, const uint8_t* mask, float* loss,
-                         float* kl, float* clip_frac, float* dtheta, void* ws, hipStream_t st, Timer* tm);
+                         float* kl, float* clip_frac, float* dtheta, void* ws, uint32_t* ticket, hipStream_t st,
+                         Timer* tm);
 size_t preference_workspace(const sagips_preference& P);
 hipError_t launch_preference(const sagips_preference& P, const float* chosen, const int32_t* n_chosen,
                              const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta,
-                             void* ws, hipStream_t st, Timer* tm);
+                             void* ws, uint32_t* ticket, hipStream_t st, Timer* tm);
 
 // muon.hip -------------------------------------------------------------------
 struct MatrixJob {

@@ -301,6 +301,102 @@ __global__ __launch_bounds__(kAdvBlock) void k_adv_apply(const float* reward, co
 }
 
 // ---- policy loss ---------------------------------------------------------------
+// Whether this workgroup is the last of its launch to come here, all the others' global
+// writes before it visible: one counter of the context, which the last puts back to 0.
+// Only which workgroup is last depends on the order, not what it computes.
+__device__ __forceinline__ bool last_block(uint32_t* ticket) {
+  __shared__ uint32_t turn;
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");   // every wave's own writes, before the workgroup is counted
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    turn = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    if (turn == gridDim.x - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  if (turn != gridDim.x - 1) return false;
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+  return true;
+}
+
+// Joins the units' sums in 64 bits and applies the average.  Every workgroup
+// forms the totals that its rows' weights need; the first writes the scalars.  Run by a
+// launch of its own, or by the last workgroup of k_policy.
+struct PolicyFinish {
+  const float4* tot;
+  const float* grad;
+  int64_t rows, E;
+  int S, by_rows, masked;
+  float *loss, *kl, *clip, *dtheta;
+};
+template <int D>
+__device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, int blocks) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
+  if (p.masked || block == 0) {
+    if (p.by_rows && p.S > 1) {        // a wave per row
+      for (int64_t row = wave; row < p.rows; row += kWaves) {
+        double u[4] = {};
+        for (int s = lane; s < p.S; s += 64) {
+          const float4 v = p.tot[row * p.S + s];
+          u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = wave_sum_d(u[i]);
+        if (lane == 0 && u[3] > 0.0) {
+          for (int i = 0; i < 4; ++i) t[i] += u[i] / u[3];
+          t[4] += 1.0;
+        }
+      }
+    } else {
+      for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) {
+        const float4 v = p.tot[k];
+        const double w = !p.by_rows ? 1.0 : v.w > 0.0f ? 1.0 / v.w : 0.0;
+        t[0] += w * v.x; t[1] += w * v.y; t[2] += w * v.z; t[3] += w * v.w;
+        t[4] += v.w > 0.0f ? 1.0 : 0.0;
+      }
+    }
+    block_sum_d<5, kThreads>(t);
+  }
+  const double all = p.by_rows ? (p.masked ? t[4] : (double)p.rows) : (p.masked ? t[3] : (double)p.rows * (double)p.E);
+  const double inv = all > 0.0 ? 1.0 / all : 0.0;
+  if (block == 0 && threadIdx.x == 0) {
+    if (p.loss) *p.loss = (float)(t[0] * inv);
+    if (p.kl) *p.kl = (float)(t[1] * inv);
+    if (p.clip) *p.clip = (float)(t[2] * inv);
+  }
+  if (!p.dtheta) return;
+  if (p.S == 1) {
+    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)blocks * kThreads) {
+      double w = inv;
+      if (p.by_rows) {
+        const float n = p.masked ? p.tot[k / (2 * D)].w : (float)p.E;
+        w = n > 0.0f ? inv / n : 0.0;
+      }
+      p.dtheta[k] = (float)(p.grad[k] * w);
+    }
+    return;
+  }
+  for (int64_t row = (int64_t)block * kWaves + wave; row < p.rows; row += (int64_t)blocks * kWaves) {
+    double u[2 * D + 1] = {};
+    for (int s = lane; s < p.S; s += 64) {
+      const int64_t k = row * p.S + s;
+      u[2 * D] += p.tot[k].w;
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) u[j] += p.grad[k * 2 * D + j];
+    }
+#pragma unroll
+    for (int j = 0; j < 2 * D + 1; ++j) u[j] = wave_sum_d(u[j]);
+    const double w = !p.by_rows ? inv : u[2 * D] > 0.0 ? inv / u[2 * D] : 0.0;
+    if (lane == 0)
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
+  }
+}
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
+  policy_finish<D>(p, blockIdx.x, gridDim.x);
+}
+
 // A unit is one slice of one row, run by a group of 2^lg lanes (a wave, or less
 // where rows have fewer events).  It leaves its sums over valid events: of the
 // loss, the KL term, the clipped events and the events, and of the gradient; where
@@ -316,6 +412,8 @@ struct PolicyArgs {
   float lo, hi, beta;
   float4* tot;   // [records]
   float* grad;   // [records][2d]
+  uint32_t* ticket;   // or NULL: a launch of k_policy_finish follows
+  PolicyFinish fin;
 };
 
 template <int D, bool kRef>
@@ -367,90 +465,56 @@ __global__ __launch_bounds__(kThreads) void k_policy(PolicyArgs p) {
       if (threadIdx.x < 2 * D) p.grad[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = v;
       else reinterpret_cast<float*>(p.tot + blockIdx.x)[threadIdx.x - 2 * D] = v;
     }
-    return;
-  }
-  if (on && l == 0) {
+  } else if (on && l == 0) {
     p.tot[unit] = make_float4(acc[2 * D], acc[2 * D + 1], acc[2 * D + 2], acc[2 * D + 3]);
 #pragma unroll
     for (int j = 0; j < 2 * D; ++j) p.grad[unit * 2 * D + j] = acc[j];
   }
+  if (p.ticket && last_block(p.ticket)) policy_finish<D>(p.fin, 0, 1);
 }
 
-// Joins the units' sums in 64 bits and applies the average.  Every workgroup
-// forms the totals that its rows' weights need; the first writes the scalars.
-struct PolicyFinish {
-  const float4* tot;
-  const float* grad;
-  int64_t rows, E;
-  int S, by_rows, masked;
-  float *loss, *kl, *clip, *dtheta;
+// ---- preference loss -----------------------------------------------------------
+// Joins the units' sums in 64 bits; as policy_finish.
+struct PrefFinish {
+  const float* in;            // [rows][S][2d + 1]
+  int64_t rows;
+  int S;
+  double beta, inv_pairs;
+  float *loss, *dtheta;
 };
 template <int D>
-__global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
+__device__ __forceinline__ void pref_finish(const PrefFinish& p, int block, int blocks) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
-  if (p.masked || blockIdx.x == 0) {
-    if (p.by_rows && p.S > 1) {        // a wave per row
-      for (int64_t row = wave; row < p.rows; row += kWaves) {
-        double u[4] = {};
-        for (int s = lane; s < p.S; s += 64) {
-          const float4 v = p.tot[row * p.S + s];
-          u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = wave_sum_d(u[i]);
-        if (lane == 0 && u[3] > 0.0) {
-          for (int i = 0; i < 4; ++i) t[i] += u[i] / u[3];
-          t[4] += 1.0;
-        }
-      }
-    } else {
-      for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) {
-        const float4 v = p.tot[k];
-        const double w = !p.by_rows ? 1.0 : v.w > 0.0f ? 1.0 / v.w : 0.0;
-        t[0] += w * v.x; t[1] += w * v.y; t[2] += w * v.z; t[3] += w * v.w;
-        t[4] += v.w > 0.0f ? 1.0 : 0.0;
-      }
-    }
-    block_sum_d<5, kThreads>(t);
-  }
-  const double all = p.by_rows ? (p.masked ? t[4] : (double)p.rows) : (p.masked ? t[3] : (double)p.rows * (double)p.E);
-  const double inv = all > 0.0 ? 1.0 / all : 0.0;
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    if (p.loss) *p.loss = (float)(t[0] * inv);
-    if (p.kl) *p.kl = (float)(t[1] * inv);
-    if (p.clip) *p.clip = (float)(t[2] * inv);
+  if (block == 0 && p.loss) {
+    double t[1] = {0.0};
+    for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) t[0] += p.in[k * (2 * D + 1) + 2 * D];
+    block_sum_d<1, kThreads>(t);
+    if (threadIdx.x == 0) *p.loss = (float)(t[0] * p.inv_pairs);
   }
   if (!p.dtheta) return;
+  const double w = p.beta * p.inv_pairs;
   if (p.S == 1) {
-    for (int64_t k = (int64_t)blockIdx.x * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)gridDim.x * kThreads) {
-      double w = inv;
-      if (p.by_rows) {
-        const float n = p.masked ? p.tot[k / (2 * D)].w : (float)p.E;
-        w = n > 0.0f ? inv / n : 0.0;
-      }
-      p.dtheta[k] = (float)(p.grad[k] * w);
-    }
+    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)blocks * kThreads)
+      p.dtheta[k] = (float)(p.in[k / (2 * D) * (2 * D + 1) + k % (2 * D)] * w);
     return;
   }
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < p.rows; row += (int64_t)gridDim.x * kWaves) {
-    double u[2 * D + 1] = {};
-    for (int s = lane; s < p.S; s += 64) {
-      const int64_t k = row * p.S + s;
-      u[2 * D] += p.tot[k].w;
+  for (int64_t row = (int64_t)block * kWaves + wave; row < p.rows; row += (int64_t)blocks * kWaves) {
+    double u[2 * D] = {};
+    for (int s = lane; s < p.S; s += 64)
 #pragma unroll
-      for (int j = 0; j < 2 * D; ++j) u[j] += p.grad[k * 2 * D + j];
-    }
+      for (int j = 0; j < 2 * D; ++j) u[j] += p.in[(row * p.S + s) * (2 * D + 1) + j];
 #pragma unroll
-    for (int j = 0; j < 2 * D + 1; ++j) u[j] = wave_sum_d(u[j]);
-    const double w = !p.by_rows ? inv : u[2 * D] > 0.0 ? inv / u[2 * D] : 0.0;
+    for (int j = 0; j < 2 * D; ++j) u[j] = wave_sum_d(u[j]);
     if (lane == 0)
 #pragma unroll
       for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
   }
 }
+template <int D>
+__global__ __launch_bounds__(kThreads) void k_pref_finish(PrefFinish p) {
+  pref_finish<D>(p, blockIdx.x, gridDim.x);
+}
 
-// ---- preference loss -----------------------------------------------------------
 // A pair's sums over its two sets, chosen minus rejected: of the log2 ratios and
 // of dl/dtheta; both are linear, so one pass over the events gives the margin
 // and, once it is known, the gradient.
@@ -462,11 +526,12 @@ struct PrefArgs {
   int64_t pairs, chunk, units;   // pairs a row; pairs (or, k_pref_slices, events) a unit
   int S, lg;
   float beta, eps;
-  double inv_pairs;           // 1 / all pairs
   float* margin;              // or NULL
   const float* part;          // k_pref<D, true>: [all pairs][slices][2d + 1]
   int slices;
   float* out;                 // [units][2d + 1] (gradient, loss), or the slices' part
+  uint32_t* ticket;           // or NULL: a launch of k_pref_finish follows, or nothing
+  PrefFinish fin;
 };
 
 template <int D>
@@ -494,11 +559,11 @@ template <int D, bool kJoin>
 __global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
   const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
   const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
-  if (unit >= p.units) return;   // the whole wave
-  const int64_t row = unit / p.S, s = unit % p.S;
+  const bool any = unit < p.units;   // of the whole wave
+  const int64_t row = any ? unit / p.S : 0, s = any ? unit % p.S : 0;
   const Row<D> r = load_row<D>(p.theta + row * 2 * D);
   const Against<D> ref = load_against<D>(p.theta_ref + row * 2 * D, r);
-  const int64_t q0 = s * p.chunk, q1 = min(p.pairs, q0 + p.chunk);
+  const int64_t q0 = s * p.chunk, q1 = any ? min(p.pairs, q0 + p.chunk) : 0;
   float acc[2 * D + 1] = {};
   for (int64_t q = q0; q < q1; q += 64 >> p.lg) {
     const int64_t mine = q + (lane >> p.lg), pair = row * p.pairs + mine;
@@ -529,9 +594,10 @@ __global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
     }
   }
   group_sum(acc, 6);
-  if (lane == 0)
+  if (any && lane == 0)
 #pragma unroll
     for (int j = 0; j < 2 * D + 1; ++j) p.out[unit * (2 * D + 1) + j] = acc[j];
+  if (p.ticket && last_block(p.ticket)) pref_finish<D>(p.fin, 0, 1);
 }
 
 // Long sets: a unit is a wave on one slice of one pair's sets.
@@ -552,31 +618,13 @@ __global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
     for (int j = 0; j < 2 * D + 1; ++j) p.out[unit * (2 * D + 1) + j] = v[j];
 }
 
-template <int D>
-__global__ __launch_bounds__(kThreads) void k_pref_finish(const float* __restrict__ in, int64_t rows, int S, double beta,
-                                                          double inv_pairs, float* loss, float* dtheta) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (blockIdx.x == 0 && loss) {
-    double t[1] = {0.0};
-    for (int64_t k = threadIdx.x; k < rows * S; k += kThreads) t[0] += in[k * (2 * D + 1) + 2 * D];
-    block_sum_d<1, kThreads>(t);
-    if (threadIdx.x == 0) *loss = (float)(t[0] * inv_pairs);
-  }
-  if (!dtheta) return;
-  for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < rows; row += (int64_t)gridDim.x * kWaves) {
-    double u[2 * D] = {};
-    for (int s = lane; s < S; s += 64)
-#pragma unroll
-      for (int j = 0; j < 2 * D; ++j) u[j] += in[(row * S + s) * (2 * D + 1) + j];
-#pragma unroll
-    for (int j = 0; j < 2 * D; ++j) u[j] = wave_sum_d(u[j]);
-    if (lane == 0)
-#pragma unroll
-      for (int j = 0; j < 2 * D; ++j) dtheta[row * 2 * D + j] = (float)(u[j] * (beta * inv_pairs));
-  }
-}
-
 // ---- plans ---------------------------------------------------------------------
+// Whether a launch ends in its last workgroup instead of in a second launch: where that has
+// few rows to join (one row of 16,384 events 12.9 us against 17.1; with 1,024 rows, one
+// workgroup's loads one after the other, 36 against 18.6, and 279 against 16.6 for pairs).
+bool ends_in_last(int64_t blocks, int64_t rows, int records, int d) {
+  return blocks <= 512 && (records == 1 ? rows * 2 * d <= 2 * kThreads : rows <= 2 * kWaves);
+}
 constexpr int64_t kTargetUnits = 8192;   // waves that fill the device: 256 compute units x 32
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -640,22 +688,24 @@ unsigned wave_blocks(int64_t waves) { return (unsigned)ceil_div(waves, kWaves); 
 
 template <int D>
 hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x, const float* adv, const uint8_t* mask,
-                    float* loss, float* kl, float* clip, float* dtheta, char* ws, hipStream_t st, Timer* tm) {
-  PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg, pl.per_block,
-               (float)(1.0 - P.clip_low), (float)(1.0 + P.clip_high), (float)P.kl_coef,
-               reinterpret_cast<float4*>(ws), reinterpret_cast<float*>(ws + pl.grad_off)};
+                    float* loss, float* kl, float* clip, float* dtheta, char* ws, uint32_t* ticket, hipStream_t st,
+                    Timer* tm) {
+  PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg,
+               pl.per_block, (float)(1.0 - P.clip_low), (float)(1.0 + P.clip_high), (float)P.kl_coef,
+               reinterpret_cast<float4*>(ws), reinterpret_cast<float*>(ws + pl.grad_off), nullptr, {}};
+  a.fin = PolicyFinish{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, P.average == SAGIPS_MEAN_ROWS,
+                       mask != nullptr, loss, kl, clip, dtheta};
   const dim3 grid(wave_blocks(ceil_div(pl.units, 64 >> pl.lg)));
+  if (ends_in_last(grid.x, P.n_theta, pl.records, D)) a.ticket = ticket;
   if (tm) tm->begin("policy");
   if (P.theta_ref) hipLaunchKernelGGL((k_policy<D, true>), grid, dim3(kThreads), 0, st, a);
   else hipLaunchKernelGGL((k_policy<D, false>), grid, dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  PolicyFinish f{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, P.average == SAGIPS_MEAN_ROWS, mask != nullptr,
-                 loss, kl, clip, dtheta};
+  if (e != hipSuccess || a.ticket) return e;
   const int64_t blocks = pl.records == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
   if (tm) tm->begin("policy_finish");
-  hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, f);
+  hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, a.fin);
   if (tm) tm->end();
   return hipGetLastError();
 }
@@ -663,7 +713,7 @@ hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x
 template <int D>
 hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* chosen, const int32_t* n_chosen,
                   const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta, char* ws,
-                  hipStream_t st, Timer* tm) {
+                  uint32_t* ticket, hipStream_t st, Timer* tm) {
   const int64_t all = (int64_t)P.n_theta * P.pairs_per_theta;
   PrefArgs a{};
   a.theta = P.theta;
@@ -677,7 +727,6 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
   a.pairs = P.pairs_per_theta;
   a.beta = (float)P.beta;
   a.eps = (float)P.label_smoothing;
-  a.inv_pairs = 1.0 / (double)all;
   a.margin = margin;
   a.slices = pl.slices;
   float* sums = reinterpret_cast<float*>(ws);
@@ -698,21 +747,30 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
   a.lg = pl.lg;
   a.part = part;
   a.out = sums;
+  a.fin = PrefFinish{sums, P.n_theta, pl.S, P.beta, 1.0 / (double)all, loss, dtheta};
+  const unsigned blocks = wave_blocks(pl.units);
+  const bool finish = loss || dtheta;
+  if (finish && ends_in_last(blocks, P.n_theta, pl.S, D)) a.ticket = ticket;
   if (tm) tm->begin("preference");
-  if (pl.slices) hipLaunchKernelGGL((k_pref<D, true>), dim3(wave_blocks(pl.units)), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_pref<D, false>), dim3(wave_blocks(pl.units)), dim3(kThreads), 0, st, a);
+  if (pl.slices) hipLaunchKernelGGL((k_pref<D, true>), dim3(blocks), dim3(kThreads), 0, st, a);
+  else hipLaunchKernelGGL((k_pref<D, false>), dim3(blocks), dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || (!loss && !dtheta)) return e;
-  const int64_t blocks = ceil_div(P.n_theta, kWaves);
+  if (e != hipSuccess || !finish || a.ticket) return e;
+  const int64_t n = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
   if (tm) tm->begin("preference_finish");
-  hipLaunchKernelGGL((k_pref_finish<D>), dim3((unsigned)(blocks > 4096 ? 4096 : blocks)), dim3(kThreads), 0, st, sums,
-                     P.n_theta, pl.S, P.beta, a.inv_pairs, loss, dtheta);
+  hipLaunchKernelGGL((k_pref_finish<D>), dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(kThreads), 0, st, a.fin);
   if (tm) tm->end();
   return hipGetLastError();
 }
 
 }  // namespace
+
+static __global__ void k_clear(uint32_t* p) { *p = 0u; }
+hipError_t launch_clear(uint32_t* p, hipStream_t st) {
+  hipLaunchKernelGGL(k_clear, dim3(1), dim3(1), 0, st, p);
+  return hipGetLastError();
+}
 
 size_t advantage_workspace(int64_t n_rows, int64_t E) {
   return E <= kAdvSlice ? 0 : (size_t)n_rows * ceil_div(E, kAdvSlice) * 3 * sizeof(double);
@@ -750,11 +808,12 @@ hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_
 size_t policy_workspace(const sagips_policy& P) { return policy_plan(P.n_theta, P.events_per_theta, P.d).bytes; }
 
 hipError_t launch_policy(const sagips_policy& P, const float* x, const float* adv, const uint8_t* mask, float* loss,
-                         float* kl, float* clip_frac, float* dtheta, void* ws, hipStream_t st, Timer* tm) {
+                         float* kl, float* clip_frac, float* dtheta, void* ws, uint32_t* ticket, hipStream_t st,
+                         Timer* tm) {
   const PolicyPlan pl = policy_plan(P.n_theta, P.events_per_theta, P.d);
   char* w = static_cast<char*>(ws);
-  return P.d == 2 ? policy_d<2>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, st, tm)
-                  : policy_d<3>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, st, tm);
+  return P.d == 2 ? policy_d<2>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, ticket, st, tm)
+                  : policy_d<3>(P, pl, x, adv, mask, loss, kl, clip_frac, dtheta, w, ticket, st, tm);
 }
 
 static PrefPlan plan_of(const sagips_preference& P) {
@@ -765,11 +824,11 @@ size_t preference_workspace(const sagips_preference& P) { return plan_of(P).byte
 
 hipError_t launch_preference(const sagips_preference& P, const float* chosen, const int32_t* n_chosen,
                              const float* rejected, const int32_t* n_rejected, float* loss, float* margin, float* dtheta,
-                             void* ws, hipStream_t st, Timer* tm) {
+                             void* ws, uint32_t* ticket, hipStream_t st, Timer* tm) {
   const PrefPlan pl = plan_of(P);
   char* w = static_cast<char*>(ws);
-  return P.d == 2 ? pref_d<2>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, st, tm)
-                  : pref_d<3>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, st, tm);
+  return P.d == 2 ? pref_d<2>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, ticket, st, tm)
+                  : pref_d<3>(P, pl, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, w, ticket, st, tm);
 }
 
 }  // namespace sagips
