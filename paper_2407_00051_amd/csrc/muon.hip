@@ -258,12 +258,13 @@ __device__ __forceinline__ void write_block(u16* at, const f32x16& v, float scal
 }
 
 template <int kMode, int TB>
-__global__ __launch_bounds__(kThreads, TB == 2 ? 2 : 1) void k_ns_gemm(GemmArgs g, Jobs jobs) {
+__global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs g, Jobs jobs) {
   constexpr bool kSym = kMode == kGram || kMode == kPoly;
-  constexpr int kDepth = TB == 4 ? 3 : 4;
+  constexpr int kDepth = TB == 4 ? 3 : TB == 3 ? 4 : 2;
   constexpr int OB = (TB * TB + 3) / 4;                // blocks a wave keeps: x TB + y in [wave OB, wave OB + OB)
   constexpr int PB = OB == 4 ? 2 : 1;                  // of them added at a time
-  __shared__ __attribute__((aligned(16))) f32x4 sums[4][4][PB][4][64];   // [from][to][block][quad of values][lane]
+  constexpr int QB = TB == 2 ? 2 : 4;                  // quads of their values at a time
+  __shared__ __attribute__((aligned(16))) f32x4 sums[4][4][PB][QB][64];   // [from][to][block][quad of values][lane]
   const int lane = threadIdx.x & 63, lr = lane & 31, lh = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int z, ti, tj;
@@ -320,28 +321,32 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 2 : 1) void k_ns_gemm(GemmArgs 
   // the four quarters of K, in the waves' order
   f32x16 o[OB];
 #pragma unroll
-  for (int pass = 0; pass < OB / PB; ++pass) {
+  for (int pass = 0; pass < OB / PB * (4 / QB); ++pass) {
+    const int b0 = pass / (4 / QB) * PB, q0 = pass % (4 / QB) * QB;
     if (pass) __syncthreads();
 #pragma unroll
     for (int to = 0; to < 4; ++to)
 #pragma unroll
       for (int b = 0; b < PB; ++b) {
-        const int at = to * OB + pass * PB + b;
+        const int at = to * OB + b0 + b;
         if (at >= TB * TB) continue;
         const f32x16& v = c[at / TB][at % TB];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sums[wave][to][b][q][lane] = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        for (int q = 0; q < QB; ++q) {
+          const int r = 4 * (q0 + q);
+          sums[wave][to][b][q][lane] = f32x4{v[r], v[r + 1], v[r + 2], v[r + 3]};
+        }
       }
     __syncthreads();
 #pragma unroll
     for (int b = 0; b < PB; ++b)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < QB; ++q) {
         f32x4 v = sums[0][wave][b][q][lane];
 #pragma unroll
         for (int w = 1; w < 4; ++w) v += sums[w][wave][b][q][lane];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[pass * PB + b][4 * q + e] = v[e];
+        for (int e = 0; e < 4; ++e) o[b0 + b][4 * (q0 + q) + e] = v[e];
       }
   }
   __syncthreads();
