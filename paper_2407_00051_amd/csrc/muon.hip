@@ -184,6 +184,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
   for (int q = threadIdx.x >> 6; q < 16; q += kThreads / 64) {   // 8 fragments of either kind
     const bool down = q >= 8;
     const int rb = (q >> 2) & 1, ks = q & 3;
+    if ((down ? l0 : i0) + 32 * rb >= (down ? lp : np) || (down ? i0 : l0) + 16 * ks >= (down ? np : lp)) continue;
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
@@ -275,10 +276,10 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
   int64_t P[TB], Q[TB];                                // offsets of the wave's first fragments
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
-    P[b] = z * pp + frag_at(min(ti * TB + b, ni - 1), wave, g.kp);
-    Q[b] = z * qp + frag_at(min(tj * TB + b, nj - 1), wave, g.kp);
+    P[b] = z * pp + frag_at(min(ti * TB + b, ni - 1), min(wave, g.kp / 16 - 1), g.kp);
+    Q[b] = z * qp + frag_at(min(tj * TB + b, nj - 1), min(wave, g.kp / 16 - 1), g.kp);
   }
-  const int steps = g.kp / 64;                         // of this wave: every fourth
+  const int steps = (g.kp / 16 - wave + 3) / 4;        // of this wave: every fourth, none if there are fewer than four
 
   const uint32_t lane16 = lane * 16;
   struct Frags {
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
   Frags f[kDepth];
   f32x16 c[TB][TB] = {};                               // [block of j][block of i], 2^24 times the product
   const auto fetch = [&](int k, Frags& o) __attribute__((always_inline)) {
-    const int64_t at = (int64_t)min(k, steps - 1) * (4 * kT * kFrag);
+    const int64_t at = (int64_t)max(0, min(k, steps - 1)) * (4 * kT * kFrag);
 #pragma unroll
     for (int b = 0; b < TB; ++b)
 #pragma unroll
@@ -799,8 +800,8 @@ Plan plan_of(int rows, int cols, int mats) {
   p.n = rows < cols ? rows : cols;
   p.L = rows < cols ? cols : rows;
   p.mats = mats;
-  p.np = (int)round_up(p.n, 64);
-  p.lp = (int)round_up(p.L, 64);
+  p.np = (int)round_up(p.n, 32);
+  p.lp = (int)round_up(p.L, 32);
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
   const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
@@ -858,7 +859,7 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws,
   hipLaunchKernelGGL(k_ns_norm, dim3((unsigned)p.mats * p.chunks), dim3(kThreads), 0, st, j, p.chunks, part);
   if (tm) tm->end();
   if (tm) tm->begin("ns_split");
-  hipLaunchKernelGGL(k_ns_split, dim3(p.lp / 64, p.np / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
+  hipLaunchKernelGGL(k_ns_split, dim3((p.lp + 63) / 64, (p.np + 63) / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
                      p.np, p.lp);
   if (tm) tm->end();
   const int gram = tile_side(true, p.np, p.np, p.lp, p.mats, n_cu), poly = tile_side(true, p.np, p.np, p.np, p.mats, n_cu);
