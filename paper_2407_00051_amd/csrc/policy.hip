@@ -162,6 +162,10 @@ __device__ __forceinline__ void group_sum(float (&v)[N], int lg) {
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], 1 << s, 64);
 }
 
+__device__ __forceinline__ double group_sum_d(double v, int lg) {
+  for (int s = 0; s < lg; ++s) v += __shfl_xor(v, 1 << s, 64);
+  return v;
+}
 __device__ __forceinline__ double wave_sum_d(double v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
@@ -336,25 +340,29 @@ struct PolicyFinish {
   const float4* tot;
   const float* grad;
   int64_t rows, E;
-  int S, by_rows, masked;
+  int S, lg, by_rows, masked;   // 2^lg lanes take a row's records (a wave a row: 1,116 us for 4,096 rows of two, 140 so)
   float *loss, *kl, *clip, *dtheta;
 };
 template <int D>
 __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, int blocks) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int step = 1 << p.lg, l = threadIdx.x & (step - 1), group = threadIdx.x >> p.lg, groups = kThreads >> p.lg;
   double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
   if (p.masked || block == 0) {
-    if (p.by_rows && p.S > 1) {        // a wave per row
-      for (int64_t row = wave; row < p.rows; row += kWaves) {
+    if (p.by_rows && p.S > 1) {
+      for (int64_t k = 0; k < p.rows; k += groups) {   // all lanes, for the sums over a group
+        const int64_t row = k + group;
         double u[4] = {};
-        for (int s = lane; s < p.S; s += 64) {
-          const float4 v = p.tot[row * p.S + s];
-          u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
-        }
+        if (row < p.rows)
+          for (int s = l; s < p.S; s += step) {
+            const float4 v = p.tot[row * p.S + s];
+            u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
+          }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = wave_sum_d(u[i]);
-        if (lane == 0 && u[3] > 0.0) {
-          for (int i = 0; i < 4; ++i) t[i] += u[i] / u[3];
+        for (int i = 0; i < 4; ++i) u[i] = group_sum_d(u[i], p.lg);
+        if (l == 0 && u[3] > 0.0) {
+          const double w = 1.0 / u[3];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t[i] += u[i] * w;
           t[4] += 1.0;
         }
       }
@@ -387,18 +395,20 @@ __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, 
     }
     return;
   }
-  for (int64_t row = (int64_t)block * kWaves + wave; row < p.rows; row += (int64_t)blocks * kWaves) {
+  for (int64_t k = (int64_t)block * groups; k < p.rows; k += (int64_t)blocks * groups) {
+    const int64_t row = k + group;
     double u[2 * D + 1] = {};
-    for (int s = lane; s < p.S; s += 64) {
-      const int64_t k = row * p.S + s;
-      u[2 * D] += p.tot[k].w;
+    if (row < p.rows)
+      for (int s = l; s < p.S; s += step) {
+        const int64_t at = row * p.S + s;
+        u[2 * D] += p.tot[at].w;
 #pragma unroll
-      for (int j = 0; j < 2 * D; ++j) u[j] += p.grad[k * 2 * D + j];
-    }
+        for (int j = 0; j < 2 * D; ++j) u[j] += p.grad[at * 2 * D + j];
+      }
 #pragma unroll
-    for (int j = 0; j < 2 * D + 1; ++j) u[j] = wave_sum_d(u[j]);
+    for (int j = 0; j < 2 * D + 1; ++j) u[j] = group_sum_d(u[j], p.lg);
     const double w = !p.by_rows ? inv : u[2 * D] > 0.0 ? inv / u[2 * D] : 0.0;
-    if (lane == 0)
+    if (l == 0 && row < p.rows)
 #pragma unroll
       for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
   }
@@ -428,7 +438,7 @@ struct PolicyArgs {
 };
 
 template <int D, bool kRef>
-__global__ __launch_bounds__(kThreads) void k_policy(PolicyArgs p) {
+__global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
   const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
   const int64_t unit = (((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) << (6 - p.lg)) + (lane >> p.lg);
   const bool on = unit < p.units;
@@ -493,13 +503,13 @@ __global__ __launch_bounds__(kThreads) void k_policy(PolicyArgs p) {
 struct PrefFinish {
   const float* in;            // [rows][S][2d + 1]
   int64_t rows;
-  int S;
+  int S, lg;                  // 2^lg lanes take a row's records
   double beta, inv_pairs;
   float *loss, *dtheta;
 };
 template <int D>
 __device__ __forceinline__ void pref_finish(const PrefFinish& p, int block, int blocks) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int step = 1 << p.lg, l = threadIdx.x & (step - 1), group = threadIdx.x >> p.lg, groups = kThreads >> p.lg;
   if (block == 0 && p.loss) {
     double t[1] = {0.0};
     for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) t[0] += p.in[k * (2 * D + 1) + 2 * D];
@@ -513,14 +523,16 @@ __device__ __forceinline__ void pref_finish(const PrefFinish& p, int block, int 
       p.dtheta[k] = (float)(p.in[k / (2 * D) * (2 * D + 1) + k % (2 * D)] * w);
     return;
   }
-  for (int64_t row = (int64_t)block * kWaves + wave; row < p.rows; row += (int64_t)blocks * kWaves) {
+  for (int64_t k = (int64_t)block * groups; k < p.rows; k += (int64_t)blocks * groups) {
+    const int64_t row = k + group;
     double u[2 * D] = {};
-    for (int s = lane; s < p.S; s += 64)
+    if (row < p.rows)
+      for (int s = l; s < p.S; s += step)
 #pragma unroll
-      for (int j = 0; j < 2 * D; ++j) u[j] += p.in[(row * p.S + s) * (2 * D + 1) + j];
+        for (int j = 0; j < 2 * D; ++j) u[j] += p.in[(row * p.S + s) * (2 * D + 1) + j];
 #pragma unroll
-    for (int j = 0; j < 2 * D; ++j) u[j] = wave_sum_d(u[j]);
-    if (lane == 0)
+    for (int j = 0; j < 2 * D; ++j) u[j] = group_sum_d(u[j], p.lg);
+    if (l == 0 && row < p.rows)
 #pragma unroll
       for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
   }
@@ -715,17 +727,16 @@ hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x
   PolicyArgs a{P.theta, P.theta_old, P.theta_ref, x, adv, mask, P.events_per_theta, pl.chunk, pl.units, pl.S, pl.lg,
                pl.per_block, (float)(1.0 - P.clip_low), (float)(1.0 + P.clip_high), (float)P.kl_coef,
                reinterpret_cast<float4*>(ws), reinterpret_cast<float*>(ws + pl.grad_off), nullptr, {}};
-  a.fin = PolicyFinish{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, P.average == SAGIPS_MEAN_ROWS,
-                       mask != nullptr, loss, kl, clip, dtheta};
+  a.fin = PolicyFinish{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, lanes_log(pl.records),
+                       P.average == SAGIPS_MEAN_ROWS, mask != nullptr, loss, kl, clip, dtheta};
   const dim3 grid(wave_blocks(ceil_div(pl.units, 64 >> pl.lg)));
   if (ends_in_last(grid.x, P.n_theta, pl.records, D)) a.ticket = ticket;
   if (tm) tm->begin("policy");
-  if (P.theta_ref) hipLaunchKernelGGL((k_policy<D, true>), grid, dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_policy<D, false>), grid, dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((P.theta_ref ? k_policy<D, true> : k_policy<D, false>), grid, dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ticket) return e;
-  const int64_t blocks = pl.records == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
+  const int64_t blocks = pl.records == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kThreads >> a.fin.lg);
   if (tm) tm->begin("policy_finish");
   hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, a.fin);
   if (tm) tm->end();
@@ -769,17 +780,16 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
   a.lg = pl.lg;
   a.part = part;
   a.out = sums;
-  a.fin = PrefFinish{sums, P.n_theta, pl.S, P.beta, 1.0 / (double)all, loss, dtheta};
+  a.fin = PrefFinish{sums, P.n_theta, pl.S, lanes_log(pl.S), P.beta, 1.0 / (double)all, loss, dtheta};
   const unsigned blocks = wave_blocks(pl.units);
   const bool finish = loss || dtheta;
   if (finish && ends_in_last(blocks, P.n_theta, pl.S, D)) a.ticket = ticket;
   if (tm) tm->begin("preference");
-  if (pl.slices) hipLaunchKernelGGL((k_pref<D, true>), dim3(blocks), dim3(kThreads), 0, st, a);
-  else hipLaunchKernelGGL((k_pref<D, false>), dim3(blocks), dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL((pl.slices ? k_pref<D, true> : k_pref<D, false>), dim3(blocks), dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !finish || a.ticket) return e;
-  const int64_t n = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kWaves);
+  const int64_t n = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kThreads >> a.fin.lg);
   if (tm) tm->begin("preference_finish");
   hipLaunchKernelGGL((k_pref_finish<D>), dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(kThreads), 0, st, a.fin);
   if (tm) tm->end();
