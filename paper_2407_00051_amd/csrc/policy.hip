@@ -43,7 +43,7 @@ __device__ __forceinline__ float one_minus_power(float a, float l2, float* w_out
 // A row that the gradient is taken at, and one that its density is compared with.
 template <int D>
 struct Row {
-  float a[D], b[D], ra[D], rb[D], bm1[D];
+  float a[D], b[D], bm1[D];
 };
 template <int D>
 struct Against {
@@ -73,8 +73,6 @@ __device__ __forceinline__ void load_rows(const float* __restrict__ th, const fl
   for (int j = 0; j < D; ++j) {
     r.a[j] = th[2 * j];
     r.b[j] = th[2 * j + 1];
-    r.ra[j] = shared[2 * j];
-    r.rb[j] = shared[2 * j + 1];
     r.bm1[j] = r.b[j] - 1.0f;
   }
 #pragma unroll
@@ -122,15 +120,22 @@ __device__ __forceinline__ float log2_ratio(const Event<D>& e, const Row<D>& r, 
   }
   return s;
 }
-// acc += wt * dl/d(a, b).
+// acc += wt * dl/d(a, b), without the terms 1/a and 1/b, which add_constants gives once to a
+// lane's finished sum of weights.
 template <int D>
 __device__ __forceinline__ void add_grad(const Event<D>& e, const Row<D>& r, float wt, float* acc) {
 #pragma unroll
   for (int j = 0; j < D; ++j) {
-    const float k = fmaf(-kLn2 * r.bm1[j], e.q[j], kLn2);
-    acc[2 * j] = fmaf(wt, fmaf(e.l2[j], k, r.ra[j]), acc[2 * j]);
-    acc[2 * j + 1] = fmaf(wt, fmaf(e.lg[j], kLn2, r.rb[j]), acc[2 * j + 1]);
+    const float u = wt * e.l2[j];
+    acc[2 * j] = fmaf(u, fmaf(-kLn2 * r.bm1[j], e.q[j], kLn2), acc[2 * j]);
+    acc[2 * j + 1] = fmaf(wt * kLn2, e.lg[j], acc[2 * j + 1]);
   }
+}
+// `inverse`: the row's 1/a and 1/b, as load_rows leaves them.
+template <int D>
+__device__ __forceinline__ void add_constants(const float* inverse, float weights, float* acc) {
+#pragma unroll
+  for (int j = 0; j < 2 * D; ++j) acc[j] = fmaf(weights, inverse[j], acc[j]);
 }
 
 template <int D>
@@ -450,9 +455,10 @@ __global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
   if constexpr (kRef) others[1] = p.theta_ref + row * 2 * D;
   Row<D> r;
   Against<D> o[kOthers];
-  load_rows<D>(p.theta + row * 2 * D, others, l, step, items + (threadIdx.x >> p.lg) * kItems, r, o);
+  float* const mine = items + (threadIdx.x >> p.lg) * kItems;
+  load_rows<D>(p.theta + row * 2 * D, others, l, step, mine, r, o);
   const int64_t e1 = on ? min(p.E, (s + 1) * p.chunk) : 0;
-  float acc[2 * D + 4] = {};   // the gradient, then loss, KL, clipped, events
+  float acc[2 * D + 4] = {}, weights = 0.0f;   // the gradient, then loss, KL, clipped, events
   for (int64_t e = s * p.chunk + l; e < e1; e += step) {
     const int64_t i = row * p.E + e;
     if (p.mask && !p.mask[i]) continue;
@@ -474,8 +480,10 @@ __global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
     acc[2 * D] += loss;
     acc[2 * D + 2] += cut ? 1.0f : 0.0f;
     acc[2 * D + 3] += 1.0f;
+    weights += wt;
     add_grad<D>(ev, r, wt, acc);
   }
+  add_constants<D>(mine, weights, acc);
   group_sum(acc, p.lg);
   if (p.per_block) {
     __shared__ float sums[kWaves][2 * D + 4];
@@ -563,7 +571,7 @@ struct PrefArgs {
 
 template <int D>
 __device__ __forceinline__ void add_set(const PrefArgs& p, int which, int64_t pair, int64_t e0, int64_t e1, int l, int step,
-                                        const Row<D>& r, const Against<D>& ref, float (&v)[2 * D + 1]) {
+                                        const Row<D>& r, const Against<D>& ref, float& weights, float (&v)[2 * D + 1]) {
   int64_t n = p.T[which];
   if (p.len[which]) {
     const int64_t given = p.len[which][pair];
@@ -576,6 +584,7 @@ __device__ __forceinline__ void add_set(const PrefArgs& p, int which, int64_t pa
     load_event<D>(p.x[which], pair * p.T[which] + e, x);
     const Event<D> ev = at_row<D>(x, r);
     v[2 * D] = fmaf(sign, log2_ratio<D>(ev, r, ref), v[2 * D]);
+    weights += sign;
     add_grad<D>(ev, r, sign, v);
   }
 }
@@ -605,8 +614,10 @@ __global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
 #pragma unroll
           for (int j = 0; j < 2 * D + 1; ++j) v[j] += p.part[(pair * p.slices + i) * (2 * D + 1) + j];
       } else {
-        add_set<D>(p, 0, pair, 0, p.T[0], l, step, r, ref[0], v);
-        add_set<D>(p, 1, pair, 0, p.T[1], l, step, r, ref[0], v);
+        float weights = 0.0f;
+        add_set<D>(p, 0, pair, 0, p.T[0], l, step, r, ref[0], weights, v);
+        add_set<D>(p, 1, pair, 0, p.T[1], l, step, r, ref[0], weights, v);
+        add_constants<D>(items[threadIdx.x >> 6], weights, v);
       }
     }
     group_sum(v, p.lg);
@@ -643,9 +654,10 @@ __global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
   Against<D> ref[1];
   load_rows<D>(p.theta + row * 2 * D, others, lane, 64, items[threadIdx.x >> 6], r, ref);
   if (!any) return;
-  float v[2 * D + 1] = {};
-  add_set<D>(p, 0, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref[0], v);
-  add_set<D>(p, 1, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref[0], v);
+  float v[2 * D + 1] = {}, weights = 0.0f;
+  add_set<D>(p, 0, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref[0], weights, v);
+  add_set<D>(p, 1, pair, s * p.chunk, (s + 1) * p.chunk, lane, 64, r, ref[0], weights, v);
+  add_constants<D>(items[threadIdx.x >> 6], weights, v);
   group_sum(v, 6);
   if (lane == 0)
 #pragma unroll
