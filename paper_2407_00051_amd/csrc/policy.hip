@@ -203,6 +203,34 @@ __device__ __forceinline__ void block_sum_d(double (&v)[N]) {
 constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing, at most
 constexpr int kAdvBlock = 1024;
 
+// Reads a lane's events e0 + i * step < E of the row at `off`: v, 0 where not valid, and a bit for
+// each valid one.  All reads are at places inside the row, so that none waits for a branch
+// (16,384 rows of 1,000 events: 160 us with a branch for each).
+template <int kHeld>
+__device__ __forceinline__ uint32_t load_rewards(const float* reward, const uint8_t* __restrict__ mask, int off, int e0, int step,
+                                                 int E, float (&v)[kHeld]) {
+  uint32_t valid = 0;
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) {
+    const int e = e0 + i * step;
+    v[i] = reward[off + (e < E ? e : E - 1)];
+    valid |= e < E ? 1u << i : 0u;
+  }
+  if (mask) {
+    uint8_t k[kHeld];
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int e = e0 + i * step;
+      k[i] = mask[off + (e < E ? e : E - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) valid &= k[i] ? ~0u : ~(1u << i);
+  }
+#pragma unroll
+  for (int i = 0; i < kHeld; ++i) v[i] = (valid >> i) & 1u ? v[i] : 0.0f;
+  return valid;
+}
+
 // A row in a group of 2^lg lanes (kBlock false; up to 64 x 16 events) or in a
 // workgroup (up to 1,024 x 16): read once, held in registers, written once.
 template <bool kBlock, int kHeld>
@@ -210,23 +238,17 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
                                                                             int n_rows, int E, int lg, float eps, int normalise,
                                                                             float* adv) {
   const int lane = threadIdx.x & 63, step = kBlock ? blockDim.x : 1 << lg;
-  const int64_t row = kBlock ? blockIdx.x
-                             : (((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) << (6 - lg)) + (lane >> lg);
   const int l = kBlock ? threadIdx.x : lane & (step - 1);
-  const bool on = row < n_rows;
-  const int64_t base = row * E;
+  // The workgroup's first row and this lane's, from the first
+  const int64_t row0 = kBlock ? blockIdx.x : (int64_t)blockIdx.x * kWaves << (6 - lg);
+  const int ahead = kBlock ? 0 : ((threadIdx.x >> 6) << (6 - lg)) + (lane >> lg), last = (int)min((int64_t)255, n_rows - 1 - row0);
+  const bool on = ahead <= last;
+  const int off = (on ? ahead : last) * E;
+  const float* from = reward + row0 * E;
+  float* to = adv + row0 * E;
   float v[kHeld];
-  uint32_t valid = 0;
   double t[2] = {0.0, 0.0};
-#pragma unroll
-  for (int i = 0; i < kHeld; ++i) {
-    const int e = l + i * step;
-    v[i] = 0.0f;
-    if (on && e < E && (!mask || mask[base + e])) {
-      v[i] = reward[base + e];
-      valid |= 1u << i;
-    }
-  }
+  const uint32_t valid = load_rewards<kHeld>(from, mask ? mask + row0 * E : nullptr, off, l, step, E, v);
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) t[0] += (double)v[i];
   t[1] = (double)__popc(valid);
@@ -254,7 +276,7 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int e = l + i * step;
-    if (on && e < E) adv[base + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
+    if (on && e < E) to[off + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
   }
 }
 
@@ -262,23 +284,17 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
 // squared deviations, then one pass that joins a row's slices (Chan's update)
 // and writes.
 constexpr int kAdvSlice = 16384;
-__global__ __launch_bounds__(kAdvBlock) void k_adv_slices(const float* __restrict__ reward, const uint8_t* __restrict__ mask,
+__global__ __launch_bounds__(kAdvBlock, 8) void k_adv_slices(const float* __restrict__ reward, const uint8_t* __restrict__ mask,
                                                           int64_t E, int n_slices, double* __restrict__ part) {
   const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices;
-  const int64_t base = row * E, e0 = s * kAdvSlice, left = E - e0;
+  const int64_t base = row * E + s * kAdvSlice;
+  const int n = (int)min((int64_t)kAdvSlice, E - s * kAdvSlice);
   float v[kAdvSlice / kAdvBlock];
-  uint32_t valid = 0;
   double t[2] = {0.0, 0.0};
+  const uint32_t valid = load_rewards<kAdvSlice / kAdvBlock>(reward + base, mask ? mask + base : nullptr, 0, threadIdx.x, kAdvBlock,
+                                                                       n, v);
 #pragma unroll
-  for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) {
-    const int e = threadIdx.x + i * kAdvBlock;
-    v[i] = 0.0f;
-    if (e < left && (!mask || mask[base + e0 + e])) {
-      v[i] = reward[base + e0 + e];
-      valid |= 1u << i;
-      t[0] += (double)v[i];
-    }
-  }
+  for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) t[0] += (double)v[i];
   t[1] = (double)__popc(valid);
   block_sum_d<2, kAdvBlock>(t);
   const double mean = t[1] > 0.0 ? t[0] / t[1] : 0.0;
@@ -293,10 +309,14 @@ __global__ __launch_bounds__(kAdvBlock) void k_adv_slices(const float* __restric
     part[(int64_t)blockIdx.x * 3 + 2] = q[0];
   }
 }
-__global__ __launch_bounds__(kAdvBlock) void k_adv_apply(const float* reward, const uint8_t* __restrict__ mask, int64_t E,
+__global__ __launch_bounds__(kAdvBlock, 8) void k_adv_apply(const float* reward, const uint8_t* __restrict__ mask, int64_t E,
                                                          int n_slices, const double* __restrict__ part, float eps,
                                                          int normalise, float* adv) {
-  const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices;
+  const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices, base = row * E + s * kAdvSlice;
+  const int n = (int)min((int64_t)kAdvSlice, E - s * kAdvSlice);
+  float v[kAdvSlice / kAdvBlock];
+  const uint32_t valid = load_rewards<kAdvSlice / kAdvBlock>(reward + base, mask ? mask + base : nullptr, 0, threadIdx.x, kAdvBlock,
+                                                                       n, v);
   const double* p = part + row * n_slices * 3;
   double t[2] = {0.0, 0.0};
   for (int i = threadIdx.x; i < n_slices; i += kAdvBlock) {
@@ -315,9 +335,11 @@ __global__ __launch_bounds__(kAdvBlock) void k_adv_apply(const float* reward, co
     block_sum_d<1, kAdvBlock>(q);
     inv = 1.0f / ((t[1] > 0.0 ? (float)sqrt(q[0] / t[1]) : 0.0f) + eps);
   }
-  const int64_t base = row * E, e1 = min(E, (s + 1) * (int64_t)kAdvSlice);
-  for (int64_t e = s * kAdvSlice + threadIdx.x; e < e1; e += kAdvBlock)
-    adv[base + e] = !mask || mask[base + e] ? (float)((double)reward[base + e] - mean) * inv : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) {
+    const int e = threadIdx.x + i * kAdvBlock;
+    if (e < n) adv[base + e] = (valid >> i) & 1u ? (float)((double)v[i] - mean) * inv : 0.0f;
+  }
 }
 
 // ---- policy loss ---------------------------------------------------------------
@@ -824,10 +846,13 @@ hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_
                             float* adv, void* ws, hipStream_t st, Timer* tm) {
   if (tm) tm->begin("advantage");
   if (E <= 64 * kAdvHeld) {
-    // the fewest lanes that hold a row, but a lane for every event up to 64
-    const int lg = lanes_log(E);
+    // a lane for every event up to 64, for the least time of one row; with more events than lanes
+    // on the device, four a lane and fewer sums over lanes
+    const bool many = n_rows * E > 256 * 2048;
+    const int held = E > 256 ? kAdvHeld : E > 64 || many ? 4 : 1;
+    const int lg = lanes_log(many ? ceil_div(E, held) : E);
     const int64_t waves = ceil_div(n_rows, 64 >> lg);
-    const auto kernel = E <= 64 ? k_advantage<false, 1> : E <= 256 ? k_advantage<false, 4> : k_advantage<false, kAdvHeld>;
+    const auto kernel = held == 1 ? k_advantage<false, 1> : held == 4 ? k_advantage<false, 4> : k_advantage<false, kAdvHeld>;
     hipLaunchKernelGGL(kernel, dim3(wave_blocks(waves)), dim3(kThreads), 0, st, reward, mask, (int)n_rows, (int)E, lg, eps,
                        (int)normalise, adv);
   } else if (E <= kAdvBlock * kAdvHeld) {
