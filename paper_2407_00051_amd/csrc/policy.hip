@@ -22,8 +22,7 @@ constexpr int kWaves = kThreads / 64;
 // Events are read clamped to the open unit interval: a draw may have rounded to
 // 0 or 1.  NaN stays NaN.
 __device__ __forceinline__ float clamp_event(float x) {
-  x = x < 0x1p-126f ? 0x1p-126f : x;
-  return x > 1.0f - 0x1p-24f ? 1.0f - 0x1p-24f : x;
+  return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, 0x1p-126f), 1.0f - 0x1p-24f);
 }
 
 // 1 - x^a, from l2 = log2 x < 0.  With t = a l2, 1 - 2^t = -t P(t): above 2^t = 3/4 by the
@@ -489,10 +488,11 @@ __global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
     const float A = p.adv[i];
     const Event<D> ev = at_row<D>(x, r);
     const float rho = fast_exp2(log2_ratio<D>(ev, r, o[0]));
-    const bool up = A > 0.0f && rho > p.hi, down = A < 0.0f && rho < p.lo;
-    const bool cut = up || down;
-    float loss = -(cut ? (up ? p.hi : p.lo) : rho) * A;
-    float wt = cut ? 0.0f : -rho * A;
+    // min(rho A, clip(rho) A)
+    const float in = fmaxf(fminf(rho, p.hi), p.lo) * A, out = rho * A;
+    const bool cut = in < out;
+    float loss = cut ? -in : -out;
+    float wt = cut ? 0.0f : -out;
     if constexpr (kRef) {
       const float t = -log2_ratio<D>(ev, r, o[kOthers - 1]) * kLn2, k = exp_minus_line(t);
       loss = fmaf(p.beta, k, loss);
