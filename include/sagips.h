@@ -20,8 +20,9 @@
  *   - Outputs are overwritten, never accumulated.  Results are bitwise
  *     reproducible for fixed inputs (fixed reduction order, no float atomics).
  *   - Device arrays must be 16-byte aligned and densely packed, row-major;
- *     the one exception is theta, which needs only 4-byte alignment so that a
- *     caller can pass the rows of one shard (theta + r * 2d).
+ *     the exceptions are theta, which needs only 4-byte alignment so that a
+ *     caller can pass the rows of one shard (theta + r * 2d), and the arrays
+ *     for which a call says otherwise.
  *   - Several contexts may share a device; each owns its own workspace.
  *   - A context is not thread-safe; calls on one context must not overlap
  *     from several host threads.
@@ -448,7 +449,9 @@ sagips_status sagips_orthogonalise(sagips_ctx* ctx, const sagips_newton_schulz* 
  *       0.2 sqrt(max(rows, cols)) (SCALE_RMS: the size of an Adam update).
  * param and m (which starts at zero) are fp32, updated in place; grad is
  * `grad_type` (SAGIPS_F32 or SAGIPS_BF16), read only.  No two arrays of a set
- * may overlap.  lr, weight_decay >= 0, 0 <= momentum < 1.                   */
+ * may overlap.  Arrays are aligned to four of their values where cols[i] is a
+ * multiple of four, to one otherwise, so that the parts of a packed stack of
+ * odd sizes serve.  lr, weight_decay >= 0, 0 <= momentum < 1.               */
 typedef enum { SAGIPS_SCALE_NONE = 0, SAGIPS_SCALE_SHAPE = 1, SAGIPS_SCALE_RMS = 2 } sagips_muon_scale;
 typedef struct {
   int32_t n_tensors;

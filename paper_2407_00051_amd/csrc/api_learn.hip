@@ -12,7 +12,8 @@ using namespace sagips;
 
 namespace {
 
-bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
+bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+bool aligned4(const void* p) { return aligned_to(p, 4); }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -247,10 +248,13 @@ sagips_status sagips_muon_step(sagips_ctx* c, const sagips_matrix_set* set, cons
     int64_t matrices = 0;
     for (int i = 0; i < set->n_tensors; ++i) {
       if (!set->param[i] || !set->grad[i] || !set->m[i]) return fail(c, SAGIPS_E_INVAL, "tensor %d has a NULL array", i);
-      if (!aligned16(set->param[i]) || !aligned16(set->grad[i]) || !aligned16(set->m[i]))
-        return fail(c, SAGIPS_E_INVAL, "tensor %d has an array that is not 16-byte aligned", i);
       s = check_stack(c, set->count[i], set->rows[i], set->cols[i], i);
       if (s != SAGIPS_OK) return s;
+      // rows of whole quads are read and written four values at a time, others one
+      const size_t at_once = set->cols[i] % 4 == 0 ? 4 : 1;
+      if (!aligned_to(set->param[i], 4 * at_once) || !aligned_to(set->m[i], 4 * at_once) ||
+          !aligned_to(set->grad[i], grad_size * at_once))
+        return fail(c, SAGIPS_E_INVAL, "tensor %d has an array that is not aligned to %d values", i, (int)at_once);
       matrices += set->count[i];
       const int32_t rows = set->rows[i], cols = set->cols[i];
       const double scale = o->scale == SAGIPS_SCALE_NONE ? 1.0

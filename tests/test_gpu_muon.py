@@ -128,6 +128,34 @@ def test_muon_step(gpu_ctx, bf16, nesterov, scale):
             p[i], m[i] = got_p, got_m          # each step from what the GPU holds
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shape", [(1, 3, 5), (3, 9, 11), (1, 127, 129), (3, 131, 61), (3, 3, 4), (1, 9, 12), (1, 135, 300)])
+def test_muon_step_on_parts_of_a_packed_stack(gpu_ctx, shape, bf16):
+    """Arrays that start wherever the one before them ends give what arrays of their own give."""
+    print(f"case packed {shape} bf16={bf16}", flush=True)
+    rng = np.random.default_rng(shape[1] * 7 + shape[2])
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    g = torch.tensor(_gradients(rng, (3 * shape[0],) + shape[1:]), dtype=dtype, device="cuda:0").reshape((3,) + shape)
+    p, m = (torch.tensor(rng.standard_normal((3,) + shape), dtype=torch.float32, device="cuda:0") for _ in range(2))
+    own = [[t[i].clone() for i in range(3)] for t in (p, g, m)]
+    gpu_ctx.muon_step(list(p), list(g), list(m), 0.05)
+    gpu_ctx.muon_step(*own, 0.05)
+    for i in range(3):
+        assert torch.equal(p[i], own[0][i]) and torch.equal(m[i], own[2][i])
+
+
+def test_muon_step_refuses_quads_off_their_alignment(gpu_ctx):
+    buf = torch.zeros(3, 4 * 8 + 4, device="cuda:0")
+    part = lambda i, off, dtype=torch.float32: buf[i].view(dtype)[off:off + 32].view(4, 8)      # noqa: E731
+    gpu_ctx.muon_step([part(0, 4)], [part(1, 0)], [part(2, 4)], 0.1)
+    for off in ((1, 0, 0), (0, 2, 0), (0, 0, 3)):
+        with pytest.raises(sg.SagipsError, match="aligned to 4 values"):
+            gpu_ctx.muon_step(*([part(i, off[i])] for i in range(3)), 0.1)
+    gpu_ctx.muon_step([part(0, 0)], [part(1, 4, torch.bfloat16)], [part(2, 0)], 0.1)
+    with pytest.raises(sg.SagipsError, match="aligned to 4 values"):
+        gpu_ctx.muon_step([part(0, 0)], [part(1, 2, torch.bfloat16)], [part(2, 0)], 0.1)
+
+
 def test_muon_on_a_stream_of_its_own(gpu_ctx):
     rng = np.random.default_rng(5)
     g = torch.tensor(_gradients(rng, (20, 128, 128)), dtype=torch.float32, device="cuda:0")
