@@ -92,7 +92,9 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 
 // ---- norm -------------------------------------------------------------------------
 // The momentum update, and each matrix's sum of squares of U in 64 bits (neither
-// large nor small gradients leave its range), in chunks of kChunk elements.
+// large nor small gradients leave its range), in chunks of kChunk elements, whose reads
+// are all in flight (2,048 x 2,048 fp32: 6-7 us for 17 MB; three of 512 x 512 with bf16
+// gradients, read and written momenta: 12 us, of which most is the latency of one chunk).
 constexpr int kChunk = 4096;
 __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double* __restrict__ part) {
   const int z = blockIdx.x / chunks, k = blockIdx.x % chunks;
@@ -149,7 +151,8 @@ constexpr int kFrag = 512;                             // values of a fragment's
 __device__ __forceinline__ int64_t frag_at(int rb, int ks, int K) { return ((int64_t)rb * (K / 16) + ks) * (kT * kFrag); }
 
 // X's terms, zero beyond n x L, in tiles of 64 x 64: XR with K along X's rows, XC with
-// K down its columns.
+// K down its columns (two copies, since a fragment's 8 values are neighbours along K).
+// 13-15 us at 2,048 x 2,048 fp32, 50 MB at 3.5 TB/s.
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
                                                        u16* __restrict__ XR, u16* __restrict__ XC, int np, int lp) {
   __shared__ float tile[64][65];
@@ -205,6 +208,10 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
 // LDS traffic and no barrier (the same tile with operands shared through LDS was bound by
 // LDS: 61 us a product at 2,048 x 2,048, of which 21 are matrix instructions).  The
 // quarters are added through LDS at the end, each wave keeping a quarter of the tile.
+// 2,048 x 2,048: the symmetric products take 33-37 us each, the others 53-59, i.e. 0.79 and
+// 0.88 PFLOP/s of fp16 products, with the matrix cores 59% and 62% busy while a unit works;
+// the rest is the first fragments' latency and the sums at the end.  Small counts (three of
+// 512 x 512: 6-8 us a product) are launches that wait for each other.
 enum Mode { kGram, kPoly, kApply, kStore };
 
 struct GemmArgs {
@@ -414,8 +421,8 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
 // All steps of one matrix in one workgroup, from the momentum update to the
 // parameters, X never leaving registers and LDS: n <= NP and L <= 16384 / NP, for NP
 // of 32, 64 and 128.  Wave (rw, cw) of RW x CW = W owns rows 32 rw .. + 31 of X and every
-// CW-th block of 32 columns, JB of them (the fewest that hold L); lane lr (of half lh) holds row 32 rw + lr, columns 8 g + 4 lh + 0..3 of
-// each block, as accumulators do.
+// CW-th block of 32 columns, JB of them (the fewest that hold L); lane lr (of half lh)
+// holds row 32 rw + lr, columns 8 g + 4 lh + 0..3 of each block, as accumulators do.
 //   A = X X^T: the wave forms columns 32 rw .. of A, summed over its own columns of X,
 //   whose terms it has in registers; waves of one rw add their sums through LDS.  A is
 //   symmetric, so a lane's accumulators are pieces of a row of A, and in the K order
@@ -427,6 +434,9 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
 // columns 32 J + 16 s + 4 h + 0..3 and + 8..11, what one lane half has of a K step, and
 // is kept at unit ^ swz(row), so that 8 lanes (rows) of a 16-byte access and the 4 rows
 // of a transposed read hit distinct banks.
+// Six of 128 x 128 take 43 us (6.5 a step), 300 of them 97-107 on 256 units; the matrix
+// cores are 40% busy: between the products stand barriers and the splitting of X, Y and A
+// into terms, with one or two waves on a SIMD to hide them.
 struct SmallJob {
   const void* src;
   float* m;
@@ -817,9 +827,10 @@ Plan plan_of(int rows, int cols, int mats) {
 
 // Blocks in a tile's side: 2, 3 or 4.  Compute units take tiles in rounds; a round takes
 // about fixed + per_k K microseconds (measured from K = 256 to 2,048; a larger side reads
-// less per product but has more to add up at the end, and only tiles of 2 run two to a
-// unit).  Products at 2,048 x 2,048: symmetric 45, 31, 37 us with sides 2, 3, 4, others
-// 63, 63, 51; at K = 512 a side of 2 is the fastest at every count.
+// less per product but has more to add up at the end, and only tiles of 2 run three to a
+// unit, which the rounds count as one after the other).  Products at 2,048 x 2,048:
+// symmetric 43, 30, 37 us with sides 2, 3, 4, others 61, 61, 50; at K = 512 a side of 2 is
+// the fastest at every count (16 of 512 x 512: 13, 20, 16 and 21, 39, 22 us).
 int tile_side(bool sym, int np, int width, int K, int mats, int n_cu) {
   static const double fixed[5] = {0, 0, 2.6, 7.6, 13.0}, per_k[5] = {0, 0, 0.0064, 0.0115, 0.018};
   int best = 2;
