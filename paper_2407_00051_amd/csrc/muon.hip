@@ -57,9 +57,15 @@ __device__ __forceinline__ int tensor_of(const int (&first)[SAGIPS_MAX_TENSORS +
   for (int k = 1; k < SAGIPS_MAX_TENSORS; ++k) t += z >= first[k];
   return t;
 }
-__device__ __forceinline__ float load_src(const void* p, int64_t i, int bf16) {
-  return bf16 ? bf16_lo(static_cast<const u16*>(p)[i]) : static_cast<const float*>(p)[i];
-}
+// n elements as they lie in memory, converted after all have been asked for.
+template <bool kBf16, int N>
+struct Raw {
+  uint32_t v[N];
+  __device__ __forceinline__ void read(int k, const void* p, int64_t i) {
+    v[k] = kBf16 ? static_cast<const u16*>(p)[i] : static_cast<const uint32_t*>(p)[i];
+  }
+  __device__ __forceinline__ float operator[](int k) const { return kBf16 ? bf16_lo(v[k]) : __uint_as_float(v[k]); }
+};
 __device__ __forceinline__ u16 to_bf16(float v) { return (u16)pk_bf16(v, 0.0f); }
 
 __device__ __forceinline__ double wave_sum_d(double v) {
@@ -93,35 +99,38 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // ---- norm -------------------------------------------------------------------------
 // The momentum update, and each matrix's sum of squares of U in 64 bits (neither
 // large nor small gradients leave its range), in chunks of kChunk elements, whose reads
-// are all in flight (2,048 x 2,048 fp32: 6-7 us for 17 MB; three of 512 x 512 with bf16
-// gradients, read and written momenta: 12 us, of which most is the latency of one chunk).
+// are all in flight (with the launch, 7 us for 2,048 x 2,048 fp32, 8 for three of 512 x 512
+// with bf16 gradients and momenta; 12 where each conversion waited for its read).
 constexpr int kChunk = 4096;
+template <bool kBf16, bool kMom>
 __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double* __restrict__ part) {
   const int z = blockIdx.x / chunks, k = blockIdx.x % chunks;
   const int t = tensor_of(j.first, z);
   const int64_t size = (int64_t)j.rows * j.cols, base = (z - j.first[t]) * size;
   const int64_t e0 = (int64_t)k * kChunk + threadIdx.x;
   constexpr int kEach = kChunk / kThreads;
-  float u[kEach], m[kEach];
+  const void* const src = j.src[t];
+  float* const mom = j.m[t];
+  Raw<kBf16, kEach> g;
+  float m[kEach];
 #pragma unroll
   for (int q = 0; q < kEach; ++q) {
-    const int64_t e = e0 + q * kThreads;
-    u[q] = m[q] = 0.0f;
-    if (e < size) {
-      u[q] = load_src(j.src[t], base + e, j.src_bf16);
-      if (j.m[t]) m[q] = j.m[t][base + e];
-    }
+    const int64_t e = base + min(e0 + q * kThreads, size - 1);   // inside: no read waits for a branch
+    g.read(q, src, e);
+    if constexpr (kMom) m[q] = mom[e];
   }
   double s = 0.0;
 #pragma unroll
   for (int q = 0; q < kEach; ++q) {
     const int64_t e = e0 + q * kThreads;
-    if (j.m[t] && e < size) {
-      const float w = fmaf(j.momentum, m[q], u[q]);
-      j.m[t][base + e] = w;
-      u[q] = j.nesterov ? fmaf(j.momentum, w, u[q]) : w;
+    float u = g[q];
+    if constexpr (kMom) {
+      const float w = fmaf(j.momentum, m[q], u);
+      if (e < size) mom[base + e] = w;
+      u = j.nesterov ? fmaf(j.momentum, w, u) : w;
     }
-    s = fma((double)u[q], (double)u[q], s);
+    u = e < size ? u : 0.0f;
+    s = fma((double)u, (double)u, s);
   }
   __shared__ double w[kThreads / 64];
   s = wave_sum_d(s);
@@ -153,6 +162,7 @@ __device__ __forceinline__ int64_t frag_at(int rb, int ks, int K) { return ((int
 // X's terms, zero beyond n x L, in tiles of 64 x 64: XR with K along X's rows, XC with
 // K down its columns (two copies, since a fragment's 8 values are neighbours along K).
 // 13-15 us at 2,048 x 2,048 fp32, 50 MB at 3.5 TB/s.
+template <bool kBf16, bool kMom>
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
                                                        u16* __restrict__ XR, u16* __restrict__ XC, int np, int lp) {
   __shared__ float tile[64][65];
@@ -162,23 +172,25 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
   // read along the source's rows, before the norm is waited for
   const int r0 = flip ? l0 : i0, c0 = flip ? i0 : l0;
   const int c = threadIdx.x & 63, col = c0 + c;
-  float u[16];
+  const void* const src = j.src[t];
+  const float* const mom = j.m[t];
+  Raw<kBf16, 16> g;
+  float m[16];
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
-    const int r = r0 + 4 * q + (threadIdx.x >> 6);
-    u[q] = 0.0f;
-    if (r < j.rows && col < j.cols) {
-      const int64_t e = base + (int64_t)r * j.cols + col;
-      if (!j.m[t]) u[q] = load_src(j.src[t], e, j.src_bf16);
-      else u[q] = j.nesterov ? fmaf(j.momentum, j.m[t][e], load_src(j.src[t], e, j.src_bf16)) : j.m[t][e];
-    }
+    const int64_t e = base + (int64_t)min(r0 + 4 * q + (int)(threadIdx.x >> 6), j.rows - 1) * j.cols + min(col, j.cols - 1);
+    g.read(q, src, e);
+    if constexpr (kMom) m[q] = mom[e];
   }
   const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const int r = 4 * q + (threadIdx.x >> 6);
-    if (flip) tile[c][r] = u[q] * inv;
-    else tile[r][c] = u[q] * inv;
+    float u = g[q];
+    if constexpr (kMom) u = j.nesterov ? fmaf(j.momentum, m[q], u) : m[q];
+    u = r0 + r < j.rows && col < j.cols ? u * inv : 0.0f;
+    if (flip) tile[c][r] = u;
+    else tile[r][c] = u;
   }
   __syncthreads();
   const int64_t size = (int64_t)kT * np * lp;
@@ -867,10 +879,14 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws,
   double* part = reinterpret_cast<double*>(ws);
   u16 *r0 = at(p.r0), *r1 = at(p.r1), *c0 = at(p.c0), *c1 = at(p.c1), *A = at(p.A), *B = at(p.B);
   if (tm) tm->begin("ns_norm");
-  hipLaunchKernelGGL(k_ns_norm, dim3((unsigned)p.mats * p.chunks), dim3(kThreads), 0, st, j, p.chunks, part);
+  const auto norm = j.m[0] ? (j.src_bf16 ? k_ns_norm<true, true> : k_ns_norm<false, true>)
+                           : (j.src_bf16 ? k_ns_norm<true, false> : k_ns_norm<false, false>);
+  const auto split = j.m[0] ? (j.src_bf16 ? k_ns_split<true, true> : k_ns_split<false, true>)
+                            : (j.src_bf16 ? k_ns_split<true, false> : k_ns_split<false, false>);
+  hipLaunchKernelGGL(norm, dim3((unsigned)p.mats * p.chunks), dim3(kThreads), 0, st, j, p.chunks, part);
   if (tm) tm->end();
   if (tm) tm->begin("ns_split");
-  hipLaunchKernelGGL(k_ns_split, dim3((p.lp + 63) / 64, (p.np + 63) / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
+  hipLaunchKernelGGL(split, dim3((p.lp + 63) / 64, (p.np + 63) / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
                      p.np, p.lp);
   if (tm) tm->end();
   const int gram = tile_side(true, p.np, p.np, p.lp, p.mats, n_cu), poly = tile_side(true, p.np, p.np, p.np, p.mats, n_cu);
