@@ -344,15 +344,24 @@ __global__ __launch_bounds__(kAdvBlock, 8) void k_adv_apply(const float* reward,
 }
 
 // ---- policy loss ---------------------------------------------------------------
-// Whether this workgroup is the last of its launch to come here, all the others' global
-// writes before it visible: one counter of the context, which the last puts back to 0.
+// A record for the launch's last workgroup (kEnds) or for the next launch.  The former goes
+// through to where every XCD sees it, so that nothing has to be written back before the
+// workgroup is counted: a release, which writes the XCD's whole L2 back, for every workgroup
+// cost 45 us at 1,024 of them.
+template <bool kEnds>
+__device__ __forceinline__ void put_record(float* p, float v) {
+  if constexpr (kEnds) __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  else *p = v;
+}
+// Whether this workgroup is the last of its launch to come here, all the others' records
+// visible to it: one counter of the context, which the last puts back to 0.
 // Only which workgroup is last depends on the order, not what it computes.
 __device__ __forceinline__ bool last_block(uint32_t* ticket) {
   __shared__ uint32_t turn;
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");   // every wave's own writes, before the workgroup is counted
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // every wave's records have arrived before the workgroup is counted
   __syncthreads();
   if (threadIdx.x == 0) {
-    turn = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    turn = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (turn == gridDim.x - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
@@ -371,35 +380,53 @@ struct PolicyFinish {
   int S, lg, by_rows, masked;   // 2^lg lanes take a row's records (a wave a row: 1,116 us for 4,096 rows of two, 140 so)
   float *loss, *kl, *clip, *dtheta;
 };
+constexpr int kAhead = 4;   // records a lane asks for before it adds the first
 template <int D>
 __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, int blocks) {
   const int step = 1 << p.lg, l = threadIdx.x & (step - 1), group = threadIdx.x >> p.lg, groups = kThreads >> p.lg;
   double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
   if (p.masked || block == 0) {
     if (p.by_rows && p.S > 1) {
-      for (int64_t k = 0; k < p.rows; k += groups) {   // all lanes, for the sums over a group
-        const int64_t row = k + group;
-        double u[4] = {};
-        if (row < p.rows)
-          for (int s = l; s < p.S; s += step) {
-            const float4 v = p.tot[row * p.S + s];
-            u[0] += v.x; u[1] += v.y; u[2] += v.z; u[3] += v.w;
+      for (int64_t k = 0; k < p.rows; k += kAhead * groups) {   // all lanes, for the sums over a group
+        float4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = p.tot[min(k + i * groups + group, p.rows - 1) * p.S + min(l, p.S - 1)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (k + i * groups >= p.rows) break;
+          const int64_t row = k + i * groups + group;
+          const bool on = row < p.rows;
+          double u[4] = {};
+          if (on && l < p.S) {
+            u[0] = v[i].x; u[1] = v[i].y; u[2] = v[i].z; u[3] = v[i].w;
+            for (int s = l + step; s < p.S; s += step) {
+              const float4 w = p.tot[row * p.S + s];
+              u[0] += w.x; u[1] += w.y; u[2] += w.z; u[3] += w.w;
+            }
           }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = group_sum_d(u[i], p.lg);
-        if (l == 0 && u[3] > 0.0) {
-          const double w = 1.0 / u[3];
+          for (int c = 0; c < 4; ++c) u[c] = group_sum_d(u[c], p.lg);
+          if (l == 0 && u[3] > 0.0) {
+            const double w = 1.0 / u[3];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) t[i] += u[i] * w;
-          t[4] += 1.0;
+            for (int c = 0; c < 4; ++c) t[c] += u[c] * w;
+            t[4] += 1.0;
+          }
         }
       }
     } else {
-      for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) {
-        const float4 v = p.tot[k];
-        const double w = !p.by_rows ? 1.0 : v.w > 0.0f ? 1.0 / v.w : 0.0;
-        t[0] += w * v.x; t[1] += w * v.y; t[2] += w * v.z; t[3] += w * v.w;
-        t[4] += v.w > 0.0f ? 1.0 : 0.0;
+      const int64_t n = p.rows * p.S;
+      for (int64_t k = threadIdx.x; k < n; k += kAhead * kThreads) {
+        float4 v[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) v[i] = p.tot[min(k + i * kThreads, n - 1)];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+          if (k + i * kThreads >= n) break;
+          const double w = !p.by_rows ? 1.0 : v[i].w > 0.0f ? 1.0 / v[i].w : 0.0;
+          t[0] += w * v[i].x; t[1] += w * v[i].y; t[2] += w * v[i].z; t[3] += w * v[i].w;
+          t[4] += v[i].w > 0.0f ? 1.0 : 0.0;
+        }
       }
     }
     block_sum_d<5, kThreads>(t);
@@ -413,13 +440,21 @@ __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, 
   }
   if (!p.dtheta) return;
   if (p.S == 1) {
-    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)blocks * kThreads) {
-      double w = inv;
-      if (p.by_rows) {
-        const float n = p.masked ? p.tot[k / (2 * D)].w : (float)p.E;
-        w = n > 0.0f ? inv / n : 0.0;
+    const int64_t n = p.rows * 2 * D, stride = (int64_t)blocks * kThreads;
+    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < n; k += kAhead * 2 * stride) {
+      float g[kAhead * 2], c[kAhead * 2];
+#pragma unroll
+      for (int i = 0; i < kAhead * 2; ++i) {
+        const int64_t at = min(k + i * stride, n - 1);
+        g[i] = p.grad[at];
+        c[i] = p.by_rows && p.masked ? p.tot[at / (2 * D)].w : (float)p.E;
       }
-      p.dtheta[k] = (float)(p.grad[k] * w);
+#pragma unroll
+      for (int i = 0; i < kAhead * 2; ++i) {
+        if (k + i * stride >= n) break;
+        const double w = !p.by_rows ? inv : c[i] > 0.0f ? inv / c[i] : 0.0;
+        p.dtheta[k + i * stride] = (float)(g[i] * w);
+      }
     }
     return;
   }
@@ -470,8 +505,9 @@ struct PolicyArgs {
   PolicyFinish fin;
 };
 
-template <int D, bool kRef>
-__global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
+// kEnds: the launch ends in its last workgroup.
+template <int D, bool kRef, bool kEnds>
+__global__ __launch_bounds__(kThreads, kEnds ? 4 : 8) void k_policy(PolicyArgs p) {
   const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
   const int64_t unit = (((int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6)) << (6 - p.lg)) + (lane >> p.lg);
   const bool on = unit < p.units;
@@ -524,15 +560,17 @@ __global__ __launch_bounds__(kThreads, 8) void k_policy(PolicyArgs p) {
       float v = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) v += sums[w][threadIdx.x];
-      if (threadIdx.x < 2 * D) p.grad[(int64_t)blockIdx.x * 2 * D + threadIdx.x] = v;
-      else reinterpret_cast<float*>(p.tot + blockIdx.x)[threadIdx.x - 2 * D] = v;
+      put_record<kEnds>(threadIdx.x < 2 * D ? p.grad + (int64_t)blockIdx.x * 2 * D + threadIdx.x
+                                            : reinterpret_cast<float*>(p.tot + blockIdx.x) + threadIdx.x - 2 * D, v);
     }
   } else if (on && l == 0) {
-    p.tot[unit] = make_float4(acc[2 * D], acc[2 * D + 1], acc[2 * D + 2], acc[2 * D + 3]);
 #pragma unroll
-    for (int j = 0; j < 2 * D; ++j) p.grad[unit * 2 * D + j] = acc[j];
+    for (int j = 0; j < 4; ++j) put_record<kEnds>(reinterpret_cast<float*>(p.tot + unit) + j, acc[2 * D + j]);
+#pragma unroll
+    for (int j = 0; j < 2 * D; ++j) put_record<kEnds>(p.grad + unit * 2 * D + j, acc[j]);
   }
-  if (p.ticket && last_block(p.ticket)) policy_finish<D>(p.fin, 0, 1);
+  if constexpr (kEnds)
+    if (last_block(p.ticket)) policy_finish<D>(p.fin, 0, 1);
 }
 
 // ---- preference loss -----------------------------------------------------------
@@ -549,29 +587,60 @@ __device__ __forceinline__ void pref_finish(const PrefFinish& p, int block, int 
   const int step = 1 << p.lg, l = threadIdx.x & (step - 1), group = threadIdx.x >> p.lg, groups = kThreads >> p.lg;
   if (block == 0 && p.loss) {
     double t[1] = {0.0};
-    for (int64_t k = threadIdx.x; k < p.rows * p.S; k += kThreads) t[0] += p.in[k * (2 * D + 1) + 2 * D];
+    const int64_t n = p.rows * p.S;
+    for (int64_t k = threadIdx.x; k < n; k += kAhead * kThreads) {
+      float v[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) v[i] = p.in[min(k + i * kThreads, n - 1) * (2 * D + 1) + 2 * D];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) t[0] += k + i * kThreads < n ? v[i] : 0.0f;
+    }
     block_sum_d<1, kThreads>(t);
     if (threadIdx.x == 0) *p.loss = (float)(t[0] * p.inv_pairs);
   }
   if (!p.dtheta) return;
   const double w = p.beta * p.inv_pairs;
   if (p.S == 1) {
-    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < p.rows * 2 * D; k += (int64_t)blocks * kThreads)
-      p.dtheta[k] = (float)(p.in[k / (2 * D) * (2 * D + 1) + k % (2 * D)] * w);
+    const int64_t n = p.rows * 2 * D, stride = (int64_t)blocks * kThreads;
+    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < n; k += kAhead * 2 * stride) {
+      float v[kAhead * 2];
+#pragma unroll
+      for (int i = 0; i < kAhead * 2; ++i) {
+        const int64_t at = min(k + i * stride, n - 1);
+        v[i] = p.in[at / (2 * D) * (2 * D + 1) + at % (2 * D)];
+      }
+#pragma unroll
+      for (int i = 0; i < kAhead * 2; ++i)
+        if (k + i * stride < n) p.dtheta[k + i * stride] = (float)(v[i] * w);
+    }
     return;
   }
-  for (int64_t k = (int64_t)block * groups; k < p.rows; k += (int64_t)blocks * groups) {
-    const int64_t row = k + group;
-    double u[2 * D] = {};
-    if (row < p.rows)
-      for (int s = l; s < p.S; s += step)
+  const int64_t stride = (int64_t)blocks * groups;
+  for (int64_t k = (int64_t)block * groups; k < p.rows; k += kAhead * stride) {
+    float v[kAhead][2 * D];
 #pragma unroll
-        for (int j = 0; j < 2 * D; ++j) u[j] += p.in[(row * p.S + s) * (2 * D + 1) + j];
+    for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-    for (int j = 0; j < 2 * D; ++j) u[j] = group_sum_d(u[j], p.lg);
-    if (l == 0 && row < p.rows)
+      for (int j = 0; j < 2 * D; ++j)
+        v[i][j] = p.in[(min(k + i * stride + group, p.rows - 1) * p.S + min(l, p.S - 1)) * (2 * D + 1) + j];
 #pragma unroll
-      for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
+    for (int i = 0; i < kAhead; ++i) {
+      if (k + i * stride >= p.rows) break;
+      const int64_t row = k + i * stride + group;
+      double u[2 * D] = {};
+      if (row < p.rows && l < p.S) {
+#pragma unroll
+        for (int j = 0; j < 2 * D; ++j) u[j] = v[i][j];
+        for (int s = l + step; s < p.S; s += step)
+#pragma unroll
+          for (int j = 0; j < 2 * D; ++j) u[j] += p.in[(row * p.S + s) * (2 * D + 1) + j];
+      }
+#pragma unroll
+      for (int j = 0; j < 2 * D; ++j) u[j] = group_sum_d(u[j], p.lg);
+      if (l == 0 && row < p.rows)
+#pragma unroll
+        for (int j = 0; j < 2 * D; ++j) p.dtheta[row * 2 * D + j] = (float)(u[j] * w);
+    }
   }
 }
 template <int D>
@@ -592,7 +661,7 @@ struct PrefArgs {
   int S, lg;
   float beta, eps;
   float* margin;              // or NULL
-  const float* part;          // k_pref<D, true>: [all pairs][slices][2d + 1]
+  const float* part;          // k_pref with kJoin: [all pairs][slices][2d + 1]
   int slices;
   float* out;                 // [units][2d + 1] (gradient, loss), or the slices' part
   uint32_t* ticket;           // or NULL: a launch of k_pref_finish follows, or nothing
@@ -621,7 +690,7 @@ __device__ __forceinline__ void add_set(const PrefArgs& p, int which, int64_t pa
 
 // A unit: one wave, some pairs of one row, 2^lg lanes a pair.  kJoin: the pairs'
 // sums come in slices from k_pref_slices.
-template <int D, bool kJoin>
+template <int D, bool kJoin, bool kEnds>
 __global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
   const int lane = threadIdx.x & 63, step = 1 << p.lg, l = lane & (step - 1);
   const int64_t unit = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6);
@@ -667,8 +736,9 @@ __global__ __launch_bounds__(kThreads) void k_pref(PrefArgs p) {
   group_sum(acc, 6);
   if (any && lane == 0)
 #pragma unroll
-    for (int j = 0; j < 2 * D + 1; ++j) p.out[unit * (2 * D + 1) + j] = acc[j];
-  if (p.ticket && last_block(p.ticket)) pref_finish<D>(p.fin, 0, 1);
+    for (int j = 0; j < 2 * D + 1; ++j) put_record<kEnds>(p.out + unit * (2 * D + 1) + j, acc[j]);
+  if constexpr (kEnds)
+    if (last_block(p.ticket)) pref_finish<D>(p.fin, 0, 1);
 }
 
 // Long sets: a unit is a wave on one slice of one pair's sets.
@@ -695,11 +765,13 @@ __global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
 }
 
 // ---- plans ---------------------------------------------------------------------
-// Whether a launch ends in its last workgroup instead of in a second launch: where that has
-// few rows to join (one row of 16,384 events 12.9 us against 17.1; with 1,024 rows, one
-// workgroup's loads one after the other, 36 against 18.6, and 279 against 16.6 for pairs).
-bool ends_in_last(int64_t blocks, int64_t rows, int records, int d) {
-  return blocks <= 512 && (records == 1 ? rows * 2 * d <= 2 * kThreads : rows <= 2 * kWaves);
+// Whether a launch ends in its last workgroup instead of in a second launch: where few
+// workgroups are counted, one after the other, and one workgroup can join what they left
+// (with 256 workgroups 1,024 rows of 100 events 15.8 us against 17.3, one row of 16,384
+// events 12.9 against 17.1; with 512 single-event pairs of 1,024 rows 18.3 against 14.8, with
+// 1,024 pairs of sets 55 against 26).
+bool ends_in_last(int64_t blocks, int64_t rows, int d) {
+  return blocks <= 256 && rows * 2 * d <= 8192;
 }
 constexpr int64_t kTargetUnits = 8192;   // waves that share an array of rows (4,096, 20,480 and 40,960: 128, 131 and 155 us against 127)
 
@@ -750,7 +822,8 @@ PrefPlan pref_plan(int64_t rows, int64_t pairs, int64_t T, int d) {
     p.slices = (int)ceil_div(T, p.slice_chunk);
   }
   p.lg = lanes_log(p.slices ? p.slices : T);
-  const int64_t most = ceil_div(pairs, 64 >> p.lg), want = kTargetUnits / rows;
+  // a wave takes its lanes' pairs at least twice where a pair is an event a lane: fewer records
+  const int64_t most = ceil_div(pairs, (64 >> p.lg) * (T <= 64 ? 2 : 1)), want = kTargetUnits / rows;
   p.S = (int)(want < 1 ? 1 : want > most ? most : want);
   p.chunk = ceil_div(pairs, p.S);
   p.S = (int)ceil_div(pairs, p.chunk);
@@ -772,9 +845,11 @@ hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x
   a.fin = PolicyFinish{a.tot, a.grad, P.n_theta, P.events_per_theta, pl.records, lanes_log(pl.records),
                        P.average == SAGIPS_MEAN_ROWS, mask != nullptr, loss, kl, clip, dtheta};
   const dim3 grid(wave_blocks(ceil_div(pl.units, 64 >> pl.lg)));
-  if (ends_in_last(grid.x, P.n_theta, pl.records, D)) a.ticket = ticket;
+  if (ends_in_last(grid.x, P.n_theta, D)) a.ticket = ticket;
   if (tm) tm->begin("policy");
-  hipLaunchKernelGGL((P.theta_ref ? k_policy<D, true> : k_policy<D, false>), grid, dim3(kThreads), 0, st, a);
+  const auto kernel = P.theta_ref ? (a.ticket ? k_policy<D, true, true> : k_policy<D, true, false>)
+                                  : (a.ticket ? k_policy<D, false, true> : k_policy<D, false, false>);
+  hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ticket) return e;
@@ -825,9 +900,11 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
   a.fin = PrefFinish{sums, P.n_theta, pl.S, lanes_log(pl.S), P.beta, 1.0 / (double)all, loss, dtheta};
   const unsigned blocks = wave_blocks(pl.units);
   const bool finish = loss || dtheta;
-  if (finish && ends_in_last(blocks, P.n_theta, pl.S, D)) a.ticket = ticket;
+  if (finish && ends_in_last(blocks, P.n_theta, D)) a.ticket = ticket;
   if (tm) tm->begin("preference");
-  hipLaunchKernelGGL((pl.slices ? k_pref<D, true> : k_pref<D, false>), dim3(blocks), dim3(kThreads), 0, st, a);
+  const auto kernel = pl.slices ? (a.ticket ? k_pref<D, true, true> : k_pref<D, true, false>)
+                                : (a.ticket ? k_pref<D, false, true> : k_pref<D, false, false>);
+  hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, st, a);
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !finish || a.ticket) return e;
