@@ -548,7 +548,9 @@ class Context:
     def _rows(self, t, name, like=None):
         """A table of parameter rows [n_theta][4] or [n_theta][6]."""
         import torch
-        _check_tensor(t, name, torch.float32, None if like is None else like.shape, self.device)
+        if like is not None:
+            return _check_tensor(t, name, torch.float32, like.shape, self.device)
+        _check_tensor(t, name, torch.float32, None, self.device)
         if t.dim() != 2 or t.shape[1] not in (4, 6):
             raise ValueError(f"{name} must be [n_theta][4] or [n_theta][6]")
 
@@ -601,13 +603,14 @@ class Context:
             raise ValueError("average must be 'events' or 'rows'")
         P = Policy(theta.data_ptr(), theta_old.data_ptr(), _ptr(theta_ref), n, d, E, clip_low, clip_high, kl_coef,
                    MEAN_ROWS if average == "rows" else MEAN_EVENTS)
-        scalars = torch.empty(3, dtype=f32, device=theta.device)
+        scalars = theta.new_empty(3, 1)
         dtheta = torch.empty_like(theta) if want_grad else None
         self._owned(scalars, dtheta, theta, theta_old, theta_ref, x, adv, mask)
         at = scalars.data_ptr()
         self._check(self.lib.sagips_policy_loss(self.h, ctypes.byref(P), x.data_ptr(), adv.data_ptr(), m, at, at + 4,
                                                 at + 8, _ptr(dtheta)))
-        return {"loss": scalars[0:1], "kl": scalars[1:2], "clip_frac": scalars[2:3], "dtheta": dtheta}
+        loss, kl, clip_frac = scalars.unbind()           # [1] each
+        return {"loss": loss, "kl": kl, "clip_frac": clip_frac, "dtheta": dtheta}
 
     def preference_loss(self, theta, theta_ref, chosen, rejected, len_chosen=None, len_rejected=None, beta: float = 0.1,
                         label_smoothing: float = 0.0, want_grad: bool = True) -> dict:
@@ -631,8 +634,7 @@ class Context:
             _check_tensor(t, name, torch.int32, (P,), dev)
         a = Preference(theta.data_ptr(), theta_ref.data_ptr(), n, d, P // n, chosen.shape[1], rejected.shape[1], beta,
                        label_smoothing)
-        loss = torch.empty(1, dtype=f32, device=theta.device)
-        margin = torch.empty(P, dtype=f32, device=theta.device)
+        loss, margin = theta.new_empty(1), theta.new_empty(P)
         dtheta = torch.empty_like(theta) if want_grad else None
         self._owned(loss, margin, dtheta, theta, theta_ref, chosen, rejected, len_chosen, len_rejected)
         self._check(self.lib.sagips_preference_loss(self.h, ctypes.byref(a), chosen.data_ptr(), _ptr(len_chosen),

@@ -74,7 +74,7 @@ struct sagips_ctx {
   void* ws = nullptr;
   size_t ws_cap = 0;
   size_t ws_refused = SIZE_MAX; // bf16: the workspace that the device refused last
-  uint32_t* ticket = nullptr;   // one counter, 0 between calls (made with the first call that needs it)
+  uint32_t* ticket = nullptr;   // counters, 0 between calls (made with the first call that needs it)
   std::string err = "no error";
   bool timing = false;
   int bf16_chunk_rows = 0;      // 0: the library's default
@@ -132,18 +132,18 @@ inline sagips_status ensure_ws(sagips_ctx* c, size_t bytes) {
   return SAGIPS_OK;
 }
 
-// The context's counter, cleared by a kernel on its stream when it is made.
+// The context's counters, cleared by a kernel on its stream when they are made.
 inline sagips_status ensure_ticket(sagips_ctx* c) {
   if (c->ticket) return SAGIPS_OK;
   void* p = nullptr;
-  if (hipMalloc(&p, 256) != hipSuccess) {
+  if (hipMalloc(&p, kTicketWords * sizeof(uint32_t)) != hipSuccess) {
     (void)hipGetLastError();
-    return fail(c, SAGIPS_E_NOMEM, "allocation of the context's counter failed");
+    return fail(c, SAGIPS_E_NOMEM, "allocation of the context's counters failed");
   }
   const hipError_t e = launch_clear(static_cast<uint32_t*>(p), c->stream);
   if (e != hipSuccess) {
     (void)hipFree(p);
-    return hip_fail(c, e, "clearing the context's counter");
+    return hip_fail(c, e, "clearing the context's counters");
   }
   c->ticket = static_cast<uint32_t*>(p);
   return SAGIPS_OK;

@@ -95,6 +95,7 @@ hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double b
 
 // policy.hip -----------------------------------------------------------------
 // `ticket`: one counter on the device, 0 before and after every launch that uses it.
+constexpr int kTicketWords = 1024;   // of a context's counters
 hipError_t launch_clear(uint32_t* p, hipStream_t st);
 size_t advantage_workspace(int64_t n_rows, int64_t E);
 hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,

@@ -354,18 +354,26 @@ __device__ __forceinline__ void put_record(float* p, float v) {
   else *p = v;
 }
 // Whether this workgroup is the last of its launch to come here, all the others' records
-// visible to it: one counter of the context, which the last puts back to 0.
+// visible to it.  16 counters of the context, then one of those that filled theirs (one for all:
+// 2 us more at 256 workgroups); whoever fills a counter puts it back to 0.
 // Only which workgroup is last depends on the order, not what it computes.
+constexpr int kCounters = 16, kApart = 32;             // a cache line each
 __device__ __forceinline__ bool last_block(uint32_t* ticket) {
-  __shared__ uint32_t turn;
+  __shared__ bool last;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // every wave's records have arrived before the workgroup is counted
   __syncthreads();
   if (threadIdx.x == 0) {
-    turn = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (turn == gridDim.x - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const auto fills = [](uint32_t* p, uint32_t n) {
+      const bool is = __hip_atomic_fetch_add(p, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+      if (is) __hip_atomic_store(p, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      return is;
+    };
+    const uint32_t mine = blockIdx.x % kCounters;
+    last = fills(ticket + (1 + mine) * kApart, (gridDim.x - mine + kCounters - 1) / kCounters) &&
+           fills(ticket, min(gridDim.x, (uint32_t)kCounters));
   }
   __syncthreads();
-  if (turn != gridDim.x - 1) return false;
+  if (!last) return false;
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
   return true;
 }
@@ -381,9 +389,21 @@ struct PolicyFinish {
   float *loss, *kl, *clip, *dtheta;
 };
 constexpr int kAhead = 4;   // records a lane asks for before it adds the first
-template <int D>
+template <int D, int kEach>   // kEach: values of a gradient of one record a row that a thread asks for at a time
 __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, int blocks) {
   const int step = 1 << p.lg, l = threadIdx.x & (step - 1), group = threadIdx.x >> p.lg, groups = kThreads >> p.lg;
+  const int64_t n_grad = p.rows * 2 * D, stride_g = (int64_t)blocks * kThreads;
+  float g[kEach], c[kEach];   // and their rows' counts, before the totals are waited for
+  const auto ask = [&](int64_t k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int64_t at = min(k + i * stride_g, n_grad - 1);
+      g[i] = p.grad[at];
+      c[i] = p.by_rows && p.masked ? p.tot[at / (2 * D)].w : (float)p.E;
+    }
+  };
+  int64_t k_grad = (int64_t)block * kThreads + threadIdx.x;
+  if (p.dtheta && p.S == 1) ask(k_grad);
   double t[5] = {};   // loss, KL, clipped, events (all weighted by 1 / events of the row if by_rows), rows with events
   if (p.masked || block == 0) {
     if (p.by_rows && p.S > 1) {
@@ -440,21 +460,15 @@ __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, 
   }
   if (!p.dtheta) return;
   if (p.S == 1) {
-    const int64_t n = p.rows * 2 * D, stride = (int64_t)blocks * kThreads;
-    for (int64_t k = (int64_t)block * kThreads + threadIdx.x; k < n; k += kAhead * 2 * stride) {
-      float g[kAhead * 2], c[kAhead * 2];
+    for (; k_grad < n_grad; k_grad += kEach * stride_g) {
 #pragma unroll
-      for (int i = 0; i < kAhead * 2; ++i) {
-        const int64_t at = min(k + i * stride, n - 1);
-        g[i] = p.grad[at];
-        c[i] = p.by_rows && p.masked ? p.tot[at / (2 * D)].w : (float)p.E;
+      for (int i = 0; i < kEach; ++i) {
+        if (k_grad + i * stride_g >= n_grad) break;
+        // a row's average in fp32, as its sum was; the average over rows in 64 bits
+        const float v = !p.by_rows ? g[i] : c[i] > 0.0f ? g[i] / c[i] : 0.0f;
+        p.dtheta[k_grad + i * stride_g] = (float)(v * inv);
       }
-#pragma unroll
-      for (int i = 0; i < kAhead * 2; ++i) {
-        if (k + i * stride >= n) break;
-        const double w = !p.by_rows ? inv : c[i] > 0.0f ? inv / c[i] : 0.0;
-        p.dtheta[k + i * stride] = (float)(g[i] * w);
-      }
+      if (k_grad + kEach * stride_g < n_grad) ask(k_grad + kEach * stride_g);
     }
     return;
   }
@@ -478,7 +492,7 @@ __device__ __forceinline__ void policy_finish(const PolicyFinish& p, int block, 
 }
 template <int D>
 __global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
-  policy_finish<D>(p, blockIdx.x, gridDim.x);
+  policy_finish<D, 2>(p, blockIdx.x, gridDim.x);
 }
 
 // A unit is one slice of one row, run by a group of 2^lg lanes (a wave, or less
@@ -570,7 +584,7 @@ __global__ __launch_bounds__(kThreads, kEnds ? 4 : 8) void k_policy(PolicyArgs p
     for (int j = 0; j < 2 * D; ++j) put_record<kEnds>(p.grad + unit * 2 * D + j, acc[j]);
   }
   if constexpr (kEnds)
-    if (last_block(p.ticket)) policy_finish<D>(p.fin, 0, 1);
+    if (last_block(p.ticket)) policy_finish<D, 12>(p.fin, 0, 1);
 }
 
 // ---- preference loss -----------------------------------------------------------
@@ -917,9 +931,10 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
 
 }  // namespace
 
-static __global__ void k_clear(uint32_t* p) { *p = 0u; }
+static __global__ void k_clear(uint32_t* p) { p[threadIdx.x] = 0u; }
 hipError_t launch_clear(uint32_t* p, hipStream_t st) {
-  hipLaunchKernelGGL(k_clear, dim3(1), dim3(1), 0, st, p);
+  static_assert((1 + kCounters) * kApart <= kTicketWords && kTicketWords <= 1024, "one workgroup clears them");
+  hipLaunchKernelGGL(k_clear, dim3(1), dim3(kTicketWords), 0, st, p);
   return hipGetLastError();
 }
 
