@@ -779,11 +779,10 @@ __global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
 }
 
 // ---- plans ---------------------------------------------------------------------
-// Whether a launch ends in its last workgroup instead of in a second launch: where few
-// workgroups are counted, one after the other, and one workgroup can join what they left
-// (with 256 workgroups 1,024 rows of 100 events 15.8 us against 17.3, one row of 16,384
-// events 12.9 against 17.1; with 512 single-event pairs of 1,024 rows 18.3 against 14.8, with
-// 1,024 pairs of sets 55 against 26).
+// Whether a launch ends in its last workgroup instead of in a second launch: where one
+// workgroup can join what the others left in the time of that launch (up to 256 of them: 1,024
+// rows of 100 events 13.7 us a call against 15.7, 1,024 x 100 single-event pairs 11.7 against
+// 14.5; beyond, 600 rows of 600 events 27 against 14, 64 x 64 pairs of 100 events 40 against 13).
 bool ends_in_last(int64_t blocks, int64_t rows, int d) {
   return blocks <= 256 && rows * 2 * d <= 8192;
 }
