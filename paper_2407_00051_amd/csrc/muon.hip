@@ -410,20 +410,21 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
       // lanes run along the rows of the caller's matrix
       const int64_t base = (int64_t)(z - jobs.first[t]) * jobs.rows * jobs.cols;
       const int r0 = 32 * (flip ? bj : bi), col = 32 * (flip ? bi : bj) + lr;
+      const auto row_of = [&](int r) __attribute__((always_inline)) { return r0 + 8 * (r >> 2) + 4 * lh + (r & 3); };
+      float old[16];   // all parameters before the first is moved, from places inside the matrix
+      if (jobs.m[t])
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          old[r] = static_cast<const float*>(jobs.out[t])[base + (int64_t)min(row_of(r), jobs.rows - 1) * jobs.cols +
+                                                          min(col, jobs.cols - 1)];
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int rr = r0 + 8 * (r >> 2) + 4 * lh + (r & 3);
-        if (rr >= jobs.rows || col >= jobs.cols) continue;
-        const int64_t to = base + (int64_t)rr * jobs.cols + col;
+        if (row_of(r) >= jobs.rows || col >= jobs.cols) continue;
+        const int64_t to = base + (int64_t)row_of(r) * jobs.cols + col;
         const float x = v[r] * kInvScale;
-        if (jobs.m[t]) {
-          float* w = static_cast<float*>(jobs.out[t]) + to;
-          *w = fmaf(-jobs.rate, x, jobs.decay * *w);
-        } else if (jobs.out_bf16) {
-          static_cast<u16*>(jobs.out[t])[to] = to_bf16(x);
-        } else {
-          static_cast<float*>(jobs.out[t])[to] = x;
-        }
+        if (jobs.m[t]) static_cast<float*>(jobs.out[t])[to] = fmaf(-jobs.rate, x, jobs.decay * old[r]);
+        else if (jobs.out_bf16) static_cast<u16*>(jobs.out[t])[to] = to_bf16(x);
+        else static_cast<float*>(jobs.out[t])[to] = x;
       }
     }
   }
