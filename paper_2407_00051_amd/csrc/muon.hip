@@ -220,8 +220,8 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
 // LDS traffic and no barrier (the same tile with operands shared through LDS was bound by
 // LDS: 61 us a product at 2,048 x 2,048, of which 21 are matrix instructions).  The
 // quarters are added through LDS at the end, each wave keeping a quarter of the tile.
-// 2,048 x 2,048: the symmetric products take 33-37 us each, the others 53-59, i.e. 0.79 and
-// 0.88 PFLOP/s of fp16 products, with the matrix cores 59% and 62% busy while a unit works;
+// 2,048 x 2,048: the symmetric products take 32-36 us each, the others 51-57, i.e. 0.83 and
+// 0.92 PFLOP/s of fp16 products, with the matrix cores 59% and 61% busy while a unit works;
 // the rest is the first fragments' latency and the sums at the end.  Small counts (three of
 // 512 x 512: 6-8 us a product) are launches that wait for each other.
 enum Mode { kGram, kPoly, kApply, kStore };

@@ -502,11 +502,11 @@ __global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
 // Bound by VALU issue: 64 events of three coordinates against two rows take 26
 // transcendental and 186 other operations, 48% of all in pairs (adds, products and
 // fmas with a literal do; compares, selects, fmac and fmas of three registers do not), and
-// the vector units issue in 99% of the cycles in which a compute unit works.  1,024 x 16,384
-// events with mask and KL term: 109 us, 116 with the
-// second launch; reading them takes 61 at the rate of a large copy.  64 registers, so that
-// the 8,192 waves are resident together: with 71, seven to a SIMD and an eighth after them,
-// 139 us.
+// the vector units issue in all of the cycles in which a compute unit works.  1,024 x 16,384
+// events with mask and KL term: 114-116 us with the second launch; reading them takes 61 at
+// the rate of a large copy.  Where no joining follows in it, the kernel is held to 64
+// registers, so that the 8,192 waves are resident together: with 71, seven to a SIMD and an
+// eighth after them, 139 us.
 struct PolicyArgs {
   const float *theta, *theta_old, *theta_ref, *x, *adv;
   const uint8_t* mask;
@@ -665,7 +665,8 @@ __global__ __launch_bounds__(kThreads) void k_pref_finish(PrefFinish p) {
 // A pair's sums over its two sets, chosen minus rejected: of the log2 ratios and
 // of dl/dtheta; both are linear, so one pass over the events gives the margin
 // and, once it is known, the gradient.  VALU issue, as k_policy, with one row to compare
-// with; 2.9 M events of two coordinates 18-19 us of kernel, in 26 with the second launch.
+// with, in 76% of the busy cycles since a wave's pairs have unequal lengths; 2.9 M events of two
+// coordinates 18-19 us of kernel, 25 with the second launch.
 struct PrefArgs {
   const float *theta, *theta_ref;
   const float* x[2];          // chosen, rejected
