@@ -339,7 +339,8 @@ sagips_status sagips_adam_step(sagips_ctx* ctx, const sagips_param_set* set, int
  *   adv = (reward - mean_i) / (std_i + eps),  std_i the population deviation;
  * with normalise == 0 only reward - mean_i.  Events outside the mask get 0 and
  * their rewards are not looked at; a row with none is all 0.  A row of equal
- * rewards gives exactly 0.
+ * rewards (up to 2^29 of them), or with one valid event, gives exactly 0,
+ * whatever eps.
  *   reward  [n_rows][events_per_row] fp32
  *   mask    [n_rows][events_per_row] bytes, nonzero = valid, any alignment; NULL: all valid
  *   adv     as reward; may be reward itself, otherwise must not overlap it

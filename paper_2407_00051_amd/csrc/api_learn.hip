@@ -130,7 +130,7 @@ sagips_status sagips_group_advantage(sagips_ctx* c, const float* reward, const u
     DeviceGuard g(c->device);
     sagips_status s = ensure_ws(c, advantage_workspace(n_rows, events_per_row));
     if (s != SAGIPS_OK) return s;
-    hipError_t e = launch_advantage(reward, mask, n_rows, events_per_row, normalise != 0, (float)eps, adv, c->ws, c->stream,
+    hipError_t e = launch_advantage(reward, mask, n_rows, events_per_row, normalise != 0, eps, adv, c->ws, c->stream,
                                     timer_of(c));
     return e == hipSuccess ? SAGIPS_OK : hip_fail(c, e, "group_advantage launch");
   });

@@ -98,7 +98,7 @@ hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double b
 constexpr int kTicketWords = 1024;   // of a context's counters
 hipError_t launch_clear(uint32_t* p, hipStream_t st);
 size_t advantage_workspace(int64_t n_rows, int64_t E);
-hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,
+hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, double eps,
                             float* adv, void* ws, hipStream_t st, Timer* tm);
 size_t policy_workspace(const sagips_policy& P);
 hipError_t launch_policy(const sagips_policy& P, const float* x, const float* adv, const uint8_t* mask, float* loss,

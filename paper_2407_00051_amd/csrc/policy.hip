@@ -196,13 +196,19 @@ __device__ __forceinline__ void block_sum_d(double (&v)[N]) {
 
 // ---- advantages --------------------------------------------------------------
 // (r - mean) / (std + eps) over a row's valid events.  The mean is a 64-bit sum,
-// so that a row of equal rewards gives zeros; deviations are formed in 64 bits
-// and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26 us
+// so that a row of equal rewards gives zeros, whatever eps; deviations and their
+// quotients are formed in 64 bits and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26 us
 // (128 MB at 4.9 TB/s), 16,384 x 1,000 22, 4,096 x 4,097 29; by the time of one read, two
 // sums over lanes and one write where they are few (6-7 us a call).
 
 constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing, at most
 constexpr int kAdvBlock = 1024;
+
+// What a row's deviations are multiplied by: 0 where there are none, since 1 / (0 + eps) may be infinite.
+__device__ __forceinline__ double inverse_deviation(double squares, double n, double eps) {
+  const double sd = n > 0.0 ? sqrt(squares / n) : 0.0;
+  return sd > 0.0 ? 1.0 / (sd + eps) : 0.0;
+}
 
 // Reads a lane's events e0 + i * step < E of the row at `off`: v, 0 where not valid, and a bit for
 // each valid one.  All reads are at places inside the row, so that none waits for a branch
@@ -236,7 +242,7 @@ __device__ __forceinline__ uint32_t load_rewards(const float* reward, const uint
 // workgroup (up to 1,024 x 16): read once, held in registers, written once.
 template <bool kBlock, int kHeld>
 __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(const float* reward, const uint8_t* __restrict__ mask,
-                                                                            int n_rows, int E, int lg, float eps, int normalise,
+                                                                            int n_rows, int E, int lg, double eps, int normalise,
                                                                             float* adv) {
   const int lane = threadIdx.x & 63, step = kBlock ? blockDim.x : 1 << lg;
   const int l = kBlock ? threadIdx.x : lane & (step - 1);
@@ -263,21 +269,20 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
   double q[1] = {0.0};
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
-    v[i] = (valid >> i) & 1u ? (float)((double)v[i] - mean) : 0.0f;
-    q[0] = fma((double)v[i], (double)v[i], q[0]);
+    const double dev = (valid >> i) & 1u ? (double)v[i] - mean : 0.0;
+    q[0] = fma(dev, dev, q[0]);
   }
-  float inv = 1.0f;
+  double inv = 1.0;
   if (normalise) {
     if constexpr (kBlock) block_sum_d<1, kAdvBlock>(q);
     else
       for (int s = 0; s < lg; ++s) q[0] += __shfl_xor(q[0], 1 << s, 64);
-    const float sd = n > 0.0 ? (float)sqrt(q[0] / n) : 0.0f;
-    inv = 1.0f / (sd + eps);
+    inv = inverse_deviation(q[0], n, eps);
   }
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int e = l + i * step;
-    if (on && e < E) to[off + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
+    if (on && e < E) to[off + e] = (valid >> i) & 1u ? (float)(((double)v[i] - mean) * inv) : 0.0f;
   }
 }
 
@@ -311,7 +316,7 @@ __global__ __launch_bounds__(kAdvBlock, 8) void k_adv_slices(const float* __rest
   }
 }
 __global__ __launch_bounds__(kAdvBlock, 8) void k_adv_apply(const float* reward, const uint8_t* __restrict__ mask, int64_t E,
-                                                         int n_slices, const double* __restrict__ part, float eps,
+                                                         int n_slices, const double* __restrict__ part, double eps,
                                                          int normalise, float* adv) {
   const int64_t row = blockIdx.x / n_slices, s = blockIdx.x % n_slices, base = row * E + s * kAdvSlice;
   const int n = (int)min((int64_t)kAdvSlice, E - s * kAdvSlice);
@@ -331,15 +336,15 @@ __global__ __launch_bounds__(kAdvBlock, 8) void k_adv_apply(const float* reward,
     const double dm = p[3 * i + 1] - mean;
     q[0] += p[3 * i] > 0.0 ? p[3 * i + 2] + p[3 * i] * dm * dm : 0.0;
   }
-  float inv = 1.0f;
+  double inv = 1.0;
   if (normalise) {
     block_sum_d<1, kAdvBlock>(q);
-    inv = 1.0f / ((t[1] > 0.0 ? (float)sqrt(q[0] / t[1]) : 0.0f) + eps);
+    inv = inverse_deviation(q[0], t[1], eps);
   }
 #pragma unroll
   for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) {
     const int e = threadIdx.x + i * kAdvBlock;
-    if (e < n) adv[base + e] = (valid >> i) & 1u ? (float)((double)v[i] - mean) * inv : 0.0f;
+    if (e < n) adv[base + e] = (valid >> i) & 1u ? (float)(((double)v[i] - mean) * inv) : 0.0f;
   }
 }
 
@@ -942,7 +947,7 @@ size_t advantage_workspace(int64_t n_rows, int64_t E) {
   return E <= kAdvSlice ? 0 : (size_t)n_rows * ceil_div(E, kAdvSlice) * 3 * sizeof(double);
 }
 
-hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, float eps,
+hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, double eps,
                             float* adv, void* ws, hipStream_t st, Timer* tm) {
   if (tm) tm->begin("advantage");
   if (E <= 64 * kAdvHeld) {
