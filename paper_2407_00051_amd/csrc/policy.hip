@@ -49,6 +49,16 @@ struct Against {
   float a[D], da[D], db[D], c;   // c: sum log2(a/a') + log2(b/b')
 };
 
+// ln(a / b) of positive a, b, as +- ln(1 + (larger - smaller) / smaller): the difference is exact
+// within a factor of two, and the quotient, unlike one over the larger, does not run into -1.  Where
+// it is beyond fp32, the difference of two logarithms of 88 or more in all.
+__device__ __forceinline__ float log_quotient(float a, float b) {
+  const bool below = a < b;
+  const float hi = below ? b : a, lo = below ? a : b, q = (hi - lo) / lo;
+  const float l = q < INFINITY ? log1pf(q) : logf(hi) - logf(lo);
+  return below ? -l : l;
+}
+
 // Reads a row and the kOthers it is compared with.  Every group of `step` lanes (this lane its
 // l-th) shares the divisions and logarithms out among its lanes, one item a lane where the group
 // has as many, and has them back through `shared` (2D (kOthers + 1) floats of the group): with
@@ -63,9 +73,7 @@ __device__ __forceinline__ void load_rows(const float* __restrict__ th, const fl
     float den = at;
 #pragma unroll
     for (int i = 0; i < kOthers; ++i) den = w == i + 1 ? others[i][j] : den;
-    // log(a/a') = log1p((a - a') / a'): the difference is exact for rows within a factor of two
-    const float q = (w ? at - den : 1.0f) / den;
-    shared[k] = w ? log1pf(q) : q;
+    shared[k] = w ? log_quotient(at, den) : 1.0f / at;
   }
   __syncthreads();
 #pragma unroll

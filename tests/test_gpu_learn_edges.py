@@ -6,7 +6,7 @@ import pytest
 
 import oracle
 from tests.parity import to_np
-from tests.test_gpu_learn import ADV_TOL, _t
+from tests.test_gpu_learn import ADV_TOL, TOL, _events, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,46 @@ def test_group_advantage_without_eps(gpu_ctx, rows, E, eps):
     some = [i for i in range(rows) if i > 1 and m[i].any()]
     ref = oracle.group_advantage(r[some], m[some], True, eps)
     assert np.all(np.abs(got[some] - ref) <= ADV_TOL * np.abs(ref).max(1, keepdims=True))
+
+
+# ---- rows far apart
+
+def _difference_terms(theta, ref, x):
+    """Of the log ratio of events x [n][d]: the sum of the absolute values of its terms, and of the
+    factors of its logarithms ln(1 - x^a)."""
+    a, b, a2, b2 = (np.float64(v) for v in (theta[0::2], theta[1::2], ref[0::2], ref[1::2]))
+    lx = np.log(np.clip(np.float64(x), oracle.learn.X_LO, oracle.learn.X_HI))
+    g, g2 = np.log(-np.expm1(a * lx)), np.log(-np.expm1(a2 * lx))
+    terms = (np.abs(np.log(a / a2)) + np.abs(np.log(b / b2)) + np.abs((a - a2) * lx) + np.abs(b - 1.0) * (np.abs(g) + np.abs(g2))
+             + np.abs((b - b2) * g2))
+    return terms.sum(1), np.sum(np.abs(b - 1.0) * 2.0 + np.abs(b - b2)) * np.ones(len(x))
+
+
+@pytest.mark.parametrize("factor", [1e-2, 1e-3, 1e-6, 1e-9, 1e3])
+@pytest.mark.parametrize("d", [2, 3])
+def test_log_ratio_of_rows_far_apart(gpu_ctx, d, factor):
+    """Sets of unequal size, so that the rows' own logarithms stay in the margin.  Tolerance: of an
+    event's terms 8 units in the last place of fp32 (a logarithm, its factor, six sums), and 6e-7 for
+    each ln(1 - x^a) times its factor."""
+    print(f"case far rows d={d} factor={factor}", flush=True)
+    rng = np.random.default_rng(int(1e4 * d) + int(-np.log10(factor)) + 20)
+    rows, T, T2 = 9, 5, 2
+    ref = rng.uniform(1.0, 5.0, (rows, 2 * d)).astype(np.float32)
+    theta = ref.copy()
+    which = rng.integers(0, 2 * d, rows)
+    theta[np.arange(rows), which] *= np.float32(factor)
+    theta[0] = ref[0] * np.float32(factor)
+    c = dict(theta=theta, theta_ref=ref, chosen=_events(rng, ref, T), rejected=_events(rng, ref, T2))
+    beta = 0.01
+    want = oracle.preference_loss(**c, len_chosen=None, len_rejected=None, beta=beta)
+    got = gpu_ctx.preference_loss(**{k: _t(v) for k, v in c.items()}, beta=beta)
+    tol = np.zeros(rows)
+    for i in range(rows):
+        for k in ("chosen", "rejected"):
+            terms, logs = _difference_terms(theta[i], ref[i], c[k][i])
+            tol[i] += beta * np.sum(8 * 2.0 ** -24 * terms + 6e-7 * logs)
+    err = np.abs(to_np(got["margin"]).astype(np.float64) - want["margin"])
+    print(f"  worst of error / tolerance {np.max(err / tol):.3f}", flush=True)
+    assert np.all(err <= tol), (err / tol)
+    assert abs(got["loss"].item() - want["loss"]) <= tol.mean() + 1e-6 * want["loss"]
+    assert np.all(np.abs(to_np(got["dtheta"]) - want["dtheta"]) <= (TOL + tol[:, None]) * want["abs_dtheta"])
