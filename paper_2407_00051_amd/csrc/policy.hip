@@ -558,8 +558,9 @@ __global__ __launch_bounds__(kThreads, kEnds ? 4 : 8) void k_policy(PolicyArgs p
     const float A = p.adv[i];
     const Event<D> ev = at_row<D>(x, r);
     const float rho = fast_exp2(log2_ratio<D>(ev, r, o[0]));
-    // min(rho A, clip(rho) A)
-    const float in = fmaxf(fminf(rho, p.hi), p.lo) * A, out = rho * A;
+    // min(rho A, clip(rho) A); of A = 0 also where rho is beyond fp32 (the clip keeps a NaN)
+    const float in = __builtin_elementwise_maximum(__builtin_elementwise_minimum(rho, p.hi), p.lo) * A;
+    const float out = A == 0.0f ? in : rho * A;
     const bool cut = in < out;
     float loss = cut ? -in : -out;
     float wt = cut ? 0.0f : -out;

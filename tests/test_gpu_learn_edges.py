@@ -6,7 +6,7 @@ import pytest
 
 import oracle
 from tests.parity import to_np
-from tests.test_gpu_learn import ADV_TOL, TOL, _events, _t
+from tests.test_gpu_learn import ADV_TOL, TOL, _check_policy, _events, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -81,3 +81,29 @@ def test_log_ratio_of_rows_far_apart(gpu_ctx, d, factor):
     assert np.all(err <= tol), (err / tol)
     assert abs(got["loss"].item() - want["loss"]) <= tol.mean() + 1e-6 * want["loss"]
     assert np.all(np.abs(to_np(got["dtheta"]) - want["dtheta"]) <= (TOL + tol[:, None]) * want["abs_dtheta"])
+
+
+# ---- ratios beyond fp32
+
+def _far_event(rng, E):
+    """Rows (a = 1 and 2.2) between which the first event, near 0, has e^103 to one of density."""
+    near, far = np.array([[1.0, 2.0, 1.5, 2.0]], np.float32), np.array([[2.2, 2.0, 1.5, 2.0]], np.float32)
+    x = _events(rng, far, E)
+    x[0, 0, 0] = 2e-38
+    return near, far, x
+
+
+@pytest.mark.parametrize("zero", [0.0, -0.0])
+def test_event_without_advantage_beyond_the_ratios_range(gpu_ctx, zero):
+    """rho A of A = 0 is 0 however large the ratio; a NaN event stays NaN."""
+    rng = np.random.default_rng(21)
+    near, far, x = _far_event(rng, 50)
+    adv = rng.standard_normal((1, 50)).astype(np.float32)
+    adv[0, 0] = zero
+    c = dict(theta=near, theta_old=far, x=x, adv=adv)
+    want = oracle.policy_loss(**c, clip_low=1.0, clip_high=50.0)
+    t = {k: _t(v) for k, v in c.items()}
+    _check_policy(gpu_ctx.policy_loss(**t, clip_low=1.0, clip_high=50.0), want)
+    t["x"][0, 0, 0] = float("nan")
+    o = gpu_ctx.policy_loss(**t, clip_low=1.0, clip_high=50.0)
+    assert torch.isnan(o["loss"]).item() and torch.isnan(o["dtheta"][0, :2]).all().item()
