@@ -566,8 +566,10 @@ __global__ __launch_bounds__(kThreads, kEnds ? 4 : 8) void k_policy(PolicyArgs p
     float wt = cut ? 0.0f : -out;
     if constexpr (kRef) {
       const float t = -log2_ratio<D>(ev, r, o[kOthers - 1]) * kLn2, k = exp_minus_line(t);
-      loss = fmaf(p.beta, k, loss);
-      wt = fmaf(-p.beta, t + k, wt);
+      if (p.beta != 0.0f) {   // of all events: no weight, also on a K beyond fp32
+        loss = fmaf(p.beta, k, loss);
+        wt = fmaf(-p.beta, t + k, wt);
+      }
       acc[2 * D + 1] += k;
     }
     acc[2 * D] += loss;

@@ -107,3 +107,15 @@ def test_event_without_advantage_beyond_the_ratios_range(gpu_ctx, zero):
     t["x"][0, 0, 0] = float("nan")
     o = gpu_ctx.policy_loss(**t, clip_low=1.0, clip_high=50.0)
     assert torch.isnan(o["loss"]).item() and torch.isnan(o["dtheta"][0, :2]).all().item()
+
+
+def test_no_weight_on_a_divergence_beyond_fp32(gpu_ctx):
+    """kl_coef = 0 leaves the loss and its gradient to the ratios, whatever the divergence that is reported."""
+    rng = np.random.default_rng(22)
+    near, far, x = _far_event(rng, 50)
+    c = dict(theta=far, theta_old=far, theta_ref=near, x=x, adv=rng.standard_normal((1, 50)).astype(np.float32))
+    want = oracle.policy_loss(**c, kl_coef=0.0)
+    got = gpu_ctx.policy_loss(**{k: _t(v) for k, v in c.items()}, kl_coef=0.0)
+    assert abs(got["loss"].item() - want["loss"]) <= TOL * max(1.0, abs(want["loss"]))
+    assert np.all(np.abs(to_np(got["dtheta"]) - want["dtheta"]) <= TOL * want["abs_dtheta"])
+    assert got["kl"].item() == np.inf and want["kl"] > 1e40
