@@ -82,9 +82,9 @@ sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJo
   }
   js->steps = ns.steps ? ns.steps : 5;
   js->eps = ns.eps;
-  // The kernels hold 2^12 X, X X^T and the polynomial of it in fp16 terms, up to 15.9:
-  // no entry exceeds the largest singular value, which starts below 1 and is bounded step
-  // by step.
+  // The kernels hold 2^12 X, X X^T and the polynomial of it in fp16 terms, up to 15.9, and
+  // 2^10 X X^T X, up to 63.9: no entry exceeds the largest singular value, which for X starts
+  // below 1 and is bounded step by step (its cube by 59.4).
   const double a = js->coef[0], b = js->coef[1], k = js->coef[2];
   double most = 1.0;
   for (int i = 0; i < js->steps; ++i) {

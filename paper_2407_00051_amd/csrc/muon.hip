@@ -14,7 +14,8 @@
 // accumulator, smallest first, therefore replace an fp32 product at 16/3 of the rate of
 // the fp32 matrix instructions.  fp16 ends at 65,504, so entries must stay below 15.9:
 // they do because the singular values do (the entry points bound them from the
-// coefficients).
+// coefficients).  A X, which the small matrices' kernel forms, has their cubes, up to
+// 59.4, and is held as 2^10 times it.
 #include <limits.h>
 
 #include "kernels.hpp"
@@ -26,6 +27,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kT = 2;                          // terms
 constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
+constexpr float kScaleY = 0.25f;               // of A X, over that of the others
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -769,12 +771,12 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)                     // 2^12 X from its terms: exact
         x[b][r] = fmaf(jobs.b * kInvScale, y[r], jobs.a * fmaf((float)xt[b].v[r / 8][0][r % 8], one, (float)xt[b].v[r / 8][1][r % 8]));
-      split(y, kInvScale, xt[b]);
+      split(y, kInvScale * kScaleY, xt[b]);
       put(ldsY, b, xt[b]);
     });
     lds_barrier();                                     // Y is there, X has been read
     times(ldsY, A, [&](int b, const f32x16& y) __attribute__((always_inline)) {
-      x[b] += (jobs.c * kInvScale) * y;
+      x[b] += (jobs.c * (kInvScale / kScaleY)) * y;
       split(x[b], one, xt[b]);
       put(ldsX, b, xt[b]);
     });
