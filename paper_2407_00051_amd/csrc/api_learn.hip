@@ -56,14 +56,12 @@ double largest_value(double a, double b, double c, double most) {
   const auto value = [&](double s) { return fabs(s * (a + s * s * (b + c * s * s))); };
   double v = value(most), q[2];
   int n = 0;
-  if (c != 0.0) {
-    const double disc = 9.0 * b * b - 20.0 * a * c;
-    if (disc >= 0.0) {
-      q[n++] = (-3.0 * b + sqrt(disc)) / (10.0 * c);
-      q[n++] = (-3.0 * b - sqrt(disc)) / (10.0 * c);
-    }
-  } else if (b != 0.0) {
-    q[n++] = -a / (3.0 * b);
+  const double disc = 9.0 * b * b - 20.0 * a * c;
+  if (disc >= 0.0) {
+    // -(3 b + its square root with b's sign): no digits cancel where c is small
+    const double t = -(3.0 * b + copysign(sqrt(disc), b));
+    if (t != 0.0) q[n++] = 2.0 * a / t;
+    if (c != 0.0) q[n++] = t / (10.0 * c);
   }
   for (int i = 0; i < n; ++i)
     if (q[i] > 0.0 && q[i] < most * most) v = fmax(v, value(sqrt(q[i])));
