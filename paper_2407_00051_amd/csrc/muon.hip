@@ -141,15 +141,29 @@ __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double
   if (threadIdx.x == 0) part[blockIdx.x] = w[0] + w[1] + w[2] + w[3];
 }
 
-// 1 / (||U||_F + eps) from the chunks' sums, in every thread.
-__device__ __forceinline__ float inverse_norm(const double* __restrict__ part, int chunks, double eps) {
+// X = U / (||U||_F + eps) as u 2^exp mul, mul in (1, 2]: the inverse itself may lie outside fp32's
+// range.  A zero matrix stays zero; an infinity or NaN makes all of it NaN.
+struct Unit {
+  float mul;
+  int exp;
+  __device__ __forceinline__ float operator()(float u) const { return __builtin_ldexpf(u, exp) * mul; }
+};
+__device__ __forceinline__ Unit unit_of(double norm, double eps) {
+  if (norm == 0.0) return {0.0f, 0};
+  if (!(norm < INFINITY)) return {NAN, 0};
+  int e;
+  const double m = frexp(norm + eps, &e);
+  return {(float)(1.0 / m), -e};
+}
+// The same from the chunks' sums, in every thread.
+__device__ __forceinline__ Unit unit_of(const double* __restrict__ part, int chunks, double eps) {
   __shared__ double w[kThreads / 64];
   double s = 0.0;
   for (int k = threadIdx.x; k < chunks; k += kThreads) s += part[k];
   s = wave_sum_d(s);
   if ((threadIdx.x & 63) == 0) w[threadIdx.x >> 6] = s;
   __syncthreads();
-  return (float)(1.0 / (sqrt(w[0] + w[1] + w[2] + w[3]) + eps));
+  return unit_of(sqrt(w[0] + w[1] + w[2] + w[3]), eps);
 }
 
 // Layout of an operand of R rows and K columns (K runs along them) in the workspace:
@@ -184,13 +198,13 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
     g.read(q, src, e);
     if constexpr (kMom) m[q] = mom[e];
   }
-  const float inv = inverse_norm(part + (int64_t)z * chunks, chunks, j.eps);
+  const Unit unit = unit_of(part + (int64_t)z * chunks, chunks, j.eps);
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const int r = 4 * q + (threadIdx.x >> 6);
     float u = g[q];
     if constexpr (kMom) u = j.nesterov ? fmaf(j.momentum, m[q], u) : m[q];
-    u = r0 + r < j.rows && col < j.cols ? u * inv : 0.0f;
+    u = r0 + r < j.rows && col < j.cols ? unit(u) : 0.0f;
     if (flip) tile[c][r] = u;
     else tile[r][c] = u;
   }
@@ -604,7 +618,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
   double total = 0.0;
 #pragma unroll
   for (int w = 0; w < W; ++w) total += sums[w];
-  const float inv = (float)(1.0 / (sqrt(total) + jobs.eps));
+  const Unit unit = unit_of(sqrt(total), jobs.eps);
 
   float one = 1.0f;                                    // not a constant to the compiler: a multiplication by it lets
   asm("" : "+s"(one));                                 // fp16 operands go straight into an fp32 fma
@@ -648,7 +662,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-        x[r] = i < n && j < L ? flat[i * pi + j * pj] * inv : 0.0f;
+        x[r] = i < n && j < L ? unit(flat[i * pi + j * pj]) : 0.0f;
       }
       split(x, kScale, xt[b]);
     }

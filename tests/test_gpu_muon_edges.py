@@ -7,6 +7,7 @@ import pytest
 
 import oracle
 from tests.parity import to_np
+from tests.test_gpu_muon import _assert_close
 
 pytestmark = pytest.mark.gpu
 
@@ -34,3 +35,15 @@ def test_coefficients_up_to_the_bound(gpu_ctx, shape, steps, coef):
     # slopes are at most coef[0] + 3 |b| s^2 + 5 |c| s^4 below 8 for the s of these steps (at most 2.7)
     tol = sum(8.0 ** k for k in range(steps + 1)) * UNIT * 3.9
     assert np.all(_norm(got - ref) <= tol), _norm(got - ref) / tol
+
+
+@pytest.mark.parametrize("shape", [(20, 30), (128, 128), (200, 150)])
+def test_norms_and_eps_at_the_ends(gpu_ctx, shape):
+    """Zero matrices, subnormal ones and ones near the largest number, at an eps below fp32's range."""
+    print(f"case norms {shape}", flush=True)
+    rng = np.random.default_rng(7)
+    g = rng.standard_normal(shape)
+    x = np.stack([g, 0.0 * g, np.sign(g) * 3e38, 1e-42 * g, 1e-39 * g]).astype(np.float32)
+    got = to_np(gpu_ctx.orthogonalise(torch.tensor(x, device="cuda:0"), eps=1e-60))
+    assert np.all(got[1] == 0.0)
+    _assert_close(got, oracle.orthogonalise(x.astype(np.float64), eps=1e-60), False)
