@@ -421,9 +421,11 @@ sagips_status sagips_preference_loss(sagips_ctx* ctx, const sagips_preference* P
  * With the default coefficients every singular value of U that is not far
  * below the largest ends between 0.68 and 1.14; singular vectors stay.
  * A zero matrix stays zero; an infinity or NaN makes the whole matrix NaN.
- * X, A and the polynomial are held as two fp16 terms (24 bits; X is scaled,
- * so the range of U does not matter) and multiplied with fp32 accumulation,
- * at or below the error of fp32 products.  `coef` all zero means
+ * X, A and the polynomial are held as two fp16 terms (24 bits) and multiplied
+ * with fp32 accumulation, at or below the error of fp32 products; X is held up
+ * by a power of two of its own while it is small, so neither the range of U
+ * nor its size beside eps matters (an X that `coef` shrinks loses a bit for
+ * every halving).  `coef` all zero means
  * (3.4445, -4.7750, 2.0315), `steps` 0 means 5.  0 <= steps <= 16, eps > 0;
  * coefficients that let singular values grow beyond 3.9 from at most 1, or
  * |b| s^2 + |c| s^4 beyond 15.9 for the largest of them s, are

@@ -68,6 +68,14 @@ double largest_value(double a, double b, double c, double most) {
   return v;
 }
 
+// max |a + b q + c q^2| over 0 <= q <= most^2: at an end, or where b + 2 c q is zero.
+double largest_growth(double a, double b, double c, double most) {
+  const auto value = [&](double q) { return fabs(a + q * (b + c * q)); };
+  const double q = c != 0.0 ? -b / (2.0 * c) : 0.0;
+  const double v = fmax(value(0.0), value(most * most));
+  return q > 0.0 && q < most * most ? fmax(v, value(q)) : v;
+}
+
 sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJobs* js) {
   if (ns.steps < 0 || ns.steps > 16) return fail(c, SAGIPS_E_INVAL, "steps = %d outside [0, 16]", ns.steps);
   if (!(ns.eps > 0.0) || !isfinite(ns.eps)) return fail(c, SAGIPS_E_INVAL, "eps must be finite and > 0");
@@ -84,14 +92,16 @@ sagips_status fill_steps(sagips_ctx* c, const sagips_newton_schulz& ns, MatrixJo
   // 2^10 X X^T X, up to 63.9: no entry exceeds the largest singular value, which for X starts
   // below 1 and is bounded step by step (its cube by 59.4).
   const double a = js->coef[0], b = js->coef[1], k = js->coef[2];
-  double most = 1.0;
+  double most = 1.0, growth = 1.0;
   for (int i = 0; i < js->steps; ++i) {
     const double poly = fabs(b) * most * most + fabs(k) * most * most * most * most;
     if (!(most <= 3.9) || !(poly <= 15.9))
       return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 3.9 within %d steps", a,
                   b, k, i + 1);
+    growth = fmax(growth, largest_growth(a, b, k, most));
     most = largest_value(a, b, k, most);
   }
+  js->grow = (int)ceil(log2(growth));
   if (!(most <= 3.9))
     return fail(c, SAGIPS_E_UNSUPPORTED, "coefficients (%g, %g, %g) let singular values grow beyond 3.9", a, b, k);
   return SAGIPS_OK;

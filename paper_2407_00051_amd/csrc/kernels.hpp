@@ -124,6 +124,7 @@ struct MatrixJobs {
   float momentum, decay, coef[3];
   double lr, eps;
   int steps;
+  int grow;          // a step multiplies no singular value by more than 2^grow
 };
 size_t muon_workspace(const MatrixJobs& js);
 hipError_t launch_muon(const MatrixJobs& js, void* ws, int n_cu, hipStream_t st, Timer* tm);

@@ -141,20 +141,26 @@ __global__ __launch_bounds__(kThreads) void k_ns_norm(Jobs j, int chunks, double
   if (threadIdx.x == 0) part[blockIdx.x] = w[0] + w[1] + w[2] + w[3];
 }
 
-// X = U / (||U||_F + eps) as u 2^exp mul, mul in (1, 2]: the inverse itself may lie outside fp32's
-// range.  A zero matrix stays zero; an infinity or NaN makes all of it NaN.
+// X = U / (||U||_F + eps), as 2^up X = u 2^exp mul, mul in (1, 2]: the inverse itself may lie outside
+// fp32's range.  A zero matrix stays zero; an infinity or NaN makes all of it NaN.
+// Where ||U|| is far below eps, X is small and fp16 would end inside its terms.  They are held of
+// 2^up X, whose norm starts in [1/2, 1); a step takes X up to at most 2^grow times its size, and so
+// many bits from up, until none is left and the bounds of the singular values hold as they are.
 struct Unit {
   float mul;
-  int exp;
+  int exp, up;
   __device__ __forceinline__ float operator()(float u) const { return __builtin_ldexpf(u, exp) * mul; }
 };
 __device__ __forceinline__ Unit unit_of(double norm, double eps) {
-  if (norm == 0.0) return {0.0f, 0};
-  if (!(norm < INFINITY)) return {NAN, 0};
-  int e;
+  if (norm == 0.0) return {0.0f, 0, 0};
+  if (!(norm < INFINITY)) return {NAN, 0, 0};
+  int e, below;
   const double m = frexp(norm + eps, &e);
-  return {(float)(1.0 / m), -e};
+  (void)frexp(norm / (norm + eps), &below);
+  const int up = max(0, -below);
+  return {(float)(1.0 / m), up - e, up};
 }
+__device__ __forceinline__ int up_after(int up, int bits) { return max(0, up - bits); }
 // The same from the chunks' sums, in every thread.
 __device__ __forceinline__ Unit unit_of(const double* __restrict__ part, int chunks, double eps) {
   __shared__ double w[kThreads / 64];
@@ -180,7 +186,8 @@ __device__ __forceinline__ int64_t frag_at(int rb, int ks, int K) { return ((int
 // 13-15 us at 2,048 x 2,048 fp32, 50 MB at 3.5 TB/s.
 template <bool kBf16, bool kMom>
 __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const double* __restrict__ part,
-                                                       u16* __restrict__ XR, u16* __restrict__ XC, int np, int lp) {
+                                                       u16* __restrict__ XR, u16* __restrict__ XC, int* __restrict__ up,
+                                                       int np, int lp) {
   __shared__ float tile[64][65];
   const int z = blockIdx.z, t = tensor_of(j.first, z), i0 = blockIdx.y * 64, l0 = blockIdx.x * 64;
   const bool flip = j.rows > j.cols;
@@ -199,6 +206,7 @@ __global__ __launch_bounds__(kThreads) void k_ns_split(Jobs j, int chunks, const
     if constexpr (kMom) m[q] = mom[e];
   }
   const Unit unit = unit_of(part + (int64_t)z * chunks, chunks, j.eps);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) up[z] = unit.up;
 #pragma unroll
   for (int q = 0; q < 16; ++q) {
     const int r = 4 * q + (threadIdx.x >> 6);
@@ -248,6 +256,8 @@ struct GemmArgs {
   const u16* old;    // kPoly: P;  kApply, kStore: X with K along its rows
   u16* out;          // the result with K along its rows
   u16* outT;         // kApply: the same with K down its columns
+  const int* up;     // [matrices] of X at the first step
+  int spent, grow;   // bits of it that the steps so far took, that a step takes
   int np, kp, width; // rows, K, columns
   int tiles_i, tiles_j, per_mat, tiles, per_xcd;   // per_mat: tiles of a matrix; tiles: of all
 };
@@ -390,15 +400,19 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
   // Each kept block: lane lr + 32 h has row i, columns 8 g + 4 h + 0..3.
   float* const turn = reinterpret_cast<float*>(sums) + wave * (32 * 33);
   const int t = kMode == kStore ? tensor_of(jobs.first, z) : 0;
+  const int up = kMode == kGram ? 0 : up_after(g.up[z], g.spent), up_next = up_after(up, g.grow);
   const bool flip = jobs.rows > jobs.cols;
 #pragma unroll
   for (int b = 0; b < OB; ++b) {
     const int at = wave * OB + b, bi = ti * TB + at % TB, bj = tj * TB + at / TB;   // in blocks of 32
     if (at >= TB * TB || bi >= ni || bj >= nj) continue;
     f32x16 v = o[b];
-    // kGram: 2^24 times the result; otherwise 2^12 times
+    // kGram: 2^24 times the result; otherwise 2^12 times.  Operands are held up by powers of two:
+    // X X^T by 2 up, its square by 4; the polynomial as it is.
     if constexpr (kMode != kGram) {
-      const float keep = kMode == kPoly ? jobs.b : jobs.a, mul = (kMode == kPoly ? jobs.c : 1.0f) * kInvScale;
+      const int to = kMode == kApply ? up_next - up : 0;
+      const float keep = kMode == kPoly ? __builtin_ldexpf(jobs.b, -2 * up) : __builtin_ldexpf(jobs.a, to);
+      const float mul = kMode == kPoly ? __builtin_ldexpf(jobs.c * kInvScale, -4 * up) : __builtin_ldexpf(kInvScale, to);
       const u16* from = g.old + z * op + frag_at(bi, 2 * bj, g.width) + lane * 8;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -437,7 +451,7 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
       for (int r = 0; r < 16; ++r) {
         if (row_of(r) >= jobs.rows || col >= jobs.cols) continue;
         const int64_t to = base + (int64_t)row_of(r) * jobs.cols + col;
-        const float x = v[r] * kInvScale;
+        const float x = __builtin_ldexpf(v[r] * kInvScale, -up);
         if (jobs.m[t]) static_cast<float*>(jobs.out[t])[to] = fmaf(-jobs.rate, x, jobs.decay * old[r]);
         else if (jobs.out_bf16) static_cast<u16*>(jobs.out[t])[to] = to_bf16(x);
         else static_cast<float*>(jobs.out[t])[to] = x;
@@ -476,7 +490,7 @@ struct SmallJob {
 struct SmallJobs {
   SmallJob job[SAGIPS_MAX_TENSORS];
   int first[SAGIPS_MAX_TENSORS + 1];
-  int src_bf16, out_bf16, nesterov, steps;
+  int src_bf16, out_bf16, nesterov, steps, grow;
   float momentum, decay, a, b, c;
   double eps;
 };
@@ -701,8 +715,14 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
     for (int y = 0; y < JB; ++y) done(y, c[y]);
   };
 
-  f32x16 x[JB];                                        // 2^12 times X
+  f32x16 x[JB];                                        // 2^(12 + up) times X
+  int up = unit.up;
   for (int step = 0; step < jobs.steps; ++step) {
+    // a X, b (X X^T) X and c (X X^T)^2 X from what is held 1, 3 and 5 up, to where the next step has it
+    const int to = up_after(up, jobs.grow) - up;
+    const float ka = __builtin_ldexpf(jobs.a, to), kb = __builtin_ldexpf(jobs.b * kInvScale, to - 2 * up);
+    const float kc = __builtin_ldexpf(jobs.c * (kInvScale / kScaleY), to - 4 * up);
+    up += to;
     lds_barrier();                                     // X is there, Y has been read
     Terms A[NI];
     {
@@ -784,13 +804,13 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
     times(ldsX, A, [&](int b, const f32x16& y) __attribute__((always_inline)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)                     // 2^12 X from its terms: exact
-        x[b][r] = fmaf(jobs.b * kInvScale, y[r], jobs.a * fmaf((float)xt[b].v[r / 8][0][r % 8], one, (float)xt[b].v[r / 8][1][r % 8]));
+        x[b][r] = fmaf(kb, y[r], ka * fmaf((float)xt[b].v[r / 8][0][r % 8], one, (float)xt[b].v[r / 8][1][r % 8]));
       split(y, kInvScale * kScaleY, xt[b]);
       put(ldsY, b, xt[b]);
     });
     lds_barrier();                                     // Y is there, X has been read
     times(ldsY, A, [&](int b, const f32x16& y) __attribute__((always_inline)) {
-      x[b] += (jobs.c * (kInvScale / kScaleY)) * y;
+      x[b] += kc * y;
       split(x[b], one, xt[b]);
       put(ldsX, b, xt[b]);
     });
@@ -804,7 +824,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      if (i < n && j < L) flat[i * pi + j * pj] = x[b][r] * kInvScale;
+      if (i < n && j < L) flat[i * pi + j * pj] = __builtin_ldexpf(x[b][r] * kInvScale, -up);
     }
   if (job.m) small_store<kN, false, true>(jobs, job, base, flat, pitch);
   else if (jobs.out_bf16) small_store<kN, true, false>(jobs, job, base, flat, pitch);
@@ -832,7 +852,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Plan {
   int n, L, np, lp, chunks, mats;
-  size_t r0, r1, c0, c1, A, B, bytes;   // offsets; the partial sums come first
+  size_t up, r0, r1, c0, c1, A, B, bytes;   // offsets; the partial sums come first
 };
 Plan plan_of(int rows, int cols, int mats) {
   Plan p;
@@ -844,7 +864,8 @@ Plan plan_of(int rows, int cols, int mats) {
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
   const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
-  p.r0 = part;
+  p.up = part;
+  p.r0 = p.up + align256((size_t)mats * sizeof(int));
   p.r1 = p.r0 + x;
   p.c0 = p.r1 + x;
   p.c1 = p.c0 + x;
@@ -891,9 +912,10 @@ void gemm(const GemmArgs& g, const Jobs& j, int mats, int side, hipStream_t st) 
   else gemm_of<kMode, 4>(g, j, mats, st);
 }
 
-hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws, hipStream_t st, Timer* tm) {
+hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int grow, int n_cu, char* ws, hipStream_t st, Timer* tm) {
   const auto at = [&](size_t offset) { return reinterpret_cast<u16*>(ws + offset); };
   double* part = reinterpret_cast<double*>(ws);
+  int* up = reinterpret_cast<int*>(ws + p.up);
   u16 *r0 = at(p.r0), *r1 = at(p.r1), *c0 = at(p.c0), *c1 = at(p.c1), *A = at(p.A), *B = at(p.B);
   if (tm) tm->begin("ns_norm");
   const auto norm = j.m[0] ? (j.src_bf16 ? k_ns_norm<true, true> : k_ns_norm<false, true>)
@@ -904,19 +926,19 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int n_cu, char* ws,
   if (tm) tm->end();
   if (tm) tm->begin("ns_split");
   hipLaunchKernelGGL(split, dim3((p.lp + 63) / 64, (p.np + 63) / 64, p.mats), dim3(kThreads), 0, st, j, p.chunks, part, r0, c0,
-                     p.np, p.lp);
+                     up, p.np, p.lp);
   if (tm) tm->end();
   const int gram = tile_side(true, p.np, p.np, p.lp, p.mats, n_cu), poly = tile_side(true, p.np, p.np, p.np, p.mats, n_cu);
   const int apply = tile_side(false, p.np, p.lp, p.np, p.mats, n_cu);
   for (int s = 0; s < steps; ++s) {
     if (tm) tm->begin("ns_gram");
-    gemm<kGram>(GemmArgs{r0, r0, nullptr, A, nullptr, p.np, p.lp, p.np}, j, p.mats, gram, st);
+    gemm<kGram>(GemmArgs{r0, r0, nullptr, A, nullptr, up, s * grow, grow, p.np, p.lp, p.np}, j, p.mats, gram, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_poly");
-    gemm<kPoly>(GemmArgs{A, A, A, B, nullptr, p.np, p.np, p.np}, j, p.mats, poly, st);
+    gemm<kPoly>(GemmArgs{A, A, A, B, nullptr, up, s * grow, grow, p.np, p.np, p.np}, j, p.mats, poly, st);
     if (tm) tm->end();
     if (tm) tm->begin("ns_apply");
-    const GemmArgs g{B, c0, r0, r1, c1, p.np, p.np, p.lp};
+    const GemmArgs g{B, c0, r0, r1, c1, up, s * grow, grow, p.np, p.np, p.lp};
     if (s + 1 < steps) gemm<kApply>(g, j, p.mats, apply, st);
     else gemm<kStore>(g, j, p.mats, apply, st);
     if (tm) tm->end();
@@ -984,6 +1006,7 @@ static hipError_t launch_small(const MatrixJobs& js, int which, hipStream_t st, 
   j.out_bf16 = js.out_bf16;
   j.nesterov = js.nesterov;
   j.steps = js.steps;
+  j.grow = js.grow;
   j.momentum = js.momentum;
   j.decay = js.decay;
   j.a = js.coef[0];
@@ -1037,7 +1060,7 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, int n_cu, hipStream_t st,
     j.c = js.coef[2];
     j.eps = js.eps;
     const Plan p = plan_of(a.rows, a.cols, total);
-    return steps_of(p, j, js.steps, n_cu, static_cast<char*>(ws), st, tm);
+    return steps_of(p, j, js.steps, js.grow, n_cu, static_cast<char*>(ws), st, tm);
   });
 }
 

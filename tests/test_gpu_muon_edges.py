@@ -47,3 +47,38 @@ def test_norms_and_eps_at_the_ends(gpu_ctx, shape):
     got = to_np(gpu_ctx.orthogonalise(torch.tensor(x, device="cuda:0"), eps=1e-60))
     assert np.all(got[1] == 0.0)
     _assert_close(got, oracle.orthogonalise(x.astype(np.float64), eps=1e-60), False)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("shape", [(20, 30), (128, 128), (70, 60), (300, 200)])
+def test_norms_far_below_eps(gpu_ctx, shape, bf16):
+    """X starts at ||U|| / eps instead of 1, and is held no worse for it: of the result the same part
+    is rounding as at ordinary norms."""
+    print(f"case norms below eps {shape} bf16={bf16}", flush=True)
+    rng = np.random.default_rng(8)
+    ratio = 10.0 ** -np.arange(0, 13)
+    g = rng.standard_normal((len(ratio),) + shape)
+    x = torch.tensor(g * (ratio * 1e-7 / _norm(g))[:, None, None], dtype=torch.bfloat16 if bf16 else torch.float32, device="cuda:0")
+    got = to_np(gpu_ctx.orthogonalise(x, eps=1e-7).float()).astype(np.float64)
+    ref = oracle.orthogonalise(to_np(x.double()), eps=1e-7)
+    tol = 485 * UNIT * ratio + 5 * UNIT * _norm(ref) + (2.0 ** -9 * _norm(ref) if bf16 else 0.0)
+    err = _norm(got - ref)
+    print(f"  worst of error / tolerance {np.max(err / tol):.3f}", flush=True)
+    assert np.all(err <= tol), err / tol
+
+
+def test_momenta_far_below_eps(gpu_ctx):
+    """The step on them: each matrix of a stack at its own scale."""
+    rng = np.random.default_rng(9)
+    for r, c in ((128, 128), (300, 200)):
+        p, m = rng.standard_normal((3, r, c)).astype(np.float32) * 1e-4, np.zeros((3, r, c), np.float32)
+        g = rng.standard_normal((3, r, c))
+        g = (g * (np.array([1.0, 1e-9, 1e-13]) / _norm(g))[:, None, None]).astype(np.float32)
+        tp, tm = torch.tensor(p, device="cuda:0"), torch.tensor(m, device="cuda:0")
+        gpu_ctx.muon_step([tp], [torch.tensor(g, device="cuda:0")], [tm], 1.0)
+        want, _ = oracle.muon_step(p, g, m, 1.0)
+        moved = want - p
+        first = np.array([1.0, 1.95e-2, 1.95e-6])          # ||U|| / eps, U = (1 + 0.95) g
+        tol = (max(1.0, r / c) ** 0.5 * 485 * first + 5 * _norm(moved)) * UNIT + 2.0 ** -23 * (_norm(p) + _norm(moved))
+        err = _norm(to_np(tp) - want)
+        assert np.all(err <= tol), err / tol
