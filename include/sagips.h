@@ -26,6 +26,11 @@
  *   - Several contexts may share a device; each owns its own workspace.
  *   - A context is not thread-safe; calls on one context must not overlap
  *     from several host threads.
+ *   - A call captured into a HIP graph keeps the workspace and the counters
+ *     of its context: replays count as that context's calls, must not overlap
+ *     others of them on the device, and end with the context or with the
+ *     next call that needs a larger workspace.  A workspace that a captured
+ *     call needs is made before, by the same call outside the capture.
  *
  * Event sampling (shared by all calls that take a sagips_source)
  *   Event k of parameter row i has id = counter_base + i*E + k.  Its random

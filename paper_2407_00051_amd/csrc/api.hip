@@ -22,6 +22,13 @@ using namespace sagips;
 constexpr size_t kScratchBytes = (size_t)64 << 20;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes + kNoallocReserve];
 
+// Sets of counters that contexts hold (kernels.hpp): 0 from the start, so that a context needs
+// neither an allocation nor a launch to have one, also where its first call is being captured into
+// a graph.  A set that an earlier context used is cleared on the new one's stream.
+constexpr int kTicketSets = 64;   // contexts beyond them do without
+static __device__ __align__(256) uint32_t tickets[kTicketSets][kTicketWords];
+static __global__ void k_clear(uint32_t* ticket) { ticket[threadIdx.x] = 0u; }
+
 namespace {
 
 // Device address of `scratch` per device (taken once, with that device current).
@@ -40,6 +47,35 @@ hipError_t scratch_address(int dev, char** ptr) {
   }
   *ptr = g_scratch_ptr[dev];
   return g_scratch_err[dev];
+}
+
+std::mutex g_tickets_mu;
+bool g_ticket_taken[kTicketSets] = {}, g_ticket_used[kTicketSets] = {};
+
+void take_ticket(sagips_ctx* c) {   // with c's device current
+  static_assert(kTicketWords <= 1024, "one workgroup clears them");
+  std::lock_guard<std::mutex> lock(g_tickets_mu);
+  void* all = nullptr;
+  if (hipGetSymbolAddress(&all, HIP_SYMBOL(tickets)) != hipSuccess || !all) {
+    (void)hipGetLastError();
+    return;
+  }
+  for (int i = 0; i < kTicketSets; ++i) {
+    if (g_ticket_taken[i]) continue;
+    uint32_t* p = static_cast<uint32_t*>(all) + (size_t)i * kTicketWords;
+    if (g_ticket_used[i]) {
+      hipLaunchKernelGGL(k_clear, dim3(1), dim3(kTicketWords), 0, c->stream, p);
+      if (hipGetLastError() != hipSuccess) return;
+    }
+    g_ticket_taken[i] = g_ticket_used[i] = true;
+    c->ticket = p;
+    c->ticket_set = i;
+    return;
+  }
+}
+void give_ticket(sagips_ctx* c) {
+  std::lock_guard<std::mutex> lock(g_tickets_mu);
+  if (c->ticket_set >= 0) g_ticket_taken[c->ticket_set] = false;
 }
 
 // Where a call's workspace comes from: the context's (grown on demand with
@@ -205,6 +241,10 @@ sagips_status sagips_create(sagips_ctx** out, int hip_device, void* hip_stream) 
   c->stream = static_cast<hipStream_t>(hip_stream);
   c->n_cu = prop.multiProcessorCount;
   c->timer.stream = c->stream;
+  {
+    DeviceGuard g(hip_device);
+    take_ticket(c);
+  }
   *out = c;
   return SAGIPS_OK;
 }
@@ -215,7 +255,7 @@ sagips_status sagips_destroy(sagips_ctx* c) {
     DeviceGuard g(c->device);
     (void)hipStreamSynchronize(c->stream);
     if (c->ws) (void)hipFree(c->ws);
-    if (c->ticket) (void)hipFree(c->ticket);
+    give_ticket(c);
   }
   delete c;
   return SAGIPS_OK;

@@ -168,7 +168,6 @@ sagips_status sagips_policy_loss(sagips_ctx* c, const sagips_policy* P, const fl
       return fail(c, SAGIPS_E_INVAL, "outputs must be 4-byte aligned");
     DeviceGuard g(c->device);
     s = ensure_ws(c, policy_workspace(*P));
-    if (s == SAGIPS_OK) s = ensure_ticket(c);
     if (s != SAGIPS_OK) return s;
     hipError_t e = launch_policy(*P, x, adv, mask, loss, kl, clip_frac, dtheta, c->ws, c->ticket, c->stream,
                                  timer_of(c));
@@ -204,7 +203,6 @@ sagips_status sagips_preference_loss(sagips_ctx* c, const sagips_preference* P, 
       return fail(c, SAGIPS_E_INVAL, "outputs must be 4-byte aligned");
     DeviceGuard g(c->device);
     s = ensure_ws(c, preference_workspace(*P));
-    if (s == SAGIPS_OK) s = ensure_ticket(c);
     if (s != SAGIPS_OK) return s;
     hipError_t e = launch_preference(*P, chosen, n_chosen, rejected, n_rejected, loss, margin, dtheta, c->ws, c->ticket,
                                      c->stream, timer_of(c));

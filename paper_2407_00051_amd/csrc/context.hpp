@@ -74,7 +74,8 @@ struct sagips_ctx {
   void* ws = nullptr;
   size_t ws_cap = 0;
   size_t ws_refused = SIZE_MAX; // bf16: the workspace that the device refused last
-  uint32_t* ticket = nullptr;   // counters, 0 between calls (made with the first call that needs it)
+  uint32_t* ticket = nullptr;   // the counters of ticket_set, or NULL
+  int ticket_set = -1;
   std::string err = "no error";
   bool timing = false;
   int bf16_chunk_rows = 0;      // 0: the library's default
@@ -129,23 +130,6 @@ inline sagips_status ensure_ws(sagips_ctx* c, size_t bytes) {
     return fail(c, SAGIPS_E_NOMEM, "workspace allocation of %zu bytes failed", want);
   }
   c->ws_cap = want;
-  return SAGIPS_OK;
-}
-
-// The context's counters, cleared by a kernel on its stream when they are made.
-inline sagips_status ensure_ticket(sagips_ctx* c) {
-  if (c->ticket) return SAGIPS_OK;
-  void* p = nullptr;
-  if (hipMalloc(&p, kTicketWords * sizeof(uint32_t)) != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(c, SAGIPS_E_NOMEM, "allocation of the context's counters failed");
-  }
-  const hipError_t e = launch_clear(static_cast<uint32_t*>(p), c->stream);
-  if (e != hipSuccess) {
-    (void)hipFree(p);
-    return hip_fail(c, e, "clearing the context's counters");
-  }
-  c->ticket = static_cast<uint32_t*>(p);
   return SAGIPS_OK;
 }
 

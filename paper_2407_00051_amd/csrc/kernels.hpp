@@ -94,9 +94,11 @@ hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double b
                        hipStream_t st, Timer* tm);
 
 // policy.hip -----------------------------------------------------------------
-// `ticket`: one counter on the device, 0 before and after every launch that uses it.
-constexpr int kTicketWords = 1024;   // of a context's counters
-hipError_t launch_clear(uint32_t* p, hipStream_t st);
+// `ticket`: the context's counters on the device, one that joins kCounters others, a cache line
+// each, all 0 before and after every launch that uses them; NULL: no launch ends in its last
+// workgroup.
+constexpr int kCounters = 16, kApart = 32;
+constexpr int kTicketWords = (1 + kCounters) * kApart;
 size_t advantage_workspace(int64_t n_rows, int64_t E);
 hipError_t launch_advantage(const float* reward, const uint8_t* mask, int64_t n_rows, int64_t E, bool normalise, double eps,
                             float* adv, void* ws, hipStream_t st, Timer* tm);

@@ -370,7 +370,6 @@ __device__ __forceinline__ void put_record(float* p, float v) {
 // visible to it.  16 counters of the context, then one of those that filled theirs (one for all:
 // 2 us more at 256 workgroups); whoever fills a counter puts it back to 0.
 // Only which workgroup is last depends on the order, not what it computes.
-constexpr int kCounters = 16, kApart = 32;             // a cache line each
 __device__ __forceinline__ bool last_block(uint32_t* ticket) {
   __shared__ bool last;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // every wave's records have arrived before the workgroup is counted
@@ -946,13 +945,6 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
 }
 
 }  // namespace
-
-static __global__ void k_clear(uint32_t* p) { p[threadIdx.x] = 0u; }
-hipError_t launch_clear(uint32_t* p, hipStream_t st) {
-  static_assert((1 + kCounters) * kApart <= kTicketWords && kTicketWords <= 1024, "one workgroup clears them");
-  hipLaunchKernelGGL(k_clear, dim3(1), dim3(kTicketWords), 0, st, p);
-  return hipGetLastError();
-}
 
 size_t advantage_workspace(int64_t n_rows, int64_t E) {
   return E <= kAdvSlice ? 0 : (size_t)n_rows * ceil_div(E, kAdvSlice) * 3 * sizeof(double);

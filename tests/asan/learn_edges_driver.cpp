@@ -7,6 +7,8 @@
 #include "sagips.h"
 
 extern "C" {
+long stub_launches();
+long stub_mallocs();
 long stub_bad_launches();
 long stub_live_events();
 long stub_live_allocs();
@@ -57,6 +59,46 @@ void bounds_of_coefficients(sagips_ctx* c) {
     expect("some coefficients zero", sagips_orthogonalise(c, &ns, SAGIPS_F32, dev(1), 1, 8, 8, dev(2)), SAGIPS_OK, c);
 }
 
+// The launches and allocations of one small policy loss.
+struct Cost {
+  long launches, mallocs;
+};
+Cost policy_cost(sagips_ctx* c) {
+  sagips_policy p;
+  memset(&p, 0, sizeof(p));
+  p.theta = dev(1);
+  p.theta_old = dev(2);
+  p.n_theta = 4;
+  p.d = 2;
+  p.events_per_theta = 100;
+  const long n = stub_launches(), m = stub_mallocs();
+  expect("policy", sagips_policy_loss(c, &p, dev(4), dev(5), nullptr, dev(7), nullptr, nullptr, dev(8)), SAGIPS_OK, c);
+  return {stub_launches() - n, stub_mallocs() - m};
+}
+
+// A call that ends in its last workgroup launches and allocates nothing else, the context's first
+// no more than a later one: a first call that is being captured into a graph leaves no preparation
+// to the replay.  Contexts beyond those that have counters launch twice; one that ends gives its
+// counters on.
+void counters_of_contexts() {
+  const int n = 70, sets = 64;
+  static sagips_ctx* c[n];
+  for (int round = 0; round < 2; ++round) {
+    int once = 0;
+    for (int i = 0; i < n; ++i) {
+      expect("create", sagips_create(&c[i], 0, nullptr), SAGIPS_OK, nullptr);
+      const Cost first = policy_cost(c[i]), second = policy_cost(c[i]);
+      expect("workspace of the first call", first.mallocs, 1, c[i]);
+      expect("allocations of the second", second.mallocs, 0, c[i]);
+      expect("launches of the second", second.launches, first.launches, c[i]);
+      if (first.launches == 1) ++once;
+      else expect("launches without counters", first.launches, 2, c[i]);
+    }
+    expect("contexts with counters", once, sets, nullptr);
+    for (int i = 0; i < n; ++i) sagips_destroy(c[i]);
+  }
+}
+
 }  // namespace
 
 int main() {
@@ -64,6 +106,7 @@ int main() {
   expect("create", sagips_create(&c, 0, nullptr), SAGIPS_OK, nullptr);
   bounds_of_coefficients(c);
   sagips_destroy(c);
+  counters_of_contexts();
   expect("events left behind", stub_live_events(), 0, nullptr);
   expect("allocations left behind", stub_live_allocs(), 0, nullptr);
   expect("bad launches", stub_bad_launches(), 0, nullptr);

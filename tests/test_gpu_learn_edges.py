@@ -6,11 +6,12 @@ import pytest
 
 import oracle
 from tests.parity import to_np
-from tests.test_gpu_learn import ADV_TOL, TOL, _check_policy, _events, _t
+from tests.test_gpu_learn import ADV_TOL, KW, TOL, _check_policy, _events, _policy_case, _pref_case, _t
 
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
+import paper_2407_00051_amd as sg  # noqa: E402
 
 
 # ---- advantages
@@ -119,3 +120,51 @@ def test_no_weight_on_a_divergence_beyond_fp32(gpu_ctx):
     assert abs(got["loss"].item() - want["loss"]) <= TOL * max(1.0, abs(want["loss"]))
     assert np.all(np.abs(to_np(got["dtheta"]) - want["dtheta"]) <= TOL * want["abs_dtheta"])
     assert got["kl"].item() == np.inf and want["kl"] > 1e40
+
+
+# ---- contexts and graphs
+
+def _both(ctx, c, p):
+    a, b = ctx.policy_loss(**c, **KW, average="rows"), ctx.preference_loss(**p)
+    return [a["loss"], a["kl"], a["clip_frac"], a["dtheta"], b["loss"], b["margin"], b["dtheta"]]
+
+
+def test_first_losses_of_a_context_in_a_graph(gpu_ctx):
+    """A context whose first losses are captured: eager calls before the first replay, replays and eager
+    calls between them all give the same bits."""
+    print("case first call captured", flush=True)
+    rng = np.random.default_rng(30)
+    c = {k: _t(v) for k, v in _policy_case(rng, 50, 70, 3, "some", True).items()}
+    p = {k: _t(v) for k, v in _pref_case(rng, 50, 3, 9, 9, 3, True).items()}
+    want = _both(gpu_ctx, c, p)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        ctx = sg.Context(0, stream=st)
+        ctx.group_advantage(torch.zeros((1, 20000), device="cuda:0"))      # makes the workspace, outside the capture
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st, capture_error_mode="relaxed"):
+            out = _both(ctx, c, p)
+        for _ in range(3):
+            eager = _both(ctx, c, p)
+            graph.replay()
+            st.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, want))
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
+        ctx.close()
+
+
+def test_more_contexts_than_counters(gpu_ctx):
+    """Contexts beyond the 64 that have counters end in a second launch, with the same bits."""
+    print("case 70 contexts", flush=True)
+    rng = np.random.default_rng(31)
+    c = {k: _t(v) for k, v in _policy_case(rng, 50, 70, 3, "some", True).items()}
+    p = {k: _t(v) for k, v in _pref_case(rng, 50, 3, 9, 9, 3, True).items()}
+    want = _both(gpu_ctx, c, p)
+    for _ in range(2):
+        many = [sg.Context(0) for _ in range(70)]
+        for ctx in many:
+            assert all(torch.equal(a, b) for a, b in zip(_both(ctx, c, p), want))
+        for ctx in many:
+            ctx.close()
