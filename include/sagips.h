@@ -444,7 +444,8 @@ typedef struct {
 /*   x, out  [count][rows][cols] of `type` (SAGIPS_F32, or SAGIPS_BF16: bf16
  *           values); out may be x itself, otherwise must not overlap it.
  * count, rows, cols >= 1; rows, cols <= 16384; count <= 65535;
- * count * rows * cols < 2^31.                                               */
+ * count * rows * cols < 2^31.  The workspace is at most 2 GiB, or what one
+ * matrix needs (6 GiB at 16384 x 16384).                                    */
 sagips_status sagips_orthogonalise(sagips_ctx* ctx, const sagips_newton_schulz* ns, int32_t type, const void* x,
                                    int32_t count, int32_t rows, int32_t cols, void* out);
 

@@ -37,8 +37,8 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 typedef MatrixJob Job;
 
-// The matrices of one launch: tensors of one shape.  Matrix z lies in the tensor
-// t with first[t] <= z < first[t + 1].
+// The matrices of one launch: a part of the tensors of one shape.  Matrix z lies in the tensor
+// t with first[t] <= z < first[t + 1] (below 0 where a tensor began in an earlier part).
 struct Jobs {
   const void* src[SAGIPS_MAX_TENSORS];   // gradients, or the matrices to orthogonalise
   float* m[SAGIPS_MAX_TENSORS];          // momenta, or NULL
@@ -875,6 +875,16 @@ Plan plan_of(int rows, int cols, int mats) {
   return p;
 }
 
+// Matrices that go through their launches together: their workspace stays within kPart bytes,
+// which 341 of 512 x 512 or 21 of 2,048 x 2,048 fill, with tens of tiles a compute unit.  All at once,
+// 65,535 of 1 x 16,384 (4.3 GB, but padded to 32 rows) would take 550 GB.
+constexpr size_t kPart = (size_t)2 << 30;
+int per_part(int rows, int cols, int mats) {
+  const size_t one = plan_of(rows, cols, 1).bytes;   // with the offsets' padding: no less than a matrix's share
+  const size_t most = kPart / one;
+  return most < 1 ? 1 : most < (size_t)mats ? (int)most : mats;
+}
+
 // Blocks in a tile's side: 2, 3 or 4.  Compute units take tiles in rounds; a round takes
 // about fixed + per_k K microseconds (measured from K = 256 to 2,048; a larger side reads
 // less per product but has more to add up at the end, and only tiles of 2 run three to a
@@ -953,8 +963,8 @@ hipError_t steps_of(const Plan& p, const Jobs& j, int steps, int grow, int n_cu,
 
 }  // namespace
 
-// Tensors of one shape go through their launches together; the shapes one after
-// the other, in the same workspace.
+// Tensors of one shape go through their launches together, or in parts; the shapes and
+// parts one after the other, in the same workspace.
 template <class F>
 static hipError_t for_each_shape(const MatrixJobs& js, F&& f) {
   bool done[SAGIPS_MAX_TENSORS] = {};
@@ -982,7 +992,7 @@ size_t muon_workspace(const MatrixJobs& js) {
   size_t most = 0;
   (void)for_each_shape(js, [&](const int* list, int n) {
     const Job& a = js.job[list[0]];
-    const size_t b = plan_of(a.rows, a.cols, total_of(js, list, n)).bytes;
+    const size_t b = plan_of(a.rows, a.cols, per_part(a.rows, a.cols, total_of(js, list, n))).bytes;
     most = b > most ? b : most;
     return hipSuccess;
   });
@@ -1059,8 +1069,15 @@ hipError_t launch_muon(const MatrixJobs& js, void* ws, int n_cu, hipStream_t st,
     j.b = js.coef[1];
     j.c = js.coef[2];
     j.eps = js.eps;
-    const Plan p = plan_of(a.rows, a.cols, total);
-    return steps_of(p, j, js.steps, js.grow, n_cu, static_cast<char*>(ws), st, tm);
+    const int each = per_part(a.rows, a.cols, total);
+    for (int z = 0; z < total; z += each) {
+      Jobs part = j;
+      for (int k = 0; k < n; ++k) part.first[k] -= z;
+      const Plan p = plan_of(a.rows, a.cols, total - z < each ? total - z : each);
+      const hipError_t e = steps_of(p, part, js.steps, js.grow, n_cu, static_cast<char*>(ws), st, tm);
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   });
 }
 

@@ -4,6 +4,8 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <initializer_list>
+
 #include "sagips.h"
 
 extern "C" {
@@ -59,6 +61,36 @@ void bounds_of_coefficients(sagips_ctx* c) {
     expect("some coefficients zero", sagips_orthogonalise(c, &ns, SAGIPS_F32, dev(1), 1, 8, 8, dev(2)), SAGIPS_OK, c);
 }
 
+// Stacks of every accepted size have a workspace of at most 2 GiB, which is as much as the stub gives,
+// or of one matrix.
+void large_stacks(sagips_ctx* c) {
+  const sagips_newton_schulz ns = coefficients(5, 0.0, 0.0, 0.0);
+  const int shapes[][3] = {{65535, 1, 16384}, {65535, 16384, 1}, {65535, 2, 16383}, {65535, 1, 513}, {7000, 513, 513}, {1000, 1024, 2048},
+                           {4, 4096, 16384}, {2, 16384, 16384}};
+  for (const auto& s : shapes)
+    for (int type : {SAGIPS_F32, SAGIPS_BF16}) {
+      const bool large = s[1] == 16384 && s[2] == 16384;    // one matrix alone needs more
+      expect("orthogonalise a large stack", sagips_orthogonalise(c, &ns, type, dev(1), s[0], s[1], s[2], dev(8)),
+             large ? SAGIPS_E_NOMEM : SAGIPS_OK, c);
+    }
+  sagips_matrix_set set;
+  memset(&set, 0, sizeof(set));
+  set.n_tensors = 3;
+  for (int i = 0; i < 3; ++i) {
+    set.param[i] = dev(10 + 3 * i);
+    set.grad[i] = dev(11 + 3 * i);
+    set.m[i] = dev(12 + 3 * i);
+    set.count[i] = 20000;
+    set.rows[i] = i == 1 ? 16384 : 1;
+    set.cols[i] = i == 1 ? 1 : 16384;
+  }
+  sagips_muon mu;
+  memset(&mu, 0, sizeof(mu));
+  mu.lr = 0.02;
+  mu.ns = ns;
+  expect("step on large stacks", sagips_muon_step(c, &set, &mu), SAGIPS_OK, c);
+}
+
 // The launches and allocations of one small policy loss.
 struct Cost {
   long launches, mallocs;
@@ -105,6 +137,7 @@ int main() {
   sagips_ctx* c = nullptr;
   expect("create", sagips_create(&c, 0, nullptr), SAGIPS_OK, nullptr);
   bounds_of_coefficients(c);
+  large_stacks(c);
   sagips_destroy(c);
   counters_of_contexts();
   expect("events left behind", stub_live_events(), 0, nullptr);

@@ -82,3 +82,21 @@ def test_momenta_far_below_eps(gpu_ctx):
         tol = (max(1.0, r / c) ** 0.5 * 485 * first + 5 * _norm(moved)) * UNIT + 2.0 ** -23 * (_norm(p) + _norm(moved))
         err = _norm(to_np(tp) - want)
         assert np.all(err <= tol), err / tol
+
+
+def test_stacks_beyond_one_part(gpu_ctx):
+    """Matrices go in parts of 2 GiB of workspace (255 of 1 x 16,384); a part may begin inside a tensor."""
+    rng = np.random.default_rng(10)
+    shape = (1, 16384)
+    x = rng.standard_normal((300,) + shape).astype(np.float32)
+    t = torch.tensor(x, device="cuda:0")
+    got = gpu_ctx.orthogonalise(t)
+    _assert_close(to_np(got), oracle.orthogonalise(x.astype(np.float64)), False)
+    assert torch.equal(got[:150], gpu_ctx.orthogonalise(t[:150].clone())) and torch.equal(got[150:], gpu_ctx.orthogonalise(t[150:].clone()))
+    p = [torch.randn((150,) + shape, device="cuda:0") for _ in range(2)]
+    m = [torch.zeros_like(v) for v in p]
+    own = [[v.clone() for v in s] for s in (p, m)]
+    gpu_ctx.muon_step(p, [t[:150], t[150:]], m, 0.1)
+    for i in range(2):
+        gpu_ctx.muon_step([own[0][i]], [t[150 * i:150 * i + 150].clone()], [own[1][i]], 0.1)
+        assert torch.equal(p[i], own[0][i]) and torch.equal(m[i], own[1][i])
