@@ -776,17 +776,13 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
       } else {
 #pragma unroll
         for (int y = 0; y < NI; ++y) {
-          if constexpr (CW == 1) {
-            split(c[y], kInvScale, A[y]);
-          } else {
-            float* part = reinterpret_cast<float*>(ldsY) + (wave * NI + y) * 16 * 64 + lane;
+          float* part = reinterpret_cast<float*>(ldsY) + (wave * NI + y) * 16 * 64 + lane;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) part[r * 64] = c[y][r];
-          }
+          for (int r = 0; r < 16; ++r) part[r * 64] = c[y][r];
         }
       }
     }
-    if constexpr (CW > 1 && !kShare) {
+    if constexpr (!kShare) {
       lds_barrier();
 #pragma unroll
       for (int ib = 0; ib < NI; ++ib) {
@@ -831,15 +827,15 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
   else small_store<kN, false, false>(jobs, job, base, flat, pitch);
 }
 
-// The workgroup that holds a matrix, as 3 (log2 NP - 5) + log2 of the blocks of 32
-// columns that four waves would have; -1: none does.
-constexpr int kSmallClasses = 9;
+// The workgroup that holds a matrix: up to 64 rows, 3 (log2 NP - 5) + log2 JB; beyond, 6 (then L is
+// beyond 64 as well); -1: none does.
+constexpr int kSmallClasses = 7;
 int small_class(int rows, int cols) {
   const int n = rows < cols ? rows : cols, L = rows < cols ? cols : rows;
-  for (int p = 0; p < 3; ++p)
+  for (int p = 0; p < 2; ++p)
     for (int b = 0; b < 3 && n <= 32 << p; ++b)
       if (L <= ((32 << b) * 4 >> p)) return 3 * p + b;   // 32 JB columns a wave, 4 / 2^p waves
-  return -1;
+  return L <= 128 ? 6 : -1;
 }
 template <int NP, int JB, int W>
 void small_kernel(const SmallJobs& j, hipStream_t st) {
@@ -1031,8 +1027,6 @@ static hipError_t launch_small(const MatrixJobs& js, int which, hipStream_t st, 
     case 3: small_kernel<64, 1, 4>(j, st); break;
     case 4: small_kernel<64, 2, 4>(j, st); break;
     case 5: small_kernel<64, 4, 4>(j, st); break;
-    case 6: small_kernel<128, 1, 4>(j, st); break;
-    case 7: small_kernel<128, 1, 8>(j, st); break;
     default: small_kernel<128, 2, 8>(j, st); break;
   }
   if (tm) tm->end();
