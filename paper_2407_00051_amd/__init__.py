@@ -652,6 +652,14 @@ class Context:
             return tuple(t.shape)
         raise ValueError("matrices must be [rows][cols] or [count][rows][cols]")
 
+    @staticmethod
+    def _newton_schulz(steps, coef, eps):
+        if steps < 1:
+            raise ValueError("steps must be >= 1")
+        if len(coef) != 3:
+            raise ValueError(f"coef must be three numbers, got {len(coef)}")
+        return NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps)
+
     def orthogonalise(self, x, steps: int = 5, coef: Sequence[float] = NS_COEF, eps: float = 1e-7, out=None):
         """Newton-Schulz steps on every matrix of x, [rows][cols] or [count][rows][cols], fp32 or bf16:
         singular values to a band around 1, singular vectors kept.  out may be x."""
@@ -664,10 +672,8 @@ class Context:
         o = out if out is not None else torch.empty_like(x)
         if out is not None:
             _check_tensor(out, "out", x.dtype, x.shape, self.device)
-        if steps < 1:
-            raise ValueError("steps must be >= 1")
+        ns = self._newton_schulz(steps, coef, eps)
         self._owned(o if out is None else None, x)
-        ns = NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps)
         self._check(self.lib.sagips_orthogonalise(self.h, ctypes.byref(ns), F32 if x.dtype == torch.float32 else BF16,
                                                   x.data_ptr(), count, rows, cols, o.data_ptr()))
         return o
@@ -682,8 +688,7 @@ class Context:
         n = len(params)
         if not (n == len(grads) == len(momenta)) or not 1 <= n <= MAX_TENSORS:
             raise ValueError("params, grads and momenta must have the same length, 1..16")
-        if steps < 1:
-            raise ValueError("steps must be >= 1")
+        ns = self._newton_schulz(steps, coef, eps)
         dtype = grads[0].dtype
         if dtype not in (torch.float32, torch.bfloat16):
             raise TypeError(f"grads must be torch.float32 or torch.bfloat16, got {dtype}")
@@ -698,8 +703,7 @@ class Context:
             ms.count[i], ms.rows[i], ms.cols[i] = self._stack(p)
             ms.param[i], ms.grad[i], ms.m[i] = p.data_ptr(), grads[i].data_ptr(), momenta[i].data_ptr()
         self._owned(params, grads, momenta)
-        o = Muon(lr, momentum, weight_decay, 1 if nesterov else 0, scale,
-                 NewtonSchulz(steps, (ctypes.c_double * 3)(*coef), eps))
+        o = Muon(lr, momentum, weight_decay, 1 if nesterov else 0, scale, ns)
         self._check(self.lib.sagips_muon_step(self.h, ctypes.byref(ms), ctypes.byref(o)))
 
 

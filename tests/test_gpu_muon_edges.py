@@ -100,3 +100,12 @@ def test_stacks_beyond_one_part(gpu_ctx):
     for i in range(2):
         gpu_ctx.muon_step([own[0][i]], [t[150 * i:150 * i + 150].clone()], [own[1][i]], 0.1)
         assert torch.equal(p[i], own[0][i]) and torch.equal(m[i], own[1][i])
+
+
+def test_coefficients_come_in_threes(gpu_ctx):
+    x = torch.zeros((8, 8), device="cuda:0")
+    for coef in ((1.5, -0.5), (1.5,), (1.5, -0.5, 0.0, 0.0)):
+        with pytest.raises(ValueError, match="three"):
+            gpu_ctx.orthogonalise(x, coef=coef)
+        with pytest.raises(ValueError, match="three"):
+            gpu_ctx.muon_step([x], [torch.zeros_like(x)], [torch.zeros_like(x)], 0.1, coef=coef)
