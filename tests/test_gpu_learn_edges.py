@@ -6,7 +6,7 @@ import pytest
 
 import oracle
 from tests.parity import to_np
-from tests.test_gpu_learn import ADV_TOL, KW, TOL, _check_policy, _events, _policy_case, _pref_case, _t
+from tests.test_gpu_learn import ADV_TOL, KW, TOL, _check_policy, _events, _mask, _policy_case, _pref_case, _t
 
 pytestmark = pytest.mark.gpu
 
@@ -168,3 +168,77 @@ def test_more_contexts_than_counters(gpu_ctx):
             assert all(torch.equal(a, b) for a, b in zip(_both(ctx, c, p), want))
         for ctx in many:
             ctx.close()
+
+
+# ---- every way in which sums are joined
+
+def _launches(ctx, call):
+    """The call's result and the names of the kernels that it launched."""
+    ctx.set_timing(True)
+    ctx.kernel_times()
+    out = call()
+    names = set(ctx.kernel_times())
+    ctx.set_timing(False)
+    return out, names
+
+
+def _sum_of_terms(c, kl_coef, average):
+    """As the oracle's abs_dtheta, but with the slope dL/dl = -rho A [not clipped] - kl_coef (e^r - 1) by
+    its terms too: over thousands of short rows it comes near 0 in some row, and there its own
+    rounding, 1e-5 of rho A and of e^r, is what is left."""
+    x, m = c["x"].astype(np.float64), np.ones(c["adv"].shape, bool) if c["mask"] is None else c["mask"]
+    rows, E, d = x.shape
+    each = lambda t: oracle.event_logp(np.repeat(t, E, 0), x.reshape(-1, d))     # noqa: E731
+    l, _, terms = each(c["theta"])
+    rho, r = np.exp(l - each(c["theta_old"])[0]), each(c["theta_ref"])[0] - l
+    A = np.where(m, c["adv"], 0.0).reshape(-1).astype(np.float64)
+    cut = np.clip(rho, 1.0 - KW["clip_low"], 1.0 + KW["clip_high"]) * A < rho * A
+    n = m.sum(1)
+    w = np.where(m, 1.0 / n.sum() if average == "events" else (1.0 / np.maximum(n, 1) / (n > 0).sum())[:, None], 0.0).reshape(-1)
+    size = w * (np.where(cut, 0.0, np.abs(rho * A)) + kl_coef * (np.exp(r) + 1.0))
+    return (size[:, None] * terms).reshape(rows, E, -1).sum(1)
+
+
+@pytest.mark.parametrize("average", ["events", "rows"])
+@pytest.mark.parametrize("mask", ["none", "holes"])
+@pytest.mark.parametrize("rows,E,two", [(60, 257, False), (60, 600, False), (60, 1000, False),         # 2, 3, 4 slices a row
+                                        (1400, 257, True), (1400, 600, True), (1400, 1000, True),
+                                        (9000, 17, True), (1300, 90, True), (1370, 3, True)])
+def test_policy_joins(gpu_ctx, rows, E, two, mask, average):
+    print(f"case policy join {rows} x {E} mask={mask} {average}", flush=True)
+    rng = np.random.default_rng(rows + E)
+    c = _policy_case(rng, rows, E, 3, mask, True)
+    want = oracle.policy_loss(**c, **KW, average=average)
+    want["abs_dtheta"] = _sum_of_terms(c, KW["kl_coef"], average)
+    if c["mask"] is not None:
+        c["adv"][~c["mask"]] = np.nan
+    got, names = _launches(gpu_ctx, lambda: gpu_ctx.policy_loss(**{k: _t(v) for k, v in c.items()}, **KW, average=average))
+    assert ("policy_finish" in names) == two, names
+    _check_policy(got, want)
+
+
+@pytest.mark.parametrize("rows,pairs,T,d,two", [(40, 64, 70, 2, True), (40, 64, 70, 3, True), (3000, 1, 5, 3, True), (3000, 1, 5, 2, True),
+                                                (1400, 7, 9, 3, True), (1, 6000, 3, 2, False), (1, 1200, 90, 3, True),
+                                                (2, 3, 4096, 2, False)])
+def test_preference_joins(gpu_ctx, rows, pairs, T, d, two):
+    print(f"case preference join {rows} x {pairs} x {T} d={d}", flush=True)
+    rng = np.random.default_rng(rows + pairs)
+    c = _pref_case(rng, rows, pairs, T, T, d, True)
+    want = oracle.preference_loss(**c, beta=0.1, label_smoothing=0.05)
+    got, names = _launches(gpu_ctx, lambda: gpu_ctx.preference_loss(**{k: _t(v) for k, v in c.items()}, beta=0.1, label_smoothing=0.05))
+    assert ("preference_finish" in names) == two, names
+    assert np.all(np.abs(to_np(got["margin"]) - want["margin"]) <= 0.1 * TOL * 2 * T)
+    assert abs(got["loss"].item() - want["loss"]) <= 0.1 * TOL * 2 * T + 1e-6 * want["loss"]
+    assert np.all(np.abs(to_np(got["dtheta"]) - want["dtheta"]) <= (TOL + 0.1 * TOL * 2 * T) * want["abs_dtheta"])
+
+
+@pytest.mark.parametrize("mask", ["none", "holes"])
+@pytest.mark.parametrize("rows,E", [(40000, 17), (3000, 200), (600, 1000), (9000, 60)])
+def test_advantages_of_many_rows(gpu_ctx, rows, E, mask):
+    print(f"case advantage {rows} x {E} mask={mask}", flush=True)
+    rng = np.random.default_rng(rows)
+    r = (rng.standard_normal((rows, E)) + 10.0 * rng.standard_normal((rows, 1))).astype(np.float32)
+    m = _mask(rng, mask, r.shape)
+    ref = oracle.group_advantage(r, m, True, 1e-6)
+    got = to_np(gpu_ctx.group_advantage(_t(r if m is None else np.where(m, r, np.float32(np.inf))), mask=_t(m))).astype(np.float64)
+    assert np.all(np.abs(got - ref) <= ADV_TOL * np.abs(ref).max(1, keepdims=True))

@@ -7,7 +7,7 @@ import pytest
 
 import oracle
 from tests.parity import to_np
-from tests.test_gpu_muon import _assert_close
+from tests.test_gpu_muon import _assert_close, _gradients
 
 pytestmark = pytest.mark.gpu
 
@@ -109,3 +109,16 @@ def test_coefficients_come_in_threes(gpu_ctx):
             gpu_ctx.orthogonalise(x, coef=coef)
         with pytest.raises(ValueError, match="three"):
             gpu_ctx.muon_step([x], [torch.zeros_like(x)], [torch.zeros_like(x)], 0.1, coef=coef)
+
+
+@pytest.mark.parametrize("shape", [(3, 1, 7), (4, 33, 65), (3, 65, 64), (7, 128, 128), (1, 129, 300), (2, 300, 129), (1, 40, 3000),
+                                   (300, 16, 20)])
+def test_bf16_is_rounded_once(gpu_ctx, shape):
+    """bf16 matrices are taken exactly and held in the same terms as fp32 ones; what is left is the
+    rounding of the result, 2^-9 of each value."""
+    print(f"case bf16 {shape}", flush=True)
+    rng = np.random.default_rng(shape[1])
+    x = torch.tensor(_gradients(rng, shape), dtype=torch.bfloat16, device="cuda:0")
+    got, ref = to_np(gpu_ctx.orthogonalise(x).float()), oracle.orthogonalise(to_np(x.double()))
+    tol = (485 + 5 * _norm(ref)) * UNIT + 2.0 ** -9 * _norm(ref)
+    assert np.all(_norm(got - ref) <= tol), _norm(got - ref) / tol
