@@ -26,7 +26,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kT = 2;                          // terms
-constexpr float kScale = 4096.0f, kInvScale = 1.0f / 4096.0f;
+constexpr int kScaleBits = 12;
+constexpr float kScale = 1 << kScaleBits, kInvScale = 1.0f / kScale;
 constexpr float kScaleY = 0.25f;               // of A X, over that of the others
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -315,6 +316,8 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int z, ti, tj;
   if (!tile_of<kSym>(g, z, ti, tj)) return;
+  // read here: where it is needed, every tile would wait for it
+  const int up = kMode == kGram ? 0 : up_after(g.up[z], g.spent), up_next = up_after(up, g.grow);
   const int64_t pp = (int64_t)kT * g.np * g.kp, qp = (int64_t)kT * g.width * g.kp, op = (int64_t)kT * g.np * g.width;
   // a tile may reach past the last block: those rows repeat it, and their results go nowhere
   const int ni = g.np / 32, nj = g.width / 32;
@@ -400,7 +403,6 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
   // Each kept block: lane lr + 32 h has row i, columns 8 g + 4 h + 0..3.
   float* const turn = reinterpret_cast<float*>(sums) + wave * (32 * 33);
   const int t = kMode == kStore ? tensor_of(jobs.first, z) : 0;
-  const int up = kMode == kGram ? 0 : up_after(g.up[z], g.spent), up_next = up_after(up, g.grow);
   const bool flip = jobs.rows > jobs.cols;
 #pragma unroll
   for (int b = 0; b < OB; ++b) {
@@ -451,7 +453,7 @@ __global__ __launch_bounds__(kThreads, TB == 2 ? 3 : 1) void k_ns_gemm(GemmArgs 
       for (int r = 0; r < 16; ++r) {
         if (row_of(r) >= jobs.rows || col >= jobs.cols) continue;
         const int64_t to = base + (int64_t)row_of(r) * jobs.cols + col;
-        const float x = __builtin_ldexpf(v[r] * kInvScale, -up);
+        const float x = __builtin_ldexpf(v[r], -kScaleBits - up);
         if (jobs.m[t]) static_cast<float*>(jobs.out[t])[to] = fmaf(-jobs.rate, x, jobs.decay * old[r]);
         else if (jobs.out_bf16) static_cast<u16*>(jobs.out[t])[to] = to_bf16(x);
         else static_cast<float*>(jobs.out[t])[to] = x;
@@ -820,7 +822,7 @@ __global__ __launch_bounds__(64 * W, 1) void k_ns_small(SmallJobs jobs) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int j = 32 * (b * CW + cw) + 8 * (r >> 2) + 4 * lh + (r & 3);
-      if (i < n && j < L) flat[i * pi + j * pj] = __builtin_ldexpf(x[b][r] * kInvScale, -up);
+      if (i < n && j < L) flat[i * pi + j * pj] = __builtin_ldexpf(x[b][r], -kScaleBits - up);
     }
   if (job.m) small_store<kN, false, true>(jobs, job, base, flat, pitch);
   else if (jobs.out_bf16) small_store<kN, true, false>(jobs, job, base, flat, pitch);
@@ -848,7 +850,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 struct Plan {
   int n, L, np, lp, chunks, mats;
-  size_t up, r0, r1, c0, c1, A, B, bytes;   // offsets; the partial sums come first
+  size_t r0, r1, c0, c1, A, B, up, bytes;   // offsets; the partial sums come first
 };
 Plan plan_of(int rows, int cols, int mats) {
   Plan p;
@@ -860,14 +862,14 @@ Plan plan_of(int rows, int cols, int mats) {
   p.chunks = (int)(((int64_t)rows * cols + kChunk - 1) / kChunk);
   const size_t part = align256((size_t)mats * p.chunks * sizeof(double));
   const size_t x = align256((size_t)mats * kT * p.np * p.lp * 2), a = align256((size_t)mats * kT * p.np * p.np * 2);
-  p.up = part;
-  p.r0 = p.up + align256((size_t)mats * sizeof(int));
+  p.r0 = part;
   p.r1 = p.r0 + x;
   p.c0 = p.r1 + x;
   p.c1 = p.c0 + x;
   p.A = p.c1 + x;
   p.B = p.A + a;
-  p.bytes = p.B + a;
+  p.up = p.B + a;
+  p.bytes = p.up + align256((size_t)mats * sizeof(int));
   return p;
 }
 
