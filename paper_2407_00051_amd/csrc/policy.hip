@@ -204,18 +204,21 @@ __device__ __forceinline__ void block_sum_d(double (&v)[N]) {
 
 // ---- advantages --------------------------------------------------------------
 // (r - mean) / (std + eps) over a row's valid events.  The mean is a 64-bit sum,
-// so that a row of equal rewards gives zeros, whatever eps; deviations and their
-// quotients are formed in 64 bits and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26 us
+// so that a row of equal rewards gives zeros, whatever eps; deviations are formed in
+// 64 bits and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26 us
 // (128 MB at 4.9 TB/s), 16,384 x 1,000 22, 4,096 x 4,097 29; by the time of one read, two
 // sums over lanes and one write where they are few (6-7 us a call).
 
 constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing, at most
 constexpr int kAdvBlock = 1024;
 
-// What a row's deviations are multiplied by: 0 where there are none, since 1 / (0 + eps) may be infinite.
-__device__ __forceinline__ double inverse_deviation(double squares, double n, double eps) {
-  const double sd = n > 0.0 ? sqrt(squares / n) : 0.0;
-  return sd > 0.0 ? 1.0 / (sd + eps) : 0.0;
+// Whether fp32 deviations times 1 / (sd + eps) in fp32 give a row's advantages.  Else (also where
+// sd + eps is 0) write_wide reads the row again and stays in 64 bits until the end.
+__device__ __forceinline__ bool fits_fp32(float inv) { return inv >= 1e-30f && inv <= 1e30f; }
+__device__ __forceinline__ void write_wide(const float* reward, const uint8_t* mask, int e0, int step, int E, double mean, double sd,
+                                           double eps, float* adv) {
+  const double inv = sd == 0.0 ? 0.0 : 1.0 / (sd + eps);   // no deviations: 0, not 0 / 0
+  for (int e = e0; e < E; e += step) adv[e] = !mask || mask[e] ? (float)(((double)reward[e] - mean) * inv) : 0.0f;
 }
 
 // Reads a lane's events e0 + i * step < E of the row at `off`: v, 0 where not valid, and a bit for
@@ -257,8 +260,8 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
   // The workgroup's first row and this lane's, from the first
   const int64_t row0 = kBlock ? blockIdx.x : (int64_t)blockIdx.x * kWaves << (6 - lg);
   const int ahead = kBlock ? 0 : ((threadIdx.x >> 6) << (6 - lg)) + (lane >> lg), last = (int)min((int64_t)255, n_rows - 1 - row0);
-  const bool on = ahead <= last;
-  const int off = (on ? ahead : last) * E;
+  const bool on = kBlock || ahead <= last;
+  const int off = kBlock ? 0 : (on ? ahead : last) * E;
   const float* from = reward + row0 * E;
   float* to = adv + row0 * E;
   float v[kHeld];
@@ -279,18 +282,24 @@ __global__ __launch_bounds__(kBlock ? kAdvBlock : kThreads) void k_advantage(con
   for (int i = 0; i < kHeld; ++i) {
     const double dev = (valid >> i) & 1u ? (double)v[i] - mean : 0.0;
     q[0] = fma(dev, dev, q[0]);
+    v[i] = (float)dev;
   }
-  double inv = 1.0;
+  float inv = 1.0f;
   if (normalise) {
     if constexpr (kBlock) block_sum_d<1, kAdvBlock>(q);
     else
       for (int s = 0; s < lg; ++s) q[0] += __shfl_xor(q[0], 1 << s, 64);
-    inv = inverse_deviation(q[0], n, eps);
+    const double sd = n > 0.0 ? sqrt(q[0] / n) : 0.0;
+    inv = 1.0f / ((float)sd + (float)eps);
+    if (__builtin_expect(!fits_fp32(inv), 0)) {
+      if (on) write_wide(from + off, mask ? mask + row0 * E + off : nullptr, l, step, E, mean, sd, eps, to + off);
+      return;
+    }
   }
 #pragma unroll
   for (int i = 0; i < kHeld; ++i) {
     const int e = l + i * step;
-    if (on && e < E) to[off + e] = (valid >> i) & 1u ? (float)(((double)v[i] - mean) * inv) : 0.0f;
+    if (on && e < E) to[off + e] = (valid >> i) & 1u ? v[i] * inv : 0.0f;
   }
 }
 
@@ -344,15 +353,20 @@ __global__ __launch_bounds__(kAdvBlock, 8) void k_adv_apply(const float* reward,
     const double dm = p[3 * i + 1] - mean;
     q[0] += p[3 * i] > 0.0 ? p[3 * i + 2] + p[3 * i] * dm * dm : 0.0;
   }
-  double inv = 1.0;
+  float inv = 1.0f;
   if (normalise) {
     block_sum_d<1, kAdvBlock>(q);
-    inv = inverse_deviation(q[0], t[1], eps);
+    const double sd = t[1] > 0.0 ? sqrt(q[0] / t[1]) : 0.0;
+    inv = 1.0f / ((float)sd + (float)eps);
+    if (__builtin_expect(!fits_fp32(inv), 0)) {
+      write_wide(reward + base, mask ? mask + base : nullptr, threadIdx.x, kAdvBlock, n, mean, sd, eps, adv + base);
+      return;
+    }
   }
 #pragma unroll
   for (int i = 0; i < kAdvSlice / kAdvBlock; ++i) {
     const int e = threadIdx.x + i * kAdvBlock;
-    if (e < n) adv[base + e] = (valid >> i) & 1u ? (float)(((double)v[i] - mean) * inv) : 0.0f;
+    if (e < n) adv[base + e] = (valid >> i) & 1u ? (float)((double)v[i] - mean) * inv : 0.0f;
   }
 }
 
