@@ -364,13 +364,15 @@ sagips_status sagips_group_advantage(sagips_ctx* ctx, const float* reward, const
  * MEAN_ROWS over each row's and then over the rows that have any.  Without
  * any valid event every output is 0.  Events outside the mask are not looked
  * at.  Events are read clamped to [2^-126, 1 - 2^-24].
- *   theta, theta_old, theta_ref  [n_theta][2d] fp32, 4-byte aligned, positive;
- *             theta_ref may be NULL; 1 <= n_theta <= 65535, d in {2, 3}
+ *   theta, theta_old, theta_ref  [n_theta][2d] fp32, 4-byte aligned, 2^-100 to
+ *             2^100 (beyond, an event's terms leave fp32's range); theta_ref may
+ *             be NULL; 1 <= n_theta <= 65535, d in {2, 3}
  *   x         [n_theta * events_per_theta][d] fp32; n_theta * E < 2^31
  *   adv       [n_theta * events_per_theta] fp32
  *   mask      [n_theta * events_per_theta] bytes as in 9., or NULL
  *   loss, kl, clip_frac [1]  L, the mean of K, the mean share of events whose
- *             clipped term is the smaller; each may be NULL
+ *             clipped term is the smaller; each may be NULL.  rho A of A = 0 is 0
+ *             and kl_coef K of kl_coef = 0 too, where rho or K is beyond fp32
  *   dtheta    [n_theta][2d] dL/dtheta, or NULL
  * 0 <= clip_low <= 1, clip_high >= 0, kl_coef >= 0.                           */
 typedef enum { SAGIPS_MEAN_EVENTS = 0, SAGIPS_MEAN_ROWS = 1 } sagips_mean;

@@ -8,7 +8,7 @@
 //   2^12 m = hi + lo,  hi = fp16(2^12 m), lo = fp16(2^12 m - hi),
 // each rounded to nearest even: |2^12 m - hi| <= 2^-12 |2^12 m|, and the rest is at most
 // 2^-24 of it, half a unit in the last place of fp32, while lo is not subnormal (|m|
-// above 6e-5; below, at most 2^-37).  Products of fp16 values are exact in fp32, and of
+// above 6e-5; below, at most 2^-37: X is held up by a power of two while it is small).  Products of fp16 values are exact in fp32, and of
 // the four term products lo lo is at most 2^-24 of the whole, no more than the rounding
 // of one fp32 product.  Three products on the fp16 matrix cores into one fp32
 // accumulator, smallest first, therefore replace an fp32 product at 16/3 of the rate of
@@ -888,7 +888,9 @@ int per_part(int rows, int cols, int mats) {
 // less per product but has more to add up at the end, and only tiles of 2 run three to a
 // unit, which the rounds count as one after the other).  Products at 2,048 x 2,048:
 // symmetric 43, 30, 37 us with sides 2, 3, 4, others 61, 61, 50; at K = 512 a side of 2 is
-// the fastest at every count (16 of 512 x 512: 13, 20, 16 and 21, 39, 22 us).
+// the fastest at every count (16 of 512 x 512: 13, 20, 16 and 21, 39, 22 us).  A round that fills
+// part of the units is faster than that (the 136 symmetric tiles of side 4 at 2,048: 37 us, 50 by the
+// model), so that a larger side may be passed over where tiles are few.
 int tile_side(bool sym, int np, int width, int K, int mats, int n_cu) {
   static const double fixed[5] = {0, 0, 2.6, 7.6, 13.0}, per_k[5] = {0, 0, 0.0064, 0.0115, 0.018};
   int best = 2;

@@ -152,7 +152,7 @@ __device__ __forceinline__ void load_event(const float* __restrict__ x, int64_t 
   for (int j = 0; j < D; ++j) v[j] = p[j];
 }
 
-// e^r - 1 - r: by its series below 1/2 (next term 2e-8 of it), where the subtraction would cancel.
+// e^r - 1 - r: by its series below 1/2 (next term at most 5e-8 of it), where the subtraction would cancel.
 __device__ __forceinline__ float exp_minus_line(float r) {
   float p = 1.0f / 40320.0f;
   p = fmaf(p, r, 1.0f / 5040.0f);
@@ -205,15 +205,16 @@ __device__ __forceinline__ void block_sum_d(double (&v)[N]) {
 // ---- advantages --------------------------------------------------------------
 // (r - mean) / (std + eps) over a row's valid events.  The mean is a 64-bit sum,
 // so that a row of equal rewards gives zeros, whatever eps; deviations are formed in
-// 64 bits and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26 us
-// (128 MB at 4.9 TB/s), 16,384 x 1,000 22, 4,096 x 4,097 29; by the time of one read, two
+// 64 bits and rounded once.  Bound by memory where rows are many: 1,000,000 x 16 take 26-31 us
+// (128 MB at 4.1 to 4.9 TB/s), 16,384 x 1,000 22, 4,096 x 4,097 28; by the time of one read, two
 // sums over lanes and one write where they are few (6-7 us a call).
 
 constexpr int kAdvHeld = 16;   // rewards a lane holds between reading and writing, at most
 constexpr int kAdvBlock = 1024;
 
 // Whether fp32 deviations times 1 / (sd + eps) in fp32 give a row's advantages.  Else (also where
-// sd + eps is 0) write_wide reads the row again and stays in 64 bits until the end.
+// sd + eps is 0) write_wide reads the row again and stays in 64 bits until the end.  With 64 bits
+// for every row 4,096 x 4,097 take 33 us instead of 28: more registers, fewer waves.
 __device__ __forceinline__ bool fits_fp32(float inv) { return inv >= 1e-30f && inv <= 1e30f; }
 __device__ __forceinline__ void write_wide(const float* reward, const uint8_t* mask, int e0, int step, int E, double mean, double sd,
                                            double eps, float* adv) {
@@ -526,10 +527,10 @@ __global__ __launch_bounds__(kThreads) void k_policy_finish(PolicyFinish p) {
 // loss, the KL term, the clipped events and the events, and of the gradient; where
 // a row has whole workgroups of slices, a workgroup's four units leave one record.
 // Bound by VALU issue: 64 events of three coordinates against two rows take 26
-// transcendental and 186 other operations, 48% of all in pairs (adds, products and
+// transcendental and 188 other operations, 51% of all in pairs (adds, products and
 // fmas with a literal do; compares, selects, fmac and fmas of three registers do not), and
 // the vector units issue in all of the cycles in which a compute unit works.  1,024 x 16,384
-// events with mask and KL term: 114-116 us with the second launch; reading them takes 61 at
+// events with mask and KL term: 113-119 us with the second launch; reading them takes 61 at
 // the rate of a large copy.  Where no joining follows in it, the kernel is held to 64
 // registers, so that the 8,192 waves are resident together: with 71, seven to a SIMD and an
 // eighth after them, 139 us.
@@ -813,10 +814,16 @@ __global__ __launch_bounds__(kThreads) void k_pref_slices(PrefArgs p) {
 // workgroup can join what the others left in the time of that launch (up to 256 of them: 1,024
 // rows of 100 events 13.7 us a call against 15.7, 1,024 x 100 single-event pairs 11.7 against
 // 14.5; beyond, 600 rows of 600 events 27 against 14, 64 x 64 pairs of 100 events 40 against 13).
+// Near the bound either may win: 300 rows of 600 events (225 workgroups, three slices a row) take 19
+// against 15, 1,300 and 1,600 rows of 90 (325 and 400 workgroups) 17-18 in one launch, 15-19 in two.
+// A gradient of more than 8,192 values is too much for one workgroup however few there are: 8,000
+// rows of 2 events 35 us against 17, 30,000 92 against 32.
 bool ends_in_last(int64_t blocks, int64_t rows, int d) {
   return blocks <= 256 && rows * 2 * d <= 8192;
 }
-constexpr int64_t kTargetUnits = 8192;   // waves that share an array of rows (4,096, 20,480 and 40,960: 128, 131 and 155 us against 127)
+// Waves that share an array of rows.  Policy loss of 1,024 x 16,384 events 116 us; with 4,096 waves
+// 133, with 16,384 116.  64 x 65,536: 38, 39 and 41.  The preference loss is alike with each.
+constexpr int64_t kTargetUnits = 8192;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -853,6 +860,9 @@ struct PrefPlan {
   int64_t chunk, units, slice_chunk;
   size_t part_off, bytes;
 };
+// Sets beyond this many events are cut into slices.  Where pairs are few that is late: one pair of
+// 4,096 events, a wave's, takes 39 us and one of 4,097 15 (cut from 1,024 or 256 on, 14-16 either),
+// 64 x 64 pairs of 4,096 110 (97); 64 x 64 ragged pairs of up to 700 take 24 however it is.
 constexpr int64_t kLongSet = 4096;
 PrefPlan pref_plan(int64_t rows, int64_t pairs, int64_t T, int d) {
   PrefPlan p;
@@ -896,6 +906,8 @@ hipError_t policy_d(const sagips_policy& P, const PolicyPlan& pl, const float* x
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ticket) return e;
+  // at most 128 workgroups, since each forms the totals: 65,535 rows of 16 events, averaged over rows,
+  // 73 us with the first launch; with up to 1,024 99, with up to 32 84
   const int64_t blocks = pl.records == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kThreads >> a.fin.lg);
   if (tm) tm->begin("policy_finish");
   hipLaunchKernelGGL((k_policy_finish<D>), dim3((unsigned)(blocks > 128 ? 128 : blocks)), dim3(kThreads), 0, st, a.fin);
@@ -951,6 +963,7 @@ hipError_t pref_d(const sagips_preference& P, const PrefPlan& pl, const float* c
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !finish || a.ticket) return e;
+  // only the first workgroup forms a total: any bound will do (128 and 1,024 are within 3% of 4,096)
   const int64_t n = pl.S == 1 ? ceil_div((int64_t)P.n_theta * 2 * D, kThreads) : ceil_div(P.n_theta, kThreads >> a.fin.lg);
   if (tm) tm->begin("preference_finish");
   hipLaunchKernelGGL((k_pref_finish<D>), dim3((unsigned)(n > 4096 ? 4096 : n)), dim3(kThreads), 0, st, a.fin);
