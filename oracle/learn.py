@@ -56,7 +56,8 @@ def group_advantage(reward, mask=None, normalise=True, eps=1e-6):
 def policy_loss(theta, theta_old, x, adv, theta_ref=None, mask=None, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
                 average="events"):
     """dict(loss, kl, clip_frac, dtheta, abs_dtheta): the last is the sum of the terms' absolute
-    values, for condition-aware comparison."""
+    values, for condition-aware comparison, with an event's slope dL/dl taken as a whole (it may
+    itself be a small rest of the ratio's and the divergence's)."""
     theta = np.asarray(theta, np.float64)
     R, E, d = x.shape
     m = np.ones((R, E), bool) if mask is None else np.asarray(mask) != 0

@@ -115,7 +115,7 @@ Cost policy_cost(sagips_ctx* c) {
 void counters_of_contexts() {
   const int n = 70, sets = 64;
   static sagips_ctx* c[n];
-  for (int round = 0; round < 2; ++round) {
+  for (int again = 0; again < 2; ++again) {
     int once = 0;
     for (int i = 0; i < n; ++i) {
       expect("create", sagips_create(&c[i], 0, nullptr), SAGIPS_OK, nullptr);
