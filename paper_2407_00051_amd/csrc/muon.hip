@@ -8,9 +8,9 @@
 //   2^12 m = hi + lo,  hi = fp16(2^12 m), lo = fp16(2^12 m - hi),
 // each rounded to nearest even: |2^12 m - hi| <= 2^-12 |2^12 m|, and the rest is at most
 // 2^-24 of it, half a unit in the last place of fp32, while lo is not subnormal (|m|
-// above 6e-5; below, at most 2^-37: X is held up by a power of two while it is small).  Products of fp16 values are exact in fp32, and of
-// the four term products lo lo is at most 2^-24 of the whole, no more than the rounding
-// of one fp32 product.  Three products on the fp16 matrix cores into one fp32
+// above 6e-5; below, at most 2^-37: X is held up by a power of two while it is small).
+// Products of fp16 values are exact in fp32, and of the four term products lo lo is at
+// most 2^-24 of the whole, no more than the rounding of one fp32 product.  Three products on the fp16 matrix cores into one fp32
 // accumulator, smallest first, therefore replace an fp32 product at 16/3 of the rate of
 // the fp32 matrix instructions.  fp16 ends at 65,504, so entries must stay below 15.9:
 // they do because the singular values do (the entry points bound them from the
