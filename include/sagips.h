@@ -483,6 +483,133 @@ typedef struct {
 
 sagips_status sagips_muon_step(sagips_ctx* ctx, const sagips_matrix_set* set, const sagips_muon* options);
 
+/* 13. Choices: log probabilities of given choices, the entropy and the most
+ * likely alternatives of a categorical distribution a row, from its logits.
+ * With z = scale * logits, m = max z and s = sum exp(z - m) over a row,
+ *   ln p_v = z_v - m - ln s,   H = -sum p_v ln p_v.
+ * A logit of -infinity is a masked choice: p = 0, and it adds nothing.  A row of
+ * nothing else has H = 0.  A NaN or +infinity in a row makes its results NaN (and
+ * its alternatives -1).
+ *   type      SAGIPS_F32 or SAGIPS_BF16: type of the logits
+ *   logits    [rows][n_choices], row r at logits + r * stride; stride >=
+ *             n_choices; aligned to one value, rows of any alignment
+ *   scale     2^-100 to 2^100 (an inverse temperature)
+ *   top       alternatives asked for, 0 to SAGIPS_MAX_TOP
+ * 1 <= rows < 2^31, 1 <= n_choices <= 2^30, stride < 2^31.                    */
+#define SAGIPS_MAX_TOP 32
+typedef struct {
+  const void* logits;
+  int64_t rows;
+  int64_t stride;
+  int32_t n_choices;
+  int32_t type;  /* sagips_precision */
+  int32_t top;
+  double scale;
+} sagips_choices;
+
+/*   choice      [rows] int32, or NULL: none given.  A row whose choice is outside
+ *               [0, n_choices) has none
+ *   logp        [rows] ln p of the row's choice: 0 where it has none, -infinity
+ *               where it is masked; NULL if choice is
+ *   entropy     [rows], or NULL
+ *   top_choice  [rows][top] int32, the choices of the largest logits in falling
+ *               order, of equal ones the lowest first; -1 beyond the choices that
+ *               are not masked
+ *   top_logp    [rows][top] their ln p; -infinity where top_choice is -1
+ *   stats       [rows][2]: m / scale (0 in a row without choices) and ln s, what
+ *               14. needs of the row; or NULL
+ * top_choice and top_logp are NULL if top is 0.  All 4-byte aligned.  Outputs
+ * must not overlap the inputs or each other.                                 */
+sagips_status sagips_choice_logprob(sagips_ctx* ctx, const sagips_choices* C, const int32_t* choice, float* logp,
+                                    float* entropy, int32_t* top_choice, float* top_logp, float* stats);
+
+/* 14. The gradient of 13.: for d_logp, d_entropy [rows] and d_top [rows][top],
+ * the derivatives of a loss with respect to logp, entropy and top_logp (each may
+ * be NULL: not in the loss; not all),
+ *   dL/dz_v = sum_i g_i ([v = c_i] - p_v) - d_entropy p_v (ln p_v + H)
+ * over the row's choice (d_logp) and its alternatives (d_top); those that 13. gave
+ * as masked or -1 take no part.  dlogits = scale * dL/dz.
+ *   choice, logp, entropy, top_choice, stats   as 13. took and gave them: choice and
+ *             logp with d_logp, entropy with d_entropy, top_choice with d_top, stats always
+ *   dlogits   [rows][n_choices] of C's type, row r at dlogits + r * dstride;
+ *             may be the logits themselves, with their stride, and must not
+ *             overlap them otherwise; columns behind n_choices are left as they were
+ * A row whose results are NaN gets NaN.  top_choice values outside [0, n_choices) are -1. */
+typedef struct {
+  const int32_t* choice;
+  const float* logp;
+  const float* entropy;
+  const int32_t* top_choice;
+  const float* stats;
+  const float* d_logp;
+  const float* d_entropy;
+  const float* d_top;
+} sagips_choice_grads;
+
+sagips_status sagips_choice_backward(sagips_ctx* ctx, const sagips_choices* C, const sagips_choice_grads* g,
+                                     void* dlogits, int64_t dstride);
+
+/* 15. Rows sorted by the member (expert) that they are given to.  Every row has
+ * `slots` members; slot k of row r is item r * slots + k.  Items are sorted by
+ * member, in their own order within a member.
+ *   member   [rows][slots] int32; an item whose member is outside [0, n_members)
+ *            is given to none
+ *   offsets  [n_members + 1] int32: member m has the sorted positions offsets[m]
+ *            .. offsets[m + 1] - 1
+ *   order    [rows * slots] int32: the item at each sorted position; -1 from
+ *            offsets[n_members] on
+ *   place    [rows][slots] int32: each item's sorted position, or -1
+ * rows, slots >= 1, slots <= 32, rows * slots < 2^31 - 2^20, 1 <= n_members <= 1024;
+ * all 4-byte aligned; outputs must not overlap the input or each other.      */
+sagips_status sagips_route(sagips_ctx* ctx, const int32_t* member, int64_t rows, int32_t slots, int32_t n_members,
+                           int32_t* offsets, int32_t* order, int32_t* place);
+
+/* 16. Rows to their members and back.  A plan of 15. (its place alone is read):
+ * positions outside [0, rows * slots) are taken as -1.  x, y, ... are of `type`
+ * (SAGIPS_F32 or SAGIPS_BF16) with `width` values a row, densely packed, aligned
+ * to one value; weight, dweight [rows][slots] fp32, 4-byte aligned.
+ * Sums are fp32, rounded once.
+ *   dispatch          sorted[place[r][k]] = x[r]
+ *   combine           out[r] = sum_k weight[r][k] y[place[r][k]]; weight NULL: 1
+ *   combine_backward  dy[place[r][k]] = weight[r][k] dout[r],
+ *                     dweight[r][k] = <dout[r], y[place[r][k]]>, 0 where place is -1;
+ *                     dy may be NULL, or y and dweight both, not all
+ * sorted, y, dy are [rows * slots][width]: positions that no item has are left as
+ * they were and not looked at.  The gradient of dispatch is combine without
+ * weights.  1 <= width < 2^31; sizes as in 15.; outputs must not overlap inputs.
+ */
+typedef struct {
+  const int32_t* place;
+  int64_t rows;
+  int32_t slots;
+  int32_t width;
+  int32_t type;  /* sagips_precision */
+} sagips_routed;
+
+sagips_status sagips_dispatch(sagips_ctx* ctx, const sagips_routed* R, const void* x, void* sorted);
+sagips_status sagips_combine(sagips_ctx* ctx, const sagips_routed* R, const void* y, const float* weight, void* out);
+sagips_status sagips_combine_backward(sagips_ctx* ctx, const sagips_routed* R, const void* dout, const void* y,
+                                      const float* weight, void* dy, float* dweight);
+
+/* 17. The members of a stack on rows of their own (5. and 6. give every member
+ * all rows): member m takes the rows offsets[m] .. offsets[m + 1] - 1, as 15. and
+ * 16. lay them out.
+ *   x        [n_rows][width[0]] fp32, 1 <= n_rows < 2^29
+ *   offsets  [n_members + 1] int32 on the device, rising, 4-byte aligned; values
+ *            outside [0, n_rows] are taken as the nearer end
+ *   theta    [n_rows][out]; rows of no member are left as they were
+ * Supported generators as for 5.  Outputs must not overlap inputs.           */
+sagips_status sagips_gen_forward_routed(sagips_ctx* ctx, const sagips_gen* G, const float* x, const int32_t* offsets,
+                                        int64_t n_rows, float* theta);
+
+/*   dL_dtheta  [n_rows][out]; rows of no member are not looked at
+ *   dW, db     as in 6.; zero for a member without rows
+ *   dx         [n_rows][width[0]] the gradient with respect to x, or NULL; rows
+ *              of no member are left as they were                            */
+sagips_status sagips_gen_backward_routed(sagips_ctx* ctx, const sagips_gen* G, const float* x, const int32_t* offsets,
+                                         int64_t n_rows, const float* dL_dtheta, float* const* dW, float* const* db,
+                                         float* dx);
+
 #ifdef __cplusplus
 }
 #endif

@@ -53,6 +53,10 @@ Parity status per function (what pins it, see tests/test_oracle_*.py):
                      losses' by finite differences, closed values at equal
                      rows, brute-force means over masks; the orthogonalisation
                      against its matrix products.
+  mixture            pinned: softmax and entropy against scipy, the choices'
+                     gradient by torch autograd and finite differences, routing
+                     against a plain sort, combine and its gradient as each
+                     other's transposes, the members' by finite differences.
 """
 from .philox import philox4x32_10, event_words  # noqa: F401
 from .sampler import (uniform_from_words, kumaraswamy_icdf, kumaraswamy_cdf,  # noqa: F401
@@ -66,3 +70,4 @@ from .gan import gan_step, initial_state  # noqa: F401
 from .generator import G_WIDTHS, generator_forward, generator_backward, ensemble_response, residual  # noqa: F401
 from .learn import (event_logp, group_advantage, policy_loss, preference_loss,  # noqa: F401
                     orthogonalise, muon_step)
+from . import mixture  # noqa: F401

@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsagips.so")
 MAX_LAYERS = 8
 MAX_TENSORS = 16
+MAX_TOP = 32
 _W_NAMES = [f"W[{l}]" for l in range(MAX_LAYERS)]
 _B_NAMES = [f"b[{l}]" for l in range(MAX_LAYERS)]
 
@@ -34,7 +35,9 @@ EXPORTED = ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_
             "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
             "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_noalloc_scratch_bytes",
             "sagips_group_advantage", "sagips_policy_loss", "sagips_preference_loss", "sagips_orthogonalise",
-            "sagips_muon_step")
+            "sagips_muon_step",
+            "sagips_choice_logprob", "sagips_choice_backward", "sagips_route", "sagips_dispatch", "sagips_combine",
+            "sagips_combine_backward", "sagips_gen_forward_routed", "sagips_gen_backward_routed")
 
 
 class SagipsError(RuntimeError):
@@ -96,6 +99,22 @@ class Muon(ctypes.Structure):
                 ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32), ("ns", NewtonSchulz)]
 
 
+class Choices(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("rows", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("n_choices", ctypes.c_int32), ("type", ctypes.c_int32), ("top", ctypes.c_int32), ("scale", ctypes.c_double)]
+
+
+class ChoiceGrads(ctypes.Structure):
+    _fields_ = [("choice", ctypes.c_void_p), ("logp", ctypes.c_void_p), ("entropy", ctypes.c_void_p),
+                ("top_choice", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("d_logp", ctypes.c_void_p),
+                ("d_entropy", ctypes.c_void_p), ("d_top", ctypes.c_void_p)]
+
+
+class Routed(ctypes.Structure):
+    _fields_ = [("place", ctypes.c_void_p), ("rows", ctypes.c_int64), ("slots", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
 class DiscOut(ctypes.Structure):
     _fields_ = [("logits_fake", ctypes.c_void_p), ("logits_real", ctypes.c_void_p),
                 ("loss_d", ctypes.c_void_p), ("loss_g", ctypes.c_void_p),
@@ -145,12 +164,23 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                          ctypes.c_int32, ctypes.c_int32, vp]
     lib.sagips_muon_step.argtypes = [vp, ctypes.POINTER(MatrixSet), ctypes.POINTER(Muon)]
     lib.sagips_preference_loss.argtypes = [vp, ctypes.POINTER(Preference), vp, vp, vp, vp, vp, vp, vp]
+    lib.sagips_choice_logprob.argtypes = [vp, ctypes.POINTER(Choices), vp, vp, vp, vp, vp, vp]
+    lib.sagips_choice_backward.argtypes = [vp, ctypes.POINTER(Choices), ctypes.POINTER(ChoiceGrads), vp, i64]
+    lib.sagips_route.argtypes = [vp, vp, i64, ctypes.c_int32, ctypes.c_int32, vp, vp, vp]
+    lib.sagips_dispatch.argtypes = [vp, ctypes.POINTER(Routed), vp, vp]
+    lib.sagips_combine.argtypes = [vp, ctypes.POINTER(Routed), vp, vp, vp]
+    lib.sagips_combine_backward.argtypes = [vp, ctypes.POINTER(Routed), vp, vp, vp, vp, vp]
+    lib.sagips_gen_forward_routed.argtypes = [vp, ctypes.POINTER(GenStack), vp, vp, i64, vp]
+    lib.sagips_gen_backward_routed.argtypes = [vp, ctypes.POINTER(GenStack), vp, vp, i64, vp, ctypes.POINTER(vp),
+                                               ctypes.POINTER(vp), vp]
     for name in ("sagips_create", "sagips_destroy", "sagips_set_stream", "sagips_set_bf16_chunk_rows",
                  "sagips_set_timing",
                  "sagips_kernel_times", "sagips_sample_events", "sagips_disc_fwd_bwd", "sagips_param_grad",
                  "sagips_bootstrap", "sagips_bootstrap_rows", "sagips_gen_forward", "sagips_gen_backward", "sagips_ensemble_response",
                  "sagips_adam_step", "sagips_disc_fwd_bwd_noalloc", "sagips_group_advantage", "sagips_policy_loss",
-                 "sagips_preference_loss", "sagips_orthogonalise", "sagips_muon_step"):
+                 "sagips_preference_loss", "sagips_orthogonalise", "sagips_muon_step", "sagips_choice_logprob",
+                 "sagips_choice_backward", "sagips_route", "sagips_dispatch", "sagips_combine", "sagips_combine_backward",
+                 "sagips_gen_forward_routed", "sagips_gen_backward_routed"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -705,6 +735,211 @@ class Context:
         self._owned(params, grads, momenta)
         o = Muon(lr, momentum, weight_decay, 1 if nesterov else 0, scale, ns)
         self._check(self.lib.sagips_muon_step(self.h, ctypes.byref(ms), ctypes.byref(o)))
+
+    # -- choices, and a mixture of members -----------------------------------------------------
+    def _choices(self, logits, top, scale) -> Choices:
+        import torch
+        if not isinstance(logits, torch.Tensor):
+            raise TypeError("logits must be a torch.Tensor")
+        if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
+            raise ValueError("logits must be [rows][choices]")
+        if not logits.is_cuda or logits.get_device() != self.device:
+            raise ValueError(f"logits must be on cuda:{self.device}")
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"logits must be torch.float32 or torch.bfloat16, got {logits.dtype}")
+        n, V = logits.shape
+        stride = logits.stride(0) if n > 1 else max(V, logits.stride(0))
+        if (V > 1 and logits.stride(1) != 1) or stride < V:
+            raise ValueError("the choices of a row must follow each other, and rows must not overlap")
+        return Choices(logits.data_ptr(), n, stride, V, F32 if logits.dtype == torch.float32 else BF16, int(top), scale)
+
+    def choice_logprob(self, logits, choice=None, top: int = 0, scale: float = 1.0) -> dict:
+        """Of the categorical distribution softmax(scale * logits) of every row of logits [rows][choices]
+        (fp32 or bf16; rows may be strided, -inf masks a choice): logp [rows] of the given choice [rows]
+        int32 (0 for a row whose choice is outside the range; None without choice), entropy [rows], the
+        `top` (up to 32) most likely alternatives top_choice [rows][top] int32 (-1 where there are
+        fewer) and their top_logp, and stats [rows][2] for choice_backward."""
+        import torch
+        self._enter()
+        C = self._choices(logits, top, scale)
+        n = C.rows
+        _check_tensor(choice, "choice", torch.int32, (n,), self.device)
+        if not 0 <= top <= MAX_TOP:
+            raise ValueError(f"top must be in [0, {MAX_TOP}]")
+        f32 = dict(dtype=torch.float32, device=logits.device)
+        held = torch.empty(n * (4 + top), **f32)            # one allocation: a call is short
+        logp, entropy, stats, top_logp = held.split([n, n, 2 * n, n * top])
+        top_choice = torch.empty((n, top), dtype=torch.int32, device=logits.device)
+        self._owned(held, top_choice, logits, choice)
+        self._check(self.lib.sagips_choice_logprob(
+            self.h, ctypes.byref(C), _ptr(choice), None if choice is None else logp.data_ptr(), entropy.data_ptr(),
+            top_choice.data_ptr() if top else None, top_logp.data_ptr() if top else None, stats.data_ptr()))
+        return {"logp": None if choice is None else logp, "entropy": entropy, "top_choice": top_choice,
+                "top_logp": top_logp.view(n, top), "stats": stats.view(n, 2)}
+
+    def choice_backward(self, logits, fwd: dict, choice=None, d_logp=None, d_entropy=None, d_top=None, scale: float = 1.0,
+                        out=None):
+        """dL/dlogits [rows][choices] in the logits' type, from what choice_logprob returned (fwd) for the
+        same logits, choice and scale, and the derivatives d_logp, d_entropy [rows], d_top [rows][top] of
+        the loss (None: not in it).  out may be the logits, and rows of it may be strided."""
+        import torch
+        self._enter()
+        f32, dev = torch.float32, self.device
+        top = 0 if d_top is None else fwd["top_choice"].shape[1]
+        C = self._choices(logits, top, scale)
+        n = C.rows
+        _check_tensor(choice, "choice", torch.int32, (n,), dev)
+        _check_tensor(d_logp, "d_logp", f32, (n,), dev)
+        _check_tensor(d_entropy, "d_entropy", f32, (n,), dev)
+        _check_tensor(d_top, "d_top", f32, (n, top), dev)
+        for name, shape, dtype in (("logp", (n,), f32), ("entropy", (n,), f32), ("stats", (n, 2), f32),
+                                   ("top_choice", (n, fwd["top_choice"].shape[1]), torch.int32)):
+            _check_tensor(fwd[name], f"fwd[{name!r}]", dtype, shape, dev)
+        if d_logp is not None and (choice is None or fwd["logp"] is None):
+            raise ValueError("d_logp needs the choice, in choice_logprob too")
+        o = out if out is not None else torch.empty((n, C.n_choices), dtype=logits.dtype, device=logits.device)
+        if o.dtype != logits.dtype or o.shape != logits.shape:
+            raise ValueError("out must have the logits' shape and type")
+        to = self._choices(o, top, scale)
+        g = ChoiceGrads(_ptr(choice), _ptr(fwd["logp"]), _ptr(fwd["entropy"]),
+                        fwd["top_choice"].data_ptr() if top else None, fwd["stats"].data_ptr(), _ptr(d_logp),
+                        _ptr(d_entropy), d_top.data_ptr() if top else None)
+        self._owned(o if out is None else None, logits, choice, d_logp, d_entropy, d_top,
+                    [fwd[k] for k in ("logp", "entropy", "stats", "top_choice")])
+        self._check(self.lib.sagips_choice_backward(self.h, ctypes.byref(C), ctypes.byref(g), o.data_ptr(), to.stride))
+        return o
+
+    def route(self, member, n_members: int) -> dict:
+        """Items sorted by the member that they are given to: of member [rows][slots] int32 (or [rows]; values
+        outside [0, n_members) give the item to none) the plan offsets [n_members + 1], order [rows * slots]
+        (the item row * slots + slot at each sorted position, then -1) and place [rows][slots] (each item's
+        sorted position, or -1), all int32."""
+        import torch
+        self._enter()
+        _check_tensor(member, "member", torch.int32, None, self.device)
+        if member.dim() not in (1, 2):
+            raise ValueError("member must be [rows][slots] or [rows]")
+        rows, slots = member.shape[0], member.shape[1] if member.dim() == 2 else 1
+        offsets = member.new_empty(int(n_members) + 1)
+        order, place = member.new_empty(rows * slots), member.new_empty(rows, slots)
+        self._owned(offsets, order, place, member)
+        self._check(self.lib.sagips_route(self.h, member.data_ptr(), rows, slots, int(n_members), offsets.data_ptr(),
+                                          order.data_ptr(), place.data_ptr()))
+        return {"offsets": offsets, "order": order, "place": place}
+
+    def _routed(self, plan, t, name, items: bool) -> Routed:
+        """The plan for rows like t, [rows][width] or (items) [rows * slots][width]."""
+        import torch
+        place = plan["place"]
+        _check_tensor(place, "place", torch.int32, None, self.device)
+        if place.dim() != 2:
+            raise ValueError("place must be [rows][slots]")
+        _check_tensor(t, name, None, None, self.device)
+        if t.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+        rows, slots = place.shape
+        want = rows * slots if items else rows
+        if t.dim() != 2 or t.shape[0] != want:
+            raise ValueError(f"{name} must be [{want}][width]")
+        return Routed(place.data_ptr(), rows, slots, t.shape[1], F32 if t.dtype == torch.float32 else BF16)
+
+    def dispatch(self, x, plan: dict, out=None):
+        """x [rows][width] (fp32 or bf16) laid out by member: out[place[r][k]] = x[r], [rows * slots][width].
+        Positions from plan["offsets"][-1] on are left as they were.  Its gradient is combine without
+        weights."""
+        self._enter()
+        R = self._routed(plan, x, "x", False)
+        shape = (R.rows * R.slots, R.width)
+        o = out if out is not None else x.new_empty(shape)
+        if out is not None:
+            _check_tensor(out, "out", x.dtype, shape, self.device)
+        self._owned(o if out is None else None, x, plan["place"])
+        self._check(self.lib.sagips_dispatch(self.h, ctypes.byref(R), x.data_ptr(), o.data_ptr()))
+        return o
+
+    def combine(self, y, plan: dict, weight=None, out=None):
+        """Rows put back: out[r] = sum_k weight[r][k] y[place[r][k]], [rows][width], of y [rows * slots][width]
+        (fp32 or bf16) and weight [rows][slots] fp32 (None: 1)."""
+        import torch
+        self._enter()
+        R = self._routed(plan, y, "y", True)
+        _check_tensor(weight, "weight", torch.float32, (R.rows, R.slots), self.device)
+        o = out if out is not None else y.new_empty((R.rows, R.width))
+        if out is not None:
+            _check_tensor(out, "out", y.dtype, (R.rows, R.width), self.device)
+        self._owned(o if out is None else None, y, weight, plan["place"])
+        self._check(self.lib.sagips_combine(self.h, ctypes.byref(R), y.data_ptr(), _ptr(weight), o.data_ptr()))
+        return o
+
+    def combine_backward(self, dout, y, plan: dict, weight=None, want_dweight: bool = True, dy=None):
+        """Gradient of combine: dy [rows * slots][width] (positions of no item are left as they were) and, if
+        wanted, dweight [rows][slots], which alone needs y."""
+        import torch
+        self._enter()
+        R = self._routed(plan, dout, "dout", False)
+        shape = (R.rows * R.slots, R.width)
+        if want_dweight and y is None:
+            raise ValueError("dweight needs y")
+        _check_tensor(y, "y", dout.dtype, shape, self.device)
+        _check_tensor(weight, "weight", torch.float32, (R.rows, R.slots), self.device)
+        g = dy if dy is not None else dout.new_empty(shape)
+        if dy is not None:
+            _check_tensor(dy, "dy", dout.dtype, shape, self.device)
+        dw = torch.empty((R.rows, R.slots), dtype=torch.float32, device=dout.device) if want_dweight else None
+        self._owned(g if dy is None else None, dw, dout, y, weight, plan["place"])
+        self._check(self.lib.sagips_combine_backward(self.h, ctypes.byref(R), dout.data_ptr(), _ptr(y) if want_dweight else None,
+                                                     _ptr(weight), g.data_ptr(), _ptr(dw)))
+        return g, dw
+
+    def gen_forward_routed(self, W: Sequence, b: Sequence, x, offsets, slope: float = 0.2, out=None):
+        """theta [n][out] = 1 + softplus(G_m(x)) with the member m that each row of x [n][in] belongs to:
+        offsets[m] .. offsets[m + 1] - 1 (route's, [n_members + 1] int32).  Rows of no member are left as
+        they were."""
+        import torch
+        self._enter()
+        g, M = self._gen(W, b, slope)
+        _check_tensor(x, "x", torch.float32, (x.shape[0], g.width[0]), self.device)
+        _check_tensor(offsets, "offsets", torch.int32, (M + 1,), self.device)
+        shape = (x.shape[0], g.width[g.n_layers])
+        th = out if out is not None else x.new_empty(shape)
+        if out is not None:
+            _check_tensor(out, "out", torch.float32, shape, self.device)
+        self._owned(th if out is None else None, W, b, x, offsets)
+        self._check(self.lib.sagips_gen_forward_routed(self.h, ctypes.byref(g), x.data_ptr(), offsets.data_ptr(), x.shape[0],
+                                                       th.data_ptr()))
+        return th
+
+    def gen_backward_routed(self, W: Sequence, b: Sequence, x, offsets, dL_dtheta, slope: float = 0.2, dW=None, db=None,
+                            want_dx: bool = False, dx=None):
+        """Gradients of sum <dL/dtheta, theta> for gen_forward_routed: (dW, db, dx) shaped like W, b and x;
+        dx (None unless wanted or given) keeps its rows of no member."""
+        import torch
+        self._enter()
+        g, M = self._gen(W, b, slope)
+        _check_tensor(x, "x", torch.float32, (x.shape[0], g.width[0]), self.device)
+        _check_tensor(offsets, "offsets", torch.int32, (M + 1,), self.device)
+        _check_tensor(dL_dtheta, "dL_dtheta", torch.float32, (x.shape[0], g.width[g.n_layers]), self.device)
+        new = []
+        if dW is None:
+            dW = [torch.empty_like(w) for w in W]
+            new += dW
+        if db is None:
+            db = [torch.empty_like(v) for v in b]
+            new += db
+        if dx is not None:
+            _check_tensor(dx, "dx", torch.float32, x.shape, self.device)
+        elif want_dx:
+            dx = torch.empty_like(x)
+            new.append(dx)
+        for l in range(g.n_layers):
+            _check_tensor(dW[l], f"dW[{l}]", torch.float32, tuple(W[l].shape), self.device)
+            _check_tensor(db[l], f"db[{l}]", torch.float32, tuple(b[l].shape), self.device)
+        self._owned(new, W, b, x, offsets, dL_dtheta)
+        pw = (ctypes.c_void_p * MAX_LAYERS)(*[t.data_ptr() for t in dW])
+        pb = (ctypes.c_void_p * MAX_LAYERS)(*[t.data_ptr() for t in db])
+        self._check(self.lib.sagips_gen_backward_routed(self.h, ctypes.byref(g), x.data_ptr(), offsets.data_ptr(), x.shape[0],
+                                                        dL_dtheta.data_ptr(), pw, pb, _ptr(dx)))
+        return dW, db, dx
 
 
 _default: Dict[int, Context] = {}

@@ -1,0 +1,622 @@
+// Choices from logits: log probabilities of given choices, entropy and the most
+// likely alternatives of a row, and their gradient.  With z = scale x over a row,
+// m = max z, s = sum exp(z - m):
+//   ln p_v = z_v - m - ln s,   H = ln s - (1/s) sum exp(z - m) (z - m),
+//   dL/dz_v = sum_i g_i ([v = c_i] - p_v) - g_H p_v (ln p_v + H).
+//
+// Forward: one pass over the logits, which stay in registers; a row is taken by
+// 2^k lanes, a wave, 256 or 1,024 threads, whatever holds it.  Every thread keeps
+// the maximum of its own values and sums relative to that; the waves' sums are
+// joined once.  The alternatives: the K-th largest of the threads' maxima is a
+// lower bound for the K-th largest value, and only K threads have values at or
+// above it, so those few are collected in LDS and ranked by counting.
+// Longer rows are read a second time for the collecting.
+#include "device_math.hpp"
+#include "kernels.hpp"
+#include "split_bf16.hpp"
+
+#include <type_traits>
+
+namespace sagips {
+namespace {
+
+constexpr int kMaxTop = SAGIPS_MAX_TOP;
+constexpr float kLowest = -INFINITY;
+constexpr uint32_t kMaskedKey = 0x007fffffu;   // order_key(-infinity)
+constexpr int kCandidates = 4096;              // of a row, in LDS
+
+struct ChoiceArgs {
+  const void* x;
+  int64_t rows, stride;
+  int n, top;
+  float scale, scale2;             // scale2 = scale log2 e
+  const int32_t* choice;
+  float *logp, *entropy;
+  int32_t* top_choice;
+  float *top_logp, *stats;
+};
+
+// Values of a 16-byte unit.
+template <class T>
+struct Unit;
+template <>
+struct Unit<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float get(const uint4& r, int j) { return __uint_as_float((&r.x)[j]); }
+};
+template <>
+struct Unit<u16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ float get(const uint4& r, int j) {
+    const uint32_t w = (&r.x)[j >> 1];
+    return j & 1 ? bf16_hi(w) : bf16_lo(w);
+  }
+};
+__device__ __forceinline__ uint32_t bits_of(float v) { return __float_as_uint(v); }
+__device__ __forceinline__ uint32_t bits_of(u16 v) { return v; }
+template <class T>
+constexpr uint32_t kFill = sizeof(T) == 4 ? 0xff800000u : 0xff80u;   // -infinity
+
+// A row in 16-byte units of memory, the first of which may begin before the row.
+// Value j of unit q is the row's q N + j - lead; values outside the row read as
+// -infinity, and nothing outside it is read.
+template <class T>
+struct RowView {
+  static constexpr int N = Unit<T>::N;
+  const char* base;
+  int lead, n;
+  __device__ __forceinline__ RowView(const void* x, int64_t off, int n_) : n(n_) {
+    const uintptr_t at = (uintptr_t)((const T*)x + off);
+    base = (const char*)(at & ~(uintptr_t)15);
+    lead = (int)((at & 15) / sizeof(T));
+  }
+  __device__ __forceinline__ int units() const { return (int)(((int64_t)n + lead + N - 1) / N); }
+  __device__ __forceinline__ int first(int q) const { return q * N - lead; }
+  __device__ __forceinline__ uint4 load(int q) const {
+    const int i0 = first(q);
+    const char* at = base + (int64_t)q * 16;
+    if (i0 >= 0 && i0 <= n - N) return *reinterpret_cast<const uint4*>(at);
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if constexpr (sizeof(T) == 4) {
+        w[k] = i0 + k >= 0 && i0 + k < n ? bits_of(((const T*)at)[k]) : kFill<T>;
+      } else {
+        const int i = i0 + 2 * k;
+        const uint32_t lo = i >= 0 && i < n ? bits_of(((const T*)at)[2 * k]) : kFill<T>;
+        const uint32_t hi = i + 1 >= 0 && i + 1 < n ? bits_of(((const T*)at)[2 * k + 1]) : kFill<T>;
+        w[k] = lo | hi << 16;
+      }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+
+// Order of candidates: the larger value first, of equal ones the lower index (as 64
+// bits, larger first).  +0 and -0 are equal.
+__device__ __forceinline__ uint32_t order_key(float v) {
+  const uint32_t u = __float_as_uint(v + 0.0f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float order_value(uint32_t k) {
+  return __uint_as_float(k ^ (k & 0x80000000u ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ uint64_t candidate(float v, int i) { return (uint64_t)order_key(v) << 32 | (0xffffffffu - (uint32_t)i); }
+__device__ __forceinline__ int candidate_index(uint64_t c) { return (int)(0xffffffffu - (uint32_t)c); }
+
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp_u(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xf, 0xf, true);
+}
+// Over groups of L lanes (a power of two), in every lane of the group.
+template <int L, class V, class F>
+__device__ __forceinline__ V group_reduce(V v, F f) {
+  const auto as = [](uint32_t u) { return __builtin_bit_cast(V, u); };
+  const auto un = [](V x) { return __builtin_bit_cast(uint32_t, x); };
+  if constexpr (L >= 2) v = f(v, as(dpp_u<0xB1>(un(v))));
+  if constexpr (L >= 4) v = f(v, as(dpp_u<0x1B>(un(v))));
+  if constexpr (L >= 8) v = f(v, as(dpp_u<0x141>(un(v))));
+  if constexpr (L >= 16) v = f(v, as(dpp_u<0x140>(un(v))));
+  if constexpr (L >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(un(v), un(v), false, false);
+    v = f(as(r[0]), as(r[1]));
+  }
+  if constexpr (L >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(un(v), un(v), false, false);
+    v = f(as(r[0]), as(r[1]));
+  }
+  return v;
+}
+template <int L>
+__device__ __forceinline__ float group_max(float v) {
+  return group_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+  return group_reduce<L>(v, [](float a, float b) { return a + b; });
+}
+template <int L>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  return group_reduce<L>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+// The first candidate of the group.
+template <int L>
+__device__ __forceinline__ uint64_t group_first(uint64_t c) {
+  const uint32_t hi = group_max<L>((uint32_t)(c >> 32));
+  const uint32_t lo = group_max<L>((uint32_t)(c >> 32) == hi ? (uint32_t)c : 0u);
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Sums of a part of a row: m its largest logit, s = sum 2^d, t = sum 2^d d with
+// d = (z - scale m) log2 e.  A part without choices has m = -infinity, s = t = 0.
+struct Sums {
+  float m, s, t;
+};
+// To a larger (or the same) m.
+__device__ __forceinline__ Sums shifted(Sums a, float m, const ChoiceArgs& p) {
+  const float d = (a.m - m) * p.scale2;              // NaN only where both are infinite
+  const float f = a.s == 0.0f ? 0.0f : fast_exp2(d);
+  return {m, a.s * f, f * fmaf(a.s, fmaxf(d, -300.0f), a.t)};   // f is 0 from -150 on: no 0 times infinity
+}
+
+// The largest of a unit's values, with those that the thread had before.
+template <class T>
+__device__ __forceinline__ float unit_max(const uint4& r, float m) {
+#pragma unroll
+  for (int j = 0; j < Unit<T>::N; ++j) m = fmaxf(m, Unit<T>::get(r, j));
+  return m;
+}
+template <class T>
+__device__ __forceinline__ void add_unit(const uint4& r, float ref, const ChoiceArgs& p, float& s, float& t) {
+#pragma unroll
+  for (int j = 0; j < Unit<T>::N; ++j) {
+    const float d = (Unit<T>::get(r, j) - ref) * p.scale2, e = fast_exp2(d);
+    s += e;
+    t = fmaf(e, fmaxf(d, -300.0f), t);
+  }
+}
+__device__ __forceinline__ float finite_or_0(float m) { return m == kLowest ? 0.0f : m; }
+
+// What a row's sums give: ln s, and the results that need nothing else.
+template <class T>
+__device__ __forceinline__ float write_row(const ChoiceArgs& p, int64_t row, const Sums& a) {
+  const float ls = logf(a.s);
+  if (p.stats) {
+    p.stats[2 * row] = finite_or_0(a.m);
+    p.stats[2 * row + 1] = ls;
+  }
+  if (p.entropy) p.entropy[row] = a.s == 0.0f ? 0.0f : ls - kLn2 * (a.t / a.s);
+  if (p.logp) {
+    const int c = p.choice[row];
+    float v = 0.0f;
+    if (c >= 0 && c < p.n) {
+      const T raw = ((const T*)p.x)[row * p.stride + c];
+      const float x = sizeof(T) == 4 ? __uint_as_float(bits_of(raw)) : __uint_as_float(bits_of(raw) << 16);
+      // a masked choice: -infinity, unless the row is NaN
+      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : fmaf(x - a.m, p.scale, -ls);
+    }
+    p.logp[row] = v;
+  }
+  return ls;
+}
+__device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int k, uint64_t c, const Sums& a, float ls) {
+  const int64_t at = row * p.top + k;
+  const bool nan = !(a.s >= 0.0f), none = (uint32_t)(c >> 32) <= kMaskedKey;
+  p.top_choice[at] = nan || none ? -1 : candidate_index(c);
+  p.top_logp[at] = nan ? a.s : none ? kLowest : fmaf(order_value((uint32_t)(c >> 32)) - a.m, p.scale, -ls);
+}
+
+// ---- short rows: L lanes each, one unit a lane ----------------------------------
+template <class T, int L>
+__global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
+  constexpr int N = Unit<T>::N;
+  const int l = threadIdx.x % L;
+  // whole groups leave: no exchange crosses them
+  for (int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L; row < p.rows; row += (int64_t)gridDim.x * (256 / L)) {
+    const RowView<T> v(p.x, row * p.stride, p.n);
+    const uint4 r = v.load(l);
+    const int i0 = v.first(l);
+    Sums a;
+    a.m = group_max<L>(unit_max<T>(r, kLowest));
+    float s = 0.0f, t = 0.0f;
+    add_unit<T>(r, finite_or_0(a.m), p, s, t);
+    a.s = group_sum<L>(s);
+    a.t = group_sum<L>(t);
+    if (l == 0) write_row<T>(p, row, a);
+    if (p.top == 0) continue;
+    const float ls = logf(a.s);
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = Unit<T>::get(r, j);
+    for (int k = 0; k < p.top; ++k) {
+      float best = kLowest;
+      int at = 0;
+#pragma unroll
+      for (int j = N - 1; j >= 0; --j)
+        if (x[j] >= best) best = x[j], at = j;       // of equal ones the lowest
+      const uint64_t first = group_first<L>(candidate(best, i0 + at));
+      const int taken = candidate_index(first) - i0;
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = j == taken ? kLowest : x[j];
+      if (l == k % L) write_top(p, row, k, first, a, ls);
+    }
+  }
+}
+
+// ---- a row a workgroup of TH threads, R units a thread and pass -------------------
+template <class T, int TH, int R, bool kOnePass>
+__global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
+  constexpr int N = Unit<T>::N, W = TH / 64;
+  static_assert(!kOnePass || R * N * kMaxTop <= kCandidates, "a row's candidates have to fit");
+  __shared__ Sums part[W];
+  __shared__ uint64_t firsts[W][kMaxTop];
+  __shared__ uint32_t held;
+  extern __shared__ uint64_t cand[];                 // kOnePass: top R N; else kCandidates
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const RowView<T> v(p.x, row * p.stride, p.n);
+    const int units = v.units();
+    const uint4 none = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);   // bf16 -infinity
+    const uint4 fill = sizeof(T) == 4 ? make_uint4(kFill<float>, kFill<float>, kFill<float>, kFill<float>) : none;
+    uint4 r[R];
+    Sums a{kLowest, 0.0f, 0.0f};
+    float best = kLowest;
+    int best_at = 0;
+    for (int q0 = 0; q0 < units; q0 += TH * R) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int q = q0 + i * TH + tid;
+        r[i] = q < units ? v.load(q) : fill;
+      }
+      float m = kLowest;
+#pragma unroll
+      for (int i = 0; i < R; ++i) m = unit_max<T>(r[i], m);
+      if (p.top && m > best) {
+        best = m;
+#pragma unroll
+        for (int i = R - 1; i >= 0; --i)
+#pragma unroll
+          for (int j = N - 1; j >= 0; --j)
+            if (Unit<T>::get(r[i], j) == m) best_at = v.first(q0 + i * TH + tid) + j;
+      }
+      m = fmaxf(m, a.m);
+      if constexpr (!kOnePass) a = shifted(a, m, p);
+      a.m = m;
+      const float ref = finite_or_0(m);
+#pragma unroll
+      for (int i = 0; i < R; ++i) add_unit<T>(r[i], ref, p, a.s, a.t);
+    }
+    a = shifted(a, group_max<64>(a.m), p);
+    a.s = group_sum<64>(a.s);
+    a.t = group_sum<64>(a.t);
+    if (lane == 0) part[wave] = a;
+    uint64_t mine = candidate(best, best_at);
+    if (p.top) {                                     // the wave's threads in order of their maxima
+      uint64_t c = mine;
+      for (int k = 0; k < p.top; ++k) {
+        const uint64_t first = group_first<64>(c);
+        if (lane == 0) firsts[wave][k] = first;
+        if (c == first) c = 0;
+      }
+      if (tid == 0) held = 0;
+    }
+    __syncthreads();
+    if constexpr (W > 1) {
+      float m = kLowest;
+#pragma unroll
+      for (int w = 0; w < W; ++w) m = fmaxf(m, part[w].m);
+      Sums all{m, 0.0f, 0.0f};
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        const Sums b = shifted(part[w], m, p);
+        all.s += b.s;
+        all.t += b.t;
+      }
+      a = all;
+    }
+    if (tid == 0) write_row<T>(p, row, a);
+    if (p.top) {
+      const float ls = logf(a.s);
+      // the top-th of the threads' maxima, by every wave from the waves' lists
+      uint64_t bound = firsts[0][p.top - 1];
+      if constexpr (W > 1) {
+        int at = 0;
+        uint64_t c = lane < W ? firsts[lane][0] : 0;
+        for (int k = 0; k < p.top; ++k) {
+          bound = group_first<64>(c);
+          if (lane < W && c == bound) c = ++at < p.top ? firsts[lane][at] : 0;
+        }
+      }
+      // fewer threads than alternatives have a choice: all that are not masked
+      if ((uint32_t)(bound >> 32) <= kMaskedKey) bound = (uint64_t)(kMaskedKey + 1) << 32 | 0x80000000u;
+      const float bound_x = order_value((uint32_t)(bound >> 32));
+      const int bound_i = candidate_index(bound);
+      const auto collect = [&](int q0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const int i0 = v.first(q0 + i * TH + tid);
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const float x = Unit<T>::get(r[i], j);
+            if (x >= bound_x && (x > bound_x || i0 + j <= bound_i)) {
+              const uint32_t at = atomicAdd(&held, 1u);
+              if (kOnePass || at < (uint32_t)kCandidates) cand[at] = candidate(x, i0 + j);
+            }
+          }
+        }
+      };
+      if (mine >= bound) {                             // a thread whose maximum is below has none
+        if constexpr (kOnePass) collect(0);
+        else
+          for (int q0 = 0; q0 < units; q0 += TH * R) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const int q = q0 + i * TH + tid;
+              r[i] = q < units ? v.load(q) : fill;
+            }
+            collect(q0);
+          }
+      }
+      __syncthreads();
+      const int n = (int)held;
+      if (kOnePass || n <= kCandidates) {
+        for (int i = tid; i < n; i += TH) {
+          const uint64_t c = cand[i];
+          int rank = 0;
+          for (int k = 0; k < n; ++k) rank += cand[k] > c;
+          if (rank < p.top) write_top(p, row, rank, c, a, ls);
+        }
+        for (int k = n + tid; k < p.top; k += TH) write_top(p, row, k, 0, a, ls);
+      } else {
+        // more than are held: one alternative a pass over the row
+        uint64_t last = ~0ull;
+        for (int k = 0; k < p.top; ++k) {
+          uint64_t c = 0;
+          for (int q = tid; q < units; q += TH) {
+            const uint4 u = v.load(q);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+              const uint64_t one = candidate(Unit<T>::get(u, j), v.first(q) + j);
+              if (one < last && one > c) c = one;
+            }
+          }
+          c = group_first<64>(c);
+          __syncthreads();
+          if (lane == 0) firsts[wave][0] = c;
+          __syncthreads();
+          c = group_first<64>(lane < W ? firsts[lane][0] : 0);
+          if (tid == 0) write_top(p, row, k, c, a, ls);
+          last = c;
+        }
+      }
+    }
+    __syncthreads();                                   // the next row's part, firsts and held
+  }
+}
+
+// ---- gradient ---------------------------------------------------------------------
+struct ChoiceGradArgs {
+  const void* x;
+  void* dx;
+  int64_t rows, stride, dstride;
+  int n, top;
+  float scale;
+  const int32_t *choice, *top_choice;
+  const float *logp, *entropy, *stats, *d_logp, *d_entropy, *d_top;
+  int chunks;                      // of a row
+};
+
+// Entry i of a row: 0 its choice, 1 .. top its alternatives.  c = -1: takes no part.
+__device__ __forceinline__ void grad_entry(const ChoiceGradArgs& p, int64_t row, int i, int& c, float& g) {
+  c = -1;
+  g = 0.0f;
+  if (i == 0) {
+    if (p.d_logp && p.logp[row] != kLowest) c = p.choice[row];
+  } else if (p.d_top && i <= p.top) {
+    c = p.top_choice[row * p.top + i - 1];
+  }
+  if (c < 0 || c >= p.n) c = -1;
+  else g = i == 0 ? p.d_logp[row] : p.d_top[row * p.top + i - 1];
+}
+
+// A unit of N values (one, where the two arrays' rows are not aligned alike) of a row.
+struct GradRow {
+  float shift, ls, a, gh, scale;
+  // scale p (a - gh ln p)
+  __device__ __forceinline__ float at(float x) const {
+    const float lp = fmaf(x - shift, scale, -ls), pr = x == kLowest ? 0.0f : fast_exp2(lp * kLog2e);
+    return pr * fmaf(-gh, fmaxf(lp, -200.0f), a);
+  }
+};
+__device__ __forceinline__ GradRow grad_row(const ChoiceGradArgs& p, int64_t row, float total) {
+  GradRow g;
+  g.shift = p.stats[2 * row];
+  g.ls = p.stats[2 * row + 1];
+  g.gh = p.d_entropy ? p.d_entropy[row] : 0.0f;
+  g.a = -total - (p.d_entropy ? g.gh * p.entropy[row] : 0.0f);
+  g.scale = p.scale;
+  return g;
+}
+
+template <class T>
+__device__ __forceinline__ T rounded(float v) {
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, v);
+  else return (T)pk_bf16(v, 0.0f);
+}
+// L lanes take a chunk of a row: a whole row where L is at most 64 (several rows a
+// wave), or L = 256 threads.  R units a lane.  kUnits: 16-byte units, the rows of both arrays being
+// aligned alike; otherwise single values.
+template <class T, int L, int R, bool kUnits>
+__global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
+  constexpr int N = kUnits ? Unit<T>::N : 1, P = 256 / L;
+  const int l = threadIdx.x % L, lane = threadIdx.x & 63;
+  const int64_t all = p.rows * p.chunks;
+  for (int64_t id = (int64_t)blockIdx.x * P + threadIdx.x / L; id < all; id += (int64_t)gridDim.x * P) {
+    const int64_t row = id / p.chunks;
+    const int q0 = (int)(id % p.chunks) * (L * R);
+    const RowView<T> v(p.x, row * p.stride, p.n);
+    const int lead = kUnits ? v.lead : 0;
+    const T* x = (const T*)p.x + row * p.stride;
+    T* dx = (T*)p.dx + row * p.dstride;
+    float val[R][N];
+    uint4 raw[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int q = q0 + i * L + l;
+      if constexpr (kUnits) {
+        if (q < v.units()) raw[i] = v.load(q);
+      } else {
+        raw[i].x = q < p.n ? bits_of(x[q]) : 0u;
+      }
+    }
+    int ec = -1;
+    float eg = 0.0f, total = 0.0f;
+    if constexpr (L >= 64) {                           // an entry a lane
+      if (lane <= p.top) grad_entry(p, row, lane, ec, eg);
+      total = group_sum<64>(eg);
+    } else {
+      for (int i = 0; i <= p.top; ++i) {
+        grad_entry(p, row, i, ec, eg);
+        total += eg;
+      }
+    }
+    const GradRow g = grad_row(p, row, total);
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if constexpr (kUnits) val[i][j] = g.at(Unit<T>::get(raw[i], j));
+        else if constexpr (sizeof(T) == 4) val[i][j] = g.at(__uint_as_float(raw[i].x));
+        else val[i][j] = g.at(__uint_as_float(raw[i].x << 16));
+      }
+    const auto add = [&](int c, float e) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int j0 = c - ((q0 + i * L + l) * N - lead);
+#pragma unroll
+        for (int j = 0; j < N; ++j) val[i][j] += j0 == j ? e : 0.0f;
+      }
+    };
+    if constexpr (L >= 64) {
+      // those in reach of the wave's units
+      const int from = (q0 + (int)(threadIdx.x % L) - lane) * N - lead, to = (q0 + (R - 1) * L + (int)(threadIdx.x % L) - lane + 64) * N - lead;
+      uint64_t on = __ballot(ec >= 0 && ec >= from && ec < to);
+      while (on) {
+        const int i = __ffsll((unsigned long long)on) - 1;
+        on &= on - 1;
+        add(__builtin_amdgcn_readlane(ec, i), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(eg), i)));
+      }
+    } else {
+      for (int i = 0; i <= p.top; ++i) {
+        grad_entry(p, row, i, ec, eg);
+        if (ec >= 0) add(ec, eg);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int q = q0 + i * L + l;
+      const int i0 = q * N - lead;
+#pragma unroll
+      for (int j = 0; j < N; ++j) val[i][j] *= p.scale;
+      if constexpr (kUnits) {
+        if (i0 >= 0 && i0 <= p.n - N) {
+          uint4 o;
+          if constexpr (sizeof(T) == 4) o = make_uint4(__float_as_uint(val[i][0]), __float_as_uint(val[i][1]), __float_as_uint(val[i][2]), __float_as_uint(val[i][3]));
+          else o = make_uint4(pk_bf16(val[i][0], val[i][1]), pk_bf16(val[i][2], val[i][3]), pk_bf16(val[i][4 % N], val[i][5 % N]), pk_bf16(val[i][6 % N], val[i][7 % N]));
+          *reinterpret_cast<uint4*>(dx + i0) = o;
+          continue;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (i0 + j >= 0 && i0 + j < p.n) dx[i0 + j] = rounded<T>(val[i][j]);
+    }
+  }
+}
+
+template <int n>
+using Int = std::integral_constant<int, n>;
+
+template <class T>
+hipError_t choice_forward(const ChoiceArgs& a, hipStream_t st) {
+  constexpr int N = Unit<T>::N;
+  // units a row has at most, wherever it begins
+  const bool aligned = ((uintptr_t)a.x & 15) == 0 && a.stride * sizeof(T) % 16 == 0;
+  const int64_t units = ((int64_t)a.n + (aligned ? N - 1 : 2 * N - 2)) / N;
+  const auto go_short = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    const int64_t blocks = (a.rows + 256 / L - 1) / (256 / L), most = 1 << 20;
+    hipLaunchKernelGGL((k_choice_short<T, L>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
+  };
+  const auto go_row = [&](auto threads, auto per, auto one) {
+    constexpr int TH = decltype(threads)::value, R = decltype(per)::value;
+    constexpr bool kOne = decltype(one)::value;
+    const size_t lds = a.top ? sizeof(uint64_t) * (kOne ? a.top * R * N : kCandidates) : 0;
+    const int64_t most = 256 * (int64_t)(2048 / TH) * 4;
+    hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), lds, st, a);
+  };
+  const std::true_type one{};
+  if (units <= 1) go_short(Int<1>{});
+  else if (units <= 2) go_short(Int<2>{});
+  else if (units <= 4) go_short(Int<4>{});
+  else if (units <= 8) go_short(Int<8>{});
+  else if (units <= 16) go_short(Int<16>{});
+  else if (units <= 32) go_short(Int<32>{});
+  else if (units <= 64) go_short(Int<64>{});
+  else if (units <= 64 * 2) go_row(Int<64>{}, Int<2>{}, one);
+  else if (units <= 64 * 4) go_row(Int<64>{}, Int<4>{}, one);
+  else if (units <= 64 * 8) go_row(Int<64>{}, Int<8>{}, one);
+  else if (units <= 256 * 4) go_row(Int<256>{}, Int<4>{}, one);
+  else if (units <= 256 * 8) go_row(Int<256>{}, Int<8>{}, one);
+  else if (units <= 1024 * 4) go_row(Int<1024>{}, Int<4>{}, one);
+  else if (units <= 1024 * 8) go_row(Int<1024>{}, Int<8>{}, one);
+  else if (units <= 1024 * 16) go_row(Int<1024>{}, Int<16>{}, one);
+  else go_row(Int<1024>{}, Int<8>{}, std::false_type{});
+  return hipGetLastError();
+}
+
+template <class T, bool kUnits>
+hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
+  constexpr int N = kUnits ? Unit<T>::N : 1;
+  const bool aligned = ((uintptr_t)a.x & 15) == 0 && a.stride * sizeof(T) % 16 == 0;
+  const int64_t units = ((int64_t)a.n + (aligned || N == 1 ? N - 1 : 2 * N - 2)) / N;
+  const auto go = [&](auto lanes, auto per) {
+    constexpr int L = decltype(lanes)::value, R = decltype(per)::value;
+    a.chunks = (int)((units + L * R - 1) / (L * R));
+    const int64_t blocks = (a.rows * a.chunks + 256 / L - 1) / (256 / L), most = 1 << 20;
+    hipLaunchKernelGGL((k_choice_grad<T, L, R, kUnits>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
+  };
+  if (units <= 4) go(Int<4>{}, Int<1>{});
+  else if (units <= 16) go(Int<16>{}, Int<1>{});
+  else if (units <= 64) go(Int<64>{}, Int<1>{});
+  else if (units <= 64 * 4) go(Int<64>{}, Int<4>{});
+  else go(Int<256>{}, Int<4>{});
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
+                         float* top_logp, float* stats, hipStream_t st, Timer* tm) {
+  ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)C.scale, (float)(C.scale * 1.4426950408889634),
+               choice, logp, entropy, top_choice, top_logp, stats};
+  if (tm) tm->begin("choice_logprob");
+  const hipError_t e = C.type == SAGIPS_BF16 ? choice_forward<u16>(a, st) : choice_forward<float>(a, st);
+  if (tm) tm->end();
+  return e;
+}
+
+hipError_t launch_choice_backward(const sagips_choices& C, const sagips_choice_grads& g, void* dlogits, int64_t dstride,
+                                  hipStream_t st, Timer* tm) {
+  ChoiceGradArgs a{C.logits, dlogits, C.rows, C.stride, dstride, C.n_choices, g.d_top ? C.top : 0, (float)C.scale,
+                   g.choice, g.top_choice, g.logp, g.entropy, g.stats, g.d_logp, g.d_entropy, g.d_top, 0};
+  const int size = C.type == SAGIPS_BF16 ? 2 : 4;
+  const bool alike = ((uintptr_t)C.logits - (uintptr_t)dlogits) % 16 == 0 && (C.rows == 1 || (C.stride - dstride) * size % 16 == 0);
+  if (tm) tm->begin("choice_backward");
+  const hipError_t e = C.type == SAGIPS_BF16 ? (alike ? choice_grad<u16, true>(a, st) : choice_grad<u16, false>(a, st))
+                                             : (alike ? choice_grad<float, true>(a, st) : choice_grad<float, false>(a, st));
+  if (tm) tm->end();
+  return e;
+}
+
+}  // namespace sagips

@@ -76,7 +76,87 @@ struct GenParams {
   float* part;                     // backward: [M][tiles][P]
   int64_t P;                       // floats per partial (all parameters of one member)
   int64_t poff_w[kMaxGenLayers], poff_b[kMaxGenLayers];
+  // Members on rows of their own: noise, theta and dtheta are [k][..], of which member m has rows
+  // offsets[m] .. offsets[m + 1] - 1.
+  const int32_t* offsets;
+  int members;
+  float* dx;                       // backward: dL/dnoise [k][in], or NULL
 };
+
+// The rows of a tile: first, the first behind the member's rows, and what is added to a row for
+// its place in theta.
+struct GenTile {
+  int m;
+  int64_t row0, end, base;
+};
+
+// Member m's rows, whatever the offsets hold, lie within [0, k].
+__device__ __forceinline__ void member_rows(const GenParams& p, int m, int64_t& lo, int64_t& hi) {
+  lo = min(max((int64_t)p.offsets[m], (int64_t)0), p.k);
+  hi = min(max((int64_t)p.offsets[m + 1], lo), p.k);
+}
+
+// Tiles of T rows of the members before `until`; and tile `want` of all (false: there are fewer).
+// A member a lane, 64 at a time; the whole wave calls it.
+template <int T>
+__device__ __forceinline__ int64_t tiles_until(const GenParams& p, int until) {
+  const int lane = threadIdx.x & 63;
+  int64_t n = 0;
+  for (int m0 = 0; m0 < until; m0 += 64) {
+    int64_t lo = 0, hi = 0;
+    if (m0 + lane < until) member_rows(p, m0 + lane, lo, hi);
+    uint32_t t = (uint32_t)((hi - lo + T - 1) / T);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) t += (uint32_t)__shfl_xor((int)t, d, 64);
+    n += t;
+  }
+  return n;
+}
+template <int T>
+__device__ __forceinline__ bool routed_tile(const GenParams& p, int64_t want, GenTile& out) {
+  const int lane = threadIdx.x & 63;
+  int64_t before = 0;
+  for (int m0 = 0; m0 < p.members; m0 += 64) {
+    int64_t lo = 0, hi = 0;
+    if (m0 + lane < p.members) member_rows(p, m0 + lane, lo, hi);
+    const uint32_t t = (uint32_t)((hi - lo + T - 1) / T);   // 64 of them below 2^32: fewer than 2^29 rows
+    uint32_t upto = t;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+      if (lane >= d) upto += o;
+    }
+    const uint64_t past = __ballot(before + upto > want);
+    if (past) {
+      const int src = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+      out.m = m0 + src;
+      lo = __builtin_amdgcn_readlane((int)lo, src);
+      hi = __builtin_amdgcn_readlane((int)hi, src);
+      out.row0 = lo + (want - before - (uint32_t)__builtin_amdgcn_readlane((int)(upto - t), src)) * T;
+      out.end = hi;
+      out.base = 0;
+      return true;
+    }
+    before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+  }
+  return false;
+}
+
+// Tile of this workgroup.  Routed: the grid may hold more workgroups than there are tiles, and is a
+// multiple of 8; an XCD (workgroup mod 8) takes tiles that follow each other.
+template <int T, bool kRouted>
+__device__ __forceinline__ bool gen_tile(const GenParams& p, GenTile& t) {
+  if constexpr (kRouted) {
+    return routed_tile<T>(p, (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), t);
+  } else {
+    int tile;
+    gen_block(gridDim.x, gridDim.y, t.m, tile);
+    t.row0 = (int64_t)tile * T;
+    t.end = p.k;
+    t.base = (int64_t)t.m * p.k;
+    return true;
+  }
+}
 
 template <int H, int NH, int kGT>
 struct Gen {
@@ -134,17 +214,17 @@ struct Gen {
     }
   }
 
-  // Forward pass of member m on rows [row0, row0 + 64) into LDS; rows past k
+  // Forward pass of member m on rows [row0, row0 + 64) into LDS; rows from end on
   // carry zero noise.  Leaves A_1..A_{NH+1} in act and the last layer's
   // pre-activation in o.
-  static __device__ void forward(const GenParams& p, Smem& sm, int m, int64_t row0) {
+  static __device__ void forward(const GenParams& p, Smem& sm, int m, int64_t row0, int64_t end) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int lr = lane & 15, lg = lane >> 4;
     const float slope = p.slope;
     for (int i = tid; i < kGT * kGMaxIO; i += kGThreads) {
       const int ev = i / kGMaxIO, j = i % kGMaxIO;
       const int64_t r = row0 + ev;
-      sm.n[ev][j] = (j < p.in && r < p.k) ? p.noise[r * p.in + j] : 0.0f;
+      sm.n[ev][j] = (j < p.in && r < end) ? p.noise[r * p.in + j] : 0.0f;
     }
     __syncthreads();
     {   // first layer: thread (feature o, part) over rows part, part + PPO, ...
@@ -200,36 +280,68 @@ struct Gen {
     __syncthreads();
   }
 
+  template <bool kRouted>
   static __device__ void run_forward(const GenParams& p) {
     __shared__ Smem sm;
-    int m, tile;
-    gen_block(gridDim.x, gridDim.y, m, tile);
-    const int64_t row0 = (int64_t)tile * kGT;
-    forward(p, sm, m, row0);
+    GenTile t;
+    if (!gen_tile<kGT, kRouted>(p, t)) return;
+    forward(p, sm, t.m, t.row0, t.end);
     for (int i = threadIdx.x; i < kGT * p.out; i += kGThreads) {
       const int ev = i / p.out, j = i % p.out;
-      const int64_t r = row0 + ev;
-      if (r < p.k) p.theta[((int64_t)m * p.k + r) * p.out + j] = 1.0f + g_softplus(sm.o[ev][j]);
+      const int64_t r = t.row0 + ev;
+      if (r < t.end) p.theta[(t.base + r) * p.out + j] = 1.0f + g_softplus(sm.o[ev][j]);
     }
   }
 
   static __device__ void run_backward(const GenParams& p) {
     __shared__ Smem sm;
+    GenTile t;
+    int tile;
+    gen_block(gridDim.x, gridDim.y, t.m, tile);
+    t.row0 = (int64_t)tile * kGT;
+    t.end = p.k;
+    t.base = (int64_t)t.m * p.k;
+    backward_tile<false>(p, sm, t, p.part + ((int64_t)t.m * gridDim.x + tile) * p.P, false);
+  }
+
+  // Of the `tiles` tiles in the order of their rows, workgroup g of `groups` (at most one a tile) takes
+  // those from g tiles / groups on, and adds up what it has of a member in slot g + m of the
+  // partials: g + m rises from each of its (g, m) to the next.
+  static __device__ void run_backward_routed(const GenParams& p) {
+    __shared__ Smem sm;
+    const int64_t tiles = tiles_until<kGT>(p, p.members);
+    const int64_t groups = min(tiles, (int64_t)gridDim.x);
+    const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (g >= groups) return;
+    int last = -1;
+    for (int64_t i = g * tiles / groups; i < (g + 1) * tiles / groups; ++i) {
+      GenTile t;
+      if (!routed_tile<kGT>(p, i, t)) return;        // (there is one)
+      __syncthreads();                               // the tile before is read
+      backward_tile<true>(p, sm, t, p.part + (g + t.m) * p.P, t.m == last);
+      last = t.m;
+    }
+  }
+
+  // The gradients of a tile to `part`, or added to what it holds.
+  template <bool kRouted>
+  static __device__ __forceinline__ void backward_tile(const GenParams& p, Smem& sm, const GenTile& t, float* part, bool more) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int lr = lane & 15, lg = lane >> 4;
-    int m, tile;
-    gen_block(gridDim.x, gridDim.y, m, tile);
-    const int64_t row0 = (int64_t)tile * kGT;
+    const int m = t.m;
     const float slope = p.slope;
-    forward(p, sm, m, row0);
-    float* part = p.part + ((int64_t)m * gridDim.x + tile) * p.P;
+    const auto put = [&](float* at, float v) __attribute__((always_inline)) {
+      if constexpr (kRouted) *at = more ? *at + v : v;
+      else *at = v;
+    };
+    forward(p, sm, m, t.row0, t.end);
 
-    // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past k
+    // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
     for (int i = tid; i < kGT * kGMaxIO; i += kGThreads) {
       const int ev = i / kGMaxIO, j = i % kGMaxIO;
-      const int64_t r = row0 + ev;
+      const int64_t r = t.row0 + ev;
       float d = 0.f;
-      if (j < p.out && r < p.k) d = p.dtheta[((int64_t)m * p.k + r) * p.out + j] * g_sigmoid(sm.o[ev][j]);
+      if (j < p.out && r < t.end) d = p.dtheta[(t.base + r) * p.out + j] * g_sigmoid(sm.o[ev][j]);
       sm.dout[ev][j] = d;
     }
     __syncthreads();
@@ -240,12 +352,12 @@ struct Gen {
       for (int j = g; j < p.out; j += PPO) {
         float s = 0.f;
         for (int ev = 0; ev < kGT; ++ev) s = fmaf(sm.dout[ev][j], sm.act[NH][ev][k], s);
-        part[p.poff_w[L] + j * H + k] = s;
+        put(part + p.poff_w[L] + j * H + k, s);
       }
       if (tid < p.out) {
         float s = 0.f;
         for (int ev = 0; ev < kGT; ++ev) s += sm.dout[ev][tid];
-        part[p.poff_b[L] + tid] = s;
+        put(part + p.poff_b[L] + tid, s);
       }
     }
     __syncthreads();
@@ -284,11 +396,11 @@ struct Gen {
 #pragma unroll
         for (int nb = 0; nb < KB; ++nb)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dW[(o0 + 4 * lg + r) * H + 16 * nb + lr] = acc[nb][r];
+          for (int r = 0; r < 4; ++r) put(dW + (o0 + 4 * lg + r) * H + 16 * nb + lr, acc[nb][r]);
         if (tid < H) {
           float s = 0.f;
           for (int ev = 0; ev < kGT; ++ev) s += dl[ev * LD + tid];
-          part[p.poff_b[1 + l] + tid] = s;
+          put(part + p.poff_b[1 + l] + tid, s);
         }
       }
       __syncthreads();   // delta_{l+1} overwrites A_{l+1}, which every wave just read
@@ -311,12 +423,24 @@ struct Gen {
       for (int j = g; j < p.in; j += PPO) {
         float s = 0.f;
         for (int ev = 0; ev < kGT; ++ev) s = fmaf(sm.act[0][ev][o], sm.n[ev][j], s);
-        part[p.poff_w[0] + o * p.in + j] = s;
+        put(part + p.poff_w[0] + o * p.in + j, s);
       }
       if (g == 0) {
         float s = 0.f;
         for (int ev = 0; ev < kGT; ++ev) s += sm.act[0][ev][o];
-        part[p.poff_b[0] + o] = s;
+        put(part + p.poff_b[0] + o, s);
+      }
+    }
+    if constexpr (kRouted) {   // dx[ev][j] = sum_o delta_1[ev][o] W_0[o][j]
+      if (p.dx) {
+        const float* W0 = p.W[0] + m * p.wsz[0];
+        for (int i = tid; i < kGT * p.in; i += kGThreads) {
+          const int ev = i / p.in, j = i % p.in;
+          float s = 0.f;
+#pragma unroll 8
+          for (int o = 0; o < H; ++o) s = fmaf(sm.act[0][ev][o], W0[o * p.in + j], s);
+          if (t.row0 + ev < t.end) p.dx[(t.row0 + ev) * p.in + j] = s;
+        }
       }
     }
   }
@@ -327,9 +451,14 @@ __global__ __launch_bounds__(kGThreads, 1) void k_gen_backward(GenParams p) {
   Gen<H, NH, T>::run_backward(p);
 }
 
-template <int H, int NH>
+template <int H, int NH, int T>
+__global__ __launch_bounds__(kGThreads, 1) void k_gen_backward_routed(GenParams p) {
+  Gen<H, NH, T>::run_backward_routed(p);
+}
+
+template <int H, int NH, bool kRouted>
 __global__ __launch_bounds__(kGThreads, 1) void k_gen_forward16(GenParams p) {
-  Gen<H, NH, 16>::run_forward(p);
+  Gen<H, NH, 16>::template run_forward<kRouted>(p);
 }
 
 // Forward pass on the bf16 matrix cores, H = 128.  Wave w owns features [32 w,
@@ -436,18 +565,20 @@ struct GenFwd : SplitLds<128, 64> {
     }
   }
 
+  template <bool kRouted>
   static __device__ void run(const GenParams& p) {
     __shared__ __attribute__((aligned(1024))) Smem sm;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Lane L = make_lane(wave, 0);
-    int m, tile;
-    gen_block(gridDim.x, gridDim.y, m, tile);
-    const int64_t row0 = (int64_t)tile * R;
+    GenTile at;
+    if (!gen_tile<R, kRouted>(p, at)) return;
+    const int m = at.m;
+    const int64_t row0 = at.row0;
     const float slope = p.slope;
     for (int i = tid; i < R * kGMaxIO; i += kFwdThreads) {
       const int ev = i % R, j = i / R;
       const int64_t r = row0 + ev;
-      sm.n[j][ev] = (j < p.in && r < p.k) ? p.noise[r * p.in + j] : 0.0f;
+      sm.n[j][ev] = (j < p.in && r < at.end) ? p.noise[r * p.in + j] : 0.0f;
     }
     __syncthreads();
     if (p.in <= 6) first_layer<6>(p, sm, m, L);
@@ -510,14 +641,14 @@ struct GenFwd : SplitLds<128, 64> {
       float o = p.b[NH + 1][m * p.bsz[NH + 1] + j];
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) o += sm.op[w][j][ev];
-      if (r < p.k) p.theta[((int64_t)m * p.k + r) * p.out + j] = 1.0f + g_softplus(o);
+      if (r < at.end) p.theta[(at.base + r) * p.out + j] = 1.0f + g_softplus(o);
     }
   }
 };
 
-template <int NH>
+template <int NH, bool kRouted>
 __global__ __launch_bounds__(kFwdThreads, 3) void k_gen_forward(GenParams p) {
-  GenFwd<NH>::run(p);
+  GenFwd<NH>::template run<kRouted>(p);
 }
 
 // Sum of the per-tile partials of member blockIdx.y in a fixed order, scattered
@@ -571,6 +702,40 @@ __global__ __launch_bounds__(256) void k_gen_reduce(GenReduceArgs r) {
     for (int q = 0; q < S; ++q) v += red[q][le];
   }
   if (e >= r.P) return;
+  for (int l = 0; l < r.n_layers; ++l) {
+    if (e >= r.poff_w[l] && e < r.poff_w[l] + r.wsz[l]) { r.dW[l][m * r.wsz[l] + (e - r.poff_w[l])] = v; return; }
+    if (e >= r.poff_b[l] && e < r.poff_b[l] + r.bsz[l]) { r.db[l][m * r.bsz[l] + (e - r.poff_b[l])] = v; return; }
+  }
+}
+
+// The same for k_gen_backward_routed: member blockIdx.y's partials are the slots g + m of the workgroups
+// g that had tiles of it, in their order.
+template <int T>
+__global__ __launch_bounds__(256) void k_gen_reduce_routed(GenReduceArgs r, GenParams p, int grid) {
+  constexpr int S = 4, C = 256 / S;
+  __shared__ float red[S][C];
+  const int m = blockIdx.y;
+  const int64_t all = tiles_until<T>(p, p.members), t0 = tiles_until<T>(p, m), t1 = tiles_until<T>(p, m + 1);
+  const int64_t groups = min(all, (int64_t)grid);
+  // tile t is workgroup ((t + 1) groups - 1) / all's
+  const int64_t g0 = t1 > t0 ? ((t0 + 1) * groups - 1) / all : 0;
+  const int n = t1 > t0 ? (int)min((t1 * groups - 1) / all - g0 + 1, groups - g0) : 0;
+  const int le = threadIdx.x % C, sl = threadIdx.x / C;
+  const int64_t e = (int64_t)blockIdx.x * C + le;
+  float v = 0.f;
+  if (e < r.P) {
+    const float* src = r.part + (g0 + m) * r.P + e;
+    int t = sl;
+    for (; t + 4 * S < n; t += 8 * S) add_tiles<S, 8>(src, t, n, r.P, v);
+    if (t + 2 * S < n) add_tiles<S, 4>(src, t, n, r.P, v);
+    else if (t < n) add_tiles<S, 2>(src, t, n, r.P, v);
+  }
+  red[sl][le] = v;
+  __syncthreads();
+  if (sl != 0 || e >= r.P) return;
+  v = 0.f;
+#pragma unroll
+  for (int q = 0; q < S; ++q) v += red[q][le];
   for (int l = 0; l < r.n_layers; ++l) {
     if (e >= r.poff_w[l] && e < r.poff_w[l] + r.wsz[l]) { r.dW[l][m * r.wsz[l] + (e - r.poff_w[l])] = v; return; }
     if (e >= r.poff_b[l] && e < r.poff_b[l] + r.bsz[l]) { r.db[l][m * r.bsz[l] + (e - r.poff_b[l])] = v; return; }
@@ -673,12 +838,16 @@ struct GenVariant {
   int H, NH;
   void (*fwd[2])(GenParams);   // 64-row, 16-row tiles
   void (*bwd[2])(GenParams);
+  void (*fwd_routed[2])(GenParams);
+  void (*bwd_routed[2])(GenParams);
 };
 
 #define SAGIPS_GEN_VARIANT(H_, NH_)                                               \
   {                                                                              \
-    H_, NH_, {k_gen_forward<NH_>, k_gen_forward16<H_, NH_>},                     \
-        {k_gen_backward<H_, NH_, 64>, k_gen_backward<H_, NH_, 16> }              \
+    H_, NH_, {k_gen_forward<NH_, false>, k_gen_forward16<H_, NH_, false>},       \
+        {k_gen_backward<H_, NH_, 64>, k_gen_backward<H_, NH_, 16> },             \
+        {k_gen_forward<NH_, true>, k_gen_forward16<H_, NH_, true>},              \
+        {k_gen_backward_routed<H_, NH_, 64>, k_gen_backward_routed<H_, NH_, 16> } \
   }
 
 const GenVariant kGenVariants[] = {SAGIPS_GEN_VARIANT(128, 1), SAGIPS_GEN_VARIANT(128, 2), SAGIPS_GEN_VARIANT(128, 3)};
@@ -711,6 +880,24 @@ GenParams gen_params(const sagips_gen& G, const float* noise, int64_t k) {
   p.slope = G.leaky_slope;
   p.noise = noise;
   return p;
+}
+
+GenReduceArgs reduce_args(const sagips_gen& G, const GenParams& p, int tiles, float* const* dW, float* const* db) {
+  GenReduceArgs r;
+  memset(&r, 0, sizeof(r));
+  r.part = p.part;
+  r.P = p.P;
+  r.tiles = tiles;
+  r.n_layers = G.n_layers;
+  for (int l = 0; l < G.n_layers; ++l) {
+    r.poff_w[l] = p.poff_w[l];
+    r.poff_b[l] = p.poff_b[l];
+    r.wsz[l] = p.wsz[l];
+    r.bsz[l] = p.bsz[l];
+    r.dW[l] = dW[l];
+    r.db[l] = db[l];
+  }
+  return r;
 }
 
 // Row tile: 64, unless 64-row tiles of all members would not cover the CUs.
@@ -769,23 +956,68 @@ hipError_t launch_gen_backward(const sagips_gen& G, const float* noise, int64_t 
   if (tm) tm->end();
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  GenReduceArgs r;
-  memset(&r, 0, sizeof(r));
-  r.part = p.part;
-  r.P = p.P;
-  r.tiles = tiles;
-  r.n_layers = G.n_layers;
-  for (int l = 0; l < G.n_layers; ++l) {
-    r.poff_w[l] = p.poff_w[l];
-    r.poff_b[l] = p.poff_b[l];
-    r.wsz[l] = p.wsz[l];
-    r.bsz[l] = p.bsz[l];
-    r.dW[l] = dW[l];
-    r.db[l] = db[l];
-  }
+  const GenReduceArgs r = reduce_args(G, p, tiles, dW, db);
   if (tm) tm->begin("gen_reduce");
   if (tiles <= 4) hipLaunchKernelGGL(k_gen_reduce<1>, dim3((unsigned)((p.P + 255) / 256), G.n_members), dim3(256), 0, st, r);
   else hipLaunchKernelGGL(k_gen_reduce<4>, dim3((unsigned)((p.P + 63) / 64), G.n_members), dim3(256), 0, st, r);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+// Members on rows of their own: tiles of 64 rows where those alone would cover half of the
+// compute units.
+namespace {
+inline int routed_rows(int64_t k, int n_cu) { return k / 64 >= n_cu / 2 ? 64 : 16; }
+// Tiles at most: every member's last one may be partly filled.
+inline int64_t routed_tiles(const sagips_gen& G, int64_t k, int T) { return k / T + (G.n_members < k ? G.n_members : k); }
+// Workgroups of the backward pass, a multiple of 8.
+inline int routed_groups(const sagips_gen& G, int64_t k, int T, int n_cu) {
+  const int64_t t = routed_tiles(G, k, T), most = (n_cu + 7) / 8 * 8;
+  return (int)(t < most ? (t + 7) / 8 * 8 : most);
+}
+}  // namespace
+
+size_t gen_backward_routed_workspace(const sagips_gen& G, int64_t k, int n_cu) {
+  const GenParams p = gen_params(G, nullptr, k);
+  return sizeof(float) * (size_t)p.P * (routed_groups(G, k, routed_rows(k, n_cu), n_cu) + G.n_members);
+}
+
+hipError_t launch_gen_forward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k, float* theta,
+                                     int n_cu, hipStream_t st, Timer* tm) {
+  GenParams p = gen_params(G, x, k);
+  p.theta = theta;
+  p.offsets = offsets;
+  p.members = G.n_members;
+  const GenVariant* v = find_gen(G);
+  const int T = routed_rows(k, n_cu);
+  if (tm) tm->begin("gen_forward_routed");
+  hipLaunchKernelGGL(v->fwd_routed[T == 64 ? 0 : 1], dim3((unsigned)((routed_tiles(G, k, T) + 7) / 8 * 8)),
+                     dim3(T == 64 ? kFwdThreads : kGThreads), 0, st, p);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k,
+                                      const float* dtheta, float* const* dW, float* const* db, float* dx, void* ws, int n_cu,
+                                      hipStream_t st, Timer* tm) {
+  GenParams p = gen_params(G, x, k);
+  p.dtheta = dtheta;
+  p.part = static_cast<float*>(ws);
+  p.offsets = offsets;
+  p.members = G.n_members;
+  p.dx = dx;
+  const GenVariant* v = find_gen(G);
+  const int T = routed_rows(k, n_cu), groups = routed_groups(G, k, T, n_cu);
+  if (tm) tm->begin("gen_backward_routed");
+  hipLaunchKernelGGL(v->bwd_routed[T == 64 ? 0 : 1], dim3(groups), dim3(kGThreads), 0, st, p);
+  if (tm) tm->end();
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const GenReduceArgs r = reduce_args(G, p, 0, dW, db);
+  const dim3 grid((unsigned)((p.P + 63) / 64), G.n_members);
+  if (tm) tm->begin("gen_reduce_routed");
+  if (T == 64) hipLaunchKernelGGL(k_gen_reduce_routed<64>, grid, dim3(256), 0, st, r, p, groups);
+  else hipLaunchKernelGGL(k_gen_reduce_routed<16>, grid, dim3(256), 0, st, r, p, groups);
   if (tm) tm->end();
   return hipGetLastError();
 }

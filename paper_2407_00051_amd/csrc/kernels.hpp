@@ -89,6 +89,29 @@ hipError_t launch_gen_backward(const sagips_gen& G, const float* noise, int64_t 
 hipError_t launch_ensemble(const sagips_gen& G, const float* noise, int64_t k, const float* p_true, float* p_hat,
                            float* sigma, float* r_hat, void* ws, int n_cu, hipStream_t st, Timer* tm);
 
+// Members on rows of their own (offsets on the device).
+size_t gen_backward_routed_workspace(const sagips_gen& G, int64_t k, int n_cu);
+hipError_t launch_gen_forward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k, float* theta,
+                                     int n_cu, hipStream_t st, Timer* tm);
+hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k,
+                                      const float* dtheta, float* const* dW, float* const* db, float* dx, void* ws, int n_cu,
+                                      hipStream_t st, Timer* tm);
+
+// choice.hip -----------------------------------------------------------------
+hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
+                         float* top_logp, float* stats, hipStream_t st, Timer* tm);
+hipError_t launch_choice_backward(const sagips_choices& C, const sagips_choice_grads& g, void* dlogits, int64_t dstride,
+                                  hipStream_t st, Timer* tm);
+
+// route.hip ------------------------------------------------------------------
+size_t route_workspace(int64_t items, int members);
+hipError_t launch_route(const int32_t* member, int64_t items, int members, int32_t* offsets, int32_t* order, int32_t* place,
+                        void* ws, hipStream_t st, Timer* tm);
+hipError_t launch_dispatch(const sagips_routed& R, const void* x, void* sorted, hipStream_t st, Timer* tm);
+hipError_t launch_combine(const sagips_routed& R, const void* y, const float* weight, void* out, hipStream_t st, Timer* tm);
+hipError_t launch_combine_backward(const sagips_routed& R, const void* dout, const void* y, const float* weight, void* dy,
+                                   float* dweight, hipStream_t st, Timer* tm);
+
 // optim.hip ------------------------------------------------------------------
 hipError_t launch_adam(const sagips_param_set& ps, int step, double lr, double beta1, double beta2, double eps,
                        hipStream_t st, Timer* tm);

@@ -1,0 +1,385 @@
+// Rows sorted by the member that they are given to, and back.
+//   route     a stable counting sort of rows * slots items by member: offsets, the
+//             item at each sorted position, and each item's position
+//   dispatch  sorted[place[r][k]] = x[r]
+//   combine   out[r] = sum_k w[r][k] y[place[r][k]], and its gradient
+// Positions outside the sorted rows are never followed.
+#include "device_math.hpp"
+#include "kernels.hpp"
+#include "split_bf16.hpp"
+
+#include <type_traits>
+
+namespace sagips {
+namespace {
+
+// ---- route ------------------------------------------------------------------------
+// A workgroup of 16 waves takes `per` items, wave w the w-th part of them in order.  A
+// wave counts its members in LDS, then walks its items again: an item's position is
+// the member's first of the wave, plus the lanes before it with the same member (a ballot a
+// bit of the member).  Beyond one workgroup the counts come from a launch before.
+constexpr int kRouteThreads = 1024, kRouteWaves = 16, kRouteMembers = 1024;
+
+struct RouteArgs {
+  const int32_t* member;
+  int n, members, per;
+  int bits;                        // of members - 1
+  int32_t *offsets, *order, *place;
+  uint32_t* counts;                // [workgroups][members]
+};
+
+// Lanes with the same m as this one (of those that are on).
+__device__ __forceinline__ uint64_t same_lanes(uint32_t m, bool on, int bits) {
+  uint64_t peers = __ballot(on);
+  for (int b = 0; b < bits; ++b) {
+    const bool set = m >> b & 1;
+    const uint64_t with = __ballot(set);
+    peers &= set ? with : ~with;
+  }
+  return peers;
+}
+
+struct WaveItems {
+  int lo, hi;                      // of the wave
+};
+__device__ __forceinline__ WaveItems wave_items(const RouteArgs& p, int block, int wave) {
+  const int64_t b0 = (int64_t)block * p.per, b1 = min(b0 + p.per, (int64_t)p.n);
+  const int each = (p.per + kRouteWaves * 64 - 1) / (kRouteWaves * 64) * 64;
+  const int64_t lo = min(b0 + (int64_t)wave * each, b1), hi = min(lo + each, b1);
+  return {(int)lo, (int)hi};
+}
+
+// counts[wave][m] of the workgroup's items; all zero before.
+__device__ __forceinline__ void count_items(const RouteArgs& p, const WaveItems& w, uint32_t* counts) {
+  for (int i = w.lo + (int)(threadIdx.x & 63); i < w.hi; i += 64) {
+    const uint32_t m = (uint32_t)p.member[i];
+    if (m < (uint32_t)p.members) atomicAdd(counts + m, 1u);
+  }
+}
+
+__global__ __launch_bounds__(kRouteThreads) void k_route_count(RouteArgs p) {
+  __shared__ uint32_t counts[kRouteMembers];
+  for (int m = threadIdx.x; m < p.members; m += kRouteThreads) counts[m] = 0;
+  __syncthreads();
+  count_items(p, wave_items(p, blockIdx.x, threadIdx.x >> 6), counts);
+  __syncthreads();
+  for (int m = threadIdx.x; m < p.members; m += kRouteThreads) p.counts[(int64_t)blockIdx.x * p.members + m] = counts[m];
+}
+
+__global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs p) {
+  __shared__ uint32_t next[kRouteWaves * kRouteMembers];   // [wave][members]: the next position
+  __shared__ uint32_t sums[kRouteWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool alone = gridDim.x == 1;
+  for (int i = tid; i < kRouteWaves * p.members; i += kRouteThreads) next[i] = 0;
+  __syncthreads();
+  const WaveItems w = wave_items(p, blockIdx.x, wave);
+  count_items(p, w, next + wave * p.members);
+  __syncthreads();
+  // thread m: member m's items in the workgroups before, in all, and in this one's waves
+  uint32_t before = 0, total = 0;
+  if (tid < p.members) {
+    if (alone) {
+      for (int v = 0; v < kRouteWaves; ++v) total += next[v * p.members + tid];
+    } else {
+#pragma unroll 8
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        const uint32_t c = p.counts[(int64_t)b * p.members + tid];
+        total += c;
+        before += b < (int)blockIdx.x ? c : 0u;
+      }
+    }
+  }
+  uint32_t upto = total;                             // members 0 .. tid: in the wave, then over the waves
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  uint32_t all = 0;
+#pragma unroll
+  for (int v = 0; v < kRouteWaves; ++v) {
+    upto += v < wave ? sums[v] : 0u;
+    all += sums[v];
+  }
+  if (tid < p.members) {
+    uint32_t at = upto - total;
+    if (blockIdx.x == 0) {
+      p.offsets[tid] = (int32_t)at;
+      if (tid == p.members - 1) p.offsets[p.members] = (int32_t)upto;
+    }
+    at += before;
+    for (int v = 0; v < kRouteWaves; ++v) {
+      const uint32_t c = next[v * p.members + tid];
+      next[v * p.members + tid] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  uint32_t* mine = next + wave * p.members;
+  for (int i0 = w.lo; i0 < w.hi; i0 += 64) {
+    const int i = i0 + lane;
+    const uint32_t m = i < w.hi ? (uint32_t)p.member[i] : 0xffffffffu;
+    const bool on = m < (uint32_t)p.members;
+    const uint64_t peers = same_lanes(m, on, p.bits);
+    int32_t at = -1;
+    if (on) {
+      at = (int32_t)(mine[m] + (uint32_t)__popcll(peers & ((1ull << lane) - 1)));
+      if (at < p.n) p.order[at] = i;                 // always, unless the members change under the call
+    }
+    // the wave's own counters: its reads before the write, the write before the next reads
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (on && lane == 63 - __builtin_clzll(peers)) mine[m] = (uint32_t)at + 1;   // the last of them
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (i < w.hi) p.place[i] = at;
+  }
+  // behind the last position; every workgroup a part
+  for (int64_t i = (int64_t)all + (int64_t)blockIdx.x * kRouteThreads + tid; i < p.n; i += (int64_t)gridDim.x * kRouteThreads)
+    p.order[i] = -1;
+}
+
+// ---- rows -------------------------------------------------------------------------
+// A row is `units` units of B bytes (16 where the rows' addresses allow, else a value).  2^lx lanes
+// of a workgroup take a row, several rows a workgroup where they are short.
+struct RowsArgs {
+  const int32_t* place;
+  int64_t rows, items;
+  int slots, units, lx;
+  const void *x, *y;
+  const float* weight;
+  void *out, *dy;
+  float* dweight;
+};
+
+template <class T, int B>
+struct Piece {
+  static constexpr int N = B / sizeof(T);
+  typedef std::conditional_t<B == 16, uint4, std::conditional_t<B == 4, uint32_t, u16>> Raw;
+  static __device__ __forceinline__ float get(const Raw& r, int j) {
+    if constexpr (B == 16) {
+      if constexpr (sizeof(T) == 4) return __uint_as_float((&r.x)[j]);
+      else return j & 1 ? bf16_hi((&r.x)[j >> 1]) : bf16_lo((&r.x)[j >> 1]);
+    } else if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(r);
+    } else {
+      return __uint_as_float((uint32_t)r << 16);
+    }
+  }
+  static __device__ __forceinline__ Raw make(const float (&v)[N]) {
+    if constexpr (B == 16) {
+      if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+      else return make_uint4(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7]));
+    } else if constexpr (sizeof(T) == 4) {
+      return __float_as_uint(v[0]);
+    } else {
+      return (u16)pk_bf16(v[0], 0.0f);
+    }
+  }
+};
+
+constexpr int kRowThreads = 256;
+constexpr int kAtOnce = 8;         // items of a row whose reads are in flight together
+
+template <class Raw>
+__global__ __launch_bounds__(kRowThreads) void k_dispatch(RowsArgs p) {
+  const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
+  for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
+    const int32_t* place = p.place + row * p.slots;
+    for (int u = l; u < p.units; u += step) {
+      const Raw v = ((const Raw*)p.x)[row * p.units + u];
+      for (int k = 0; k < p.slots; ++k) {
+        const int64_t at = place[k];
+        if (at >= 0 && at < p.items) ((Raw*)p.out)[at * p.units + u] = v;
+      }
+    }
+  }
+}
+
+template <class T, int B>
+__global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
+  typedef Piece<T, B> P;
+  typedef typename P::Raw Raw;
+  const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
+  for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
+    const int32_t* place = p.place + row * p.slots;
+    const float* weight = p.weight ? p.weight + row * p.slots : nullptr;
+    for (int u = l; u < p.units; u += step) {
+      float s[P::N] = {};
+      for (int k0 = 0; k0 < p.slots; k0 += kAtOnce) {
+        Raw v[kAtOnce];
+        float w[kAtOnce];
+        bool on[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          const int64_t at = k0 + i < p.slots ? place[k0 + i] : -1;
+          on[i] = at >= 0 && at < p.items;
+          if (on[i]) {
+            v[i] = ((const Raw*)p.y)[at * p.units + u];
+            w[i] = weight ? weight[k0 + i] : 1.0f;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          if (on[i])
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) s[j] = fmaf(w[i], P::get(v[i], j), s[j]);
+      }
+      ((Raw*)p.out)[row * p.units + u] = P::make(s);
+    }
+  }
+}
+
+// 2^lx lanes, at most a wave, take a row, so that <dout, y> needs no exchange between waves.
+template <class T, int B>
+__global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
+  typedef Piece<T, B> P;
+  typedef typename P::Raw Raw;
+  const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
+  for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
+    const int32_t* place = p.place + row * p.slots;
+    for (int k0 = 0; k0 < p.slots; k0 += kAtOnce) {
+      float dot[kAtOnce] = {}, w[kAtOnce];
+      int64_t at[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        at[i] = k0 + i < p.slots ? place[k0 + i] : -1;
+        if (at[i] >= p.items) at[i] = -1;
+        w[i] = p.weight && k0 + i < p.slots ? p.weight[row * p.slots + k0 + i] : 1.0f;
+      }
+      for (int u = l; u < p.units; u += step) {
+        const Raw g = ((const Raw*)p.x)[row * p.units + u];
+        Raw v[kAtOnce];
+        if (p.dweight) {
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i)
+            if (at[i] >= 0) v[i] = ((const Raw*)p.y)[at[i] * p.units + u];
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          if (at[i] < 0) continue;
+          if (p.dy) {
+            float o[P::N];
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) o[j] = w[i] * P::get(g, j);
+            ((Raw*)p.dy)[at[i] * p.units + u] = P::make(o);
+          }
+          if (p.dweight)
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) dot[i] = fmaf(P::get(g, j), P::get(v[i], j), dot[i]);
+        }
+      }
+      if (p.dweight) {
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          float s = dot[i];
+          for (int d = 1; d < step; d <<= 1) s += __shfl_xor(s, d, 64);
+          if (l == 0 && k0 + i < p.slots) p.dweight[row * p.slots + k0 + i] = s;
+        }
+      }
+    }
+  }
+}
+
+// Items a workgroup sorts: one workgroup up to 16,384; at most 256 workgroups.
+int route_per(int64_t n) {
+  if (n <= 16384) return (int)((n + kRouteThreads - 1) / kRouteThreads * kRouteThreads);
+  const int64_t per = (n + 255) / 256;
+  return (int)((per < 4096 ? 4096 : per + kRouteThreads - 1) / kRouteThreads * kRouteThreads);
+}
+int route_blocks(int64_t n) { return (int)((n + route_per(n) - 1) / route_per(n)); }
+
+// Bytes of a unit: 16 where every row of every array begins on 16 bytes.
+template <class... Ptr>
+bool whole_units(const sagips_routed& R, Ptr... p) {
+  const int size = R.type == SAGIPS_BF16 ? 2 : 4;
+  return (int64_t)R.width * size % 16 == 0 && ((((uintptr_t)p & 15) == 0) && ...);
+}
+RowsArgs rows_args(const sagips_routed& R, bool whole, int most_lx) {
+  RowsArgs a{};
+  a.place = R.place;
+  a.rows = R.rows;
+  a.items = R.rows * R.slots;
+  a.slots = R.slots;
+  const int size = R.type == SAGIPS_BF16 ? 2 : 4;
+  a.units = whole ? (int)((int64_t)R.width * size / 16) : R.width;
+  while (a.lx < most_lx && (1 << a.lx) < a.units) ++a.lx;
+  return a;
+}
+dim3 rows_grid(const RowsArgs& a) {
+  const int64_t per = kRowThreads >> a.lx, blocks = (a.rows + per - 1) / per, most = 1 << 20;
+  return dim3((unsigned)(blocks < most ? blocks : most));
+}
+
+}  // namespace
+
+size_t route_workspace(int64_t n, int members) {
+  const int blocks = route_blocks(n);
+  return blocks == 1 ? 0 : sizeof(uint32_t) * (size_t)blocks * members;
+}
+
+hipError_t launch_route(const int32_t* member, int64_t n, int members, int32_t* offsets, int32_t* order, int32_t* place,
+                        void* ws, hipStream_t st, Timer* tm) {
+  RouteArgs a{member, (int)n, members, route_per(n), 0, offsets, order, place, static_cast<uint32_t*>(ws)};
+  while ((1 << a.bits) < members) ++a.bits;
+  const int blocks = route_blocks(n);
+  if (blocks > 1) {
+    if (tm) tm->begin("route_count");
+    hipLaunchKernelGGL(k_route_count, dim3(blocks), dim3(kRouteThreads), 0, st, a);
+    if (tm) tm->end();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (tm) tm->begin("route_place");
+  hipLaunchKernelGGL(k_route_place, dim3(blocks), dim3(kRouteThreads), 0, st, a);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+hipError_t launch_dispatch(const sagips_routed& R, const void* x, void* sorted, hipStream_t st, Timer* tm) {
+  const bool whole = whole_units(R, x, sorted);
+  RowsArgs a = rows_args(R, whole, 8);
+  a.x = x;
+  a.out = sorted;
+  if (tm) tm->begin("dispatch");
+  if (whole) hipLaunchKernelGGL(k_dispatch<uint4>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  else if (R.type == SAGIPS_F32) hipLaunchKernelGGL(k_dispatch<uint32_t>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  else hipLaunchKernelGGL(k_dispatch<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+hipError_t launch_combine(const sagips_routed& R, const void* y, const float* weight, void* out, hipStream_t st, Timer* tm) {
+  const bool whole = whole_units(R, y, out), f32 = R.type == SAGIPS_F32;
+  RowsArgs a = rows_args(R, whole, 8);
+  a.y = y;
+  a.weight = weight;
+  a.out = out;
+  const auto kernel = whole ? (f32 ? k_combine<float, 16> : k_combine<u16, 16>) : (f32 ? k_combine<float, 4> : k_combine<u16, 2>);
+  if (tm) tm->begin("combine");
+  hipLaunchKernelGGL(kernel, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+hipError_t launch_combine_backward(const sagips_routed& R, const void* dout, const void* y, const float* weight, void* dy,
+                                   float* dweight, hipStream_t st, Timer* tm) {
+  const bool whole = whole_units(R, dout, y, dy), f32 = R.type == SAGIPS_F32;
+  RowsArgs a = rows_args(R, whole, 6);
+  a.x = dout;
+  a.y = y;
+  a.weight = weight;
+  a.dy = dy;
+  a.dweight = dweight;
+  const auto kernel = whole ? (f32 ? k_combine_grad<float, 16> : k_combine_grad<u16, 16>)
+                            : (f32 ? k_combine_grad<float, 4> : k_combine_grad<u16, 2>);
+  if (tm) tm->begin("combine_backward");
+  hipLaunchKernelGGL(kernel, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  if (tm) tm->end();
+  return hipGetLastError();
+}
+
+}  // namespace sagips

@@ -1,0 +1,150 @@
+"""GPU parity of routing (sort by member), dispatch, combine and its gradient against the
+float64 oracle, through the C ABI.  Whole numbers and copies are equal.  combine adds up to
+32 terms in fp32, each product and addition rounded together: at most slots u of the sum of absolute
+terms, u = 2^-24, then half a step of the output's type.  dweight: a lane's chain of ceil(width / 64 /
+values a unit) units of at most 8 values and six exchanges: (width / 64 + 8 + 6) u.  dy: one rounding of
+an fp32 product (u) and one of the output's type."""
+import numpy as np
+import pytest
+
+from oracle import mixture as mx
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2407_00051_amd as sg  # noqa: E402
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _member(rows, slots, members, seed, low=-1, high=0):
+    """int32 members from low to members - 1 + high: some are none."""
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    return torch.randint(low, members + high, (rows, slots), generator=g, device="cuda:0", dtype=torch.int32)
+
+
+def _check_plan(p, member, members):
+    ref = mx.route(member.cpu().numpy(), members)
+    for k in ("offsets", "order", "place"):
+        np.testing.assert_array_equal(p[k].cpu().numpy(), ref[k], err_msg=k)
+    return ref
+
+
+@pytest.mark.parametrize("rows,slots,members", [
+    (1, 1, 1), (1, 32, 3), (63, 1, 2), (64, 1, 64), (65, 3, 65), (1000, 2, 8), (1024, 16, 257), (5461, 3, 1024),
+    (16384, 1, 5), (16385, 1, 5), (4097, 8, 100), (100003, 2, 1024), (300000, 4, 17), (1200000, 1, 300)])
+def test_route_matches_oracle(gpu_ctx, rows, slots, members):
+    print(f"case route {rows} x {slots} of {members}", flush=True)
+    m = _member(rows, slots, members, rows, low=-2, high=2)
+    p = gpu_ctx.route(m, members)
+    torch.cuda.synchronize()
+    _check_plan(p, m, members)
+
+
+@pytest.mark.parametrize("rows", [500, 40000])
+def test_route_of_one_member_of_none_and_of_odd_values(gpu_ctx, rows):
+    for v in (0, 6, -1, 7, 2 ** 31 - 1, -2 ** 31):
+        m = torch.full((rows, 2), v, dtype=torch.int32, device="cuda:0")
+        p = gpu_ctx.route(m, 7)
+        torch.cuda.synchronize()
+        _check_plan(p, m, 7)
+
+
+WIDTHS = [(1, "f32"), (1, "bf16"), (6, "f32"), (7, "bf16"), (8, "bf16"), (64, "f32"), (333, "bf16"), (1000, "f32"), (2048, "bf16"),
+          (4104, "bf16"), (5001, "f32")]
+
+
+@pytest.mark.parametrize("width,dtype", WIDTHS)
+@pytest.mark.parametrize("rows,slots,members", [(1, 1, 2), (37, 3, 5), (130, 9, 4), (70, 32, 300)])
+def test_dispatch_combine_and_gradient(gpu_ctx, rows, slots, members, width, dtype):
+    print(f"case rows {rows} x {slots} of {members}, {width} {dtype}", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(rows + width)
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda:0")     # noqa: E731
+    p = gpu_ctx.route(_member(rows, slots, members, rows + slots), members)
+    place = p["place"].cpu().numpy()
+    x, y, dout = randn(rows, width).to(DT[dtype]), randn(rows * slots, width).to(DT[dtype]), randn(rows, width).to(DT[dtype])
+    w = randn(rows, slots)
+    n = int(p["offsets"][-1])
+    y[n:] = float("nan")                                               # positions of no item are not looked at
+    held = torch.full((rows * slots, width), 7.0, dtype=DT[dtype], device="cuda:0")
+    s = gpu_ctx.dispatch(x, p, out=held)
+    order = p["order"].long()
+    torch.cuda.synchronize()
+    assert torch.equal(s[:n], x[order[:n] // slots]) and (s[n:] == 7.0).all()
+    half = torch.finfo(DT[dtype]).eps / 2
+    for weight in (w, None):
+        out = gpu_ctx.combine(y, p, weight)
+        torch.cuda.synchronize()
+        ref, terms = mx.combine(y.cpu().double().numpy(), place, None if weight is None else weight.cpu().numpy())
+        err = np.abs(out.cpu().double().numpy() - ref)
+        assert (err <= half * np.abs(ref) + (1 + half) * U * slots * terms).all()
+        dy = torch.full((rows * slots, width), 7.0, dtype=DT[dtype], device="cuda:0")
+        dy, dw = gpu_ctx.combine_backward(dout, y, p, weight, dy=dy)
+        torch.cuda.synchronize()
+        rdy, rdw, rterms = mx.combine_backward(dout.cpu().double().numpy(), y.cpu().double().numpy(), place,
+                                               None if weight is None else weight.cpu().numpy())
+        assert (dy[n:] == 7.0).all()
+        got = dy[:n].cpu().double().numpy()
+        assert (np.abs(got - rdy[:n]) <= (half + 2 * U) * np.abs(rdy[:n])).all()
+        assert (np.abs(dw.cpu().double().numpy() - rdw) <= U * (width / 64 + 14) * rterms).all()
+        only, none = gpu_ctx.combine_backward(dout, None, p, weight, want_dweight=False, dy=torch.full_like(dy, 7.0))
+        torch.cuda.synchronize()
+        assert none is None and torch.equal(only, dy)
+
+
+def test_places_outside_the_rows_are_none(gpu_ctx):
+    """A plan of the caller's own: positions outside [0, rows * slots) are followed nowhere."""
+    place = torch.tensor([[0, 6], [-7, 2 ** 31 - 1], [3, -2 ** 31]], dtype=torch.int32, device="cuda:0")
+    p = {"place": place}
+    x = torch.arange(12.0, device="cuda:0").view(3, 4)
+    held = torch.full((6, 4), 7.0, device="cuda:0")
+    s = gpu_ctx.dispatch(x, p, out=held)
+    y = torch.ones((6, 4), device="cuda:0")
+    out = gpu_ctx.combine(y, p)
+    dy, dw = gpu_ctx.combine_backward(x, y, p, dy=torch.full((6, 4), 7.0, device="cuda:0"))
+    torch.cuda.synchronize()
+    assert torch.equal(s[0], x[0]) and torch.equal(s[3], x[2]) and (s[[1, 2, 4, 5]] == 7.0).all()
+    assert out[:, 0].tolist() == [1.0, 0.0, 1.0]
+    assert dw.tolist() == [[6.0, 0.0], [0.0, 0.0], [38.0, 0.0]] and (dy[[1, 2, 4, 5]] == 7.0).all()
+
+
+def test_unaligned_rows(gpu_ctx):
+    """Arrays that begin on one value only, of a width whose rows are whole 16-byte units."""
+    for dtype in ("f32", "bf16"):
+        p = gpu_ctx.route(_member(50, 2, 4, 1), 4)
+        n = int(p["offsets"][-1])
+        held = torch.randn(50 * 16 + 1, device="cuda:0").to(DT[dtype])
+        x = held[1:].view(50, 16)
+        a, b = gpu_ctx.dispatch(x, p), gpu_ctx.dispatch(x.clone(), p)
+        y = torch.randn(100 * 16 + 1, device="cuda:0").to(DT[dtype])[1:].view(100, 16)
+        c, d = gpu_ctx.combine(y, p), gpu_ctx.combine(y.clone(), p)
+        torch.cuda.synchronize()
+        assert torch.equal(a[:n], b[:n]) and torch.equal(c, d)
+
+
+def test_refusals(gpu_ctx):
+    m = _member(10, 2, 4, 1)
+    p = gpu_ctx.route(m, 4)
+    x, y = torch.zeros((10, 6), device="cuda:0"), torch.zeros((20, 6), device="cuda:0")
+    for bad in (0, 1025):
+        with pytest.raises(sg.SagipsError):
+            gpu_ctx.route(m, bad)
+    with pytest.raises(TypeError):
+        gpu_ctx.route(m.long(), 4)
+    with pytest.raises(sg.SagipsError):
+        gpu_ctx.route(torch.zeros((1, 33), dtype=torch.int32, device="cuda:0"), 4)
+    with pytest.raises(sg.SagipsError):
+        gpu_ctx.route(m[:0], 4)
+    with pytest.raises(ValueError):
+        gpu_ctx.dispatch(y, p)
+    with pytest.raises(ValueError):
+        gpu_ctx.combine(x, p)
+    with pytest.raises(TypeError):
+        gpu_ctx.dispatch(x.half(), p)
+    with pytest.raises(ValueError):
+        gpu_ctx.combine(y, p, torch.zeros((10, 3), device="cuda:0"))
+    with pytest.raises(ValueError):
+        gpu_ctx.combine_backward(x, None, p)
+    with pytest.raises(sg.SagipsError):
+        gpu_ctx.combine(y, p, out=y[:10])
