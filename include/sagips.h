@@ -516,8 +516,8 @@ typedef struct {
  *               order, of equal ones the lowest first; -1 beyond the choices that
  *               are not masked
  *   top_logp    [rows][top] their ln p; -infinity where top_choice is -1
- *   stats       [rows][2]: m / scale (0 in a row without choices) and ln s, what
- *               14. needs of the row; or NULL
+ *   stats       [rows][2]: the largest logit and log2 s (0 and -infinity in a row
+ *               without choices), what 14. needs of the row; or NULL
  * top_choice and top_logp are NULL if top is 0.  All 4-byte aligned.  Outputs
  * must not overlap the inputs or each other.                                 */
 sagips_status sagips_choice_logprob(sagips_ctx* ctx, const sagips_choices* C, const int32_t* choice, float* logp,
@@ -534,7 +534,8 @@ sagips_status sagips_choice_logprob(sagips_ctx* ctx, const sagips_choices* C, co
  *   dlogits   [rows][n_choices] of C's type, row r at dlogits + r * dstride;
  *             may be the logits themselves, with their stride, and must not
  *             overlap them otherwise; columns behind n_choices are left as they were
- * A row whose results are NaN gets NaN.  top_choice values outside [0, n_choices) are -1. */
+ * A row whose results are NaN gets NaN, but for its masked choices.  top_choice
+ * values outside [0, n_choices) are taken as -1.                              */
 typedef struct {
   const int32_t* choice;
   const float* logp;

@@ -7,9 +7,9 @@
 // Forward: one pass over the logits, which stay in registers; a row is taken by
 // 2^k lanes, a wave, 256 or 1,024 threads, whatever holds it.  Every thread keeps
 // the maximum of its own values and sums relative to that; the waves' sums are
-// joined once.  The alternatives: the K-th largest of the threads' maxima is a
-// lower bound for the K-th largest value, and only K threads have values at or
-// above it, so those few are collected in LDS and ranked by counting.
+// joined once.  The alternatives: the K-th largest of 64 groups' maxima is a lower
+// bound for the K-th largest value, and hardly more than K values reach it (64 ln 2 =
+// 44 on average at K = 32, 9 at K = 8); they are collected in LDS and ranked by counting.
 // Longer rows are read a second time for the collecting.
 #include "device_math.hpp"
 #include "kernels.hpp"
@@ -23,13 +23,12 @@ namespace {
 constexpr int kMaxTop = SAGIPS_MAX_TOP;
 constexpr float kLowest = -INFINITY;
 constexpr uint32_t kMaskedKey = 0x007fffffu;   // order_key(-infinity)
-constexpr int kCandidates = 4096;              // of a row, in LDS
 
 struct ChoiceArgs {
   const void* x;
   int64_t rows, stride;
   int n, top;
-  float scale, scale2;             // scale2 = scale log2 e
+  float scale2;                    // scale log2 e
   const int32_t* choice;
   float *logp, *entropy;
   int32_t* top_choice;
@@ -128,8 +127,8 @@ __device__ __forceinline__ V group_reduce(V v, F f) {
   return v;
 }
 template <int L>
-__device__ __forceinline__ float group_max(float v) {
-  return group_reduce<L>(v, [](float a, float b) { return fmaxf(a, b); });
+__device__ __forceinline__ float group_max(float v) {   // NaN where one is
+  return group_reduce<L>(v, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
 }
 template <int L>
 __device__ __forceinline__ float group_sum(float v) {
@@ -147,53 +146,61 @@ __device__ __forceinline__ uint64_t group_first(uint64_t c) {
   return (uint64_t)hi << 32 | lo;
 }
 
-// Sums of a part of a row: m its largest logit, s = sum 2^d, t = sum 2^d d with
-// d = (z - scale m) log2 e.  A part without choices has m = -infinity, s = t = 0.
+// Sums of a part of a row: m its largest logit, s = sum 2^d, t = sum 2^d d with d = (x - m) scale2 (the
+// difference first: a row's only choice has d = 0 and ln p = 0).  A part without choices has
+// m = -infinity, s = t = 0.
 struct Sums {
   float m, s, t;
 };
+// 0 where d is below: no 0 times infinity in 2^d d.  NaN stays.
+__device__ __forceinline__ float held_up(float d) { return __builtin_elementwise_maximum(d, -300.0f); }
 // To a larger (or the same) m.
-__device__ __forceinline__ Sums shifted(Sums a, float m, const ChoiceArgs& p) {
-  const float d = (a.m - m) * p.scale2;              // NaN only where both are infinite
-  const float f = a.s == 0.0f ? 0.0f : fast_exp2(d);
-  return {m, a.s * f, f * fmaf(a.s, fmaxf(d, -300.0f), a.t)};   // f is 0 from -150 on: no 0 times infinity
+__device__ __forceinline__ Sums shifted(const Sums& a, float m, float scale2) {
+  const float d = a.s == 0.0f ? 0.0f : held_up((a.m - m) * scale2), f = a.s == 0.0f ? 0.0f : fast_exp2(d);
+  return {m, a.s * f, f * fmaf(a.s, d, a.t)};
 }
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
-// The largest of a unit's values, with those that the thread had before.
+// The largest of a unit's values and m; NaN where one is.
 template <class T>
 __device__ __forceinline__ float unit_max(const uint4& r, float m) {
 #pragma unroll
-  for (int j = 0; j < Unit<T>::N; ++j) m = fmaxf(m, Unit<T>::get(r, j));
+  for (int j = 0; j < Unit<T>::N; j += 2) m = larger(larger(Unit<T>::get(r, j), Unit<T>::get(r, j + 1)), m);
   return m;
 }
+// A unit's sums are formed apart, so that a thread's chain is one addition a unit.
 template <class T>
-__device__ __forceinline__ void add_unit(const uint4& r, float ref, const ChoiceArgs& p, float& s, float& t) {
+__device__ __forceinline__ void add_unit(const uint4& r, float m, float scale2, float& s, float& t) {
+  float us = 0.0f, ut = 0.0f;
 #pragma unroll
   for (int j = 0; j < Unit<T>::N; ++j) {
-    const float d = (Unit<T>::get(r, j) - ref) * p.scale2, e = fast_exp2(d);
-    s += e;
-    t = fmaf(e, fmaxf(d, -300.0f), t);
+    const float d = held_up((Unit<T>::get(r, j) - m) * scale2), e = fast_exp2(d);
+    us += e;
+    ut = fmaf(e, d, ut);
   }
+  s += us;
+  t += ut;
 }
+// What values are taken relative to: their largest, or 0 where there are none.
 __device__ __forceinline__ float finite_or_0(float m) { return m == kLowest ? 0.0f : m; }
 
-// What a row's sums give: ln s, and the results that need nothing else.
+// What a row's sums give: log2 s, and the results that need nothing else.
 template <class T>
 __device__ __forceinline__ float write_row(const ChoiceArgs& p, int64_t row, const Sums& a) {
-  const float ls = logf(a.s);
+  const float ls = log2f(a.s);
   if (p.stats) {
     p.stats[2 * row] = finite_or_0(a.m);
     p.stats[2 * row + 1] = ls;
   }
-  if (p.entropy) p.entropy[row] = a.s == 0.0f ? 0.0f : ls - kLn2 * (a.t / a.s);
+  if (p.entropy) p.entropy[row] = a.s == 0.0f ? 0.0f : kLn2 * (ls - a.t / a.s);
   if (p.logp) {
     const int c = p.choice[row];
     float v = 0.0f;
     if (c >= 0 && c < p.n) {
-      const T raw = ((const T*)p.x)[row * p.stride + c];
-      const float x = sizeof(T) == 4 ? __uint_as_float(bits_of(raw)) : __uint_as_float(bits_of(raw) << 16);
+      const uint32_t raw = bits_of(((const T*)p.x)[row * p.stride + c]);
+      const float x = __uint_as_float(sizeof(T) == 4 ? raw : raw << 16);
       // a masked choice: -infinity, unless the row is NaN
-      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : fmaf(x - a.m, p.scale, -ls);
+      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : kLn2 * fmaf(x - a.m, p.scale2, -ls);
     }
     p.logp[row] = v;
   }
@@ -203,7 +210,7 @@ __device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int 
   const int64_t at = row * p.top + k;
   const bool nan = !(a.s >= 0.0f), none = (uint32_t)(c >> 32) <= kMaskedKey;
   p.top_choice[at] = nan || none ? -1 : candidate_index(c);
-  p.top_logp[at] = nan ? a.s : none ? kLowest : fmaf(order_value((uint32_t)(c >> 32)) - a.m, p.scale, -ls);
+  p.top_logp[at] = nan ? a.s : none ? kLowest : kLn2 * fmaf(order_value((uint32_t)(c >> 32)) - a.m, p.scale2, -ls);
 }
 
 // ---- short rows: L lanes each, one unit a lane ----------------------------------
@@ -219,12 +226,12 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
     Sums a;
     a.m = group_max<L>(unit_max<T>(r, kLowest));
     float s = 0.0f, t = 0.0f;
-    add_unit<T>(r, finite_or_0(a.m), p, s, t);
+    add_unit<T>(r, finite_or_0(a.m), p.scale2, s, t);
     a.s = group_sum<L>(s);
     a.t = group_sum<L>(t);
     if (l == 0) write_row<T>(p, row, a);
     if (p.top == 0) continue;
-    const float ls = logf(a.s);
+    const float ls = log2f(a.s);
     float x[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) x[j] = Unit<T>::get(r, j);
@@ -244,71 +251,68 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
 }
 
 // ---- a row a workgroup of TH threads, R units a thread and pass -------------------
+// The k-th largest key of the wave's 64, by its bits.
+__device__ __forceinline__ uint32_t wave_kth(uint32_t key, int k) {
+  uint32_t at = 0;
+#pragma unroll
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t up = at | 1u << b;
+    if (__popcll(__ballot(key >= up)) >= k) at = up;
+  }
+  return at;
+}
+
 template <class T, int TH, int R, bool kOnePass>
 __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
-  constexpr int N = Unit<T>::N, W = TH / 64;
-  static_assert(!kOnePass || R * N * kMaxTop <= kCandidates, "a row's candidates have to fit");
+  constexpr int N = Unit<T>::N, W = TH / 64, G = TH / 64, kHeld = TH == 64 ? 256 : 1024;
   __shared__ Sums part[W];
-  __shared__ uint64_t firsts[W][kMaxTop];
+  __shared__ float group[64];                        // the largest logit of every G threads
+  __shared__ uint64_t cand[kHeld], firsts[W];
   __shared__ uint32_t held;
-  extern __shared__ uint64_t cand[];                 // kOnePass: top R N; else kCandidates
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint32_t inf2 = 0xff80ff80u;
+  const uint4 fill = sizeof(T) == 4 ? make_uint4(kFill<float>, kFill<float>, kFill<float>, kFill<float>) : make_uint4(inf2, inf2, inf2, inf2);
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const RowView<T> v(p.x, row * p.stride, p.n);
     const int units = v.units();
-    const uint4 none = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u);   // bf16 -infinity
-    const uint4 fill = sizeof(T) == 4 ? make_uint4(kFill<float>, kFill<float>, kFill<float>, kFill<float>) : none;
     uint4 r[R];
-    Sums a{kLowest, 0.0f, 0.0f};
-    float best = kLowest;
-    int best_at = 0;
-    for (int q0 = 0; q0 < units; q0 += TH * R) {
+    const auto load = [&](int q0) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const int q = q0 + i * TH + tid;
         r[i] = q < units ? v.load(q) : fill;
       }
-      float m = kLowest;
+    };
+    float best = kLowest;                            // of the thread
+    Sums a{kLowest, 0.0f, 0.0f};
+    for (int q0 = 0; q0 < units; q0 += TH * R) {
+      load(q0);
 #pragma unroll
-      for (int i = 0; i < R; ++i) m = unit_max<T>(r[i], m);
-      if (p.top && m > best) {
-        best = m;
+      for (int i = 0; i < R; ++i) best = unit_max<T>(r[i], best);
+      if constexpr (!kOnePass) a = shifted(a, best, p.scale2);
+      a.m = best;
+      const float m = finite_or_0(best);
 #pragma unroll
-        for (int i = R - 1; i >= 0; --i)
-#pragma unroll
-          for (int j = N - 1; j >= 0; --j)
-            if (Unit<T>::get(r[i], j) == m) best_at = v.first(q0 + i * TH + tid) + j;
-      }
-      m = fmaxf(m, a.m);
-      if constexpr (!kOnePass) a = shifted(a, m, p);
-      a.m = m;
-      const float ref = finite_or_0(m);
-#pragma unroll
-      for (int i = 0; i < R; ++i) add_unit<T>(r[i], ref, p, a.s, a.t);
+      for (int i = 0; i < R; ++i) add_unit<T>(r[i], m, p.scale2, a.s, a.t);
     }
-    a = shifted(a, group_max<64>(a.m), p);
+    if (p.top) {
+      const float g = group_max<G>(best);
+      if (tid % G == 0) group[tid / G] = g;
+      if (tid == 0) held = 0;
+    }
+    a = shifted(a, group_max<64>(a.m), p.scale2);
     a.s = group_sum<64>(a.s);
     a.t = group_sum<64>(a.t);
     if (lane == 0) part[wave] = a;
-    uint64_t mine = candidate(best, best_at);
-    if (p.top) {                                     // the wave's threads in order of their maxima
-      uint64_t c = mine;
-      for (int k = 0; k < p.top; ++k) {
-        const uint64_t first = group_first<64>(c);
-        if (lane == 0) firsts[wave][k] = first;
-        if (c == first) c = 0;
-      }
-      if (tid == 0) held = 0;
-    }
     __syncthreads();
     if constexpr (W > 1) {
       float m = kLowest;
 #pragma unroll
-      for (int w = 0; w < W; ++w) m = fmaxf(m, part[w].m);
+      for (int w = 0; w < W; ++w) m = larger(m, part[w].m);
       Sums all{m, 0.0f, 0.0f};
 #pragma unroll
       for (int w = 0; w < W; ++w) {
-        const Sums b = shifted(part[w], m, p);
+        const Sums b = shifted(part[w], m, p.scale2);
         all.s += b.s;
         all.t += b.t;
       }
@@ -316,50 +320,36 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
     }
     if (tid == 0) write_row<T>(p, row, a);
     if (p.top) {
-      const float ls = logf(a.s);
-      // the top-th of the threads' maxima, by every wave from the waves' lists
-      uint64_t bound = firsts[0][p.top - 1];
-      if constexpr (W > 1) {
-        int at = 0;
-        uint64_t c = lane < W ? firsts[lane][0] : 0;
-        for (int k = 0; k < p.top; ++k) {
-          bound = group_first<64>(c);
-          if (lane < W && c == bound) c = ++at < p.top ? firsts[lane][at] : 0;
-        }
-      }
-      // fewer threads than alternatives have a choice: all that are not masked
-      if ((uint32_t)(bound >> 32) <= kMaskedKey) bound = (uint64_t)(kMaskedKey + 1) << 32 | 0x80000000u;
-      const float bound_x = order_value((uint32_t)(bound >> 32));
-      const int bound_i = candidate_index(bound);
+      const float ls = log2f(a.s);
+      // at least top values are no less than the top-th of the 64 groups' largest
+      const uint32_t key = max(wave_kth(order_key(group[lane]), p.top), kMaskedKey + 1);
+      const float bound = order_value(key);
       const auto collect = [&](int q0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
+          if (!(unit_max<T>(r[i], kLowest) >= bound)) continue;
           const int i0 = v.first(q0 + i * TH + tid);
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             const float x = Unit<T>::get(r[i], j);
-            if (x >= bound_x && (x > bound_x || i0 + j <= bound_i)) {
+            if (x >= bound) {
               const uint32_t at = atomicAdd(&held, 1u);
-              if (kOnePass || at < (uint32_t)kCandidates) cand[at] = candidate(x, i0 + j);
+              if (at < (uint32_t)kHeld) cand[at] = candidate(x, i0 + j);
             }
           }
         }
       };
-      if (mine >= bound) {                             // a thread whose maximum is below has none
+      if (best >= bound) {                             // a thread whose largest is below has none
         if constexpr (kOnePass) collect(0);
         else
           for (int q0 = 0; q0 < units; q0 += TH * R) {
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-              const int q = q0 + i * TH + tid;
-              r[i] = q < units ? v.load(q) : fill;
-            }
+            load(q0);
             collect(q0);
           }
       }
       __syncthreads();
       const int n = (int)held;
-      if (kOnePass || n <= kCandidates) {
+      if (n <= kHeld) {
         for (int i = tid; i < n; i += TH) {
           const uint64_t c = cand[i];
           int rank = 0;
@@ -368,7 +358,7 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
         }
         for (int k = n + tid; k < p.top; k += TH) write_top(p, row, k, 0, a, ls);
       } else {
-        // more than are held: one alternative a pass over the row
+        // more equal values than are held: one alternative a pass over the row
         uint64_t last = ~0ull;
         for (int k = 0; k < p.top; ++k) {
           uint64_t c = 0;
@@ -382,15 +372,15 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
           }
           c = group_first<64>(c);
           __syncthreads();
-          if (lane == 0) firsts[wave][0] = c;
+          if (lane == 0) firsts[wave] = c;
           __syncthreads();
-          c = group_first<64>(lane < W ? firsts[lane][0] : 0);
+          c = group_first<64>(lane < W ? firsts[lane] : 0);
           if (tid == 0) write_top(p, row, k, c, a, ls);
           last = c;
         }
       }
     }
-    __syncthreads();                                   // the next row's part, firsts and held
+    __syncthreads();                                   // the next row's part, group and held
   }
 }
 
@@ -400,7 +390,7 @@ struct ChoiceGradArgs {
   void* dx;
   int64_t rows, stride, dstride;
   int n, top;
-  float scale;
+  float scale, scale2;
   const int32_t *choice, *top_choice;
   const float *logp, *entropy, *stats, *d_logp, *d_entropy, *d_top;
   int chunks;                      // of a row
@@ -421,20 +411,21 @@ __device__ __forceinline__ void grad_entry(const ChoiceGradArgs& p, int64_t row,
 
 // A unit of N values (one, where the two arrays' rows are not aligned alike) of a row.
 struct GradRow {
-  float shift, ls, a, gh, scale;
-  // scale p (a - gh ln p)
+  float m, ls, a, gh, scale2;      // gh in log2 p's terms
+  // p (a - gh ln p)
   __device__ __forceinline__ float at(float x) const {
-    const float lp = fmaf(x - shift, scale, -ls), pr = x == kLowest ? 0.0f : fast_exp2(lp * kLog2e);
-    return pr * fmaf(-gh, fmaxf(lp, -200.0f), a);
+    const float lp = fmaf(x - m, scale2, -ls);
+    return x == kLowest ? 0.0f : fast_exp2(lp) * fmaf(-gh, held_up(lp), a);
   }
 };
 __device__ __forceinline__ GradRow grad_row(const ChoiceGradArgs& p, int64_t row, float total) {
   GradRow g;
-  g.shift = p.stats[2 * row];
+  g.m = p.stats[2 * row];
   g.ls = p.stats[2 * row + 1];
-  g.gh = p.d_entropy ? p.d_entropy[row] : 0.0f;
-  g.a = -total - (p.d_entropy ? g.gh * p.entropy[row] : 0.0f);
-  g.scale = p.scale;
+  const float gh = p.d_entropy ? p.d_entropy[row] : 0.0f;
+  g.a = -total - (p.d_entropy ? gh * p.entropy[row] : 0.0f);
+  g.gh = gh * kLn2;
+  g.scale2 = p.scale2;
   return g;
 }
 
@@ -551,9 +542,8 @@ hipError_t choice_forward(const ChoiceArgs& a, hipStream_t st) {
   const auto go_row = [&](auto threads, auto per, auto one) {
     constexpr int TH = decltype(threads)::value, R = decltype(per)::value;
     constexpr bool kOne = decltype(one)::value;
-    const size_t lds = a.top ? sizeof(uint64_t) * (kOne ? a.top * R * N : kCandidates) : 0;
     const int64_t most = 256 * (int64_t)(2048 / TH) * 4;
-    hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), lds, st, a);
+    hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), 0, st, a);
   };
   const std::true_type one{};
   if (units <= 1) go_short(Int<1>{});
@@ -598,7 +588,7 @@ hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
 
 hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
                          float* top_logp, float* stats, hipStream_t st, Timer* tm) {
-  ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)C.scale, (float)(C.scale * 1.4426950408889634),
+  ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)(C.scale * 1.4426950408889634),
                choice, logp, entropy, top_choice, top_logp, stats};
   if (tm) tm->begin("choice_logprob");
   const hipError_t e = C.type == SAGIPS_BF16 ? choice_forward<u16>(a, st) : choice_forward<float>(a, st);
@@ -608,7 +598,7 @@ hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* 
 
 hipError_t launch_choice_backward(const sagips_choices& C, const sagips_choice_grads& g, void* dlogits, int64_t dstride,
                                   hipStream_t st, Timer* tm) {
-  ChoiceGradArgs a{C.logits, dlogits, C.rows, C.stride, dstride, C.n_choices, g.d_top ? C.top : 0, (float)C.scale,
+  ChoiceGradArgs a{C.logits, dlogits, C.rows, C.stride, dstride, C.n_choices, g.d_top ? C.top : 0, (float)C.scale, (float)(C.scale * 1.4426950408889634),
                    g.choice, g.top_choice, g.logp, g.entropy, g.stats, g.d_logp, g.d_entropy, g.d_top, 0};
   const int size = C.type == SAGIPS_BF16 ? 2 : 4;
   const bool alike = ((uintptr_t)C.logits - (uintptr_t)dlogits) % 16 == 0 && (C.rows == 1 || (C.stride - dstride) * size % 16 == 0);
