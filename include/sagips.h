@@ -495,7 +495,7 @@ sagips_status sagips_muon_step(sagips_ctx* ctx, const sagips_matrix_set* set, co
  *             n_choices; aligned to one value, rows of any alignment
  *   scale     2^-100 to 2^100 (an inverse temperature)
  *   top       alternatives asked for, 0 to SAGIPS_MAX_TOP
- * 1 <= rows < 2^31, 1 <= n_choices <= 2^30, stride < 2^31.                    */
+ * 1 <= rows < 2^31, 1 <= n_choices <= 2^29, stride < 2^31.                    */
 #define SAGIPS_MAX_TOP 32
 typedef struct {
   const void* logits;

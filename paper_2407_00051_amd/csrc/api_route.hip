@@ -50,7 +50,7 @@ sagips_status check_choices(sagips_ctx* c, const sagips_choices* C) {
   if (!known_type(C->type)) return fail(c, SAGIPS_E_INVAL, "unknown type %d", C->type);
   if ((uintptr_t)C->logits % value_bytes(C->type)) return fail(c, SAGIPS_E_INVAL, "logits is not aligned to its values");
   if (C->rows < 1 || C->rows >= ((int64_t)1 << 31)) return fail(c, SAGIPS_E_INVAL, "rows = %lld outside [1, 2^31)", (long long)C->rows);
-  if (C->n_choices < 1 || C->n_choices > (1 << 30)) return fail(c, SAGIPS_E_INVAL, "n_choices = %d outside [1, 2^30]", C->n_choices);
+  if (C->n_choices < 1 || C->n_choices > (1 << 29)) return fail(c, SAGIPS_E_INVAL, "n_choices = %d outside [1, 2^29]", C->n_choices);
   if (C->stride < C->n_choices || C->stride >= ((int64_t)1 << 31))
     return fail(c, SAGIPS_E_INVAL, "stride = %lld outside [n_choices = %d, 2^31)", (long long)C->stride, C->n_choices);
   if (C->top < 0 || C->top > SAGIPS_MAX_TOP) return fail(c, SAGIPS_E_INVAL, "top = %d outside [0, %d]", C->top, SAGIPS_MAX_TOP);

@@ -36,18 +36,20 @@ struct ChoiceArgs {
 };
 
 // Values of a 16-byte unit.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint32_t word(u32x4 r, int k) { return k < 2 ? (k == 0 ? r.x : r.y) : (k == 2 ? r.z : r.w); }
 template <class T>
 struct Unit;
 template <>
 struct Unit<float> {
   static constexpr int N = 4;
-  static __device__ __forceinline__ float get(const uint4& r, int j) { return __uint_as_float((&r.x)[j]); }
+  static __device__ __forceinline__ float get(u32x4 r, int j) { return __uint_as_float(word(r, j)); }
 };
 template <>
 struct Unit<u16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ float get(const uint4& r, int j) {
-    const uint32_t w = (&r.x)[j >> 1];
+  static __device__ __forceinline__ float get(u32x4 r, int j) {
+    const uint32_t w = word(r, j >> 1);
     return j & 1 ? bf16_hi(w) : bf16_lo(w);
   }
 };
@@ -71,10 +73,11 @@ struct RowView {
   }
   __device__ __forceinline__ int units() const { return (int)(((int64_t)n + lead + N - 1) / N); }
   __device__ __forceinline__ int first(int q) const { return q * N - lead; }
-  __device__ __forceinline__ uint4 load(int q) const {
+  __device__ __forceinline__ u32x4 load_whole(int q) const { return *reinterpret_cast<const u32x4*>(base + (uint32_t)q * 16u); }
+  __device__ __forceinline__ u32x4 load(int q) const {
     const int i0 = first(q);
-    const char* at = base + (int64_t)q * 16;
-    if (i0 >= 0 && i0 <= n - N) return *reinterpret_cast<const uint4*>(at);
+    const char* at = base + (uint32_t)q * 16u;
+    if (i0 >= 0 && i0 <= n - N) return load_whole(q);
     uint32_t w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
@@ -87,7 +90,7 @@ struct RowView {
         w[k] = lo | hi << 16;
       }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return u32x4{w[0], w[1], w[2], w[3]};
   }
 };
 
@@ -163,14 +166,14 @@ __device__ __forceinline__ float larger(float a, float b) { return __builtin_ele
 
 // The largest of a unit's values and m; NaN where one is.
 template <class T>
-__device__ __forceinline__ float unit_max(const uint4& r, float m) {
+__device__ __forceinline__ float unit_max(u32x4 r, float m) {
 #pragma unroll
   for (int j = 0; j < Unit<T>::N; j += 2) m = larger(larger(Unit<T>::get(r, j), Unit<T>::get(r, j + 1)), m);
   return m;
 }
 // A unit's sums are formed apart, so that a thread's chain is one addition a unit.
 template <class T>
-__device__ __forceinline__ void add_unit(const uint4& r, float m, float scale2, float& s, float& t) {
+__device__ __forceinline__ void add_unit(u32x4 r, float m, float scale2, float& s, float& t) {
   float us = 0.0f, ut = 0.0f;
 #pragma unroll
   for (int j = 0; j < Unit<T>::N; ++j) {
@@ -213,6 +216,10 @@ __device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int 
   p.top_logp[at] = nan ? a.s : none ? kLowest : kLn2 * fmaf(order_value((uint32_t)(c >> 32)) - a.m, p.scale2, -ls);
 }
 
+// Values are taken out of a unit again where they are next needed: kept as floats from one use to the
+// next they would need twice the registers, and half the waves would be resident.
+__device__ __forceinline__ void forget(u32x4& r) { asm volatile("" : "+v"(r)); }
+
 // ---- short rows: L lanes each, one unit a lane ----------------------------------
 template <class T, int L>
 __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
@@ -221,7 +228,7 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
   // whole groups leave: no exchange crosses them
   for (int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L; row < p.rows; row += (int64_t)gridDim.x * (256 / L)) {
     const RowView<T> v(p.x, row * p.stride, p.n);
-    const uint4 r = v.load(l);
+    const u32x4 r = v.load(l);
     const int i0 = v.first(l);
     Sums a;
     a.m = group_max<L>(unit_max<T>(r, kLowest));
@@ -251,11 +258,12 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
 }
 
 // ---- a row a workgroup of TH threads, R units a thread and pass -------------------
-// The k-th largest key of the wave's 64, by its bits.
+// The k-th largest key of the wave's 64, by its upper 16 bits, which are a bf16 value's all; the lower
+// ones are 0: no larger than the k-th largest.
 __device__ __forceinline__ uint32_t wave_kth(uint32_t key, int k) {
   uint32_t at = 0;
 #pragma unroll
-  for (int b = 31; b >= 0; --b) {
+  for (int b = 31; b >= 16; --b) {
     const uint32_t up = at | 1u << b;
     if (__popcll(__ballot(key >= up)) >= k) at = up;
   }
@@ -263,24 +271,31 @@ __device__ __forceinline__ uint32_t wave_kth(uint32_t key, int k) {
 }
 
 template <class T, int TH, int R, bool kOnePass>
-__global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
+__global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p) {
   constexpr int N = Unit<T>::N, W = TH / 64, G = TH / 64, kHeld = TH == 64 ? 256 : 1024;
   __shared__ Sums part[W];
   __shared__ float group[64];                        // the largest logit of every G threads
   __shared__ uint64_t cand[kHeld], firsts[W];
   __shared__ uint32_t held;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const uint32_t inf2 = 0xff80ff80u;
-  const uint4 fill = sizeof(T) == 4 ? make_uint4(kFill<float>, kFill<float>, kFill<float>, kFill<float>) : make_uint4(inf2, inf2, inf2, inf2);
+  constexpr uint32_t none = sizeof(T) == 4 ? kFill<T> : kFill<T> << 16 | kFill<T>;
+  const u32x4 fill = {none, none, none, none};
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const RowView<T> v(p.x, row * p.stride, p.n);
     const int units = v.units();
-    uint4 r[R];
+    u32x4 r[R];
+    // all whole units' reads first, with no branch between them; then those at the row's ends
+    const int whole0 = v.lead ? 1 : 0, whole1 = (v.n + v.lead) / N - 1;
     const auto load = [&](int q0) __attribute__((always_inline)) {
+      if (whole1 >= whole0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) r[i] = v.load_whole(min(max(q0 + i * TH + tid, whole0), whole1));
+      }
+      if (whole0 == 0 && q0 + R * TH - 1 <= whole1) return;
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const int q = q0 + i * TH + tid;
-        r[i] = q < units ? v.load(q) : fill;
+        if (q < whole0 || q > whole1) r[i] = q < units ? v.load(q) : fill;
       }
     };
     float best = kLowest;                            // of the thread
@@ -293,7 +308,11 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
       a.m = best;
       const float m = finite_or_0(best);
 #pragma unroll
-      for (int i = 0; i < R; ++i) add_unit<T>(r[i], m, p.scale2, a.s, a.t);
+      for (int i = 0; i < R; ++i) {
+        forget(r[i]);
+        add_unit<T>(r[i], m, p.scale2, a.s, a.t);
+        forget(r[i]);
+      }
     }
     if (p.top) {
       const float g = group_max<G>(best);
@@ -306,17 +325,10 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
     if (lane == 0) part[wave] = a;
     __syncthreads();
     if constexpr (W > 1) {
-      float m = kLowest;
-#pragma unroll
-      for (int w = 0; w < W; ++w) m = larger(m, part[w].m);
-      Sums all{m, 0.0f, 0.0f};
-#pragma unroll
-      for (int w = 0; w < W; ++w) {
-        const Sums b = shifted(part[w], m, p.scale2);
-        all.s += b.s;
-        all.t += b.t;
-      }
-      a = all;
+      a = part[lane % W];
+      a = shifted(a, group_max<W>(a.m), p.scale2);
+      a.s = group_sum<W>(a.s);
+      a.t = group_sum<W>(a.t);
     }
     if (tid == 0) write_row<T>(p, row, a);
     if (p.top) {
@@ -327,15 +339,14 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
       const auto collect = [&](int q0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-          if (!(unit_max<T>(r[i], kLowest) >= bound)) continue;
-          const int i0 = v.first(q0 + i * TH + tid);
+          uint32_t on = 0;
 #pragma unroll
-          for (int j = 0; j < N; ++j) {
-            const float x = Unit<T>::get(r[i], j);
-            if (x >= bound) {
-              const uint32_t at = atomicAdd(&held, 1u);
-              if (at < (uint32_t)kHeld) cand[at] = candidate(x, i0 + j);
-            }
+          for (int j = 0; j < N; ++j) on |= Unit<T>::get(r[i], j) >= bound ? 1u << j : 0u;
+          while (on) {                                 // a few units of the row
+            const int j = __ffs(on) - 1;
+            on &= on - 1;
+            const uint32_t at = atomicAdd(&held, 1u);
+            if (at < (uint32_t)kHeld) cand[at] = candidate(Unit<T>::get(r[i], j), v.first(q0 + i * TH + tid) + j);
           }
         }
       };
@@ -363,7 +374,7 @@ __global__ __launch_bounds__(TH) void k_choice_row(ChoiceArgs p) {
         for (int k = 0; k < p.top; ++k) {
           uint64_t c = 0;
           for (int q = tid; q < units; q += TH) {
-            const uint4 u = v.load(q);
+            const u32x4 u = v.load(q);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
               const uint64_t one = candidate(Unit<T>::get(u, j), v.first(q) + j);
@@ -450,7 +461,7 @@ __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
     const T* x = (const T*)p.x + row * p.stride;
     T* dx = (T*)p.dx + row * p.dstride;
     float val[R][N];
-    uint4 raw[R];
+    u32x4 raw[R];
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int q = q0 + i * L + l;
@@ -511,10 +522,10 @@ __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
       for (int j = 0; j < N; ++j) val[i][j] *= p.scale;
       if constexpr (kUnits) {
         if (i0 >= 0 && i0 <= p.n - N) {
-          uint4 o;
-          if constexpr (sizeof(T) == 4) o = make_uint4(__float_as_uint(val[i][0]), __float_as_uint(val[i][1]), __float_as_uint(val[i][2]), __float_as_uint(val[i][3]));
-          else o = make_uint4(pk_bf16(val[i][0], val[i][1]), pk_bf16(val[i][2], val[i][3]), pk_bf16(val[i][4 % N], val[i][5 % N]), pk_bf16(val[i][6 % N], val[i][7 % N]));
-          *reinterpret_cast<uint4*>(dx + i0) = o;
+          u32x4 o;
+          if constexpr (sizeof(T) == 4) o = u32x4{__float_as_uint(val[i][0]), __float_as_uint(val[i][1]), __float_as_uint(val[i][2]), __float_as_uint(val[i][3])};
+          else o = u32x4{pk_bf16(val[i][0], val[i][1]), pk_bf16(val[i][2], val[i][3]), pk_bf16(val[i][4 % N], val[i][5 % N]), pk_bf16(val[i][6 % N], val[i][7 % N])};
+          *reinterpret_cast<u32x4*>(dx + i0) = o;
           continue;
         }
       }
