@@ -235,6 +235,7 @@ class Context:
 
     def __init__(self, device: int = 0, stream=None):
         import torch
+        self._torch = torch
         self.lib = load_library()
         self.device = device
         self._follow = stream is None
@@ -738,20 +739,26 @@ class Context:
 
     # -- choices, and a mixture of members -----------------------------------------------------
     def _choices(self, logits, top, scale) -> Choices:
-        import torch
-        if not isinstance(logits, torch.Tensor):
-            raise TypeError("logits must be a torch.Tensor")
-        if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
-            raise ValueError("logits must be [rows][choices]")
-        if not logits.is_cuda or logits.get_device() != self.device:
+        torch = self._torch
+        dtype = logits.dtype
+        if dtype is torch.float32:
+            kind = F32
+        elif dtype is torch.bfloat16:
+            kind = BF16
+        else:
+            raise TypeError(f"logits must be torch.float32 or torch.bfloat16, got {dtype}")
+        if logits.get_device() != self.device or not logits.is_cuda:
             raise ValueError(f"logits must be on cuda:{self.device}")
-        if logits.dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"logits must be torch.float32 or torch.bfloat16, got {logits.dtype}")
-        n, V = logits.shape
-        stride = logits.stride(0) if n > 1 else max(V, logits.stride(0))
-        if (V > 1 and logits.stride(1) != 1) or stride < V:
+        shape = logits.shape
+        if len(shape) != 2 or shape[0] < 1 or shape[1] < 1:
+            raise ValueError("logits must be [rows][choices]")
+        n, V = shape
+        rows, each = logits.stride()
+        if n == 1:
+            rows = max(rows, V)
+        if (each != 1 and V > 1) or rows < V:
             raise ValueError("the choices of a row must follow each other, and rows must not overlap")
-        return Choices(logits.data_ptr(), n, stride, V, F32 if logits.dtype == torch.float32 else BF16, int(top), scale)
+        return Choices(logits.data_ptr(), n, rows, V, kind, top, scale)
 
     def choice_logprob(self, logits, choice=None, top: int = 0, scale: float = 1.0) -> dict:
         """Of the categorical distribution softmax(scale * logits) of every row of logits [rows][choices]
@@ -759,21 +766,24 @@ class Context:
         int32 (0 for a row whose choice is outside the range; None without choice), entropy [rows], the
         `top` (up to 32) most likely alternatives top_choice [rows][top] int32 (-1 where there are
         fewer) and their top_logp, and stats [rows][2] for choice_backward."""
-        import torch
+        torch = self._torch
         self._enter()
-        C = self._choices(logits, top, scale)
-        n = C.rows
-        _check_tensor(choice, "choice", torch.int32, (n,), self.device)
         if not 0 <= top <= MAX_TOP:
             raise ValueError(f"top must be in [0, {MAX_TOP}]")
-        f32 = dict(dtype=torch.float32, device=logits.device)
-        held = torch.empty(n * (4 + top), **f32)            # one allocation: a call is short
-        logp, entropy, stats, top_logp = held.split([n, n, 2 * n, n * top])
-        top_choice = torch.empty((n, top), dtype=torch.int32, device=logits.device)
-        self._owned(held, top_choice, logits, choice)
+        C = self._choices(logits, top, scale)
+        n = C.rows
+        # one allocation for the fp32 results: a call is short
+        held = logits.new_empty(n * (4 + top), dtype=torch.float32)
+        logp, entropy, stats, top_logp = held.split_with_sizes((n, n, 2 * n, n * top))
+        top_choice = logits.new_empty((n, top), dtype=torch.int32)
+        if choice is not None:
+            _check_tensor(choice, "choice", torch.int32, (n,), self.device)
+        if not self._follow:
+            self._owned(held, top_choice, logits, choice)
+        at = held.data_ptr()
         self._check(self.lib.sagips_choice_logprob(
-            self.h, ctypes.byref(C), _ptr(choice), None if choice is None else logp.data_ptr(), entropy.data_ptr(),
-            top_choice.data_ptr() if top else None, top_logp.data_ptr() if top else None, stats.data_ptr()))
+            self.h, ctypes.byref(C), None if choice is None else choice.data_ptr(), None if choice is None else at,
+            at + 4 * n, top_choice.data_ptr() if top else None, at + 16 * n if top else None, at + 8 * n))
         return {"logp": None if choice is None else logp, "entropy": entropy, "top_choice": top_choice,
                 "top_logp": top_logp.view(n, top), "stats": stats.view(n, 2)}
 
@@ -782,66 +792,78 @@ class Context:
         """dL/dlogits [rows][choices] in the logits' type, from what choice_logprob returned (fwd) for the
         same logits, choice and scale, and the derivatives d_logp, d_entropy [rows], d_top [rows][top] of
         the loss (None: not in it).  out may be the logits, and rows of it may be strided."""
-        import torch
+        torch = self._torch
         self._enter()
         f32, dev = torch.float32, self.device
-        top = 0 if d_top is None else fwd["top_choice"].shape[1]
+        tops = fwd["top_choice"]
+        top = 0 if d_top is None else tops.shape[1]
         C = self._choices(logits, top, scale)
         n = C.rows
-        _check_tensor(choice, "choice", torch.int32, (n,), dev)
-        _check_tensor(d_logp, "d_logp", f32, (n,), dev)
-        _check_tensor(d_entropy, "d_entropy", f32, (n,), dev)
-        _check_tensor(d_top, "d_top", f32, (n, top), dev)
-        for name, shape, dtype in (("logp", (n,), f32), ("entropy", (n,), f32), ("stats", (n, 2), f32),
-                                   ("top_choice", (n, fwd["top_choice"].shape[1]), torch.int32)):
-            _check_tensor(fwd[name], f"fwd[{name!r}]", dtype, shape, dev)
-        if d_logp is not None and (choice is None or fwd["logp"] is None):
-            raise ValueError("d_logp needs the choice, in choice_logprob too")
-        o = out if out is not None else torch.empty((n, C.n_choices), dtype=logits.dtype, device=logits.device)
-        if o.dtype != logits.dtype or o.shape != logits.shape:
-            raise ValueError("out must have the logits' shape and type")
-        to = self._choices(o, top, scale)
-        g = ChoiceGrads(_ptr(choice), _ptr(fwd["logp"]), _ptr(fwd["entropy"]),
-                        fwd["top_choice"].data_ptr() if top else None, fwd["stats"].data_ptr(), _ptr(d_logp),
-                        _ptr(d_entropy), d_top.data_ptr() if top else None)
-        self._owned(o if out is None else None, logits, choice, d_logp, d_entropy, d_top,
-                    [fwd[k] for k in ("logp", "entropy", "stats", "top_choice")])
-        self._check(self.lib.sagips_choice_backward(self.h, ctypes.byref(C), ctypes.byref(g), o.data_ptr(), to.stride))
-        return o
+        g = ChoiceGrads()
+        stats = fwd["stats"]
+        _check_tensor(stats, "fwd['stats']", f32, (n, 2), dev)
+        g.stats = stats.data_ptr()
+        if d_logp is not None:
+            if choice is None or fwd["logp"] is None:
+                raise ValueError("d_logp needs the choice, in choice_logprob too")
+            _check_tensor(d_logp, "d_logp", f32, (n,), dev)
+            _check_tensor(choice, "choice", torch.int32, (n,), dev)
+            _check_tensor(fwd["logp"], "fwd['logp']", f32, (n,), dev)
+            g.d_logp, g.choice, g.logp = d_logp.data_ptr(), choice.data_ptr(), fwd["logp"].data_ptr()
+        if d_entropy is not None:
+            _check_tensor(d_entropy, "d_entropy", f32, (n,), dev)
+            _check_tensor(fwd["entropy"], "fwd['entropy']", f32, (n,), dev)
+            g.d_entropy, g.entropy = d_entropy.data_ptr(), fwd["entropy"].data_ptr()
+        if top:
+            _check_tensor(d_top, "d_top", f32, (n, top), dev)
+            _check_tensor(tops, "fwd['top_choice']", torch.int32, (n, top), dev)
+            g.d_top, g.top_choice = d_top.data_ptr(), tops.data_ptr()
+        stride = C.n_choices
+        if out is None:
+            out = logits.new_empty((n, stride))
+        else:
+            if out.dtype != logits.dtype or out.shape != logits.shape:
+                raise ValueError("out must have the logits' shape and type")
+            stride = self._choices(out, top, scale).stride
+        if not self._follow:
+            self._owned(out, logits, choice, d_logp, d_entropy, d_top, [fwd[k] for k in ("logp", "entropy", "stats", "top_choice")])
+        self._check(self.lib.sagips_choice_backward(self.h, ctypes.byref(C), ctypes.byref(g), out.data_ptr(), stride))
+        return out
 
     def route(self, member, n_members: int) -> dict:
         """Items sorted by the member that they are given to: of member [rows][slots] int32 (or [rows]; values
         outside [0, n_members) give the item to none) the plan offsets [n_members + 1], order [rows * slots]
         (the item row * slots + slot at each sorted position, then -1) and place [rows][slots] (each item's
         sorted position, or -1), all int32."""
-        import torch
         self._enter()
-        _check_tensor(member, "member", torch.int32, None, self.device)
-        if member.dim() not in (1, 2):
+        _check_tensor(member, "member", self._torch.int32, None, self.device)
+        shape = member.shape
+        if len(shape) not in (1, 2):
             raise ValueError("member must be [rows][slots] or [rows]")
-        rows, slots = member.shape[0], member.shape[1] if member.dim() == 2 else 1
-        offsets = member.new_empty(int(n_members) + 1)
-        order, place = member.new_empty(rows * slots), member.new_empty(rows, slots)
-        self._owned(offsets, order, place, member)
-        self._check(self.lib.sagips_route(self.h, member.data_ptr(), rows, slots, int(n_members), offsets.data_ptr(),
+        rows, slots = shape[0], shape[1] if len(shape) == 2 else 1
+        offsets, order, place = member.new_empty(max(0, n_members) + 1), member.new_empty(rows * slots), member.new_empty((rows, slots))
+        if not self._follow:
+            self._owned(offsets, order, place, member)
+        self._check(self.lib.sagips_route(self.h, member.data_ptr(), rows, slots, n_members, offsets.data_ptr(),
                                           order.data_ptr(), place.data_ptr()))
         return {"offsets": offsets, "order": order, "place": place}
 
     def _routed(self, plan, t, name, items: bool) -> Routed:
         """The plan for rows like t, [rows][width] or (items) [rows * slots][width]."""
-        import torch
+        torch = self._torch
         place = plan["place"]
         _check_tensor(place, "place", torch.int32, None, self.device)
+        _check_tensor(t, name, None, None, self.device)
+        dtype = t.dtype
+        if dtype is not torch.float32 and dtype is not torch.bfloat16:
+            raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {dtype}")
         if place.dim() != 2:
             raise ValueError("place must be [rows][slots]")
-        _check_tensor(t, name, None, None, self.device)
-        if t.dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
-        rows, slots = place.shape
+        (rows, slots), shape = place.shape, t.shape
         want = rows * slots if items else rows
-        if t.dim() != 2 or t.shape[0] != want:
+        if len(shape) != 2 or shape[0] != want:
             raise ValueError(f"{name} must be [{want}][width]")
-        return Routed(place.data_ptr(), rows, slots, t.shape[1], F32 if t.dtype == torch.float32 else BF16)
+        return Routed(place.data_ptr(), rows, slots, shape[1], F32 if dtype is torch.float32 else BF16)
 
     def dispatch(self, x, plan: dict, out=None):
         """x [rows][width] (fp32 or bf16) laid out by member: out[place[r][k]] = x[r], [rows * slots][width].
@@ -850,46 +872,54 @@ class Context:
         self._enter()
         R = self._routed(plan, x, "x", False)
         shape = (R.rows * R.slots, R.width)
-        o = out if out is not None else x.new_empty(shape)
-        if out is not None:
+        if out is None:
+            out = x.new_empty(shape)
+        else:
             _check_tensor(out, "out", x.dtype, shape, self.device)
-        self._owned(o if out is None else None, x, plan["place"])
-        self._check(self.lib.sagips_dispatch(self.h, ctypes.byref(R), x.data_ptr(), o.data_ptr()))
-        return o
+        if not self._follow:
+            self._owned(out, x, plan["place"])
+        self._check(self.lib.sagips_dispatch(self.h, ctypes.byref(R), x.data_ptr(), out.data_ptr()))
+        return out
 
     def combine(self, y, plan: dict, weight=None, out=None):
         """Rows put back: out[r] = sum_k weight[r][k] y[place[r][k]], [rows][width], of y [rows * slots][width]
         (fp32 or bf16) and weight [rows][slots] fp32 (None: 1)."""
-        import torch
         self._enter()
         R = self._routed(plan, y, "y", True)
-        _check_tensor(weight, "weight", torch.float32, (R.rows, R.slots), self.device)
-        o = out if out is not None else y.new_empty((R.rows, R.width))
-        if out is not None:
+        if weight is not None:
+            _check_tensor(weight, "weight", self._torch.float32, (R.rows, R.slots), self.device)
+        if out is None:
+            out = y.new_empty((R.rows, R.width))
+        else:
             _check_tensor(out, "out", y.dtype, (R.rows, R.width), self.device)
-        self._owned(o if out is None else None, y, weight, plan["place"])
-        self._check(self.lib.sagips_combine(self.h, ctypes.byref(R), y.data_ptr(), _ptr(weight), o.data_ptr()))
-        return o
+        if not self._follow:
+            self._owned(out, y, weight, plan["place"])
+        self._check(self.lib.sagips_combine(self.h, ctypes.byref(R), y.data_ptr(), _ptr(weight), out.data_ptr()))
+        return out
 
     def combine_backward(self, dout, y, plan: dict, weight=None, want_dweight: bool = True, dy=None):
         """Gradient of combine: dy [rows * slots][width] (positions of no item are left as they were) and, if
         wanted, dweight [rows][slots], which alone needs y."""
-        import torch
         self._enter()
         R = self._routed(plan, dout, "dout", False)
-        shape = (R.rows * R.slots, R.width)
-        if want_dweight and y is None:
-            raise ValueError("dweight needs y")
-        _check_tensor(y, "y", dout.dtype, shape, self.device)
-        _check_tensor(weight, "weight", torch.float32, (R.rows, R.slots), self.device)
-        g = dy if dy is not None else dout.new_empty(shape)
-        if dy is not None:
+        shape, f32 = (R.rows * R.slots, R.width), self._torch.float32
+        if weight is not None:
+            _check_tensor(weight, "weight", f32, (R.rows, R.slots), self.device)
+        if dy is None:
+            dy = dout.new_empty(shape)
+        else:
             _check_tensor(dy, "dy", dout.dtype, shape, self.device)
-        dw = torch.empty((R.rows, R.slots), dtype=torch.float32, device=dout.device) if want_dweight else None
-        self._owned(g if dy is None else None, dw, dout, y, weight, plan["place"])
+        dw = None
+        if want_dweight:
+            if y is None:
+                raise ValueError("dweight needs y")
+            _check_tensor(y, "y", dout.dtype, shape, self.device)
+            dw = dout.new_empty((R.rows, R.slots), dtype=f32)
+        if not self._follow:
+            self._owned(dy, dw, dout, y, weight, plan["place"])
         self._check(self.lib.sagips_combine_backward(self.h, ctypes.byref(R), dout.data_ptr(), _ptr(y) if want_dweight else None,
-                                                     _ptr(weight), g.data_ptr(), _ptr(dw)))
-        return g, dw
+                                                     _ptr(weight), dy.data_ptr(), _ptr(dw)))
+        return dy, dw
 
     def gen_forward_routed(self, W: Sequence, b: Sequence, x, offsets, slope: float = 0.2, out=None):
         """theta [n][out] = 1 + softplus(G_m(x)) with the member m that each row of x [n][in] belongs to:
