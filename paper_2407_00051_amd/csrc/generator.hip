@@ -81,6 +81,7 @@ struct GenParams {
   const int32_t* offsets;
   int members;
   float* dx;                       // backward: dL/dnoise [k][in], or NULL
+  int* slots;                      // backward: [members][2]
 };
 
 // The rows of a tile: first, the first behind the member's rows, and what is added to a row for
@@ -96,22 +97,48 @@ __device__ __forceinline__ void member_rows(const GenParams& p, int m, int64_t& 
   hi = min(max((int64_t)p.offsets[m + 1], lo), p.k);
 }
 
-// Tiles of T rows of the members before `until`; and tile `want` of all (false: there are fewer).
-// A member a lane, 64 at a time; the whole wave calls it.
+// Tiles of T rows of all members.  A member a lane, 64 at a time; the whole wave calls it.  The workgroups of a
+// backward pass, of which number g takes the tiles from g tiles / groups on (groups: the grid, at most one
+// a tile), note in slots[m] = (first, number) the partials of the members between them: those of the
+// workgroups that have tiles of member m, tile t being workgroup ((t + 1) groups - 1) / tiles's.
 template <int T>
-__device__ __forceinline__ int64_t tiles_until(const GenParams& p, int until) {
+__device__ __forceinline__ int64_t write_slots(const GenParams& p) {
   const int lane = threadIdx.x & 63;
   int64_t n = 0;
-  for (int m0 = 0; m0 < until; m0 += 64) {
+  for (int m0 = 0; m0 < p.members; m0 += 64) {
     int64_t lo = 0, hi = 0;
-    if (m0 + lane < until) member_rows(p, m0 + lane, lo, hi);
+    if (m0 + lane < p.members) member_rows(p, m0 + lane, lo, hi);
     uint32_t t = (uint32_t)((hi - lo + T - 1) / T);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) t += (uint32_t)__shfl_xor((int)t, d, 64);
     n += t;
   }
+  if (blockIdx.x == 0 && threadIdx.x < 64) {
+    const int64_t groups = min(n, (int64_t)gridDim.x);
+    int64_t before = 0;
+    for (int m0 = 0; m0 < p.members; m0 += 64) {
+      const int m = m0 + lane;
+      int64_t lo = 0, hi = 0;
+      if (m < p.members) member_rows(p, m, lo, hi);
+      const uint32_t t = (uint32_t)((hi - lo + T - 1) / T);
+      uint32_t upto = t;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+        if (lane >= d) upto += o;
+      }
+      if (m < p.members) {
+        const int64_t t1 = before + upto, t0 = t1 - t;
+        const int64_t g0 = t ? min(((t0 + 1) * groups - 1) / n, groups - 1) : 0;
+        p.slots[2 * m] = (int)(g0 + m);
+        p.slots[2 * m + 1] = t ? (int)(min((t1 * groups - 1) / n, groups - 1) - g0) + 1 : 0;
+      }
+      before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+  }
   return n;
 }
+// Tile `want` of all; false: there are fewer.
 template <int T>
 __device__ __forceinline__ bool routed_tile(const GenParams& p, int64_t want, GenTile& out) {
   const int lane = threadIdx.x & 63;
@@ -309,7 +336,7 @@ struct Gen {
   // partials: g + m rises from each of its (g, m) to the next.
   static __device__ void run_backward_routed(const GenParams& p) {
     __shared__ Smem sm;
-    const int64_t tiles = tiles_until<kGT>(p, p.members);
+    const int64_t tiles = write_slots<kGT>(p);
     const int64_t groups = min(tiles, (int64_t)gridDim.x);
     const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     if (g >= groups) return;
@@ -451,9 +478,9 @@ __global__ __launch_bounds__(kGThreads, 1) void k_gen_backward(GenParams p) {
   Gen<H, NH, T>::run_backward(p);
 }
 
-template <int H, int NH, int T>
-__global__ __launch_bounds__(kGThreads, 1) void k_gen_backward_routed(GenParams p) {
-  Gen<H, NH, T>::run_backward_routed(p);
+template <int H, int NH>
+__global__ __launch_bounds__(kGThreads, 1) void k_gen_backward_routed16(GenParams p) {
+  Gen<H, NH, 16>::run_backward_routed(p);
 }
 
 template <int H, int NH, bool kRouted>
@@ -651,6 +678,345 @@ __global__ __launch_bounds__(kFwdThreads, 3) void k_gen_forward(GenParams p) {
   GenFwd<NH>::template run<kRouted>(p);
 }
 
+// Backward pass of members on rows of their own, on the bf16 matrix cores (split_bf16.hpp).  One workgroup
+// of 8 waves takes tiles of up to 64 rows of a member, in blocks of 32: wave (wf, we) owns features
+// [32 wf, 32 wf + 32) of block we, so that the two waves of a SIMD share its matrix core and one's vector
+// work runs beside the other's products; a tile of one block leaves the second wave idle and takes half the
+// time.  The activations A_1 .. A_NH live split in three buffers (144 KB); the top signal takes A_1's
+// place, which is formed again after it.  Every other signal overwrites the activation it belongs to.
+// Weights are split as they are read, row-wise for the forward pass, column-wise for the signals.
+// A weight gradient has K = the tile's rows; each wave forms 32 x 64 of it.
+template <int NH>
+struct GenBwd : SplitLds<128, 64> {
+  static constexpr int H = 128, KS = H / 16, PD = 6;
+  static constexpr int NBUF = NH < 3 ? NH + 1 : 3, kTop = NH < 3 ? NH : 0;
+  typedef GenFwd<NH> Fwd;
+  typedef typename Fwd::Raw Raw;
+
+  struct Smem {
+    char act[NBUF * BUF];
+    float n[kGMaxIO][64];          // inputs, transposed
+    float dout[kGMaxIO][64];       // dL/d(last pre-activation)
+    float op[4][kGMaxIO][64];      // sums over a wave's features; also [kGMaxIO][H] of the second block's waves
+    float dbs[2][2][H];            // [turn][we]: sums of a signal over a block's rows
+  };
+
+  // acc = act W^T (kT: act W) for the wave's features and block we.
+  template <bool kT>
+  static __device__ __forceinline__ void product(const float* __restrict__ W, const char* buf, const Lane& L, int we, f32x16& out) {
+    const float* wrow = kT ? W + 8 * L.lh * H + 32 * L.wf + L.lr : W + (32 * L.wf + L.lr) * H + 8 * L.lh;
+    f32x16 acc[1], corr[1];
+    Raw raw[PD + 1];
+    bf16x8 w[2][kTerms], a[2][1][kTerms];
+    auto load = [&](int ks) __attribute__((always_inline)) {
+      Raw& r = raw[ks % (PD + 1)];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if constexpr (kT) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) r[q][i] = wrow[(16 * ks + 4 * q + i) * H];
+        } else {
+          r[q] = *reinterpret_cast<const f32x4*>(wrow + 16 * ks + 4 * q);
+        }
+      }
+    };
+#pragma unroll
+    for (int q = 0; q < PD; ++q) load(q);
+    read_tr(buf, L, we, 0, a[0][0]);
+    Fwd::split_raw(raw[0], w[0]);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (ks + PD < KS) load(ks + PD);
+      if (ks + 1 < KS) {
+        read_tr(buf, L, we, ks + 1, a[(ks + 1) & 1][0]);
+        Fwd::split_raw(raw[(ks + 1) % (PD + 1)], w[(ks + 1) & 1]);
+      }
+      if (ks == 0) split_mfma_apart<true, false>(a[0], w[0], acc, corr);
+      else split_mfma_apart<false, false>(a[ks & 1], w[ks & 1], acc, corr);
+      interleave<kT ? 8 : 2, 8, 6>();
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    out = acc[0] + corr[0];
+  }
+
+  // dW rows 32 wf .., columns 64 we .. = (more: +=) signal^T A over `steps` times 16 rows.
+  static __device__ __forceinline__ void wgrad(const char* sig, const char* A, const Lane& L, int we, int steps, float* dW, bool more) {
+    f32x16 c[2] = {f32x16{}, f32x16{}}, d[2] = {f32x16{}, f32x16{}};
+    float* at = dW + (32 * L.wf + 4 * L.lh) * H + 64 * we + L.lr;
+    float old[2][16] = {};
+    if (more)                                        // read beside the products, all together
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) old[k][i] = at[(8 * (i / 4) + i % 4) * H + 32 * k];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s >= steps) break;
+      bf16x8 a[kTerms], b[2][kTerms];
+      read_ev(sig, L, L.wf, s, a);
+      read_ev(A, L, 2 * we, s, b[0]);
+      read_ev(A, L, 2 * we + 1, s, b[1]);
+      split_mfma2(b[0], b[1], a, c[0], c[1], d[0], d[1]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) at[(8 * (i / 4) + i % 4) * H + 32 * k] = old[k][i] + (c[k][i] + d[k][i]);
+  }
+
+  // Pre-activations of the first layer: the wave's features, 4 rows from `row` on.
+  static __device__ __forceinline__ void pre1(const Smem& sm, const float (&w0)[kGMaxIO], float b0, int row, float (&v)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = b0;
+#pragma unroll
+    for (int j = 0; j < kGMaxIO; ++j) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.n[j][row]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = fmaf(w0[j], x[q], v[q]);
+    }
+  }
+  static __device__ __forceinline__ void first_layer(Smem& sm, const float (&w0)[kGMaxIO], float b0, float slope, const Lane& L, int we) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Step d;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float h[4];
+        pre1(sm, w0, b0, 32 * we + 16 * s + 8 * u + 4 * L.lh, h);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) h[q] = g_leaky(h[q], slope);
+        split4(h, u, d);
+      }
+      store_step(sm.act, L, 2 * we + s, d);
+    }
+  }
+  // 16 values of the lane's feature (rows 32 we + 8 (i / 4) + 4 lh + i % 4), split, into a buffer.
+  static __device__ __forceinline__ void store_block(char* buf, const Lane& L, int we, const float (&v)[16]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      Step d;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float h[4] = {v[8 * s + 4 * u], v[8 * s + 4 * u + 1], v[8 * s + 4 * u + 2], v[8 * s + 4 * u + 3]};
+        split4(h, u, d);
+      }
+      store_step(buf, L, 2 * we + s, d);
+    }
+  }
+  // op[wf][j][row] = sum over the wave's features of v[i] w[j], two columns j at a time.
+  static __device__ __forceinline__ void over_features(Smem& sm, const Lane& L, int we, const float (&v)[16], const float (&w)[kGMaxIO], int n) {
+    const int i = L.lr & 15, row = 32 * we + 8 * (i >> 2) + 4 * L.lh + (i & 3);
+#pragma unroll
+    for (int j = 0; j < kGMaxIO; j += 2) {
+      if (j >= n) break;
+      float z[32];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) z[k] = v[k] * w[j], z[16 + k] = v[k] * w[j + 1];
+      sm.op[L.wf][j + (L.lr >> 4)][row] = half_scatter_sum(z, L.lr);
+    }
+  }
+  // The gradient of a layer with few columns: per column j the sum over the lane's rows of v[i] x[j][row]; the
+  // two blocks' waves meet in op.  In all threads; barriers inside.
+  template <typename Put>
+  static __device__ __forceinline__ void over_rows(Smem& sm, const Lane& L, int we, bool on, const float (&v)[16], const float (&x)[kGMaxIO][64],
+                                                   int n, float* dW, int stride_f, int stride_j, Put put) {
+    float (*stage)[H] = reinterpret_cast<float (*)[H]>(&sm.op[0][0][0]);
+    const int fo = 32 * L.wf + L.lr;
+    float s[kGMaxIO];
+#pragma unroll
+    for (int j = 0; j < kGMaxIO; ++j) {
+      s[j] = 0.0f;
+      if (on && j < n) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][32 * we + 8 * g + 4 * L.lh]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) s[j] = fmaf(v[4 * g + q], e[q], s[j]);
+        }
+      }
+      s[j] = add_xor32(s[j]);
+    }
+    __syncthreads();                                 // op is read
+    if (we == 1 && L.lh == 0)
+#pragma unroll
+      for (int j = 0; j < kGMaxIO; ++j) stage[j][fo] = s[j];
+    __syncthreads();
+    if (we == 0 && L.lh == 0)
+#pragma unroll
+      for (int j = 0; j < kGMaxIO; ++j)
+        if (j < n) put(dW + fo * stride_f + j * stride_j, s[j] + stage[j][fo]);
+  }
+
+  // A tile: `rows` (1 to 64) rows of member m from row0 on; its gradients to `part`, or added to what it holds.
+  static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, int m, int64_t row0, int rows, float* part, bool more) {
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), we = wave >> 2;
+    const Lane L = make_lane(wave & 3, 0);
+    const int fo = 32 * L.wf + L.lr, steps = rows > 32 ? 4 : 2;
+    const bool on = rows > 32 * we;                  // the wave has a block
+    const float slope = p.slope;
+    const auto put = [&](float* at, float v) __attribute__((always_inline)) { *at = more ? *at + v : v; };
+    const auto buf = [&](int i) __attribute__((always_inline)) { return &sm.act[i * BUF]; };
+    {   // thread (row, column)
+      const int ev = tid & 63, j = tid >> 6;
+      const bool here = ev < rows;
+      sm.n[j][ev] = here && j < p.in ? p.noise[(row0 + ev) * p.in + j] : 0.0f;
+      sm.dout[j][ev] = here && j < p.out ? p.dtheta[(row0 + ev) * p.out + j] : 0.0f;
+    }
+    float w0[kGMaxIO], wo[kGMaxIO], bh[NH];
+#pragma unroll
+    for (int j = 0; j < kGMaxIO; ++j) {
+      w0[j] = j < p.in ? p.W[0][m * p.wsz[0] + fo * p.in + j] : 0.0f;
+      wo[j] = j < p.out ? p.W[NH + 1][m * p.wsz[NH + 1] + j * H + fo] : 0.0f;
+    }
+    const float b0 = p.b[0][m * p.bsz[0] + fo];
+#pragma unroll
+    for (int l = 0; l < NH; ++l) bh[l] = p.b[1 + l][m * p.bsz[1 + l] + fo];
+    __syncthreads();
+    if (on) first_layer(sm, w0, b0, slope, L, we);
+    __syncthreads();
+    // ---- forward
+    uint32_t mask[NH];                               // bit i: value i of A_{l+2} positive
+    float v[16];
+#pragma unroll
+    for (int l = 0; l < NH; ++l) {
+      if (on) {
+        f32x16 acc;
+        product<false>(p.W[1 + l] + m * p.wsz[1 + l], buf(l), L, we, acc);
+        uint32_t k = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float z = acc[i] + bh[l];
+          k |= z > 0.0f ? 1u << i : 0u;
+          v[i] = g_leaky(z, slope);
+        }
+        mask[l] = k;
+        if (l < NH - 1) store_block(buf(l + 1), L, we, v);
+      }
+      if (l < NH - 1) __syncthreads();
+    }
+    // ---- output layer: v = A_{NH+1}
+    if (on) over_features(sm, L, we, v, wo, p.out);
+    __syncthreads();
+    {   // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
+      const int ev = tid & 63, j = tid >> 6;
+      float d = 0.0f;
+      if (ev < rows && j < p.out) {
+        const float o = p.b[NH + 1][m * p.bsz[NH + 1] + j] + ((sm.op[0][j][ev] + sm.op[1][j][ev]) + (sm.op[2][j][ev] + sm.op[3][j][ev]));
+        d = sm.dout[j][ev] * g_sigmoid(o);
+        sm.dout[j][ev] = d;
+      }
+      d = wave_total(d);
+      if ((tid & 63) == 0 && j < p.out) put(part + p.poff_b[NH + 1] + j, d);
+    }
+    __syncthreads();
+    over_rows(sm, L, we, on, v, sm.dout, p.out, part + p.poff_w[NH + 1], 1, H, put);
+    // ---- top signal
+    float sum = 0.0f;
+    if (on) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        float t[4] = {};
+#pragma unroll
+        for (int j = 0; j < kGMaxIO; ++j) {
+          const f32x4 e = *reinterpret_cast<const f32x4*>(&sm.dout[j][32 * we + 8 * g + 4 * L.lh]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) t[q] = fmaf(e[q], wo[j], t[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float d = mask[NH - 1] >> (4 * g + q) & 1 ? t[q] : slope * t[q];
+          v[4 * g + q] = d;
+          sum += d;
+        }
+      }
+      store_block(buf(kTop), L, we, v);
+    }
+    sum = add_xor32(sum);
+    if (L.lh == 0) sm.dbs[NH & 1][we][fo] = sum;
+    __syncthreads();
+    // ---- hidden layers: layer 1 + l maps A_{l+1} (buffer l) -> A_{l+2}
+#pragma unroll
+    for (int l = NH - 1; l >= 0; --l) {
+      const char* sig = buf(l == NH - 1 ? kTop : l + 1);
+      if (tid < H) put(part + p.poff_b[1 + l] + tid, sm.dbs[(l + 1) & 1][0][tid] + sm.dbs[(l + 1) & 1][1][tid]);
+      wgrad(sig, buf(l), L, we, steps, part + p.poff_w[1 + l], more);
+      f32x16 acc;
+      if (on) product<true>(p.W[1 + l] + m * p.wsz[1 + l], sig, L, we, acc);
+      sum = 0.0f;
+      if (l > 0) {
+        if (on) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            v[i] = mask[l - 1] >> i & 1 ? acc[i] : slope * acc[i];
+            sum += v[i];
+          }
+        }
+        sum = add_xor32(sum);
+        if (L.lh == 0) sm.dbs[l & 1][we][fo] = sum;
+        __syncthreads();                             // every wave is done with buffer l and the signal
+        if (on) {
+          store_block(buf(l), L, we, v);
+          if (kTop == 0 && l == NH - 1) first_layer(sm, w0, b0, slope, L, we);
+        }
+        __syncthreads();
+      } else {
+        if (on) {
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            float z[4];
+            pre1(sm, w0, b0, 32 * we + 8 * g + 4 * L.lh, z);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              v[4 * g + q] = z[q] > 0.0f ? acc[4 * g + q] : slope * acc[4 * g + q];
+              sum += v[4 * g + q];
+            }
+          }
+        }
+        sum = add_xor32(sum);
+        if (L.lh == 0) sm.dbs[0][we][fo] = sum;
+      }
+    }
+    // ---- first layer: v = delta_1
+    over_rows(sm, L, we, on, v, sm.n, p.in, part + p.poff_w[0], p.in, 1, put);   // (its barriers cover dbs)
+    if (tid < H) put(part + p.poff_b[0] + tid, sm.dbs[0][0][tid] + sm.dbs[0][1][tid]);
+    if (p.dx) {
+      __syncthreads();                               // stage is read
+      if (on) over_features(sm, L, we, v, w0, p.in);
+      __syncthreads();
+      const int ev = tid & 63, j = tid >> 6;
+      if (ev < rows && j < p.in)
+        p.dx[(row0 + ev) * p.in + j] = (sm.op[0][j][ev] + sm.op[1][j][ev]) + (sm.op[2][j][ev] + sm.op[3][j][ev]);
+    }
+  }
+
+  // Of the `blocks` blocks of 32 rows in the order of their rows, workgroup g of `groups` (at most one a
+  // block) takes those from g blocks / groups on, two of a member together, and adds up what it has of a
+  // member in slot g + m of the partials: g + m rises from each of its (g, m) to the next.
+  static __device__ void run(const GenParams& p) {
+    __shared__ __attribute__((aligned(1024))) Smem sm;
+    const int64_t blocks = write_slots<32>(p);
+    const int64_t groups = min(blocks, (int64_t)gridDim.x);
+    const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (g >= groups) return;
+    int last = -1;
+    for (int64_t i = g * blocks / groups, end = (g + 1) * blocks / groups; i < end;) {
+      GenTile t;
+      if (!routed_tile<32>(p, i, t)) return;         // (there is one)
+      const int rows = (int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32));
+      __syncthreads();                               // the tile before is read
+      tile(p, sm, t.m, t.row0, rows, p.part + (g + t.m) * p.P, t.m == last);
+      last = t.m;
+      i += rows > 32 ? 2 : 1;
+    }
+  }
+};
+
+template <int NH>
+__global__ __launch_bounds__(kGThreads, 1) void k_gen_backward_routed(GenParams p) {
+  GenBwd<NH>::run(p);
+}
+
 // Sum of the per-tile partials of member blockIdx.y in a fixed order, scattered
 // to the caller's gradient arrays.
 struct GenReduceArgs {
@@ -708,23 +1074,16 @@ __global__ __launch_bounds__(256) void k_gen_reduce(GenReduceArgs r) {
   }
 }
 
-// The same for k_gen_backward_routed: member blockIdx.y's partials are the slots g + m of the workgroups
-// g that had tiles of it, in their order.
-template <int T>
-__global__ __launch_bounds__(256) void k_gen_reduce_routed(GenReduceArgs r, GenParams p, int grid) {
+// The same for members on rows of their own: member blockIdx.y's partials are slots[m]'s.
+__global__ __launch_bounds__(256) void k_gen_reduce_routed(GenReduceArgs r, const int* __restrict__ slots) {
   constexpr int S = 4, C = 256 / S;
   __shared__ float red[S][C];
-  const int m = blockIdx.y;
-  const int64_t all = tiles_until<T>(p, p.members), t0 = tiles_until<T>(p, m), t1 = tiles_until<T>(p, m + 1);
-  const int64_t groups = min(all, (int64_t)grid);
-  // tile t is workgroup ((t + 1) groups - 1) / all's
-  const int64_t g0 = t1 > t0 ? ((t0 + 1) * groups - 1) / all : 0;
-  const int n = t1 > t0 ? (int)min((t1 * groups - 1) / all - g0 + 1, groups - g0) : 0;
+  const int m = blockIdx.y, first = slots[2 * m], n = slots[2 * m + 1];
   const int le = threadIdx.x % C, sl = threadIdx.x / C;
   const int64_t e = (int64_t)blockIdx.x * C + le;
   float v = 0.f;
   if (e < r.P) {
-    const float* src = r.part + (g0 + m) * r.P + e;
+    const float* src = r.part + (int64_t)first * r.P + e;
     int t = sl;
     for (; t + 4 * S < n; t += 8 * S) add_tiles<S, 8>(src, t, n, r.P, v);
     if (t + 2 * S < n) add_tiles<S, 4>(src, t, n, r.P, v);
@@ -847,7 +1206,7 @@ struct GenVariant {
     H_, NH_, {k_gen_forward<NH_, false>, k_gen_forward16<H_, NH_, false>},       \
         {k_gen_backward<H_, NH_, 64>, k_gen_backward<H_, NH_, 16> },             \
         {k_gen_forward<NH_, true>, k_gen_forward16<H_, NH_, true>},              \
-        {k_gen_backward_routed<H_, NH_, 64>, k_gen_backward_routed<H_, NH_, 16> } \
+        {k_gen_backward_routed<NH_>, k_gen_backward_routed16<H_, NH_>}            \
   }
 
 const GenVariant kGenVariants[] = {SAGIPS_GEN_VARIANT(128, 1), SAGIPS_GEN_VARIANT(128, 2), SAGIPS_GEN_VARIANT(128, 3)};
@@ -972,14 +1331,15 @@ inline int routed_rows(int64_t k, int n_cu) { return k / 64 >= n_cu / 2 ? 64 : 1
 inline int64_t routed_tiles(const sagips_gen& G, int64_t k, int T) { return k / T + (G.n_members < k ? G.n_members : k); }
 // Workgroups of the backward pass, a multiple of 8.
 inline int routed_groups(const sagips_gen& G, int64_t k, int T, int n_cu) {
-  const int64_t t = routed_tiles(G, k, T), most = (n_cu + 7) / 8 * 8;
+  const int64_t t = routed_tiles(G, k, T == 64 ? 32 : 16), most = (n_cu + 7) / 8 * 8;
   return (int)(t < most ? (t + 7) / 8 * 8 : most);
 }
 }  // namespace
 
 size_t gen_backward_routed_workspace(const sagips_gen& G, int64_t k, int n_cu) {
   const GenParams p = gen_params(G, nullptr, k);
-  return sizeof(float) * (size_t)p.P * (routed_groups(G, k, routed_rows(k, n_cu), n_cu) + G.n_members);
+  const size_t partials = routed_groups(G, k, routed_rows(k, n_cu), n_cu) + (size_t)G.n_members;
+  return sizeof(float) * (size_t)p.P * partials + sizeof(int) * 2 * (size_t)G.n_members;
 }
 
 hipError_t launch_gen_forward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k, float* theta,
@@ -1008,6 +1368,7 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
   p.dx = dx;
   const GenVariant* v = find_gen(G);
   const int T = routed_rows(k, n_cu), groups = routed_groups(G, k, T, n_cu);
+  p.slots = reinterpret_cast<int*>(p.part + (size_t)p.P * (groups + (size_t)G.n_members));
   if (tm) tm->begin("gen_backward_routed");
   hipLaunchKernelGGL(v->bwd_routed[T == 64 ? 0 : 1], dim3(groups), dim3(kGThreads), 0, st, p);
   if (tm) tm->end();
@@ -1016,8 +1377,7 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
   const GenReduceArgs r = reduce_args(G, p, 0, dW, db);
   const dim3 grid((unsigned)((p.P + 63) / 64), G.n_members);
   if (tm) tm->begin("gen_reduce_routed");
-  if (T == 64) hipLaunchKernelGGL(k_gen_reduce_routed<64>, grid, dim3(256), 0, st, r, p, groups);
-  else hipLaunchKernelGGL(k_gen_reduce_routed<16>, grid, dim3(256), 0, st, r, p, groups);
+  hipLaunchKernelGGL(k_gen_reduce_routed, grid, dim3(256), 0, st, r, p.slots);
   if (tm) tm->end();
   return hipGetLastError();
 }
