@@ -848,6 +848,13 @@ struct GenBwd : SplitLds<128, 64> {
         if (j < n) put(dW + fo * stride_f + j * stride_j, s[j] + stage[j][fo]);
   }
 
+  // Hidden-to-hidden layer l's array (a choice among registers: an index would go through memory), and where
+  // its gradients begin in a partial.
+  static __device__ __forceinline__ const float* hidden(const float* const (&a)[kMaxGenLayers], int l) {
+    return NH == 1 || l == 0 ? a[1] : NH == 2 || l == 1 ? a[2] : a[3];
+  }
+  static __device__ __forceinline__ int at_layer(int in, int l) { return H * in + H + l * (H * H + H); }
+
   // A tile: `rows` (1 to 64) rows of member m from row0 on; its gradients to `part`, or added to what it holds.
   static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, int m, int64_t row0, int rows, float* part, bool more) {
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), we = wave >> 2;
@@ -863,34 +870,34 @@ struct GenBwd : SplitLds<128, 64> {
       sm.n[j][ev] = here && j < p.in ? p.noise[(row0 + ev) * p.in + j] : 0.0f;
       sm.dout[j][ev] = here && j < p.out ? p.dtheta[(row0 + ev) * p.out + j] : 0.0f;
     }
-    float w0[kGMaxIO], wo[kGMaxIO], bh[NH];
+    float w0[kGMaxIO], wo[kGMaxIO];
 #pragma unroll
     for (int j = 0; j < kGMaxIO; ++j) {
       w0[j] = j < p.in ? p.W[0][m * p.wsz[0] + fo * p.in + j] : 0.0f;
       wo[j] = j < p.out ? p.W[NH + 1][m * p.wsz[NH + 1] + j * H + fo] : 0.0f;
     }
     const float b0 = p.b[0][m * p.bsz[0] + fo];
-#pragma unroll
-    for (int l = 0; l < NH; ++l) bh[l] = p.b[1 + l][m * p.bsz[1 + l] + fo];
     __syncthreads();
     if (on) first_layer(sm, w0, b0, slope, L, we);
     __syncthreads();
-    // ---- forward
-    uint32_t mask[NH];                               // bit i: value i of A_{l+2} positive
+    // ---- forward.  The layers' loops stay loops: unrolled, a tile is 88 KB of code, more than the
+    // instruction cache holds.
+    uint64_t mask = 0;                               // bit 16 l + i: value i of A_{l+2} positive
     float v[16];
-#pragma unroll
+#pragma unroll 1
     for (int l = 0; l < NH; ++l) {
       if (on) {
         f32x16 acc;
-        product<false>(p.W[1 + l] + m * p.wsz[1 + l], buf(l), L, we, acc);
+        const float bh = hidden(p.b, l)[m * (int64_t)H + fo];
+        product<false>(hidden(p.W, l) + m * (int64_t)(H * H), buf(l), L, we, acc);
         uint32_t k = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float z = acc[i] + bh[l];
+          const float z = acc[i] + bh;
           k |= z > 0.0f ? 1u << i : 0u;
           v[i] = g_leaky(z, slope);
         }
-        mask[l] = k;
+        mask |= (uint64_t)k << 16 * l;
         if (l < NH - 1) store_block(buf(l + 1), L, we, v);
       }
       if (l < NH - 1) __syncthreads();
@@ -925,7 +932,7 @@ struct GenBwd : SplitLds<128, 64> {
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const float d = mask[NH - 1] >> (4 * g + q) & 1 ? t[q] : slope * t[q];
+          const float d = mask >> (16 * (NH - 1) + 4 * g + q) & 1 ? t[q] : slope * t[q];
           v[4 * g + q] = d;
           sum += d;
         }
@@ -936,19 +943,20 @@ struct GenBwd : SplitLds<128, 64> {
     if (L.lh == 0) sm.dbs[NH & 1][we][fo] = sum;
     __syncthreads();
     // ---- hidden layers: layer 1 + l maps A_{l+1} (buffer l) -> A_{l+2}
-#pragma unroll
+#pragma unroll 1
     for (int l = NH - 1; l >= 0; --l) {
       const char* sig = buf(l == NH - 1 ? kTop : l + 1);
-      if (tid < H) put(part + p.poff_b[1 + l] + tid, sm.dbs[(l + 1) & 1][0][tid] + sm.dbs[(l + 1) & 1][1][tid]);
-      wgrad(sig, buf(l), L, we, steps, part + p.poff_w[1 + l], more);
+      float* dW = part + at_layer(p.in, l);
+      if (tid < H) put(dW + H * H + tid, sm.dbs[(l + 1) & 1][0][tid] + sm.dbs[(l + 1) & 1][1][tid]);
+      wgrad(sig, buf(l), L, we, steps, dW, more);
       f32x16 acc;
-      if (on) product<true>(p.W[1 + l] + m * p.wsz[1 + l], sig, L, we, acc);
+      if (on) product<true>(hidden(p.W, l) + m * (int64_t)(H * H), sig, L, we, acc);
       sum = 0.0f;
       if (l > 0) {
         if (on) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            v[i] = mask[l - 1] >> i & 1 ? acc[i] : slope * acc[i];
+            v[i] = mask >> (16 * l - 16 + i) & 1 ? acc[i] : slope * acc[i];
             sum += v[i];
           }
         }
