@@ -82,6 +82,7 @@ struct GenParams {
   int members;
   float* dx;                       // backward: dL/dnoise [k][in], or NULL
   int* slots;                      // backward: [members][2]
+  const u16* split;                // backward, 64-row tiles: split copies of the hidden layers
 };
 
 // The rows of a tile: first, the first behind the member's rows, and what is added to a row for
@@ -678,121 +679,122 @@ __global__ __launch_bounds__(kFwdThreads, 3) void k_gen_forward(GenParams p) {
   GenFwd<NH>::template run<kRouted>(p);
 }
 
-// Backward pass of members on rows of their own, on the bf16 matrix cores (split_bf16.hpp).  One workgroup
-// of 8 waves takes tiles of up to 64 rows of a member, in blocks of 32: wave (wf, we) owns features
-// [32 wf, 32 wf + 32) of block we, so that the two waves of a SIMD share its matrix core and one's vector
-// work runs beside the other's products; a tile of one block leaves the second wave idle and takes half the
-// time.  The activations A_1 .. A_NH live split in three buffers (144 KB); the top signal takes A_1's
-// place, which is formed again after it.  Every other signal overwrites the activation it belongs to.
-// Weights are split as they are read, row-wise for the forward pass, column-wise for the signals.
-// A weight gradient has K = the tile's rows; each wave forms 32 x 64 of it.
+// Split copies (split_bf16.hpp) of every member's hidden-to-hidden layers: of member m and layer l the copy
+// of W at (2 NH m + l), that of W^T at (2 NH m + NH + l).  blockIdx.y = copy, blockIdx.z = member.
+__global__ __launch_bounds__(256) void k_split_members(GenParams p, u16* out, int NH) {
+  constexpr int H = 128, KS = H / 16;
+  const int t = blockIdx.x * 256 + threadIdx.x, lane = t % 64, ks = t / 64 % KS, nb = t / (64 * KS);
+  const int copy = blockIdx.y, l = copy % NH, m = blockIdx.z;
+  const float* W = (l == 0 ? p.W[1] : l == 1 ? p.W[2] : p.W[3]) + (int64_t)m * H * H;
+  const int n = 32 * nb + (lane & 31), k0 = 16 * ks + 8 * (lane >> 5);
+  float v[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q) v[q] = copy >= NH ? W[(k0 + q) * H + n] : W[n * H + k0 + q];
+  split_piece(v, out + ((size_t)m * 2 * NH + copy) * (split_copy_bytes(H) / 2), nb, ks, KS, lane);
+}
+
+// Backward pass of members on rows of their own, on the bf16 matrix cores.  One workgroup of 8 waves takes
+// tiles of up to 64 rows of a member, in blocks of 32: wave (wf, we) owns features [32 wf, 32 wf + 32) of
+// block we, so that the two waves of a SIMD share its matrix core and one's vector work runs beside the
+// other's products; a tile of one block leaves the second wave idle and takes half the time.  The
+// activations A_1 .. A_NH live split in three buffers (144 KB); the top signal takes A_1's place, which is
+// formed again after it.  Every other signal overwrites the activation it belongs to.  Weights come split
+// (k_split_members): splitting them as they are read took as long as the products.  A weight
+// gradient has K = the tile's rows; each wave has 32 x 64 of it, in the accumulation registers
+// for as long as the workgroup stays with a member.
 template <int NH>
 struct GenBwd : SplitLds<128, 64> {
-  static constexpr int H = 128, KS = H / 16, PD = 6;
+  static constexpr int H = 128, KS = H / 16, PD = 2;
   static constexpr int NBUF = NH < 3 ? NH + 1 : 3, kTop = NH < 3 ? NH : 0;
-  typedef GenFwd<NH> Fwd;
-  typedef typename Fwd::Raw Raw;
+  static constexpr int kCopy = (int)split_copy_bytes(H);
 
   struct Smem {
     char act[NBUF * BUF];
     float n[kGMaxIO][64];          // inputs, transposed
     float dout[kGMaxIO][64];       // dL/d(last pre-activation)
-    float op[4][kGMaxIO][64];      // sums over a wave's features; also [kGMaxIO][H] of the second block's waves
-    float dbs[2][2][H];            // [turn][we]: sums of a signal over a block's rows
+    float w0[kGMaxIO][H];          // the member's first layer, transposed, and its last
+    float wo[kGMaxIO][H];
+  };
+  // The wave and the lane, and the lane's offsets in a buffer.
+  struct Me {
+    int lane, lr, lh, wf, we, fo;
+    uint32_t w[4], own[2], tr[2];  // unit of a 16-row step; of the block's two steps; transposed reads of the block
+  };
+  // Offsets for one phase: kept from phase to phase, what the compiler forms of them beforehand would
+  // take more registers than there are.
+  static __device__ __forceinline__ uint32_t fresh(uint32_t o) {
+    asm volatile("" : "+v"(o));
+    return o;
+  }
+  // Sums over the rows of the lane's feature that a wave keeps of a member.
+  struct Sums {
+    f32x16 W[NH][2];               // rows 32 wf .., columns 64 we .. of a hidden layer's gradient
+    float b[NH + 1], in[kGMaxIO], out[kGMaxIO], bo;
+  };
+  struct Prefetch {
+    bf16x8 w[PD][kTerms];          // the next product's first weight steps
   };
 
-  // acc = act W^T (kT: act W) for the wave's features and block we.
-  template <bool kT>
-  static __device__ __forceinline__ void product(const float* __restrict__ W, const char* buf, const Lane& L, int we, f32x16& out) {
-    const float* wrow = kT ? W + 8 * L.lh * H + 32 * L.wf + L.lr : W + (32 * L.wf + L.lr) * H + 8 * L.lh;
+  static __device__ __forceinline__ void load_w(Rsrc R, uint32_t woff, int copy, int ks, bf16x8 (&w)[kTerms]) {
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) w[t] = split_load(R, woff + t * 1024u, (uint32_t)(copy * kCopy + ks * kTerms * 1024));
+  }
+  static __device__ __forceinline__ void read_rows(const char* at0, const char* at1, int ks, bf16x8 (&a)[kTerms]) {
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) {
+      const int o = t * PL + ks * 16 * RB;
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at0 + o));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at1 + o));
+      a[t] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  }
+
+  // out = act B for the wave's features and block, B the given split copy; pf holds the copy's first steps, and in
+  // the end those of `next`.
+  static __device__ __forceinline__ void product(Rsrc R, int copy, int next, uint32_t woff, Prefetch& pf, const char* buf, const Me& L,
+                                                 f32x16& out) {
     f32x16 acc[1], corr[1];
-    Raw raw[PD + 1];
-    bf16x8 w[2][kTerms], a[2][1][kTerms];
-    auto load = [&](int ks) __attribute__((always_inline)) {
-      Raw& r = raw[ks % (PD + 1)];
+    bf16x8 w[PD + 1][kTerms], a[2][1][kTerms];
+    const char *at0 = buf + fresh(L.tr[0]), *at1 = buf + fresh(L.tr[1]);
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        if constexpr (kT) {
+    for (int q = 0; q < PD; ++q)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) r[q][i] = wrow[(16 * ks + 4 * q + i) * H];
-        } else {
-          r[q] = *reinterpret_cast<const f32x4*>(wrow + 16 * ks + 4 * q);
-        }
-      }
-    };
-#pragma unroll
-    for (int q = 0; q < PD; ++q) load(q);
-    read_tr(buf, L, we, 0, a[0][0]);
-    Fwd::split_raw(raw[0], w[0]);
+      for (int t = 0; t < kTerms; ++t) w[q][t] = pf.w[q][t];
+    read_rows(at0, at1, 0, a[0][0]);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       __builtin_amdgcn_sched_barrier(0);
-      if (ks + PD < KS) load(ks + PD);
-      if (ks + 1 < KS) {
-        read_tr(buf, L, we, ks + 1, a[(ks + 1) & 1][0]);
-        Fwd::split_raw(raw[(ks + 1) % (PD + 1)], w[(ks + 1) & 1]);
-      }
-      if (ks == 0) split_mfma_apart<true, false>(a[0], w[0], acc, corr);
-      else split_mfma_apart<false, false>(a[ks & 1], w[ks & 1], acc, corr);
-      interleave<kT ? 8 : 2, 8, 6>();
+      if (ks + PD < KS) load_w(R, woff, copy, ks + PD, w[(ks + PD) % (PD + 1)]);
+      else load_w(R, woff, next, ks + PD - KS, pf.w[ks + PD - KS]);
+      if (ks + 1 < KS) read_rows(at0, at1, ks + 1, a[(ks + 1) & 1][0]);
       __builtin_amdgcn_sched_barrier(0);
+      if (ks == 0) split_mfma_apart<true, false>(a[0], w[0], acc, corr);
+      else split_mfma_apart<false, false>(a[ks & 1], w[ks % (PD + 1)], acc, corr);
     }
+    __builtin_amdgcn_sched_barrier(0);
     out = acc[0] + corr[0];
   }
 
-  // dW rows 32 wf .., columns 64 we .. = (more: +=) signal^T A over `steps` times 16 rows.
-  static __device__ __forceinline__ void wgrad(const char* sig, const char* A, const Lane& L, int we, int steps, float* dW, bool more) {
-    f32x16 c[2] = {f32x16{}, f32x16{}}, d[2] = {f32x16{}, f32x16{}};
-    float* at = dW + (32 * L.wf + 4 * L.lh) * H + 64 * we + L.lr;
-    float old[2][16] = {};
-    if (more)                                        // read beside the products, all together
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) old[k][i] = at[(8 * (i / 4) + i % 4) * H + 32 * k];
+  // W += signal^T A over `steps` times 16 rows.
+  static __device__ __forceinline__ void wgrad(const char* sig, const char* A, const Me& L, int steps, f32x16 (&W)[2]) {
+    const uint32_t row = fresh((uint32_t)L.wf * 32 * RB), col = fresh((uint32_t)L.we * 64 * RB);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       if (s >= steps) break;
       bf16x8 a[kTerms], b[2][kTerms];
-      read_ev(sig, L, L.wf, s, a);
-      read_ev(A, L, 2 * we, s, b[0]);
-      read_ev(A, L, 2 * we + 1, s, b[1]);
-      split_mfma2(b[0], b[1], a, c[0], c[1], d[0], d[1]);
+      const uint32_t o = fresh(L.w[s]);
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) {
+        a[t] = *reinterpret_cast<const bf16x8*>(sig + (o + row) + t * PL);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) b[k][t] = *reinterpret_cast<const bf16x8*>(A + (o + col) + t * PL + k * 32 * RB);
+      }
+      split_mfma2(b[0], b[1], a, W[0], W[1], W[0], W[1]);
     }
-#pragma unroll
-    for (int k = 0; k < 2; ++k)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) at[(8 * (i / 4) + i % 4) * H + 32 * k] = old[k][i] + (c[k][i] + d[k][i]);
   }
 
-  // Pre-activations of the first layer: the wave's features, 4 rows from `row` on.
-  static __device__ __forceinline__ void pre1(const Smem& sm, const float (&w0)[kGMaxIO], float b0, int row, float (&v)[4]) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = b0;
-#pragma unroll
-    for (int j = 0; j < kGMaxIO; ++j) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.n[j][row]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] = fmaf(w0[j], x[q], v[q]);
-    }
-  }
-  static __device__ __forceinline__ void first_layer(Smem& sm, const float (&w0)[kGMaxIO], float b0, float slope, const Lane& L, int we) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      Step d;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float h[4];
-        pre1(sm, w0, b0, 32 * we + 16 * s + 8 * u + 4 * L.lh, h);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) h[q] = g_leaky(h[q], slope);
-        split4(h, u, d);
-      }
-      store_step(sm.act, L, 2 * we + s, d);
-    }
-  }
   // 16 values of the lane's feature (rows 32 we + 8 (i / 4) + 4 lh + i % 4), split, into a buffer.
-  static __device__ __forceinline__ void store_block(char* buf, const Lane& L, int we, const float (&v)[16]) {
+  static __device__ __forceinline__ void store_block(char* buf, const Me& L, const float (&v)[16]) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       Step d;
@@ -801,221 +803,268 @@ struct GenBwd : SplitLds<128, 64> {
         const float h[4] = {v[8 * s + 4 * u], v[8 * s + 4 * u + 1], v[8 * s + 4 * u + 2], v[8 * s + 4 * u + 3]};
         split4(h, u, d);
       }
-      store_step(buf, L, 2 * we + s, d);
+      char* at = buf + fresh(L.own[s] + (uint32_t)L.wf * 32 * RB);
+#pragma unroll
+      for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(at + t * PL) = make_uint4(d[t][0], d[t][1], d[t][2], d[t][3]);
     }
   }
-  // op[wf][j][row] = sum over the wave's features of v[i] w[j], two columns j at a time.
-  static __device__ __forceinline__ void over_features(Smem& sm, const Lane& L, int we, const float (&v)[16], const float (&w)[kGMaxIO], int n) {
-    const int i = L.lr & 15, row = 32 * we + 8 * (i >> 2) + 4 * L.lh + (i & 3);
+  // v[i] = c + sum_j w[j][fo] x[j][row]: a layer of few inputs, for the wave's features and rows.
+  static __device__ __forceinline__ void from_few(const float (&w)[kGMaxIO][H], const float (&x)[kGMaxIO][64], float c, int n, const Me& L,
+                                                  float (&v)[16]) {
 #pragma unroll
-    for (int j = 0; j < kGMaxIO; j += 2) {
-      if (j >= n) break;
+    for (int i = 0; i < 16; ++i) v[i] = c;
+    const int o = (int)fresh((uint32_t)(32 * L.we + 4 * L.lh)), f = (int)fresh((uint32_t)L.fo);
+#pragma unroll 1
+    for (int j = 0; j < n; ++j) {
+      const float wj = w[j][f];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][o + 8 * g]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[4 * g + q] = fmaf(wj, e[q], v[4 * g + q]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void first_layer(Smem& sm, float b0, int in, float slope, const Me& L) {
+    float v[16];
+    from_few(sm.w0, sm.n, b0, in, L, v);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = g_leaky(v[i], slope);
+    store_block(sm.act, L, v);
+  }
+  // op[wf][j][row] = sum over the wave's features of v[i] w[j][fo], two columns j at a time.
+  typedef float Op[kGMaxIO][64];
+  static __device__ __forceinline__ void over_features(Op* op, const Me& L, const float (&v)[16], const float (&w)[kGMaxIO][H], int n) {
+    const int i = L.lr & 15, row = 32 * L.we + 8 * (i >> 2) + 4 * L.lh + (i & 3), f = (int)fresh((uint32_t)L.fo);
+#pragma unroll 1
+    for (int j = 0; j < n; j += 2) {
+      const float wa = w[j][f], wb = w[j + 1][f];    // the rows behind the last are 0
       float z[32];
 #pragma unroll
-      for (int k = 0; k < 16; ++k) z[k] = v[k] * w[j], z[16 + k] = v[k] * w[j + 1];
-      sm.op[L.wf][j + (L.lr >> 4)][row] = half_scatter_sum(z, L.lr);
+      for (int k = 0; k < 16; ++k) z[k] = v[k] * wa, z[16 + k] = v[k] * wb;
+      op[L.wf][j + (L.lr >> 4)][row] = half_scatter_sum(z, L.lr);
     }
   }
-  // The gradient of a layer with few columns: per column j the sum over the lane's rows of v[i] x[j][row]; the
-  // two blocks' waves meet in op.  In all threads; barriers inside.
-  template <typename Put>
-  static __device__ __forceinline__ void over_rows(Smem& sm, const Lane& L, int we, bool on, const float (&v)[16], const float (&x)[kGMaxIO][64],
-                                                   int n, float* dW, int stride_f, int stride_j, Put put) {
-    float (*stage)[H] = reinterpret_cast<float (*)[H]>(&sm.op[0][0][0]);
-    const int fo = 32 * L.wf + L.lr;
-    float s[kGMaxIO];
+  // s[j] += the sum over the lane's rows of v[i] x[j][row].
+  static __device__ __forceinline__ void over_rows(const Me& L, const float (&v)[16], const float (&x)[kGMaxIO][64], int n,
+                                                   float (&s)[kGMaxIO]) {
+    const int o = (int)fresh((uint32_t)(32 * L.we + 4 * L.lh));
 #pragma unroll
     for (int j = 0; j < kGMaxIO; ++j) {
-      s[j] = 0.0f;
-      if (on && j < n) {
+      if (j >= n) break;
+      float t = 0.0f;
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][32 * we + 8 * g + 4 * L.lh]);
+      for (int g = 0; g < 4; ++g) {
+        const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][o + 8 * g]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) s[j] = fmaf(v[4 * g + q], e[q], s[j]);
-        }
+        for (int q = 0; q < 4; ++q) t = fmaf(v[4 * g + q], e[q], t);
       }
-      s[j] = add_xor32(s[j]);
+      s[j] += t;
     }
-    __syncthreads();                                 // op is read
-    if (we == 1 && L.lh == 0)
+  }
+  static __device__ __forceinline__ float total_of(const float (&v)[16]) {
+    float t = 0.0f;
 #pragma unroll
-      for (int j = 0; j < kGMaxIO; ++j) stage[j][fo] = s[j];
-    __syncthreads();
-    if (we == 0 && L.lh == 0)
-#pragma unroll
-      for (int j = 0; j < kGMaxIO; ++j)
-        if (j < n) put(dW + fo * stride_f + j * stride_j, s[j] + stage[j][fo]);
+    for (int g = 0; g < 4; ++g) t += (v[4 * g] + v[4 * g + 1]) + (v[4 * g + 2] + v[4 * g + 3]);
+    return t;
   }
 
-  // Hidden-to-hidden layer l's array (a choice among registers: an index would go through memory), and where
-  // its gradients begin in a partial.
-  static __device__ __forceinline__ const float* hidden(const float* const (&a)[kMaxGenLayers], int l) {
-    return NH == 1 || l == 0 ? a[1] : NH == 2 || l == 1 ? a[2] : a[3];
-  }
-  static __device__ __forceinline__ int at_layer(int in, int l) { return H * in + H + l * (H * H + H); }
-
-  // A tile: `rows` (1 to 64) rows of member m from row0 on; its gradients to `part`, or added to what it holds.
-  static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, int m, int64_t row0, int rows, float* part, bool more) {
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), we = wave >> 2;
-    const Lane L = make_lane(wave & 3, 0);
-    const int fo = 32 * L.wf + L.lr, steps = rows > 32 ? 4 : 2;
-    const bool on = rows > 32 * we;                  // the wave has a block
+  // A tile: `rows` (1 to 64) rows of member m from row0 on.  b0, bh: the member's biases of the lane's feature.
+  static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, const Me& L, int m, int64_t row0, int rows, Rsrc R, float b0,
+                                              const float (&bh)[NH], Prefetch& pf, Sums& S) {
+    const int tid = threadIdx.x, steps = rows > 32 ? 4 : 2;
+    const uint32_t woff = (uint32_t)(L.wf * KS * kTerms * 64 + L.lane) * 16u;
+    const bool on = rows > 32 * L.we;                // the wave has a block
     const float slope = p.slope;
-    const auto put = [&](float* at, float v) __attribute__((always_inline)) { *at = more ? *at + v : v; };
     const auto buf = [&](int i) __attribute__((always_inline)) { return &sm.act[i * BUF]; };
-    {   // thread (row, column)
-      const int ev = tid & 63, j = tid >> 6;
+    const int ev = tid & 63, col = tid >> 6;         // a thread's row and column of the inputs and outputs
+    {
       const bool here = ev < rows;
-      sm.n[j][ev] = here && j < p.in ? p.noise[(row0 + ev) * p.in + j] : 0.0f;
-      sm.dout[j][ev] = here && j < p.out ? p.dtheta[(row0 + ev) * p.out + j] : 0.0f;
+      sm.n[col][ev] = here && col < p.in ? p.noise[(row0 + ev) * p.in + col] : 0.0f;
+      sm.dout[col][ev] = here && col < p.out ? p.dtheta[(row0 + ev) * p.out + col] : 0.0f;
     }
-    float w0[kGMaxIO], wo[kGMaxIO];
-#pragma unroll
-    for (int j = 0; j < kGMaxIO; ++j) {
-      w0[j] = j < p.in ? p.W[0][m * p.wsz[0] + fo * p.in + j] : 0.0f;
-      wo[j] = j < p.out ? p.W[NH + 1][m * p.wsz[NH + 1] + j * H + fo] : 0.0f;
-    }
-    const float b0 = p.b[0][m * p.bsz[0] + fo];
     __syncthreads();
-    if (on) first_layer(sm, w0, b0, slope, L, we);
+    if (on) first_layer(sm, b0, p.in, slope, L);
     __syncthreads();
-    // ---- forward.  The layers' loops stay loops: unrolled, a tile is 88 KB of code, more than the
-    // instruction cache holds.
-    uint64_t mask = 0;                               // bit 16 l + i: value i of A_{l+2} positive
+    // ---- forward
+    uint32_t mask[NH];                               // bit i: value i of A_{l+2} positive
     float v[16];
-#pragma unroll 1
+#pragma unroll
     for (int l = 0; l < NH; ++l) {
+      mask[l] = 0;
       if (on) {
         f32x16 acc;
-        const float bh = hidden(p.b, l)[m * (int64_t)H + fo];
-        product<false>(hidden(p.W, l) + m * (int64_t)(H * H), buf(l), L, we, acc);
+        product(R, l, l < NH - 1 ? l + 1 : 2 * NH - 1, woff, pf, buf(l), L, acc);
         uint32_t k = 0;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float z = acc[i] + bh;
+          const float z = acc[i] + bh[l];
           k |= z > 0.0f ? 1u << i : 0u;
           v[i] = g_leaky(z, slope);
         }
-        mask |= (uint64_t)k << 16 * l;
-        if (l < NH - 1) store_block(buf(l + 1), L, we, v);
+        asm volatile("" : "+v"(k));                  // packed here, not where it is used
+        mask[l] = k;
+        if (l < NH - 1) store_block(buf(l + 1), L, v);
       }
-      if (l < NH - 1) __syncthreads();
+      __syncthreads();                               // the last: the top buffer is read
     }
-    // ---- output layer: v = A_{NH+1}
-    if (on) over_features(sm, L, we, v, wo, p.out);
+    // ---- output layer: v = A_{NH+1}; its sums lie where the top signal will
+    Op* op = reinterpret_cast<Op*>(buf(kTop));
+    if (on) over_features(op, L, v, sm.wo, p.out);
     __syncthreads();
-    {   // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
-      const int ev = tid & 63, j = tid >> 6;
-      float d = 0.0f;
-      if (ev < rows && j < p.out) {
-        const float o = p.b[NH + 1][m * p.bsz[NH + 1] + j] + ((sm.op[0][j][ev] + sm.op[1][j][ev]) + (sm.op[2][j][ev] + sm.op[3][j][ev]));
-        d = sm.dout[j][ev] * g_sigmoid(o);
-        sm.dout[j][ev] = d;
-      }
-      d = wave_total(d);
-      if ((tid & 63) == 0 && j < p.out) put(part + p.poff_b[NH + 1] + j, d);
+    if (col < p.out && ev < rows) {   // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
+      const float o = p.b[NH + 1][m * p.bsz[NH + 1] + col] + ((op[0][col][ev] + op[1][col][ev]) + (op[2][col][ev] + op[3][col][ev]));
+      const float d = sm.dout[col][ev] * g_sigmoid(o);
+      sm.dout[col][ev] = d;
+      S.bo += d;
     }
     __syncthreads();
-    over_rows(sm, L, we, on, v, sm.dout, p.out, part + p.poff_w[NH + 1], 1, H, put);
-    // ---- top signal
-    float sum = 0.0f;
     if (on) {
+      over_rows(L, v, sm.dout, p.out, S.out);
+      from_few(sm.wo, sm.dout, 0.0f, p.out, L, v);   // the top signal
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        float t[4] = {};
-#pragma unroll
-        for (int j = 0; j < kGMaxIO; ++j) {
-          const f32x4 e = *reinterpret_cast<const f32x4*>(&sm.dout[j][32 * we + 8 * g + 4 * L.lh]);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) t[q] = fmaf(e[q], wo[j], t[q]);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float d = mask >> (16 * (NH - 1) + 4 * g + q) & 1 ? t[q] : slope * t[q];
-          v[4 * g + q] = d;
-          sum += d;
-        }
-      }
-      store_block(buf(kTop), L, we, v);
+      for (int i = 0; i < 16; ++i) v[i] = mask[NH - 1] >> i & 1 ? v[i] : slope * v[i];
+      S.b[NH] += total_of(v);
+      store_block(buf(kTop), L, v);
     }
-    sum = add_xor32(sum);
-    if (L.lh == 0) sm.dbs[NH & 1][we][fo] = sum;
     __syncthreads();
     // ---- hidden layers: layer 1 + l maps A_{l+1} (buffer l) -> A_{l+2}
-#pragma unroll 1
+#pragma unroll
     for (int l = NH - 1; l >= 0; --l) {
       const char* sig = buf(l == NH - 1 ? kTop : l + 1);
-      float* dW = part + at_layer(p.in, l);
-      if (tid < H) put(dW + H * H + tid, sm.dbs[(l + 1) & 1][0][tid] + sm.dbs[(l + 1) & 1][1][tid]);
-      wgrad(sig, buf(l), L, we, steps, dW, more);
+      wgrad(sig, buf(l), L, steps, S.W[l]);
       f32x16 acc;
-      if (on) product<true>(hidden(p.W, l) + m * (int64_t)(H * H), sig, L, we, acc);
-      sum = 0.0f;
+      if (on) product(R, NH + l, l > 0 ? NH + l - 1 : 0, woff, pf, sig, L, acc);
       if (l > 0) {
         if (on) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            v[i] = mask >> (16 * l - 16 + i) & 1 ? acc[i] : slope * acc[i];
-            sum += v[i];
-          }
+          for (int i = 0; i < 16; ++i) v[i] = mask[l - 1] >> i & 1 ? acc[i] : slope * acc[i];
+          S.b[l] += total_of(v);
         }
-        sum = add_xor32(sum);
-        if (L.lh == 0) sm.dbs[l & 1][we][fo] = sum;
         __syncthreads();                             // every wave is done with buffer l and the signal
         if (on) {
-          store_block(buf(l), L, we, v);
-          if (kTop == 0 && l == NH - 1) first_layer(sm, w0, b0, slope, L, we);
+          store_block(buf(l), L, v);
+          if (kTop == 0 && l == NH - 1) first_layer(sm, b0, p.in, slope, L);
         }
         __syncthreads();
-      } else {
-        if (on) {
+      } else if (on) {
+        from_few(sm.w0, sm.n, b0, p.in, L, v);       // A_1's pre-activations again, for their signs
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            float z[4];
-            pre1(sm, w0, b0, 32 * we + 8 * g + 4 * L.lh, z);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              v[4 * g + q] = z[q] > 0.0f ? acc[4 * g + q] : slope * acc[4 * g + q];
-              sum += v[4 * g + q];
-            }
-          }
-        }
-        sum = add_xor32(sum);
-        if (L.lh == 0) sm.dbs[0][we][fo] = sum;
+        for (int i = 0; i < 16; ++i) v[i] = v[i] > 0.0f ? acc[i] : slope * acc[i];
       }
     }
     // ---- first layer: v = delta_1
-    over_rows(sm, L, we, on, v, sm.n, p.in, part + p.poff_w[0], p.in, 1, put);   // (its barriers cover dbs)
-    if (tid < H) put(part + p.poff_b[0] + tid, sm.dbs[0][0][tid] + sm.dbs[0][1][tid]);
+    if (on) {
+      S.b[0] += total_of(v);
+      over_rows(L, v, sm.n, p.in, S.in);
+    }
     if (p.dx) {
-      __syncthreads();                               // stage is read
-      if (on) over_features(sm, L, we, v, w0, p.in);
+      Op* od = reinterpret_cast<Op*>(buf(NBUF - 1));   // of three buffers the last products read the others
+      if (NH == 1) __syncthreads();
+      if (on) over_features(od, L, v, sm.w0, p.in);
       __syncthreads();
-      const int ev = tid & 63, j = tid >> 6;
-      if (ev < rows && j < p.in)
-        p.dx[(row0 + ev) * p.in + j] = (sm.op[0][j][ev] + sm.op[1][j][ev]) + (sm.op[2][j][ev] + sm.op[3][j][ev]);
+      if (ev < rows && col < p.in) p.dx[(row0 + ev) * p.in + col] = (od[0][col][ev] + od[1][col][ev]) + (od[2][col][ev] + od[3][col][ev]);
     }
   }
 
+  // What the workgroup has of a member, to its partial.  The two blocks' sums of a feature meet in LDS.
+  static __device__ __forceinline__ void flush(const GenParams& p, Smem& sm, const Me& L, float* part, const Sums& S) {
+#pragma unroll
+    for (int l = 0; l < NH; ++l) {
+      float* at = part + p.poff_w[1 + l] + (32 * L.wf + 4 * L.lh) * H + 64 * L.we + L.lr;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) at[(8 * (i / 4) + i % 4) * H + 32 * k] = S.W[l][k][i];
+    }
+    constexpr int N = NH + 1 + 2 * kGMaxIO;
+    float (*stage)[H] = reinterpret_cast<float (*)[H]>(sm.act);
+    float s[N];
+#pragma unroll
+    for (int i = 0; i <= NH; ++i) s[i] = add_xor32(S.b[i]);
+#pragma unroll
+    for (int j = 0; j < kGMaxIO; ++j) {
+      s[NH + 1 + j] = add_xor32(S.in[j]);
+      s[NH + 1 + kGMaxIO + j] = add_xor32(S.out[j]);
+    }
+    __syncthreads();                                 // act is read
+    if (L.we == 1 && L.lh == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) stage[i][L.fo] = s[i];
+    __syncthreads();
+    if (L.we == 0 && L.lh == 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] += stage[i][L.fo];
+#pragma unroll
+      for (int l = 0; l <= NH; ++l) part[p.poff_b[l] + L.fo] = s[l];
+#pragma unroll
+      for (int j = 0; j < kGMaxIO; ++j) {
+        if (j < p.in) part[p.poff_w[0] + L.fo * p.in + j] = s[NH + 1 + j];
+        if (j < p.out) part[p.poff_w[NH + 1] + j * H + L.fo] = s[NH + 1 + kGMaxIO + j];
+      }
+    }
+    const float bo = wave_total(S.bo);
+    if (L.lane == 0 && (int)(threadIdx.x >> 6) < p.out) part[p.poff_b[NH + 1] + (threadIdx.x >> 6)] = bo;
+  }
+
   // Of the `blocks` blocks of 32 rows in the order of their rows, workgroup g of `groups` (at most one a
-  // block) takes those from g blocks / groups on, two of a member together, and adds up what it has of a
-  // member in slot g + m of the partials: g + m rises from each of its (g, m) to the next.
+  // block) takes those from g blocks / groups on, two of a member together; what it has of a member goes to
+  // slot g + m of the partials: g + m rises from each of its (g, m) to the next.
   static __device__ void run(const GenParams& p) {
     __shared__ __attribute__((aligned(1024))) Smem sm;
     const int64_t blocks = write_slots<32>(p);
     const int64_t groups = min(blocks, (int64_t)gridDim.x);
     const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     if (g >= groups) return;
-    int last = -1;
-    for (int64_t i = g * blocks / groups, end = (g + 1) * blocks / groups; i < end;) {
-      GenTile t;
-      if (!routed_tile<32>(p, i, t)) return;         // (there is one)
-      const int rows = (int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32));
-      __syncthreads();                               // the tile before is read
-      tile(p, sm, t.m, t.row0, rows, p.part + (g + t.m) * p.P, t.m == last);
-      last = t.m;
-      i += rows > 32 ? 2 : 1;
+    Me L;
+    {
+      const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+      const Lane A = make_lane(wave & 3, 0);
+      L.lane = A.lane;
+      L.lr = A.lr;
+      L.lh = A.lh;
+      L.wf = A.wf;
+      L.we = wave >> 2;
+      L.fo = 32 * L.wf + L.lr;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) L.w[q] = A.w[q];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        L.own[q] = L.we ? A.w[2 + q] : A.w[q];
+        L.tr[q] = L.we ? A.tr[1][q] : A.tr[0][q];
+      }
+    }
+    const uint32_t woff = (uint32_t)(L.wf * KS * kTerms * 64 + L.lane) * 16u;
+    int64_t i = g * blocks / groups;
+    const int64_t end = (g + 1) * blocks / groups;
+    GenTile t;
+    bool more = i < end && routed_tile<32>(p, i, t);
+    while (more) {                                   // a member
+      const int m = __builtin_amdgcn_readfirstlane(t.m);
+      const Rsrc R = split_rsrc(p.split + (size_t)m * 2 * NH * (kCopy / 2), (uint32_t)(2 * NH * kCopy));
+      Sums S = {};
+      Prefetch pf;
+#pragma unroll
+      for (int q = 0; q < PD; ++q) load_w(R, woff, 0, q, pf.w[q]);
+      const float b0 = p.b[0][m * p.bsz[0] + L.fo];
+      float bh[NH];
+#pragma unroll
+      for (int l = 0; l < NH; ++l) bh[l] = p.b[1 + l][m * p.bsz[1 + l] + L.fo];
+      __syncthreads();                               // the member before is read
+      for (int k = threadIdx.x; k < kGMaxIO * H; k += kGThreads) {
+        const int j = k / H, f = k % H;
+        sm.w0[j][f] = j < p.in ? p.W[0][m * p.wsz[0] + f * p.in + j] : 0.0f;
+        sm.wo[j][f] = j < p.out ? p.W[NH + 1][m * p.wsz[NH + 1] + k] : 0.0f;
+      }
+      do {
+        const int rows = __builtin_amdgcn_readfirstlane((int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32)));
+        __syncthreads();                             // the tile before is read
+        tile(p, sm, L, m, t.row0, rows, R, b0, bh, pf, S);
+        i += rows > 32 ? 2 : 1;
+        t.row0 += rows;
+        more = i < end && (t.row0 < t.end || routed_tile<32>(p, i, t));
+      } while (more && t.m == m);
+      flush(p, sm, L, p.part + (g + m) * p.P, S);
     }
   }
 };
@@ -1342,12 +1391,17 @@ inline int routed_groups(const sagips_gen& G, int64_t k, int T, int n_cu) {
   const int64_t t = routed_tiles(G, k, T == 64 ? 32 : 16), most = (n_cu + 7) / 8 * 8;
   return (int)(t < most ? (t + 7) / 8 * 8 : most);
 }
+// Bytes of the split copies.
+inline size_t routed_split_bytes(const sagips_gen& G) {
+  return (size_t)G.n_members * 2 * (G.n_layers - 2) * split_copy_bytes(128);
+}
 }  // namespace
 
 size_t gen_backward_routed_workspace(const sagips_gen& G, int64_t k, int n_cu) {
   const GenParams p = gen_params(G, nullptr, k);
-  const size_t partials = routed_groups(G, k, routed_rows(k, n_cu), n_cu) + (size_t)G.n_members;
-  return sizeof(float) * (size_t)p.P * partials + sizeof(int) * 2 * (size_t)G.n_members;
+  const int T = routed_rows(k, n_cu);
+  const size_t partials = routed_groups(G, k, T, n_cu) + (size_t)G.n_members;
+  return (T == 64 ? routed_split_bytes(G) : 0) + sizeof(float) * (size_t)p.P * partials + sizeof(int) * 2 * (size_t)G.n_members;
 }
 
 hipError_t launch_gen_forward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k, float* theta,
@@ -1369,13 +1423,22 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
                                       const float* dtheta, float* const* dW, float* const* db, float* dx, void* ws, int n_cu,
                                       hipStream_t st, Timer* tm) {
   GenParams p = gen_params(G, x, k);
+  const int T = routed_rows(k, n_cu), groups = routed_groups(G, k, T, n_cu), NH = G.n_layers - 2;
   p.dtheta = dtheta;
-  p.part = static_cast<float*>(ws);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + (T == 64 ? routed_split_bytes(G) : 0));
   p.offsets = offsets;
   p.members = G.n_members;
   p.dx = dx;
   const GenVariant* v = find_gen(G);
-  const int T = routed_rows(k, n_cu), groups = routed_groups(G, k, T, n_cu);
+  if (T == 64) {
+    u16* copies = static_cast<u16*>(ws);
+    p.split = copies;
+    if (tm) tm->begin("gen_split");
+    hipLaunchKernelGGL(k_split_members, dim3(128 * 128 / 8 / 256, 2 * NH, G.n_members), dim3(256), 0, st, p, copies, NH);
+    if (tm) tm->end();
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   p.slots = reinterpret_cast<int*>(p.part + (size_t)p.P * (groups + (size_t)G.n_members));
   if (tm) tm->begin("gen_backward_routed");
   hipLaunchKernelGGL(v->bwd_routed[T == 64 ? 0 : 1], dim3(groups), dim3(kGThreads), 0, st, p);
