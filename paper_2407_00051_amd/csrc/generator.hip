@@ -82,6 +82,7 @@ struct GenParams {
   int members;
   float* dx;                       // backward: dL/dnoise [k][in], or NULL
   int* slots;                      // backward: [members][2]
+  int64_t PS;                      // floats from one partial to the next
   const u16* split;                // backward, 64-row tiles: split copies of the hidden layers
 };
 
@@ -98,84 +99,89 @@ __device__ __forceinline__ void member_rows(const GenParams& p, int m, int64_t& 
   hi = min(max((int64_t)p.offsets[m + 1], lo), p.k);
 }
 
-// Tiles of T rows of all members.  A member a lane, 64 at a time; the whole wave calls it.  The workgroups of a
-// backward pass, of which number g takes the tiles from g tiles / groups on (groups: the grid, at most one
-// a tile), note in slots[m] = (first, number) the partials of the members between them: those of the
-// workgroups that have tiles of member m, tile t being workgroup ((t + 1) groups - 1) / tiles's.
+// The members' rows in tiles of T rows, in order; a member a lane, 64 at a time.  Up to 64 members stay in
+// the lanes; of more, each search reads the offsets again.  The whole wave calls all of it.
 template <int T>
-__device__ __forceinline__ int64_t write_slots(const GenParams& p) {
-  const int lane = threadIdx.x & 63;
-  int64_t n = 0;
-  for (int m0 = 0; m0 < p.members; m0 += 64) {
-    int64_t lo = 0, hi = 0;
-    if (m0 + lane < p.members) member_rows(p, m0 + lane, lo, hi);
-    uint32_t t = (uint32_t)((hi - lo + T - 1) / T);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) t += (uint32_t)__shfl_xor((int)t, d, 64);
-    n += t;
-  }
-  if (blockIdx.x == 0 && threadIdx.x < 64) {
-    const int64_t groups = min(n, (int64_t)gridDim.x);
-    int64_t before = 0;
-    for (int m0 = 0; m0 < p.members; m0 += 64) {
-      const int m = m0 + lane;
-      int64_t lo = 0, hi = 0;
-      if (m < p.members) member_rows(p, m, lo, hi);
-      const uint32_t t = (uint32_t)((hi - lo + T - 1) / T);
-      uint32_t upto = t;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
-        if (lane >= d) upto += o;
-      }
-      if (m < p.members) {
-        const int64_t t1 = before + upto, t0 = t1 - t;
-        const int64_t g0 = t ? min(((t0 + 1) * groups - 1) / n, groups - 1) : 0;
-        p.slots[2 * m] = (int)(g0 + m);
-        p.slots[2 * m + 1] = t ? (int)(min((t1 * groups - 1) / n, groups - 1) - g0) + 1 : 0;
-      }
-      before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-    }
-  }
-  return n;
-}
-// Tile `want` of all; false: there are fewer.
-template <int T>
-__device__ __forceinline__ bool routed_tile(const GenParams& p, int64_t want, GenTile& out) {
-  const int lane = threadIdx.x & 63;
-  int64_t before = 0;
-  for (int m0 = 0; m0 < p.members; m0 += 64) {
-    int64_t lo = 0, hi = 0;
-    if (m0 + lane < p.members) member_rows(p, m0 + lane, lo, hi);
-    const uint32_t t = (uint32_t)((hi - lo + T - 1) / T);   // 64 of them below 2^32: fewer than 2^29 rows
-    uint32_t upto = t;
+struct RoutedRows {
+  int lo, hi;                      // rows of member `lane`
+  uint32_t upto;                   // tiles of members 0 .. lane
+  int64_t tiles;                   // of all members
+
+  __device__ __forceinline__ void read(const GenParams& p, int m0) {
+    const int lane = threadIdx.x & 63, m = m0 + lane;
+    int64_t a = 0, b = 0;
+    if (m < p.members) member_rows(p, m, a, b);
+    lo = (int)a;
+    hi = (int)b;
+    upto = count();                // 64 of them below 2^32: fewer than 2^29 rows
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
       if (lane >= d) upto += o;
     }
-    const uint64_t past = __ballot(before + upto > want);
-    if (past) {
-      const int src = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
-      out.m = m0 + src;
-      lo = __builtin_amdgcn_readlane((int)lo, src);
-      hi = __builtin_amdgcn_readlane((int)hi, src);
-      out.row0 = lo + (want - before - (uint32_t)__builtin_amdgcn_readlane((int)(upto - t), src)) * T;
-      out.end = hi;
-      out.base = 0;
-      return true;
-    }
-    before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   }
-  return false;
-}
+  __device__ __forceinline__ uint32_t count() const { return (uint32_t)((hi - lo + T - 1) / T); }
+  __device__ __forceinline__ uint32_t sum() const { return (uint32_t)__builtin_amdgcn_readlane((int)upto, 63); }
+
+  __device__ __forceinline__ explicit RoutedRows(const GenParams& p) {
+    tiles = 0;
+    for (int m0 = (p.members - 1) / 64 * 64; m0 >= 0; m0 -= 64) {   // the first 64 last: they stay
+      read(p, m0);
+      tiles += sum();
+    }
+  }
+  // Tile `want` of all; false (only where the offsets do not rise, or want is not below tiles): there is none.
+  __device__ __forceinline__ bool find(const GenParams& p, int64_t want, GenTile& t) const {
+    RoutedRows r = *this;
+    int64_t before = 0;
+    for (int m0 = 0;;) {
+      const uint64_t past = __ballot(before + r.upto > want);
+      if (past) {
+        const int src = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+        t.m = m0 + src;
+        const int first = __builtin_amdgcn_readlane(r.lo, src);
+        t.end = __builtin_amdgcn_readlane(r.hi, src);
+        t.row0 = first + (want - before - (uint32_t)__builtin_amdgcn_readlane((int)(r.upto - r.count()), src)) * T;
+        t.base = 0;
+        return true;
+      }
+      before += r.sum();
+      m0 += 64;
+      if (m0 >= p.members) return false;
+      r.read(p, m0);
+    }
+  }
+  // The workgroups of a backward pass, of which number g takes the tiles from g tiles / groups on, share the
+  // partials of member m between them: slots[m] = (first, number), those of the workgroups that have tiles of it,
+  // tile t being workgroup ((t + 1) groups - 1) / tiles's.  One workgroup writes it.
+  __device__ __forceinline__ void write_slots(const GenParams& p, int64_t groups) const {
+    if (threadIdx.x >= 64) return;
+    RoutedRows r = *this;
+    int64_t before = 0;
+    for (int m0 = 0;;) {
+      const int m = m0 + (int)threadIdx.x;
+      if (m < p.members) {
+        const uint32_t n = r.count();
+        const int64_t t1 = before + r.upto, t0 = t1 - n;
+        const int64_t g0 = n ? min(((t0 + 1) * groups - 1) / tiles, groups - 1) : 0;
+        p.slots[2 * m] = (int)(g0 + m);
+        p.slots[2 * m + 1] = n ? (int)(min((t1 * groups - 1) / tiles, groups - 1) - g0) + 1 : 0;
+      }
+      before += r.sum();
+      m0 += 64;
+      if (m0 >= p.members) return;
+      r.read(p, m0);
+    }
+  }
+};
 
 // Tile of this workgroup.  Routed: the grid may hold more workgroups than there are tiles, and is a
 // multiple of 8; an XCD (workgroup mod 8) takes tiles that follow each other.
 template <int T, bool kRouted>
 __device__ __forceinline__ bool gen_tile(const GenParams& p, GenTile& t) {
   if constexpr (kRouted) {
-    return routed_tile<T>(p, (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), t);
+    const RoutedRows<T> r(p);
+    return r.find(p, (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3), t);
   } else {
     int tile;
     gen_block(gridDim.x, gridDim.y, t.m, tile);
@@ -337,16 +343,17 @@ struct Gen {
   // partials: g + m rises from each of its (g, m) to the next.
   static __device__ void run_backward_routed(const GenParams& p) {
     __shared__ Smem sm;
-    const int64_t tiles = write_slots<kGT>(p);
-    const int64_t groups = min(tiles, (int64_t)gridDim.x);
+    const RoutedRows<kGT> rr(p);
+    const int64_t groups = min(rr.tiles, (int64_t)gridDim.x);
     const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (blockIdx.x == 0) rr.write_slots(p, groups);
     if (g >= groups) return;
     int last = -1;
-    for (int64_t i = g * tiles / groups; i < (g + 1) * tiles / groups; ++i) {
+    for (int64_t i = g * rr.tiles / groups; i < (g + 1) * rr.tiles / groups; ++i) {
       GenTile t;
-      if (!routed_tile<kGT>(p, i, t)) return;        // (there is one)
+      if (!rr.find(p, i, t)) return;                 // (there is one)
       __syncthreads();                               // the tile before is read
-      backward_tile<true>(p, sm, t, p.part + (g + t.m) * p.P, t.m == last);
+      backward_tile<true>(p, sm, t, p.part + (g + t.m) * p.PS, t.m == last);
       last = t.m;
     }
   }
@@ -702,11 +709,14 @@ __global__ __launch_bounds__(256) void k_split_members(GenParams p, u16* out, in
 // (k_split_members): splitting them as they are read took as long as the products.  A weight
 // gradient has K = the tile's rows; each wave has 32 x 64 of it, in the accumulation registers
 // for as long as the workgroup stays with a member.
+// What decides its time is the code that a workgroup runs once and the registers: a product, its epilogue and
+// the stores are there once, in a loop over the 2 NH products (unrolled, 53 KB of code that most workgroups
+// run for one tile only, and 265 spilled registers).
 template <int NH>
 struct GenBwd : SplitLds<128, 64> {
-  static constexpr int H = 128, KS = H / 16, PD = 2;
+  static constexpr int H = 128, KS = H / 16, PD = 3;
   static constexpr int NBUF = NH < 3 ? NH + 1 : 3, kTop = NH < 3 ? NH : 0;
-  static constexpr int kCopy = (int)split_copy_bytes(H);
+  static constexpr uint32_t kCopy = (uint32_t)split_copy_bytes(H), kStep = kTerms * 1024;
 
   struct Smem {
     char act[NBUF * BUF];
@@ -714,14 +724,19 @@ struct GenBwd : SplitLds<128, 64> {
     float dout[kGMaxIO][64];       // dL/d(last pre-activation)
     float w0[kGMaxIO][H];          // the member's first layer, transposed, and its last
     float wo[kGMaxIO][H];
+    float bias[NH + 1][H], bo[kGMaxIO];
   };
+  // Where a member's gradients lie in its partial.
+  static constexpr int kHidden = H * H + H;
+  static __device__ __forceinline__ int at_hidden(int in, int l) { return H * in + H + l * kHidden; }
   // The wave and the lane, and the lane's offsets in a buffer.
   struct Me {
     int lane, lr, lh, wf, we, fo;
-    uint32_t w[4], own[2], tr[2];  // unit of a 16-row step; of the block's two steps; transposed reads of the block
+    uint32_t own[2], tr[2];        // units of the block's two 16-row steps; transposed reads of the block
+    uint32_t woff;                 // in a split copy
   };
-  // Offsets for one phase: kept from phase to phase, what the compiler forms of them beforehand would
-  // take more registers than there are.
+  // An offset for one phase: kept from phase to phase, what the compiler forms of it beforehand would take
+  // more registers than there are.
   static __device__ __forceinline__ uint32_t fresh(uint32_t o) {
     asm volatile("" : "+v"(o));
     return o;
@@ -729,65 +744,66 @@ struct GenBwd : SplitLds<128, 64> {
   // Sums over the rows of the lane's feature that a wave keeps of a member.
   struct Sums {
     f32x16 W[NH][2];               // rows 32 wf .., columns 64 we .. of a hidden layer's gradient
-    float b[NH + 1], in[kGMaxIO], out[kGMaxIO], bo;
+    float b[NH + 1], bo;
+    float in[kGMaxIO / 2], out[kGMaxIO / 2];   // first and last layer: lane half lh has columns 2 k + lh, over both halves' rows
   };
-  struct Prefetch {
-    bf16x8 w[PD][kTerms];          // the next product's first weight steps
-  };
+  typedef bf16x8 Ring[PD + 1][kTerms];   // weight steps: the next product's first three between products
 
-  static __device__ __forceinline__ void load_w(Rsrc R, uint32_t woff, int copy, int ks, bf16x8 (&w)[kTerms]) {
+  static __device__ __forceinline__ void load_w(Rsrc R, uint32_t woff, uint32_t at, bf16x8 (&w)[kTerms]) {
 #pragma unroll
-    for (int t = 0; t < kTerms; ++t) w[t] = split_load(R, woff + t * 1024u, (uint32_t)(copy * kCopy + ks * kTerms * 1024));
+    for (int t = 0; t < kTerms; ++t) w[t] = split_load(R, woff + t * 1024u, at);
   }
-  static __device__ __forceinline__ void read_rows(const char* at0, const char* at1, int ks, bf16x8 (&a)[kTerms]) {
+  static __device__ __forceinline__ void read_rows(const char* at0, const char* at1, int o, bf16x8 (&a)[kTerms]) {
 #pragma unroll
     for (int t = 0; t < kTerms; ++t) {
-      const int o = t * PL + ks * 16 * RB;
-      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at0 + o));
-      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at1 + o));
+      const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at0 + t * PL + o));
+      const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at1 + t * PL + o));
       a[t] = bf16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
   }
 
-  // out = act B for the wave's features and block, B the given split copy; pf holds the copy's first steps, and in
-  // the end those of `next`.
-  static __device__ __forceinline__ void product(Rsrc R, int copy, int next, uint32_t woff, Prefetch& pf, const char* buf, const Me& L,
-                                                 f32x16& out) {
-    f32x16 acc[1], corr[1];
-    bf16x8 w[PD + 1][kTerms], a[2][1][kTerms];
-    const char *at0 = buf + fresh(L.tr[0]), *at1 = buf + fresh(L.tr[1]);
+  // act B for the wave's features and block, B the split copy at `copy` (bytes); w holds the copy's first steps,
+  // and in the end those of the one at `next`.  Six products a step into one accumulator, smallest first.
+  static __device__ __forceinline__ f32x16 product(Rsrc R, uint32_t copy, uint32_t next, Ring& w, const char* buf, const Me& L) {
+    constexpr int ta[6] = {2, 0, 1, 1, 0, 0}, tb[6] = {0, 2, 1, 0, 1, 0};
+    f32x16 acc = {};
+    bf16x8 a[2][kTerms];
+    const char *at0 = buf + L.tr[0], *at1 = buf + L.tr[1];
+    read_rows(at0, at1, 0, a[0]);
+    uint32_t more = copy + PD * kStep;
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      // the step behind the half: the other half's first, or (unused) the first again
+      const int turn = half ? -3 * 16 * RB - 4 * 16 * RB : 16 * RB;
 #pragma unroll
-    for (int q = 0; q < PD; ++q)
+      for (int q = 0; q < 4; ++q) {
+        __builtin_amdgcn_sched_barrier(0);
+        load_w(R, L.woff, more, w[(q + PD) % (PD + 1)]);
+        more = q == 0 && half ? next : more + kStep;   // step 7 is loaded at step 4
+        read_rows(at0, at1, q < 3 ? 16 * RB : turn, a[(q + 1) & 1]);
+        at0 += q < 3 ? 16 * RB : turn;
+        at1 += q < 3 ? 16 * RB : turn;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int t = 0; t < kTerms; ++t) w[q][t] = pf.w[q][t];
-    read_rows(at0, at1, 0, a[0][0]);
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      __builtin_amdgcn_sched_barrier(0);
-      if (ks + PD < KS) load_w(R, woff, copy, ks + PD, w[(ks + PD) % (PD + 1)]);
-      else load_w(R, woff, next, ks + PD - KS, pf.w[ks + PD - KS]);
-      if (ks + 1 < KS) read_rows(at0, at1, ks + 1, a[(ks + 1) & 1][0]);
-      __builtin_amdgcn_sched_barrier(0);
-      if (ks == 0) split_mfma_apart<true, false>(a[0], w[0], acc, corr);
-      else split_mfma_apart<false, false>(a[ks & 1], w[ks % (PD + 1)], acc, corr);
+        for (int k = 0; k < 6; ++k) acc = mfma32(a[q & 1][ta[k]], w[q][tb[k]], acc);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
-    out = acc[0] + corr[0];
+    return acc;
   }
 
   // W += signal^T A over `steps` times 16 rows.
   static __device__ __forceinline__ void wgrad(const char* sig, const char* A, const Me& L, int steps, f32x16 (&W)[2]) {
-    const uint32_t row = fresh((uint32_t)L.wf * 32 * RB), col = fresh((uint32_t)L.we * 64 * RB);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s >= steps) break;
+    const char *s0 = sig + L.lr * RB + L.wf * 32 * RB, *a0 = A + L.lr * RB + L.we * 64 * RB;
+#pragma unroll 1
+    for (int s = 0; s < steps; ++s) {
       bf16x8 a[kTerms], b[2][kTerms];
-      const uint32_t o = fresh(L.w[s]);
+      const uint32_t o = ((uint32_t)(2 * s + L.lh) ^ swz(L.lr)) << 4;
 #pragma unroll
       for (int t = 0; t < kTerms; ++t) {
-        a[t] = *reinterpret_cast<const bf16x8*>(sig + (o + row) + t * PL);
+        a[t] = *reinterpret_cast<const bf16x8*>(s0 + o + t * PL);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) b[k][t] = *reinterpret_cast<const bf16x8*>(A + (o + col) + t * PL + k * 32 * RB);
+        for (int k = 0; k < 2; ++k) b[k][t] = *reinterpret_cast<const bf16x8*>(a0 + o + t * PL + k * 32 * RB);
       }
       split_mfma2(b[0], b[1], a, W[0], W[1], W[0], W[1]);
     }
@@ -803,7 +819,7 @@ struct GenBwd : SplitLds<128, 64> {
         const float h[4] = {v[8 * s + 4 * u], v[8 * s + 4 * u + 1], v[8 * s + 4 * u + 2], v[8 * s + 4 * u + 3]};
         split4(h, u, d);
       }
-      char* at = buf + fresh(L.own[s] + (uint32_t)L.wf * 32 * RB);
+      char* at = buf + fresh(L.own[s]);
 #pragma unroll
       for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(at + t * PL) = make_uint4(d[t][0], d[t][1], d[t][2], d[t][3]);
     }
@@ -813,53 +829,69 @@ struct GenBwd : SplitLds<128, 64> {
                                                   float (&v)[16]) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = c;
-    const int o = (int)fresh((uint32_t)(32 * L.we + 4 * L.lh)), f = (int)fresh((uint32_t)L.fo);
-#pragma unroll 1
+    const float *e0 = &x[0][32 * L.we + 4 * L.lh], *w0 = &w[0][L.fo];
+#pragma unroll 2
     for (int j = 0; j < n; ++j) {
-      const float wj = w[j][f];
+      const float wj = w0[j * H];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][o + 8 * g]);
+        const f32x4 e = *reinterpret_cast<const f32x4*>(e0 + 64 * j + 8 * g);
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[4 * g + q] = fmaf(wj, e[q], v[4 * g + q]);
       }
     }
   }
-  static __device__ __forceinline__ void first_layer(Smem& sm, float b0, int in, float slope, const Me& L) {
-    float v[16];
-    from_few(sm.w0, sm.n, b0, in, L, v);
+  // LeakyReLU of A_1 or of a hidden layer: the signs as bits, and the values.
+  static __device__ __forceinline__ uint32_t signs(const float (&v)[16]) {
+    uint32_t k = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = g_leaky(v[i], slope);
+    for (int i = 0; i < 16; ++i) k |= v[i] > 0.0f ? 1u << i : 0u;
+    return k;
+  }
+  static __device__ __forceinline__ void leak(float (&v)[16], uint32_t positive, float slope) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= positive >> i & 1 ? 1.0f : slope;
+  }
+  static __device__ __forceinline__ uint32_t first_layer(Smem& sm, int in, float slope, const Me& L) {
+    float v[16];
+    from_few(sm.w0, sm.n, sm.bias[0][L.fo], in, L, v);
+    const uint32_t k = signs(v);
+    leak(v, k, slope);
     store_block(sm.act, L, v);
+    return k;
   }
   // op[wf][j][row] = sum over the wave's features of v[i] w[j][fo], two columns j at a time.
   typedef float Op[kGMaxIO][64];
   static __device__ __forceinline__ void over_features(Op* op, const Me& L, const float (&v)[16], const float (&w)[kGMaxIO][H], int n) {
-    const int i = L.lr & 15, row = 32 * L.we + 8 * (i >> 2) + 4 * L.lh + (i & 3), f = (int)fresh((uint32_t)L.fo);
+    const int i = L.lr & 15, row = 32 * L.we + 8 * (i >> 2) + 4 * L.lh + (i & 3);
+    const float* w0 = &w[0][L.fo];
 #pragma unroll 1
     for (int j = 0; j < n; j += 2) {
-      const float wa = w[j][f], wb = w[j + 1][f];    // the rows behind the last are 0
+      const float wa = w0[j * H], wb = w0[(j + 1) * H];   // rows behind the last are 0
       float z[32];
 #pragma unroll
       for (int k = 0; k < 16; ++k) z[k] = v[k] * wa, z[16 + k] = v[k] * wb;
       op[L.wf][j + (L.lr >> 4)][row] = half_scatter_sum(z, L.lr);
     }
   }
-  // s[j] += the sum over the lane's rows of v[i] x[j][row].
+  // The sums over a lane's rows of v[i] x[j][row], added over the halves: column 2 k + lh to s[k].
   static __device__ __forceinline__ void over_rows(const Me& L, const float (&v)[16], const float (&x)[kGMaxIO][64], int n,
-                                                   float (&s)[kGMaxIO]) {
-    const int o = (int)fresh((uint32_t)(32 * L.we + 4 * L.lh));
+                                                   float (&s)[kGMaxIO / 2]) {
+    const float* e0 = &x[0][32 * L.we + 4 * L.lh];
 #pragma unroll
-    for (int j = 0; j < kGMaxIO; ++j) {
-      if (j >= n) break;
-      float t = 0.0f;
+    for (int k = 0; k < kGMaxIO / 2; ++k) {
+      if (2 * k >= n) break;
+      float t[2] = {};
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4 e = *reinterpret_cast<const f32x4*>(&x[j][o + 8 * g]);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) t = fmaf(v[4 * g + q], e[q], t);
-      }
-      s[j] += t;
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 e = *reinterpret_cast<const f32x4*>(e0 + 64 * (2 * k + h) + 8 * g);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) t[h] = fmaf(v[4 * g + q], e[q], t[h]);
+        }
+      const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[0]), __float_as_uint(t[1]), false, false);
+      s[k] += __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
   }
   static __device__ __forceinline__ float total_of(const float (&v)[16]) {
@@ -869,95 +901,85 @@ struct GenBwd : SplitLds<128, 64> {
     return t;
   }
 
-  // A tile: `rows` (1 to 64) rows of member m from row0 on.  b0, bh: the member's biases of the lane's feature.
-  static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, const Me& L, int m, int64_t row0, int rows, Rsrc R, float b0,
-                                              const float (&bh)[NH], Prefetch& pf, Sums& S) {
-    const int tid = threadIdx.x, steps = rows > 32 ? 4 : 2;
-    const uint32_t woff = (uint32_t)(L.wf * KS * kTerms * 64 + L.lane) * 16u;
+  // A thread's input and dL/dtheta of a tile: row ev, column col of both.
+  struct Inputs {
+    float x, d;
+  };
+  static __device__ __forceinline__ Inputs inputs(const GenParams& p, const GenTile& t, int rows) {
+    const int ev = min((int)(threadIdx.x & 63), rows - 1), col = threadIdx.x >> 6;
+    return {p.noise[(t.row0 + ev) * p.in + min(col, p.in - 1)], p.dtheta[(t.row0 + ev) * p.out + min(col, p.out - 1)]};
+  }
+
+  // A tile: `rows` (1 to 64) rows of a member from row0 on.
+  static __device__ __forceinline__ void tile(const GenParams& p, Smem& sm, const Me& L, int64_t row0, int rows, Inputs given, Rsrc R,
+                                              Ring& w, Sums& S) {
+    const int steps = rows > 32 ? 4 : 2;
     const bool on = rows > 32 * L.we;                // the wave has a block
     const float slope = p.slope;
-    const auto buf = [&](int i) __attribute__((always_inline)) { return &sm.act[i * BUF]; };
-    const int ev = tid & 63, col = tid >> 6;         // a thread's row and column of the inputs and outputs
-    {
-      const bool here = ev < rows;
-      sm.n[col][ev] = here && col < p.in ? p.noise[(row0 + ev) * p.in + col] : 0.0f;
-      sm.dout[col][ev] = here && col < p.out ? p.dtheta[(row0 + ev) * p.out + col] : 0.0f;
-    }
+    const auto buf = [&](int i) __attribute__((always_inline)) { return sm.act + i * BUF; };
+    const int ev = threadIdx.x & 63, col = threadIdx.x >> 6;   // a thread's row and column of the inputs and outputs
+    sm.n[col][ev] = ev < rows && col < p.in ? given.x : 0.0f;
+    sm.dout[col][ev] = ev < rows && col < p.out ? given.d : 0.0f;
     __syncthreads();
-    if (on) first_layer(sm, b0, p.in, slope, L);
-    __syncthreads();
-    // ---- forward
-    uint32_t mask[NH];                               // bit i: value i of A_{l+2} positive
+    uint64_t mask = 0;                               // bit 16 l + i: value i of A_{l+1} positive
     float v[16];
-#pragma unroll
-    for (int l = 0; l < NH; ++l) {
-      mask[l] = 0;
-      if (on) {
-        f32x16 acc;
-        product(R, l, l < NH - 1 ? l + 1 : 2 * NH - 1, woff, pf, buf(l), L, acc);
-        uint32_t k = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float z = acc[i] + bh[l];
-          k |= z > 0.0f ? 1u << i : 0u;
-          v[i] = g_leaky(z, slope);
-        }
-        asm volatile("" : "+v"(k));                  // packed here, not where it is used
-        mask[l] = k;
-        if (l < NH - 1) store_block(buf(l + 1), L, v);
-      }
-      __syncthreads();                               // the last: the top buffer is read
-    }
-    // ---- output layer: v = A_{NH+1}; its sums lie where the top signal will
-    Op* op = reinterpret_cast<Op*>(buf(kTop));
-    if (on) over_features(op, L, v, sm.wo, p.out);
+    if (on) mask = first_layer(sm, p.in, slope, L);
     __syncthreads();
-    if (col < p.out && ev < rows) {   // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
-      const float o = p.b[NH + 1][m * p.bsz[NH + 1] + col] + ((op[0][col][ev] + op[1][col][ev]) + (op[2][col][ev] + op[3][col][ev]));
-      const float d = sm.dout[col][ev] * g_sigmoid(o);
-      sm.dout[col][ev] = d;
-      S.bo += d;
-    }
-    __syncthreads();
-    if (on) {
-      over_rows(L, v, sm.dout, p.out, S.out);
-      from_few(sm.wo, sm.dout, 0.0f, p.out, L, v);   // the top signal
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = mask[NH - 1] >> i & 1 ? v[i] : slope * v[i];
-      S.b[NH] += total_of(v);
-      store_block(buf(kTop), L, v);
-    }
-    __syncthreads();
-    // ---- hidden layers: layer 1 + l maps A_{l+1} (buffer l) -> A_{l+2}
-#pragma unroll
-    for (int l = NH - 1; l >= 0; --l) {
-      const char* sig = buf(l == NH - 1 ? kTop : l + 1);
-      wgrad(sig, buf(l), L, steps, S.W[l]);
-      f32x16 acc;
-      if (on) product(R, NH + l, l > 0 ? NH + l - 1 : 0, woff, pf, sig, L, acc);
-      if (l > 0) {
-        if (on) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) v[i] = mask[l - 1] >> i & 1 ? acc[i] : slope * acc[i];
-          S.b[l] += total_of(v);
-        }
-        __syncthreads();                             // every wave is done with buffer l and the signal
-        if (on) {
-          store_block(buf(l), L, v);
-          if (kTop == 0 && l == NH - 1) first_layer(sm, b0, p.in, slope, L);
+    // The products: layer 1 + l maps A_{l+1} (buffer l) -> A_{l+2}, forward in turn, then the signals back.
+#pragma unroll 1
+    for (int st = 0; st < 2 * NH; ++st) {
+      const bool fwd = st < NH;
+      const int l = fwd ? st : 2 * NH - 1 - st;
+      const char* from = buf(fwd ? l : l == NH - 1 ? kTop : l + 1);
+      if (st == NH) {
+        // output layer: v = A_{NH+1}; its sums lie where the top signal will
+        Op* op = reinterpret_cast<Op*>(buf(kTop));
+        if (on) over_features(op, L, v, sm.wo, p.out);
+        __syncthreads();
+        if (col < p.out && ev < rows) {   // dL/d(last pre-activation) = dL/dtheta * sigmoid(o); zero on rows past the end
+          const float o = sm.bo[col] + ((op[0][col][ev] + op[1][col][ev]) + (op[2][col][ev] + op[3][col][ev]));
+          const float d = sm.dout[col][ev] * g_sigmoid(o);
+          sm.dout[col][ev] = d;
+          S.bo += d;
         }
         __syncthreads();
-      } else if (on) {
-        from_few(sm.w0, sm.n, b0, p.in, L, v);       // A_1's pre-activations again, for their signs
-#pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = v[i] > 0.0f ? acc[i] : slope * acc[i];
+        if (on) {
+          over_rows(L, v, sm.dout, p.out, S.out);
+          from_few(sm.wo, sm.dout, 0.0f, p.out, L, v);
+          leak(v, (uint32_t)(mask >> 16 * NH), slope);
+          S.b[NH] += total_of(v);
+          store_block(buf(kTop), L, v);
+        }
+        __syncthreads();
       }
+      if (!fwd) {                                    // (a choice: an index would put the sums into memory)
+        if (l == 0) wgrad(from, buf(0), L, steps, S.W[0]);
+        else if (l == 1) wgrad(from, buf(1), L, steps, S.W[NH > 1 ? 1 : 0]);
+        else wgrad(from, buf(2), L, steps, S.W[NH > 2 ? 2 : 0]);
+      }
+      if (on) {
+        // copies 0 .. NH - 1 forward, NH .. 2 NH - 1 the transposed ones, from the last back; then the next tile's first
+        const int copy = fwd ? st : NH + l, next = st < NH - 1 ? st + 1 : st == NH - 1 ? 2 * NH - 1 : l > 0 ? copy - 1 : 0;
+        const f32x16 acc = product(R, copy * kCopy, next * kCopy, w, from, L);
+        const float bias = fwd ? sm.bias[1 + l][L.fo] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = acc[i] + bias;
+        if (fwd) mask |= (uint64_t)signs(v) << 16 * (l + 1);
+        leak(v, (uint32_t)(mask >> 16 * (fwd ? l + 1 : l)), slope);
+        if (!fwd) {
+          const float t = total_of(v);
+#pragma unroll
+          for (int k = 0; k < NH; ++k) S.b[k] += k == l ? t : 0.0f;
+        }
+      }
+      if (st == 2 * NH - 1) break;                   // v = delta_1
+      if (!fwd) __syncthreads();                     // every wave is done with buffer l and the signal
+      if (on && st != NH - 1) store_block(buf(fwd ? l + 1 : l), L, v);
+      if (kTop == 0 && st == NH && on) (void)first_layer(sm, p.in, slope, L);
+      __syncthreads();
     }
-    // ---- first layer: v = delta_1
-    if (on) {
-      S.b[0] += total_of(v);
-      over_rows(L, v, sm.n, p.in, S.in);
-    }
+    // ---- first layer
+    if (on) over_rows(L, v, sm.n, p.in, S.in);
     if (p.dx) {
       Op* od = reinterpret_cast<Op*>(buf(NBUF - 1));   // of three buffers the last products read the others
       if (NH == 1) __syncthreads();
@@ -969,42 +991,42 @@ struct GenBwd : SplitLds<128, 64> {
 
   // What the workgroup has of a member, to its partial.  The two blocks' sums of a feature meet in LDS.
   static __device__ __forceinline__ void flush(const GenParams& p, Smem& sm, const Me& L, float* part, const Sums& S) {
+    const int in = p.in, out = p.out;
+    float* at = part + at_hidden(in, 0) + (32 * L.wf + 4 * L.lh) * H + 64 * L.we + L.lr;
 #pragma unroll
-    for (int l = 0; l < NH; ++l) {
-      float* at = part + p.poff_w[1 + l] + (32 * L.wf + 4 * L.lh) * H + 64 * L.we + L.lr;
+    for (int l = 0; l < NH; ++l, at += kHidden - 32 * H)
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int g = 0; g < 4; ++g, at += 8 * H)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) at[(8 * (i / 4) + i % 4) * H + 32 * k] = S.W[l][k][i];
-    }
-    constexpr int N = NH + 1 + 2 * kGMaxIO;
-    float (*stage)[H] = reinterpret_cast<float (*)[H]>(sm.act);
-    float s[N];
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int i = 0; i <= NH; ++i) s[i] = add_xor32(S.b[i]);
-#pragma unroll
-    for (int j = 0; j < kGMaxIO; ++j) {
-      s[NH + 1 + j] = add_xor32(S.in[j]);
-      s[NH + 1 + kGMaxIO + j] = add_xor32(S.out[j]);
-    }
+          for (int k = 0; k < 2; ++k) at[i * H + 32 * k] = S.W[l][k][4 * g + i];
+    constexpr int K = kGMaxIO / 2;
+    float (*stage)[2][H] = reinterpret_cast<float (*)[2][H]>(sm.act);   // [value][lane half][feature]
     __syncthreads();                                 // act is read
-    if (L.we == 1 && L.lh == 0)
+    if (L.we == 1) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) stage[i][L.fo] = s[i];
+      for (int k = 0; k < K; ++k) stage[k][L.lh][L.fo] = S.in[k], stage[K + k][L.lh][L.fo] = S.out[k];
+#pragma unroll
+      for (int l = 0; l <= NH; ++l) stage[2 * K + l][L.lh][L.fo] = S.b[l];
+    }
     __syncthreads();
-    if (L.we == 0 && L.lh == 0) {
+    if (L.we == 0) {
+      float* last = part + at_hidden(in, NH);        // [out][H], then out biases
 #pragma unroll
-      for (int i = 0; i < N; ++i) s[i] += stage[i][L.fo];
+      for (int k = 0; k < K; ++k) {
+        const int j = 2 * k + L.lh;
+        if (j < in) part[L.fo * in + j] = S.in[k] + stage[k][L.lh][L.fo];
+        if (j < out) last[j * H + L.fo] = S.out[k] + stage[K + k][L.lh][L.fo];
+      }
 #pragma unroll
-      for (int l = 0; l <= NH; ++l) part[p.poff_b[l] + L.fo] = s[l];
-#pragma unroll
-      for (int j = 0; j < kGMaxIO; ++j) {
-        if (j < p.in) part[p.poff_w[0] + L.fo * p.in + j] = s[NH + 1 + j];
-        if (j < p.out) part[p.poff_w[NH + 1] + j * H + L.fo] = s[NH + 1 + kGMaxIO + j];
+      for (int l = 0; l <= NH; ++l) {
+        const float s = add_xor32(S.b[l] + stage[2 * K + l][L.lh][L.fo]);
+        if (L.lh == 0) part[(l == 0 ? H * in : at_hidden(in, l - 1) + H * H) + L.fo] = s;
       }
     }
     const float bo = wave_total(S.bo);
-    if (L.lane == 0 && (int)(threadIdx.x >> 6) < p.out) part[p.poff_b[NH + 1] + (threadIdx.x >> 6)] = bo;
+    if (L.lane == 0 && (int)(threadIdx.x >> 6) < out) part[at_hidden(in, NH) + out * H + (threadIdx.x >> 6)] = bo;
   }
 
   // Of the `blocks` blocks of 32 rows in the order of their rows, workgroup g of `groups` (at most one a
@@ -1012,9 +1034,10 @@ struct GenBwd : SplitLds<128, 64> {
   // slot g + m of the partials: g + m rises from each of its (g, m) to the next.
   static __device__ void run(const GenParams& p) {
     __shared__ __attribute__((aligned(1024))) Smem sm;
-    const int64_t blocks = write_slots<32>(p);
-    const int64_t groups = min(blocks, (int64_t)gridDim.x);
+    const RoutedRows<32> rr(p);
+    const int64_t groups = min(rr.tiles, (int64_t)gridDim.x);
     const int64_t g = (int64_t)(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    if (blockIdx.x == 0) rr.write_slots(p, groups);
     if (g >= groups) return;
     Me L;
     {
@@ -1027,44 +1050,63 @@ struct GenBwd : SplitLds<128, 64> {
       L.we = wave >> 2;
       L.fo = 32 * L.wf + L.lr;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) L.w[q] = A.w[q];
-#pragma unroll
       for (int q = 0; q < 2; ++q) {
-        L.own[q] = L.we ? A.w[2 + q] : A.w[q];
+        L.own[q] = (L.we ? A.w[2 + q] : A.w[q]) + (uint32_t)L.wf * 32 * RB;
         L.tr[q] = L.we ? A.tr[1][q] : A.tr[0][q];
       }
+      L.woff = (uint32_t)(L.wf * KS * kTerms * 64 + L.lane) * 16u;
     }
-    const uint32_t woff = (uint32_t)(L.wf * KS * kTerms * 64 + L.lane) * 16u;
-    int64_t i = g * blocks / groups;
-    const int64_t end = (g + 1) * blocks / groups;
+    int64_t i = g * rr.tiles / groups;
+    const int64_t end = (g + 1) * rr.tiles / groups;
     GenTile t;
-    bool more = i < end && routed_tile<32>(p, i, t);
+    bool more = rr.find(p, i, t);                    // (there is one)
     while (more) {                                   // a member
-      const int m = __builtin_amdgcn_readfirstlane(t.m);
-      const Rsrc R = split_rsrc(p.split + (size_t)m * 2 * NH * (kCopy / 2), (uint32_t)(2 * NH * kCopy));
-      Sums S = {};
-      Prefetch pf;
+      const int m = t.m;
+      const Rsrc R = split_rsrc(p.split + (size_t)m * 2 * NH * (kCopy / 2), 2 * NH * kCopy);
+      Ring w;
 #pragma unroll
-      for (int q = 0; q < PD; ++q) load_w(R, woff, 0, q, pf.w[q]);
-      const float b0 = p.b[0][m * p.bsz[0] + L.fo];
-      float bh[NH];
+      for (int q = 0; q < PD; ++q) load_w(R, L.woff, q * kStep, w[q]);
+      int rows = (int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32));
+      Inputs given = inputs(p, t, rows);
+      // all reads before the first is used
+      const int f = threadIdx.x % H, j0 = threadIdx.x / H;   // 4 columns at a time
+      const float *W0 = p.W[0] + (int64_t)m * H * p.in + f * p.in, *WL = p.W[NH + 1] + (int64_t)m * H * p.out + f;
+      float e0[2], eo[2];
 #pragma unroll
-      for (int l = 0; l < NH; ++l) bh[l] = p.b[1 + l][m * p.bsz[1 + l] + L.fo];
-      __syncthreads();                               // the member before is read
-      for (int k = threadIdx.x; k < kGMaxIO * H; k += kGThreads) {
-        const int j = k / H, f = k % H;
-        sm.w0[j][f] = j < p.in ? p.W[0][m * p.wsz[0] + f * p.in + j] : 0.0f;
-        sm.wo[j][f] = j < p.out ? p.W[NH + 1][m * p.wsz[NH + 1] + k] : 0.0f;
+      for (int k = 0; k < 2; ++k) {
+        e0[k] = W0[min(j0 + 4 * k, p.in - 1)];
+        eo[k] = WL[min(j0 + 4 * k, p.out - 1) * H];
       }
+      const float* bias = j0 == 0 ? p.b[0] : NH == 1 || j0 == 1 ? p.b[1] : NH == 2 || j0 == 2 ? p.b[2] : p.b[3];
+      const float eb = bias[(int64_t)m * H + f], ebo = p.b[NH + 1][(int64_t)m * p.out + min(f, p.out - 1)];
+      __syncthreads();                               // the member before is read
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        sm.w0[j0 + 4 * k][f] = j0 + 4 * k < p.in ? e0[k] : 0.0f;
+        sm.wo[j0 + 4 * k][f] = j0 + 4 * k < p.out ? eo[k] : 0.0f;
+      }
+      if (j0 <= NH) sm.bias[j0][f] = eb;
+      if (threadIdx.x < kGMaxIO) sm.bo[threadIdx.x] = ebo;
+      Sums S = {};
+      bool same;
       do {
-        const int rows = __builtin_amdgcn_readfirstlane((int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32)));
-        __syncthreads();                             // the tile before is read
-        tile(p, sm, L, m, t.row0, rows, R, b0, bh, pf, S);
+        // the next tile, its inputs read while this one is worked on
+        const int64_t row0 = t.row0;
+        const int now = rows;
+        const Inputs here = given;
         i += rows > 32 ? 2 : 1;
         t.row0 += rows;
-        more = i < end && (t.row0 < t.end || routed_tile<32>(p, i, t));
-      } while (more && t.m == m);
-      flush(p, sm, L, p.part + (g + m) * p.P, S);
+        more = i < end;
+        if (more && t.row0 >= t.end) more = rr.find(p, i, t);
+        same = more && t.m == m;
+        if (same) {
+          rows = (int)min(t.end - t.row0, (int64_t)(i + 1 < end ? 64 : 32));
+          given = inputs(p, t, rows);
+        }
+        __syncthreads();                             // the tile before is read
+        tile(p, sm, L, row0, now, here, R, w, S);
+      } while (same);
+      flush(p, sm, L, p.part + (g + m) * p.PS, S);
     }
   }
 };
@@ -1131,30 +1173,38 @@ __global__ __launch_bounds__(256) void k_gen_reduce(GenReduceArgs r) {
   }
 }
 
-// The same for members on rows of their own: member blockIdx.y's partials are slots[m]'s.
-__global__ __launch_bounds__(256) void k_gen_reduce_routed(GenReduceArgs r, const int* __restrict__ slots) {
+// The same for members on rows of their own: member blockIdx.y's partials are slots[m]'s.  A thread takes four
+// values (partials are padded to 16 bytes), four slices of the partials side by side: with one value a thread
+// the blocks of 100 members took 51 us, four times as many as these.
+__global__ __launch_bounds__(256) void k_gen_reduce_routed(GenReduceArgs r, const int* __restrict__ slots, int64_t PS) {
   constexpr int S = 4, C = 256 / S;
-  __shared__ float red[S][C];
+  __shared__ f32x4 red[S][C];
   const int m = blockIdx.y, first = slots[2 * m], n = slots[2 * m + 1];
   const int le = threadIdx.x % C, sl = threadIdx.x / C;
-  const int64_t e = (int64_t)blockIdx.x * C + le;
-  float v = 0.f;
-  if (e < r.P) {
-    const float* src = r.part + (int64_t)first * r.P + e;
-    int t = sl;
-    for (; t + 4 * S < n; t += 8 * S) add_tiles<S, 8>(src, t, n, r.P, v);
-    if (t + 2 * S < n) add_tiles<S, 4>(src, t, n, r.P, v);
-    else if (t < n) add_tiles<S, 2>(src, t, n, r.P, v);
+  const int64_t e0 = ((int64_t)blockIdx.x * C + le) * 4;
+  f32x4 v = {};
+  if (e0 < r.P) {
+    const float* src = r.part + (int64_t)first * PS + e0;
+    for (int t = sl; t < n; t += 4 * S) {
+      f32x4 x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = *reinterpret_cast<const f32x4*>(src + (int64_t)min(t + u * S, n - 1) * PS);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (t + u * S < n) v += x[u];
+    }
   }
   red[sl][le] = v;
   __syncthreads();
-  if (sl != 0 || e >= r.P) return;
-  v = 0.f;
+  // thread (value q of a group of four): all 256 write, one each
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= r.P) return;
+  float t = 0.f;
 #pragma unroll
-  for (int q = 0; q < S; ++q) v += red[q][le];
+  for (int q = 0; q < S; ++q) t += reinterpret_cast<const float*>(&red[q][0])[threadIdx.x];
   for (int l = 0; l < r.n_layers; ++l) {
-    if (e >= r.poff_w[l] && e < r.poff_w[l] + r.wsz[l]) { r.dW[l][m * r.wsz[l] + (e - r.poff_w[l])] = v; return; }
-    if (e >= r.poff_b[l] && e < r.poff_b[l] + r.bsz[l]) { r.db[l][m * r.bsz[l] + (e - r.poff_b[l])] = v; return; }
+    if (e >= r.poff_w[l] && e < r.poff_w[l] + r.wsz[l]) { r.dW[l][m * r.wsz[l] + (e - r.poff_w[l])] = t; return; }
+    if (e >= r.poff_b[l] && e < r.poff_b[l] + r.bsz[l]) { r.db[l][m * r.bsz[l] + (e - r.poff_b[l])] = t; return; }
   }
 }
 
@@ -1383,14 +1433,19 @@ hipError_t launch_gen_backward(const sagips_gen& G, const float* noise, int64_t 
 // Members on rows of their own: tiles of 64 rows where those alone would cover half of the
 // compute units.
 namespace {
-inline int routed_rows(int64_t k, int n_cu) { return k / 64 >= n_cu / 2 ? 64 : 16; }
 // Tiles at most: every member's last one may be partly filled.
 inline int64_t routed_tiles(const sagips_gen& G, int64_t k, int T) { return k / T + (G.n_members < k ? G.n_members : k); }
+inline int routed_rows(int64_t k, int n_cu) { return k / 64 >= n_cu / 2 ? 64 : 16; }
+// The backward pass: where tiles of 16 rows would take a second turn of the compute units (4,096 rows of 8
+// members: 97 us in tiles of 16, 61 in tiles of 64).
+inline int routed_rows_back(const sagips_gen& G, int64_t k, int n_cu) { return routed_tiles(G, k, 16) > n_cu ? 64 : 16; }
+
 // Workgroups of the backward pass, a multiple of 8.
 inline int routed_groups(const sagips_gen& G, int64_t k, int T, int n_cu) {
   const int64_t t = routed_tiles(G, k, T == 64 ? 32 : 16), most = (n_cu + 7) / 8 * 8;
   return (int)(t < most ? (t + 7) / 8 * 8 : most);
 }
+inline int64_t padded_partial(int64_t P) { return (P + 3) & ~(int64_t)3; }
 // Bytes of the split copies.
 inline size_t routed_split_bytes(const sagips_gen& G) {
   return (size_t)G.n_members * 2 * (G.n_layers - 2) * split_copy_bytes(128);
@@ -1399,9 +1454,9 @@ inline size_t routed_split_bytes(const sagips_gen& G) {
 
 size_t gen_backward_routed_workspace(const sagips_gen& G, int64_t k, int n_cu) {
   const GenParams p = gen_params(G, nullptr, k);
-  const int T = routed_rows(k, n_cu);
+  const int T = routed_rows_back(G, k, n_cu);
   const size_t partials = routed_groups(G, k, T, n_cu) + (size_t)G.n_members;
-  return (T == 64 ? routed_split_bytes(G) : 0) + sizeof(float) * (size_t)p.P * partials + sizeof(int) * 2 * (size_t)G.n_members;
+  return (T == 64 ? routed_split_bytes(G) : 0) + sizeof(float) * (size_t)padded_partial(p.P) * partials + sizeof(int) * 2 * (size_t)G.n_members;
 }
 
 hipError_t launch_gen_forward_routed(const sagips_gen& G, const float* x, const int32_t* offsets, int64_t k, float* theta,
@@ -1423,7 +1478,7 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
                                       const float* dtheta, float* const* dW, float* const* db, float* dx, void* ws, int n_cu,
                                       hipStream_t st, Timer* tm) {
   GenParams p = gen_params(G, x, k);
-  const int T = routed_rows(k, n_cu), groups = routed_groups(G, k, T, n_cu), NH = G.n_layers - 2;
+  const int T = routed_rows_back(G, k, n_cu), groups = routed_groups(G, k, T, n_cu), NH = G.n_layers - 2;
   p.dtheta = dtheta;
   p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + (T == 64 ? routed_split_bytes(G) : 0));
   p.offsets = offsets;
@@ -1439,16 +1494,17 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  p.slots = reinterpret_cast<int*>(p.part + (size_t)p.P * (groups + (size_t)G.n_members));
+  p.PS = padded_partial(p.P);
+  p.slots = reinterpret_cast<int*>(p.part + (size_t)p.PS * (groups + (size_t)G.n_members));
   if (tm) tm->begin("gen_backward_routed");
   hipLaunchKernelGGL(v->bwd_routed[T == 64 ? 0 : 1], dim3(groups), dim3(kGThreads), 0, st, p);
   if (tm) tm->end();
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const GenReduceArgs r = reduce_args(G, p, 0, dW, db);
-  const dim3 grid((unsigned)((p.P + 63) / 64), G.n_members);
+  const dim3 grid((unsigned)((p.P + 255) / 256), G.n_members);
   if (tm) tm->begin("gen_reduce_routed");
-  hipLaunchKernelGGL(k_gen_reduce_routed, grid, dim3(256), 0, st, r, p.slots);
+  hipLaunchKernelGGL(k_gen_reduce_routed, grid, dim3(256), 0, st, r, p.slots, p.PS);
   if (tm) tm->end();
   return hipGetLastError();
 }
