@@ -138,7 +138,9 @@ sagips_status sagips_choice_logprob(sagips_ctx* c, const sagips_choices* C, cons
     if (s == SAGIPS_OK) s = apart(c, in, out);
     if (s != SAGIPS_OK) return s;
     DeviceGuard g(c->device);
-    return done(c, launch_choice(*C, choice, logp, entropy, top_choice, top_logp, stats, c->stream, timer_of(c)),
+    s = ensure_ws(c, choice_workspace(*C));
+    if (s != SAGIPS_OK) return s;
+    return done(c, launch_choice(*C, choice, logp, entropy, top_choice, top_logp, stats, c->ws, c->ticket, c->stream, timer_of(c)),
                 "choice_logprob launch");
   });
 }

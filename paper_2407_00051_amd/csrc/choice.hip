@@ -33,6 +33,11 @@ struct ChoiceArgs {
   float *logp, *entropy;
   int32_t* top_choice;
   float *top_logp, *stats;
+  // Rows cut into parts of `per` units: a record of each, and a counter a row that finds the part
+  // which ends last (NULL: k_choice_join follows).
+  int parts, per;
+  char* records;
+  uint32_t* ticket;
 };
 
 // Values of a 16-byte unit.
@@ -270,7 +275,91 @@ __device__ __forceinline__ uint32_t wave_kth(uint32_t key, int k) {
   return at;
 }
 
-template <class T, int TH, int R, bool kOnePass>
+
+// A part's record: its alternatives in order, then its sums.  Stored through to where every XCD sees it.
+__device__ __forceinline__ size_t record_bytes(int top) { return (size_t)top * 8 + 16; }
+struct Record {
+  char* at;
+  int top;
+  __device__ __forceinline__ Record(const ChoiceArgs& p, int64_t row, int part) : at(p.records + (row * p.parts + part) * record_bytes(p.top)), top(p.top) {}
+  __device__ __forceinline__ uint64_t* tops() const { return reinterpret_cast<uint64_t*>(at); }
+  __device__ __forceinline__ float* sums() const { return reinterpret_cast<float*>(at + (size_t)top * 8); }
+  __device__ __forceinline__ void put_top(int k, uint64_t c) const { __hip_atomic_store(tops() + k, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+  __device__ __forceinline__ void put(const Sums& a) const {
+    __hip_atomic_store(sums(), a.m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(sums() + 1, a.s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(sums() + 2, a.t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+};
+
+// Joins the records of a row (at most 64), by one wave: a part a lane.  Every part's list is in order, so that,
+// with j = (top - 1) / parts, the ceil(top / (j + 1))-th largest of the lists' entries j is no more than the
+// top-th largest of all; those from there on are collected and ranked.
+constexpr int kJoinHeld = 256;
+template <class T>
+__device__ __forceinline__ void join_parts(const ChoiceArgs& p, int64_t row, uint64_t* held, uint32_t* count) {
+  const int lane = threadIdx.x & 63;
+  const bool on = lane < p.parts;
+  const Record r(p, row, on ? lane : 0);
+  Sums a{kLowest, 0.0f, 0.0f};
+  const int j = p.top ? (p.top - 1) / p.parts : 0;
+  uint64_t entry = 0;
+  if (on) {
+    a = Sums{r.sums()[0], r.sums()[1], r.sums()[2]};
+    if (p.top) entry = r.tops()[j];
+  }
+  a = shifted(a, group_max<64>(a.m), p.scale2);
+  a.s = group_sum<64>(a.s);
+  a.t = group_sum<64>(a.t);
+  if (lane == 0) write_row<T>(p, row, a);
+  if (p.top == 0) return;
+  const float ls = log2f(a.s);
+  const uint32_t bound = max(wave_kth((uint32_t)(entry >> 32), (p.top + j) / (j + 1)), kMaskedKey + 1);
+  if (lane == 0) *count = 0;
+  __builtin_amdgcn_wave_barrier();
+  for (int k0 = 0; k0 < p.top; k0 += 8) {
+    uint64_t c[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = on && k0 + i < p.top ? r.tops()[k0 + i] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((uint32_t)(c[i] >> 32) >= bound) {
+        const uint32_t at = atomicAdd(count, 1u);
+        if (at < (uint32_t)kJoinHeld) held[at] = c[i];
+      }
+    if (!__any((uint32_t)(c[7] >> 32) >= bound)) break;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int n = __builtin_amdgcn_readfirstlane((int)*count);
+  if (n <= kJoinHeld) {
+    for (int i = lane; i < n; i += 64) {
+      const uint64_t c = held[i];
+      int rank = 0;
+      for (int k = 0; k < n; ++k) rank += held[k] > c;
+      if (rank < p.top) write_top(p, row, rank, c, a, ls);
+    }
+    for (int k = n + lane; k < p.top; k += 64) write_top(p, row, k, 0, a, ls);
+    return;
+  }
+  // many equal ones: the next of all, one after the other
+  int at = 0;
+  uint64_t c = on ? r.tops()[0] : 0;
+  for (int k = 0; k < p.top; ++k) {
+    const uint64_t first = group_first<64>(c);
+    if (lane == k) write_top(p, row, k, first, a, ls);
+    if (on && c == first) c = ++at < p.top ? r.tops()[at] : 0;
+  }
+}
+template <class T>
+__global__ __launch_bounds__(64) void k_choice_join(ChoiceArgs p) {
+  __shared__ uint64_t held[kJoinHeld];
+  __shared__ uint32_t count;
+  join_parts<T>(p, blockIdx.x, held, &count);
+}
+
+// kParts: a workgroup takes a part of a row.
+template <class T, int TH, int R, bool kOnePass, bool kParts>
 __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p) {
   constexpr int N = Unit<T>::N, W = TH / 64, G = TH / 64, kHeld = TH == 64 ? 256 : 1024;
   __shared__ Sums part[W];
@@ -280,18 +369,20 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   constexpr uint32_t none = sizeof(T) == 4 ? kFill<T> : kFill<T> << 16 | kFill<T>;
   const u32x4 fill = {none, none, none, none};
-  for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+  for (int64_t id = blockIdx.x; id < (kParts ? p.rows * p.parts : p.rows); id += gridDim.x) {
+    const int64_t row = kParts ? id / p.parts : id;
+    const int part_of = kParts ? (int)(id % p.parts) : 0;
     const RowView<T> v(p.x, row * p.stride, p.n);
-    const int units = v.units();
+    const int begin = kParts ? part_of * p.per : 0, units = kParts ? min(v.units(), begin + p.per) : v.units();
     u32x4 r[R];
     // all whole units' reads first, with no branch between them; then those at the row's ends
-    const int whole0 = v.lead ? 1 : 0, whole1 = (v.n + v.lead) / N - 1;
+    const int whole0 = max(v.lead ? 1 : 0, begin), whole1 = min((v.n + v.lead) / N, units) - 1;
     const auto load = [&](int q0) __attribute__((always_inline)) {
       if (whole1 >= whole0) {
 #pragma unroll
         for (int i = 0; i < R; ++i) r[i] = v.load_whole(min(max(q0 + i * TH + tid, whole0), whole1));
       }
-      if (whole0 == 0 && q0 + R * TH - 1 <= whole1) return;
+      if (whole0 <= q0 && q0 + R * TH - 1 <= whole1) return;
 #pragma unroll
       for (int i = 0; i < R; ++i) {
         const int q = q0 + i * TH + tid;
@@ -300,7 +391,7 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
     };
     float best = kLowest;                            // of the thread
     Sums a{kLowest, 0.0f, 0.0f};
-    for (int q0 = 0; q0 < units; q0 += TH * R) {
+    for (int q0 = begin; q0 < units; q0 += TH * R) {
       load(q0);
 #pragma unroll
       for (int i = 0; i < R; ++i) best = unit_max<T>(r[i], best);
@@ -330,9 +421,16 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
       a.s = group_sum<W>(a.s);
       a.t = group_sum<W>(a.t);
     }
-    if (tid == 0) write_row<T>(p, row, a);
+    if (tid == 0) {
+      if constexpr (kParts) Record(p, row, part_of).put(a);
+      else write_row<T>(p, row, a);
+    }
     if (p.top) {
       const float ls = log2f(a.s);
+      const auto put = [&](int k, uint64_t c) __attribute__((always_inline)) {
+        if constexpr (kParts) Record(p, row, part_of).put_top(k, c);
+        else write_top(p, row, k, c, a, ls);
+      };
       // at least top values are no less than the top-th of the 64 groups' largest
       const uint32_t key = max(wave_kth(order_key(group[lane]), p.top), kMaskedKey + 1);
       const float bound = order_value(key);
@@ -351,9 +449,9 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
         }
       };
       if (best >= bound) {                             // a thread whose largest is below has none
-        if constexpr (kOnePass) collect(0);
+        if constexpr (kOnePass) collect(begin);
         else
-          for (int q0 = 0; q0 < units; q0 += TH * R) {
+          for (int q0 = begin; q0 < units; q0 += TH * R) {
             load(q0);
             collect(q0);
           }
@@ -365,15 +463,15 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
           const uint64_t c = cand[i];
           int rank = 0;
           for (int k = 0; k < n; ++k) rank += cand[k] > c;
-          if (rank < p.top) write_top(p, row, rank, c, a, ls);
+          if (rank < p.top) put(rank, c);
         }
-        for (int k = n + tid; k < p.top; k += TH) write_top(p, row, k, 0, a, ls);
+        for (int k = n + tid; k < p.top; k += TH) put(k, 0);
       } else {
         // more equal values than are held: one alternative a pass over the row
         uint64_t last = ~0ull;
         for (int k = 0; k < p.top; ++k) {
           uint64_t c = 0;
-          for (int q = tid; q < units; q += TH) {
+          for (int q = begin + tid; q < units; q += TH) {
             const u32x4 u = v.load(q);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
@@ -386,8 +484,25 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
           if (lane == 0) firsts[wave] = c;
           __syncthreads();
           c = group_first<64>(lane < W ? firsts[lane] : 0);
-          if (tid == 0) write_top(p, row, k, c, a, ls);
+          if (tid == 0) put(k, c);
           last = c;
+        }
+      }
+    }
+    if constexpr (kParts) {
+      if (p.ticket) {                                  // one part a workgroup: the last of a row joins it
+        __shared__ bool last;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // every wave's records have arrived before the part is counted
+        __syncthreads();
+        if (tid == 0) {
+          uint32_t* counter = p.ticket + (1 + row) * kApart;
+          last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)p.parts - 1;
+          if (last) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (last && wave == 0) {
+          __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+          join_parts<T>(p, row, cand, &held);
         }
       }
     }
@@ -539,12 +654,30 @@ __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
 template <int n>
 using Int = std::integral_constant<int, n>;
 
+// Units a row has at most, wherever it begins.
 template <class T>
-hipError_t choice_forward(const ChoiceArgs& a, hipStream_t st) {
+int64_t most_units(const void* x, int64_t stride, int n) {
   constexpr int N = Unit<T>::N;
-  // units a row has at most, wherever it begins
-  const bool aligned = ((uintptr_t)a.x & 15) == 0 && a.stride * sizeof(T) % 16 == 0;
-  const int64_t units = ((int64_t)a.n + (aligned ? N - 1 : 2 * N - 2)) / N;
+  const bool aligned = ((uintptr_t)x & 15) == 0 && stride * sizeof(T) % 16 == 0;
+  return ((int64_t)n + (aligned ? N - 1 : 2 * N - 2)) / N;
+}
+
+// Rows in parts: where fewer rows than half of the compute units are longer than 32 KiB.  A part has 32 KiB, or
+// more where there would be over 64 or over 512 of them in all.  (One row of 131,072 bf16 logits, 20
+// alternatives: 16 us by one workgroup, 12 in parts.)
+constexpr int kPartUnits = 256 * 8, kPartsMost = 64;
+int choice_parts(int64_t rows, int64_t units) {
+  if (rows >= 128 || units <= kPartUnits) return 1;
+  int64_t n = (units + kPartUnits - 1) / kPartUnits;
+  n = n < kPartsMost ? n : kPartsMost;
+  return (int)(n < 512 / rows ? n : 512 / rows);
+}
+int64_t choice_units(const sagips_choices& C) {
+  return C.type == SAGIPS_BF16 ? most_units<u16>(C.logits, C.stride, C.n_choices) : most_units<float>(C.logits, C.stride, C.n_choices);
+}
+
+template <class T>
+hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
   const auto go_short = [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
     const int64_t blocks = (a.rows + 256 / L - 1) / (256 / L), most = 1 << 20;
@@ -554,10 +687,21 @@ hipError_t choice_forward(const ChoiceArgs& a, hipStream_t st) {
     constexpr int TH = decltype(threads)::value, R = decltype(per)::value;
     constexpr bool kOne = decltype(one)::value;
     const int64_t most = 256 * (int64_t)(2048 / TH) * 4;
-    hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), 0, st, a);
+    hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne, false>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), 0, st, a);
   };
   const std::true_type one{};
-  if (units <= 1) go_short(Int<1>{});
+  if (a.parts > 1) {
+    a.per = (int)((units + a.parts - 1) / a.parts);
+    const dim3 grid((unsigned)(a.rows * a.parts));
+    if (a.rows > kCounters) a.ticket = nullptr;
+    if (a.per <= kPartUnits) hipLaunchKernelGGL((k_choice_row<T, 256, 8, true, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((k_choice_row<T, 1024, 8, false, true>), grid, dim3(1024), 0, st, a);
+    if (!a.ticket) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      hipLaunchKernelGGL(k_choice_join<T>, dim3((unsigned)a.rows), dim3(64), 0, st, a);
+    }
+  } else if (units <= 1) go_short(Int<1>{});
   else if (units <= 2) go_short(Int<2>{});
   else if (units <= 4) go_short(Int<4>{});
   else if (units <= 8) go_short(Int<8>{});
@@ -578,9 +722,7 @@ hipError_t choice_forward(const ChoiceArgs& a, hipStream_t st) {
 
 template <class T, bool kUnits>
 hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
-  constexpr int N = kUnits ? Unit<T>::N : 1;
-  const bool aligned = ((uintptr_t)a.x & 15) == 0 && a.stride * sizeof(T) % 16 == 0;
-  const int64_t units = ((int64_t)a.n + (aligned || N == 1 ? N - 1 : 2 * N - 2)) / N;
+  const int64_t units = kUnits ? most_units<T>(a.x, a.stride, a.n) : a.n;
   const auto go = [&](auto lanes, auto per) {
     constexpr int L = decltype(lanes)::value, R = decltype(per)::value;
     a.chunks = (int)((units + L * R - 1) / (L * R));
@@ -597,12 +739,19 @@ hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
 
 }  // namespace
 
+size_t choice_workspace(const sagips_choices& C) {
+  const int parts = choice_parts(C.rows, choice_units(C));
+  return parts > 1 ? (size_t)C.rows * parts * ((size_t)C.top * 8 + 16) : 0;
+}
+
 hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
-                         float* top_logp, float* stats, hipStream_t st, Timer* tm) {
-  ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)(C.scale * 1.4426950408889634),
-               choice, logp, entropy, top_choice, top_logp, stats};
+                         float* top_logp, float* stats, void* ws, uint32_t* ticket, hipStream_t st, Timer* tm) {
+  const int64_t units = choice_units(C);
+  const ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)(C.scale * 1.4426950408889634),
+                     choice, logp, entropy, top_choice, top_logp, stats, choice_parts(C.rows, units), 0,
+                     static_cast<char*>(ws), ticket};
   if (tm) tm->begin("choice_logprob");
-  const hipError_t e = C.type == SAGIPS_BF16 ? choice_forward<u16>(a, st) : choice_forward<float>(a, st);
+  const hipError_t e = C.type == SAGIPS_BF16 ? choice_forward<u16>(a, units, st) : choice_forward<float>(a, units, st);
   if (tm) tm->end();
   return e;
 }

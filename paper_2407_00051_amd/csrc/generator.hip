@@ -763,13 +763,12 @@ struct GenBwd : SplitLds<128, 64> {
   }
 
   // act B for the wave's features and block, B the split copy at `copy` (bytes); w holds the copy's first steps,
-  // and in the end those of the one at `next`.  Six products a step into one accumulator, smallest first.
+  // and in the end those of the one at `next`.
   static __device__ __forceinline__ f32x16 product(Rsrc R, uint32_t copy, uint32_t next, Ring& w, const char* buf, const Me& L) {
-    constexpr int ta[6] = {2, 0, 1, 1, 0, 0}, tb[6] = {0, 2, 1, 0, 1, 0};
-    f32x16 acc = {};
-    bf16x8 a[2][kTerms];
+    f32x16 acc[1] = {}, corr[1] = {};
+    bf16x8 a[2][1][kTerms];
     const char *at0 = buf + L.tr[0], *at1 = buf + L.tr[1];
-    read_rows(at0, at1, 0, a[0]);
+    read_rows(at0, at1, 0, a[0][0]);
     uint32_t more = copy + PD * kStep;
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
@@ -780,16 +779,15 @@ struct GenBwd : SplitLds<128, 64> {
         __builtin_amdgcn_sched_barrier(0);
         load_w(R, L.woff, more, w[(q + PD) % (PD + 1)]);
         more = q == 0 && half ? next : more + kStep;   // step 7 is loaded at step 4
-        read_rows(at0, at1, q < 3 ? 16 * RB : turn, a[(q + 1) & 1]);
+        read_rows(at0, at1, q < 3 ? 16 * RB : turn, a[(q + 1) & 1][0]);
         at0 += q < 3 ? 16 * RB : turn;
         at1 += q < 3 ? 16 * RB : turn;
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int k = 0; k < 6; ++k) acc = mfma32(a[q & 1][ta[k]], w[q][tb[k]], acc);
+        split_mfma_apart<false, false>(a[q & 1], w[q], acc, corr);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    return acc;
+    return acc[0] + corr[0];
   }
 
   // W += signal^T A over `steps` times 16 rows.

@@ -98,8 +98,10 @@ hipError_t launch_gen_backward_routed(const sagips_gen& G, const float* x, const
                                       hipStream_t st, Timer* tm);
 
 // choice.hip -----------------------------------------------------------------
+// `ticket`: see policy.hip below.
+size_t choice_workspace(const sagips_choices& C);
 hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
-                         float* top_logp, float* stats, hipStream_t st, Timer* tm);
+                         float* top_logp, float* stats, void* ws, uint32_t* ticket, hipStream_t st, Timer* tm);
 hipError_t launch_choice_backward(const sagips_choices& C, const sagips_choice_grads& g, void* dlogits, int64_t dstride,
                                   hipStream_t st, Timer* tm);
 
