@@ -143,82 +143,106 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs p) {
 }
 
 // ---- rows -------------------------------------------------------------------------
-// A row is `units` units of B bytes (16 where the rows' addresses allow, else a value).  2^lx lanes
-// of a workgroup take a row, several rows a workgroup where they are short.
+// A row is taken in pieces of 16 bytes, wherever it begins (rows of odd widths begin on any value, and the memory
+// takes such reads and writes whole: for 16,384 x 8 rows of 333 bf16 values dispatch took 38 us in single values
+// and takes 20 so, combine 73 and 23, its backward 73 and 47), and the values behind the last whole piece one by
+// one.  Both go through one loop: with a loop of their own behind it the single values waited for a second round
+// trip (combine 34 us, backward 59).  2^lx lanes of a workgroup take a row, several rows a workgroup where they
+// are short.
 struct RowsArgs {
   const int32_t* place;
   int64_t rows, items;
-  int slots, units, lx;
+  int slots, width, lx;
   const void *x, *y;
   const float* weight;
   void *out, *dy;
   float* dweight;
 };
 
-template <class T, int B>
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_by2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_by4 __attribute__((aligned(4)));
+template <class T>
 struct Piece {
-  static constexpr int N = B / sizeof(T);
-  typedef std::conditional_t<B == 16, uint4, std::conditional_t<B == 4, uint32_t, u16>> Raw;
-  static __device__ __forceinline__ float get(const Raw& r, int j) {
-    if constexpr (B == 16) {
-      if constexpr (sizeof(T) == 4) return __uint_as_float((&r.x)[j]);
-      else return j & 1 ? bf16_hi((&r.x)[j >> 1]) : bf16_lo((&r.x)[j >> 1]);
-    } else if constexpr (sizeof(T) == 4) {
-      return __uint_as_float(r);
-    } else {
-      return __uint_as_float((uint32_t)r << 16);
-    }
+  static constexpr int N = 16 / sizeof(T);
+  typedef std::conditional_t<sizeof(T) == 4, uint32_t, u16> One;
+  typedef std::conditional_t<sizeof(T) == 4, u32x4_by4, u32x4_by2> Loose;
+  // A single value stands first, with zeros behind it.
+  static __device__ __forceinline__ u32x4 load(const T* at, bool whole) {
+    u32x4 r = {0, 0, 0, 0};
+    if (whole) r = *reinterpret_cast<const Loose*>(at);
+    else r.x = *reinterpret_cast<const One*>(at);
+    return r;
   }
-  static __device__ __forceinline__ Raw make(const float (&v)[N]) {
-    if constexpr (B == 16) {
-      if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-      else return make_uint4(pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4], v[5]), pk_bf16(v[6], v[7]));
-    } else if constexpr (sizeof(T) == 4) {
-      return __float_as_uint(v[0]);
-    } else {
-      return (u16)pk_bf16(v[0], 0.0f);
-    }
+  static __device__ __forceinline__ void store(T* at, bool whole, u32x4 v) {
+    if (whole) *reinterpret_cast<Loose*>(at) = v;
+    else *reinterpret_cast<One*>(at) = (One)v.x;
+  }
+  static __device__ __forceinline__ float get(u32x4 r, int j) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(r[j]);
+    else return j & 1 ? bf16_hi(r[j >> 1]) : bf16_lo(r[j >> 1]);
+  }
+  static __device__ __forceinline__ u32x4 make(const float (&v)[N]) {
+    if constexpr (sizeof(T) == 4) return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else return u32x4{pk_bf16(v[0], v[1]), pk_bf16(v[2], v[3]), pk_bf16(v[4 % N], v[5 % N]), pk_bf16(v[6 % N], v[7 % N])};
   }
 };
 
 constexpr int kRowThreads = 256;
 constexpr int kAtOnce = 8;         // items of a row whose reads are in flight together
 
-template <class Raw>
+// Where value v of the row at a position lies.  The position is opaque, so that the addresses of all items are not
+// formed before the loop over a row and kept in registers (combine's backward, 65,536 rows of 1,000 fp32 values:
+// 183 us with them, 169 so).
+template <class T>
+__device__ __forceinline__ T* item_at(T* base, int32_t position, int width, int v) {
+  asm volatile("" : "+v"(position));
+  return base + (int64_t)position * width + v;
+}
+
+// What a thread does of a row: f(first value, whole) for its pieces, the whole ones first.
+template <class T, class F>
+__device__ __forceinline__ void over_pieces(const RowsArgs& p, F f) {
+  constexpr int N = Piece<T>::N;
+  const int full = p.width / N, all = full + p.width % N, step = 1 << p.lx;
+  for (int u = threadIdx.x & (step - 1); u < all; u += step) f(u < full ? u * N : full * N + (u - full), u < full);
+}
+
+template <class T>
 __global__ __launch_bounds__(kRowThreads) void k_dispatch(RowsArgs p) {
-  const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
+  typedef Piece<T> P;
+  const int per = kRowThreads >> p.lx;
   for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
     const int32_t* place = p.place + row * p.slots;
-    for (int u = l; u < p.units; u += step) {
-      const Raw v = ((const Raw*)p.x)[row * p.units + u];
+    over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
+      const u32x4 raw = P::load((const T*)p.x + row * p.width + v, whole);
       for (int k = 0; k < p.slots; ++k) {
         const int64_t at = place[k];
-        if (at >= 0 && at < p.items) ((Raw*)p.out)[at * p.units + u] = v;
+        if (at >= 0 && at < p.items) P::store((T*)p.out + at * p.width + v, whole, raw);
       }
-    }
+    });
   }
 }
 
-template <class T, int B>
+template <class T>
 __global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
-  typedef Piece<T, B> P;
-  typedef typename P::Raw Raw;
-  const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
+  typedef Piece<T> P;
+  const int per = kRowThreads >> p.lx;
   for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
     const int32_t* place = p.place + row * p.slots;
     const float* weight = p.weight ? p.weight + row * p.slots : nullptr;
-    for (int u = l; u < p.units; u += step) {
+    over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
       float s[P::N] = {};
       for (int k0 = 0; k0 < p.slots; k0 += kAtOnce) {
-        Raw v[kAtOnce];
+        u32x4 y[kAtOnce];
         float w[kAtOnce];
         bool on[kAtOnce];
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          const int64_t at = k0 + i < p.slots ? place[k0 + i] : -1;
+          const int32_t at = k0 + i < p.slots ? place[k0 + i] : -1;
           on[i] = at >= 0 && at < p.items;
           if (on[i]) {
-            v[i] = ((const Raw*)p.y)[at * p.units + u];
+            y[i] = P::load(item_at((const T*)p.y, at, p.width, v), whole);
             w[i] = weight ? weight[k0 + i] : 1.0f;
           }
         }
@@ -226,37 +250,37 @@ __global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
         for (int i = 0; i < kAtOnce; ++i)
           if (on[i])
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) s[j] = fmaf(w[i], P::get(v[i], j), s[j]);
+            for (int j = 0; j < P::N; ++j) s[j] = fmaf(w[i], P::get(y[i], j), s[j]);
       }
-      ((Raw*)p.out)[row * p.units + u] = P::make(s);
-    }
+      P::store((T*)p.out + row * p.width + v, whole, P::make(s));
+    });
   }
 }
 
-// 2^lx lanes, at most a wave, take a row, so that <dout, y> needs no exchange between waves.
-template <class T, int B>
+// 2^lx lanes take a row: at most a wave (then <dout, y> needs no exchange between waves), or the workgroup.
+template <class T>
 __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
-  typedef Piece<T, B> P;
-  typedef typename P::Raw Raw;
+  typedef Piece<T> P;
+  __shared__ float part[kRowThreads / 64][kAtOnce];
   const int l = threadIdx.x & ((1 << p.lx) - 1), step = 1 << p.lx, per = kRowThreads >> p.lx;
   for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
     const int32_t* place = p.place + row * p.slots;
     for (int k0 = 0; k0 < p.slots; k0 += kAtOnce) {
       float dot[kAtOnce] = {}, w[kAtOnce];
-      int64_t at[kAtOnce];
+      int32_t at[kAtOnce];
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         at[i] = k0 + i < p.slots ? place[k0 + i] : -1;
         if (at[i] >= p.items) at[i] = -1;
         w[i] = p.weight && k0 + i < p.slots ? p.weight[row * p.slots + k0 + i] : 1.0f;
       }
-      for (int u = l; u < p.units; u += step) {
-        const Raw g = ((const Raw*)p.x)[row * p.units + u];
-        Raw v[kAtOnce];
+      over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
+        const u32x4 g = P::load((const T*)p.x + row * p.width + v, whole);
+        u32x4 y[kAtOnce];
         if (p.dweight) {
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i)
-            if (at[i] >= 0) v[i] = ((const Raw*)p.y)[at[i] * p.units + u];
+            if (at[i] >= 0) y[i] = P::load(item_at((const T*)p.y, at[i], p.width, v), whole);
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
@@ -265,19 +289,29 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
             float o[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) o[j] = w[i] * P::get(g, j);
-            ((Raw*)p.dy)[at[i] * p.units + u] = P::make(o);
+            P::store(item_at((T*)p.dy, at[i], p.width, v), whole, P::make(o));
           }
           if (p.dweight)
 #pragma unroll
-            for (int j = 0; j < P::N; ++j) dot[i] = fmaf(P::get(g, j), P::get(v[i], j), dot[i]);
+            for (int j = 0; j < P::N; ++j)           // (zeros behind a single value, in both)
+              dot[i] = fmaf(P::get(g, j), P::get(y[i], j), dot[i]);
         }
-      }
+      });
       if (p.dweight) {
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
-          float s = dot[i];
-          for (int d = 1; d < step; d <<= 1) s += __shfl_xor(s, d, 64);
-          if (l == 0 && k0 + i < p.slots) p.dweight[row * p.slots + k0 + i] = s;
+          for (int d = 1; d < min(step, 64); d <<= 1) dot[i] += __shfl_xor(dot[i], d, 64);
+          if (step > 64 && (l & 63) == 0) part[l >> 6][i] = dot[i];
+        }
+        if (step > 64) {                             // the workgroup's only row
+          __syncthreads();
+          if (l < kAtOnce && k0 + l < p.slots)
+            p.dweight[row * p.slots + k0 + l] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
+          __syncthreads();
+        } else if (l == 0) {
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i)
+            if (k0 + i < p.slots) p.dweight[row * p.slots + k0 + i] = dot[i];
         }
       }
     }
@@ -292,21 +326,15 @@ int route_per(int64_t n) {
 }
 int route_blocks(int64_t n) { return (int)((n + route_per(n) - 1) / route_per(n)); }
 
-// Bytes of a unit: 16 where every row of every array begins on 16 bytes.
-template <class... Ptr>
-bool whole_units(const sagips_routed& R, Ptr... p) {
-  const int size = R.type == SAGIPS_BF16 ? 2 : 4;
-  return (int64_t)R.width * size % 16 == 0 && ((((uintptr_t)p & 15) == 0) && ...);
-}
-RowsArgs rows_args(const sagips_routed& R, bool whole, int most_lx) {
+RowsArgs rows_args(const sagips_routed& R) {
   RowsArgs a{};
   a.place = R.place;
   a.rows = R.rows;
   a.items = R.rows * R.slots;
   a.slots = R.slots;
-  const int size = R.type == SAGIPS_BF16 ? 2 : 4;
-  a.units = whole ? (int)((int64_t)R.width * size / 16) : R.width;
-  while (a.lx < most_lx && (1 << a.lx) < a.units) ++a.lx;
+  a.width = R.width;
+  const int n = R.type == SAGIPS_BF16 ? 8 : 4, pieces = R.width / n + R.width % n;
+  while (a.lx < 8 && (1 << a.lx) < pieces) ++a.lx;
   return a;
 }
 dim3 rows_grid(const RowsArgs& a) {
@@ -340,44 +368,39 @@ hipError_t launch_route(const int32_t* member, int64_t n, int members, int32_t* 
 }
 
 hipError_t launch_dispatch(const sagips_routed& R, const void* x, void* sorted, hipStream_t st, Timer* tm) {
-  const bool whole = whole_units(R, x, sorted);
-  RowsArgs a = rows_args(R, whole, 8);
+  RowsArgs a = rows_args(R);
   a.x = x;
   a.out = sorted;
   if (tm) tm->begin("dispatch");
-  if (whole) hipLaunchKernelGGL(k_dispatch<uint4>, rows_grid(a), dim3(kRowThreads), 0, st, a);
-  else if (R.type == SAGIPS_F32) hipLaunchKernelGGL(k_dispatch<uint32_t>, rows_grid(a), dim3(kRowThreads), 0, st, a);
-  else hipLaunchKernelGGL(k_dispatch<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_dispatch<float> : k_dispatch<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
   if (tm) tm->end();
   return hipGetLastError();
 }
 
 hipError_t launch_combine(const sagips_routed& R, const void* y, const float* weight, void* out, hipStream_t st, Timer* tm) {
-  const bool whole = whole_units(R, y, out), f32 = R.type == SAGIPS_F32;
-  RowsArgs a = rows_args(R, whole, 8);
+  RowsArgs a = rows_args(R);
   a.y = y;
   a.weight = weight;
   a.out = out;
-  const auto kernel = whole ? (f32 ? k_combine<float, 16> : k_combine<u16, 16>) : (f32 ? k_combine<float, 4> : k_combine<u16, 2>);
   if (tm) tm->begin("combine");
-  hipLaunchKernelGGL(kernel, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_combine<float> : k_combine<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
   if (tm) tm->end();
   return hipGetLastError();
 }
 
 hipError_t launch_combine_backward(const sagips_routed& R, const void* dout, const void* y, const float* weight, void* dy,
                                    float* dweight, hipStream_t st, Timer* tm) {
-  const bool whole = whole_units(R, dout, y, dy), f32 = R.type == SAGIPS_F32;
-  RowsArgs a = rows_args(R, whole, 6);
+  RowsArgs a = rows_args(R);
+  // a wave a row where there are rows enough for all; long rows otherwise by a workgroup (8 slots of 8,192 bf16
+  // values: 300 rows 51 us by a wave each and 23 so, one row 38 and 19)
+  if (a.lx > 6) a.lx = R.rows < 2048 ? 8 : 6;
   a.x = dout;
   a.y = y;
   a.weight = weight;
   a.dy = dy;
   a.dweight = dweight;
-  const auto kernel = whole ? (f32 ? k_combine_grad<float, 16> : k_combine_grad<u16, 16>)
-                            : (f32 ? k_combine_grad<float, 4> : k_combine_grad<u16, 2>);
   if (tm) tm->begin("combine_backward");
-  hipLaunchKernelGGL(kernel, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_combine_grad<float> : k_combine_grad<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
   if (tm) tm->end();
   return hipGetLastError();
 }
