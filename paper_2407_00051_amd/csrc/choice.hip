@@ -20,7 +20,6 @@
 namespace sagips {
 namespace {
 
-constexpr int kMaxTop = SAGIPS_MAX_TOP;
 constexpr float kLowest = -INFINITY;
 constexpr uint32_t kMaskedKey = 0x007fffffu;   // order_key(-infinity)
 
@@ -138,9 +137,14 @@ template <int L>
 __device__ __forceinline__ float group_max(float v) {   // NaN where one is
   return group_reduce<L>(v, [](float a, float b) { return __builtin_elementwise_maximum(a, b); });
 }
+// The same bits in every lane: every exchange is between two lanes that add the same two numbers.  With a product
+// before it one lane's could become a fused one (then which lane writes an alternative would show in its ln p).
 template <int L>
 __device__ __forceinline__ float group_sum(float v) {
-  return group_reduce<L>(v, [](float a, float b) { return a + b; });
+  return group_reduce<L>(v, [](float a, float b) {
+#pragma clang fp contract(off)
+    return a + b;
+  });
 }
 template <int L>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {

@@ -46,7 +46,8 @@ class Mixture:
         return [t for pair in zip(self.dW, self.db) for t in pair] + [self.dWr, self.dbr]
 
     def forward(self, noise):
-        """theta [k][out]; what backward needs is kept until the next call."""
+        """theta [k][out]; what backward needs is kept until the next call.  A row whose logits hold a NaN or +inf
+        has no members: its theta is NaN, not the 0 of an empty sum."""
         import torch
         c = self.ctx
         logits = torch.addmm(self.br, noise, self.Wr.t())
@@ -57,7 +58,8 @@ class Mixture:
         x = c.dispatch(noise, plan)
         theta = c.gen_forward_routed(self.W, self.b, x, plan["offsets"], slope=self.slope)
         self._held = (noise, logits, chosen, own, weight, plan, x, theta)
-        return c.combine(theta, plan, weight)
+        nan = chosen["entropy"][:, None]                               # finite otherwise
+        return c.combine(theta, plan, weight).addcmul_(nan, nan, value=0.0)
 
     def backward(self, dL_dtheta) -> None:
         """The gradients of the last forward call's parameters from dL/dtheta [k][out]."""

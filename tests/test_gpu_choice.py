@@ -164,6 +164,63 @@ def test_alternatives_that_one_thread_holds(gpu_ctx, n, V, dtype):
         _check_forward(f, x, None, 32, 1.0, f"pattern {k}")
 
 
+@pytest.mark.parametrize("n,V,dtype", [(16, 9001, "f32"), (17, 9001, "f32"), (40, 20011, "bf16"), (127, 17001, "bf16"),
+                                       (128, 17001, "bf16"), (20, 70001, "f32"), (1, 600011, "bf16")])
+def test_few_long_rows(gpu_ctx, n, V, dtype):
+    """Rows in parts, joined by the last part or by a second launch, and the first number of rows that are not."""
+    print(f"case parts {n} x {V} {dtype}", flush=True)
+    x = _logits(n, V, dtype, V, 0.2, 1)
+    x[n // 2] = 1.5                                       # equal alternatives in every part
+    x[n // 2, 5] = float("-inf")
+    x[n - 1, 70:] = float("-inf") if n > 1 else 0.25      # parts of nothing
+    choice = (np.arange(n) * 11 + 3) % V
+    c = torch.tensor(choice.astype(np.int32), device="cuda:0")
+    f = gpu_ctx.choice_logprob(x, c, top=32, scale=0.9)
+    again = gpu_ctx.choice_logprob(x, c, top=32, scale=0.9)
+    torch.cuda.synchronize()
+    _check_forward(f, x, choice, 32, 0.9, f"parts {n} x {V}")
+    assert all(torch.equal(f[k], again[k]) for k in f)
+
+
+def test_more_contexts_than_counters(gpu_ctx):
+    """Contexts beyond the 64 that have counters join the parts in a second launch, with the same bits."""
+    print("case 70 contexts", flush=True)
+    x = _logits(2, 30001, "f32", 5)
+    c = torch.tensor([1, 30000], dtype=torch.int32, device="cuda:0")
+    want = gpu_ctx.choice_logprob(x, c, top=20)
+    many = [sg.Context(0) for _ in range(70)]
+    for ctx in many:
+        f = ctx.choice_logprob(x, c, top=20)
+        assert all(torch.equal(f[k], want[k]) for k in f)
+    for ctx in many:
+        ctx.close()
+
+
+def test_parts_in_a_graph(gpu_ctx):
+    """Rows in parts captured and replayed, with eager calls of the context between: the counters are left as found."""
+    print("case parts captured", flush=True)
+    x = _logits(3, 40001, "bf16", 6)
+    c = torch.tensor([7, 0, 40000], dtype=torch.int32, device="cuda:0")
+    want = gpu_ctx.choice_logprob(x, c, top=9)
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    with torch.cuda.stream(st):
+        ctx = sg.Context(0, stream=st)
+        ctx.choice_logprob(x, c, top=9)                   # makes the workspace, outside the capture
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st, capture_error_mode="relaxed"):
+            out = ctx.choice_logprob(x, c, top=9)
+        for _ in range(3):
+            for t in out.values():
+                t.fill_(-2)
+            eager = ctx.choice_logprob(x, c, top=9)
+            graph.replay()
+            st.synchronize()
+            assert all(torch.equal(out[k], want[k]) and torch.equal(eager[k], want[k]) for k in want)
+        ctx.close()
+
+
 def test_gradient_in_place_strided_and_of_other_alignment(gpu_ctx):
     for dtype in ("f32", "bf16"):
         for V, pad, opad in ((37, 3, 0), (37, 0, 5), (1500, 4, 4), (5000, 1, 2), (40, 24, 8)):

@@ -205,6 +205,21 @@ def test_a_router_that_leaves_a_row_without_members(gpu_ctx):
     assert (theta[1] == 0).all() and (theta[0] > 1).all() and torch.isfinite(d).all() and (d[1] == 0).all()
 
 
+def test_nan_in_the_router_shows(gpu_ctx):
+    """A row whose logits are NaN or +inf has theta NaN; the others are those of the router without them."""
+    _, (W, b, Wr, br, n) = _setup(4, 10, 8)
+    mix = Mixture(gpu_ctx, W, b, Wr, br)
+    good = mix.forward(n).clone()
+    n[3, 2], n[6] = float("nan"), float("inf")
+    theta = mix.forward(n)
+    mix.backward(torch.ones_like(theta))
+    torch.cuda.synchronize()
+    rest = [i for i in range(10) if i not in (3, 6)]
+    # the router's product is the library's: its bits need not be the same, and a weight moves by 2 u |logit| at most
+    assert torch.isnan(theta[[3, 6]]).all() and torch.allclose(theta[rest], good[rest], rtol=1e-5)
+    assert torch.isnan(mix.dWr).any() and all(torch.isfinite(t).all() for t in mix.dW)
+
+
 def test_gan_loop_with_a_mixture(gpu_ctx):
     """Runs, moves every parameter that has a gradient, and keeps them finite."""
     (_, _, _, _, _), (W, b, Wr, br, n) = _setup(4, 128, 7)

@@ -93,6 +93,30 @@ def test_dispatch_combine_and_gradient(gpu_ctx, rows, slots, members, width, dty
         assert none is None and torch.equal(only, dy)
 
 
+@pytest.mark.parametrize("rows,slots,width,dtype", [
+    (2047, 2, 1030, "bf16"), (2048, 2, 1030, "bf16"), (2500, 9, 515, "f32"), (1, 32, 20001, "bf16"), (3, 5, 9999, "f32")])
+def test_gradient_of_rows_by_a_wave_and_by_a_workgroup(gpu_ctx, rows, slots, width, dtype):
+    """Few long rows and many: <dout, y> joined in a wave and across a workgroup's waves."""
+    print(f"case gradient rows {rows} x {slots}, {width} {dtype}", flush=True)
+    g = torch.Generator(device="cuda:0").manual_seed(width)
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda:0")     # noqa: E731
+    p = gpu_ctx.route(_member(rows, slots, 6, rows), 6)
+    n, place = int(p["offsets"][-1]), p["place"].long()
+    y, dout, w = randn(rows * slots, width).to(DT[dtype]), randn(rows, width).to(DT[dtype]), randn(rows, slots)
+    dy, dw = gpu_ctx.combine_backward(dout, y, p, w)
+    torch.cuda.synchronize()
+    # in float64 on the device (the oracle's loops would take minutes here)
+    items = torch.where((place < 0)[..., None], torch.zeros((), dtype=torch.float64, device="cuda:0"), y.double()[place.clamp(min=0)])
+    prod = items * dout.double()[:, None]
+    assert ((dw.double() - prod.sum(2)).abs() <= U * (width / 64 + 14) * prod.abs().sum(2)).all()
+    order = p["order"][:n].long()
+    ref = w.double().view(-1)[order, None] * dout.double()[order // slots]
+    half = torch.finfo(DT[dtype]).eps / 2
+    assert ((dy[:n].double() - ref).abs() <= (half + 2 * U) * ref.abs()).all()
+    assert all(torch.equal(a[:n], b[:n]) if a.dim() == 2 and a.shape[0] == rows * slots else torch.equal(a, b)
+               for a, b in zip((dy, dw), gpu_ctx.combine_backward(dout, y, p, w)))
+
+
 def test_places_outside_the_rows_are_none(gpu_ctx):
     """A plan of the caller's own: positions outside [0, rows * slots) are followed nowhere."""
     place = torch.tensor([[0, 6], [-7, 2 ** 31 - 1], [3, -2 ** 31]], dtype=torch.int32, device="cuda:0")
