@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kRouteThreads) void k_route_place(RouteArgs p) {
 // ---- rows -------------------------------------------------------------------------
 // A row is taken in pieces of 16 bytes, wherever it begins (rows of odd widths begin on any value, and the memory
 // takes such reads and writes whole: for 16,384 x 8 rows of 333 bf16 values dispatch took 38 us in single values
-// and takes 20 so, combine 73 and 23, its backward 73 and 47), and the values behind the last whole piece one by
+// and takes 20 so, combine 73 and 23, its backward 73 and 42), and the values behind the last whole piece one by
 // one.  Both go through one loop: with a loop of their own behind it the single values waited for a second round
 // trip (combine 34 us, backward 59).  2^lx lanes of a workgroup take a row, several rows a workgroup where they
 // are short.
@@ -192,29 +192,35 @@ constexpr int kRowThreads = 256;
 constexpr int kAtOnce = 8;         // items of a row whose reads are in flight together
 
 // Where value v of the row at a position lies.  The position is opaque, so that the addresses of all items are not
-// formed before the loop over a row and kept in registers (combine's backward, 65,536 rows of 1,000 fp32 values:
-// 183 us with them, 169 so).
-template <class T>
+// formed before the loop over a row and kept in registers (kLoop; combine's backward, 65,536 rows of 1,000 fp32
+// values: 183 us with them, 169 so).
+template <bool kLoop, class T>
 __device__ __forceinline__ T* item_at(T* base, int32_t position, int width, int v) {
-  asm volatile("" : "+v"(position));
+  if constexpr (kLoop) asm volatile("" : "+v"(position));
   return base + (int64_t)position * width + v;
 }
 
-// What a thread does of a row: f(first value, whole) for its pieces, the whole ones first.
-template <class T, class F>
+// What a thread does of a row: f(first value, whole) for its pieces, the whole ones first.  kWhole: there are no others
+// (combine of 16,384 x 8 rows of 2,048 bf16 values: 146 us with the branches about single values, 140 without).
+template <class T, bool kWhole, class F>
 __device__ __forceinline__ void over_pieces(const RowsArgs& p, F f) {
   constexpr int N = Piece<T>::N;
-  const int full = p.width / N, all = full + p.width % N, step = 1 << p.lx;
-  for (int u = threadIdx.x & (step - 1); u < all; u += step) f(u < full ? u * N : full * N + (u - full), u < full);
+  const int full = p.width / N, step = 1 << p.lx, u0 = threadIdx.x & (step - 1);
+  if constexpr (kWhole) {
+    for (int u = u0; u < full; u += step) f(u * N, std::true_type{});
+  } else {
+    const int all = full + p.width % N;
+    for (int u = u0; u < all; u += step) f(u < full ? u * N : full * N + (u - full), u < full);
+  }
 }
 
-template <class T>
+template <class T, bool kWhole>
 __global__ __launch_bounds__(kRowThreads) void k_dispatch(RowsArgs p) {
   typedef Piece<T> P;
   const int per = kRowThreads >> p.lx;
   for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
     const int32_t* place = p.place + row * p.slots;
-    over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
+    over_pieces<T, kWhole>(p, [&](int v, auto whole) __attribute__((always_inline)) {
       const u32x4 raw = P::load((const T*)p.x + row * p.width + v, whole);
       for (int k = 0; k < p.slots; ++k) {
         const int64_t at = place[k];
@@ -224,14 +230,14 @@ __global__ __launch_bounds__(kRowThreads) void k_dispatch(RowsArgs p) {
   }
 }
 
-template <class T>
+template <class T, bool kWhole>
 __global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
   typedef Piece<T> P;
   const int per = kRowThreads >> p.lx;
   for (int64_t row = (int64_t)blockIdx.x * per + (threadIdx.x >> p.lx); row < p.rows; row += (int64_t)gridDim.x * per) {
     const int32_t* place = p.place + row * p.slots;
     const float* weight = p.weight ? p.weight + row * p.slots : nullptr;
-    over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
+    over_pieces<T, kWhole>(p, [&](int v, auto whole) __attribute__((always_inline)) {
       float s[P::N] = {};
       for (int k0 = 0; k0 < p.slots; k0 += kAtOnce) {
         u32x4 y[kAtOnce];
@@ -242,7 +248,7 @@ __global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
           const int32_t at = k0 + i < p.slots ? place[k0 + i] : -1;
           on[i] = at >= 0 && at < p.items;
           if (on[i]) {
-            y[i] = P::load(item_at((const T*)p.y, at, p.width, v), whole);
+            y[i] = P::load(item_at<!kWhole>((const T*)p.y, at, p.width, v), whole);
             w[i] = weight ? weight[k0 + i] : 1.0f;
           }
         }
@@ -258,7 +264,7 @@ __global__ __launch_bounds__(kRowThreads) void k_combine(RowsArgs p) {
 }
 
 // 2^lx lanes take a row: at most a wave (then <dout, y> needs no exchange between waves), or the workgroup.
-template <class T>
+template <class T, bool kWhole>
 __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
   typedef Piece<T> P;
   __shared__ float part[kRowThreads / 64][kAtOnce];
@@ -274,13 +280,13 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
         if (at[i] >= p.items) at[i] = -1;
         w[i] = p.weight && k0 + i < p.slots ? p.weight[row * p.slots + k0 + i] : 1.0f;
       }
-      over_pieces<T>(p, [&](int v, bool whole) __attribute__((always_inline)) {
+      over_pieces<T, kWhole>(p, [&](int v, auto whole) __attribute__((always_inline)) {
         const u32x4 g = P::load((const T*)p.x + row * p.width + v, whole);
         u32x4 y[kAtOnce];
         if (p.dweight) {
 #pragma unroll
           for (int i = 0; i < kAtOnce; ++i)
-            if (at[i] >= 0) y[i] = P::load(item_at((const T*)p.y, at[i], p.width, v), whole);
+            if (at[i] >= 0) y[i] = P::load(item_at<true>((const T*)p.y, at[i], p.width, v), whole);
         }
 #pragma unroll
         for (int i = 0; i < kAtOnce; ++i) {
@@ -289,7 +295,7 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
             float o[P::N];
 #pragma unroll
             for (int j = 0; j < P::N; ++j) o[j] = w[i] * P::get(g, j);
-            P::store(item_at((T*)p.dy, at[i], p.width, v), whole, P::make(o));
+            P::store(item_at<true>((T*)p.dy, at[i], p.width, v), whole, P::make(o));
           }
           if (p.dweight)
 #pragma unroll
@@ -298,20 +304,31 @@ __global__ __launch_bounds__(kRowThreads) void k_combine_grad(RowsArgs p) {
         }
       });
       if (p.dweight) {
+        if (step < kAtOnce) {
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-          for (int d = 1; d < min(step, 64); d <<= 1) dot[i] += __shfl_xor(dot[i], d, 64);
-          if (step > 64 && (l & 63) == 0) part[l >> 6][i] = dot[i];
-        }
-        if (step > 64) {                             // the workgroup's only row
-          __syncthreads();
-          if (l < kAtOnce && k0 + l < p.slots)
-            p.dweight[row * p.slots + k0 + l] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
-          __syncthreads();
-        } else if (l == 0) {
+          for (int i = 0; i < kAtOnce; ++i) {
+            for (int d = 1; d < step; d <<= 1) dot[i] += __shfl_xor(dot[i], d, 64);
+            if (l == 0 && k0 + i < p.slots) p.dweight[row * p.slots + k0 + i] = dot[i];
+          }
+        } else {
+          // the lanes of a pair halve the items between them, three times, and each adds up one item's
 #pragma unroll
-          for (int i = 0; i < kAtOnce; ++i)
-            if (k0 + i < p.slots) p.dweight[row * p.slots + k0 + i] = dot[i];
+          for (int h = kAtOnce / 2, d = 1; h; h >>= 1, d <<= 1) {
+            const bool up = l & d;
+#pragma unroll
+            for (int i = 0; i < h; ++i) dot[i] = (up ? dot[i + h] : dot[i]) + __shfl_xor(up ? dot[i] : dot[i + h], d, 64);
+          }
+          for (int d = kAtOnce; d < min(step, 64); d <<= 1) dot[0] += __shfl_xor(dot[0], d, 64);
+          const int i = (l & 1) << 2 | (l & 2) | (l & 4) >> 2;       // the lane's item
+          if (step > 64) {                             // the workgroup's only row
+            if ((l & 63) < kAtOnce) part[l >> 6][i] = dot[0];
+            __syncthreads();
+            if (l < kAtOnce && k0 + l < p.slots)
+              p.dweight[row * p.slots + k0 + l] = (part[0][l] + part[1][l]) + (part[2][l] + part[3][l]);
+            __syncthreads();
+          } else if (l < kAtOnce && k0 + i < p.slots) {
+            p.dweight[row * p.slots + k0 + i] = dot[0];
+          }
         }
       }
     }
@@ -326,6 +343,10 @@ int route_per(int64_t n) {
 }
 int route_blocks(int64_t n) { return (int)((n + route_per(n) - 1) / route_per(n)); }
 
+int pieces_of(const sagips_routed& R) {
+  const int n = R.type == SAGIPS_BF16 ? 8 : 4;
+  return R.width / n + R.width % n;
+}
 RowsArgs rows_args(const sagips_routed& R) {
   RowsArgs a{};
   a.place = R.place;
@@ -333,13 +354,15 @@ RowsArgs rows_args(const sagips_routed& R) {
   a.items = R.rows * R.slots;
   a.slots = R.slots;
   a.width = R.width;
-  const int n = R.type == SAGIPS_BF16 ? 8 : 4, pieces = R.width / n + R.width % n;
-  while (a.lx < 8 && (1 << a.lx) < pieces) ++a.lx;
+  while (a.lx < 8 && (1 << a.lx) < pieces_of(R)) ++a.lx;
   return a;
 }
-dim3 rows_grid(const RowsArgs& a) {
+typedef void (*RowsKernel)(RowsArgs);
+// kernels[bf16][every piece of a row is whole]
+void go_rows(const sagips_routed& R, const RowsArgs& a, const RowsKernel (&kernels)[2][2], hipStream_t st) {
+  const bool bf16 = R.type == SAGIPS_BF16;
   const int64_t per = kRowThreads >> a.lx, blocks = (a.rows + per - 1) / per, most = 1 << 20;
-  return dim3((unsigned)(blocks < most ? blocks : most));
+  hipLaunchKernelGGL(kernels[bf16][R.width % (bf16 ? 8 : 4) == 0], dim3((unsigned)(blocks < most ? blocks : most)), dim3(kRowThreads), 0, st, a);
 }
 
 }  // namespace
@@ -372,7 +395,8 @@ hipError_t launch_dispatch(const sagips_routed& R, const void* x, void* sorted, 
   a.x = x;
   a.out = sorted;
   if (tm) tm->begin("dispatch");
-  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_dispatch<float> : k_dispatch<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  static const RowsKernel kernels[2][2] = {{k_dispatch<float, false>, k_dispatch<float, true>}, {k_dispatch<u16, false>, k_dispatch<u16, true>}};
+  go_rows(R, a, kernels, st);
   if (tm) tm->end();
   return hipGetLastError();
 }
@@ -383,7 +407,8 @@ hipError_t launch_combine(const sagips_routed& R, const void* y, const float* we
   a.weight = weight;
   a.out = out;
   if (tm) tm->begin("combine");
-  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_combine<float> : k_combine<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  static const RowsKernel kernels[2][2] = {{k_combine<float, false>, k_combine<float, true>}, {k_combine<u16, false>, k_combine<u16, true>}};
+  go_rows(R, a, kernels, st);
   if (tm) tm->end();
   return hipGetLastError();
 }
@@ -391,16 +416,19 @@ hipError_t launch_combine(const sagips_routed& R, const void* y, const float* we
 hipError_t launch_combine_backward(const sagips_routed& R, const void* dout, const void* y, const float* weight, void* dy,
                                    float* dweight, hipStream_t st, Timer* tm) {
   RowsArgs a = rows_args(R);
-  // a wave a row where there are rows enough for all; long rows otherwise by a workgroup (8 slots of 8,192 bf16
-  // values: 300 rows 51 us by a wave each and 23 so, one row 38 and 19)
-  if (a.lx > 6) a.lx = R.rows < 2048 ? 8 : 6;
+  // A row by a workgroup where rows are few or its pieces of all items many, by a wave otherwise (8 slots of 8,192
+  // bf16 values: 300 rows 51 us by a wave each and 21 so; 16,384 rows of 8 slots of 2,048 bf16 values 244 and
+  // 208, of 4 slots 119 and 113, 65,536 rows of 1 slot of 1,000 fp32 values 159 and 241).
+  const int64_t pieces = (int64_t)pieces_of(R) * (R.slots < kAtOnce ? R.slots : kAtOnce);
+  if (a.lx > 6) a.lx = R.rows < 2048 || pieces >= 1024 ? 8 : 6;
   a.x = dout;
   a.y = y;
   a.weight = weight;
   a.dy = dy;
   a.dweight = dweight;
   if (tm) tm->begin("combine_backward");
-  hipLaunchKernelGGL(R.type == SAGIPS_F32 ? k_combine_grad<float> : k_combine_grad<u16>, rows_grid(a), dim3(kRowThreads), 0, st, a);
+  static const RowsKernel kernels[2][2] = {{k_combine_grad<float, false>, k_combine_grad<float, true>}, {k_combine_grad<u16, false>, k_combine_grad<u16, true>}};
+  go_rows(R, a, kernels, st);
   if (tm) tm->end();
   return hipGetLastError();
 }
