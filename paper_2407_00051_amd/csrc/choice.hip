@@ -248,20 +248,40 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
     if (l == 0) write_row<T>(p, row, a);
     if (p.top == 0) continue;
     const float ls = log2f(a.s);
-    float x[N];
+    // One alternative a round, which lane k % L keeps; L of them are written together.  A bf16 value's key and its
+    // index go in one word (an index is below 64 units' 512), fp32 values take a second exchange.
+    constexpr bool kWord = sizeof(T) == 2;
+    uint32_t key[N], kept = 0, kept_lo = 0;            // key 0: masked, outside the row, or taken
 #pragma unroll
-    for (int j = 0; j < N; ++j) x[j] = Unit<T>::get(r, j);
+    for (int j = 0; j < N; ++j) {
+      const float x = Unit<T>::get(r, j);
+      const uint32_t u = order_key(x);
+      key[j] = x == kLowest ? 0u : kWord ? (u & 0xffff0000u) | (0xffffu - (uint32_t)(i0 + j)) : u;
+    }
     for (int k = 0; k < p.top; ++k) {
-      float best = kLowest;
-      int at = 0;
+      uint32_t hi = 0;
 #pragma unroll
-      for (int j = N - 1; j >= 0; --j)
-        if (x[j] >= best) best = x[j], at = j;       // of equal ones the lowest
-      const uint64_t first = group_first<L>(candidate(best, i0 + at));
-      const int taken = candidate_index(first) - i0;
+      for (int j = 0; j < N; ++j) hi = max(hi, key[j]);
+      hi = group_max<L>(hi);
+      uint32_t lo = 0;
+      if constexpr (!kWord) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = j == taken ? kLowest : x[j];
-      if (l == k % L) write_top(p, row, k, first, a, ls);
+        for (int j = 0; j < N; ++j) lo = max(lo, key[j] == hi ? 0xffffffffu - (uint32_t)(i0 + j) : 0u);   // of equal ones the lowest
+        lo = group_max<L>(lo);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) key[j] = (kWord ? key[j] == hi : 0xffffffffu - (uint32_t)(i0 + j) == lo) ? 0u : key[j];
+      const int at = k % L;
+      if (l == at) kept = hi, kept_lo = lo;
+      if (at == L - 1 || k == p.top - 1) {
+        if (l <= at) {
+          if constexpr (kWord) {                       // the whole key again, whose lower bits are the value's zeros
+            kept_lo = 0xffff0000u | kept;
+            kept = kept & 0x80000000u ? kept & 0xffff0000u : kept ? kept | 0xffffu : 0u;
+          }
+          write_top(p, row, k - at + l, (uint64_t)kept << 32 | kept_lo, a, ls);
+        }
+      }
     }
   }
 }
@@ -559,18 +579,33 @@ __device__ __forceinline__ GradRow grad_row(const ChoiceGradArgs& p, int64_t row
   return g;
 }
 
+// Orders a wave's own accesses of shared memory.
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 template <class T>
 __device__ __forceinline__ T rounded(float v) {
   if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, v);
   else return (T)pk_bf16(v, 0.0f);
 }
-// L lanes take a chunk of a row: a whole row where L is at most 64 (several rows a
-// wave), or L = 256 threads.  R units a lane.  kUnits: 16-byte units, the rows of both arrays being
-// aligned alike; otherwise single values.
+// L lanes (at most a wave) take a chunk of a row, R units a lane; several rows a wave where they are short.  (Long
+// rows by 256 threads and a chunk of 1,024 units each: 65,536 rows of 1,100 fp32 logits with 8 alternatives 290 us,
+// 160 by a wave a chunk of 256; 4,096 of 50,001 bf16 ones the same 162.)  The choice and the alternatives are
+// added to the value they belong to by the lane that has it, which a table in shared memory tells (each lane
+// looking through all of them: 65,536 rows of 256 bf16 logits with 8 alternatives 46 us, 35 so, and 22 by the 32
+// lanes that they need instead of 64).
+// kUnits: 16-byte units, the rows of both arrays being aligned alike; otherwise single values.
 template <class T, int L, int R, bool kUnits>
 __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
   constexpr int N = kUnits ? Unit<T>::N : 1, P = 256 / L;
-  const int l = threadIdx.x % L, lane = threadIdx.x & 63;
+  struct Entry {
+    int c;
+    float g;
+  };
+  __shared__ unsigned long long owner[256];          // bit i: the thread has entry i
+  __shared__ Entry entry[P][SAGIPS_MAX_TOP + 1];
+  const int l = threadIdx.x % L;
   const int64_t all = p.rows * p.chunks;
   for (int64_t id = (int64_t)blockIdx.x * P + threadIdx.x / L; id < all; id += (int64_t)gridDim.x * P) {
     const int64_t row = id / p.chunks;
@@ -592,15 +627,19 @@ __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
     }
     int ec = -1;
     float eg = 0.0f, total = 0.0f;
-    if constexpr (L >= 64) {                           // an entry a lane
-      if (lane <= p.top) grad_entry(p, row, lane, ec, eg);
-      total = group_sum<64>(eg);
-    } else {
-      for (int i = 0; i <= p.top; ++i) {
-        grad_entry(p, row, i, ec, eg);
-        total += eg;
+    owner[threadIdx.x] = 0;
+    wave_sync();
+    for (int i = l; i <= p.top; i += L) {
+      grad_entry(p, row, i, ec, eg);
+      total += eg;
+      const int q = ec < 0 ? -1 : (ec + lead) / N - q0;
+      if (q >= 0 && q < L * R) {
+        entry[threadIdx.x / L][i] = Entry{ec, eg};
+        atomicOr(&owner[threadIdx.x - l + q % L], 1ull << i);
       }
     }
+    total = group_sum<L>(total);
+    wave_sync();
     const GradRow g = grad_row(p, row, total);
 #pragma unroll
     for (int i = 0; i < R; ++i)
@@ -610,29 +649,16 @@ __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
         else if constexpr (sizeof(T) == 4) val[i][j] = g.at(__uint_as_float(raw[i].x));
         else val[i][j] = g.at(__uint_as_float(raw[i].x << 16));
       }
-    const auto add = [&](int c, float e) __attribute__((always_inline)) {
+    for (unsigned long long mine = owner[threadIdx.x]; mine; mine &= mine - 1) {
+      const Entry e = entry[threadIdx.x / L][__ffsll(mine) - 1];
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const int j0 = c - ((q0 + i * L + l) * N - lead);
+        const int j0 = e.c - ((q0 + i * L + l) * N - lead);
 #pragma unroll
-        for (int j = 0; j < N; ++j) val[i][j] += j0 == j ? e : 0.0f;
-      }
-    };
-    if constexpr (L >= 64) {
-      // those in reach of the wave's units
-      const int from = (q0 + (int)(threadIdx.x % L) - lane) * N - lead, to = (q0 + (R - 1) * L + (int)(threadIdx.x % L) - lane + 64) * N - lead;
-      uint64_t on = __ballot(ec >= 0 && ec >= from && ec < to);
-      while (on) {
-        const int i = __ffsll((unsigned long long)on) - 1;
-        on &= on - 1;
-        add(__builtin_amdgcn_readlane(ec, i), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(eg), i)));
-      }
-    } else {
-      for (int i = 0; i <= p.top; ++i) {
-        grad_entry(p, row, i, ec, eg);
-        if (ec >= 0) add(ec, eg);
+        for (int j = 0; j < N; ++j) val[i][j] += j0 == j ? e.g : 0.0f;
       }
     }
+    wave_sync();                                       // the next row's
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int q = q0 + i * L + l;
@@ -705,6 +731,11 @@ hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(k_choice_join<T>, dim3((unsigned)a.rows), dim3(64), 0, st, a);
     }
+  } else if (units <= 64 && units > 32 && a.top >= 4) {
+    // a round an alternative costs more than the bound from 4 on (65,536 rows of 256 fp32 logits: 4 alternatives
+    // 37 us in rounds and 30 so, 8 57 and 33, 32 177 and 51; 3 33 and 30, but of 264 bf16 ones 39 and 37,
+    // 300 38 and 40)
+    go_row(Int<64>{}, Int<1>{}, one);
   } else if (units <= 1) go_short(Int<1>{});
   else if (units <= 2) go_short(Int<2>{});
   else if (units <= 4) go_short(Int<4>{});
@@ -734,10 +765,12 @@ hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
     hipLaunchKernelGGL((k_choice_grad<T, L, R, kUnits>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
   };
   if (units <= 4) go(Int<4>{}, Int<1>{});
+  else if (units <= 8) go(Int<8>{}, Int<1>{});
   else if (units <= 16) go(Int<16>{}, Int<1>{});
+  else if (units <= 32) go(Int<32>{}, Int<1>{});
   else if (units <= 64) go(Int<64>{}, Int<1>{});
-  else if (units <= 64 * 4) go(Int<64>{}, Int<4>{});
-  else go(Int<256>{}, Int<4>{});
+  else if (units <= 64 * 2) go(Int<64>{}, Int<2>{});
+  else go(Int<64>{}, Int<4>{});
   return hipGetLastError();
 }
 
