@@ -384,18 +384,18 @@ __global__ __launch_bounds__(64) void k_choice_join(ChoiceArgs p) {
 
 // kParts: a workgroup takes a part of a row.
 template <class T, int TH, int R, bool kOnePass, bool kParts>
-__global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p) {
+__global__ __launch_bounds__(TH, R <= 8 && !(kParts && TH == 256) ? 8 : 4) void k_choice_row(ChoiceArgs p) {
   constexpr int N = Unit<T>::N, W = TH / 64, G = TH / 64, kHeld = TH == 64 ? 256 : 1024;
   __shared__ Sums part[W];
   __shared__ float group[64];                        // the largest logit of every G threads
   __shared__ uint64_t cand[kHeld], firsts[W];
   __shared__ uint32_t held;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   constexpr uint32_t none = sizeof(T) == 4 ? kFill<T> : kFill<T> << 16 | kFill<T>;
   const u32x4 fill = {none, none, none, none};
   for (int64_t id = blockIdx.x; id < (kParts ? p.rows * p.parts : p.rows); id += gridDim.x) {
-    const int64_t row = kParts ? id / p.parts : id;
-    const int part_of = kParts ? (int)(id % p.parts) : 0;
+    const int64_t row = kParts ? (uint32_t)id / (uint32_t)p.parts : id;
+    const int part_of = kParts ? (int)((uint32_t)id % (uint32_t)p.parts) : 0;
     const RowView<T> v(p.x, row * p.stride, p.n);
     const int begin = kParts ? part_of * p.per : 0, units = kParts ? min(v.units(), begin + p.per) : v.units();
     u32x4 r[R];
@@ -461,6 +461,7 @@ __global__ __launch_bounds__(TH, R <= 8 ? 8 : 4) void k_choice_row(ChoiceArgs p)
       const auto collect = [&](int q0) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
+          if (!(unit_max<T>(r[i], kLowest) >= bound)) continue;
           uint32_t on = 0;
 #pragma unroll
           for (int j = 0; j < N; ++j) on |= Unit<T>::get(r[i], j) >= bound ? 1u << j : 0u;
