@@ -16,6 +16,7 @@ keeps it from settling before its members differ.
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from typing import Sequence
 
 from . import Context
@@ -45,33 +46,45 @@ class Mixture:
     def gradients(self):
         return [t for pair in zip(self.dW, self.db) for t in pair] + [self.dWr, self.dbr]
 
+    def on_stream(self):
+        """The context's stream as torch's current one: what torch computes here stands between the library's calls."""
+        import torch
+        return nullcontext() if self.ctx._follow else torch.cuda.stream(self.ctx.stream)
+
     def forward(self, noise):
         """theta [k][out]; what backward needs is kept until the next call.  A row whose logits hold a NaN or +inf
         has no members: its theta is NaN, not the 0 of an empty sum."""
         import torch
         c = self.ctx
-        logits = torch.addmm(self.br, noise, self.Wr.t())
-        chosen = c.choice_logprob(logits, top=self.top)
-        own = c.choice_logprob(chosen["top_logp"], top=self.top)       # already in falling order: choice i is the i-th
-        weight = own["top_logp"].exp()
-        plan = c.route(chosen["top_choice"], self.M)
-        x = c.dispatch(noise, plan)
-        theta = c.gen_forward_routed(self.W, self.b, x, plan["offsets"], slope=self.slope)
-        self._held = (noise, logits, chosen, own, weight, plan, x, theta)
-        nan = chosen["entropy"][:, None]                               # finite otherwise
-        return c.combine(theta, plan, weight).addcmul_(nan, nan, value=0.0)
+        c._owned(noise)
+        with self.on_stream():
+            logits = torch.addmm(self.br, noise, self.Wr.t())
+            chosen = c.choice_logprob(logits, top=self.top)
+            own = c.choice_logprob(chosen["top_logp"], top=self.top)   # already in falling order: choice i is the i-th
+            weight = own["top_logp"].exp()
+            plan = c.route(chosen["top_choice"], self.M)
+            x = c.dispatch(noise, plan)
+            theta = c.gen_forward_routed(self.W, self.b, x, plan["offsets"], slope=self.slope)
+            self._held = (noise, logits, chosen, own, weight, plan, x, theta)
+            nan = chosen["entropy"][:, None]                           # finite otherwise
+            out = c.combine(theta, plan, weight).addcmul_(nan, nan, value=0.0)
+        if not c._follow:
+            out.record_stream(torch.cuda.current_stream(c.device))     # the caller's, who may drop it at any time
+        return out
 
     def backward(self, dL_dtheta) -> None:
         """The gradients of the last forward call's parameters from dL/dtheta [k][out]."""
         import torch
         c = self.ctx
         noise, logits, chosen, own, weight, plan, x, theta = self._held
-        d_member, d_weight = c.combine_backward(dL_dtheta, theta, plan, weight)
-        c.gen_backward_routed(self.W, self.b, x, plan["offsets"], d_member, slope=self.slope, dW=self.dW, db=self.db)
-        d_top = c.choice_backward(chosen["top_logp"], own, d_top=d_weight * weight)
-        d_entropy = torch.full_like(chosen["entropy"], -self.entropy_coef / noise.shape[0]) if self.entropy_coef else None
-        d_logits = c.choice_backward(logits, chosen, d_top=d_top, d_entropy=d_entropy)
-        # (one product for both: a library's sum over many rows may clear memory first, which graphs replay wrongly)
-        d = torch.mm(d_logits.t(), torch.cat([noise, torch.ones_like(noise[:, :1])], 1))
-        self.dWr.copy_(d[:, :-1])
-        self.dbr.copy_(d[:, -1])
+        c._owned(dL_dtheta)
+        with self.on_stream():
+            d_member, d_weight = c.combine_backward(dL_dtheta, theta, plan, weight)
+            c.gen_backward_routed(self.W, self.b, x, plan["offsets"], d_member, slope=self.slope, dW=self.dW, db=self.db)
+            d_top = c.choice_backward(chosen["top_logp"], own, d_top=d_weight * weight)
+            d_entropy = torch.full_like(chosen["entropy"], -self.entropy_coef / noise.shape[0]) if self.entropy_coef else None
+            d_logits = c.choice_backward(logits, chosen, d_top=d_top, d_entropy=d_entropy)
+            # (one product for both: a library's sum over many rows may clear memory first, which graphs replay wrongly)
+            d = torch.mm(d_logits.t(), torch.cat([noise, torch.ones_like(noise[:, :1])], 1))
+            self.dWr.copy_(d[:, :-1])
+            self.dbr.copy_(d[:, -1])

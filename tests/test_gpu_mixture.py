@@ -184,6 +184,37 @@ def test_contexts_on_streams_of_their_own():
         c.close()
 
 
+def test_mixture_on_a_stream_that_is_not_the_current_one(gpu_ctx):
+    """A context on a stream of its own with work queued on it: torch's part of a step runs there too, between
+    the library's calls that it depends on, and inputs and results may be dropped at once."""
+    print("case mixture on its own stream", flush=True)
+    busy = torch.randn((2048, 65536), device="cuda:0")
+    results = []
+    for own in (False, True):
+        _, (W, b, Wr, br, n) = _setup(4, 3000, 30)
+        g = torch.ones((3000, 6), device="cuda:0")
+        ctx = sg.Context(0, stream=torch.cuda.Stream()) if own else sg.Context(0)
+        mix = Mixture(ctx, W, b, Wr, br, entropy_coef=0.1)
+        m, v = ([torch.zeros_like(p) for p in mix.parameters()] for _ in range(2))
+        torch.cuda.synchronize()
+        thetas = []
+        for t in range(3):
+            ctx.choice_logprob(busy)
+            theta = mix.forward(n)
+            mix.backward(g)
+            ctx.adam_step(mix.parameters(), mix.gradients(), m, v, t + 1, 1e-3)
+            with mix.on_stream():
+                thetas.append(theta.clone())
+            del theta
+        torch.cuda.synchronize()
+        results.append(thetas + mix.parameters())
+        ctx.close()
+    # Adam's first steps are lr g / |g|: a gradient's rounding (the library's product may sum in another order) shows
+    # only where it is near eps = 1e-8 of the step
+    assert all(torch.allclose(a, c, rtol=1e-4, atol=1e-4) for a, c in zip(*results))
+    assert not torch.equal(results[0][0], results[0][1])
+
+
 def test_a_router_that_leaves_a_row_without_members(gpu_ctx):
     """Members masked by -inf take no rows; a row whose members are all masked gives theta 0 and no gradient."""
     x = torch.zeros((3, 4), device="cuda:0")
