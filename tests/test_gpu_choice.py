@@ -221,6 +221,27 @@ def test_parts_in_a_graph(gpu_ctx):
         ctx.close()
 
 
+@pytest.mark.parametrize("n,V,dtype,top,opad", [(40003, 525, "bf16", 4, 0), (40003, 200, "f32", 5, 0), (5000, 2300, "f32", 7, 1),
+                                                (4300000, 300, "bf16", 2, 1)])
+def test_more_rows_than_a_launch_has_groups(gpu_ctx, n, V, dtype, top, opad):
+    """Workgroups that take several rows, forward, and several chunks of rows in the gradient (the last case)."""
+    if n > 10 ** 6 and torch.cuda.get_device_properties(0).total_memory < 64 << 30:
+        pytest.skip("needs 64 GB")
+    print(f"case {n} x {V} {dtype}", flush=True)
+    x = _logits(n, V, dtype, n, 0.1)
+    c = torch.randint(0, V, (n,), device="cuda:0", dtype=torch.int32)
+    gl, gH, gt = torch.ones(n, device="cuda:0"), torch.full((n,), 0.3, device="cuda:0"), torch.ones((n, top), device="cuda:0")
+    f = gpu_ctx.choice_logprob(x, c, top=top)
+    out = torch.empty((n, V + opad), dtype=x.dtype, device="cuda:0")[:, :V]
+    d = gpu_ctx.choice_backward(x, f, c, gl, gH, gt, out=out)
+    torch.cuda.synchronize()
+    some = np.unique(np.concatenate([np.arange(40), np.random.default_rng(1).choice(n, 60), np.arange(n - 40, n)]))
+    part = {k: v[torch.tensor(some, device="cuda:0")] for k, v in f.items()}
+    choice = c.cpu().numpy()[some]
+    _check_forward(part, x[some], choice, top, 1.0, f"{n} x {V}")
+    _check_grad(d[some], x[some], choice, gl[some], gH[some], gt[some], 1.0, f"{n} x {V}")
+
+
 def test_gradient_in_place_strided_and_of_other_alignment(gpu_ctx):
     for dtype in ("f32", "bf16"):
         for V, pad, opad in ((37, 3, 0), (37, 0, 5), (1500, 4, 4), (5000, 1, 2), (40, 24, 8)):

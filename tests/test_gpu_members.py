@@ -104,6 +104,33 @@ def test_offsets_outside_the_rows_are_taken_as_the_nearer_end(gpu_ctx, n):
     assert torch.equal(a, c) and torch.equal(p[2], q[2]) and all(torch.equal(s, t) for s, t in zip(p[0] + p[1], q[0] + q[1]))
 
 
+def test_offsets_pass_32_bits(gpu_ctx):
+    """370,000,000 rows of 6 (8.9 GB an array): the last member's 1,000 agree with a call of their own."""
+    if torch.cuda.get_device_properties(0).total_memory < 96 << 30:
+        pytest.skip("needs 96 GB")
+    print("case rows 370000000", flush=True)
+    n, last = 370_000_000, 1000
+    W, b = gen.generator_stack((6, 128, 128, 6), 2, seed=3)
+    x, g = torch.zeros((n, 6), device="cuda:0"), torch.zeros((n, 6), device="cuda:0")
+    noise = gen.noise(last, 6, seed=4)
+    dth = np.random.default_rng(5).standard_normal((last, 6)).astype(np.float32)
+    dth[_kinks(W, b, noise, [0, 0, last])] = 0.0
+    x[-last:], g[-last:] = torch.tensor(noise, device="cuda:0"), torch.tensor(dth, device="cuda:0")
+    W, b = _dev(W), _dev(b)
+    off = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda:0")     # noqa: E731
+    theta = gpu_ctx.gen_forward_routed(W, b, x, off(0, n - last, n))
+    own = gpu_ctx.gen_forward_routed(W, b, x[-last:].clone(), off(0, 0, last))
+    dW, db, dx = gpu_ctx.gen_backward_routed(W, b, x, off(0, n - last, n), g, want_dx=True)
+    ownW, ownb, owndx = gpu_ctx.gen_backward_routed(W, b, x[-last:].clone(), off(0, 0, last), g[-last:].clone(), want_dx=True)
+    torch.cuda.synchronize()
+    # either form of the tiles is within the library's normwise bar of the exact result
+    near = lambda a, c: ((a - c).abs() <= 2 * TOL * c.abs().max()).all()     # noqa: E731
+    assert near(theta[-last:], own) and near(dx[-last:], owndx)
+    assert all(near(a[1], c[1]) for a, c in zip(dW + db, ownW + ownb))
+    assert all((a[0] == 0).all() for a in dW + db)                           # no gradient, and none of a neighbour's
+    assert torch.equal(theta[:64], theta[n - last - 64:n - last])            # equal inputs
+
+
 def test_agrees_with_the_whole_stack(gpu_ctx):
     """Every member on the same rows, by gen_forward / gen_backward, and on copies of its own."""
     M, k = 4, 1100

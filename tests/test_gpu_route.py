@@ -117,6 +117,26 @@ def test_gradient_of_rows_by_a_wave_and_by_a_workgroup(gpu_ctx, rows, slots, wid
                for a, b in zip((dy, dw), gpu_ctx.combine_backward(dout, y, p, w)))
 
 
+def test_offsets_pass_32_bits(gpu_ctx):
+    """1,100,000 rows of 2,048 bf16 values (4.5 GB): out and back again, and the gradient."""
+    if torch.cuda.get_device_properties(0).total_memory < 64 << 30:
+        pytest.skip("needs 64 GB")
+    print("case rows 1100000 x 2048", flush=True)
+    rows, width = 1_100_000, 2048
+    p = gpu_ctx.route(_member(rows, 1, 5, 1, low=0), 5)
+    x = torch.empty((rows, width), dtype=torch.bfloat16, device="cuda:0")
+    x.view(torch.int16)[:] = torch.arange(rows, device="cuda:0", dtype=torch.int32)[:, None].remainder(16000).to(torch.int16)
+    x.view(torch.int16)[:, 7] = torch.arange(rows, device="cuda:0", dtype=torch.int32).floor_divide(16000).to(torch.int16)
+    s = gpu_ctx.dispatch(x, p)
+    assert torch.equal(s[-1000:], x[p["order"][-1000:].long()])
+    assert torch.equal(gpu_ctx.combine(s, p), x)
+    dy, dw = gpu_ctx.combine_backward(x, s, p)
+    torch.cuda.synchronize()
+    assert torch.equal(dy, s)
+    ref = (x[-1000:].double() ** 2).sum(1)
+    assert ((dw[-1000:, 0].double() - ref).abs() <= U * (width / 64 + 14) * ref).all()
+
+
 def test_places_outside_the_rows_are_none(gpu_ctx):
     """A plan of the caller's own: positions outside [0, rows * slots) are followed nowhere."""
     place = torch.tensor([[0, 6], [-7, 2 ** 31 - 1], [3, -2 ** 31]], dtype=torch.int32, device="cuda:0")
