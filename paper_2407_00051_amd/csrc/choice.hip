@@ -71,9 +71,11 @@ struct RowView {
   const char* base;
   int lead, n;
   __device__ __forceinline__ RowView(const void* x, int64_t off, int n_) : n(n_) {
-    const uintptr_t at = (uintptr_t)((const T*)x + off);
-    base = (const char*)(at & ~(uintptr_t)15);
-    lead = (int)((at & 15) / sizeof(T));
+    // (by pointer arithmetic: from an integer the reads would be flat ones)
+    const char* at = (const char*)((const T*)x + off);
+    const int over = (int)((uintptr_t)at & 15);
+    base = at - over;
+    lead = over / (int)sizeof(T);
   }
   __device__ __forceinline__ int units() const { return (int)(((int64_t)n + lead + N - 1) / N); }
   __device__ __forceinline__ int first(int q) const { return q * N - lead; }
