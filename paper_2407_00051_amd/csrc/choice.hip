@@ -596,8 +596,9 @@ __device__ __forceinline__ T rounded(float v) {
 // rows by 256 threads and a chunk of 1,024 units each: 65,536 rows of 1,100 fp32 logits with 8 alternatives 290 us,
 // 160 by a wave a chunk of 256; 4,096 of 50,001 bf16 ones the same 162.)  The choice and the alternatives are
 // added to the value they belong to by the lane that has it, which a table in shared memory tells (each lane
-// looking through all of them: 65,536 rows of 256 bf16 logits with 8 alternatives 46 us, 35 so, and 22 by the 32
-// lanes that they need instead of 64).
+// looking through all of them: 65,536 rows of 256 bf16 logits with 8 alternatives 46 us, 35 so, and 22 by as many
+// lanes as they need).  Two units a lane from 8 on, since what is done once a row weighs (500 bf16 logits 44 us
+// with one, 39 with two).
 // kUnits: 16-byte units, the rows of both arrays being aligned alike; otherwise single values.
 template <class T, int L, int R, bool kUnits>
 __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
@@ -772,11 +773,12 @@ hipError_t choice_grad(ChoiceGradArgs a, hipStream_t st) {
     hipLaunchKernelGGL((k_choice_grad<T, L, R, kUnits>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
   };
   if (units <= 4) go(Int<4>{}, Int<1>{});
-  else if (units <= 8) go(Int<8>{}, Int<1>{});
-  else if (units <= 16) go(Int<16>{}, Int<1>{});
-  else if (units <= 32) go(Int<32>{}, Int<1>{});
-  else if (units <= 64) go(Int<64>{}, Int<1>{});
-  else if (units <= 64 * 2) go(Int<64>{}, Int<2>{});
+  else if (units <= 8) go(Int<4>{}, Int<2>{});
+  else if (units <= 16) go(Int<8>{}, Int<2>{});
+  else if (units <= 32) go(Int<16>{}, Int<2>{});
+  else if (units <= 64) go(Int<32>{}, Int<2>{});
+  else if (units <= 64 * 2) go(Int<32>{}, Int<4>{});
+  else if (units <= 64 * 3) go(Int<64>{}, Int<3>{});
   else go(Int<64>{}, Int<4>{});
   return hipGetLastError();
 }
