@@ -5,9 +5,9 @@
 //   dL/dz_v = sum_i g_i ([v = c_i] - p_v) - g_H p_v (ln p_v + H).
 //
 // Forward: one pass over the logits, which stay in registers; a row is taken by
-// 2^k lanes, a wave, 256 or 1,024 threads, whatever holds it.  Every thread keeps
+// 2^k lanes, a wave, 256 or 1,024 threads, whatever holds it, or few long rows in parts.  Every thread keeps
 // the maximum of its own values and sums relative to that; the waves' sums are
-// joined once.  The alternatives: the K-th largest of 64 groups' maxima is a lower
+// joined once.  The alternatives of a short row are taken one a round; of others the K-th largest of 64 groups' maxima is a lower
 // bound for the K-th largest value, and hardly more than K values reach it (64 ln 2 =
 // 44 on average at K = 32, 9 at K = 8); they are collected in LDS and ranked by counting.
 // Longer rows are read a second time for the collecting.
@@ -231,48 +231,55 @@ __device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int 
 // next they would need twice the registers, and half the waves would be resident.
 __device__ __forceinline__ void forget(u32x4& r) { asm volatile("" : "+v"(r)); }
 
-// ---- short rows: L lanes each, one unit a lane ----------------------------------
-template <class T, int L>
+// ---- short rows: L lanes each, R units a lane -----------------------------------
+// Several units a lane, since what is done once a row weighs (65,536 rows of 500 bf16 logits with one alternative: 32 us
+// by 64 lanes, 27 by 32 and 23 by 16; of 256 with 8 26, 22 and 21).
+template <class T, int L, int R>
 __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
   constexpr int N = Unit<T>::N;
   const int l = threadIdx.x % L;
   // whole groups leave: no exchange crosses them
   for (int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L; row < p.rows; row += (int64_t)gridDim.x * (256 / L)) {
     const RowView<T> v(p.x, row * p.stride, p.n);
-    const u32x4 r = v.load(l);
     const int i0 = v.first(l);
-    Sums a;
-    a.m = group_max<L>(unit_max<T>(r, kLowest));
-    float s = 0.0f, t = 0.0f;
-    add_unit<T>(r, finite_or_0(a.m), p.scale2, s, t);
-    a.s = group_sum<L>(s);
-    a.t = group_sum<L>(t);
+    u32x4 r[R];
+    float best = kLowest;
+#pragma unroll
+    for (int i = 0; i < R; ++i) r[i] = v.load(i * L + l);
+#pragma unroll
+    for (int i = 0; i < R; ++i) best = unit_max<T>(r[i], best);
+    Sums a{group_max<L>(best), 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < R; ++i) add_unit<T>(r[i], finite_or_0(a.m), p.scale2, a.s, a.t);
+    a.s = group_sum<L>(a.s);
+    a.t = group_sum<L>(a.t);
     if (l == 0) write_row<T>(p, row, a);
     if (p.top == 0) continue;
     const float ls = log2f(a.s);
     // One alternative a round, which lane k % L keeps; L of them are written together.  A bf16 value's key and its
     // index go in one word (an index is below 64 units' 512), fp32 values take a second exchange.
     constexpr bool kWord = sizeof(T) == 2;
-    uint32_t key[N], kept = 0, kept_lo = 0;            // key 0: masked, outside the row, or taken
+    uint32_t key[R * N], kept = 0, kept_lo = 0;        // key 0: masked, outside the row, or taken
+    const auto index = [&](int e) __attribute__((always_inline)) { return i0 + e / N * (L * N) + e % N; };
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float x = Unit<T>::get(r, j);
+    for (int e = 0; e < R * N; ++e) {
+      const float x = Unit<T>::get(r[e / N], e % N);
       const uint32_t u = order_key(x);
-      key[j] = x == kLowest ? 0u : kWord ? (u & 0xffff0000u) | (0xffffu - (uint32_t)(i0 + j)) : u;
+      key[e] = x == kLowest ? 0u : kWord ? (u & 0xffff0000u) | (0xffffu - (uint32_t)index(e)) : u;
     }
     for (int k = 0; k < p.top; ++k) {
       uint32_t hi = 0;
 #pragma unroll
-      for (int j = 0; j < N; ++j) hi = max(hi, key[j]);
+      for (int e = 0; e < R * N; ++e) hi = max(hi, key[e]);
       hi = group_max<L>(hi);
       uint32_t lo = 0;
       if constexpr (!kWord) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) lo = max(lo, key[j] == hi ? 0xffffffffu - (uint32_t)(i0 + j) : 0u);   // of equal ones the lowest
+        for (int e = 0; e < R * N; ++e) lo = max(lo, key[e] == hi ? 0xffffffffu - (uint32_t)index(e) : 0u);   // of equal ones the lowest
         lo = group_max<L>(lo);
       }
 #pragma unroll
-      for (int j = 0; j < N; ++j) key[j] = (kWord ? key[j] == hi : 0xffffffffu - (uint32_t)(i0 + j) == lo) ? 0u : key[j];
+      for (int e = 0; e < R * N; ++e) key[e] = (kWord ? key[e] == hi : 0xffffffffu - (uint32_t)index(e) == lo) ? 0u : key[e];
       const int at = k % L;
       if (l == at) kept = hi, kept_lo = lo;
       if (at == L - 1 || k == p.top - 1) {
@@ -712,10 +719,10 @@ int64_t choice_units(const sagips_choices& C) {
 
 template <class T>
 hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
-  const auto go_short = [&](auto lanes) {
-    constexpr int L = decltype(lanes)::value;
+  const auto go_short = [&](auto lanes, auto per) {
+    constexpr int L = decltype(lanes)::value, R = decltype(per)::value;
     const int64_t blocks = (a.rows + 256 / L - 1) / (256 / L), most = 1 << 20;
-    hipLaunchKernelGGL((k_choice_short<T, L>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_choice_short<T, L, R>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, st, a);
   };
   const auto go_row = [&](auto threads, auto per, auto one) {
     constexpr int TH = decltype(threads)::value, R = decltype(per)::value;
@@ -724,6 +731,11 @@ hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
     hipLaunchKernelGGL((k_choice_row<T, TH, R, kOne, false>), dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(TH), 0, st, a);
   };
   const std::true_type one{};
+  // Alternatives up to which rounds cost less than the bound (65,536 rows; us in rounds and by the bound): of 256 fp32
+  // logits 8 alternatives 35 and 33, 16 58 and 39; of 500 bf16 ones 12 47 and 47, 16 56 and 50; of 350 fp32 ones 2
+  // 33 and 37, 4 44 and 39; of 1,000 bf16 ones 2 40 and 44, 4 49 and 46.  Rows of up to 32 units have too few
+  // groups for a bound of many alternatives (128 fp32 logits: 8 of them 19 and 34, 32 80 and 115).
+  const int rounds = units <= 32 ? SAGIPS_MAX_TOP : units <= 64 ? (sizeof(T) == 2 ? 12 : 8) : units <= 128 ? 2 : -1;
   if (a.parts > 1) {
     a.per = (int)((units + a.parts - 1) / a.parts);
     const dim3 grid((unsigned)(a.rows * a.parts));
@@ -735,20 +747,18 @@ hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
       if (e != hipSuccess) return e;
       hipLaunchKernelGGL(k_choice_join<T>, dim3((unsigned)a.rows), dim3(64), 0, st, a);
     }
-  } else if (units <= 64 && units > 32 && a.top >= 4) {
-    // a round an alternative costs more than the bound from 4 on (65,536 rows of 256 fp32 logits: 4 alternatives
-    // 37 us in rounds and 30 so, 8 57 and 33, 32 177 and 51; 3 33 and 30, but of 264 bf16 ones 39 and 37,
-    // 300 38 and 40)
-    go_row(Int<64>{}, Int<1>{}, one);
-  } else if (units <= 1) go_short(Int<1>{});
-  else if (units <= 2) go_short(Int<2>{});
-  else if (units <= 4) go_short(Int<4>{});
-  else if (units <= 8) go_short(Int<8>{});
-  else if (units <= 16) go_short(Int<16>{});
-  else if (units <= 32) go_short(Int<32>{});
-  else if (units <= 64) go_short(Int<64>{});
+  } else if (a.top <= rounds) {
+    if (units <= 1) go_short(Int<1>{}, Int<1>{});
+    else if (units <= 2) go_short(Int<2>{}, Int<1>{});
+    else if (units <= 4) go_short(Int<4>{}, Int<1>{});
+    else if (units <= 8) go_short(Int<4>{}, Int<2>{});
+    else if (units <= 16) go_short(Int<8>{}, Int<2>{});
+    else if (units <= 32) go_short(Int<8>{}, Int<4>{});
+    else if (units <= 64) go_short(Int<16>{}, Int<4>{});
+    else go_short(Int<32>{}, Int<4>{});
   // as many units a thread as are needed, in steps: what lies behind the row is summed too (45,000 bf16 logits with 8
   // units a thread 104 us, with 6 90)
+  } else if (units <= 64) go_row(Int<64>{}, Int<1>{}, one);
   else if (units <= 64 * 2) go_row(Int<64>{}, Int<2>{}, one);
   else if (units <= 64 * 4) go_row(Int<64>{}, Int<4>{}, one);
   else if (units <= 64 * 8) go_row(Int<64>{}, Int<8>{}, one);
