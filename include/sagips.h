@@ -487,9 +487,10 @@ sagips_status sagips_muon_step(sagips_ctx* ctx, const sagips_matrix_set* set, co
  * likely alternatives of a categorical distribution a row, from its logits.
  * With z = scale * logits, m = max z and s = sum exp(z - m) over a row,
  *   ln p_v = z_v - m - ln s,   H = -sum p_v ln p_v.
- * A logit of -infinity is a masked choice: p = 0, and it adds nothing.  A row of
- * nothing else has H = 0.  A NaN or +infinity in a row makes its results NaN (and
- * its alternatives -1).
+ * A logit of -infinity, and no other, is a masked choice: p = 0, and it adds
+ * nothing.  A row of nothing else has H = 0.  An ln p below fp32's lowest finite
+ * number (logits near the type's lowest) is given as that number.  A NaN or
+ * +infinity in a row makes its results NaN (and its alternatives -1).
  *   type      SAGIPS_F32 or SAGIPS_BF16: type of the logits
  *   logits    [rows][n_choices], row r at logits + r * stride; stride >=
  *             n_choices; aligned to one value, rows of any alignment

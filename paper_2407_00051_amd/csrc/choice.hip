@@ -15,6 +15,8 @@
 #include "kernels.hpp"
 #include "split_bf16.hpp"
 
+#include <float.h>
+
 #include <type_traits>
 
 namespace sagips {
@@ -28,6 +30,7 @@ struct ChoiceArgs {
   int64_t rows, stride;
   int n, top;
   float scale2;                    // scale log2 e
+  float twice;                     // 2 scale
   const int32_t* choice;
   float *logp, *entropy;
   int32_t* top_choice;
@@ -198,6 +201,13 @@ __device__ __forceinline__ void add_unit(u32x4 r, float m, float scale2, float& 
 // What values are taken relative to: their largest, or 0 where there are none.
 __device__ __forceinline__ float finite_or_0(float m) { return m == kLowest ? 0.0f : m; }
 
+// ln p of a logit x that is not masked, ls = log2 s: (x - m) scale - ln s, in natural units and from halves (exact
+// ones), since with x near the type's lowest value x - m, or its product with log2 e, may pass fp32 where ln p does
+// not.  What lies below fp32 is its lowest number: -infinity means masked, to a caller and to the gradient.  NaN stays.
+__device__ __forceinline__ float ln_p(const ChoiceArgs& p, float x, float m, float ls) {
+  return larger(fmaf(0.5f * x - 0.5f * m, p.twice, -kLn2 * ls), -FLT_MAX);
+}
+
 // What a row's sums give: log2 s, and the results that need nothing else.
 template <class T>
 __device__ __forceinline__ float write_row(const ChoiceArgs& p, int64_t row, const Sums& a) {
@@ -214,7 +224,7 @@ __device__ __forceinline__ float write_row(const ChoiceArgs& p, int64_t row, con
       const uint32_t raw = bits_of(((const T*)p.x)[row * p.stride + c]);
       const float x = __uint_as_float(sizeof(T) == 4 ? raw : raw << 16);
       // a masked choice: -infinity, unless the row is NaN
-      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : kLn2 * fmaf(x - a.m, p.scale2, -ls);
+      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : ln_p(p, x, a.m, ls);
     }
     p.logp[row] = v;
   }
@@ -224,7 +234,7 @@ __device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int 
   const int64_t at = row * p.top + k;
   const bool nan = !(a.s >= 0.0f), none = (uint32_t)(c >> 32) <= kMaskedKey;
   p.top_choice[at] = nan || none ? -1 : candidate_index(c);
-  p.top_logp[at] = nan ? a.s : none ? kLowest : kLn2 * fmaf(order_value((uint32_t)(c >> 32)) - a.m, p.scale2, -ls);
+  p.top_logp[at] = nan ? a.s : none ? kLowest : ln_p(p, order_value((uint32_t)(c >> 32)), a.m, ls);
 }
 
 // Values are taken out of a unit again where they are next needed: kept as floats from one use to the
@@ -803,7 +813,7 @@ size_t choice_workspace(const sagips_choices& C) {
 hipError_t launch_choice(const sagips_choices& C, const int32_t* choice, float* logp, float* entropy, int32_t* top_choice,
                          float* top_logp, float* stats, void* ws, uint32_t* ticket, hipStream_t st, Timer* tm) {
   const int64_t units = choice_units(C);
-  const ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)(C.scale * 1.4426950408889634),
+  const ChoiceArgs a{C.logits, C.rows, C.stride, C.n_choices, C.top, (float)(C.scale * 1.4426950408889634), (float)(2 * C.scale),
                      choice, logp, entropy, top_choice, top_logp, stats, choice_parts(C.rows, units), 0,
                      static_cast<char*>(ws), ticket};
   if (tm) tm->begin("choice_logprob");
