@@ -535,8 +535,9 @@ sagips_status sagips_choice_logprob(sagips_ctx* ctx, const sagips_choices* C, co
  *   dlogits   [rows][n_choices] of C's type, row r at dlogits + r * dstride;
  *             may be the logits themselves, with their stride, and must not
  *             overlap them otherwise; columns behind n_choices are left as they were
- * A row whose results are NaN gets NaN, but for its masked choices.  top_choice
- * values outside [0, n_choices) are taken as -1.                              */
+ * A row whose results are NaN gets NaN, and 0 for its masked choices, whether
+ * they are given or not.  top_choice values outside [0, n_choices) are taken as
+ * -1.                                                                         */
 typedef struct {
   const int32_t* choice;
   const float* logp;

@@ -571,7 +571,8 @@ __device__ __forceinline__ void grad_entry(const ChoiceGradArgs& p, int64_t row,
   c = -1;
   g = 0.0f;
   if (i == 0) {
-    if (p.d_logp && p.logp[row] != kLowest) c = p.choice[row];
+    // neither masked nor of a NaN row, which is NaN without it, but for its masked choices
+    if (p.d_logp && p.logp[row] > kLowest) c = p.choice[row];
   } else if (p.d_top && i <= p.top) {
     c = p.top_choice[row * p.top + i - 1];
   }

@@ -90,3 +90,23 @@ def test_a_lowest_choice_by_hand(gpu_ctx):
         p0 = 1 / (1 + np.exp(-1.5))
         assert f["top_choice"].tolist() == [[0, 1, 2]] and abs(f["logp"].item() - low) <= 4 * U * -low
         np.testing.assert_allclose(_np(d)[0], [-p0, p0 - 1, 1.0], rtol=torch.finfo(DT[dtype]).eps / 2 + 200 * U)
+
+
+@pytest.mark.parametrize("n,V,dtype", [(6, 9, "f32"), (6, 300, "bf16"), (6, 5000, "f32"), (6, 40001, "bf16")])
+def test_masked_choice_of_a_nan_row_has_no_gradient(gpu_ctx, n, V, dtype):
+    """A row whose results are NaN has a NaN gradient but for its masked choices, whose gradient is 0, the given
+    choice among them."""
+    print(f"case nan {n} x {V} {dtype}", flush=True)
+    x = _logits(n, V, dtype, 5)
+    x[:, V // 2] = float("-inf")
+    x[1, 0], x[3, V - 1] = float("nan"), float("inf")
+    choice = np.array([V // 2, V // 2, 1, V // 2, V - 2, V // 2])
+    c = torch.tensor(choice.astype(np.int32), device="cuda:0")
+    one = torch.ones(n, device="cuda:0")
+    f = gpu_ctx.choice_logprob(x, c, top=2)
+    d = gpu_ctx.choice_backward(x, f, c, one, one, torch.ones((n, 2), device="cuda:0"))
+    torch.cuda.synchronize()
+    nan = torch.tensor([False, True, False, True, False, False], device="cuda:0")
+    assert torch.equal(torch.isnan(f["logp"]), nan) and (d[:, V // 2] == 0).all()
+    rest = torch.arange(V, device="cuda:0") != V // 2
+    assert torch.isnan(d[nan][:, rest]).all() and torch.isfinite(d[~nan]).all()
