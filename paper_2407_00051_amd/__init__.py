@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libsagips.so")
 MAX_LAYERS = 8
 MAX_TENSORS = 16
 MAX_TOP = 32
+_INT32 = (1 << 31) - 1   # the ABI's 32-bit fields take what is beyond modulo 2^32
 _W_NAMES = [f"W[{l}]" for l in range(MAX_LAYERS)]
 _B_NAMES = [f"b[{l}]" for l in range(MAX_LAYERS)]
 
@@ -841,6 +842,8 @@ class Context:
         if len(shape) not in (1, 2):
             raise ValueError("member must be [rows][slots] or [rows]")
         rows, slots = shape[0], shape[1] if len(shape) == 2 else 1
+        if slots > _INT32 or not -_INT32 <= n_members <= _INT32:
+            raise ValueError(f"slots = {slots} or n_members = {n_members} does not fit in 32 bits")
         offsets, order, place = member.new_empty(max(0, n_members) + 1), member.new_empty(rows * slots), member.new_empty((rows, slots))
         if not self._follow:
             self._owned(offsets, order, place, member)
@@ -863,6 +866,8 @@ class Context:
         want = rows * slots if items else rows
         if len(shape) != 2 or shape[0] != want:
             raise ValueError(f"{name} must be [{want}][width]")
+        if slots > _INT32 or shape[1] > _INT32:
+            raise ValueError(f"slots = {slots} or width = {shape[1]} does not fit in 32 bits")
         return Routed(place.data_ptr(), rows, slots, shape[1], F32 if dtype is torch.float32 else BF16)
 
     def dispatch(self, x, plan: dict, out=None):

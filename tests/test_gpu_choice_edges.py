@@ -11,6 +11,7 @@ from tests.test_gpu_choice import DT, U, _chain, _check_grad, _logits, _np
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
+import paper_2407_00051_amd as sg  # noqa: E402
 
 LOWEST = float(np.finfo(np.float32).min)
 
@@ -110,3 +111,26 @@ def test_masked_choice_of_a_nan_row_has_no_gradient(gpu_ctx, n, V, dtype):
     assert torch.equal(torch.isnan(f["logp"]), nan) and (d[:, V // 2] == 0).all()
     rest = torch.arange(V, device="cuda:0") != V // 2
     assert torch.isnan(d[nan][:, rest]).all() and torch.isfinite(d[~nan]).all()
+
+
+def test_sizes_beyond_32_bits_are_refused(gpu_ctx):
+    """Sizes that the C ABI's 32-bit fields cannot hold are refused, not taken modulo 2^32."""
+    if torch.cuda.get_device_properties(0).total_memory < 96 << 30:
+        pytest.skip("needs 96 GB")
+    over = 1 << 32
+    wide = torch.empty((1, over + 8), dtype=torch.bfloat16, device="cuda:0")
+    few = torch.zeros((4, 2), dtype=torch.int32, device="cuda:0")
+    with pytest.raises(sg.SagipsError):
+        gpu_ctx.choice_logprob(wide)
+    with pytest.raises(ValueError):
+        gpu_ctx.dispatch(wide, {"place": few[:1]})
+    with pytest.raises(ValueError):
+        gpu_ctx.route(few, over + 8)
+    del wide
+    many = torch.empty((1, over + 2), dtype=torch.int32, device="cuda:0")
+    with pytest.raises(ValueError):
+        gpu_ctx.route(many, 4)
+    with pytest.raises(ValueError):
+        gpu_ctx.combine(torch.empty((over + 2, 1), dtype=torch.bfloat16, device="cuda:0"), {"place": many})
+    del many
+    torch.cuda.empty_cache()
