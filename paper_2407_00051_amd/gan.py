@@ -97,9 +97,13 @@ class GanLoop:
     def residual(self, noise, theta_star) -> dict:
         """p_hat (mean prediction over the noise batch) and r_hat = (theta* - p_hat) / theta*."""
         if self.mixture:
+            theta = self.mixture.forward(noise)
+            self.ctx._owned(theta_star)
             with self.mixture.on_stream():
-                p_hat = self.mixture.forward(noise).mean(0)
-                return {"p_hat": p_hat, "r_hat": (theta_star - p_hat) / theta_star}
+                p_hat = theta.mean(0)
+                r_hat = (theta_star - p_hat) / theta_star
+            self.mixture.hand_out(p_hat, r_hat)
+            return {"p_hat": p_hat, "r_hat": r_hat}
         return self.ctx.ensemble_response(self.G_W, self.G_b, noise, p_true=theta_star, slope=self.slope)
 
 

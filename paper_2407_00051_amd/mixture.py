@@ -51,6 +51,14 @@ class Mixture:
         import torch
         return nullcontext() if self.ctx._follow else torch.cuda.stream(self.ctx.stream)
 
+    def hand_out(self, *results):
+        """Marks what was allocated under on_stream() as used by the caller's stream: the caller may drop it at any time.
+        Called outside on_stream(), where that stream is torch's current one."""
+        import torch
+        if not self.ctx._follow:
+            for t in results:
+                t.record_stream(torch.cuda.current_stream(self.ctx.device))
+
     def forward(self, noise):
         """theta [k][out]; what backward needs is kept until the next call.  A row whose logits hold a NaN or +inf
         has no members: its theta is NaN, not the 0 of an empty sum."""
@@ -68,8 +76,7 @@ class Mixture:
             self._held = (noise, logits, chosen, own, weight, plan, x, theta)
             nan = chosen["entropy"][:, None]                           # finite otherwise
             out = c.combine(theta, plan, weight).addcmul_(nan, nan, value=0.0)
-        if not c._follow:
-            out.record_stream(torch.cuda.current_stream(c.device))     # the caller's, who may drop it at any time
+        self.hand_out(out)
         return out
 
     def backward(self, dL_dtheta) -> None:
