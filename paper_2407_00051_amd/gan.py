@@ -95,15 +95,18 @@ class GanLoop:
         c.adam_step(self._g_params, self._g_grads, self.G_m, self.G_v, self.t, self.lr_g)
 
     def residual(self, noise, theta_star) -> dict:
-        """p_hat (mean prediction over the noise batch) and r_hat = (theta* - p_hat) / theta*."""
+        """p_hat (mean prediction over the noise batch), sigma (0: the spread of an ensemble, here of one generator) and
+        r_hat = (theta* - p_hat) / theta* (None without theta*)."""
         if self.mixture:
+            import torch
             theta = self.mixture.forward(noise)
             self.ctx._owned(theta_star)
             with self.mixture.on_stream():
                 p_hat = theta.mean(0)
-                r_hat = (theta_star - p_hat) / theta_star
-            self.mixture.hand_out(p_hat, r_hat)
-            return {"p_hat": p_hat, "r_hat": r_hat}
+                r = {"p_hat": p_hat, "sigma": torch.zeros_like(p_hat),
+                     "r_hat": None if theta_star is None else (theta_star - p_hat) / theta_star}
+            self.mixture.hand_out(*r.values())
+            return r
         return self.ctx.ensemble_response(self.G_W, self.G_b, noise, p_true=theta_star, slope=self.slope)
 
 

@@ -57,7 +57,8 @@ class Mixture:
         import torch
         if not self.ctx._follow:
             for t in results:
-                t.record_stream(torch.cuda.current_stream(self.ctx.device))
+                if t is not None:
+                    t.record_stream(torch.cuda.current_stream(self.ctx.device))
 
     def forward(self, noise):
         """theta [k][out]; what backward needs is kept until the next call.  A row whose logits hold a NaN or +inf

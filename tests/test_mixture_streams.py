@@ -115,3 +115,14 @@ def test_a_pass_marks_its_inputs_and_theta(record):
     mix.backward(d)
     assert record.streams(noise) == [record.own] and record.streams(d) == [record.own]
     assert record.streams(theta) == [record.caller]
+
+
+def test_residual_has_what_a_single_generator_gives(record):
+    """p_hat, sigma and r_hat, as ensemble_response: one generator has no spread, and without theta* there is no r_hat."""
+    loop = _loop(_Context(record))
+    r = loop.residual(torch.randn(K, IN), torch.full((OUT,), 2.0))
+    assert set(r) == {"p_hat", "sigma", "r_hat"} and r["sigma"].tolist() == [0.0] * OUT
+    assert record.caller in record.streams(r["sigma"])
+    assert torch.allclose(r["r_hat"], (2.0 - r["p_hat"]) / 2.0)
+    none = loop.residual(torch.randn(K, IN), None)
+    assert none["r_hat"] is None and none["p_hat"].shape == (OUT,)
