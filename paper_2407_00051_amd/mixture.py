@@ -38,7 +38,7 @@ class Mixture:
         self.top, self.slope, self.entropy_coef = int(top), slope, entropy_coef
         self.dW, self.db = [torch.empty_like(w) for w in self.W], [torch.empty_like(v) for v in self.b]
         self.dWr, self.dbr = torch.empty_like(Wr), torch.empty_like(br)
-        self._held = None
+        self._held, self._marked = None, None
 
     def parameters(self):
         return [t for pair in zip(self.W, self.b) for t in pair] + [self.Wr, self.br]
@@ -50,6 +50,18 @@ class Mixture:
         """The context's stream as torch's current one: what torch computes here stands between the library's calls."""
         import torch
         return nullcontext() if self.ctx._follow else torch.cuda.stream(self.ctx.stream)
+
+    def _take(self, *inputs):
+        """Marks what the context's stream uses and torch's current one may own: inputs, and once a stream the parameters
+        and gradients (a mark lasts as long as the memory)."""
+        import torch
+        c = self.ctx
+        if c._follow or torch.cuda.current_stream(c.device).cuda_stream == c.stream.cuda_stream:
+            return
+        c._owned(*inputs)
+        if self._marked is not c.stream:
+            c._owned(self.parameters(), self.gradients())
+            self._marked = c.stream
 
     def hand_out(self, *results):
         """Marks what was allocated under on_stream() as used by the caller's stream: the caller may drop it at any time.
@@ -65,7 +77,7 @@ class Mixture:
         has no members: its theta is NaN, not the 0 of an empty sum."""
         import torch
         c = self.ctx
-        c._owned(noise)
+        self._take(noise)
         with self.on_stream():
             logits = torch.addmm(self.br, noise, self.Wr.t())
             chosen = c.choice_logprob(logits, top=self.top)
@@ -85,7 +97,7 @@ class Mixture:
         import torch
         c = self.ctx
         noise, logits, chosen, own, weight, plan, x, theta = self._held
-        c._owned(dL_dtheta)
+        self._take(dL_dtheta)
         with self.on_stream():
             d_member, d_weight = c.combine_backward(dL_dtheta, theta, plan, weight)
             c.gen_backward_routed(self.W, self.b, x, plan["offsets"], d_member, slope=self.slope, dW=self.dW, db=self.db)

@@ -126,3 +126,22 @@ def test_residual_has_what_a_single_generator_gives(record):
     assert torch.allclose(r["r_hat"], (2.0 - r["p_hat"]) / 2.0)
     none = loop.residual(torch.randn(K, IN), None)
     assert none["r_hat"] is None and none["p_hat"].shape == (OUT,)
+
+
+def test_parameters_and_gradients_are_marked(record):
+    """A mixture may be dropped, parameters and gradients with it, while the context's stream works on them; a
+    stream set later is marked too."""
+    W, b, Wr, br = _stack()
+    ctx = _Context(record)
+    mix = Mixture(ctx, W, b, Wr, br, top=TOP)
+    with mix.on_stream():                                  # a caller who is on that stream already
+        mix.forward(torch.randn(K, IN))
+    mix.forward(torch.randn(K, IN))
+    mix.backward(torch.zeros(K, OUT))
+    for t in mix.parameters() + mix.gradients():
+        assert record.streams(t) == [record.own]
+    mix.forward(torch.randn(K, IN))
+    other = ctx._stream = _Stream(3)
+    mix.forward(torch.randn(K, IN))
+    for t in mix.parameters() + mix.gradients():
+        assert record.streams(t) == [record.own, other]
