@@ -134,3 +134,21 @@ def test_sizes_beyond_32_bits_are_refused(gpu_ctx):
         gpu_ctx.combine(torch.empty((over + 2, 1), dtype=torch.bfloat16, device="cuda:0"), {"place": many})
     del many
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,pad", [(37, 3), (37, 8), (1500, 1), (1500, 4), (5000, 5), (40, 24), (20001, 7)])
+def test_in_place_gradient_leaves_what_is_between_the_rows(gpu_ctx, V, pad, dtype):
+    """Columns behind the choices of a strided buffer keep their bits, also where the gradient is written over the logits."""
+    print(f"case in place {V} {dtype} pad {pad}", flush=True)
+    x = _logits(6, V, dtype, V, 0.1, pad)
+    held = x._base                                         # [6][V + pad]
+    assert held.shape == (6, V + pad) and held.data_ptr() == x.data_ptr()
+    held[:, V:] = torch.randn((6, pad), device="cuda:0").to(DT[dtype])
+    before = held.clone()
+    c = torch.arange(6, device="cuda:0", dtype=torch.int32)
+    f = gpu_ctx.choice_logprob(x, c, top=2)
+    d = gpu_ctx.choice_backward(x, f, c, torch.ones(6, device="cuda:0"), d_top=torch.ones((6, 2), device="cuda:0"))
+    gpu_ctx.choice_backward(x, f, c, torch.ones(6, device="cuda:0"), d_top=torch.ones((6, 2), device="cuda:0"), out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(x, d) and torch.equal(held[:, V:], before[:, V:])
