@@ -201,12 +201,16 @@ __device__ __forceinline__ void add_unit(u32x4 r, float m, float scale2, float& 
 // What values are taken relative to: their largest, or 0 where there are none.
 __device__ __forceinline__ float finite_or_0(float m) { return m == kLowest ? 0.0f : m; }
 
-// ln p of a logit x that is not masked, ls = log2 s: (x - m) scale - ln s, in natural units and from halves (exact
-// ones), since with x near the type's lowest value x - m, or its product with log2 e, may pass fp32 where ln p does
-// not.  What lies below fp32 is its lowest number: -infinity means masked, to a caller and to the gradient.  NaN stays.
-__device__ __forceinline__ float ln_p(const ChoiceArgs& p, float x, float m, float ls) {
-  return larger(fmaf(0.5f * x - 0.5f * m, p.twice, -kLn2 * ls), -FLT_MAX);
-}
+// ln p of a row's logits that are not masked: (x - m) scale - ln s, in natural units and from halves (exact ones),
+// since with x near the type's lowest value x - m, or its product with log2 e, may pass fp32 where ln p does not.
+// What lies below fp32 is its lowest number: -infinity means masked, to a caller and to the gradient.  NaN stays.
+struct RowLn {
+  float half_m, minus_ln_s, s;
+  __device__ __forceinline__ RowLn(const Sums& a, float ls) : half_m(0.5f * a.m), minus_ln_s(-kLn2 * ls), s(a.s) {}
+  __device__ __forceinline__ float at(const ChoiceArgs& p, float x) const {
+    return larger(fmaf(fmaf(0.5f, x, -half_m), p.twice, minus_ln_s), -FLT_MAX);
+  }
+};
 
 // What a row's sums give: log2 s, and the results that need nothing else.
 template <class T>
@@ -224,17 +228,17 @@ __device__ __forceinline__ float write_row(const ChoiceArgs& p, int64_t row, con
       const uint32_t raw = bits_of(((const T*)p.x)[row * p.stride + c]);
       const float x = __uint_as_float(sizeof(T) == 4 ? raw : raw << 16);
       // a masked choice: -infinity, unless the row is NaN
-      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : ln_p(p, x, a.m, ls);
+      v = x == kLowest ? (a.s >= 0.0f ? kLowest : a.s) : RowLn(a, ls).at(p, x);
     }
     p.logp[row] = v;
   }
   return ls;
 }
-__device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int k, uint64_t c, const Sums& a, float ls) {
+__device__ __forceinline__ void write_top(const ChoiceArgs& p, int64_t row, int k, uint64_t c, const RowLn& r) {
   const int64_t at = row * p.top + k;
-  const bool nan = !(a.s >= 0.0f), none = (uint32_t)(c >> 32) <= kMaskedKey;
+  const bool nan = !(r.s >= 0.0f), none = (uint32_t)(c >> 32) <= kMaskedKey;
   p.top_choice[at] = nan || none ? -1 : candidate_index(c);
-  p.top_logp[at] = nan ? a.s : none ? kLowest : ln_p(p, order_value((uint32_t)(c >> 32)), a.m, ls);
+  p.top_logp[at] = nan ? r.s : none ? kLowest : r.at(p, order_value((uint32_t)(c >> 32)));
 }
 
 // Values are taken out of a unit again where they are next needed: kept as floats from one use to the
@@ -265,7 +269,7 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
     a.t = group_sum<L>(a.t);
     if (l == 0) write_row<T>(p, row, a);
     if (p.top == 0) continue;
-    const float ls = log2f(a.s);
+    const RowLn ln(a, log2f(a.s));
     // One alternative a round, which lane k % L keeps; L of them are written together.  A bf16 value's key and its
     // index go in one word (an index is below 64 units' 512), fp32 values take a second exchange.
     constexpr bool kWord = sizeof(T) == 2;
@@ -298,7 +302,7 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
             kept_lo = 0xffff0000u | kept;
             kept = kept & 0x80000000u ? kept & 0xffff0000u : kept ? kept | 0xffffu : 0u;
           }
-          write_top(p, row, k - at + l, (uint64_t)kept << 32 | kept_lo, a, ls);
+          write_top(p, row, k - at + l, (uint64_t)kept << 32 | kept_lo, ln);
         }
       }
     }
@@ -356,7 +360,7 @@ __device__ __forceinline__ void join_parts(const ChoiceArgs& p, int64_t row, uin
   a.t = group_sum<64>(a.t);
   if (lane == 0) write_row<T>(p, row, a);
   if (p.top == 0) return;
-  const float ls = log2f(a.s);
+  const RowLn ln(a, log2f(a.s));
   const uint32_t bound = max(wave_kth((uint32_t)(entry >> 32), (p.top + j) / (j + 1)), kMaskedKey + 1);
   if (lane == 0) *count = 0;
   __builtin_amdgcn_wave_barrier();
@@ -380,9 +384,9 @@ __device__ __forceinline__ void join_parts(const ChoiceArgs& p, int64_t row, uin
       const uint64_t c = held[i];
       int rank = 0;
       for (int k = 0; k < n; ++k) rank += held[k] > c;
-      if (rank < p.top) write_top(p, row, rank, c, a, ls);
+      if (rank < p.top) write_top(p, row, rank, c, ln);
     }
-    for (int k = n + lane; k < p.top; k += 64) write_top(p, row, k, 0, a, ls);
+    for (int k = n + lane; k < p.top; k += 64) write_top(p, row, k, 0, ln);
     return;
   }
   // many equal ones: the next of all, one after the other
@@ -390,7 +394,7 @@ __device__ __forceinline__ void join_parts(const ChoiceArgs& p, int64_t row, uin
   uint64_t c = on ? r.tops()[0] : 0;
   for (int k = 0; k < p.top; ++k) {
     const uint64_t first = group_first<64>(c);
-    if (lane == k) write_top(p, row, k, first, a, ls);
+    if (lane == k) write_top(p, row, k, first, ln);
     if (on && c == first) c = ++at < p.top ? r.tops()[at] : 0;
   }
 }
@@ -469,10 +473,10 @@ __global__ __launch_bounds__(TH, R <= 8 && !(kParts && TH == 256) ? 8 : 4) void 
       else write_row<T>(p, row, a);
     }
     if (p.top) {
-      const float ls = log2f(a.s);
+      const RowLn ln(a, log2f(a.s));
       const auto put = [&](int k, uint64_t c) __attribute__((always_inline)) {
         if constexpr (kParts) Record(p, row, part_of).put_top(k, c);
-        else write_top(p, row, k, c, a, ls);
+        else write_top(p, row, k, c, ln);
       };
       // at least top values are no less than the top-th of the 64 groups' largest
       const uint32_t key = max(wave_kth(order_key(group[lane]), p.top), kMaskedKey + 1);
