@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256) void k_choice_short(ChoiceArgs p) {
     if (p.top == 0) continue;
     const RowLn ln(a, log2f(a.s));
     // One alternative a round, which lane k % L keeps; L of them are written together.  A bf16 value's key and its
-    // index go in one word (an index is below 64 units' 512), fp32 values take a second exchange.
+    // index go in one word (an index is below 128 units' 1,024), fp32 values take a second exchange.
     constexpr bool kWord = sizeof(T) == 2;
     uint32_t key[R * N], kept = 0, kept_lo = 0;        // key 0: masked, outside the row, or taken
     const auto index = [&](int e) __attribute__((always_inline)) { return i0 + e / N * (L * N) + e % N; };
@@ -747,10 +747,11 @@ hipError_t choice_forward(ChoiceArgs a, int64_t units, hipStream_t st) {
   };
   const std::true_type one{};
   // Alternatives up to which rounds cost less than the bound (65,536 rows; us in rounds and by the bound): of 256 fp32
-  // logits 8 alternatives 35 and 33, 16 58 and 39; of 500 bf16 ones 12 47 and 47, 16 56 and 50; of 350 fp32 ones 2
-  // 33 and 37, 4 44 and 39; of 1,000 bf16 ones 2 40 and 44, 4 49 and 46.  Rows of up to 32 units have too few
-  // groups for a bound of many alternatives (128 fp32 logits: 8 of them 19 and 34, 32 80 and 115).
-  const int rounds = units <= 32 ? SAGIPS_MAX_TOP : units <= 64 ? (sizeof(T) == 2 ? 12 : 8) : units <= 128 ? 2 : -1;
+  // logits 6 alternatives 29 and 30, 7 32 and 30, 8 34 and 31; of 500 bf16 ones 10 41 and 43, 11 44 and 44, 12 46 and
+  // 44 (of 400 10 39 and 38, 12 43 and 40); of 350 fp32 ones 2 31 and 34, 3 35 and 35; of 1,000 bf16 ones 2 39 and 42,
+  // 3 44 and 44, 4 49 and 45.  Rows of up to 32 units have too few groups for a bound of many alternatives (128 fp32 logits:
+  // 8 of them 19 and 34, 32 80 and 115).
+  const int rounds = units <= 32 ? SAGIPS_MAX_TOP : units <= 64 ? (sizeof(T) == 2 ? 10 : 6) : units <= 128 ? 2 : -1;
   if (a.parts > 1) {
     a.per = (int)((units + a.parts - 1) / a.parts);
     const dim3 grid((unsigned)(a.rows * a.parts));
