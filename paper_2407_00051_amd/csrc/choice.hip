@@ -515,7 +515,8 @@ __global__ __launch_bounds__(TH, R <= 8 && !(kParts && TH == 256) ? 8 : 4) void 
         }
         for (int k = n + tid; k < p.top; k += TH) put(k, 0);
       } else {
-        // more equal values than are held: one alternative a pass over the row
+        // more values at the bound than are held (equal ones, fp32 ones equal in their upper 16 bits): one
+        // alternative a pass over the row (4,096 equal rows of 65,536 bf16 logits with 8 of them 735 us, normal ones 108)
         uint64_t last = ~0ull;
         for (int k = 0; k < p.top; ++k) {
           uint64_t c = 0;
@@ -621,7 +622,8 @@ __device__ __forceinline__ T rounded(float v) {
 // looking through all of them: 65,536 rows of 256 bf16 logits with 8 alternatives 46 us, 35 so, and 22 by as many
 // lanes as they need).  Two units a lane from 8 on, since what is done once a row weighs (500 bf16 logits 44 us
 // with one, 39 with two).
-// kUnits: 16-byte units, the rows of both arrays being aligned alike; otherwise single values.
+// kUnits: 16-byte units, the rows of both arrays being aligned alike; otherwise single values (4,096 rows of 50,257 of
+// 50,304 bf16 logits to dense rows 469 us, between dense rows 163; 32,001 of 32,007 fp32 ones 239 and 214).
 template <class T, int L, int R, bool kUnits>
 __global__ __launch_bounds__(256) void k_choice_grad(ChoiceGradArgs p) {
   constexpr int N = kUnits ? Unit<T>::N : 1, P = 256 / L;
