@@ -69,6 +69,23 @@ def test_every_product_to_fp32(gpu_ctx, widths, M, n):
             _near(to_np(db[l]).astype(np.float64), rb[l], 22.88 * h + 20, f"db[{l}]")
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,at", [(50, 0), (50, 50), (300, 7), (20000, 0), (20000, 20000)])
+def test_no_member_has_rows(gpu_ctx, n, at):
+    """Offsets that are all the same: no row is looked at or written, and every gradient of a parameter is 0."""
+    print(f"case empty n={n} at={at}", flush=True)
+    W, b, x, g = _chains((6, H, H, H, H, 6), 70, n, 1)
+    dev = lambda a: torch.tensor(a, device="cuda:0")                        # noqa: E731
+    Wd, bd = [dev(w) for w in W], [dev(v) for v in b]
+    off = torch.full((71,), at, dtype=torch.int32, device="cuda:0")
+    held = torch.full((n, 6), 7.0, device="cuda:0")
+    x, g = torch.full_like(held, float("nan")), torch.full_like(held, float("nan"))
+    theta = gpu_ctx.gen_forward_routed(Wd, bd, x, off, out=held.clone())
+    dW, db, dx = gpu_ctx.gen_backward_routed(Wd, bd, x, off, g, dx=held.clone())
+    torch.cuda.synchronize()
+    assert torch.equal(theta, held) and torch.equal(dx, held) and all((t == 0).all() for t in dW + db)
+
+
 def _bf16(x):
     return torch.tensor(np.asarray(x, dtype=np.float64)).float().bfloat16().double().numpy()
 
